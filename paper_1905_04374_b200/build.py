@@ -33,14 +33,20 @@ def _units():
              ("k2_select.cu", "k2_select.o", []),
              ("k3_dispatch.cu", "k3_dispatch.o", []),
              ("gar_api.cu", "gar_api.o", [])]
+    for name in ("logprobs", "checkpoint", "wgrad", "api"):
+        units.append((f"worker_{name}.cu", f"worker_{name}.o", []))
     for p in K3_P:
         units.append(("k3_inst.cu", f"k3_inst_{p}.o", [f"-DK3_P={p}", f"-DK3_EXACT={1 if p <= 32 else 0}"]))
     return units
 
 
-def _newest_header() -> float:
-    hdrs = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
+def _newest_header(worker: bool) -> float:
+    """The newest header a unit depends on: the worker-side operators' own headers concern their units only."""
+    hdrs = [os.path.join(CSRC, f) for f in os.listdir(CSRC)
+            if f.endswith((".cuh", ".h")) and (worker or not f.startswith("worker_"))]
     hdrs.append(os.path.join(ROOT, "include", "gar.h"))
+    if worker:
+        hdrs.append(os.path.join(ROOT, "include", "gar_worker.h"))
     hdrs.append(os.path.abspath(__file__))
     return max(os.path.getmtime(h) for h in hdrs)
 
@@ -49,11 +55,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every translation unit that is out of date and link libgar.so."""
     os.makedirs(OBJ, exist_ok=True)
     nvcc = _nvcc()
-    hdr_time = _newest_header()
+    hdr_time = {w: _newest_header(w) for w in (False, True)}
     jobs = []
     for src, obj, extra in _units():
         s, o = os.path.join(CSRC, src), os.path.join(OBJ, obj)
-        if force or not os.path.exists(o) or os.path.getmtime(o) < max(os.path.getmtime(s), hdr_time):
+        if force or not os.path.exists(o) or os.path.getmtime(o) < max(os.path.getmtime(s), hdr_time[src.startswith("worker_")]):
             jobs.append([nvcc, *NVCC_FLAGS, *extra, "-c", s, "-o", o])
 
     def run(cmd):

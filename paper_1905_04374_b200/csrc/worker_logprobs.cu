@@ -1,0 +1,684 @@
+// Token log probabilities with entropy and top alternatives, and their gradient (gar_worker.h).
+//
+// Forward.  Every thread runs the softmax recurrence over its share of a row: with m the largest
+// value so far, s = sum e^(x-m) and u = sum e^(x-m) (x-m) log2(e); a larger m' rescales
+//     f = e^(m-m'),  u <- f (u + s (m-m') log2(e)),  s <- f s.
+// x - m is formed before the product with log2(e), so large logits lose nothing to cancellation,
+// and it is held above -1e4 so that a masked entry (-inf) contributes e = 0 and 0 to u.  Shares are
+// joined by the same rescaling: lanes, warps, then (rows split over a cluster) CTAs through
+// distributed shared memory.
+//
+// The k best entries need nothing in that loop: m IS the largest value of the thread's share.  An
+// entry of the top k lies in the share of a thread whose m is among the k largest of the CTA (ties
+// included), so only those shares are read again (they are in L2), by whole warps; entries not
+// below the k-th largest m are collected, ranked by counting and stored.  A 64-bit key (value in
+// an order-preserving code, complement of the index) makes the order total: equal values go to the
+// lowest index.  If more entries qualify than the list holds (rows with many equal values, such as
+// fully masked ones) the k best are extracted one by one instead.
+#include <cooperative_groups.h>
+
+#include "worker_common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace gar {
+namespace worker {
+namespace {
+
+constexpr int LP_THREADS = 256;
+constexpr int LP_WARPS = LP_THREADS / 32;
+constexpr int LP_UNROLL = 4;            // 16-byte loads in flight per thread
+constexpr int LP_LIST = 512;            // candidate entries of a CTA
+constexpr int LP_MAX_CLUSTER = 8;
+constexpr float LP_FLOOR = -1e4f;       // exponents below this are 0 in fp32
+
+struct Softmax {
+    float m, s, u;
+};
+__device__ __forceinline__ float centre(float m) { return m == -CUDART_INF_F ? 0.f : m; }
+
+__device__ __forceinline__ void raise(Softmax& a, float m) {
+    if (a.m == -CUDART_INF_F) {          // nothing but masked (or NaN) entries so far: they have added 0 (or NaN)
+        a.m = m;
+        return;
+    }
+    const float d = (a.m - m) * kLog2e, f = ex2(d);
+    // f == 0 drops the old sums; d may be -inf then
+    a.u = f > 0.f ? f * (a.u + a.s * d) : (a.u + a.s) * 0.f;
+    a.s = a.s * f;
+    a.m = m;
+}
+__device__ __forceinline__ void join(Softmax& a, Softmax b) {
+    if (b.m > a.m) raise(a, b.m);
+    else if (a.m > b.m) raise(b, a.m);
+    a.s += b.s;
+    a.u += b.u;
+}
+__device__ __forceinline__ void add_one(Softmax& a, float x) {
+    if (x > a.m) raise(a, x);
+    const float t = max_nan((x - centre(a.m)) * kLog2e, LP_FLOOR), e = ex2(t);
+    a.s += e;
+    a.u += e * t;
+}
+
+// Order-preserving code of a value: larger value, larger code; -0 = +0; NaN lowest.
+__device__ __forceinline__ unsigned code_of(float x) {
+    if (x != x) return 0u;
+    const unsigned b = __float_as_uint(x + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(unsigned c) {
+    if (c == 0u) return CUDART_NAN_F;
+    return __uint_as_float(c & 0x80000000u ? c & 0x7fffffffu : ~c);
+}
+__device__ __forceinline__ unsigned long long key_of(float x, unsigned idx) {
+    return (static_cast<unsigned long long>(code_of(x)) << 32) | (0xffffffffu - idx);
+}
+
+__device__ __forceinline__ unsigned long long shfl_xor64(unsigned long long v, int o) {
+    return __shfl_xor_sync(0xffffffffu, v, o);
+}
+
+// What a row comes to, from its joined sums.
+struct RowResult {
+    float lse, lse_lo, entropy, log_s, m;
+    bool  empty, bad;
+};
+__device__ __forceinline__ RowResult finish(const Softmax& a) {
+    RowResult r;
+    r.m = a.m;
+    r.bad = a.s != a.s;                          // a NaN or +inf in the row
+    r.empty = !r.bad && a.m == -CUDART_INF_F;
+    r.log_s = logf(a.s);
+    r.lse = r.bad ? CUDART_NAN_F : r.empty ? -CUDART_INF_F : a.m + r.log_s;
+    // the rounding error of m + log s, exactly (two-sum)
+    const float part = __fsub_rn(r.lse, a.m);
+    r.lse_lo = r.bad || r.empty ? 0.f : __fadd_rn(__fsub_rn(a.m, __fsub_rn(r.lse, part)), __fsub_rn(r.log_s, part));
+    r.entropy = r.bad ? CUDART_NAN_F : r.empty ? 0.f : r.log_s - (a.u / a.s) * 0.69314718055994531f;
+    return r;
+}
+__device__ __forceinline__ float logprob_of(const RowResult& r, float x) {
+    if (r.bad) return CUDART_NAN_F;
+    if (r.empty) return -CUDART_INF_F;
+    return (x - r.m) - r.log_s;
+}
+
+template <typename T>
+__device__ __forceinline__ float load_one(const T* row, int64_t j) { return Elem<T>::widen(row[j]); }
+
+struct ForwardArgs {
+    const void*    logits;
+    int64_t        rows, vocab, ld;
+    const int64_t* targets;
+    float *        logprobs, *entropy, *lse, *lse_lo, *top_logprobs;
+    int64_t*       top_index;
+    int            top;
+};
+
+template <typename T>
+__device__ void store_row(const ForwardArgs& a, int64_t row, const RowResult& r) {
+    if (a.lse) a.lse[row] = r.lse;
+    if (a.lse_lo) a.lse_lo[row] = r.lse_lo;
+    if (a.entropy) a.entropy[row] = r.entropy;
+    if (a.logprobs) {
+        const int64_t t = a.targets[row];
+        float lp = 0.f;
+        if (t >= a.vocab) lp = CUDART_NAN_F;
+        else if (t >= 0) lp = logprob_of(r, load_one(static_cast<const T*>(a.logits) + row * a.ld, t));
+        a.logprobs[row] = lp;
+    }
+}
+__device__ __forceinline__ void store_top(const ForwardArgs& a, int64_t row, int rank, unsigned long long key, const RowResult& r) {
+    a.top_logprobs[row * a.top + rank] = logprob_of(r, value_of(unsigned(key >> 32)));
+    a.top_index[row * a.top + rank] = int64_t(0xffffffffu - unsigned(key));
+}
+
+// ---- rows of up to 1024 entries: L lanes hold a row in registers, EPL entries each -------------
+template <typename T, int L, int EPL>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_small_kernel(const ForwardArgs a) {
+    const int lane = threadIdx.x % L;
+    const int64_t row = (int64_t(blockIdx.x) * LP_THREADS + threadIdx.x) / L;
+    const bool live = row < a.rows;
+    const T* x = static_cast<const T*>(a.logits) + (live ? row : 0) * a.ld;
+    const int vocab = int(a.vocab);
+    float v[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        const int j = lane + i * L;
+        v[i] = j < vocab ? load_one(x, j) : -CUDART_INF_F;
+    }
+    Softmax st{-CUDART_INF_F, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) st.m = fmaxf(st.m, v[i]);
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) st.m = fmaxf(st.m, __shfl_xor_sync(0xffffffffu, st.m, o));
+    const float c = centre(st.m);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        const float t = max_nan((v[i] - c) * kLog2e, LP_FLOOR), e = ex2(t);
+        st.s += e;
+        st.u += e * t;
+    }
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) {
+        st.s += __shfl_xor_sync(0xffffffffu, st.s, o);
+        st.u += __shfl_xor_sync(0xffffffffu, st.u, o);
+    }
+    const RowResult r = finish(st);
+    if (live && lane == 0) store_row<T>(a, row, r);
+    // k rounds: the best key below the previous one
+    unsigned long long last = ~0ull;
+    for (int k = 0; k < a.top; ++k) {
+        unsigned long long best = 0;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            const int j = lane + i * L;
+            const unsigned long long key = j < vocab ? key_of(v[i], unsigned(j)) : 0ull;
+            if (key < last && key > best) best = key;
+        }
+#pragma unroll
+        for (int o = L / 2; o; o >>= 1) {
+            const unsigned long long other = shfl_xor64(best, o);
+            if (other > best) best = other;
+        }
+        if (live && lane == 0) store_top(a, row, k, best, r);
+        last = best;
+    }
+}
+
+// ---- longer rows: a CTA, or a cluster of up to eight, per row ------------------------------------
+struct ForwardShared {
+    Softmax            part[LP_WARPS];
+    Softmax            total;                      // of this CTA: read by the cluster's first
+    alignas(16) float  best[LP_THREADS];           // the threads' largest values, read four at a time
+    int                shares[LP_THREADS];         // threads whose share is read again
+    int                nshares, nlist, overflow;
+    float              threshold;
+    unsigned long long list[LP_LIST];
+    unsigned long long top[GAR_MAX_TOP];           // this CTA's best, in order (0: none): read by the cluster's first
+    unsigned long long warp_key[LP_WARPS];
+};
+
+// A row as 16-byte slots: slot i holds elements [i E - head, (i + 1) E - head); the row's first and
+// last slot may be incomplete and are then read by element ("edge" entries).
+template <typename T> struct RowView {
+    const T* x;              // the row
+    const T* base;           // x - head: 16-byte aligned
+    int      head;           // elements of slot 0 before the row
+    int64_t  vocab;
+    int64_t  first, last;    // this CTA's complete slots [first, last)
+    int64_t  lead, tail;     // edge entries of this CTA: [0, lead) and [vocab - tail, vocab)
+};
+template <typename T>
+__device__ __forceinline__ RowView<T> view_row(const T* x, int64_t vocab, unsigned rank, unsigned parts) {
+    constexpr int E = Elem<T>::PER16;
+    RowView<T> v;
+    v.x = x;
+    v.vocab = vocab;
+    v.head = int((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
+    v.base = x - v.head;
+    const int64_t whole_first = v.head ? 1 : 0, whole_last = (vocab + v.head) / E;       // complete slots
+    const int64_t n = whole_last > whole_first ? whole_last - whole_first : 0;
+    v.first = whole_first + n * rank / parts;
+    v.last = whole_first + n * (rank + 1) / parts;
+    v.lead = v.tail = 0;
+    if (rank == 0 && v.head) v.lead = E - v.head;
+    if (rank == parts - 1) v.tail = (vocab + v.head) - whole_last * E;
+    return v;
+}
+// the edge entry of a thread (at most 14 of them), or -1
+template <typename T>
+__device__ __forceinline__ int64_t edge_entry(const RowView<T>& v, int tid) {
+    if (tid < v.lead) return tid;
+    if (tid >= 32 && tid - 32 < v.tail) return v.vocab - v.tail + (tid - 32);
+    return -1;
+}
+
+__device__ __forceinline__ void offer(ForwardShared& sh, float x, int64_t idx) {
+    const int at = atomicAdd(&sh.nlist, 1);
+    if (at < LP_LIST) sh.list[at] = key_of(x, unsigned(idx));
+}
+
+// best key below `bound` in a thread's share
+template <typename T>
+__device__ unsigned long long best_below(const RowView<T>& v, int tid, unsigned long long bound) {
+    constexpr int E = Elem<T>::PER16;
+    unsigned long long best = 0;
+    for (int64_t slot = v.first + tid; slot < v.last; slot += LP_THREADS) {
+        float f[E];
+        widen16B(*reinterpret_cast<const uint4*>(v.base + slot * E), f, static_cast<const T*>(nullptr));
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const unsigned long long key = key_of(f[e], unsigned(slot * E + e - v.head));
+            if (key < bound && key > best) best = key;
+        }
+    }
+    const int64_t j = edge_entry(v, tid);
+    if (j >= 0) {
+        const unsigned long long key = key_of(load_one(v.x, j), unsigned(j));
+        if (key < bound && key > best) best = key;
+    }
+    return best;
+}
+
+// The CTA's `top` best entries of its part of the row into sh.top, in order (zeros beyond what there is).
+template <typename T>
+__device__ void find_top(ForwardShared& sh, const RowView<T>& v, float mine, int top) {
+    constexpr int E = Elem<T>::PER16;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    sh.best[tid] = mine;
+    if (tid == 0) {
+        sh.nshares = sh.nlist = sh.overflow = 0;
+        sh.threshold = CUDART_INF_F;
+    }
+    if (tid < GAR_MAX_TOP) sh.top[tid] = 0;
+    __syncthreads();
+    int above = 0;
+    for (int j = 0; j < LP_THREADS; j += 4) {
+        const float4 b = *reinterpret_cast<const float4*>(&sh.best[j]);
+        above += (b.x > mine) + (b.y > mine) + (b.z > mine) + (b.w > mine);
+    }
+    // the threads with fewer than `top` larger maxima; the smallest of those maxima bounds the answer from below
+    if (above < top) {
+        sh.shares[atomicAdd(&sh.nshares, 1)] = tid;
+    }
+    float low = above < top ? mine : CUDART_INF_F;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
+    if (lane == 0) sh.part[warp].m = low;
+    __syncthreads();
+    low = sh.part[0].m;
+#pragma unroll
+    for (int w = 1; w < LP_WARPS; ++w) low = fminf(low, sh.part[w].m);
+    const int nshares = sh.nshares;
+    if (nshares <= 4 * GAR_MAX_TOP) {
+        for (int c = warp; c < nshares; c += LP_WARPS) {
+            const int owner = sh.shares[c];
+            for (int64_t slot = v.first + owner + int64_t(lane) * LP_THREADS; slot < v.last; slot += 32 * LP_THREADS) {
+                float f[E];
+                widen16B(*reinterpret_cast<const uint4*>(v.base + slot * E), f, static_cast<const T*>(nullptr));
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (!(f[e] < low)) offer(sh, f[e], slot * E + e - v.head);
+            }
+            const int64_t j = edge_entry(v, owner);
+            if (lane == 0 && j >= 0) {
+                const float f = load_one(v.x, j);
+                if (!(f < low)) offer(sh, f, j);
+            }
+        }
+    }
+    __syncthreads();
+    const int nlist = sh.nlist;
+    if (nshares <= 4 * GAR_MAX_TOP && nlist <= LP_LIST) {
+        for (int i = tid; i < nlist; i += LP_THREADS) {
+            const unsigned long long key = sh.list[i];
+            int rank = 0;
+            for (int j = 0; j < nlist; ++j) rank += sh.list[j] > key;
+            if (rank < top) sh.top[rank] = key;
+        }
+        __syncthreads();
+        return;
+    }
+    // too many equal values for the list: one by one
+    unsigned long long cur = best_below(v, tid, ~0ull);
+    for (int k = 0; k < top; ++k) {
+        unsigned long long best = cur;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            const unsigned long long other = shfl_xor64(best, o);
+            if (other > best) best = other;
+        }
+        if (lane == 0) sh.warp_key[warp] = best;
+        __syncthreads();
+        best = sh.warp_key[0];
+#pragma unroll
+        for (int w = 1; w < LP_WARPS; ++w) best = sh.warp_key[w] > best ? sh.warp_key[w] : best;
+        if (tid == 0) sh.top[k] = best;
+        if (best != 0 && cur == best) cur = best_below(v, tid, best);
+        __syncthreads();
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(const ForwardArgs a, int parts) {
+    constexpr int E = Elem<T>::PER16;
+    __shared__ __align__(16) ForwardShared sh;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const unsigned rank = blockIdx.x % unsigned(parts);
+    const int64_t row = blockIdx.x / unsigned(parts);
+    const RowView<T> v = view_row(static_cast<const T*>(a.logits) + row * a.ld, a.vocab, rank, unsigned(parts));
+
+    Softmax st{-CUDART_INF_F, 0.f, 0.f};
+    f32x2 s2 = pack2(0.f, 0.f), u2 = pack2(0.f, 0.f);
+    const f32x2 scale = pack2(kLog2e, kLog2e);
+    auto tile = [&](const uint4 (&raw)[LP_UNROLL], int count) {
+        float f[LP_UNROLL][E];
+        float m = st.m;
+#pragma unroll
+        for (int i = 0; i < LP_UNROLL; ++i) {
+            if (i < count) {
+                widen16B(raw[i], f[i], static_cast<const T*>(nullptr));
+#pragma unroll
+                for (int e = 0; e < E; ++e) m = fmaxf(m, f[i][e]);
+            }
+        }
+        if (m > st.m) {
+            float s0, s1, u0, u1;
+            unpack2(s2, s0, s1);
+            unpack2(u2, u0, u1);
+            st.s = s0 + s1;
+            st.u = u0 + u1;
+            raise(st, m);
+            s2 = pack2(st.s, 0.f);
+            u2 = pack2(st.u, 0.f);
+        }
+        const float c = centre(st.m);
+        const f32x2 nc = pack2(-c, -c);
+#pragma unroll
+        for (int i = 0; i < LP_UNROLL; ++i) {
+            if (i < count) {
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    float t0, t1;
+                    unpack2(mul2(add2(pack2(f[i][e], f[i][e + 1]), nc), scale), t0, t1);
+                    t0 = max_nan(t0, LP_FLOOR);
+                    t1 = max_nan(t1, LP_FLOOR);
+                    const f32x2 ex = pack2(ex2(t0), ex2(t1));
+                    s2 = add2(s2, ex);
+                    u2 = fma2(ex, pack2(t0, t1), u2);
+                }
+            }
+        }
+    };
+    int64_t slot = v.first + tid;
+    for (; slot + (LP_UNROLL - 1) * LP_THREADS < v.last; slot += LP_UNROLL * LP_THREADS) {
+        uint4 raw[LP_UNROLL];
+#pragma unroll
+        for (int i = 0; i < LP_UNROLL; ++i) raw[i] = *reinterpret_cast<const uint4*>(v.base + (slot + i * LP_THREADS) * E);
+        tile(raw, LP_UNROLL);
+    }
+    for (; slot < v.last; slot += LP_THREADS) {
+        uint4 raw[LP_UNROLL];
+        raw[0] = *reinterpret_cast<const uint4*>(v.base + slot * E);
+        tile(raw, 1);
+    }
+    {
+        float s0, s1, u0, u1;
+        unpack2(s2, s0, s1);
+        unpack2(u2, u0, u1);
+        st.s = s0 + s1;
+        st.u = u0 + u1;
+    }
+    const int64_t edge = edge_entry(v, tid);
+    if (edge >= 0) add_one(st, load_one(v.x, edge));
+    const float mine = st.m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        Softmax b;
+        b.m = __shfl_xor_sync(0xffffffffu, st.m, o);
+        b.s = __shfl_xor_sync(0xffffffffu, st.s, o);
+        b.u = __shfl_xor_sync(0xffffffffu, st.u, o);
+        join(st, b);
+    }
+    if (lane == 0) sh.part[warp] = st;
+    __syncthreads();
+    Softmax total = sh.part[0];
+#pragma unroll
+    for (int w = 1; w < LP_WARPS; ++w) join(total, sh.part[w]);
+    __syncthreads();
+    if (a.top) find_top(sh, v, mine, a.top);
+
+    if (parts == 1) {
+        const RowResult r = finish(total);
+        if (tid == 0) store_row<T>(a, row, r);
+        if (tid < a.top) store_top(a, row, tid, sh.top[tid], r);
+        return;
+    }
+    // the cluster's first CTA joins the others' results
+    cg::cluster_group cluster = cg::this_cluster();
+    if (tid == 0) sh.total = total;
+    cluster.sync();
+    if (rank == 0) {
+        for (int p = 1; p < parts; ++p) join(total, cluster.map_shared_rank(&sh, p)->total);
+        const RowResult r = finish(total);
+        if (tid == 0) store_row<T>(a, row, r);
+        if (a.top) {
+            const int n = parts * a.top;               // at most 256 = one entry per thread
+            unsigned long long key = 0;
+            if (tid < n) key = cluster.map_shared_rank(&sh, tid / a.top)->top[tid % a.top];
+            if (tid < n) sh.list[tid] = key;
+            __syncthreads();
+            if (key != 0) {
+                int at = 0;
+                for (int j = 0; j < n; ++j) at += sh.list[j] > key;
+                if (at < a.top) store_top(a, row, at, key, r);
+            }
+        }
+    }
+    cluster.sync();
+}
+
+template <typename T>
+cudaError_t forward(const ForwardArgs& a, int sm_count, cudaStream_t stream) {
+    if (a.vocab <= 1024) {
+        const int lanes = a.vocab <= 64 ? 8 : 32;
+        const int64_t blocks = (a.rows + LP_THREADS / lanes - 1) / (LP_THREADS / lanes);
+        if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+        const unsigned g = unsigned(blocks);
+        if (a.vocab <= 16) logprobs_small_kernel<T, 8, 2><<<g, LP_THREADS, 0, stream>>>(a);
+        else if (a.vocab <= 64) logprobs_small_kernel<T, 8, 8><<<g, LP_THREADS, 0, stream>>>(a);
+        else if (a.vocab <= 256) logprobs_small_kernel<T, 32, 8><<<g, LP_THREADS, 0, stream>>>(a);
+        else logprobs_small_kernel<T, 32, 32><<<g, LP_THREADS, 0, stream>>>(a);
+        return cudaGetLastError();
+    }
+    // A row is split over a cluster while that still leaves SMs without work and every CTA a tile
+    // of its own (LP_UNROLL slots per thread).
+    int parts = 1;
+    const int64_t slots = a.vocab / Elem<T>::PER16;
+    while (parts < LP_MAX_CLUSTER && a.rows * parts < 2 * sm_count && slots >= int64_t(2 * parts) * LP_THREADS * LP_UNROLL) parts *= 2;
+    if (a.rows * parts > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(a.rows * parts));
+    cfg.blockDim = dim3(LP_THREADS);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(parts);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = parts > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, logprobs_kernel<T>, a, parts);
+}
+
+// ---- gradient --------------------------------------------------------------------------------
+struct BackwardArgs {
+    const void*    logits;
+    void*          dlogits;
+    int64_t        rows, vocab, ld, ldo;
+    const int64_t* targets;
+    const float *  lse, *lse_lo, *entropy;
+    const int64_t* top_index;
+    const float *  grad_logprobs, *grad_entropy, *grad_top;
+    int            top;
+};
+
+// A row's constants and the entries that carry a term of their own.
+struct RowGrad {
+    float   lse, lse_lo, entropy, c, sum;  // sum = a + sum_i b_i
+    bool    empty;
+};
+
+// entry `i` of a row's list of special entries: the target (i = 0) and the top alternatives
+__device__ __forceinline__ int64_t special_index(const BackwardArgs& g, int64_t row, int i) {
+    if (i == 0) {
+        const int64_t t = g.grad_logprobs ? g.targets[row] : -1;
+        return t >= 0 ? t : -1;
+    }
+    return g.top_index[row * g.top + i - 1];
+}
+__device__ __forceinline__ float special_grad(const BackwardArgs& g, int64_t row, int i) {
+    return i == 0 ? g.grad_logprobs[row] : g.grad_top[row * g.top + i - 1];
+}
+__device__ __forceinline__ RowGrad row_grad(const BackwardArgs& g, int64_t row) {
+    RowGrad r;
+    r.lse = g.lse[row];
+    r.lse_lo = g.lse_lo ? g.lse_lo[row] : 0.f;
+    r.empty = r.lse == -CUDART_INF_F;
+    r.c = g.grad_entropy ? g.grad_entropy[row] : 0.f;
+    r.entropy = g.grad_entropy ? g.entropy[row] : 0.f;
+    r.sum = 0.f;
+    if (g.grad_logprobs) {
+        const int64_t t = g.targets[row];
+        if (t >= g.vocab) r.sum = CUDART_NAN_F;
+        else if (t >= 0) r.sum = g.grad_logprobs[row];
+    }
+    for (int i = 0; i < g.top; ++i) {
+        const int64_t t = g.top_index[row * g.top + i];
+        r.sum += (t < 0 || t >= g.vocab) ? CUDART_NAN_F : g.grad_top[row * g.top + i];
+    }
+    return r;
+}
+__device__ __forceinline__ float grad_at(const RowGrad& r, float x) {
+    const float lp = max_nan((x - r.lse) - r.lse_lo, LP_FLOOR);
+    const float p = ex2(lp * kLog2e);
+    const float d = -p * fmaf(r.c, lp + r.entropy, r.sum);
+    return r.empty ? 0.f : d;
+}
+
+// gradient of special entry i, its base value included: the terms of every special entry at the same place
+template <typename T>
+__device__ __forceinline__ float special_value(const BackwardArgs& g, int64_t row, const RowGrad& r, int64_t at, float x) {
+    float d = grad_at(r, x);
+    if (r.empty) return 0.f;
+    for (int i = 0; i <= g.top; ++i)
+        if (special_index(g, row, i) == at) d += special_grad(g, row, i);
+    return d;
+}
+
+// Rows of up to 1024 entries: L lanes per row.
+template <typename T, int L>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_backward_small_kernel(const BackwardArgs g) {
+    const int lane = threadIdx.x % L;
+    const int64_t row = (int64_t(blockIdx.x) * LP_THREADS + threadIdx.x) / L;
+    const bool live = row < g.rows;
+    const T* x = static_cast<const T*>(g.logits) + (live ? row : 0) * g.ld;
+    T* dx = static_cast<T*>(g.dlogits) + (live ? row : 0) * g.ldo;
+    // the special entries' logits are read before anything is written: dx may be x
+    constexpr int MINE = (GAR_MAX_TOP + L) / L;
+    float at_x[MINE];
+    int64_t at[MINE];
+    RowGrad r{};
+    if (live) {
+        r = row_grad(g, row);
+#pragma unroll
+        for (int q = 0; q < MINE; ++q) {
+            const int i = lane + q * L;
+            at[q] = i <= g.top ? special_index(g, row, i) : -1;
+            if (at[q] >= g.vocab) at[q] = -1;
+            at_x[q] = at[q] >= 0 ? load_one(x, at[q]) : 0.f;
+        }
+    }
+    __syncwarp();
+    if (live)
+        for (int64_t j = lane; j < g.vocab; j += L) dx[j] = Elem<T>::narrow(grad_at(r, load_one(x, j)));
+    __syncwarp();
+    if (live) {
+#pragma unroll
+        for (int q = 0; q < MINE; ++q)
+            if (at[q] >= 0) dx[at[q]] = Elem<T>::narrow(special_value<T>(g, row, r, at[q], at_x[q]));
+    }
+}
+
+// Longer rows: a CTA takes LPB_SLOTS 16-byte slots per thread of one row.  The special entries are
+// overwritten after a barrier (the CTA that owns an entry owns all writes to it).
+constexpr int LPB_SLOTS = 4;
+
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_backward_kernel(const BackwardArgs g, unsigned chunks) {
+    constexpr int E = Elem<T>::PER16;
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x / chunks;
+    const unsigned chunk = blockIdx.x % chunks;
+    const T* x = static_cast<const T*>(g.logits) + row * g.ld;
+    T* dx = static_cast<T*>(g.dlogits) + row * g.ldo;
+    const int head = int((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
+    const bool together = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 15) == 0;
+    // slot i: elements [i E - head, (i + 1) E - head)
+    const int64_t slot0 = int64_t(chunk) * (LP_THREADS * LPB_SLOTS) + tid;
+    const int64_t lo = int64_t(chunk) * (LP_THREADS * LPB_SLOTS * E) - head;
+    const int64_t hi = lo + LP_THREADS * LPB_SLOTS * E;
+
+    uint4 raw[LPB_SLOTS];
+    bool whole[LPB_SLOTS];
+#pragma unroll
+    for (int i = 0; i < LPB_SLOTS; ++i) {
+        const int64_t j = (slot0 + i * LP_THREADS) * E - head;
+        whole[i] = together && j >= 0 && j + E <= g.vocab;
+        if (whole[i]) raw[i] = load_stream(x + j);
+    }
+    const RowGrad r = row_grad(g, row);
+    int64_t at = -1;
+    float at_x = 0.f;
+    if (tid <= g.top) {
+        at = special_index(g, row, tid);
+        if (at < lo || at >= hi || at >= g.vocab) at = -1;
+        if (at >= 0) at_x = load_one(x, at);
+    }
+    __syncthreads();                      // read before anything is written: dx may be x
+#pragma unroll
+    for (int i = 0; i < LPB_SLOTS; ++i) {
+        const int64_t j = (slot0 + i * LP_THREADS) * E - head;
+        if (whole[i]) {
+            float f[E];
+            widen16B(raw[i], f, static_cast<const T*>(nullptr));
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[e] = grad_at(r, f[e]);
+            store_stream(dx + j, narrow16B(f, static_cast<const T*>(nullptr)));
+        } else {
+            for (int e = 0; e < E; ++e)
+                if (j + e >= 0 && j + e < g.vocab) dx[j + e] = Elem<T>::narrow(grad_at(r, load_one(x, j + e)));
+        }
+    }
+    __syncthreads();
+    if (at >= 0) dx[at] = Elem<T>::narrow(special_value<T>(g, row, r, at, at_x));
+}
+
+template <typename T>
+cudaError_t backward(const BackwardArgs& g, cudaStream_t stream) {
+    if (g.vocab <= 1024) {
+        const int lanes = g.vocab <= 64 ? 8 : 32;
+        const int64_t blocks = (g.rows + LP_THREADS / lanes - 1) / (LP_THREADS / lanes);
+        if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+        if (lanes == 8) logprobs_backward_small_kernel<T, 8><<<unsigned(blocks), LP_THREADS, 0, stream>>>(g);
+        else logprobs_backward_small_kernel<T, 32><<<unsigned(blocks), LP_THREADS, 0, stream>>>(g);
+        return cudaGetLastError();
+    }
+    constexpr int64_t per = int64_t(LP_THREADS) * LPB_SLOTS * Elem<T>::PER16;
+    const int64_t chunks = (g.vocab + Elem<T>::PER16 - 1 + per - 1) / per;      // with the largest head
+    if (g.rows * chunks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    logprobs_backward_kernel<T><<<unsigned(g.rows * chunks), LP_THREADS, 0, stream>>>(g, unsigned(chunks));
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_logprobs(const gar_logprobs_params_t& p, int64_t ld, int sm_count) {
+    const ForwardArgs a{p.logits, p.rows, p.vocab, ld, p.targets, p.logprobs, p.entropy, p.lse, p.lse_lo, p.top_logprobs, p.top_index, p.top};
+    cudaStream_t s = static_cast<cudaStream_t>(p.stream);
+    if (p.dtype == GAR_F32) return forward<float>(a, sm_count, s);
+    if (p.dtype == GAR_BF16) return forward<__nv_bfloat16>(a, sm_count, s);
+    return forward<__half>(a, sm_count, s);
+}
+
+cudaError_t launch_logprobs_backward(const gar_logprobs_grad_params_t& p, int64_t ld, int64_t ldo) {
+    const BackwardArgs g{p.logits, p.dlogits, p.rows, p.vocab, ld, ldo, p.targets, p.lse, p.lse_lo, p.entropy, p.top_index,
+                         p.grad_logprobs, p.grad_entropy, p.grad_top, p.top};
+    cudaStream_t s = static_cast<cudaStream_t>(p.stream);
+    if (p.dtype == GAR_F32) return backward<float>(g, s);
+    if (p.dtype == GAR_BF16) return backward<__nv_bfloat16>(g, s);
+    return backward<__half>(g, s);
+}
+
+}  // namespace worker
+}  // namespace gar
