@@ -86,7 +86,7 @@ int gar_token_logprobs_backward(const gar_logprobs_grad_params_t* params);
 /*
  * Activation checkpoints in 8 bits.  Every `group` (32, 64 or 128) consecutive columns of a row
  * share one fp32 scale; with A the largest magnitude of the group
- *     scale = A / 127,   q = rint(x * (127 / A))  (int8, ties to even),
+ *     scale = A / 127,   q = rint(x * ((1 / A) * 127))   (int8, ties to even, each step rounded to fp32),
  * and a restored value is q * scale rounded once to the activation's element type, at most half a
  * step (plus that rounding) from the original.  A group with A < 2^-100 is stored as zeros; a
  * group that holds a NaN or an infinity gets scale NaN and is restored as NaN throughout.

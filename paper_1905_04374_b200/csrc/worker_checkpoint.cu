@@ -13,9 +13,6 @@ namespace {
 constexpr int CK_THREADS = 256;
 constexpr float CK_TINY = 7.888609052210118e-31f;     // 2^-100
 
-// a / b and a * b with IEEE rounding, never contracted
-__device__ __forceinline__ float div_rn(float a, float b) { return __fdiv_rn(a, b); }
-
 // Division of a task number by the tasks per row: exact for numerators below 2^31.
 struct FastDiv {
     unsigned d = 1, mul = 1, shift = 0;
@@ -71,12 +68,12 @@ __device__ __forceinline__ void save8(const float (&v)[8], int count, int lanes,
     for (int o = lanes >> 1; o; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (count <= 0) return;
     const bool sound = top <= 3.402823466e38f, zero = top < CK_TINY;
-    const float inv = sound && !zero ? div_rn(127.f, top) : 0.f;
-    if (leader) *scale = !sound ? CUDART_NAN_F : zero ? 0.f : div_rn(top, 127.f);
+    const float inv = sound && !zero ? __fmul_rn(__frcp_rn(top), 127.f) : 0.f;
+    if (leader) *scale = !sound ? CUDART_NAN_F : zero ? 0.f : __fdiv_rn(top, 127.f);
     unsigned r[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        // |v inv| <= 127 (1 + 2^-23): the sum's low byte is the nearest integer, ties to even
+        // |v inv| <= 127 (1 + 2^-22): the sum's low byte is the nearest integer, ties to even
         const unsigned b = __float_as_uint(__fadd_rn(__fmul_rn(v[i], inv), 12582912.f));
         r[i] = sound ? b : 0u;
     }

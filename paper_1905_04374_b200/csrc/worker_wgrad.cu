@@ -1,93 +1,554 @@
 // Per-worker weight gradients from 8-bit checkpoints (gar_worker.h): dW_w = dY_w^T X'_w, written
-// into the rows of the gradient block.
+// into the rows of the gradient block, on the fifth-generation tensor cores.
 //
-// Plain tiled form: a CTA forms a 64 x 64 tile of one worker's gradient, 16 tokens at a time
-// through shared memory, 4 x 4 fp32 accumulators per thread.
+// A restored activation x' is a value of dy's own 16-bit type, so the products of the two are exact
+// and tcgen05.mma (kind::f16, fp32 accumulators in tensor memory) sums them in fp32.  The contraction
+// runs over tokens, which are the ROWS of both matrices: both operands are "MN-major" (the output
+// dimension is the contiguous one), which the tensor core takes as they lie, no transpose.
+//
+// One persistent CTA per SM, tiles of 128 outputs x 256 inputs of one worker, 64 tokens a step:
+//   TMA warp       dy: two 64-column boxes per step, 128-byte swizzle, straight into the operand
+//                  layout; codes: one 256-byte wide box.  The tensor maps are three-dimensional
+//                  (columns, tokens, workers): what lies past a worker's tokens arrives as zeros and
+//                  no other worker's rows are read.
+//   restore warps  eight: codes -> 16-bit values (byte permute into fp32, subtract, multiply by the
+//                  row group's scale, one rounding) -> operand tile in shared memory, same layout
+//   MMA warp       one lane, four 128 x 256 x 16 instructions per step
+//   store warps    four: tensor memory -> shared memory -> coalesced stores, while the next tile's
+//                  products run into the other half of tensor memory
+// The bias is one more column tile whose second operand is a block of ones.
+// Hand-offs are mbarriers; every wait is bounded: a wait that gives up raises an error flag, all
+// roles leave their loops once what they have in flight has landed, and the CTA's tiles become NaN.
+#include <cuda.h>
+
+#include "gar_internal.cuh"
+#include "mbar.cuh"
 #include "worker_common.cuh"
 
 namespace gar {
 namespace worker {
 namespace {
 
-constexpr int WG_TILE = 64, WG_K = 16, WG_THREADS = 256;
+constexpr int WG_M = 128, WG_N = 256, WG_K = 64;      // tile and tokens per step
+constexpr int WG_STAGES = 3;
+constexpr int WG_THREADS = 512;
+constexpr int WG_TMA_WARP = 0, WG_MMA_WARP = 1, WG_ALLOC_WARP = 2;
+constexpr int WG_STORE_WARP0 = 4;                     // 4..7: tensor-memory lanes 32 (warp % 4) ..
+constexpr int WG_RESTORE_WARP0 = 8, WG_RESTORE_WARPS = 8;
+constexpr int WG_BLOCK = 64 * 128;                    // bytes of 64 tokens x 64 columns of an operand
+constexpr int WG_A_BYTES = WG_M / 64 * WG_BLOCK, WG_B_BYTES = WG_N / 64 * WG_BLOCK, WG_Q_BYTES = WG_K * WG_N;
+constexpr int WG_PAD = 36;                            // floats per staged row of the store warps
+constexpr int WG_GROUP_M = 8;                         // row tiles that go round a column tile together
+constexpr int WG_BIAS_N = 16;
 
-struct WeightGradArgs {
+struct __align__(1024) WGSmem {
+    uint8_t a[WG_STAGES][WG_A_BYTES];
+    uint8_t b[WG_STAGES][WG_B_BYTES];
+    uint8_t q[WG_STAGES][WG_Q_BYTES];
+    float   out[4][32 * WG_PAD];
+    alignas(1024) uint16_t ones[512];
+    unsigned long long a_full[WG_STAGES], q_full[WG_STAGES], q_empty[WG_STAGES], b_full[WG_STAGES], empty[WG_STAGES];
+    unsigned long long acc_full[2], acc_empty[2];
+    unsigned tmem_base;
+    int      error;
+};
+
+struct WGArgs {
     const void*    dy;
-    const int8_t*  q;
     const float*   scales;
     const int32_t* lengths;
     void *         dw, *db;
-    int64_t        tokens, out, in, ld_dy, ldq, ld_grads;
-    int            groups, group_shift;
+    int64_t        tokens, out, in, ld_dy, ld_grads;
+    int            workers, groups, group_shift;
+    int            mt, nt;                // row tiles, column tiles (the bias tile, if any, is one more)
+    int            columns;               // nt + 1 with a bias
+    int            wide;                  // rows of the result start on 16 bytes
 };
 
-template <typename G> __device__ __forceinline__ void put(G* p, float v) { *p = Elem<G>::narrow(v); }
+// ---- tcgen05 ------------------------------------------------------------------------------------
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-template <typename T, typename G>
-__global__ void __launch_bounds__(WG_THREADS) weight_grad_kernel(const WeightGradArgs a) {
-    __shared__ float sa[WG_K][WG_TILE], sb[WG_K][WG_TILE];
-    const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
-    const int64_t i0 = int64_t(blockIdx.x) * WG_TILE, o0 = int64_t(blockIdx.y) * WG_TILE;
-    const int w = blockIdx.z;
-    int64_t len = a.tokens;
-    if (a.lengths) {
-        const int64_t l = a.lengths[w];
-        len = l < 0 ? 0 : l < len ? l : len;
+// Operand descriptor.  MN-major, 128-byte swizzle: blocks of 64 columns `lbo` bytes apart, groups of
+// eight tokens 1024 bytes apart.  Bits [0,14) address / 16, [16,30) lbo / 16, [32,46) sbo / 16,
+// [46,48) = 1 (version), [61,64) = 2 (128-byte swizzle).
+__device__ __forceinline__ unsigned long long operand_desc(unsigned saddr, unsigned lbo, unsigned sbo, unsigned layout) {
+    return static_cast<unsigned long long>((saddr >> 4) & 0x3fffu) | (static_cast<unsigned long long>(lbo >> 4) << 16) |
+           (static_cast<unsigned long long>(sbo >> 4) << 32) | (1ull << 46) | (static_cast<unsigned long long>(layout) << 61);
+}
+// Instruction descriptor, kind::f16: fp32 accumulators (1 at bit 4), both operands bf16 (1) or
+// binary16 (0) at bits 7 and 10, both MN-major (bits 15, 16), N / 8 at bit 17, M / 16 at bit 24.
+__host__ __device__ constexpr unsigned instruction_desc(int type, int n) {
+    return (1u << 4) | (unsigned(type) << 7) | (unsigned(type) << 10) | (1u << 15) | (1u << 16) | (unsigned(n >> 3) << 17) |
+           (unsigned(WG_M >> 4) << 24);
+}
+__device__ __forceinline__ void mma_f16(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+}
+__device__ __forceinline__ void mma_commit(unsigned long long* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(kb_smem_u32(bar)) : "memory");
+}
+// this thread's lane of tensor memory, 32 consecutive columns
+__device__ __forceinline__ void tmem_ld32(unsigned taddr, float (&v)[32]) {
+    unsigned r[32];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+                   "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+                   "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+
+// ---- tiles --------------------------------------------------------------------------------------
+struct Tile {
+    int     worker, m, n;        // n == nt: the bias
+    int     steps;               // of WG_K tokens
+    int64_t len;                 // the worker's tokens that count
+};
+__device__ __forceinline__ int64_t worker_len(const WGArgs& a, int w) {
+    if (!a.lengths) return a.tokens;
+    const int64_t l = a.lengths[w];
+    return l < 0 ? 0 : l < a.tokens ? l : a.tokens;
+}
+__device__ __forceinline__ Tile tile_at(const WGArgs& a, int64_t index) {
+    Tile t;
+    const int per = a.mt * a.columns;
+    t.worker = int(index / per);
+    const int r = int(index - int64_t(t.worker) * per);
+    const int g = r / (WG_GROUP_M * a.columns), in_group = r - g * WG_GROUP_M * a.columns;
+    const int rows = min(WG_GROUP_M, a.mt - g * WG_GROUP_M);
+    t.n = in_group / rows;
+    t.m = g * WG_GROUP_M + in_group % rows;
+    t.len = worker_len(a, t.worker);
+    t.steps = int((t.len + WG_K - 1) / WG_K);
+    return t;
+}
+__device__ __forceinline__ int64_t tile_count(const WGArgs& a) { return int64_t(a.workers) * a.mt * a.columns; }
+
+// Position in a ring of `depth` buffers and the parity of its round.
+struct Ring {
+    int slot = 0;
+    unsigned parity = 0;
+    __device__ __forceinline__ void next(int depth) {
+        if (++slot == depth) {
+            slot = 0;
+            parity ^= 1u;
+        }
     }
-    float acc[4][4] = {}, bias[4] = {};
-    for (int64_t t0 = 0; t0 < len; t0 += WG_K) {
-        for (int e = tid; e < WG_K * WG_TILE; e += WG_THREADS) {
-            const int k = e / WG_TILE, c = e % WG_TILE;
-            const int64_t t = t0 + k, row = int64_t(w) * a.tokens + t;
-            sa[k][c] = t < len && o0 + c < a.out ? Elem<T>::widen(static_cast<const T*>(a.dy)[row * a.ld_dy + o0 + c]) : 0.f;
-            float x = 0.f;
-            if (t < len && i0 + c < a.in)
-                x = Elem<T>::widen(Elem<T>::narrow(float(a.q[row * a.ldq + i0 + c]) * a.scales[row * a.groups + ((i0 + c) >> a.group_shift)]));
-            sb[k][c] = x;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < WG_K; ++k) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float d = sa[k][ty * 4 + i];
-                bias[i] += d;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(d, sb[k][tx * 4 + j], acc[i][j]);
-            }
-        }
-        __syncthreads();
-    }
-    G* dw = static_cast<G*>(a.dw) + int64_t(w) * a.ld_grads;
-    for (int i = 0; i < 4; ++i) {
-        const int64_t o = o0 + ty * 4 + i;
-        if (o >= a.out) break;
-        for (int j = 0; j < 4; ++j) {
-            const int64_t c = i0 + tx * 4 + j;
-            if (c < a.in) put(dw + o * a.in + c, acc[i][j]);
-        }
-        if (a.db && blockIdx.x == 0 && tx == 0) put(static_cast<G*>(a.db) + int64_t(w) * a.ld_grads + o, bias[i]);
+};
+
+// two codes' bytes of a word -> fp32 codes -> times the scale -> a pair of T
+template <typename T>
+__device__ __forceinline__ unsigned restore_pair(unsigned biased, unsigned sel0, unsigned sel1, f32x2 scale) {
+    const f32x2 v = pack2(__uint_as_float(__byte_perm(biased, 0x4b000000u, sel0)), __uint_as_float(__byte_perm(biased, 0x4b000000u, sel1)));
+    float x, y;
+    unpack2(mul2(add2(v, pack2(-8388736.f, -8388736.f)), scale), x, y);
+    if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value) {
+        const __half2 h = __floats2half2_rn(x, y);
+        return *reinterpret_cast<const unsigned*>(&h);
+    } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        return *reinterpret_cast<const unsigned*>(&h);
     }
 }
 
+template <typename G> __device__ __forceinline__ void put4(G* p, const float4& v);
+template <> __device__ __forceinline__ void put4(float* p, const float4& v) { __stcs(reinterpret_cast<float4*>(p), v); }
+template <> __device__ __forceinline__ void put4(__nv_bfloat16* p, const float4& v) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    __stcs(reinterpret_cast<uint2*>(p), make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b)));
+}
+template <> __device__ __forceinline__ void put4(__half* p, const float4& v) {
+    const __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
+    __stcs(reinterpret_cast<uint2*>(p), make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b)));
+}
+
+// dy by plain loads into the operand layout (rows that do not start on 16 bytes): warp `w` of the
+// restore warps fills tokens 8 w .. 8 w + 7.
 template <typename T>
-cudaError_t weight_grad(const WeightGradArgs& a, int workers, int grads_dtype, cudaStream_t stream) {
-    const dim3 grid(unsigned((a.in + WG_TILE - 1) / WG_TILE), unsigned((a.out + WG_TILE - 1) / WG_TILE), unsigned(workers));
-    if (grads_dtype == GAR_F32) weight_grad_kernel<T, float><<<grid, WG_THREADS, 0, stream>>>(a);
-    else if (grads_dtype == GAR_BF16) weight_grad_kernel<T, __nv_bfloat16><<<grid, WG_THREADS, 0, stream>>>(a);
-    else weight_grad_kernel<T, __half><<<grid, WG_THREADS, 0, stream>>>(a);
+__device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int step, uint8_t* tile, int w, int lane) {
+    const unsigned short* dy = static_cast<const unsigned short*>(a.dy);
+#pragma unroll 2
+    for (int k = 0; k < 8; ++k) {
+        const int row = 8 * w + k;
+        const int64_t token = int64_t(step) * WG_K + row;
+        const unsigned short* src = dy + (int64_t(t.worker) * a.tokens + token) * a.ld_dy;
+#pragma unroll
+        for (int i = 0; i < WG_M / 32; ++i) {
+            const int c = lane + 32 * i;
+            const int64_t o = int64_t(t.m) * WG_M + c;
+            const unsigned short v = token < t.len && o < a.out ? __ldg(src + o) : static_cast<unsigned short>(0);
+            const int at = (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4) + (c % 8) * 2;
+            *reinterpret_cast<unsigned short*>(tile + at) = v;
+        }
+    }
+}
+
+// TMA_A: dy comes by TMA (else the restore warps load it).
+template <typename T, typename G, bool TMA_A>
+__global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs a, const __grid_constant__ CUtensorMap map_dy,
+                                                                    const __grid_constant__ CUtensorMap map_q) {
+    extern __shared__ uint8_t raw[];
+    WGSmem& sm = *reinterpret_cast<WGSmem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    volatile int* error = &sm.error;
+    if (tid == 0) {
+        sm.error = 0;
+        for (int s = 0; s < WG_STAGES; ++s) {
+            kb_init(&sm.a_full[s], 1);
+            kb_init(&sm.q_full[s], 1);
+            kb_init(&sm.q_empty[s], WG_RESTORE_WARPS);
+            kb_init(&sm.b_full[s], WG_RESTORE_WARPS);
+            kb_init(&sm.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            kb_init(&sm.acc_full[b], 1);
+            kb_init(&sm.acc_empty[b], 4);
+        }
+        kb_fence_init();
+    }
+    for (int i = tid; i < 512; i += WG_THREADS) sm.ones[i] = std::is_same<T, __half>::value ? 0x3c00 : 0x3f80;
+    fence_async_smem();
+    if (warp == WG_ALLOC_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kb_smem_u32(&sm.tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const unsigned tmem = sm.tmem_base;
+    const int64_t tiles = tile_count(a);
+
+    if (warp == WG_TMA_WARP) {
+        if (lane == 0) {
+            Ring ra, rq;
+            bool ok = true;
+            for (int64_t i = blockIdx.x; ok && i < tiles; i += gridDim.x) {
+                const Tile t = tile_at(a, i);
+                for (int s = 0; s < t.steps; ++s) {
+                    if (t.n < a.nt) {
+                        if (!kb_wait(kb_smem_u32(&sm.q_empty[rq.slot]), rq.parity ^ 1u, error)) { ok = false; break; }
+                        const unsigned bar = kb_smem_u32(&sm.q_full[rq.slot]);
+                        kb_expect_tx(bar, WG_Q_BYTES);
+                        tma_load(kb_smem_u32(sm.q[rq.slot]), &map_q, t.n * WG_N, s * WG_K, t.worker, bar);
+                        rq.next(WG_STAGES);
+                    }
+                    if (TMA_A) {
+                        if (!kb_wait(kb_smem_u32(&sm.empty[ra.slot]), ra.parity ^ 1u, error)) { ok = false; break; }
+                        const unsigned bar = kb_smem_u32(&sm.a_full[ra.slot]), dst = kb_smem_u32(sm.a[ra.slot]);
+                        kb_expect_tx(bar, WG_A_BYTES);
+                        tma_load(dst, &map_dy, t.m * WG_M, s * WG_K, t.worker, bar);
+                        tma_load(dst + WG_BLOCK, &map_dy, t.m * WG_M + 64, s * WG_K, t.worker, bar);
+                        ra.next(WG_STAGES);
+                    }
+                }
+            }
+            if (!ok) {
+                // the copies in flight land before the CTA's shared memory is given back
+                for (int k = 0; k < WG_STAGES; ++k) {
+                    // the slot's latest copy completed the phase before the ring's position
+                    kb_wait(kb_smem_u32(&sm.q_full[k]), k < rq.slot ? rq.parity : rq.parity ^ 1u, error, true, 1u << 10);
+                    if (TMA_A) kb_wait(kb_smem_u32(&sm.a_full[k]), k < ra.slot ? ra.parity : ra.parity ^ 1u, error, true, 1u << 10);
+                }
+            }
+        }
+    } else if (warp == WG_MMA_WARP) {
+        if (lane == 0) {
+            Ring r, acc;
+            bool ok = true;
+            const unsigned idesc = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, WG_N);
+            const unsigned idesc_bias = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, WG_BIAS_N);
+            for (int64_t i = blockIdx.x; ok && i < tiles; i += gridDim.x) {
+                const Tile t = tile_at(a, i);
+                if (t.steps == 0) continue;
+                if (!kb_wait(kb_smem_u32(&sm.acc_empty[acc.slot]), acc.parity ^ 1u, error)) { ok = false; break; }
+                tc_fence_after();
+                const unsigned d = tmem + unsigned(acc.slot) * WG_N;
+                const bool bias = t.n == a.nt;
+                for (int s = 0; s < t.steps; ++s) {
+                    if (TMA_A && !kb_wait(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error)) { ok = false; break; }
+                    if (!kb_wait(kb_smem_u32(&sm.b_full[r.slot]), r.parity, error)) { ok = false; break; }
+                    tc_fence_after();
+                    const unsigned sa = kb_smem_u32(sm.a[r.slot]), sb = kb_smem_u32(sm.b[r.slot]);
+#pragma unroll
+                    for (int k = 0; k < WG_K / 16; ++k) {
+                        const unsigned long long da = operand_desc(sa + k * 2048, WG_BLOCK, 1024, 2);
+                        // a block of ones needs no layout: every address the descriptor reaches holds 1
+                        const unsigned long long db = bias ? operand_desc(kb_smem_u32(sm.ones), 256, 256, 0)
+                                                           : operand_desc(sb + k * 2048, WG_BLOCK, 1024, 2);
+                        mma_f16(d, da, db, bias ? idesc_bias : idesc, s > 0 || k > 0);
+                    }
+                    mma_commit(&sm.empty[r.slot]);
+                    r.next(WG_STAGES);
+                }
+                if (ok) {
+                    mma_commit(&sm.acc_full[acc.slot]);
+                    acc.next(2);
+                }
+            }
+            // nothing is in flight when the tensor memory is freed: on the good path the store warps have
+            // seen every accumulator; after a wait that gave up, wait for what was issued
+            if (!ok) {
+                mma_commit(&sm.acc_full[acc.slot]);
+                kb_wait(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error, true, 1u << 10);
+            }
+        }
+    } else if (warp >= WG_RESTORE_WARP0) {
+        const int w = warp - WG_RESTORE_WARP0, tl = lane & 7, sub = lane >> 3;
+        Ring r, rq;
+        bool ok = true;
+        for (int64_t i = blockIdx.x; ok && i < tiles; i += gridDim.x) {
+            const Tile t = tile_at(a, i);
+            const bool bias = t.n == a.nt;
+            const int row = 8 * w + tl;                           // this lane's token of a step
+            const int64_t base = int64_t(t.worker) * a.tokens;
+            // the lane's four 16-column pieces of the row: a diagonal over the eight lanes of a phase, so
+            // that neither the reads of the codes nor the swizzled stores meet in a bank
+            int piece[4];
+            int64_t group[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                piece[k] = ((tl + sub + 4 * (k & 1)) & 7) + 8 * (k >> 1);
+                group[k] = (int64_t(t.n) * WG_N + piece[k] * 16) >> a.group_shift;
+            }
+            float next[4];
+            auto fetch_scales = [&](int s) {
+                const int64_t token = int64_t(s) * WG_K + row;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    next[k] = !bias && token < t.len && group[k] < a.groups ? __ldg(a.scales + (base + token) * a.groups + group[k]) : 0.f;
+            };
+            if (t.steps) fetch_scales(0);
+            for (int s = 0; s < t.steps; ++s) {
+                float scale[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) scale[k] = next[k];
+                if (s + 1 < t.steps) fetch_scales(s + 1);
+                if (!kb_wait_warp(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
+                if (!bias) {
+                    if (!kb_wait_warp(kb_smem_u32(&sm.q_full[rq.slot]), rq.parity, error)) { ok = false; break; }
+                    const uint8_t* q = sm.q[rq.slot];
+                    uint8_t* b = sm.b[r.slot];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint4 c = *reinterpret_cast<const uint4*>(q + row * WG_N + piece[k] * 16);
+                        const unsigned words[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
+                        const f32x2 sc = pack2(scale[k], scale[k]);
+                        unsigned v[8];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            v[2 * j] = restore_pair<T>(words[j], 0x7440, 0x7441, sc);
+                            v[2 * j + 1] = restore_pair<T>(words[j], 0x7442, 0x7443, sc);
+                        }
+                        uint8_t* dst = b + (piece[k] >> 2) * WG_BLOCK + row * 128;
+                        const int chunk = (piece[k] & 3) * 2;
+                        *reinterpret_cast<uint4*>(dst + ((chunk ^ tl) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4*>(dst + (((chunk + 1) ^ tl) << 4)) = make_uint4(v[4], v[5], v[6], v[7]);
+                    }
+                }
+                if (!TMA_A) {
+                    load_dy<T>(a, t, s, sm.a[r.slot], w, lane);
+                } else if (a.lengths && int64_t(s + 1) * WG_K > t.len) {
+                    // tokens behind the worker's length: zeros in place of what the copy brought
+                    if (!kb_wait_warp(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error)) { ok = false; break; }
+                    for (int k = 0; k < 8; ++k) {
+                        const int rr = 8 * w + k;
+                        if (int64_t(s) * WG_K + rr >= t.len && lane < WG_A_BYTES / WG_BLOCK * 8)
+                            *reinterpret_cast<uint4*>(sm.a[r.slot] + (lane / 8) * WG_BLOCK + rr * 128 + (lane % 8) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    kb_arrive(&sm.b_full[r.slot]);
+                    if (!bias) kb_arrive(&sm.q_empty[rq.slot]);
+                }
+                r.next(WG_STAGES);
+                if (!bias) rq.next(WG_STAGES);
+            }
+        }
+    } else if (warp >= WG_STORE_WARP0) {
+        const int quarter = warp - WG_STORE_WARP0;               // == warp % 4: tensor-memory lanes 32 quarter ..
+        float* stage = sm.out[quarter];
+        Ring acc;
+        bool ok = true;
+        for (int64_t i = blockIdx.x; ok && i < tiles; i += gridDim.x) {
+            const Tile t = tile_at(a, i);
+            const int64_t o0 = int64_t(t.m) * WG_M + quarter * 32;
+            const unsigned src = tmem + unsigned(acc.slot) * WG_N + (unsigned(quarter * 32) << 16);
+            if (t.steps) {
+                if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error)) { ok = false; break; }
+                tc_fence_after();
+            }
+            if (t.n == a.nt) {
+                float v[32];
+                if (t.steps) tmem_ld32(src, v);
+                else v[0] = 0.f;
+                if (o0 + lane < a.out) static_cast<G*>(a.db)[int64_t(t.worker) * a.ld_grads + o0 + lane] = Elem<G>::narrow(v[0]);
+            } else {
+                G* dw = static_cast<G*>(a.dw) + int64_t(t.worker) * a.ld_grads + o0 * a.in;
+                const int rows = int(min(int64_t(32), a.out - o0));
+                const int64_t left = a.in - int64_t(t.n) * WG_N;
+                const int cols = left < WG_N ? int(left) : WG_N;
+                dw += int64_t(t.n) * WG_N;
+                for (int c0 = 0; c0 < cols; c0 += 32) {
+                    float v[32];
+                    if (t.steps) {
+                        tmem_ld32(src + unsigned(c0), v);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = 0.f;
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4)
+                        *reinterpret_cast<float4*>(stage + lane * WG_PAD + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    __syncwarp();
+                    if (a.wide && cols - c0 >= 32) {
+                        const int c = (lane % 8) * 4;
+#pragma unroll
+                        for (int rr = 0; rr < 32; rr += 4) {
+                            const int row = rr + lane / 8;
+                            if (row < rows) put4(dw + int64_t(row) * a.in + c0 + c, *reinterpret_cast<const float4*>(stage + row * WG_PAD + c));
+                        }
+                    } else if (lane < cols - c0) {
+                        for (int row = 0; row < rows; ++row) dw[int64_t(row) * a.in + c0 + lane] = Elem<G>::narrow(stage[row * WG_PAD + lane]);
+                    }
+                }
+            }
+            if (t.steps) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) kb_arrive(&sm.acc_empty[acc.slot]);
+                acc.next(2);
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == WG_ALLOC_WARP)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    if (sm.error) {
+        // a wait gave up: nothing this CTA was to write may look like a gradient
+        for (int64_t i = blockIdx.x; i < tiles; i += gridDim.x) {
+            const Tile t = tile_at(a, i);
+            for (int e = tid; e < WG_M * WG_N; e += WG_THREADS) {
+                const int64_t o = int64_t(t.m) * WG_M + e / WG_N, c = int64_t(t.n) * WG_N + e % WG_N;
+                if (o >= a.out) continue;
+                if (t.n == a.nt) {
+                    if (e % WG_N == 0) static_cast<G*>(a.db)[int64_t(t.worker) * a.ld_grads + o] = Elem<G>::narrow(CUDART_NAN_F);
+                } else if (c < a.in) {
+                    static_cast<G*>(a.dw)[int64_t(t.worker) * a.ld_grads + o * a.in + c] = Elem<G>::narrow(CUDART_NAN_F);
+                }
+            }
+        }
+    }
+}
+
+// ---- launch -------------------------------------------------------------------------------------
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's entry point, looked up once.
+EncodeTiled encode_tiled() {
+    static const EncodeTiled found = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult how;
+        const cudaError_t err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &how);
+        return err == cudaSuccess && how == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(p) : nullptr;
+    }();
+    return found;
+}
+
+// [workers][tokens][cols] with row stride `pitch` bytes; boxes of `box` columns x WG_K tokens
+cudaError_t make_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t cols, int64_t tokens, int workers,
+                     int64_t pitch, int box, CUtensorMapSwizzle swizzle) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t rows = tokens > 0 ? cuuint64_t(tokens) : 1;
+    const cuuint64_t dims[3] = {cuuint64_t(cols), rows, cuuint64_t(workers)};
+    const cuuint64_t strides[2] = {cuuint64_t(pitch), cuuint64_t(pitch) * rows};
+    const cuuint32_t boxes[3] = {cuuint32_t(box), WG_K, 1}, steps[3] = {1, 1, 1};
+    const CUresult r = encode(map, type, 3, const_cast<void*>(base), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <typename T, typename G, bool TMA_A>
+cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_q, int sm_count, cudaStream_t stream) {
+    constexpr int bytes = int(sizeof(WGSmem)) + 1024;
+    auto kernel = weight_grad_kernel<T, G, TMA_A>;
+    if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
+    const int64_t tiles = int64_t(a.workers) * a.mt * a.columns;
+    const unsigned grid = unsigned(tiles < sm_count ? tiles : sm_count);
+    kernel<<<grid, WG_THREADS, bytes, stream>>>(a, map_dy, map_q);
     return cudaGetLastError();
+}
+template <typename T, bool TMA_A>
+cudaError_t launch_by_grads(int grads_dtype, const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_q, int sm_count,
+                            cudaStream_t stream) {
+    if (grads_dtype == GAR_F32) return launch<T, float, TMA_A>(a, map_dy, map_q, sm_count, stream);
+    if (grads_dtype == GAR_BF16) return launch<T, __nv_bfloat16, TMA_A>(a, map_dy, map_q, sm_count, stream);
+    return launch<T, __half, TMA_A>(a, map_dy, map_q, sm_count, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy, int) {
-    const WeightGradArgs a{p.dy, p.x_saved.q, p.x_saved.scales, p.lengths, p.weight_grads, p.bias_grads, p.tokens,
-                           p.out_features, p.in_features, ld_dy, p.x_saved.ldq, p.ld_grads,
-                           int((p.in_features + p.group - 1) / p.group), p.group == 32 ? 5 : p.group == 64 ? 6 : 7};
+cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy, int sm_count) {
+    WGArgs a{};
+    a.dy = p.dy;
+    a.scales = p.x_saved.scales;
+    a.lengths = p.lengths;
+    a.dw = p.weight_grads;
+    a.db = p.bias_grads;
+    a.tokens = p.tokens;
+    a.out = p.out_features;
+    a.in = p.in_features;
+    a.ld_dy = ld_dy;
+    a.ld_grads = p.ld_grads;
+    a.workers = p.workers;
+    a.groups = int((p.in_features + p.group - 1) / p.group);
+    a.group_shift = p.group == 32 ? 5 : p.group == 64 ? 6 : 7;
+    a.mt = int((p.out_features + WG_M - 1) / WG_M);
+    a.nt = int((p.in_features + WG_N - 1) / WG_N);
+    a.columns = a.nt + (p.bias_grads ? 1 : 0);
+    if (int64_t(a.mt) * a.columns >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
+    const int64_t gs = p.grads_dtype == GAR_F32 ? 4 : 2;
+    const int64_t unit = 4 * gs;                  // a store of four gradients
+    a.wide = reinterpret_cast<uintptr_t>(p.weight_grads) % unit == 0 && (p.workers == 1 || p.ld_grads * gs % unit == 0) &&
+             p.in_features * gs % unit == 0;
+
+    CUtensorMap map_q, map_dy;
+    if (cudaError_t err = make_map(&map_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.x_saved.q, p.in_features, p.tokens, p.workers,
+                                   p.x_saved.ldq, WG_N, CU_TENSOR_MAP_SWIZZLE_NONE)) return err;
+    // TMA needs rows of dy that start on 16 bytes
+    const bool tma_a = reinterpret_cast<uintptr_t>(p.dy) % 16 == 0 && ld_dy % 8 == 0;
+    if (tma_a) {
+        if (cudaError_t err = make_map(&map_dy, p.dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                                       p.dy, p.out_features, p.tokens, p.workers, ld_dy * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+    } else {
+        map_dy = map_q;                           // not used
+    }
     cudaStream_t s = static_cast<cudaStream_t>(p.stream);
-    return p.dtype == GAR_BF16 ? weight_grad<__nv_bfloat16>(a, p.workers, p.grads_dtype, s)
-                               : weight_grad<__half>(a, p.workers, p.grads_dtype, s);
+    if (p.dtype == GAR_BF16)
+        return tma_a ? launch_by_grads<__nv_bfloat16, true>(p.grads_dtype, a, map_dy, map_q, sm_count, s)
+                     : launch_by_grads<__nv_bfloat16, false>(p.grads_dtype, a, map_dy, map_q, sm_count, s);
+    return tma_a ? launch_by_grads<__half, true>(p.grads_dtype, a, map_dy, map_q, sm_count, s)
+                 : launch_by_grads<__half, false>(p.grads_dtype, a, map_dy, map_q, sm_count, s);
 }
 
 }  // namespace worker

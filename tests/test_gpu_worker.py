@@ -287,7 +287,7 @@ def codes_32(x, group):
             top = np.abs(v).max(axis=1)
             sound = np.isfinite(v).all(axis=1)
             live = sound & (top >= np.float32(2.0 ** -100))
-            inv = np.where(live, np.float32(127.0) / np.where(live, top, np.float32(1.0)), np.float32(0.0)).astype(np.float32)
+            inv = np.where(live, (np.float32(1.0) / np.where(live, top, np.float32(1.0))) * np.float32(127.0), np.float32(0.0)).astype(np.float32)
             s[:, g] = np.where(sound, np.where(live, top / np.float32(127.0), np.float32(0.0)), np.float32(np.nan))
             prod = np.where(sound[:, None], np.where(sound[:, None], v, np.float32(0.0)) * inv[:, None], np.float32(0.0))
             q[:, g * group:(g + 1) * group] = np.rint(prod).astype(np.int8)
