@@ -6,14 +6,21 @@
 // runs over tokens, which are the ROWS of both matrices: both operands are "MN-major" (the output
 // dimension is the contiguous one), which the tensor core takes as they lie, no transpose.
 //
-// One persistent CTA per SM, tiles of 128 outputs x 256 inputs of one worker, 64 tokens a step:
-//   TMA warp       dy: two 64-column boxes per step, 128-byte swizzle, straight into the operand
-//                  layout; codes: one 256-byte wide box.  The tensor maps are three-dimensional
+// Pairs of CTAs (clusters of two, one CTA per SM) take tiles of 256 outputs x 256 inputs of one
+// worker, 64 tokens a step, with the paired instruction (cta_group::2): each CTA holds 128 of the
+// outputs of dy and restores 128 of the inputs, and its tensor memory gets its own 128 rows of the
+// tile.  One CTA alone (128 x 256, restoring all 256 columns) moves 128 KB through its shared memory
+// per step, 1024 cycles against the 512 of the products; the pair halves the operand reads and the
+// restored bytes per CTA: 80 KB.
+//   dy warp, codes warp   TMA.  dy: two 64-column boxes per step, 128-byte swizzle, straight into the
+//                  operand layout; codes: one box of 128 bytes.  The tensor maps are three-dimensional
 //                  (columns, tokens, workers): what lies past a worker's tokens arrives as zeros and
 //                  no other worker's rows are read.
-//   restore warps  eight: codes -> 16-bit values (byte permute into fp32, subtract, multiply by the
-//                  row group's scale, one rounding) -> operand tile in shared memory, same layout
-//   MMA warp       one lane, four 128 x 256 x 16 instructions per step
+//   restore warps  two groups of four take steps in turn: codes -> 16-bit values (byte permute into
+//                  fp32, subtract, multiply by the row group's scale, one rounding) -> operand tile in
+//                  shared memory, same layout; they also see dy's copy land and then tell the
+//                  leading CTA's MMA warp
+//   MMA warp       of the leading CTA, one lane: four 256 x 256 x 16 instructions per step
 //   store warps    four: tensor memory -> shared memory -> coalesced stores, while the next tile's
 //                  products run into the other half of tensor memory
 // The bias is one more column tile whose second operand is a block of ones.
@@ -29,26 +36,29 @@ namespace gar {
 namespace worker {
 namespace {
 
-constexpr int WG_M = 128, WG_N = 256, WG_K = 64;      // tile and tokens per step
-constexpr int WG_STAGES = 3;
+constexpr int WG_M = 128, WG_N = 256, WG_K = 64;      // rows of a CTA, columns of a pair, tokens per step
+constexpr int WG_HALF = WG_N / 2;                     // columns a CTA restores
+// Buffers in flight: dy's copies and the codes' run on their own ahead of the restored tiles, so that
+// the latency of a copy (about 1.3 us under load) is not part of a restored tile's round.
+constexpr int WG_A_RING = 6, WG_Q_RING = 6, WG_B_RING = 4;
 constexpr int WG_THREADS = 512;
-constexpr int WG_TMA_WARP = 0, WG_MMA_WARP = 1, WG_ALLOC_WARP = 2;
+constexpr int WG_DY_WARP = 0, WG_MMA_WARP = 1, WG_ALLOC_WARP = 2, WG_CODES_WARP = 3;
 constexpr int WG_STORE_WARP0 = 4;                     // 4..7: tensor-memory lanes 32 (warp % 4) ..
-constexpr int WG_RESTORE_WARP0 = 8, WG_RESTORE_WARPS = 8;
+constexpr int WG_RESTORE_WARP0 = 8, WG_RESTORE_GROUP = 4;    // 8..11 take even steps, 12..15 odd ones
 constexpr int WG_BLOCK = 64 * 128;                    // bytes of 64 tokens x 64 columns of an operand
-constexpr int WG_A_BYTES = WG_M / 64 * WG_BLOCK, WG_B_BYTES = WG_N / 64 * WG_BLOCK, WG_Q_BYTES = WG_K * WG_N;
-constexpr int WG_PAD = 36;                            // floats per staged row of the store warps
-constexpr int WG_GROUP_M = 8;                         // row tiles that go round a column tile together
+constexpr int WG_A_BYTES = WG_M / 64 * WG_BLOCK, WG_B_BYTES = WG_HALF / 64 * WG_BLOCK, WG_Q_BYTES = WG_K * WG_HALF;
+constexpr int WG_GROUP_M = 8;                         // (pair) row tiles that go round a column tile together
 constexpr int WG_BIAS_N = 16;
 
 struct __align__(1024) WGSmem {
-    uint8_t a[WG_STAGES][WG_A_BYTES];
-    uint8_t b[WG_STAGES][WG_B_BYTES];
-    uint8_t q[WG_STAGES][WG_Q_BYTES];
-    float   out[4][32 * WG_PAD];
-    alignas(1024) uint16_t ones[512];
-    unsigned long long a_full[WG_STAGES], q_full[WG_STAGES], q_empty[WG_STAGES], b_full[WG_STAGES], empty[WG_STAGES];
-    unsigned long long acc_full[2], acc_empty[2];
+    uint8_t  a[WG_A_RING][WG_A_BYTES];
+    uint8_t  b[WG_B_RING][WG_B_BYTES];
+    uint8_t  q[WG_Q_RING][WG_Q_BYTES];
+    float    out[4][32 * 32];                             // a store warp's 32 x 32 piece of the tile
+    uint16_t ones[512];
+    unsigned long long a_full[WG_A_RING], a_empty[WG_A_RING], q_full[WG_Q_RING], q_empty[WG_Q_RING], b_empty[WG_B_RING];
+    unsigned long long acc_full[2];
+    unsigned long long full[WG_B_RING], acc_empty[2];     // the leading CTA's are used: both CTAs arrive there
     unsigned tmem_base;
     int      error;
 };
@@ -60,7 +70,7 @@ struct WGArgs {
     void *         dw, *db;
     int64_t        tokens, out, in, ld_dy, ld_grads;
     int            workers, groups, group_shift;
-    int            mt, nt;                // row tiles, column tiles (the bias tile, if any, is one more)
+    int            mt, nt;                // pair row tiles, column tiles (the bias tile, if any, is one more)
     int            columns;               // nt + 1 with a bias
     int            wide;                  // rows of the result start on 16 bytes
 };
@@ -81,15 +91,38 @@ __device__ __forceinline__ unsigned long long operand_desc(unsigned saddr, unsig
 // binary16 (0) at bits 7 and 10, both MN-major (bits 15, 16), N / 8 at bit 17, M / 16 at bit 24.
 __host__ __device__ constexpr unsigned instruction_desc(int type, int n) {
     return (1u << 4) | (unsigned(type) << 7) | (unsigned(type) << 10) | (1u << 15) | (1u << 16) | (unsigned(n >> 3) << 17) |
-           (unsigned(WG_M >> 4) << 24);
+           (unsigned(2 * WG_M >> 4) << 24);
 }
 __device__ __forceinline__ void mma_f16(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// arrives on the barrier of both CTAs once the instructions issued so far have finished
 __device__ __forceinline__ void mma_commit(unsigned long long* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(kb_smem_u32(bar)) : "memory");
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(kb_smem_u32(bar)), "h"(static_cast<unsigned short>(3)) : "memory");
+}
+// ---- the pair -------------------------------------------------------------------------------------
+__device__ __forceinline__ unsigned cta_rank() {
+    unsigned r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void pair_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// this CTA's shared-memory address in CTA `rank` of the pair
+__device__ __forceinline__ unsigned pair_address(unsigned addr, unsigned rank) {
+    unsigned r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+// What is handed over lies in this CTA's own shared or tensor memory and is read by the tensor core
+// (async proxy, after this CTA's own proxy or tcgen05 fence), so the arrival orders nothing at cluster
+// scope: .release.cluster here waits for every load and store the warp has in flight, 1500 cycles a step.
+__device__ __forceinline__ void arrive_at_leader(unsigned long long* bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(pair_address(kb_smem_u32(bar), 0)) : "memory");
 }
 // this thread's lane of tensor memory, 32 consecutive columns
 __device__ __forceinline__ void tmem_ld32(unsigned taddr, float (&v)[32]) {
@@ -174,20 +207,20 @@ template <> __device__ __forceinline__ void put4(__half* p, const float4& v) {
     __stcs(reinterpret_cast<uint2*>(p), make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b)));
 }
 
-// dy by plain loads into the operand layout (rows that do not start on 16 bytes): warp `w` of the
-// restore warps fills tokens 8 w .. 8 w + 7.
+// dy by plain loads into the operand layout (rows that do not start on 16 bytes): warp `w` of a
+// group of restore warps fills tokens 16 w .. 16 w + 15.
 template <typename T>
-__device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int step, uint8_t* tile, int w, int lane) {
+__device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t o0, int step, uint8_t* tile, int w, int lane) {
     const unsigned short* dy = static_cast<const unsigned short*>(a.dy);
 #pragma unroll 2
-    for (int k = 0; k < 8; ++k) {
-        const int row = 8 * w + k;
+    for (int k = 0; k < 16; ++k) {
+        const int row = 16 * w + k;
         const int64_t token = int64_t(step) * WG_K + row;
         const unsigned short* src = dy + (int64_t(t.worker) * a.tokens + token) * a.ld_dy;
 #pragma unroll
         for (int i = 0; i < WG_M / 32; ++i) {
             const int c = lane + 32 * i;
-            const int64_t o = int64_t(t.m) * WG_M + c;
+            const int64_t o = o0 + c;
             const unsigned short v = token < t.len && o < a.out ? __ldg(src + o) : static_cast<unsigned short>(0);
             const int at = (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4) + (c % 8) * 2;
             *reinterpret_cast<unsigned short*>(tile + at) = v;
@@ -203,73 +236,87 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
     WGSmem& sm = *reinterpret_cast<WGSmem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     volatile int* error = &sm.error;
+    const unsigned rank = cta_rank();
+    const int64_t pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     if (tid == 0) {
         sm.error = 0;
-        for (int s = 0; s < WG_STAGES; ++s) {
-            kb_init(&sm.a_full[s], 1);
-            kb_init(&sm.q_full[s], 1);
-            kb_init(&sm.q_empty[s], WG_RESTORE_WARPS);
-            kb_init(&sm.b_full[s], WG_RESTORE_WARPS);
-            kb_init(&sm.empty[s], 1);
+        for (int k = 0; k < WG_A_RING; ++k) {
+            kb_init(&sm.a_full[k], 1);
+            kb_init(&sm.a_empty[k], 1);
+        }
+        for (int k = 0; k < WG_Q_RING; ++k) {
+            kb_init(&sm.q_full[k], 1);
+            kb_init(&sm.q_empty[k], WG_RESTORE_GROUP);
+        }
+        for (int k = 0; k < WG_B_RING; ++k) {
+            kb_init(&sm.full[k], 2 * WG_RESTORE_GROUP);
+            kb_init(&sm.b_empty[k], 1);
         }
         for (int b = 0; b < 2; ++b) {
             kb_init(&sm.acc_full[b], 1);
-            kb_init(&sm.acc_empty[b], 4);
+            kb_init(&sm.acc_empty[b], 8);
         }
         kb_fence_init();
     }
     for (int i = tid; i < 512; i += WG_THREADS) sm.ones[i] = std::is_same<T, __half>::value ? 0x3c00 : 0x3f80;
     fence_async_smem();
     if (warp == WG_ALLOC_WARP) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kb_smem_u32(&sm.tmem_base)), "r"(512u) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kb_smem_u32(&sm.tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
+    pair_sync();                              // the other CTA's barriers are initialised
     tc_fence_after();
     const unsigned tmem = sm.tmem_base;
     const int64_t tiles = tile_count(a);
 
-    if (warp == WG_TMA_WARP) {
-        if (lane == 0) {
-            Ring ra, rq;
+    if (warp == WG_DY_WARP) {
+        if (TMA_A && lane == 0) {
+            Ring ra;
             bool ok = true;
-            for (int64_t i = blockIdx.x; ok && i < tiles; i += gridDim.x) {
+            for (int64_t i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
+                const int o0 = (2 * t.m + int(rank)) * WG_M;
                 for (int s = 0; s < t.steps; ++s) {
-                    if (t.n < a.nt) {
-                        if (!kb_wait(kb_smem_u32(&sm.q_empty[rq.slot]), rq.parity ^ 1u, error)) { ok = false; break; }
-                        const unsigned bar = kb_smem_u32(&sm.q_full[rq.slot]);
-                        kb_expect_tx(bar, WG_Q_BYTES);
-                        tma_load(kb_smem_u32(sm.q[rq.slot]), &map_q, t.n * WG_N, s * WG_K, t.worker, bar);
-                        rq.next(WG_STAGES);
-                    }
-                    if (TMA_A) {
-                        if (!kb_wait(kb_smem_u32(&sm.empty[ra.slot]), ra.parity ^ 1u, error)) { ok = false; break; }
-                        const unsigned bar = kb_smem_u32(&sm.a_full[ra.slot]), dst = kb_smem_u32(sm.a[ra.slot]);
-                        kb_expect_tx(bar, WG_A_BYTES);
-                        tma_load(dst, &map_dy, t.m * WG_M, s * WG_K, t.worker, bar);
-                        tma_load(dst + WG_BLOCK, &map_dy, t.m * WG_M + 64, s * WG_K, t.worker, bar);
-                        ra.next(WG_STAGES);
-                    }
+                    if (!kb_wait(kb_smem_u32(&sm.a_empty[ra.slot]), ra.parity ^ 1u, error)) { ok = false; break; }
+                    const unsigned bar = kb_smem_u32(&sm.a_full[ra.slot]), dst = kb_smem_u32(sm.a[ra.slot]);
+                    kb_expect_tx(bar, WG_A_BYTES);
+                    tma_load(dst, &map_dy, o0, s * WG_K, t.worker, bar);
+                    tma_load(dst + WG_BLOCK, &map_dy, o0 + 64, s * WG_K, t.worker, bar);
+                    ra.next(WG_A_RING);
                 }
             }
-            if (!ok) {
-                // the copies in flight land before the CTA's shared memory is given back
-                for (int k = 0; k < WG_STAGES; ++k) {
-                    // the slot's latest copy completed the phase before the ring's position
-                    kb_wait(kb_smem_u32(&sm.q_full[k]), k < rq.slot ? rq.parity : rq.parity ^ 1u, error, true, 1u << 10);
-                    if (TMA_A) kb_wait(kb_smem_u32(&sm.a_full[k]), k < ra.slot ? ra.parity : ra.parity ^ 1u, error, true, 1u << 10);
+            // after a wait that gave up: the copies in flight land before the CTA's shared memory is given
+            // back (a slot's latest copy completed the phase before the ring's position)
+            for (int k = 0; !ok && k < WG_A_RING; ++k)
+                kb_wait(kb_smem_u32(&sm.a_full[k]), k < ra.slot ? ra.parity : ra.parity ^ 1u, error, true, 1u << 10);
+        }
+    } else if (warp == WG_CODES_WARP) {
+        if (lane == 0) {
+            Ring rq;
+            bool ok = true;
+            for (int64_t i = pair; ok && i < tiles; i += pairs) {
+                const Tile t = tile_at(a, i);
+                if (t.n == a.nt) continue;
+                for (int s = 0; s < t.steps; ++s) {
+                    if (!kb_wait(kb_smem_u32(&sm.q_empty[rq.slot]), rq.parity ^ 1u, error)) { ok = false; break; }
+                    const unsigned bar = kb_smem_u32(&sm.q_full[rq.slot]);
+                    kb_expect_tx(bar, WG_Q_BYTES);
+                    tma_load(kb_smem_u32(sm.q[rq.slot]), &map_q, t.n * WG_N + int(rank) * WG_HALF, s * WG_K, t.worker, bar);
+                    rq.next(WG_Q_RING);
                 }
             }
+            for (int k = 0; !ok && k < WG_Q_RING; ++k)
+                kb_wait(kb_smem_u32(&sm.q_full[k]), k < rq.slot ? rq.parity : rq.parity ^ 1u, error, true, 1u << 10);
         }
     } else if (warp == WG_MMA_WARP) {
-        if (lane == 0) {
-            Ring r, acc;
+        if (lane == 0 && rank == 0) {
+            Ring ra, rb, acc;
             bool ok = true;
             const unsigned idesc = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, WG_N);
             const unsigned idesc_bias = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, WG_BIAS_N);
-            for (int64_t i = blockIdx.x; ok && i < tiles; i += gridDim.x) {
+            for (int64_t i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
                 if (t.steps == 0) continue;
                 if (!kb_wait(kb_smem_u32(&sm.acc_empty[acc.slot]), acc.parity ^ 1u, error)) { ok = false; break; }
@@ -277,10 +324,9 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
                 const unsigned d = tmem + unsigned(acc.slot) * WG_N;
                 const bool bias = t.n == a.nt;
                 for (int s = 0; s < t.steps; ++s) {
-                    if (TMA_A && !kb_wait(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error)) { ok = false; break; }
-                    if (!kb_wait(kb_smem_u32(&sm.b_full[r.slot]), r.parity, error)) { ok = false; break; }
+                    if (!kb_wait(kb_smem_u32(&sm.full[rb.slot]), rb.parity, error)) { ok = false; break; }
                     tc_fence_after();
-                    const unsigned sa = kb_smem_u32(sm.a[r.slot]), sb = kb_smem_u32(sm.b[r.slot]);
+                    const unsigned sa = kb_smem_u32(sm.a[ra.slot]), sb = kb_smem_u32(sm.b[rb.slot]);
 #pragma unroll
                     for (int k = 0; k < WG_K / 16; ++k) {
                         const unsigned long long da = operand_desc(sa + k * 2048, WG_BLOCK, 1024, 2);
@@ -289,8 +335,10 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
                                                            : operand_desc(sb + k * 2048, WG_BLOCK, 1024, 2);
                         mma_f16(d, da, db, bias ? idesc_bias : idesc, s > 0 || k > 0);
                     }
-                    mma_commit(&sm.empty[r.slot]);
-                    r.next(WG_STAGES);
+                    mma_commit(&sm.a_empty[ra.slot]);
+                    mma_commit(&sm.b_empty[rb.slot]);
+                    ra.next(WG_A_RING);
+                    rb.next(WG_B_RING);
                 }
                 if (ok) {
                     mma_commit(&sm.acc_full[acc.slot]);
@@ -305,77 +353,84 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
             }
         }
     } else if (warp >= WG_RESTORE_WARP0) {
-        const int w = warp - WG_RESTORE_WARP0, tl = lane & 7, sub = lane >> 3;
-        Ring r, rq;
+        const int w = (warp - WG_RESTORE_WARP0) % WG_RESTORE_GROUP, tl = lane & 7, sub = lane >> 3;
+        const unsigned mine = unsigned(warp - WG_RESTORE_WARP0) / WG_RESTORE_GROUP;
+        unsigned turn = 0;                                        // steps so far, over all tiles
+        Ring ra, rb, rq;
         bool ok = true;
-        for (int64_t i = blockIdx.x; ok && i < tiles; i += gridDim.x) {
+        for (int64_t i = pair; ok && i < tiles; i += pairs) {
             const Tile t = tile_at(a, i);
             const bool bias = t.n == a.nt;
-            const int row = 8 * w + tl;                           // this lane's token of a step
+            const int row = 16 * w + tl;                          // this lane's tokens of a step: row and row + 8
             const int64_t base = int64_t(t.worker) * a.tokens;
-            // the lane's four 16-column pieces of the row: a diagonal over the eight lanes of a phase, so
-            // that neither the reads of the codes nor the swizzled stores meet in a bank
-            int piece[4];
-            int64_t group[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                piece[k] = ((tl + sub + 4 * (k & 1)) & 7) + 8 * (k >> 1);
-                group[k] = (int64_t(t.n) * WG_N + piece[k] * 16) >> a.group_shift;
-            }
+            // the lane's two 16-column pieces of a row: a diagonal over the eight lanes of a phase, so that
+            // neither the reads of the codes nor the swizzled stores meet in a bank
+            const int piece[2] = {(tl + sub) & 7, (tl + sub + 4) & 7};
+            const int64_t c0 = int64_t(t.n) * WG_N + rank * WG_HALF;
             float next[4];
             auto fetch_scales = [&](int s) {
-                const int64_t token = int64_t(s) * WG_K + row;
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    next[k] = !bias && token < t.len && group[k] < a.groups ? __ldg(a.scales + (base + token) * a.groups + group[k]) : 0.f;
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t token = int64_t(s) * WG_K + row + 8 * (k >> 1), group = (c0 + piece[k & 1] * 16) >> a.group_shift;
+                    next[k] = !bias && token < t.len && group < a.groups ? __ldg(a.scales + (base + token) * a.groups + group) : 0.f;
+                }
             };
-            if (t.steps) fetch_scales(0);
-            for (int s = 0; s < t.steps; ++s) {
-                float scale[4];
+            const int first = int((turn ^ mine) & 1u);            // this group's first step of the tile
+            if (first < t.steps) fetch_scales(first);
+            for (int s = 0; s < t.steps; ++s, ++turn) {
+                if (((turn ^ mine) & 1u) == 0) {
+                    float scale[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) scale[k] = next[k];
-                if (s + 1 < t.steps) fetch_scales(s + 1);
-                if (!kb_wait_warp(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
-                if (!bias) {
-                    if (!kb_wait_warp(kb_smem_u32(&sm.q_full[rq.slot]), rq.parity, error)) { ok = false; break; }
-                    const uint8_t* q = sm.q[rq.slot];
-                    uint8_t* b = sm.b[r.slot];
+                    for (int k = 0; k < 4; ++k) scale[k] = next[k];
+                    if (s + 2 < t.steps) fetch_scales(s + 2);
+                    if (!kb_wait_warp(kb_smem_u32(&sm.b_empty[rb.slot]), rb.parity ^ 1u, error)) { ok = false; break; }
+                    if (!bias) {
+                        if (!kb_wait_warp(kb_smem_u32(&sm.q_full[rq.slot]), rq.parity, error)) { ok = false; break; }
+                        const uint8_t* q = sm.q[rq.slot] + row * WG_HALF;
+                        uint8_t* b = sm.b[rb.slot] + row * 128;
+                        uint4 c[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint4 c = *reinterpret_cast<const uint4*>(q + row * WG_N + piece[k] * 16);
-                        const unsigned words[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
-                        const f32x2 sc = pack2(scale[k], scale[k]);
-                        unsigned v[8];
+                        for (int k = 0; k < 4; ++k) c[k] = *reinterpret_cast<const uint4*>(q + (k >> 1) * 8 * WG_HALF + piece[k & 1] * 16);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            v[2 * j] = restore_pair<T>(words[j], 0x7440, 0x7441, sc);
-                            v[2 * j + 1] = restore_pair<T>(words[j], 0x7442, 0x7443, sc);
+                        for (int k = 0; k < 4; ++k) {
+                            const unsigned words[4] = {c[k].x ^ 0x80808080u, c[k].y ^ 0x80808080u, c[k].z ^ 0x80808080u, c[k].w ^ 0x80808080u};
+                            const f32x2 sc = pack2(scale[k], scale[k]);
+                            unsigned v[8];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                v[2 * j] = restore_pair<T>(words[j], 0x7440, 0x7441, sc);
+                                v[2 * j + 1] = restore_pair<T>(words[j], 0x7442, 0x7443, sc);
+                            }
+                            uint8_t* dst = b + (k >> 1) * 1024 + (piece[k & 1] >> 2) * WG_BLOCK;
+                            const int chunk = (piece[k & 1] & 3) * 2;
+                            *reinterpret_cast<uint4*>(dst + ((chunk ^ tl) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                            *reinterpret_cast<uint4*>(dst + (((chunk + 1) ^ tl) << 4)) = make_uint4(v[4], v[5], v[6], v[7]);
                         }
-                        uint8_t* dst = b + (piece[k] >> 2) * WG_BLOCK + row * 128;
-                        const int chunk = (piece[k] & 3) * 2;
-                        *reinterpret_cast<uint4*>(dst + ((chunk ^ tl) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
-                        *reinterpret_cast<uint4*>(dst + (((chunk + 1) ^ tl) << 4)) = make_uint4(v[4], v[5], v[6], v[7]);
+                    }
+                    if (!TMA_A) {
+                        if (!kb_wait_warp(kb_smem_u32(&sm.a_empty[ra.slot]), ra.parity ^ 1u, error)) { ok = false; break; }
+                        load_dy<T>(a, t, int64_t(2 * t.m + int(rank)) * WG_M, s, sm.a[ra.slot], w, lane);
+                    } else {
+                        if (!kb_wait_warp(kb_smem_u32(&sm.a_full[ra.slot]), ra.parity, error)) { ok = false; break; }
+                        if (a.lengths && int64_t(s + 1) * WG_K > t.len) {
+                            // tokens behind the worker's length: zeros in place of what the copy brought
+                            for (int k = 0; k < 16; ++k) {
+                                const int rr = 16 * w + k;
+                                if (int64_t(s) * WG_K + rr >= t.len && lane < WG_A_BYTES / WG_BLOCK * 8)
+                                    *reinterpret_cast<uint4*>(sm.a[ra.slot] + (lane / 8) * WG_BLOCK + rr * 128 + (lane % 8) * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                        }
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        arrive_at_leader(&sm.full[rb.slot]);
+                        if (!bias) kb_arrive(&sm.q_empty[rq.slot]);
                     }
                 }
-                if (!TMA_A) {
-                    load_dy<T>(a, t, s, sm.a[r.slot], w, lane);
-                } else if (a.lengths && int64_t(s + 1) * WG_K > t.len) {
-                    // tokens behind the worker's length: zeros in place of what the copy brought
-                    if (!kb_wait_warp(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error)) { ok = false; break; }
-                    for (int k = 0; k < 8; ++k) {
-                        const int rr = 8 * w + k;
-                        if (int64_t(s) * WG_K + rr >= t.len && lane < WG_A_BYTES / WG_BLOCK * 8)
-                            *reinterpret_cast<uint4*>(sm.a[r.slot] + (lane / 8) * WG_BLOCK + rr * 128 + (lane % 8) * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    kb_arrive(&sm.b_full[r.slot]);
-                    if (!bias) kb_arrive(&sm.q_empty[rq.slot]);
-                }
-                r.next(WG_STAGES);
-                if (!bias) rq.next(WG_STAGES);
+                ra.next(WG_A_RING);
+                rb.next(WG_B_RING);
+                if (!bias) rq.next(WG_Q_RING);
             }
         }
     } else if (warp >= WG_STORE_WARP0) {
@@ -383,9 +438,9 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
         float* stage = sm.out[quarter];
         Ring acc;
         bool ok = true;
-        for (int64_t i = blockIdx.x; ok && i < tiles; i += gridDim.x) {
+        for (int64_t i = pair; ok && i < tiles; i += pairs) {
             const Tile t = tile_at(a, i);
-            const int64_t o0 = int64_t(t.m) * WG_M + quarter * 32;
+            const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M + quarter * 32;
             const unsigned src = tmem + unsigned(acc.slot) * WG_N + (unsigned(quarter * 32) << 16);
             if (t.steps) {
                 if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error)) { ok = false; break; }
@@ -412,25 +467,27 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
                     }
                     __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4)
-                        *reinterpret_cast<float4*>(stage + lane * WG_PAD + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    for (int j = 0; j < 8; ++j)                  // four columns each, in an order that meets in no bank
+                        *reinterpret_cast<float4*>(stage + lane * 32 + ((j ^ (lane & 7)) << 2)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                     __syncwarp();
                     if (a.wide && cols - c0 >= 32) {
-                        const int c = (lane % 8) * 4;
+                        const int j = lane % 8;
 #pragma unroll
                         for (int rr = 0; rr < 32; rr += 4) {
                             const int row = rr + lane / 8;
-                            if (row < rows) put4(dw + int64_t(row) * a.in + c0 + c, *reinterpret_cast<const float4*>(stage + row * WG_PAD + c));
+                            if (row < rows)
+                                put4(dw + int64_t(row) * a.in + c0 + 4 * j, *reinterpret_cast<const float4*>(stage + row * 32 + ((j ^ (row & 7)) << 2)));
                         }
                     } else if (lane < cols - c0) {
-                        for (int row = 0; row < rows; ++row) dw[int64_t(row) * a.in + c0 + lane] = Elem<G>::narrow(stage[row * WG_PAD + lane]);
+                        for (int row = 0; row < rows; ++row)
+                            dw[int64_t(row) * a.in + c0 + lane] = Elem<G>::narrow(stage[row * 32 + (((lane >> 2) ^ (row & 7)) << 2) + (lane & 3)]);
                     }
                 }
             }
             if (t.steps) {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) kb_arrive(&sm.acc_empty[acc.slot]);
+                if (lane == 0) arrive_at_leader(&sm.acc_empty[acc.slot]);
                 acc.next(2);
             }
         }
@@ -438,15 +495,19 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    pair_sync();                              // the other CTA's products and arrivals have ended too
     tc_fence_after();
     if (warp == WG_ALLOC_WARP)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
-    if (sm.error) {
-        // a wait gave up: nothing this CTA was to write may look like a gradient
-        for (int64_t i = blockIdx.x; i < tiles; i += gridDim.x) {
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    int other;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(other) : "r"(pair_address(kb_smem_u32(&sm.error), rank ^ 1u)) : "memory");
+    pair_sync();                              // read before either CTA ends
+    if (sm.error || other) {
+        // a wait gave up: nothing the pair was to write may look like a gradient
+        for (int64_t i = pair; i < tiles; i += pairs) {
             const Tile t = tile_at(a, i);
             for (int e = tid; e < WG_M * WG_N; e += WG_THREADS) {
-                const int64_t o = int64_t(t.m) * WG_M + e / WG_N, c = int64_t(t.n) * WG_N + e % WG_N;
+                const int64_t o = int64_t(2 * t.m + int(rank)) * WG_M + e / WG_N, c = int64_t(t.n) * WG_N + e % WG_N;
                 if (o >= a.out) continue;
                 if (t.n == a.nt) {
                     if (e % WG_N == 0) static_cast<G*>(a.db)[int64_t(t.worker) * a.ld_grads + o] = Elem<G>::narrow(CUDART_NAN_F);
@@ -491,12 +552,23 @@ cudaError_t make_map(CUtensorMap* map, CUtensorMapDataType type, const void* bas
 template <typename T, typename G, bool TMA_A>
 cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_q, int sm_count, cudaStream_t stream) {
     constexpr int bytes = int(sizeof(WGSmem)) + 1024;
+    static_assert(bytes <= 232448, "a CTA's shared memory");
     auto kernel = weight_grad_kernel<T, G, TMA_A>;
     if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
     const int64_t tiles = int64_t(a.workers) * a.mt * a.columns;
-    const unsigned grid = unsigned(tiles < sm_count ? tiles : sm_count);
-    kernel<<<grid, WG_THREADS, bytes, stream>>>(a, map_dy, map_q);
-    return cudaGetLastError();
+    const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(2 * (tiles < pairs ? tiles : pairs)));
+    cfg.blockDim = dim3(WG_THREADS);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a, map_dy, map_q);
 }
 template <typename T, bool TMA_A>
 cudaError_t launch_by_grads(int grads_dtype, const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_q, int sm_count,
@@ -523,7 +595,7 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     a.workers = p.workers;
     a.groups = int((p.in_features + p.group - 1) / p.group);
     a.group_shift = p.group == 32 ? 5 : p.group == 64 ? 6 : 7;
-    a.mt = int((p.out_features + WG_M - 1) / WG_M);
+    a.mt = int((p.out_features + 2 * WG_M - 1) / (2 * WG_M));
     a.nt = int((p.in_features + WG_N - 1) / WG_N);
     a.columns = a.nt + (p.bias_grads ? 1 : 0);
     if (int64_t(a.mt) * a.columns >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
@@ -534,7 +606,7 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
 
     CUtensorMap map_q, map_dy;
     if (cudaError_t err = make_map(&map_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.x_saved.q, p.in_features, p.tokens, p.workers,
-                                   p.x_saved.ldq, WG_N, CU_TENSOR_MAP_SWIZZLE_NONE)) return err;
+                                   p.x_saved.ldq, WG_HALF, CU_TENSOR_MAP_SWIZZLE_NONE)) return err;
     // TMA needs rows of dy that start on 16 bytes
     const bool tma_a = reinterpret_cast<uintptr_t>(p.dy) % 16 == 0 && ld_dy % 8 == 0;
     if (tma_a) {
