@@ -16,10 +16,9 @@
 //                  operand layout; codes: one box of 128 bytes.  The tensor maps are three-dimensional
 //                  (columns, tokens, workers): what lies past a worker's tokens arrives as zeros and
 //                  no other worker's rows are read.
-//   restore warps  two groups of four take steps in turn: codes -> 16-bit values (byte permute into
+//   restore warps  three groups of four take steps in turn: codes -> 16-bit values (byte permute into
 //                  fp32, subtract, multiply by the row group's scale, one rounding) -> operand tile in
-//                  shared memory, same layout; they also see dy's copy land and then tell the
-//                  leading CTA's MMA warp
+//                  shared memory, same layout
 //   MMA warp       of the leading CTA, one lane: four 256 x 256 x 16 instructions per step
 //   store warps    four: tensor memory -> shared memory -> coalesced stores, while the next tile's
 //                  products run into the other half of tensor memory
@@ -38,27 +37,27 @@ namespace {
 
 constexpr int WG_M = 128, WG_N = 256, WG_K = 64;      // rows of a CTA, columns of a pair, tokens per step
 constexpr int WG_HALF = WG_N / 2;                     // columns a CTA restores
-// Buffers in flight: dy's copies and the codes' run on their own ahead of the restored tiles, so that
-// the latency of a copy (about 1.3 us under load) is not part of a restored tile's round.
-constexpr int WG_A_RING = 6, WG_Q_RING = 6, WG_B_RING = 4;
-constexpr int WG_THREADS = 512;
+// Steps in flight: operand tiles (dy's copy and the restored one share a slot), copies of the codes.
+constexpr int WG_RING = 5, WG_Q_RING = 6;
 constexpr int WG_DY_WARP = 0, WG_MMA_WARP = 1, WG_ALLOC_WARP = 2, WG_CODES_WARP = 3;
 constexpr int WG_STORE_WARP0 = 4;                     // 4..7: tensor-memory lanes 32 (warp % 4) ..
-constexpr int WG_RESTORE_WARP0 = 8, WG_RESTORE_GROUP = 4;    // 8..11 take even steps, 12..15 odd ones
+// Groups of four restore warps take steps in turn: a step takes a group about 1500 cycles from its slot
+// being free to the arrival (waits, reads, 220 instructions, fence), three times what the products take.
+constexpr int WG_RESTORE_WARP0 = 8, WG_GROUP_WARPS = 4, WG_GROUPS = 3;
+constexpr int WG_THREADS = 32 * (WG_RESTORE_WARP0 + WG_GROUP_WARPS * WG_GROUPS);
 constexpr int WG_BLOCK = 64 * 128;                    // bytes of 64 tokens x 64 columns of an operand
 constexpr int WG_A_BYTES = WG_M / 64 * WG_BLOCK, WG_B_BYTES = WG_HALF / 64 * WG_BLOCK, WG_Q_BYTES = WG_K * WG_HALF;
 constexpr int WG_GROUP_M = 8;                         // (pair) row tiles that go round a column tile together
 constexpr int WG_BIAS_N = 16;
 
 struct __align__(1024) WGSmem {
-    uint8_t  a[WG_A_RING][WG_A_BYTES];
-    uint8_t  b[WG_B_RING][WG_B_BYTES];
+    uint8_t  a[WG_RING][WG_A_BYTES];
+    uint8_t  b[WG_RING][WG_B_BYTES];
     uint8_t  q[WG_Q_RING][WG_Q_BYTES];
     float    out[4][32 * 32];                             // a store warp's 32 x 32 piece of the tile
     uint16_t ones[512];
-    unsigned long long a_full[WG_A_RING], a_empty[WG_A_RING], q_full[WG_Q_RING], q_empty[WG_Q_RING], b_empty[WG_B_RING];
-    unsigned long long acc_full[2];
-    unsigned long long full[WG_B_RING], acc_empty[2];     // the leading CTA's are used: both CTAs arrive there
+    unsigned long long empty[WG_RING], q_full[WG_Q_RING], q_empty[WG_Q_RING], acc_full[2];
+    unsigned long long a_full[WG_RING], b_full[WG_RING], acc_empty[2];     // the leading CTA's are used, for both
     unsigned tmem_base;
     int      error;
 };
@@ -103,6 +102,12 @@ __device__ __forceinline__ void mma_commit(unsigned long long* bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(kb_smem_u32(bar)), "h"(static_cast<unsigned short>(3)) : "memory");
 }
+// true in one lane of the warp
+__device__ __forceinline__ bool elect_one() {
+    unsigned r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 // ---- the pair -------------------------------------------------------------------------------------
 __device__ __forceinline__ unsigned cta_rank() {
     unsigned r;
@@ -142,6 +147,11 @@ __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, i
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+// into this CTA's shared memory, counted in on a barrier of either CTA of the pair
+__device__ __forceinline__ void tma_load_pair(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
 
 // ---- tiles --------------------------------------------------------------------------------------
 struct Tile {
@@ -169,16 +179,10 @@ __device__ __forceinline__ Tile tile_at(const WGArgs& a, int64_t index) {
 }
 __device__ __forceinline__ int64_t tile_count(const WGArgs& a) { return int64_t(a.workers) * a.mt * a.columns; }
 
-// Position in a ring of `depth` buffers and the parity of its round.
-struct Ring {
-    int slot = 0;
-    unsigned parity = 0;
-    __device__ __forceinline__ void next(int depth) {
-        if (++slot == depth) {
-            slot = 0;
-            parity ^= 1u;
-        }
-    }
+// Slot of a running number in a ring of DEPTH buffers, and the parity of the slot's round.
+template <int DEPTH> struct Ring {
+    unsigned slot, parity;
+    __device__ __forceinline__ explicit Ring(unsigned number) : slot(number % DEPTH), parity((number / DEPTH) & 1u) {}
 };
 
 // two codes' bytes of a word -> fp32 codes -> times the scale -> a pair of T
@@ -207,28 +211,53 @@ template <> __device__ __forceinline__ void put4(__half* p, const float4& v) {
     __stcs(reinterpret_cast<uint2*>(p), make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b)));
 }
 
-// dy by plain loads into the operand layout (rows that do not start on 16 bytes): warp `w` of a
-// group of restore warps fills tokens 16 w .. 16 w + 15.
-template <typename T>
+// dy by plain loads into the operand layout, zeros past the worker's tokens: warp `w` of a group of
+// restore warps fills tokens 16 w .. 16 w + 15.  VEC: rows start on 16 bytes.
+template <bool VEC>
 __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t o0, int step, uint8_t* tile, int w, int lane) {
     const unsigned short* dy = static_cast<const unsigned short*>(a.dy);
-#pragma unroll 2
-    for (int k = 0; k < 16; ++k) {
-        const int row = 16 * w + k;
-        const int64_t token = int64_t(step) * WG_K + row;
-        const unsigned short* src = dy + (int64_t(t.worker) * a.tokens + token) * a.ld_dy;
+    if (VEC) {
+        uint4 v[8];
+        const int c = (lane % 16) * 8;                    // eight columns of tokens 16 w + lane / 16, + 2, + 4, ..
+        const int64_t o = o0 + c;
 #pragma unroll
-        for (int i = 0; i < WG_M / 32; ++i) {
-            const int c = lane + 32 * i;
-            const int64_t o = o0 + c;
-            const unsigned short v = token < t.len && o < a.out ? __ldg(src + o) : static_cast<unsigned short>(0);
-            const int at = (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4) + (c % 8) * 2;
-            *reinterpret_cast<unsigned short*>(tile + at) = v;
+        for (int k = 0; k < 8; ++k) {
+            const int64_t token = int64_t(step) * WG_K + 16 * w + 2 * k + lane / 16;
+            const unsigned short* src = dy + (int64_t(t.worker) * a.tokens + token) * a.ld_dy + o;
+            v[k] = make_uint4(0, 0, 0, 0);
+            if (token < t.len && o + 8 <= a.out) {
+                v[k] = __ldg(reinterpret_cast<const uint4*>(src));
+            } else if (token < t.len && o < a.out) {
+                unsigned h[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] = o + j < a.out ? __ldg(src + j) : 0u;
+                v[k] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int row = 16 * w + 2 * k + lane / 16;
+            *reinterpret_cast<uint4*>(tile + (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4)) = v[k];
+        }
+    } else {
+#pragma unroll 2
+        for (int k = 0; k < 16; ++k) {
+            const int row = 16 * w + k;
+            const int64_t token = int64_t(step) * WG_K + row;
+            const unsigned short* src = dy + (int64_t(t.worker) * a.tokens + token) * a.ld_dy;
+#pragma unroll
+            for (int i = 0; i < WG_M / 32; ++i) {
+                const int c = lane + 32 * i;
+                const int64_t o = o0 + c;
+                const unsigned short v = token < t.len && o < a.out ? __ldg(src + o) : static_cast<unsigned short>(0);
+                *reinterpret_cast<unsigned short*>(tile + (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4) + (c % 8) * 2) = v;
+            }
         }
     }
 }
 
-// TMA_A: dy comes by TMA (else the restore warps load it).
+// TMA_A: dy comes by TMA, except a worker's last step where only some of its tokens count (the
+// restore warps load that one, and every step without TMA_A).
 template <typename T, typename G, bool TMA_A>
 __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs a, const __grid_constant__ CUtensorMap map_dy,
                                                                     const __grid_constant__ CUtensorMap map_q) {
@@ -240,17 +269,14 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
     const int64_t pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     if (tid == 0) {
         sm.error = 0;
-        for (int k = 0; k < WG_A_RING; ++k) {
+        for (int k = 0; k < WG_RING; ++k) {
+            kb_init(&sm.empty[k], 1);
             kb_init(&sm.a_full[k], 1);
-            kb_init(&sm.a_empty[k], 1);
+            kb_init(&sm.b_full[k], 2 * WG_GROUP_WARPS);
         }
         for (int k = 0; k < WG_Q_RING; ++k) {
             kb_init(&sm.q_full[k], 1);
-            kb_init(&sm.q_empty[k], WG_RESTORE_GROUP);
-        }
-        for (int k = 0; k < WG_B_RING; ++k) {
-            kb_init(&sm.full[k], 2 * WG_RESTORE_GROUP);
-            kb_init(&sm.b_empty[k], 1);
+            kb_init(&sm.q_empty[k], WG_GROUP_WARPS);
         }
         for (int b = 0; b < 2; ++b) {
             kb_init(&sm.acc_full[b], 1);
@@ -270,178 +296,201 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
     tc_fence_after();
     const unsigned tmem = sm.tmem_base;
     const int64_t tiles = tile_count(a);
+    // step s of a tile is number g + s of all the CTA's steps; of those with codes, number gq + s
+    unsigned g = 0, gq = 0;
+    bool ok = true;
 
     if (warp == WG_DY_WARP) {
         if (TMA_A && lane == 0) {
-            Ring ra;
-            bool ok = true;
+            const unsigned leader_full = pair_address(kb_smem_u32(sm.a_full), 0);
             for (int64_t i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
                 const int o0 = (2 * t.m + int(rank)) * WG_M;
-                for (int s = 0; s < t.steps; ++s) {
-                    if (!kb_wait(kb_smem_u32(&sm.a_empty[ra.slot]), ra.parity ^ 1u, error)) { ok = false; break; }
-                    const unsigned bar = kb_smem_u32(&sm.a_full[ra.slot]), dst = kb_smem_u32(sm.a[ra.slot]);
-                    kb_expect_tx(bar, WG_A_BYTES);
-                    tma_load(dst, &map_dy, o0, s * WG_K, t.worker, bar);
-                    tma_load(dst + WG_BLOCK, &map_dy, o0 + 64, s * WG_K, t.worker, bar);
-                    ra.next(WG_A_RING);
+                for (int s = 0; s < t.steps; ++s, ++g) {
+                    const Ring<WG_RING> r(g);
+                    if (!kb_wait(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
+                    if (a.lengths && int64_t(s + 1) * WG_K > t.len) {
+                        if (rank == 0) kb_arrive(&sm.a_full[r.slot]);
+                        continue;
+                    }
+                    if (rank == 0) kb_expect_tx(kb_smem_u32(&sm.a_full[r.slot]), 2 * WG_A_BYTES);
+                    const unsigned bar = leader_full + r.slot * 8, dst = kb_smem_u32(sm.a[r.slot]);
+                    tma_load_pair(dst, &map_dy, o0, s * WG_K, t.worker, bar);
+                    tma_load_pair(dst + WG_BLOCK, &map_dy, o0 + 64, s * WG_K, t.worker, bar);
                 }
             }
-            // after a wait that gave up: the copies in flight land before the CTA's shared memory is given
-            // back (a slot's latest copy completed the phase before the ring's position)
-            for (int k = 0; !ok && k < WG_A_RING; ++k)
-                kb_wait(kb_smem_u32(&sm.a_full[k]), k < ra.slot ? ra.parity : ra.parity ^ 1u, error, true, 1u << 10);
+            // after a wait that gave up: the copies in flight land (the leading CTA counts them in) before
+            // either CTA's shared memory is given back
+            for (unsigned k = 0; !ok && rank == 0 && k < WG_RING && k < g; ++k) {
+                const Ring<WG_RING> r(g - 1 - k);
+                kb_wait(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error, true, 1u << 10);
+            }
         }
     } else if (warp == WG_CODES_WARP) {
         if (lane == 0) {
-            Ring rq;
-            bool ok = true;
             for (int64_t i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
                 if (t.n == a.nt) continue;
-                for (int s = 0; s < t.steps; ++s) {
-                    if (!kb_wait(kb_smem_u32(&sm.q_empty[rq.slot]), rq.parity ^ 1u, error)) { ok = false; break; }
-                    const unsigned bar = kb_smem_u32(&sm.q_full[rq.slot]);
+                for (int s = 0; s < t.steps; ++s, ++gq) {
+                    const Ring<WG_Q_RING> r(gq);
+                    if (!kb_wait(kb_smem_u32(&sm.q_empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
+                    const unsigned bar = kb_smem_u32(&sm.q_full[r.slot]);
                     kb_expect_tx(bar, WG_Q_BYTES);
-                    tma_load(kb_smem_u32(sm.q[rq.slot]), &map_q, t.n * WG_N + int(rank) * WG_HALF, s * WG_K, t.worker, bar);
-                    rq.next(WG_Q_RING);
+                    tma_load(kb_smem_u32(sm.q[r.slot]), &map_q, t.n * WG_N + int(rank) * WG_HALF, s * WG_K, t.worker, bar);
                 }
             }
-            for (int k = 0; !ok && k < WG_Q_RING; ++k)
-                kb_wait(kb_smem_u32(&sm.q_full[k]), k < rq.slot ? rq.parity : rq.parity ^ 1u, error, true, 1u << 10);
+            for (unsigned k = 0; !ok && k < WG_Q_RING && k < gq; ++k) {
+                const Ring<WG_Q_RING> r(gq - 1 - k);
+                kb_wait(kb_smem_u32(&sm.q_full[r.slot]), r.parity, error, true, 1u << 10);
+            }
         }
     } else if (warp == WG_MMA_WARP) {
-        if (lane == 0 && rank == 0) {
-            Ring ra, rb, acc;
-            bool ok = true;
+        // The whole warp walks the loop and one elected lane issues: what the instructions take is then the
+        // same in every lane, and the compiler keeps it where they read it from.
+        if (rank == 0) {
             const unsigned idesc = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, WG_N);
             const unsigned idesc_bias = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, WG_BIAS_N);
+            const unsigned long long desc_a = operand_desc(kb_smem_u32(sm.a), WG_BLOCK, 1024, 2);
+            const unsigned long long desc_b = operand_desc(kb_smem_u32(sm.b), WG_BLOCK, 1024, 2);
+            // a block of ones needs no layout: every address the descriptor reaches holds 1
+            const unsigned long long desc_ones = operand_desc(kb_smem_u32(sm.ones), 256, 256, 0);
+            unsigned n_acc = 0;
             for (int64_t i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
-                if (t.steps == 0) continue;
-                if (!kb_wait(kb_smem_u32(&sm.acc_empty[acc.slot]), acc.parity ^ 1u, error)) { ok = false; break; }
+                const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
+                if (steps == 0) continue;
+                const Ring<2> acc(n_acc);
+                if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[acc.slot]), acc.parity ^ 1u, error)) { ok = false; break; }
                 tc_fence_after();
-                const unsigned d = tmem + unsigned(acc.slot) * WG_N;
+                const unsigned d = tmem + acc.slot * WG_N;
                 const bool bias = t.n == a.nt;
-                for (int s = 0; s < t.steps; ++s) {
-                    if (!kb_wait(kb_smem_u32(&sm.full[rb.slot]), rb.parity, error)) { ok = false; break; }
+                for (int s = 0; s < steps; ++s, ++g) {
+                    const Ring<WG_RING> r(g);
+                    if (TMA_A && !kb_wait_warp(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error)) { ok = false; break; }
+                    if (!kb_wait_warp(kb_smem_u32(&sm.b_full[r.slot]), r.parity, error)) { ok = false; break; }
                     tc_fence_after();
-                    const unsigned sa = kb_smem_u32(sm.a[ra.slot]), sb = kb_smem_u32(sm.b[rb.slot]);
+                    // 16 tokens are 2048 bytes; addresses count 16 bytes
+                    const unsigned long long da = desc_a + r.slot * (WG_A_BYTES / 16);
+                    const unsigned long long db = bias ? desc_ones : desc_b + r.slot * (WG_B_BYTES / 16);
+                    const unsigned kind = bias ? idesc_bias : idesc, db_step = bias ? 0u : 128u;
+                    if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < WG_K / 16; ++k) {
-                        const unsigned long long da = operand_desc(sa + k * 2048, WG_BLOCK, 1024, 2);
-                        // a block of ones needs no layout: every address the descriptor reaches holds 1
-                        const unsigned long long db = bias ? operand_desc(kb_smem_u32(sm.ones), 256, 256, 0)
-                                                           : operand_desc(sb + k * 2048, WG_BLOCK, 1024, 2);
-                        mma_f16(d, da, db, bias ? idesc_bias : idesc, s > 0 || k > 0);
+                        for (int k = 0; k < WG_K / 16; ++k) mma_f16(d, da + k * 128u, db + k * db_step, kind, s > 0 || k > 0);
+                        mma_commit(&sm.empty[r.slot]);
                     }
-                    mma_commit(&sm.a_empty[ra.slot]);
-                    mma_commit(&sm.b_empty[rb.slot]);
-                    ra.next(WG_A_RING);
-                    rb.next(WG_B_RING);
+                    __syncwarp();
                 }
                 if (ok) {
-                    mma_commit(&sm.acc_full[acc.slot]);
-                    acc.next(2);
+                    if (elect_one()) mma_commit(&sm.acc_full[acc.slot]);
+                    __syncwarp();
+                    ++n_acc;
                 }
             }
             // nothing is in flight when the tensor memory is freed: on the good path the store warps have
             // seen every accumulator; after a wait that gave up, wait for what was issued
             if (!ok) {
-                mma_commit(&sm.acc_full[acc.slot]);
+                const Ring<2> acc(n_acc);
+                if (elect_one()) mma_commit(&sm.acc_full[acc.slot]);
+                __syncwarp();
                 kb_wait(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error, true, 1u << 10);
             }
         }
     } else if (warp >= WG_RESTORE_WARP0) {
-        const int w = (warp - WG_RESTORE_WARP0) % WG_RESTORE_GROUP, tl = lane & 7, sub = lane >> 3;
-        const unsigned mine = unsigned(warp - WG_RESTORE_WARP0) / WG_RESTORE_GROUP;
-        unsigned turn = 0;                                        // steps so far, over all tiles
-        Ring ra, rb, rq;
-        bool ok = true;
+        const int w = (warp - WG_RESTORE_WARP0) % WG_GROUP_WARPS, tl = lane & 7, sub = lane >> 3;
+        const unsigned mine = unsigned(warp - WG_RESTORE_WARP0) / WG_GROUP_WARPS;
+        const int row = 16 * w + tl;                              // this lane's tokens of a step: row and row + 8
+        // the lane's two 16-column pieces of a row: a diagonal over the eight lanes of a phase, so that
+        // neither the reads of the codes nor the swizzled stores meet in a bank
+        const int piece[2] = {(tl + sub) & 7, (tl + sub + 4) & 7};
+        const int q_at = row * WG_HALF;
+        int b_at[2][2];                                           // the two halves of a piece in the operand tile
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                b_at[k][h] = row * 128 + (piece[k] >> 2) * WG_BLOCK + ((((piece[k] & 3) * 2 + h) ^ tl) << 4);
         for (int64_t i = pair; ok && i < tiles; i += pairs) {
             const Tile t = tile_at(a, i);
             const bool bias = t.n == a.nt;
-            const int row = 16 * w + tl;                          // this lane's tokens of a step: row and row + 8
-            const int64_t base = int64_t(t.worker) * a.tokens;
-            // the lane's two 16-column pieces of a row: a diagonal over the eight lanes of a phase, so that
-            // neither the reads of the codes nor the swizzled stores meet in a bank
-            const int piece[2] = {(tl + sub) & 7, (tl + sub + 4) & 7};
             const int64_t c0 = int64_t(t.n) * WG_N + rank * WG_HALF;
+            const int len = int(t.len);
+            const float* scale_at[2];                             // of the first row, for each piece
+            bool inside[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int64_t group = (c0 + piece[k] * 16) >> a.group_shift;
+                inside[k] = !bias && group < a.groups;
+                scale_at[k] = a.scales + (int64_t(t.worker) * a.tokens + row) * a.groups + group;
+            }
             float next[4];
             auto fetch_scales = [&](int s) {
+                const int64_t at = int64_t(s) * WG_K * a.groups;
+                const int token = s * WG_K + row;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int64_t token = int64_t(s) * WG_K + row + 8 * (k >> 1), group = (c0 + piece[k & 1] * 16) >> a.group_shift;
-                    next[k] = !bias && token < t.len && group < a.groups ? __ldg(a.scales + (base + token) * a.groups + group) : 0.f;
-                }
+                for (int k = 0; k < 4; ++k)
+                    next[k] = inside[k & 1] && token + 8 * (k >> 1) < len ? __ldg(scale_at[k & 1] + at + 8 * (k >> 1) * a.groups) : 0.f;
             };
-            const int first = int((turn ^ mine) & 1u);            // this group's first step of the tile
-            if (first < t.steps) fetch_scales(first);
-            for (int s = 0; s < t.steps; ++s, ++turn) {
-                if (((turn ^ mine) & 1u) == 0) {
-                    float scale[4];
+            int s = int((mine + WG_GROUPS - g % WG_GROUPS) % WG_GROUPS);       // this group's first step of the tile
+            if (s < t.steps) fetch_scales(s);
+            bool ready = false;                                   // the step's slots have been seen free and filled
+            for (; s < t.steps; s += WG_GROUPS) {
+                const Ring<WG_RING> r(g + s);
+                const Ring<WG_Q_RING> rq(gq + s);
+                float scale[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) scale[k] = next[k];
-                    if (s + 2 < t.steps) fetch_scales(s + 2);
-                    if (!kb_wait_warp(kb_smem_u32(&sm.b_empty[rb.slot]), rb.parity ^ 1u, error)) { ok = false; break; }
-                    if (!bias) {
-                        if (!kb_wait_warp(kb_smem_u32(&sm.q_full[rq.slot]), rq.parity, error)) { ok = false; break; }
-                        const uint8_t* q = sm.q[rq.slot] + row * WG_HALF;
-                        uint8_t* b = sm.b[rb.slot] + row * 128;
-                        uint4 c[4];
+                for (int k = 0; k < 4; ++k) scale[k] = next[k];
+                if (s + WG_GROUPS < t.steps) fetch_scales(s + WG_GROUPS);
+                if (!__all_sync(0xffffffffu, ready)) {
+                    if (!kb_wait_warp(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
+                    if (!bias && !kb_wait_warp(kb_smem_u32(&sm.q_full[rq.slot]), rq.parity, error)) { ok = false; break; }
+                }
+                // asked early, so that the answer is there when the next step of this group begins
+                const Ring<WG_RING> r2(g + s + WG_GROUPS);
+                const Ring<WG_Q_RING> rq2(gq + s + WG_GROUPS);
+                ready = s + WG_GROUPS < t.steps && !bias;
+                if (ready) ready = kb_test(kb_smem_u32(&sm.empty[r2.slot]), r2.parity ^ 1u) & kb_test(kb_smem_u32(&sm.q_full[rq2.slot]), rq2.parity);
+                if (!bias) {
+                    const uint8_t* q = sm.q[rq.slot] + q_at;
+                    uint8_t* b = sm.b[r.slot];
+                    uint4 c[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) c[k] = *reinterpret_cast<const uint4*>(q + (k >> 1) * 8 * WG_HALF + piece[k & 1] * 16);
+                    for (int k = 0; k < 4; ++k) c[k] = *reinterpret_cast<const uint4*>(q + (k >> 1) * 8 * WG_HALF + piece[k & 1] * 16);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const unsigned words[4] = {c[k].x ^ 0x80808080u, c[k].y ^ 0x80808080u, c[k].z ^ 0x80808080u, c[k].w ^ 0x80808080u};
-                            const f32x2 sc = pack2(scale[k], scale[k]);
-                            unsigned v[8];
+                    for (int k = 0; k < 4; ++k) {
+                        const unsigned words[4] = {c[k].x ^ 0x80808080u, c[k].y ^ 0x80808080u, c[k].z ^ 0x80808080u, c[k].w ^ 0x80808080u};
+                        const f32x2 sc = pack2(scale[k], scale[k]);
+                        unsigned v[8];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                v[2 * j] = restore_pair<T>(words[j], 0x7440, 0x7441, sc);
-                                v[2 * j + 1] = restore_pair<T>(words[j], 0x7442, 0x7443, sc);
-                            }
-                            uint8_t* dst = b + (k >> 1) * 1024 + (piece[k & 1] >> 2) * WG_BLOCK;
-                            const int chunk = (piece[k & 1] & 3) * 2;
-                            *reinterpret_cast<uint4*>(dst + ((chunk ^ tl) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
-                            *reinterpret_cast<uint4*>(dst + (((chunk + 1) ^ tl) << 4)) = make_uint4(v[4], v[5], v[6], v[7]);
+                        for (int j = 0; j < 4; ++j) {
+                            v[2 * j] = restore_pair<T>(words[j], 0x7440, 0x7441, sc);
+                            v[2 * j + 1] = restore_pair<T>(words[j], 0x7442, 0x7443, sc);
                         }
-                    }
-                    if (!TMA_A) {
-                        if (!kb_wait_warp(kb_smem_u32(&sm.a_empty[ra.slot]), ra.parity ^ 1u, error)) { ok = false; break; }
-                        load_dy<T>(a, t, int64_t(2 * t.m + int(rank)) * WG_M, s, sm.a[ra.slot], w, lane);
-                    } else {
-                        if (!kb_wait_warp(kb_smem_u32(&sm.a_full[ra.slot]), ra.parity, error)) { ok = false; break; }
-                        if (a.lengths && int64_t(s + 1) * WG_K > t.len) {
-                            // tokens behind the worker's length: zeros in place of what the copy brought
-                            for (int k = 0; k < 16; ++k) {
-                                const int rr = 16 * w + k;
-                                if (int64_t(s) * WG_K + rr >= t.len && lane < WG_A_BYTES / WG_BLOCK * 8)
-                                    *reinterpret_cast<uint4*>(sm.a[ra.slot] + (lane / 8) * WG_BLOCK + rr * 128 + (lane % 8) * 16) = make_uint4(0, 0, 0, 0);
-                            }
-                        }
-                    }
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        arrive_at_leader(&sm.full[rb.slot]);
-                        if (!bias) kb_arrive(&sm.q_empty[rq.slot]);
+                        *reinterpret_cast<uint4*>(b + (k >> 1) * 1024 + b_at[k & 1][0]) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4*>(b + (k >> 1) * 1024 + b_at[k & 1][1]) = make_uint4(v[4], v[5], v[6], v[7]);
                     }
                 }
-                ra.next(WG_A_RING);
-                rb.next(WG_B_RING);
-                if (!bias) rq.next(WG_Q_RING);
+                const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M;
+                if (!TMA_A) load_dy<false>(a, t, o0, s, sm.a[r.slot], w, lane);
+                else if (a.lengths && (s + 1) * WG_K > len) load_dy<true>(a, t, o0, s, sm.a[r.slot], w, lane);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    arrive_at_leader(&sm.b_full[r.slot]);
+                    if (!bias) kb_arrive(&sm.q_empty[rq.slot]);
+                }
             }
+            g += t.steps;
+            if (!bias) gq += t.steps;
         }
     } else if (warp >= WG_STORE_WARP0) {
         const int quarter = warp - WG_STORE_WARP0;               // == warp % 4: tensor-memory lanes 32 quarter ..
         float* stage = sm.out[quarter];
-        Ring acc;
-        bool ok = true;
+        unsigned n_acc = 0;
         for (int64_t i = pair; ok && i < tiles; i += pairs) {
             const Tile t = tile_at(a, i);
+            const Ring<2> acc(n_acc);
             const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M + quarter * 32;
-            const unsigned src = tmem + unsigned(acc.slot) * WG_N + (unsigned(quarter * 32) << 16);
+            const unsigned src = tmem + acc.slot * WG_N + (unsigned(quarter * 32) << 16);
             if (t.steps) {
                 if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error)) { ok = false; break; }
                 tc_fence_after();
@@ -488,7 +537,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) arrive_at_leader(&sm.acc_empty[acc.slot]);
-                acc.next(2);
+                ++n_acc;
             }
         }
     }
