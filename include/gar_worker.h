@@ -8,8 +8,8 @@
  * Conventions are those of gar.h: device pointers of the current device, all
  * buffers owned by the caller, every call asynchronous on `stream`, argument
  * errors returned before anything is launched, GAR_ERR_CUDA for launch
- * failures, no exceptions, no CPU fallback, no workspace, bit-identical output
- * for the same input.  Matrices are row-major with unit column stride and a
+ * failures, no exceptions, no CPU fallback, bit-identical output for the same
+ * input.  Matrices are row-major with unit column stride and a
  * row stride `ld` in elements (0 means the number of columns); any alignment
  * of the element type is accepted unless stated otherwise.  Element types are
  * a gar_dtype_t; all arithmetic and every sum are fp32 and each output is
@@ -173,9 +173,16 @@ typedef struct gar_weight_grad_params_t {
     void*            weight_grads;/* dev */
     void*            bias_grads;  /* dev; NULL: none */
     int64_t          ld_grads;    /* elements between workers; >= out_features * in_features when workers > 1 */
+    void*            workspace;   /* dev, 256-byte aligned, >= gar_weight_grad_workspace_bytes: x' is restored into it
+                                     once (and dy copied there if its rows do not start on 16 bytes), for layers wide
+                                     enough that restoring it per tile costs more.  NULL: no workspace, every tile
+                                     restores what it multiplies.  The results are the same */
+    size_t           workspace_bytes;
     void*            stream;
 } gar_weight_grad_params_t;
 int gar_linear_weight_grad(const gar_weight_grad_params_t* params);
+/* Bytes of that workspace (host, pure; only sizes and dy's alignment are looked at).  0 on invalid sizes. */
+size_t gar_weight_grad_workspace_bytes(const gar_weight_grad_params_t* params);
 
 #ifdef __cplusplus
 }

@@ -16,5 +16,5 @@ from .binding import (  # noqa: F401
 from .worker import (  # noqa: F401
     ACTIVATIONS, GAR_MAX_TOP, Activation, ActivationGrad, Checkpoint, GarActivationGradParams, GarActivationParams, GarCheckpoint,
     GarLogprobsGradParams, GarLogprobsParams, GarWeightGradParams, TokenLogprobs, gar_activation_backward, gar_activation_forward,
-    gar_checkpoint_pack, gar_checkpoint_unpack, gar_linear_weight_grad, gar_token_logprobs, gar_token_logprobs_backward,
+    gar_checkpoint_pack, gar_checkpoint_unpack, gar_linear_weight_grad, gar_weight_grad_workspace_bytes, gar_token_logprobs, gar_token_logprobs_backward,
 )

@@ -181,6 +181,13 @@ int gar_checkpoint_unpack(int dtype, const gar_checkpoint_t* saved, int64_t rows
                                                              static_cast<cudaStream_t>(stream)));
 }
 
+size_t gar_weight_grad_workspace_bytes(const gar_weight_grad_params_t* p) {
+    const int64_t limit = int64_t(1) << 31;
+    if (!p || p->workers < 1 || p->workers > GAR_MAX_N || p->tokens < 0 || p->tokens >= limit / p->workers) return 0;
+    if (p->out_features < 1 || p->in_features < 1 || p->out_features >= limit || p->in_features >= limit) return 0;
+    return gar::worker::weight_grad_workspace_bytes(*p, p->ld_dy ? p->ld_dy : p->out_features);
+}
+
 int gar_linear_weight_grad(const gar_weight_grad_params_t* p) {
     if (!p || !dtype_ok(p->dtype) || !dtype_ok(p->grads_dtype) || !group_ok(p->group)) return GAR_ERR_INVALID_ARG;
     if (p->workers < 1 || p->tokens < 0 || p->out_features < 1 || p->in_features < 1) return GAR_ERR_INVALID_ARG;
@@ -204,6 +211,12 @@ int gar_linear_weight_grad(const gar_weight_grad_params_t* p) {
     const Span ins[4] = {span(p->dy, rows, p->out_features, ld_dy, es), span(p->x_saved.q, rows, p->in_features, p->x_saved.ldq, 1),
                          span(p->x_saved.scales, rows, g, g, 4), span(p->lengths, 1, p->workers, 0, 4)};
     if (clash(outs, 2, ins, 4)) return GAR_ERR_INVALID_ARG;
+    if (p->workspace) {
+        if (!aligned(p->workspace, 256) || p->workspace_bytes < gar_weight_grad_workspace_bytes(p)) return GAR_ERR_WORKSPACE;
+        const Span ws[1] = {span(p->workspace, 1, int64_t(p->workspace_bytes), 0, 1)};
+        const Span rest[6] = {dw, db, ins[0], ins[1], ins[2], ins[3]};
+        if (clash(ws, 1, rest, 6)) return GAR_ERR_INVALID_ARG;
+    }
     int sms = 0;
     if (int rc = sm_count(&sms)) return rc;
     return cuda_status(gar::worker::launch_weight_grad(*p, ld_dy, sms));

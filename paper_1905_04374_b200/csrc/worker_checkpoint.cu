@@ -239,8 +239,10 @@ struct RestoreArgs {
     unsigned tasks;
     FastDiv  per_row;
     int      groups, lane_shift;
+    const int32_t* lengths;         // MASKED: row w * tokens + t is restored as zeros from t = lengths[w] on
+    int64_t  tokens;
 };
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool MASKED>
 __global__ void __launch_bounds__(CK_THREADS) checkpoint_restore_kernel(const RestoreArgs a) {
     const unsigned task = blockIdx.x * CK_THREADS + threadIdx.x;
     if (task >= a.tasks) return;
@@ -251,7 +253,12 @@ __global__ void __launch_bounds__(CK_THREADS) checkpoint_restore_kernel(const Re
     if (left <= 0) return;
     const int count = left < 8 ? int(left) : 8;
     float v[8];
-    restore8<T>(a.s.q + row * a.s.ld + col, a.s.scales + row * a.groups + (t >> a.lane_shift), count, v);
+    if (MASKED && row % a.tokens >= a.lengths[row / a.tokens]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    } else {
+        restore8<T>(a.s.q + row * a.s.ld + col, a.s.scales + row * a.groups + (t >> a.lane_shift), count, v);
+    }
     store8<T, VEC>(static_cast<T*>(a.x) + row * a.ldx + col, count, v);
 }
 
@@ -352,8 +359,9 @@ cudaError_t launch_activation_backward(const gar_activation_grad_params_t& p) {
     });
 }
 
-cudaError_t launch_checkpoint_unpack(int dtype, const gar_checkpoint_t& saved, int64_t rows, int64_t cols, int group, void* x,
-                                     int64_t ldx, cudaStream_t stream) {
+namespace {
+cudaError_t restore(int dtype, const gar_checkpoint_t& saved, int64_t rows, int64_t cols, int group, void* x, int64_t ldx,
+                    const int32_t* lengths, int64_t tokens, cudaStream_t stream) {
     const unsigned per_row = tasks_per_row(cols, group);
     if (!per_row) return cudaErrorInvalidConfiguration;
     RestoreArgs a{};
@@ -364,14 +372,27 @@ cudaError_t launch_checkpoint_unpack(int dtype, const gar_checkpoint_t& saved, i
     a.per_row = FastDiv(per_row);
     a.groups = int((cols + group - 1) / group);
     a.lane_shift = log2_lanes(group);
+    a.lengths = lengths;
+    a.tokens = tokens;
     const bool vec = aligned16(x, ldx, esize_of(dtype));
     return over_rows(rows, per_row, [&](int64_t r0, unsigned tasks, unsigned blocks) {
         a.row0 = r0;
         a.tasks = tasks;
         by_type(dtype, vec, [&](auto t, auto v) {
-            checkpoint_restore_kernel<decltype(t), decltype(v)::value != 0><<<blocks, CK_THREADS, 0, stream>>>(a);
+            constexpr bool VEC = decltype(v)::value != 0;
+            if (lengths) checkpoint_restore_kernel<decltype(t), VEC, true><<<blocks, CK_THREADS, 0, stream>>>(a);
+            else checkpoint_restore_kernel<decltype(t), VEC, false><<<blocks, CK_THREADS, 0, stream>>>(a);
         });
     });
+}
+}  // namespace
+
+cudaError_t launch_checkpoint_unpack(int dtype, const gar_checkpoint_t& saved, int64_t rows, int64_t cols, int group, void* x,
+                                     int64_t ldx, cudaStream_t stream) {
+    return restore(dtype, saved, rows, cols, group, x, ldx, nullptr, 1, stream);
+}
+cudaError_t launch_checkpoint_restore_masked(const gar_weight_grad_params_t& p, void* x, int64_t ldx, cudaStream_t stream) {
+    return restore(p.dtype, p.x_saved, p.tokens * p.workers, p.in_features, p.group, x, ldx, p.lengths, p.tokens, stream);
 }
 
 }  // namespace worker

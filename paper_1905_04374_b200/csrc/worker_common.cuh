@@ -121,6 +121,9 @@ cudaError_t launch_activation_forward(const gar_activation_params_t& p);
 cudaError_t launch_activation_backward(const gar_activation_grad_params_t& p);
 cudaError_t launch_checkpoint_unpack(int dtype, const gar_checkpoint_t& saved, int64_t rows, int64_t cols, int group, void* x,
                                      int64_t ldx, cudaStream_t stream);
+// The checkpoint of a weight gradient restored in the type of dy, zeros for tokens past the workers' lengths.
+cudaError_t launch_checkpoint_restore_masked(const gar_weight_grad_params_t& p, void* x, int64_t ldx, cudaStream_t stream);
+size_t weight_grad_workspace_bytes(const gar_weight_grad_params_t& p, int64_t ld_dy);
 cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy, int sm_count);
 
 }  // namespace worker

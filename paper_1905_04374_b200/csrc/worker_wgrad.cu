@@ -37,27 +37,32 @@ namespace {
 
 constexpr int WG_M = 128, WG_N = 256, WG_K = 64;      // rows of a CTA, columns of a pair, tokens per step
 constexpr int WG_HALF = WG_N / 2;                     // columns a CTA restores
-// Steps in flight: operand tiles (dy's copy and the restored one share a slot), copies of the codes.
-constexpr int WG_RING = 5, WG_Q_RING = 6;
+// How the operands come: the restore warps load dy and restore x (rows of dy that do not start on 16
+// bytes); dy by TMA; both by TMA, x restored beforehand in the caller's workspace.
+enum Mode { WG_PLAIN_DY = 0, WG_FUSED = 1, WG_RESTORED = 2 };
+// Steps in flight: operand tiles (dy's and x's share a slot), copies of the codes.
+__host__ __device__ constexpr int wg_ring(int mode) { return mode == WG_RESTORED ? 6 : 5; }
+__host__ __device__ constexpr int wg_q_ring(int mode) { return mode == WG_RESTORED ? 1 : 6; }
 constexpr int WG_DY_WARP = 0, WG_MMA_WARP = 1, WG_ALLOC_WARP = 2, WG_CODES_WARP = 3;
 constexpr int WG_STORE_WARP0 = 4;                     // 4..7: tensor-memory lanes 32 (warp % 4) ..
 // Groups of four restore warps take steps in turn: a step takes a group about 1500 cycles from its slot
 // being free to the arrival (waits, reads, 220 instructions, fence), three times what the products take.
-constexpr int WG_RESTORE_WARP0 = 8, WG_GROUP_WARPS = 4, WG_GROUPS = 3;
-constexpr int WG_THREADS = 32 * (WG_RESTORE_WARP0 + WG_GROUP_WARPS * WG_GROUPS);
+constexpr int WG_RESTORE_WARP0 = 8, WG_GROUP_WARPS = 4;
+__host__ __device__ constexpr int wg_groups(int mode) { return mode == WG_RESTORED ? 1 : 3; }
+__host__ __device__ constexpr int wg_threads(int mode) { return 32 * (WG_RESTORE_WARP0 + WG_GROUP_WARPS * wg_groups(mode)); }
 constexpr int WG_BLOCK = 64 * 128;                    // bytes of 64 tokens x 64 columns of an operand
 constexpr int WG_A_BYTES = WG_M / 64 * WG_BLOCK, WG_B_BYTES = WG_HALF / 64 * WG_BLOCK, WG_Q_BYTES = WG_K * WG_HALF;
 constexpr int WG_GROUP_M = 8;                         // (pair) row tiles that go round a column tile together
 constexpr int WG_BIAS_N = 16;
 
-struct __align__(1024) WGSmem {
-    uint8_t  a[WG_RING][WG_A_BYTES];
-    uint8_t  b[WG_RING][WG_B_BYTES];
-    uint8_t  q[WG_Q_RING][WG_Q_BYTES];
+template <int RING, int Q_RING> struct __align__(1024) WGSmem {
+    uint8_t  a[RING][WG_A_BYTES];
+    uint8_t  b[RING][WG_B_BYTES];
+    uint8_t  q[Q_RING][WG_Q_BYTES];
     float    out[4][32 * 32];                             // a store warp's 32 x 32 piece of the tile
     uint16_t ones[512];
-    unsigned long long empty[WG_RING], q_full[WG_Q_RING], q_empty[WG_Q_RING], acc_full[2];
-    unsigned long long a_full[WG_RING], b_full[WG_RING], acc_empty[2];     // the leading CTA's are used, for both
+    unsigned long long empty[RING], q_full[Q_RING], q_empty[Q_RING], late[RING], acc_full[2];
+    unsigned long long a_full[RING], b_full[RING], acc_empty[2];           // the leading CTA's are used, for both
     unsigned tmem_base;
     int      error;
 };
@@ -256,13 +261,16 @@ __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t 
     }
 }
 
-// TMA_A: dy comes by TMA, except a worker's last step where only some of its tokens count (the
-// restore warps load that one, and every step without TMA_A).
-template <typename T, typename G, bool TMA_A>
-__global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs a, const __grid_constant__ CUtensorMap map_dy,
-                                                                    const __grid_constant__ CUtensorMap map_q) {
+// map_x: the codes, or (WG_RESTORED) the restored activation.  Where dy comes by TMA the restore warps
+// still load a worker's last step if only some of its tokens count.
+template <typename T, typename G, int MODE>
+__global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const WGArgs a, const __grid_constant__ CUtensorMap map_dy,
+                                                                          const __grid_constant__ CUtensorMap map_x) {
+    constexpr int WG_RING = wg_ring(MODE), WG_Q_RING = wg_q_ring(MODE), WG_GROUPS = wg_groups(MODE), WG_THREADS = wg_threads(MODE);
+    constexpr bool TMA_A = MODE != WG_PLAIN_DY;
+    typedef WGSmem<WG_RING, WG_Q_RING> Smem;
     extern __shared__ uint8_t raw[];
-    WGSmem& sm = *reinterpret_cast<WGSmem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     volatile int* error = &sm.error;
     const unsigned rank = cta_rank();
@@ -272,6 +280,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
         for (int k = 0; k < WG_RING; ++k) {
             kb_init(&sm.empty[k], 1);
             kb_init(&sm.a_full[k], 1);
+            kb_init(&sm.late[k], 1);
             kb_init(&sm.b_full[k], 2 * WG_GROUP_WARPS);
         }
         for (int k = 0; k < WG_Q_RING; ++k) {
@@ -303,20 +312,33 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
     if (warp == WG_DY_WARP) {
         if (TMA_A && lane == 0) {
             const unsigned leader_full = pair_address(kb_smem_u32(sm.a_full), 0);
+            unsigned n_late = 0;
             for (int64_t i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
                 const int o0 = (2 * t.m + int(rank)) * WG_M;
                 for (int s = 0; s < t.steps; ++s, ++g) {
                     const Ring<WG_RING> r(g);
                     if (!kb_wait(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
-                    if (a.lengths && int64_t(s + 1) * WG_K > t.len) {
-                        if (rank == 0) kb_arrive(&sm.a_full[r.slot]);
-                        continue;
+                    // dy's part of a step that the restore warps load is missing; a bias tile has no x
+                    const bool copy_dy = !(a.lengths && int64_t(s + 1) * WG_K > t.len), copy_x = MODE == WG_RESTORED && t.n < a.nt;
+                    const unsigned bytes = (copy_dy ? WG_A_BYTES : 0) + (copy_x ? WG_B_BYTES : 0);
+                    if (MODE == WG_RESTORED && !copy_dy) kb_arrive(&sm.late[n_late++ % WG_RING]);
+                    if (rank == 0) {
+                        if (bytes) kb_expect_tx(kb_smem_u32(&sm.a_full[r.slot]), 2 * bytes);
+                        else kb_arrive(&sm.a_full[r.slot]);
                     }
-                    if (rank == 0) kb_expect_tx(kb_smem_u32(&sm.a_full[r.slot]), 2 * WG_A_BYTES);
-                    const unsigned bar = leader_full + r.slot * 8, dst = kb_smem_u32(sm.a[r.slot]);
-                    tma_load_pair(dst, &map_dy, o0, s * WG_K, t.worker, bar);
-                    tma_load_pair(dst + WG_BLOCK, &map_dy, o0 + 64, s * WG_K, t.worker, bar);
+                    const unsigned bar = leader_full + r.slot * 8;
+                    if (copy_dy) {
+                        const unsigned dst = kb_smem_u32(sm.a[r.slot]);
+                        tma_load_pair(dst, &map_dy, o0, s * WG_K, t.worker, bar);
+                        tma_load_pair(dst + WG_BLOCK, &map_dy, o0 + 64, s * WG_K, t.worker, bar);
+                    }
+                    if (copy_x) {
+                        const unsigned dst = kb_smem_u32(sm.b[r.slot]);
+                        const int c0 = t.n * WG_N + int(rank) * WG_HALF;
+                        tma_load_pair(dst, &map_x, c0, s * WG_K, t.worker, bar);
+                        tma_load_pair(dst + WG_BLOCK, &map_x, c0 + 64, s * WG_K, t.worker, bar);
+                    }
                 }
             }
             // after a wait that gave up: the copies in flight land (the leading CTA counts them in) before
@@ -327,7 +349,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
             }
         }
     } else if (warp == WG_CODES_WARP) {
-        if (lane == 0) {
+        if (MODE != WG_RESTORED && lane == 0) {
             for (int64_t i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
                 if (t.n == a.nt) continue;
@@ -336,7 +358,7 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
                     if (!kb_wait(kb_smem_u32(&sm.q_empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
                     const unsigned bar = kb_smem_u32(&sm.q_full[r.slot]);
                     kb_expect_tx(bar, WG_Q_BYTES);
-                    tma_load(kb_smem_u32(sm.q[r.slot]), &map_q, t.n * WG_N + int(rank) * WG_HALF, s * WG_K, t.worker, bar);
+                    tma_load(kb_smem_u32(sm.q[r.slot]), &map_x, t.n * WG_N + int(rank) * WG_HALF, s * WG_K, t.worker, bar);
                 }
             }
             for (unsigned k = 0; !ok && k < WG_Q_RING && k < gq; ++k) {
@@ -354,10 +376,11 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
             const unsigned long long desc_b = operand_desc(kb_smem_u32(sm.b), WG_BLOCK, 1024, 2);
             // a block of ones needs no layout: every address the descriptor reaches holds 1
             const unsigned long long desc_ones = operand_desc(kb_smem_u32(sm.ones), 256, 256, 0);
-            unsigned n_acc = 0;
+            unsigned n_acc = 0, n_late = 0;
             for (int64_t i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
                 const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
+                const bool partial = t.len % WG_K != 0;
                 if (steps == 0) continue;
                 const Ring<2> acc(n_acc);
                 if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[acc.slot]), acc.parity ^ 1u, error)) { ok = false; break; }
@@ -367,7 +390,11 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
                 for (int s = 0; s < steps; ++s, ++g) {
                     const Ring<WG_RING> r(g);
                     if (TMA_A && !kb_wait_warp(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error)) { ok = false; break; }
-                    if (!kb_wait_warp(kb_smem_u32(&sm.b_full[r.slot]), r.parity, error)) { ok = false; break; }
+                    if (MODE != WG_RESTORED && !kb_wait_warp(kb_smem_u32(&sm.b_full[r.slot]), r.parity, error)) { ok = false; break; }
+                    if (MODE == WG_RESTORED && a.lengths && s + 1 == steps && partial) {
+                        const Ring<WG_RING> late(n_late++);
+                        if (!kb_wait_warp(kb_smem_u32(&sm.b_full[late.slot]), late.parity, error)) { ok = false; break; }
+                    }
                     tc_fence_after();
                     // 16 tokens are 2048 bytes; addresses count 16 bytes
                     const unsigned long long da = desc_a + r.slot * (WG_A_BYTES / 16);
@@ -394,6 +421,23 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
                 __syncwarp();
                 kb_wait(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error, true, 1u << 10);
             }
+        }
+    } else if (warp >= WG_RESTORE_WARP0 && MODE == WG_RESTORED) {
+        // Only dy's last step of a worker whose length ends inside it.  These steps go round barriers on a
+        // count of their own, and the dy warp says when the slot is free: a parity cannot be waited for by
+        // who does not follow the slot from round to round.
+        const int w = warp - WG_RESTORE_WARP0;
+        unsigned n_late = 0;
+        for (int64_t i = pair; a.lengths && i < tiles; i += pairs) {
+            const Tile t = tile_at(a, i);
+            g += t.steps;
+            if (t.len % WG_K == 0) continue;
+            const Ring<WG_RING> r(g - 1), late(n_late++);
+            if (!kb_wait_warp(kb_smem_u32(&sm.late[late.slot]), late.parity, error)) { ok = false; break; }
+            load_dy<true>(a, t, int64_t(2 * t.m + int(rank)) * WG_M, t.steps - 1, sm.a[r.slot], w, lane);
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) arrive_at_leader(&sm.b_full[late.slot]);
         }
     } else if (warp >= WG_RESTORE_WARP0) {
         const int w = (warp - WG_RESTORE_WARP0) % WG_GROUP_WARPS, tl = lane & 7, sub = lane >> 3;
@@ -568,6 +612,20 @@ __global__ void __launch_bounds__(WG_THREADS, 1) weight_grad_kernel(const WGArgs
     }
 }
 
+// Rows of 16-bit elements copied to rows that start on 16 bytes (zeros behind the last column), eight
+// elements per thread and turn.
+__global__ void __launch_bounds__(256) align_rows_kernel(const unsigned short* src, int64_t ld, int64_t cols, int64_t pieces,
+                                                         uint4* dst, int64_t per_row) {
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += int64_t(gridDim.x) * 256) {
+        const int64_t row = i / per_row, c = (i - row * per_row) * 8;
+        const unsigned short* p = src + row * ld + c;
+        unsigned v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? __ldg(p + j) : 0u;
+        dst[i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    }
+}
+
 // ---- launch -------------------------------------------------------------------------------------
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -598,17 +656,17 @@ cudaError_t make_map(CUtensorMap* map, CUtensorMapDataType type, const void* bas
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <typename T, typename G, bool TMA_A>
-cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_q, int sm_count, cudaStream_t stream) {
-    constexpr int bytes = int(sizeof(WGSmem)) + 1024;
+template <typename T, typename G, int MODE>
+cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x, int sm_count, cudaStream_t stream) {
+    constexpr int bytes = int(sizeof(WGSmem<wg_ring(MODE), wg_q_ring(MODE)>)) + 1024;
     static_assert(bytes <= 232448, "a CTA's shared memory");
-    auto kernel = weight_grad_kernel<T, G, TMA_A>;
+    auto kernel = weight_grad_kernel<T, G, MODE>;
     if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
     const int64_t tiles = int64_t(a.workers) * a.mt * a.columns;
     const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(unsigned(2 * (tiles < pairs ? tiles : pairs)));
-    cfg.blockDim = dim3(WG_THREADS);
+    cfg.blockDim = dim3(wg_threads(MODE));
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -617,15 +675,25 @@ cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, map_dy, map_q);
+    return cudaLaunchKernelEx(&cfg, kernel, a, map_dy, map_x);
 }
-template <typename T, bool TMA_A>
-cudaError_t launch_by_grads(int grads_dtype, const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_q, int sm_count,
+template <typename T, int MODE>
+cudaError_t launch_by_grads(int grads_dtype, const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x, int sm_count,
                             cudaStream_t stream) {
-    if (grads_dtype == GAR_F32) return launch<T, float, TMA_A>(a, map_dy, map_q, sm_count, stream);
-    if (grads_dtype == GAR_BF16) return launch<T, __nv_bfloat16, TMA_A>(a, map_dy, map_q, sm_count, stream);
-    return launch<T, __half, TMA_A>(a, map_dy, map_q, sm_count, stream);
+    if (grads_dtype == GAR_F32) return launch<T, float, MODE>(a, map_dy, map_x, sm_count, stream);
+    if (grads_dtype == GAR_BF16) return launch<T, __nv_bfloat16, MODE>(a, map_dy, map_x, sm_count, stream);
+    return launch<T, __half, MODE>(a, map_dy, map_x, sm_count, stream);
 }
+template <typename T>
+cudaError_t launch_by_mode(int mode, int grads_dtype, const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x,
+                           int sm_count, cudaStream_t stream) {
+    if (mode == WG_RESTORED) return launch_by_grads<T, WG_RESTORED>(grads_dtype, a, map_dy, map_x, sm_count, stream);
+    if (mode == WG_FUSED) return launch_by_grads<T, WG_FUSED>(grads_dtype, a, map_dy, map_x, sm_count, stream);
+    return launch_by_grads<T, WG_PLAIN_DY>(grads_dtype, a, map_dy, map_x, sm_count, stream);
+}
+
+bool rows_on_16(const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }
+int64_t round8(int64_t v) { return (v + 7) / 8 * 8; }
 
 }  // namespace
 
@@ -653,23 +721,43 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     a.wide = reinterpret_cast<uintptr_t>(p.weight_grads) % unit == 0 && (p.workers == 1 || p.ld_grads * gs % unit == 0) &&
              p.in_features * gs % unit == 0;
 
-    CUtensorMap map_q, map_dy;
-    if (cudaError_t err = make_map(&map_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.x_saved.q, p.in_features, p.tokens, p.workers,
-                                   p.x_saved.ldq, WG_HALF, CU_TENSOR_MAP_SWIZZLE_NONE)) return err;
-    // TMA needs rows of dy that start on 16 bytes
-    const bool tma_a = reinterpret_cast<uintptr_t>(p.dy) % 16 == 0 && ld_dy % 8 == 0;
-    if (tma_a) {
-        if (cudaError_t err = make_map(&map_dy, p.dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                                       p.dy, p.out_features, p.tokens, p.workers, ld_dy * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
-    } else {
-        map_dy = map_q;                           // not used
+    const CUtensorMapDataType type = p.dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
+    CUtensorMap map_x, map_dy;
+    int mode = rows_on_16(p.dy, ld_dy) ? WG_FUSED : WG_PLAIN_DY;
+    if (p.workspace && p.tokens > 0) {
+        // x restored once (and dy copied, if its rows do not start on 16 bytes), then products of plain copies
+        mode = WG_RESTORED;
+        const int64_t rows = p.tokens * p.workers, ldx = round8(p.in_features);
+        char* x = static_cast<char*>(p.workspace);
+        if (cudaError_t err = launch_checkpoint_restore_masked(p, x, ldx, stream)) return err;
+        if (cudaError_t err = make_map(&map_x, type, x, p.in_features, p.tokens, p.workers, ldx * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+        if (!rows_on_16(p.dy, ld_dy)) {
+            char* dy = x + gar::align256(size_t(rows) * size_t(ldx) * 2);
+            const int64_t ld = round8(p.out_features);
+            const int64_t pieces = rows * (ld / 8);
+            const unsigned blocks = unsigned(min(int64_t(16 * sm_count), (pieces + 255) / 256));
+            align_rows_kernel<<<blocks, 256, 0, stream>>>(static_cast<const unsigned short*>(p.dy), ld_dy, p.out_features, pieces,
+                                                          reinterpret_cast<uint4*>(dy), ld / 8);
+            if (cudaError_t err = cudaGetLastError()) return err;
+            a.dy = dy;
+            a.ld_dy = ld;
+        }
+    } else if (cudaError_t err = make_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.x_saved.q, p.in_features, p.tokens, p.workers,
+                                          p.x_saved.ldq, WG_HALF, CU_TENSOR_MAP_SWIZZLE_NONE)) {
+        return err;
     }
-    cudaStream_t s = static_cast<cudaStream_t>(p.stream);
-    if (p.dtype == GAR_BF16)
-        return tma_a ? launch_by_grads<__nv_bfloat16, true>(p.grads_dtype, a, map_dy, map_q, sm_count, s)
-                     : launch_by_grads<__nv_bfloat16, false>(p.grads_dtype, a, map_dy, map_q, sm_count, s);
-    return tma_a ? launch_by_grads<__half, true>(p.grads_dtype, a, map_dy, map_q, sm_count, s)
-                 : launch_by_grads<__half, false>(p.grads_dtype, a, map_dy, map_q, sm_count, s);
+    if (mode == WG_PLAIN_DY) map_dy = map_x;      // not used
+    else if (cudaError_t err = make_map(&map_dy, type, a.dy, p.out_features, p.tokens, p.workers, a.ld_dy * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+    return p.dtype == GAR_BF16 ? launch_by_mode<__nv_bfloat16>(mode, p.grads_dtype, a, map_dy, map_x, sm_count, stream)
+                               : launch_by_mode<__half>(mode, p.grads_dtype, a, map_dy, map_x, sm_count, stream);
+}
+
+size_t weight_grad_workspace_bytes(const gar_weight_grad_params_t& p, int64_t ld_dy) {
+    const int64_t rows = p.tokens * p.workers;
+    size_t bytes = gar::align256(size_t(rows) * size_t(round8(p.in_features)) * 2);
+    if (!rows_on_16(p.dy, ld_dy)) bytes += gar::align256(size_t(rows) * size_t(round8(p.out_features)) * 2);
+    return bytes;
 }
 
 }  // namespace worker

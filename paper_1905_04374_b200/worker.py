@@ -14,6 +14,9 @@ import torch
 from .binding import GRAD_DTYPES, _check, _stream, lib as _base_lib
 
 GAR_MAX_TOP = 32
+# Outputs from which gar_linear_weight_grad takes a workspace by itself: every 256 outputs restore the
+# activation once more.
+WORKSPACE_OUT = 1024
 ACTIVATIONS = {"identity": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 
@@ -57,7 +60,8 @@ class GarWeightGradParams(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("grads_dtype", C.c_int32), ("group", C.c_int32), ("workers", C.c_int32),
                 ("tokens", C.c_int64), ("out_features", C.c_int64), ("in_features", C.c_int64), ("dy", C.c_void_p),
                 ("ld_dy", C.c_int64), ("x_saved", GarCheckpoint), ("lengths", C.c_void_p), ("weight_grads", C.c_void_p),
-                ("bias_grads", C.c_void_p), ("ld_grads", C.c_int64), ("stream", C.c_void_p)]
+                ("bias_grads", C.c_void_p), ("ld_grads", C.c_int64), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
 
 
 _typed = False
@@ -77,6 +81,8 @@ def lib():
         L.gar_checkpoint_unpack.argtypes = [C.c_int, C.POINTER(GarCheckpoint), C.c_int64, C.c_int64, C.c_int, C.c_void_p,
                                             C.c_int64, C.c_void_p]
         L.gar_linear_weight_grad.argtypes = [C.POINTER(GarWeightGradParams)]
+        L.gar_weight_grad_workspace_bytes.argtypes = [C.POINTER(GarWeightGradParams)]
+        L.gar_weight_grad_workspace_bytes.restype = C.c_size_t
         _typed = True
     return L
 
@@ -301,13 +307,7 @@ def gar_activation_backward(act: str, dy: torch.Tensor, x: Checkpoint, up: Optio
     return ActivationGrad(dx, dup)
 
 
-def gar_linear_weight_grad(dy: torch.Tensor, x: Checkpoint, grads: Optional[torch.Tensor] = None, weight_offset: int = 0,
-                           bias_offset: Optional[int] = None, lengths: Optional[torch.Tensor] = None,
-                           grads_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
-    """gar_linear_weight_grad: dy [workers, tokens, out] and the checkpoint of x [workers * tokens, in]
-    into the gradient block `grads` [workers, d]: row w gets dW_w (out x in, row-major) from column
-    weight_offset on and, with bias_offset, db_w from there on.  lengths int32 [workers]: tokens that
-    count.  Without `grads` a block [workers, out * in] of grads_dtype is made."""
+def _weight_grad_params(dy: torch.Tensor, x: Checkpoint) -> GarWeightGradParams:
     if dy.dim() != 3 or not dy.is_cuda or dy.dtype not in GRAD_DTYPES or (dy.shape[2] > 1 and dy.stride(2) != 1):
         raise ValueError("dy must be a CUDA tensor [workers, tokens, out] with unit column stride")
     workers, tokens, out = dy.shape
@@ -316,6 +316,29 @@ def gar_linear_weight_grad(dy: torch.Tensor, x: Checkpoint, grads: Optional[torc
         raise ValueError("dy: the workers' tokens must be evenly spaced rows")
     if dy.dtype != x.dtype:
         raise TypeError("dy and the checkpoint must be of one type")
+    p = GarWeightGradParams()
+    p.dtype, p.group, p.workers = GRAD_DTYPES[dy.dtype], x.group, workers
+    p.tokens, p.out_features, p.in_features = tokens, out, x.cols
+    p.dy, p.ld_dy = dy.data_ptr() or 16, ld_dy
+    return p
+
+
+def gar_weight_grad_workspace_bytes(dy: torch.Tensor, x: Checkpoint) -> int:
+    """Bytes of the workspace gar_linear_weight_grad takes for these operands."""
+    return lib().gar_weight_grad_workspace_bytes(C.byref(_weight_grad_params(dy, x)))
+
+
+def gar_linear_weight_grad(dy: torch.Tensor, x: Checkpoint, grads: Optional[torch.Tensor] = None, weight_offset: int = 0,
+                           bias_offset: Optional[int] = None, lengths: Optional[torch.Tensor] = None,
+                           grads_dtype: torch.dtype = torch.float32, workspace=None, stream=None) -> torch.Tensor:
+    """gar_linear_weight_grad: dy [workers, tokens, out] and the checkpoint of x [workers * tokens, in]
+    into the gradient block `grads` [workers, d]: row w gets dW_w (out x in, row-major) from column
+    weight_offset on and, with bias_offset, db_w from there on.  lengths int32 [workers]: tokens that
+    count.  Without `grads` a block [workers, out * in] of grads_dtype is made.  workspace: None lets the
+    call allocate one for layers where it is faster, False never (the codes are then restored tile by
+    tile), or a uint8 CUDA tensor of gar_weight_grad_workspace_bytes."""
+    p = _weight_grad_params(dy, x)
+    workers, tokens, out = dy.shape
     dev = dy.device
     if grads is None:
         if weight_offset != 0 or bias_offset is not None:
@@ -327,14 +350,15 @@ def gar_linear_weight_grad(dy: torch.Tensor, x: Checkpoint, grads: Optional[torc
         raise ValueError("grads must have a row per worker and room for the weights at weight_offset")
     if bias_offset is not None and (bias_offset < 0 or bias_offset + out > d):
         raise ValueError("grads has no room for the bias at bias_offset")
-    p = GarWeightGradParams()
-    p.dtype, p.grads_dtype, p.group, p.workers = GRAD_DTYPES[dy.dtype], GRAD_DTYPES[grads.dtype], x.group, workers
-    p.tokens, p.out_features, p.in_features = tokens, out, x.cols
-    p.dy, p.ld_dy = dy.data_ptr() or 16, ld_dy
+    p.grads_dtype = GRAD_DTYPES[grads.dtype]
     p.x_saved = _saved(x, "x", dev, workers * tokens, x.cols)
     p.lengths = _vector(lengths, "lengths", torch.int32, workers, dev)
     p.weight_grads, p.ld_grads = ptr + weight_offset * grads.element_size(), ld
     p.bias_grads = ptr + bias_offset * grads.element_size() if bias_offset is not None else None
+    if workspace is None and out > WORKSPACE_OUT:
+        workspace = torch.empty(lib().gar_weight_grad_workspace_bytes(C.byref(p)), dtype=torch.uint8, device=dev)
+    if workspace is not None and workspace is not False:
+        p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     with torch.cuda.device(dev):
         p.stream = _stream(stream)
         st = lib().gar_linear_weight_grad(C.byref(p))

@@ -459,8 +459,13 @@ def check_weight_grad(pkg, dy, ck, grads_dtype="f32", lengths=None, off=0, gap=0
     weights = out * ck.cols
     d = off + weights + gap + out + tail
     grads = torch.full((n, d), 7.0, dtype=DTYPES[grads_dtype], device=DEV)
-    r = pkg.gar_linear_weight_grad(dy, ck, grads, weight_offset=off, bias_offset=off + weights + gap, lengths=lengths)
+    place = dict(weight_offset=off, bias_offset=off + weights + gap, lengths=lengths)
+    r = pkg.gar_linear_weight_grad(dy, ck, grads, workspace=False, **place)
     assert r is grads
+    # with the activation restored beforehand: the same products in the same order, the same bits
+    space = torch.empty(pkg.gar_weight_grad_workspace_bytes(dy, ck), dtype=torch.uint8, device=DEV)
+    other = pkg.gar_linear_weight_grad(dy, ck, torch.full_like(grads, 7.0), workspace=space, **place)
+    assert torch.equal(other, grads)
     dw, db, sw, sb = weight_grad_64(dy, ck, pkg, lengths)
     unit = 2.0 ** -23 * max(t, 8)
     got = grads[:, off:off + weights].reshape(n, out, ck.cols)
@@ -511,6 +516,16 @@ def test_weight_grad_lengths(pkg, out, inp):
     assert torch.equal(a[0], b[0]) and torch.all(a[1] == 0)
 
 
+@pytest.mark.parametrize("tokens", [40, 150, 257])
+def test_weight_grad_lengths_over_many_tiles(pkg, tokens):
+    """Several tiles per CTA pair, workers that end inside a step, on its edge, and empty ones among them."""
+    n, out, inp = 12, 1100, 2100
+    dy, x = normal((n, tokens, out), "bf16", 1), normal((n * tokens, inp), "bf16", 2)
+    lengths = torch.randint(0, tokens + 1, (n,), generator=gen(tokens), device=DEV, dtype=torch.int32)
+    lengths[0], lengths[5], lengths[11] = tokens, 0, min(tokens, 128)
+    check_weight_grad(pkg, dy, pkg.gar_checkpoint_pack(x, 128), lengths=lengths)
+
+
 def test_weight_grad_workers_do_not_meet(pkg):
     """A NaN of one worker (a Byzantine one, say) stays in its own row: the others' bits do not change."""
     n, t = 4, 70                                             # 70 tokens: every worker ends inside a tile
@@ -519,8 +534,10 @@ def test_weight_grad_workers_do_not_meet(pkg):
         clean = pkg.gar_linear_weight_grad(dy, pkg.gar_checkpoint_pack(x, 64))
         dy[2] = math.nan
         x[2 * t:3 * t] = math.inf
-        got = pkg.gar_linear_weight_grad(dy, pkg.gar_checkpoint_pack(x, 64))
-        assert torch.equal(got[[0, 1, 3]], clean[[0, 1, 3]]) and torch.isnan(got[2]).all()
+        ck = pkg.gar_checkpoint_pack(x, 64)
+        for space in (False, torch.empty(pkg.gar_weight_grad_workspace_bytes(dy, ck), dtype=torch.uint8, device=DEV)):
+            got = pkg.gar_linear_weight_grad(dy, ck, workspace=space)
+            assert torch.equal(got[[0, 1, 3]], clean[[0, 1, 3]]) and torch.isnan(got[2]).all()
 
 
 def test_weight_grad_strided_dy_and_no_tokens(pkg):

@@ -24,7 +24,7 @@ def test_every_declared_symbol_is_exported(pkg):
     text = open(os.path.join(ROOT, "include", "gar_worker.h")).read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
     names = sorted(set(re.findall(r"\b(gar_[a-z_0-9]+)\s*\(", text)))
-    assert len(names) == 7
+    assert len(names) == 8
     for name in names:
         assert hasattr(pkg.lib(), name), f"{name} declared in gar_worker.h but not exported"
         assert hasattr(pkg, name), f"{name} has no Python entry point"
@@ -160,5 +160,11 @@ def test_weight_grad_refusals(pkg):
         dict(dy=None), dict(weight_grads=None), dict(ld_dy=19), dict(ld_grads=599), dict(ld_grads=-1), {"x_saved.q": None},
         {"x_saved.ldq": 16}, dict(bias_grads=(1 << 22) + 4 * 599), dict(bias_grads=(1 << 22) + 4 * 601), dict(dy=1 << 22),
         dict(weight_grads=(1 << 22) + 2), dict(lengths=1 << 22), dict(ld_grads=1 << 60)])
+    L = pkg.worker.lib()
+    need = L.gar_weight_grad_workspace_bytes(C.byref(params()))
+    assert need == 30 * 32 * 2 + 256 - (30 * 32 * 2) % 256 + 30 * 24 * 2 + 256 - (30 * 24 * 2) % 256      # x, and dy (rows of 20)
+    refuses(pkg, "gar_linear_weight_grad", params, [
+        dict(workspace=1 << 30, workspace_bytes=need - 1), dict(workspace=(1 << 30) + 128, workspace_bytes=need)], 4)
+    refuses(pkg, "gar_linear_weight_grad", params, [dict(workspace=1 << 20, workspace_bytes=need)])
     refuses(pkg, "gar_linear_weight_grad", params, [
         dict(dtype=0), dict(workers=65, ld_grads=1 << 40), dict(out_features=1 << 31), dict(tokens=1 << 30)], UNSUPPORTED)
