@@ -12,6 +12,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgar.so")
+WORKER_MODULE = os.path.join(PKG, "_gar_worker.so")
 
 # Slot counts the coordinate kernel is compiled for: keep identical to K3_P_LIST in k3_dispatch.cu.
 K3_P = list(range(1, 33)) + [36, 40, 44, 48, 52, 56, 60, 64]     # <= 32: theta fixed at compile time
@@ -75,7 +76,26 @@ def build(force: bool = False, verbose: bool = False) -> str:
     objs = [os.path.join(OBJ, obj) for _, obj, _ in _units()]
     if jobs or not os.path.exists(LIB):
         run([nvcc, "-shared", "-o", LIB, *objs, "-gencode", "arch=compute_100a,code=sm_100a"])
+    _build_worker_module(run, force)
     return LIB
+
+
+def _build_worker_module(run, force: bool) -> None:
+    """Compile the tensor marshalling of the worker-side operators against the installed torch."""
+    src = os.path.join(CSRC, "worker_binding.cpp")
+    deps = [src, os.path.join(ROOT, "include", "gar.h"), os.path.join(ROOT, "include", "gar_worker.h"), os.path.abspath(__file__)]
+    if not force and os.path.exists(WORKER_MODULE) and os.path.getmtime(WORKER_MODULE) >= max(map(os.path.getmtime, deps)):
+        return
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc()))
+    libs = os.path.join(base, "lib")
+    run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+         "-I" + os.path.join(ROOT, "include"), "-isystem", os.path.join(base, "include"), "-isystem", sysconfig.get_paths()["include"],
+         "-isystem", os.path.join(cuda, "include"), src, "-o", WORKER_MODULE, "-L" + PKG, "-lgar", "-L" + libs, "-lc10", "-lc10_cuda",
+         "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + libs])
 
 
 if __name__ == "__main__":
