@@ -11,6 +11,7 @@ namespace worker {
 namespace {
 
 constexpr int CK_THREADS = 256;
+constexpr int CK_TASKS = 2;                            // per thread: all loads before the arithmetic
 constexpr float CK_TINY = 7.888609052210118e-31f;     // 2^-100
 
 // Division of a task number by the tasks per row: exact for numerators below 2^31.
@@ -24,88 +25,180 @@ struct FastDiv {
     __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
 };
 
-// eight consecutive elements: 16-byte accesses where the row starts allow it, single ones otherwise
+// Eight consecutive elements as they lie in memory (Raw8: one or two 16-byte words).
+template <typename T> struct Raw8;
+template <> struct Raw8<float> { uint4 a, b; };
+template <> struct Raw8<__nv_bfloat16> { uint4 a; };
+template <> struct Raw8<__half> { uint4 a; };
+
+// 16-byte accesses where the row starts allow it, single ones otherwise; columns that are not there read as 0
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int count, float (&v)[8]) {
-    if (VEC && count == 8) {
-        if constexpr (sizeof(T) == 4) {
-            const uint4 a = load_stream(p), b = load_stream(p + 4);
-            float x[4], y[4];
-            widen16B(a, x, static_cast<const T*>(nullptr));
-            widen16B(b, y, static_cast<const T*>(nullptr));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = x[i]; v[4 + i] = y[i]; }
+__device__ __forceinline__ Raw8<T> load8(const T* p, int count) {
+    Raw8<T> r{};
+    if constexpr (sizeof(T) == 4) {
+        if (VEC && count == 8) {
+            r.a = load_stream(p);
+            r.b = load_stream(p + 4);
         } else {
-            widen16B(load_stream(p), v, static_cast<const T*>(nullptr));
+            unsigned w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = i < count ? __float_as_uint(p[i]) : 0u;
+            r.a = make_uint4(w[0], w[1], w[2], w[3]);
+            r.b = make_uint4(w[4], w[5], w[6], w[7]);
         }
     } else {
+        if (VEC && count == 8) {
+            r.a = load_stream(p);
+        } else {
+            const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+            unsigned w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < count ? Elem<T>::widen(p[i]) : 0.f;
+            for (int i = 0; i < 8; ++i) w[i] = i < count ? h[i] : 0u;
+            r.a = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+        }
     }
+    return r;
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, int count, const float (&v)[8]) {
-    if (VEC && count == 8) {
-        if constexpr (sizeof(T) == 4) {
-            const float x[4] = {v[0], v[1], v[2], v[3]}, y[4] = {v[4], v[5], v[6], v[7]};
-            store_stream(p, narrow16B(x, static_cast<const T*>(nullptr)));
-            store_stream(p + 4, narrow16B(y, static_cast<const T*>(nullptr)));
+__device__ __forceinline__ void store8(T* p, int count, const Raw8<T>& r) {
+    if constexpr (sizeof(T) == 4) {
+        if (VEC && count == 8) {
+            store_stream(p, r.a);
+            store_stream(p + 4, r.b);
         } else {
-            store_stream(p, narrow16B(v, static_cast<const T*>(nullptr)));
+            const unsigned w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) p[i] = __uint_as_float(w[i]);
         }
     } else {
+        if (VEC && count == 8) {
+            store_stream(p, r.a);
+        } else {
+            const unsigned w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+            unsigned short* h = reinterpret_cast<unsigned short*>(p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < count) p[i] = Elem<T>::narrow(v[i]);
+            for (int i = 0; i < 8; ++i)
+                if (i < count) h[i] = static_cast<unsigned short>(w[i >> 1] >> (16 * (i & 1)));
+        }
     }
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw8<T>& r, float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        float x[4], y[4];
+        widen16B(r.a, x, static_cast<const T*>(nullptr));
+        widen16B(r.b, y, static_cast<const T*>(nullptr));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = x[i]; v[4 + i] = y[i]; }
+    } else {
+        widen16B(r.a, v, static_cast<const T*>(nullptr));
+    }
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> narrow8(const float (&v)[8]) {
+    Raw8<T> r;
+    if constexpr (sizeof(T) == 4) {
+        const float x[4] = {v[0], v[1], v[2], v[3]}, y[4] = {v[4], v[5], v[6], v[7]};
+        r.a = narrow16B(x, static_cast<const T*>(nullptr));
+        r.b = narrow16B(y, static_cast<const T*>(nullptr));
+    } else {
+        r.a = narrow16B(v, static_cast<const T*>(nullptr));
+    }
+    return r;
 }
 
-// The checkpoint of eight columns; the `lanes` neighbours of the group take part (all 32 lanes call).
-__device__ __forceinline__ void save8(const float (&v)[8], int count, int lanes, bool leader, int8_t* q, float* scale) {
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(v[i]));
-    for (int o = lanes >> 1; o; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (count <= 0) return;
-    const bool sound = top <= 3.402823466e38f, zero = top < CK_TINY;
-    const float inv = sound && !zero ? __fmul_rn(__frcp_rn(top), 127.f) : 0.f;
-    if (leader) *scale = !sound ? CUDART_NAN_F : zero ? 0.f : __fdiv_rn(top, 127.f);
-    unsigned r[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        // |v inv| <= 127 (1 + 2^-22): the sum's low byte is the nearest integer, ties to even
-        const unsigned b = __float_as_uint(__fadd_rn(__fmul_rn(v[i], inv), 12582912.f));
-        r[i] = sound ? b : 0u;
+// ---- the scale of a group ---------------------------------------------------------------------
+// Magnitudes are compared as unsigned integers: the sign bit cleared, a NaN is above infinity and
+// infinity above every number.  For the 16-bit types two maxima travel in one register.
+template <typename T>
+__device__ __forceinline__ unsigned top8(const Raw8<T>& r) {                  // of eight elements, in T's own bits
+    if constexpr (sizeof(T) == 4) {
+        const unsigned m = 0x7fffffffu;
+        return max(max(max(r.a.x & m, r.a.y & m), max(r.a.z & m, r.a.w & m)), max(max(r.b.x & m, r.b.y & m), max(r.b.z & m, r.b.w & m)));
+    } else {
+        const unsigned m = 0x7fff7fffu;
+        const unsigned t = __vmaxu2(__vmaxu2(r.a.x & m, r.a.y & m), __vmaxu2(r.a.z & m, r.a.w & m));
+        return max(t & 0xffffu, t >> 16);
     }
-    const unsigned lo = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
-    const unsigned hi = __byte_perm(__byte_perm(r[4], r[5], 0x0040), __byte_perm(r[6], r[7], 0x0040), 0x5410);
+}
+// Over the `lanes` neighbours of a group (all 32 lanes of the warp call).
+template <typename T>
+__device__ __forceinline__ void group_top(unsigned& x, unsigned& u, bool two, int lanes) {
+    if constexpr (sizeof(T) == 4) {
+        for (int o = lanes >> 1; o; o >>= 1) {
+            x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+            if (two) u = max(u, __shfl_xor_sync(0xffffffffu, u, o));
+        }
+    } else {
+        unsigned both = x | u << 16;
+        for (int o = lanes >> 1; o; o >>= 1) both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, o));
+        x = both & 0xffffu;
+        u = both >> 16;
+    }
+}
+template <typename T>
+__device__ __forceinline__ float magnitude(unsigned bits) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(bits);
+    else if constexpr (std::is_same<T, __half>::value) return __half2float(__ushort_as_half(static_cast<unsigned short>(bits)));
+    else return __uint_as_float(bits << 16);
+}
+
+// The codes and, from the group's first lane, the scale of eight columns with group maximum `top`.
+__device__ __forceinline__ void save8(const float (&v)[8], float top, int count, bool leader, int8_t* q, float* scale) {
+    if (count <= 0) return;
+    const bool sound = top <= 3.402823466e38f, live = sound && top >= CK_TINY;
+    const float inv = live ? __fmul_rn(__frcp_rn(top), 127.f) : 0.f;
+    if (leader) {
+        // top / 127, correctly rounded: Markstein's correction of the product with the rounded reciprocal
+        const float y = 1.f / 127.f, q0 = __fmul_rn(top, y);
+        const float s = __fmaf_rn(__fmaf_rn(-127.f, q0, top), y, q0);
+        *scale = !sound ? CUDART_NAN_F : live ? s : 0.f;
+    }
+    // |v inv| <= 127 (1 + 2^-22): the low byte of the sum with 1.5 * 2^23 is the nearest integer, ties to even
+    // (the products one by one: as a pair, product and sum were contracted to one rounding)
+    const f32x2 magic = pack2(12582912.f, 12582912.f);
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) unpack2(add2(pack2(__fmul_rn(v[i], inv), __fmul_rn(v[i + 1], inv)), magic), r[i], r[i + 1]);
+    unsigned lo = __byte_perm(__byte_perm(__float_as_uint(r[0]), __float_as_uint(r[1]), 0x0040),
+                              __byte_perm(__float_as_uint(r[2]), __float_as_uint(r[3]), 0x0040), 0x5410);
+    unsigned hi = __byte_perm(__byte_perm(__float_as_uint(r[4]), __float_as_uint(r[5]), 0x0040),
+                              __byte_perm(__float_as_uint(r[6]), __float_as_uint(r[7]), 0x0040), 0x5410);
+    if (!sound) lo = hi = 0u;
     if (count == 8) {
         __stcs(reinterpret_cast<uint2*>(q), make_uint2(lo, hi));
     } else {
         for (int i = 0; i < count; ++i) q[i] = int8_t(((i < 4 ? lo : hi) >> (8 * (i & 3))) & 0xff);
     }
 }
+__device__ __forceinline__ uint2 load_codes(const int8_t* q, int count) {
+    if (count == 8) return __ldcs(reinterpret_cast<const uint2*>(q));
+    unsigned w[2] = {0, 0};
+    for (int i = 0; i < count; ++i) w[i >> 2] |= unsigned(uint8_t(q[i])) << (8 * (i & 3));
+    return make_uint2(w[0], w[1]);
+}
 // Eight restored values, rounded to T.
 template <typename T>
-__device__ __forceinline__ void restore8(const int8_t* q, const float* scale, int count, float (&v)[8]) {
-    unsigned w[2] = {0, 0};
-    if (count == 8) {
-        const uint2 r = __ldcs(reinterpret_cast<const uint2*>(q));
-        w[0] = r.x;
-        w[1] = r.y;
-    } else {
-        for (int i = 0; i < count; ++i) w[i >> 2] |= unsigned(uint8_t(q[i])) << (8 * (i & 3));
-    }
-    const float s = __ldg(scale);
+__device__ __forceinline__ Raw8<T> restore8(const uint2& codes, float scale) {
+    const unsigned w[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
+    const f32x2 s = pack2(scale, scale), bias = pack2(-8388736.f, -8388736.f);
+    float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; i += 2) {
         // byte ^ 0x80 = code + 128 in the low bits of 2^23
-        const float c = __uint_as_float(__byte_perm(w[i >> 2] ^ 0x80808080u, 0x4b000000u, 0x7440 + (i & 3))) - 8388736.f;
-        v[i] = Elem<T>::widen(Elem<T>::narrow(c * s));
+        const f32x2 c = pack2(__uint_as_float(__byte_perm(w[i >> 2], 0x4b000000u, 0x7440 + (i & 3))),
+                              __uint_as_float(__byte_perm(w[i >> 2], 0x4b000000u, 0x7441 + (i & 3))));
+        unpack2(mul2(add2(c, bias), s), v[i], v[i + 1]);
     }
+    return narrow8<T>(v);
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + ex2(-x * kLog2e)); }
+__device__ __forceinline__ float sigmoid(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(-x * kLog2e)));
+    return r;
+}
 
 template <int ACT>
 __device__ __forceinline__ float act(float x) {
@@ -134,6 +227,24 @@ __device__ __forceinline__ void act_slope(float x, float& y, float& slope) {
     }
 }
 
+// A thread's task: eight columns of a row.
+struct Task {
+    int64_t row, col, group;
+    int     count;                 // columns that exist; 0: nothing to do
+};
+template <typename A>
+__device__ __forceinline__ Task task_at(const A& a, unsigned number) {
+    Task t;
+    const bool live = number < a.tasks;
+    const unsigned n = live ? number : 0u, r = a.per_row.quotient(n), c = n - r * a.per_row.d;
+    t.row = a.row0 + r;
+    t.col = int64_t(c) * 8;
+    t.group = t.row * a.groups + (c >> a.lane_shift);
+    const int64_t left = a.cols - t.col;
+    t.count = !live || left <= 0 ? 0 : left < 8 ? int(left) : 8;
+    return t;
+}
+
 struct Saved {
     int8_t* q;
     float*  scales;
@@ -151,36 +262,47 @@ struct ForwardArgs {
     int         groups, lanes, lane_shift;
 };
 
-template <typename T, int ACT, bool VEC>
+// GATED: y = act(x) * up
+template <typename T, int ACT, bool VEC, bool GATED>
 __global__ void __launch_bounds__(CK_THREADS) activation_forward_kernel(const ForwardArgs a) {
-    const unsigned task = blockIdx.x * CK_THREADS + threadIdx.x;
-    const bool live = task < a.tasks;
-    const unsigned r = a.per_row.quotient(live ? task : 0u);
-    const unsigned t = (live ? task : 0u) - r * a.per_row.d;
-    const int64_t row = a.row0 + r, col = int64_t(t) * 8;
-    const int64_t left = a.cols - col;
-    const int count = !live || left <= 0 ? 0 : left < 8 ? int(left) : 8;
-    const bool leader = (threadIdx.x & (a.lanes - 1)) == 0;
-    const int64_t group = row * a.groups + (t >> a.lane_shift);
-
-    float x[8], y[8];
-    load8<T, VEC>(static_cast<const T*>(a.x) + row * a.ldx + col, count, x);
-    if (a.up) {
-        float u[8];
-        load8<T, VEC>(static_cast<const T*>(a.up) + row * a.ldup + col, count, u);
+    Task t[CK_TASKS];
+    Raw8<T> x[CK_TASKS], u[CK_TASKS];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = act<ACT>(x[i]) * u[i];
-        if (a.sup.q) save8(u, count, a.lanes, leader, a.sup.q + row * a.sup.ld + col, a.sup.scales + group);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = act<ACT>(x[i]);
+    for (int k = 0; k < CK_TASKS; ++k) {
+        t[k] = task_at(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
+        x[k] = load8<T, VEC>(static_cast<const T*>(a.x) + t[k].row * a.ldx + t[k].col, t[k].count);
+        if (GATED) u[k] = load8<T, VEC>(static_cast<const T*>(a.up) + t[k].row * a.ldup + t[k].col, t[k].count);
     }
-    if (a.sx.q) save8(x, count, a.lanes, leader, a.sx.q + row * a.sx.ld + col, a.sx.scales + group);
-    if (a.y) store8<T, VEC>(static_cast<T*>(a.y) + row * a.ldy + col, count, y);
-    if (a.sy.q) {
+    const bool leader = (threadIdx.x & (a.lanes - 1)) == 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = i < count ? Elem<T>::widen(Elem<T>::narrow(y[i])) : 0.f;
-        save8(y, count, a.lanes, leader, a.sy.q + row * a.sy.ld + col, a.sy.scales + group);
+    for (int k = 0; k < CK_TASKS; ++k) {
+        const int count = t[k].count;
+        unsigned top_x = 0, top_u = 0;
+        if (a.sx.q || a.sup.q) {
+            top_x = top8<T>(x[k]);
+            if (GATED) top_u = top8<T>(u[k]);
+            group_top<T>(top_x, top_u, GATED, a.lanes);
+        }
+        float v[8], y[8];
+        widen8<T>(x[k], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = act<ACT>(v[i]);
+        if (a.sx.q) save8(v, magnitude<T>(top_x), count, leader, a.sx.q + t[k].row * a.sx.ld + t[k].col, a.sx.scales + t[k].group);
+        if (GATED) {
+            widen8<T>(u[k], v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] *= v[i];
+            if (a.sup.q) save8(v, magnitude<T>(top_u), count, leader, a.sup.q + t[k].row * a.sup.ld + t[k].col, a.sup.scales + t[k].group);
+        }
+        const Raw8<T> out = narrow8<T>(y);
+        if (a.y) store8<T, VEC>(static_cast<T*>(a.y) + t[k].row * a.ldy + t[k].col, count, out);
+        if (a.sy.q) {
+            // y of a column that does not exist is act(0) = 0
+            unsigned top_y = top8<T>(out), none = 0;
+            group_top<T>(top_y, none, false, a.lanes);
+            widen8<T>(out, v);
+            save8(v, magnitude<T>(top_y), count, leader, a.sy.q + t[k].row * a.sy.ld + t[k].col, a.sy.scales + t[k].group);
+        }
     }
 }
 
@@ -195,41 +317,52 @@ struct BackwardArgs {
     int         groups, lane_shift;
 };
 
-template <typename T, int ACT, bool VEC>
+template <typename T, int ACT, bool VEC, bool GATED>
 __global__ void __launch_bounds__(CK_THREADS) activation_backward_kernel(const BackwardArgs a) {
-    const unsigned task = blockIdx.x * CK_THREADS + threadIdx.x;
-    if (task >= a.tasks) return;
-    const unsigned r = a.per_row.quotient(task);
-    const unsigned t = task - r * a.per_row.d;
-    const int64_t row = a.row0 + r, col = int64_t(t) * 8;
-    const int64_t left = a.cols - col;
-    if (left <= 0) return;
-    const int count = left < 8 ? int(left) : 8;
-    const int64_t group = row * a.groups + (t >> a.lane_shift);
-
-    float dy[8], x[8], dx[8];
-    load8<T, VEC>(static_cast<const T*>(a.dy) + row * a.lddy + col, count, dy);
-    restore8<T>(a.sx.q + row * a.sx.ld + col, a.sx.scales + group, count, x);
-    if (a.sup.q) {
-        float u[8], du[8];
-        restore8<T>(a.sup.q + row * a.sup.ld + col, a.sup.scales + group, count, u);
+    Task t[CK_TASKS];
+    Raw8<T> dy[CK_TASKS];
+    uint2 cx[CK_TASKS], cu[CK_TASKS];
+    float sx[CK_TASKS], su[CK_TASKS];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float y, slope;
-            act_slope<ACT>(x[i], y, slope);
-            du[i] = dy[i] * y;
-            dx[i] = dy[i] * u[i] * slope;
-        }
-        store8<T, VEC>(static_cast<T*>(a.dup) + row * a.lddup + col, count, du);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float y, slope;
-            act_slope<ACT>(x[i], y, slope);
-            dx[i] = dy[i] * slope;
+    for (int k = 0; k < CK_TASKS; ++k) {
+        t[k] = task_at(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
+        const int count = t[k].count;
+        dy[k] = load8<T, VEC>(static_cast<const T*>(a.dy) + t[k].row * a.lddy + t[k].col, count);
+        cx[k] = count ? load_codes(a.sx.q + t[k].row * a.sx.ld + t[k].col, count) : make_uint2(0, 0);
+        sx[k] = count ? __ldg(a.sx.scales + t[k].group) : 0.f;
+        if (GATED) {
+            cu[k] = count ? load_codes(a.sup.q + t[k].row * a.sup.ld + t[k].col, count) : make_uint2(0, 0);
+            su[k] = count ? __ldg(a.sup.scales + t[k].group) : 0.f;
         }
     }
-    store8<T, VEC>(static_cast<T*>(a.dx) + row * a.lddx + col, count, dx);
+#pragma unroll
+    for (int k = 0; k < CK_TASKS; ++k) {
+        const int count = t[k].count;
+        if (count == 0) continue;
+        float d[8], x[8], dx[8];
+        widen8<T>(dy[k], d);
+        widen8<T>(restore8<T>(cx[k], sx[k]), x);
+        if (GATED) {
+            float u[8], du[8];
+            widen8<T>(restore8<T>(cu[k], su[k]), u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float y, slope;
+                act_slope<ACT>(x[i], y, slope);
+                du[i] = d[i] * y;
+                dx[i] = d[i] * u[i] * slope;
+            }
+            store8<T, VEC>(static_cast<T*>(a.dup) + t[k].row * a.lddup + t[k].col, count, narrow8<T>(du));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float y, slope;
+                act_slope<ACT>(x[i], y, slope);
+                dx[i] = d[i] * slope;
+            }
+        }
+        store8<T, VEC>(static_cast<T*>(a.dx) + t[k].row * a.lddx + t[k].col, count, narrow8<T>(dx));
+    }
 }
 
 struct RestoreArgs {
@@ -244,22 +377,19 @@ struct RestoreArgs {
 };
 template <typename T, bool VEC, bool MASKED>
 __global__ void __launch_bounds__(CK_THREADS) checkpoint_restore_kernel(const RestoreArgs a) {
-    const unsigned task = blockIdx.x * CK_THREADS + threadIdx.x;
-    if (task >= a.tasks) return;
-    const unsigned r = a.per_row.quotient(task);
-    const unsigned t = task - r * a.per_row.d;
-    const int64_t row = a.row0 + r, col = int64_t(t) * 8;
-    const int64_t left = a.cols - col;
-    if (left <= 0) return;
-    const int count = left < 8 ? int(left) : 8;
-    float v[8];
-    if (MASKED && row % a.tokens >= a.lengths[row / a.tokens]) {
+    Task t[CK_TASKS];
+    uint2 codes[CK_TASKS];
+    float scale[CK_TASKS];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    } else {
-        restore8<T>(a.s.q + row * a.s.ld + col, a.s.scales + row * a.groups + (t >> a.lane_shift), count, v);
+    for (int k = 0; k < CK_TASKS; ++k) {
+        t[k] = task_at(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
+        const bool read = t[k].count && !(MASKED && t[k].row % a.tokens >= a.lengths[t[k].row / a.tokens]);
+        codes[k] = read ? load_codes(a.s.q + t[k].row * a.s.ld + t[k].col, t[k].count) : make_uint2(0, 0);
+        scale[k] = read ? __ldg(a.s.scales + t[k].group) : 0.f;
     }
-    store8<T, VEC>(static_cast<T*>(a.x) + row * a.ldx + col, count, v);
+#pragma unroll
+    for (int k = 0; k < CK_TASKS; ++k)
+        store8<T, VEC>(static_cast<T*>(a.x) + t[k].row * a.ldx + t[k].col, t[k].count, restore8<T>(codes[k], scale[k]));
 }
 
 // ---- launches ---------------------------------------------------------------------------------
@@ -273,12 +403,12 @@ size_t esize_of(int dtype) { return dtype == GAR_F32 ? 4 : 2; }
 // Calls f(row0, tasks, blocks) for row ranges of fewer than 2^31 tasks.
 template <typename F>
 cudaError_t over_rows(int64_t rows, unsigned per_row, F f) {
-    const int64_t step = ((int64_t(1) << 31) - CK_THREADS) / per_row;
+    const int64_t step = ((int64_t(1) << 31) - CK_THREADS * CK_TASKS) / per_row;
     if (step < 1) return cudaErrorInvalidConfiguration;
     for (int64_t r0 = 0; r0 < rows; r0 += step) {
         const int64_t n = rows - r0 < step ? rows - r0 : step;
         const unsigned tasks = unsigned(n * per_row);
-        f(r0, tasks, (tasks + CK_THREADS - 1) / CK_THREADS);
+        f(r0, tasks, (tasks + CK_THREADS * CK_TASKS - 1) / (CK_THREADS * CK_TASKS));
         if (cudaError_t err = cudaGetLastError()) return err;
     }
     return cudaSuccess;
@@ -328,7 +458,9 @@ cudaError_t launch_activation_forward(const gar_activation_params_t& p) {
         a.tasks = tasks;
         by_type(p.dtype, vec, [&](auto t, auto v) {
             by_act(p.act, [&](auto f) {
-                activation_forward_kernel<decltype(t), decltype(f)::value, decltype(v)::value != 0><<<blocks, CK_THREADS, 0, stream>>>(a);
+                constexpr bool VEC = decltype(v)::value != 0;
+                if (a.up) activation_forward_kernel<decltype(t), decltype(f)::value, VEC, true><<<blocks, CK_THREADS, 0, stream>>>(a);
+                else activation_forward_kernel<decltype(t), decltype(f)::value, VEC, false><<<blocks, CK_THREADS, 0, stream>>>(a);
             });
         });
     });
@@ -353,7 +485,9 @@ cudaError_t launch_activation_backward(const gar_activation_grad_params_t& p) {
         a.tasks = tasks;
         by_type(p.dtype, vec, [&](auto t, auto v) {
             by_act(p.act, [&](auto f) {
-                activation_backward_kernel<decltype(t), decltype(f)::value, decltype(v)::value != 0><<<blocks, CK_THREADS, 0, stream>>>(a);
+                constexpr bool VEC = decltype(v)::value != 0;
+                if (a.sup.q) activation_backward_kernel<decltype(t), decltype(f)::value, VEC, true><<<blocks, CK_THREADS, 0, stream>>>(a);
+                else activation_backward_kernel<decltype(t), decltype(f)::value, VEC, false><<<blocks, CK_THREADS, 0, stream>>>(a);
             });
         });
     });

@@ -3,18 +3,18 @@
 // Forward.  Every thread runs the softmax recurrence over its share of a row: with m the largest
 // value so far, s = sum e^(x-m) and u = sum e^(x-m) (x-m) log2(e); a larger m' rescales
 //     f = e^(m-m'),  u <- f (u + s (m-m') log2(e)),  s <- f s.
-// x - m is formed before the product with log2(e), so large logits lose nothing to cancellation,
-// and it is held above -1e4 so that a masked entry (-inf) contributes e = 0 and 0 to u.  Shares are
-// joined by the same rescaling: lanes, warps, then (rows split over a cluster) CTAs through
-// distributed shared memory.
+// x - m is formed before the product with log2(e), so large logits lose nothing to cancellation.  A
+// masked entry (-inf) must add e = 0 and 0 to u, not 0 * inf: where a tile holds one, the exponents
+// are kept above -1e4.  Shares are joined by the same rescaling: lanes, warps, then (rows split over
+// a cluster) CTAs through distributed shared memory.
 //
-// The k best entries need nothing in that loop: m IS the largest value of the thread's share.  An
-// entry of the top k lies in the share of a thread whose m is among the k largest of the CTA (ties
-// included), so only those shares are read again (they are in L2), by whole warps; entries not
-// below the k-th largest m are collected, ranked by counting and stored.  A 64-bit key (value in
-// an order-preserving code, complement of the index) makes the order total: equal values go to the
-// lowest index.  If more entries qualify than the list holds (rows with many equal values, such as
-// fully masked ones) the k best are extracted one by one instead.
+// The k best entries cost that loop one store: the maximum of every tile of a thread's share (32 bytes
+// to 16 KB).  With j = ceil(k / warps), the j-th largest of a warp's thread maxima, taken as the least
+// over the warps, has at least k entries not below it; only the tiles whose maximum reaches it are read
+// again, about two k of them, and of those the entries that reach it are ranked by counting.  A 64-bit
+// key (value in an order-preserving code, complement of the index) makes the order total: equal values
+// go to the lowest index.  If more entries qualify than the list holds (rows with many equal values,
+// such as heavily masked ones) the k best are extracted one by one instead.
 #include <cooperative_groups.h>
 
 #include "worker_common.cuh"
@@ -27,10 +27,13 @@ namespace {
 
 constexpr int LP_THREADS = 256;
 constexpr int LP_WARPS = LP_THREADS / 32;
-constexpr int LP_UNROLL = 4;            // 16-byte loads in flight per thread
+constexpr int LP_UNROLL = 4;            // 16-byte slots of a thread's turn (find_top's shift counts on 4)
 constexpr int LP_LIST = 512;            // candidate entries of a CTA
+constexpr int LP_TILES = 16;            // tiles of a thread's share
+constexpr int LP_SHARES = 256;          // tiles that are read again
 constexpr int LP_MAX_CLUSTER = 8;
 constexpr float LP_FLOOR = -1e4f;       // exponents below this are 0 in fp32
+constexpr float LP_HUGE = 1e30f;        // between -LP_HUGE and LP_HUGE no exponent overflows
 
 struct Softmax {
     float m, s, u;
@@ -188,12 +191,12 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_small_kernel(const Forwar
 
 // ---- longer rows: a CTA, or a cluster of up to eight, per row ------------------------------------
 struct ForwardShared {
+    float              tile_max[LP_TILES][LP_THREADS];
     Softmax            part[LP_WARPS];
     Softmax            total;                      // of this CTA: read by the cluster's first
-    alignas(16) float  best[LP_THREADS];           // the threads' largest values, read four at a time
-    int                shares[LP_THREADS];         // threads whose share is read again
-    int                nshares, nlist, overflow;
-    float              threshold;
+    unsigned           warp_code[LP_WARPS];
+    int                shares[LP_SHARES];          // thread + LP_THREADS * tile
+    int                nshares, nlist;
     unsigned long long list[LP_LIST];
     unsigned long long top[GAR_MAX_TOP];           // this CTA's best, in order (0: none): read by the cluster's first
     unsigned long long warp_key[LP_WARPS];
@@ -261,56 +264,61 @@ __device__ unsigned long long best_below(const RowView<T>& v, int tid, unsigned 
     return best;
 }
 
-// The CTA's `top` best entries of its part of the row into sh.top, in order (zeros beyond what there is).
+// The CTA's `top` best entries of its part of the row into sh.top, in order (zeros beyond what there
+// is).  `mine`: the largest value of the thread's share; tiles of (1 << shift) slots.
 template <typename T>
-__device__ void find_top(ForwardShared& sh, const RowView<T>& v, float mine, int top) {
+__device__ void find_top(ForwardShared& sh, const RowView<T>& v, float mine, int top, int shift) {
     constexpr int E = Elem<T>::PER16;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    sh.best[tid] = mine;
-    if (tid == 0) {
-        sh.nshares = sh.nlist = sh.overflow = 0;
-        sh.threshold = CUDART_INF_F;
-    }
+    if (tid == 0) sh.nshares = sh.nlist = 0;
     if (tid < GAR_MAX_TOP) sh.top[tid] = 0;
-    __syncthreads();
-    int above = 0;
-    for (int j = 0; j < LP_THREADS; j += 4) {
-        const float4 b = *reinterpret_cast<const float4*>(&sh.best[j]);
-        above += (b.x > mine) + (b.y > mine) + (b.z > mine) + (b.w > mine);
+    // warps whose 32 threads all have a slot; a share without a number or with masked entries only counts as 0
+    const int64_t slots = v.last - v.first;
+    const int full = slots >= LP_THREADS ? LP_WARPS : int(slots / 32);
+    const unsigned own = mine == -CUDART_INF_F ? 0u : code_of(mine);
+    unsigned least = 0xffffffffu;
+    if (warp < full) {
+        unsigned rest = own;
+        for (int j = (top + full - 1) / full; j > 0; --j) {
+            least = __reduce_max_sync(0xffffffffu, rest);
+            if (lane == __ffs(__ballot_sync(0xffffffffu, rest == least)) - 1) rest = 0u;
+        }
     }
-    // the threads with fewer than `top` larger maxima; the smallest of those maxima bounds the answer from below
-    if (above < top) {
-        sh.shares[atomicAdd(&sh.nshares, 1)] = tid;
-    }
-    float low = above < top ? mine : CUDART_INF_F;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
-    if (lane == 0) sh.part[warp].m = low;
+    if (lane == 0) sh.warp_code[warp] = least;
     __syncthreads();
-    low = sh.part[0].m;
-#pragma unroll
-    for (int w = 1; w < LP_WARPS; ++w) low = fminf(low, sh.part[w].m);
+    unsigned low = full ? sh.warp_code[0] : 0u;
+    for (int w = 1; w < full; ++w) low = min(low, sh.warp_code[w]);
+    const int64_t edge = edge_entry(v, tid);
+    if (own >= low) {
+        const int tiles = int((slots - tid + LP_THREADS - 1) / LP_THREADS + (1 << shift) - 1) >> shift;      // of this thread
+        for (int i = 0; i < tiles; ++i)
+            if (low == 0u || code_of(sh.tile_max[i][tid]) >= low) {
+                const int at = atomicAdd(&sh.nshares, 1);
+                if (at < LP_SHARES) sh.shares[at] = tid + LP_THREADS * i;
+            }
+        if (edge >= 0) {
+            const float f = load_one(v.x, edge);
+            if (code_of(f) >= low) offer(sh, f, edge);
+        }
+    }
+    __syncthreads();
     const int nshares = sh.nshares;
-    if (nshares <= 4 * GAR_MAX_TOP) {
-        for (int c = warp; c < nshares; c += LP_WARPS) {
-            const int owner = sh.shares[c];
-            for (int64_t slot = v.first + owner + int64_t(lane) * LP_THREADS; slot < v.last; slot += 32 * LP_THREADS) {
+    if (nshares <= LP_SHARES) {
+        for (int i = tid; i < nshares << shift; i += LP_THREADS) {
+            const int share = sh.shares[i >> shift];
+            const int64_t slot = v.first + share % LP_THREADS + int64_t(((share / LP_THREADS) << shift) + (i & ((1 << shift) - 1))) * LP_THREADS;
+            if (slot < v.last) {
                 float f[E];
                 widen16B(*reinterpret_cast<const uint4*>(v.base + slot * E), f, static_cast<const T*>(nullptr));
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (!(f[e] < low)) offer(sh, f[e], slot * E + e - v.head);
-            }
-            const int64_t j = edge_entry(v, owner);
-            if (lane == 0 && j >= 0) {
-                const float f = load_one(v.x, j);
-                if (!(f < low)) offer(sh, f, j);
+                    if (code_of(f[e]) >= low) offer(sh, f[e], slot * E + e - v.head);
             }
         }
     }
     __syncthreads();
     const int nlist = sh.nlist;
-    if (nshares <= 4 * GAR_MAX_TOP && nlist <= LP_LIST) {
+    if (nshares <= LP_SHARES && nlist <= LP_LIST) {
         for (int i = tid; i < nlist; i += LP_THREADS) {
             const unsigned long long key = sh.list[i];
             int rank = 0;
@@ -340,8 +348,74 @@ __device__ void find_top(ForwardShared& sh, const RowView<T>& v, float mine, int
     }
 }
 
+// Largest value (NaN entries do not count) of a tile, and whether a masked entry (-inf, or so low that the
+// exponent may overflow) may be in it.
+__device__ __forceinline__ void tile_range(const uint4 (&raw)[LP_UNROLL], float& top, bool& masked, const float*) {
+    top = -CUDART_INF_F;
+#pragma unroll
+    for (int i = 0; i < LP_UNROLL; ++i)
+        top = fmaxf(fmaxf(fmaxf(top, __uint_as_float(raw[i].x)), fmaxf(__uint_as_float(raw[i].y), __uint_as_float(raw[i].z))), __uint_as_float(raw[i].w));
+    masked = true;                       // four entries per 16 bytes: keeping the exponents in range costs less than asking
+}
+template <typename H2, typename From, typename Max, typename Min>
+__device__ __forceinline__ void tile_range_16(const uint4 (&raw)[LP_UNROLL], float& top, bool& masked, From from, Max mx, Min mn) {
+    H2 hi = from(raw[0].x), lo = hi;
+#pragma unroll
+    for (int i = 0; i < LP_UNROLL; ++i) {
+        const unsigned w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            hi = mx(hi, from(w[j]));
+            lo = mn(lo, from(w[j]));
+        }
+    }
+    top = fmaxf(fmaxf(-CUDART_INF_F, float(hi.x)), float(hi.y));     // a tile of NaN: -inf
+    masked = !(float(lo.x) >= -LP_HUGE && float(lo.y) >= -LP_HUGE);
+}
+__device__ __forceinline__ void tile_range(const uint4 (&raw)[LP_UNROLL], float& top, bool& masked, const __nv_bfloat16*) {
+    tile_range_16<__nv_bfloat162>(raw, top, masked, [](unsigned w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); },
+                                  [](__nv_bfloat162 a, __nv_bfloat162 b) { return __hmax2(a, b); },
+                                  [](__nv_bfloat162 a, __nv_bfloat162 b) { return __hmin2(a, b); });
+}
+__device__ __forceinline__ void tile_range(const uint4 (&raw)[LP_UNROLL], float& top, bool& masked, const __half*) {
+    tile_range_16<__half2>(raw, top, masked, [](unsigned w) { return *reinterpret_cast<const __half2*>(&w); },
+                           [](__half2 a, __half2 b) { return __hmax2(a, b); }, [](__half2 a, __half2 b) { return __hmin2(a, b); });
+}
+// 16 bytes of -inf
+template <typename T> __device__ __forceinline__ uint4 nothing() {
+    const unsigned w = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
+}
+template <typename T, bool MASKED>
+__device__ __forceinline__ void add_tile(const uint4 (&raw)[LP_UNROLL], float centre_at, f32x2& s2, f32x2& u2) {
+    constexpr int E = Elem<T>::PER16;
+    const f32x2 nc = pack2(-centre_at, -centre_at), scale = pack2(kLog2e, kLog2e);
+#pragma unroll
+    for (int i = 0; i < LP_UNROLL; ++i) {
+        float f[E];
+        widen16B(raw[i], f, static_cast<const T*>(nullptr));
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            f32x2 t = mul2(add2(pack2(f[e], f[e + 1]), nc), scale);
+            float t0, t1;
+            unpack2(t, t0, t1);
+            if (MASKED) {
+                t0 = max_nan(t0, LP_FLOOR);
+                t1 = max_nan(t1, LP_FLOOR);
+                t = pack2(t0, t1);
+            }
+            const f32x2 ex = pack2(ex2(t0), ex2(t1));
+            s2 = add2(s2, ex);
+            u2 = fma2(ex, t, u2);
+        }
+    }
+}
+
+// Bound by memory for 16-bit logits as long as the loop stays under the issue rate: per entry about one
+// exponential (of 16 a cycle and SM, 1.4 at the memory's rate) and five instructions.  The next tile's
+// loads are in flight while a tile is worked on.
 template <typename T>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(const ForwardArgs a, int parts) {
+__global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const ForwardArgs a, int parts) {
     constexpr int E = Elem<T>::PER16;
     __shared__ __align__(16) ForwardShared sh;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -349,59 +423,46 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(const ForwardArgs 
     const int64_t row = blockIdx.x / unsigned(parts);
     const RowView<T> v = view_row(static_cast<const T*>(a.logits) + row * a.ld, a.vocab, rank, unsigned(parts));
 
+    // turns of LP_UNROLL slots per thread; a tile is (1 << turn_shift) turns
+    const int turns = int((v.last - v.first + LP_UNROLL * LP_THREADS - 1) / (LP_UNROLL * LP_THREADS));
+    int turn_shift = 0;
+    while ((turns + (1 << turn_shift) - 1) >> turn_shift > LP_TILES) ++turn_shift;
+
     Softmax st{-CUDART_INF_F, 0.f, 0.f};
     f32x2 s2 = pack2(0.f, 0.f), u2 = pack2(0.f, 0.f);
-    const f32x2 scale = pack2(kLog2e, kLog2e);
-    auto tile = [&](const uint4 (&raw)[LP_UNROLL], int count) {
-        float f[LP_UNROLL][E];
-        float m = st.m;
+    const T* at = v.base + (v.first + tid) * E;
+    int64_t left = v.last - v.first - tid;                       // slots from `at` on, at a stride of LP_THREADS
+    auto fetch = [&](uint4 (&raw)[LP_UNROLL]) {
 #pragma unroll
-        for (int i = 0; i < LP_UNROLL; ++i) {
-            if (i < count) {
-                widen16B(raw[i], f[i], static_cast<const T*>(nullptr));
-#pragma unroll
-                for (int e = 0; e < E; ++e) m = fmaxf(m, f[i][e]);
-            }
-        }
-        if (m > st.m) {
+        for (int i = 0; i < LP_UNROLL; ++i)
+            raw[i] = left > i * LP_THREADS ? load_stream(at + i * LP_THREADS * E) : nothing<T>();
+        at += LP_UNROLL * LP_THREADS * E;
+        left -= LP_UNROLL * LP_THREADS;
+    };
+    uint4 raw[LP_UNROLL], next[LP_UNROLL];
+    float tile_top = -CUDART_INF_F;
+    if (turns > 0) fetch(raw);
+    for (int turn = 0; turn < turns; ++turn) {
+        if (turn + 1 < turns) fetch(next);
+        float top;
+        bool masked;
+        tile_range(raw, top, masked, static_cast<const T*>(nullptr));
+        tile_top = (turn & ((1 << turn_shift) - 1)) ? fmaxf(tile_top, top) : top;
+        if (a.top) sh.tile_max[turn >> turn_shift][tid] = tile_top;
+        if (top > st.m) {
             float s0, s1, u0, u1;
             unpack2(s2, s0, s1);
             unpack2(u2, u0, u1);
             st.s = s0 + s1;
             st.u = u0 + u1;
-            raise(st, m);
+            raise(st, top);
             s2 = pack2(st.s, 0.f);
             u2 = pack2(st.u, 0.f);
         }
-        const float c = centre(st.m);
-        const f32x2 nc = pack2(-c, -c);
+        if (masked || st.m > LP_HUGE) add_tile<T, true>(raw, centre(st.m), s2, u2);
+        else add_tile<T, false>(raw, centre(st.m), s2, u2);
 #pragma unroll
-        for (int i = 0; i < LP_UNROLL; ++i) {
-            if (i < count) {
-#pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    float t0, t1;
-                    unpack2(mul2(add2(pack2(f[i][e], f[i][e + 1]), nc), scale), t0, t1);
-                    t0 = max_nan(t0, LP_FLOOR);
-                    t1 = max_nan(t1, LP_FLOOR);
-                    const f32x2 ex = pack2(ex2(t0), ex2(t1));
-                    s2 = add2(s2, ex);
-                    u2 = fma2(ex, pack2(t0, t1), u2);
-                }
-            }
-        }
-    };
-    int64_t slot = v.first + tid;
-    for (; slot + (LP_UNROLL - 1) * LP_THREADS < v.last; slot += LP_UNROLL * LP_THREADS) {
-        uint4 raw[LP_UNROLL];
-#pragma unroll
-        for (int i = 0; i < LP_UNROLL; ++i) raw[i] = *reinterpret_cast<const uint4*>(v.base + (slot + i * LP_THREADS) * E);
-        tile(raw, LP_UNROLL);
-    }
-    for (; slot < v.last; slot += LP_THREADS) {
-        uint4 raw[LP_UNROLL];
-        raw[0] = *reinterpret_cast<const uint4*>(v.base + slot * E);
-        tile(raw, 1);
+        for (int i = 0; i < LP_UNROLL; ++i) raw[i] = next[i];
     }
     {
         float s0, s1, u0, u1;
@@ -427,7 +488,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(const ForwardArgs 
 #pragma unroll
     for (int w = 1; w < LP_WARPS; ++w) join(total, sh.part[w]);
     __syncthreads();
-    if (a.top) find_top(sh, v, mine, a.top);
+    if (a.top) find_top(sh, v, mine, a.top, turn_shift + 2);
 
     if (parts == 1) {
         const RowResult r = finish(total);
