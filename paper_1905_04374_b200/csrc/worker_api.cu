@@ -110,7 +110,9 @@ int gar_token_logprobs_backward(const gar_logprobs_grad_params_t* p) {
                          span(p->grad_entropy, 1, p->rows, 0, 4), span(p->grad_top, p->rows, p->top, p->top, 4)};
     if (clash(outs, 1, ins, 9)) return GAR_ERR_INVALID_ARG;
     if (p->rows == 0) return GAR_OK;
-    return cuda_status(gar::worker::launch_logprobs_backward(*p, ld, ldo));
+    int sms = 0;
+    if (int rc = sm_count(&sms)) return rc;
+    return cuda_status(gar::worker::launch_logprobs_backward(*p, ld, ldo, sms));
 }
 
 int gar_activation_forward(const gar_activation_params_t* params) {

@@ -116,7 +116,7 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
 
 // ---- launchers (arguments checked by the C entry points) ------------------------------------
 cudaError_t launch_logprobs(const gar_logprobs_params_t& p, int64_t ld, int sm_count);
-cudaError_t launch_logprobs_backward(const gar_logprobs_grad_params_t& p, int64_t ld, int64_t ldo);
+cudaError_t launch_logprobs_backward(const gar_logprobs_grad_params_t& p, int64_t ld, int64_t ldo, int sm_count);
 cudaError_t launch_activation_forward(const gar_activation_params_t& p);
 cudaError_t launch_activation_backward(const gar_activation_grad_params_t& p);
 cudaError_t launch_checkpoint_unpack(int dtype, const gar_checkpoint_t& saved, int64_t rows, int64_t cols, int group, void* x,

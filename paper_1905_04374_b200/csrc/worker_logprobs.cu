@@ -9,8 +9,8 @@
 // a cluster) CTAs through distributed shared memory.
 //
 // The k best entries cost that loop one store: the maximum of every tile of a thread's share (32 bytes
-// to 16 KB).  With j = ceil(k / warps), the j-th largest of a warp's thread maxima, taken as the least
-// over the warps, has at least k entries not below it; only the tiles whose maximum reaches it are read
+// to 16 KB).  With j = ceil(k / warps), the j-th largest of the tile maxima of a warp (two of each thread
+// count), taken as the least over the warps, has at least k entries not below it; only the tiles whose maximum reaches it are read
 // again, about two k of them, and of those the entries that reach it are ranked by counting.  A 64-bit
 // key (value in an order-preserving code, complement of the index) makes the order total: equal values
 // go to the lowest index.  If more entries qualify than the list holds (rows with many equal values,
@@ -28,10 +28,9 @@ namespace {
 constexpr int LP_THREADS = 256;
 constexpr int LP_WARPS = LP_THREADS / 32;
 constexpr int LP_UNROLL = 4;            // 16-byte slots of a thread's turn (find_top's shift counts on 4)
-constexpr int LP_LIST = 512;            // candidate entries of a CTA
 constexpr int LP_TILES = 16;            // tiles of a thread's share
-constexpr int LP_SHARES = 256;          // tiles that are read again
 constexpr int LP_MAX_CLUSTER = 8;
+constexpr int LP_WARP_VOCAB = 16384;    // longest row that one warp takes
 constexpr float LP_FLOOR = -1e4f;       // exponents below this are 0 in fp32
 constexpr float LP_HUGE = 1e30f;        // between -LP_HUGE and LP_HUGE no exponent overflows
 
@@ -118,25 +117,32 @@ struct ForwardArgs {
     int            top;
 };
 
+// The target's logit, asked for before the row is worked on.
+struct Target {
+    int64_t index;               // < 0: none
+    float   x;
+};
 template <typename T>
-__device__ void store_row(const ForwardArgs& a, int64_t row, const RowResult& r) {
+__device__ __forceinline__ Target read_target(const ForwardArgs& a, int64_t row) {
+    Target t{-1, 0.f};
+    if (a.logprobs) {
+        t.index = a.targets[row];
+        if (t.index >= 0 && t.index < a.vocab) t.x = load_one(static_cast<const T*>(a.logits) + row * a.ld, t.index);
+    }
+    return t;
+}
+__device__ __forceinline__ void store_row(const ForwardArgs& a, int64_t row, const RowResult& r, const Target& t) {
     if (a.lse) a.lse[row] = r.lse;
     if (a.lse_lo) a.lse_lo[row] = r.lse_lo;
     if (a.entropy) a.entropy[row] = r.entropy;
-    if (a.logprobs) {
-        const int64_t t = a.targets[row];
-        float lp = 0.f;
-        if (t >= a.vocab) lp = CUDART_NAN_F;
-        else if (t >= 0) lp = logprob_of(r, load_one(static_cast<const T*>(a.logits) + row * a.ld, t));
-        a.logprobs[row] = lp;
-    }
+    if (a.logprobs) a.logprobs[row] = t.index < 0 ? 0.f : t.index >= a.vocab ? CUDART_NAN_F : logprob_of(r, t.x);
 }
 __device__ __forceinline__ void store_top(const ForwardArgs& a, int64_t row, int rank, unsigned long long key, const RowResult& r) {
     a.top_logprobs[row * a.top + rank] = logprob_of(r, value_of(unsigned(key >> 32)));
     a.top_index[row * a.top + rank] = int64_t(0xffffffffu - unsigned(key));
 }
 
-// ---- rows of up to 1024 entries: L lanes hold a row in registers, EPL entries each -------------
+// ---- rows of up to 256 entries: L lanes hold a row in registers, EPL entries each ----------------
 template <typename T, int L, int EPL>
 __global__ void __launch_bounds__(LP_THREADS) logprobs_small_kernel(const ForwardArgs a) {
     const int lane = threadIdx.x % L;
@@ -150,6 +156,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_small_kernel(const Forwar
         const int j = lane + i * L;
         v[i] = j < vocab ? load_one(x, j) : -CUDART_INF_F;
     }
+    const Target target = live && lane == 0 ? read_target<T>(a, row) : Target{-1, 0.f};
     Softmax st{-CUDART_INF_F, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < EPL; ++i) st.m = fmaxf(st.m, v[i]);
@@ -168,39 +175,59 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_small_kernel(const Forwar
         st.u += __shfl_xor_sync(0xffffffffu, st.u, o);
     }
     const RowResult r = finish(st);
-    if (live && lane == 0) store_row<T>(a, row, r);
-    // k rounds: the best key below the previous one
-    unsigned long long last = ~0ull;
+    if (live && lane == 0) store_row(a, row, r, target);
+    if (a.top == 0) return;
+    // a.top rounds: the largest code left, of equal ones the lowest index (an entry that is not there or is
+    // taken has code 0 and index -1)
+    unsigned code[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) code[i] = code_of(v[i]);
+    unsigned gone = 0;
     for (int k = 0; k < a.top; ++k) {
-        unsigned long long best = 0;
+        unsigned best = 0, at = 0xffffffffu;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-            const int j = lane + i * L;
-            const unsigned long long key = j < vocab ? key_of(v[i], unsigned(j)) : 0ull;
-            if (key < last && key > best) best = key;
-        }
+        for (int i = EPL - 1; i >= 0; --i)
+            if (lane + i * L < vocab && !(gone >> i & 1u) && code[i] >= best) {
+                best = code[i];
+                at = unsigned(lane + i * L);
+            }
+        if (L == 32) {
+            const unsigned top = __reduce_max_sync(0xffffffffu, best);
+            at = __reduce_min_sync(0xffffffffu, best == top ? at : 0xffffffffu);
+            best = top;
+        } else {
 #pragma unroll
-        for (int o = L / 2; o; o >>= 1) {
-            const unsigned long long other = shfl_xor64(best, o);
-            if (other > best) best = other;
+            for (int o = L / 2; o; o >>= 1) {
+                const unsigned c2 = __shfl_xor_sync(0xffffffffu, best, o), a2 = __shfl_xor_sync(0xffffffffu, at, o);
+                if (c2 > best || (c2 == best && a2 < at)) {
+                    best = c2;
+                    at = a2;
+                }
+            }
         }
-        if (live && lane == 0) store_top(a, row, k, best, r);
-        last = best;
+        if (int(at % L) == lane) gone |= 1u << (at / L);
+        if (live && lane == 0) store_top(a, row, k, (static_cast<unsigned long long>(best) << 32) | (0xffffffffu - at), r);
     }
 }
 
-// ---- longer rows: a CTA, or a cluster of up to eight, per row ------------------------------------
-struct ForwardShared {
-    float              tile_max[LP_TILES][LP_THREADS];
-    Softmax            part[LP_WARPS];
+// ---- longer rows: a team of WARPS warps per row: one warp, a CTA (eight), or a cluster of up to eight CTAs
+template <int WARPS> struct ForwardShared {
+    static constexpr int LIST = WARPS == 1 ? 256 : 512;         // candidate entries
+    static constexpr int SHARES = WARPS == 1 ? 192 : 256;       // tiles that are read again
+    float              tile_max[LP_TILES][32 * WARPS];
+    Softmax            part[WARPS];
     Softmax            total;                      // of this CTA: read by the cluster's first
-    unsigned           warp_code[LP_WARPS];
-    int                shares[LP_SHARES];          // thread + LP_THREADS * tile
+    unsigned           warp_code[WARPS];
+    int                shares[SHARES];             // thread + threads * tile
     int                nshares, nlist;
-    unsigned long long list[LP_LIST];
+    unsigned long long list[LIST];
     unsigned long long top[GAR_MAX_TOP];           // this CTA's best, in order (0: none): read by the cluster's first
-    unsigned long long warp_key[LP_WARPS];
+    unsigned long long warp_key[WARPS];
 };
+template <int WARPS> __device__ __forceinline__ void team_sync() {
+    if (WARPS == 1) __syncwarp();
+    else __syncthreads();
+}
 
 // A row as 16-byte slots: slot i holds elements [i E - head, (i + 1) E - head); the row's first and
 // last slot may be incomplete and are then read by element ("edge" entries).
@@ -222,8 +249,8 @@ __device__ __forceinline__ RowView<T> view_row(const T* x, int64_t vocab, unsign
     v.base = x - v.head;
     const int64_t whole_first = v.head ? 1 : 0, whole_last = (vocab + v.head) / E;       // complete slots
     const int64_t n = whole_last > whole_first ? whole_last - whole_first : 0;
-    v.first = whole_first + n * rank / parts;
-    v.last = whole_first + n * (rank + 1) / parts;
+    v.first = parts == 1 ? whole_first : whole_first + n * rank / parts;
+    v.last = parts == 1 ? whole_first + n : whole_first + n * (rank + 1) / parts;
     v.lead = v.tail = 0;
     if (rank == 0 && v.head) v.lead = E - v.head;
     if (rank == parts - 1) v.tail = (vocab + v.head) - whole_last * E;
@@ -233,21 +260,22 @@ __device__ __forceinline__ RowView<T> view_row(const T* x, int64_t vocab, unsign
 template <typename T>
 __device__ __forceinline__ int64_t edge_entry(const RowView<T>& v, int tid) {
     if (tid < v.lead) return tid;
-    if (tid >= 32 && tid - 32 < v.tail) return v.vocab - v.tail + (tid - 32);
+    if (tid >= 16 && tid - 16 < v.tail) return v.vocab - v.tail + (tid - 16);
     return -1;
 }
 
-__device__ __forceinline__ void offer(ForwardShared& sh, float x, int64_t idx) {
+template <int WARPS>
+__device__ __forceinline__ void offer(ForwardShared<WARPS>& sh, float x, int64_t idx) {
     const int at = atomicAdd(&sh.nlist, 1);
-    if (at < LP_LIST) sh.list[at] = key_of(x, unsigned(idx));
+    if (at < sh.LIST) sh.list[at] = key_of(x, unsigned(idx));
 }
 
 // best key below `bound` in a thread's share
-template <typename T>
+template <typename T, int THREADS>
 __device__ unsigned long long best_below(const RowView<T>& v, int tid, unsigned long long bound) {
     constexpr int E = Elem<T>::PER16;
     unsigned long long best = 0;
-    for (int64_t slot = v.first + tid; slot < v.last; slot += LP_THREADS) {
+    for (int64_t slot = v.first + tid; slot < v.last; slot += THREADS) {
         float f[E];
         widen16B(*reinterpret_cast<const uint4*>(v.base + slot * E), f, static_cast<const T*>(nullptr));
 #pragma unroll
@@ -265,48 +293,51 @@ __device__ unsigned long long best_below(const RowView<T>& v, int tid, unsigned 
 }
 
 // The CTA's `top` best entries of its part of the row into sh.top, in order (zeros beyond what there
-// is).  `mine`: the largest value of the thread's share; tiles of (1 << shift) slots.
-template <typename T>
-__device__ void find_top(ForwardShared& sh, const RowView<T>& v, float mine, int top, int shift) {
-    constexpr int E = Elem<T>::PER16;
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+// is).  `first`, `second`: the thread's two largest tile maxima; tiles of (1 << shift) slots.
+template <typename T, int WARPS>
+__device__ void find_top(ForwardShared<WARPS>& sh, const RowView<T>& v, float first, float second, int top, int shift) {
+    constexpr int E = Elem<T>::PER16, THREADS = 32 * WARPS;
+    const int tid = threadIdx.x % THREADS, warp = tid / 32, lane = tid % 32;
     if (tid == 0) sh.nshares = sh.nlist = 0;
     if (tid < GAR_MAX_TOP) sh.top[tid] = 0;
-    // warps whose 32 threads all have a slot; a share without a number or with masked entries only counts as 0
+    // warps whose 32 threads all have a slot (a team of one warp may have idle lanes: they count as 0); a share without a number or with masked entries only counts as 0
     const int64_t slots = v.last - v.first;
-    const int full = slots >= LP_THREADS ? LP_WARPS : int(slots / 32);
-    const unsigned own = mine == -CUDART_INF_F ? 0u : code_of(mine);
+    const int full = WARPS == 1 ? 1 : slots >= THREADS ? WARPS : int(slots / 32);
+    const unsigned own = first == -CUDART_INF_F ? 0u : code_of(first);
     unsigned least = 0xffffffffu;
     if (warp < full) {
-        unsigned rest = own;
+        unsigned rest = own, again = second == -CUDART_INF_F ? 0u : code_of(second);
         for (int j = (top + full - 1) / full; j > 0; --j) {
             least = __reduce_max_sync(0xffffffffu, rest);
-            if (lane == __ffs(__ballot_sync(0xffffffffu, rest == least)) - 1) rest = 0u;
+            if (lane == __ffs(__ballot_sync(0xffffffffu, rest == least)) - 1) {
+                rest = again;
+                again = 0u;
+            }
         }
     }
     if (lane == 0) sh.warp_code[warp] = least;
-    __syncthreads();
+    team_sync<WARPS>();
     unsigned low = full ? sh.warp_code[0] : 0u;
     for (int w = 1; w < full; ++w) low = min(low, sh.warp_code[w]);
-    const int64_t edge = edge_entry(v, tid);
     if (own >= low) {
-        const int tiles = int((slots - tid + LP_THREADS - 1) / LP_THREADS + (1 << shift) - 1) >> shift;      // of this thread
+        const int tiles = int((slots - tid + THREADS - 1) / THREADS + (1 << shift) - 1) >> shift;      // of this thread
         for (int i = 0; i < tiles; ++i)
             if (low == 0u || code_of(sh.tile_max[i][tid]) >= low) {
                 const int at = atomicAdd(&sh.nshares, 1);
-                if (at < LP_SHARES) sh.shares[at] = tid + LP_THREADS * i;
+                if (at < sh.SHARES) sh.shares[at] = tid + THREADS * i;
             }
-        if (edge >= 0) {
-            const float f = load_one(v.x, edge);
-            if (code_of(f) >= low) offer(sh, f, edge);
-        }
     }
-    __syncthreads();
+    const int64_t edge = edge_entry(v, tid);
+    if (edge >= 0) {
+        const float f = load_one(v.x, edge);
+        if (code_of(f) >= low) offer(sh, f, edge);
+    }
+    team_sync<WARPS>();
     const int nshares = sh.nshares;
-    if (nshares <= LP_SHARES) {
-        for (int i = tid; i < nshares << shift; i += LP_THREADS) {
+    if (nshares <= sh.SHARES) {
+        for (int i = tid; i < nshares << shift; i += THREADS) {
             const int share = sh.shares[i >> shift];
-            const int64_t slot = v.first + share % LP_THREADS + int64_t(((share / LP_THREADS) << shift) + (i & ((1 << shift) - 1))) * LP_THREADS;
+            const int64_t slot = v.first + share % THREADS + int64_t(((share / THREADS) << shift) + (i & ((1 << shift) - 1))) * THREADS;
             if (slot < v.last) {
                 float f[E];
                 widen16B(*reinterpret_cast<const uint4*>(v.base + slot * E), f, static_cast<const T*>(nullptr));
@@ -316,20 +347,20 @@ __device__ void find_top(ForwardShared& sh, const RowView<T>& v, float mine, int
             }
         }
     }
-    __syncthreads();
+    team_sync<WARPS>();
     const int nlist = sh.nlist;
-    if (nshares <= LP_SHARES && nlist <= LP_LIST) {
-        for (int i = tid; i < nlist; i += LP_THREADS) {
+    if (nshares <= sh.SHARES && nlist <= sh.LIST) {
+        for (int i = tid; i < nlist; i += THREADS) {
             const unsigned long long key = sh.list[i];
             int rank = 0;
             for (int j = 0; j < nlist; ++j) rank += sh.list[j] > key;
             if (rank < top) sh.top[rank] = key;
         }
-        __syncthreads();
+        team_sync<WARPS>();
         return;
     }
     // too many equal values for the list: one by one
-    unsigned long long cur = best_below(v, tid, ~0ull);
+    unsigned long long cur = best_below<T, THREADS>(v, tid, ~0ull);
     for (int k = 0; k < top; ++k) {
         unsigned long long best = cur;
 #pragma unroll
@@ -338,13 +369,13 @@ __device__ void find_top(ForwardShared& sh, const RowView<T>& v, float mine, int
             if (other > best) best = other;
         }
         if (lane == 0) sh.warp_key[warp] = best;
-        __syncthreads();
+        team_sync<WARPS>();
         best = sh.warp_key[0];
 #pragma unroll
-        for (int w = 1; w < LP_WARPS; ++w) best = sh.warp_key[w] > best ? sh.warp_key[w] : best;
+        for (int w = 1; w < WARPS; ++w) best = sh.warp_key[w] > best ? sh.warp_key[w] : best;
         if (tid == 0) sh.top[k] = best;
-        if (best != 0 && cur == best) cur = best_below(v, tid, best);
-        __syncthreads();
+        if (best != 0 && cur == best) cur = best_below<T, THREADS>(v, tid, best);
+        team_sync<WARPS>();
     }
 }
 
@@ -414,41 +445,51 @@ __device__ __forceinline__ void add_tile(const uint4 (&raw)[LP_UNROLL], float ce
 // Bound by memory for 16-bit logits as long as the loop stays under the issue rate: per entry about one
 // exponential (of 16 a cycle and SM, 1.4 at the memory's rate) and five instructions.  The next tile's
 // loads are in flight while a tile is worked on.
-template <typename T>
+template <typename T, int WARPS>
 __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const ForwardArgs a, int parts) {
-    constexpr int E = Elem<T>::PER16;
-    __shared__ __align__(16) ForwardShared sh;
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    const unsigned rank = blockIdx.x % unsigned(parts);
-    const int64_t row = blockIdx.x / unsigned(parts);
+    constexpr int E = Elem<T>::PER16, THREADS = 32 * WARPS, TEAMS = LP_THREADS / THREADS;
+    __shared__ __align__(16) ForwardShared<WARPS> shared[TEAMS];
+    ForwardShared<WARPS>& sh = shared[threadIdx.x / THREADS];
+    const int tid = threadIdx.x % THREADS, warp = tid / 32, lane = tid % 32;
+    if (WARPS == 1) parts = 1;                                   // a cluster has CTAs for teams
+    const unsigned rank = WARPS == 1 ? 0u : blockIdx.x % unsigned(parts);
+    const int64_t row = int64_t(WARPS == 1 ? blockIdx.x : blockIdx.x / unsigned(parts)) * TEAMS + threadIdx.x / THREADS;
+    if (TEAMS > 1 && row >= a.rows) return;
     const RowView<T> v = view_row(static_cast<const T*>(a.logits) + row * a.ld, a.vocab, rank, unsigned(parts));
 
     // turns of LP_UNROLL slots per thread; a tile is (1 << turn_shift) turns
-    const int turns = int((v.last - v.first + LP_UNROLL * LP_THREADS - 1) / (LP_UNROLL * LP_THREADS));
+    const int turns = int((v.last - v.first + LP_UNROLL * THREADS - 1) / (LP_UNROLL * THREADS));
     int turn_shift = 0;
     while ((turns + (1 << turn_shift) - 1) >> turn_shift > LP_TILES) ++turn_shift;
 
     Softmax st{-CUDART_INF_F, 0.f, 0.f};
     f32x2 s2 = pack2(0.f, 0.f), u2 = pack2(0.f, 0.f);
     const T* at = v.base + (v.first + tid) * E;
-    int64_t left = v.last - v.first - tid;                       // slots from `at` on, at a stride of LP_THREADS
+    int64_t left = v.last - v.first - tid;                       // slots from `at` on, at a stride of THREADS
     auto fetch = [&](uint4 (&raw)[LP_UNROLL]) {
 #pragma unroll
         for (int i = 0; i < LP_UNROLL; ++i)
-            raw[i] = left > i * LP_THREADS ? load_stream(at + i * LP_THREADS * E) : nothing<T>();
-        at += LP_UNROLL * LP_THREADS * E;
-        left -= LP_UNROLL * LP_THREADS;
+            raw[i] = left > i * THREADS ? load_stream(at + i * THREADS * E) : nothing<T>();
+        at += LP_UNROLL * THREADS * E;
+        left -= LP_UNROLL * THREADS;
     };
     uint4 raw[LP_UNROLL], next[LP_UNROLL];
-    float tile_top = -CUDART_INF_F;
+    float tile_top = -CUDART_INF_F, first = -CUDART_INF_F, second = -CUDART_INF_F;
     if (turns > 0) fetch(raw);
+    const Target target = tid == 0 && rank == 0 ? read_target<T>(a, row) : Target{-1, 0.f};      // behind the first loads
     for (int turn = 0; turn < turns; ++turn) {
         if (turn + 1 < turns) fetch(next);
         float top;
         bool masked;
         tile_range(raw, top, masked, static_cast<const T*>(nullptr));
-        tile_top = (turn & ((1 << turn_shift) - 1)) ? fmaxf(tile_top, top) : top;
-        if (a.top) sh.tile_max[turn >> turn_shift][tid] = tile_top;
+        if (a.top) {
+            tile_top = (turn & ((1 << turn_shift) - 1)) ? fmaxf(tile_top, top) : top;
+            sh.tile_max[turn >> turn_shift][tid] = tile_top;
+            if (turn + 1 == turns || ((turn + 1) & ((1 << turn_shift) - 1)) == 0) {      // the tile's last turn
+                second = fmaxf(second, fminf(first, tile_top));
+                first = fmaxf(first, tile_top);
+            }
+        }
         if (top > st.m) {
             float s0, s1, u0, u1;
             unpack2(s2, s0, s1);
@@ -473,7 +514,6 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const ForwardAr
     }
     const int64_t edge = edge_entry(v, tid);
     if (edge >= 0) add_one(st, load_one(v.x, edge));
-    const float mine = st.m;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         Softmax b;
@@ -482,17 +522,20 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const ForwardAr
         b.u = __shfl_xor_sync(0xffffffffu, st.u, o);
         join(st, b);
     }
-    if (lane == 0) sh.part[warp] = st;
-    __syncthreads();
-    Softmax total = sh.part[0];
+    Softmax total = st;
+    if (WARPS > 1) {
+        if (lane == 0) sh.part[warp] = st;
+        __syncthreads();
+        total = sh.part[0];
 #pragma unroll
-    for (int w = 1; w < LP_WARPS; ++w) join(total, sh.part[w]);
-    __syncthreads();
-    if (a.top) find_top(sh, v, mine, a.top, turn_shift + 2);
+        for (int w = 1; w < WARPS; ++w) join(total, sh.part[w]);
+        __syncthreads();
+    }
+    if (a.top) find_top<T, WARPS>(sh, v, first, second, a.top, turn_shift + 2);
 
-    if (parts == 1) {
+    if (WARPS == 1 || parts == 1) {
         const RowResult r = finish(total);
-        if (tid == 0) store_row<T>(a, row, r);
+        if (tid == 0) store_row(a, row, r, target);
         if (tid < a.top) store_top(a, row, tid, sh.top[tid], r);
         return;
     }
@@ -503,7 +546,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const ForwardAr
     if (rank == 0) {
         for (int p = 1; p < parts; ++p) join(total, cluster.map_shared_rank(&sh, p)->total);
         const RowResult r = finish(total);
-        if (tid == 0) store_row<T>(a, row, r);
+        if (tid == 0) store_row(a, row, r, target);
         if (a.top) {
             const int n = parts * a.top;               // at most 256 = one entry per thread
             unsigned long long key = 0;
@@ -522,15 +565,23 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const ForwardAr
 
 template <typename T>
 cudaError_t forward(const ForwardArgs& a, int sm_count, cudaStream_t stream) {
-    if (a.vocab <= 1024) {
+    if (a.vocab <= 256) {
         const int lanes = a.vocab <= 64 ? 8 : 32;
         const int64_t blocks = (a.rows + LP_THREADS / lanes - 1) / (LP_THREADS / lanes);
         if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-        const unsigned g = unsigned(blocks);
-        if (a.vocab <= 16) logprobs_small_kernel<T, 8, 2><<<g, LP_THREADS, 0, stream>>>(a);
-        else if (a.vocab <= 64) logprobs_small_kernel<T, 8, 8><<<g, LP_THREADS, 0, stream>>>(a);
-        else if (a.vocab <= 256) logprobs_small_kernel<T, 32, 8><<<g, LP_THREADS, 0, stream>>>(a);
-        else logprobs_small_kernel<T, 32, 32><<<g, LP_THREADS, 0, stream>>>(a);
+        const unsigned n = unsigned(blocks);
+        if (a.vocab <= 16) logprobs_small_kernel<T, 8, 2><<<n, LP_THREADS, 0, stream>>>(a);
+        else if (a.vocab <= 64) logprobs_small_kernel<T, 8, 8><<<n, LP_THREADS, 0, stream>>>(a);
+        else if (a.vocab <= 128) logprobs_small_kernel<T, 32, 4><<<n, LP_THREADS, 0, stream>>>(a);
+        else logprobs_small_kernel<T, 32, 8><<<n, LP_THREADS, 0, stream>>>(a);
+        return cudaGetLastError();
+    }
+    // A warp per row has no barriers: it is the faster team as long as the rows give every SM eight of
+    // them, or the row is no more than a turn.
+    if (a.vocab <= 1024 || (a.vocab <= LP_WARP_VOCAB && a.rows >= 8 * int64_t(sm_count))) {
+        const int64_t blocks = (a.rows + LP_WARPS - 1) / LP_WARPS;
+        if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+        logprobs_kernel<T, 1><<<unsigned(blocks), LP_THREADS, 0, stream>>>(a, 1);
         return cudaGetLastError();
     }
     // A row is split over a cluster while that still leaves SMs without work and every CTA a tile
@@ -549,7 +600,7 @@ cudaError_t forward(const ForwardArgs& a, int sm_count, cudaStream_t stream) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = parts > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, logprobs_kernel<T>, a, parts);
+    return cudaLaunchKernelEx(&cfg, logprobs_kernel<T, LP_WARPS>, a, parts);
 }
 
 // ---- gradient --------------------------------------------------------------------------------
@@ -564,40 +615,49 @@ struct BackwardArgs {
     int            top;
 };
 
-// A row's constants and the entries that carry a term of their own.
+// A row's constants, and this lane's special entry (one of the top alternatives).
 struct RowGrad {
     float   lse, lse_lo, entropy, c, sum;  // sum = a + sum_i b_i
     bool    empty;
+    float   a;                             // gradient of the target's log probability
+    int64_t target;                        // -1: none
+    int64_t at;                            // lane i: top_index[i], -1 beyond the list
+    float   b;                             // its gradient
 };
-
-// entry `i` of a row's list of special entries: the target (i = 0) and the top alternatives
-__device__ __forceinline__ int64_t special_index(const BackwardArgs& g, int64_t row, int i) {
-    if (i == 0) {
-        const int64_t t = g.grad_logprobs ? g.targets[row] : -1;
-        return t >= 0 ? t : -1;
-    }
-    return g.top_index[row * g.top + i - 1];
-}
-__device__ __forceinline__ float special_grad(const BackwardArgs& g, int64_t row, int i) {
-    return i == 0 ? g.grad_logprobs[row] : g.grad_top[row * g.top + i - 1];
-}
-__device__ __forceinline__ RowGrad row_grad(const BackwardArgs& g, int64_t row) {
+// All 32 lanes of a warp call.
+__device__ __forceinline__ RowGrad row_grad(const BackwardArgs& g, int64_t row, int lane) {
     RowGrad r;
     r.lse = g.lse[row];
     r.lse_lo = g.lse_lo ? g.lse_lo[row] : 0.f;
     r.empty = r.lse == -CUDART_INF_F;
     r.c = g.grad_entropy ? g.grad_entropy[row] : 0.f;
     r.entropy = g.grad_entropy ? g.entropy[row] : 0.f;
-    r.sum = 0.f;
+    r.target = -1;
+    r.a = 0.f;
     if (g.grad_logprobs) {
         const int64_t t = g.targets[row];
-        if (t >= g.vocab) r.sum = CUDART_NAN_F;
-        else if (t >= 0) r.sum = g.grad_logprobs[row];
+        if (t >= g.vocab) r.a = CUDART_NAN_F;
+        else if (t >= 0) {
+            r.target = t;
+            r.a = g.grad_logprobs[row];
+        }
     }
-    for (int i = 0; i < g.top; ++i) {
-        const int64_t t = g.top_index[row * g.top + i];
-        r.sum += (t < 0 || t >= g.vocab) ? CUDART_NAN_F : g.grad_top[row * g.top + i];
+    r.at = -1;
+    r.b = 0.f;
+    if (lane < g.top) {
+        r.at = g.top_index[row * g.top + lane];
+        r.b = g.grad_top[row * g.top + lane];
+        if (r.at < 0 || r.at >= g.vocab) {
+            r.at = -1;
+            r.b = CUDART_NAN_F;
+        }
     }
+    r.sum = r.b;
+    if (g.top) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) r.sum += __shfl_xor_sync(0xffffffffu, r.sum, o);
+    }
+    r.sum += r.a;
     return r;
 }
 __device__ __forceinline__ float grad_at(const RowGrad& r, float x) {
@@ -607,118 +667,153 @@ __device__ __forceinline__ float grad_at(const RowGrad& r, float x) {
     return r.empty ? 0.f : d;
 }
 
-// gradient of special entry i, its base value included: the terms of every special entry at the same place
+// The special entries of a row: their logits, read before anything is written (dx may be x), and their
+// gradients, written over the plain ones.  A place that occurs more than once gets every term, in one
+// order, whoever writes it.  Entries outside [lo, hi) are somebody else's.
+struct Special {
+    float x, x_target;
+};
 template <typename T>
-__device__ __forceinline__ float special_value(const BackwardArgs& g, int64_t row, const RowGrad& r, int64_t at, float x) {
-    float d = grad_at(r, x);
-    if (r.empty) return 0.f;
-    for (int i = 0; i <= g.top; ++i)
-        if (special_index(g, row, i) == at) d += special_grad(g, row, i);
-    return d;
+__device__ __forceinline__ Special read_special(const RowGrad& r, const T* x, int64_t lo, int64_t hi) {
+    Special s{0.f, 0.f};
+    if (r.at >= lo && r.at < hi) s.x = load_one(x, r.at);
+    if (r.target >= lo && r.target < hi) s.x_target = load_one(x, r.target);
+    return s;
+}
+template <typename T>
+__device__ __forceinline__ void write_special(const BackwardArgs& g, const RowGrad& r, const Special& s, T* dx, int64_t lo, int64_t hi, int lane) {
+    const bool here = (r.at >= lo && r.at < hi) || (r.target >= lo && r.target < hi);
+    if (r.empty || !__any_sync(0xffffffffu, here)) return;
+    float own = grad_at(r, s.x), target = grad_at(r, s.x_target);
+    for (int j = 0; j < g.top; ++j) {
+        const int64_t at = __shfl_sync(0xffffffffu, r.at, j);
+        const float b = __shfl_sync(0xffffffffu, r.b, j);
+        if (at == r.at) own += b;
+        if (at == r.target) target += b;
+    }
+    if (r.at == r.target) own += r.a;
+    target += r.a;
+    if (r.at >= 0 && r.at >= lo && r.at < hi) dx[r.at] = Elem<T>::narrow(own);
+    if (lane == 0 && r.target >= 0 && r.target >= lo && r.target < hi) dx[r.target] = Elem<T>::narrow(target);
 }
 
-// Rows of up to 1024 entries: L lanes per row.
-template <typename T, int L>
+// Rows of up to 64 entries: eight lanes per row, plain accesses; every lane adds the special terms to
+// its own entries.
+template <typename T>
 __global__ void __launch_bounds__(LP_THREADS) logprobs_backward_small_kernel(const BackwardArgs g) {
+    constexpr int L = 8, EPL = 8;
     const int lane = threadIdx.x % L;
     const int64_t row = (int64_t(blockIdx.x) * LP_THREADS + threadIdx.x) / L;
-    const bool live = row < g.rows;
-    const T* x = static_cast<const T*>(g.logits) + (live ? row : 0) * g.ld;
-    T* dx = static_cast<T*>(g.dlogits) + (live ? row : 0) * g.ldo;
-    // the special entries' logits are read before anything is written: dx may be x
-    constexpr int MINE = (GAR_MAX_TOP + L) / L;
-    float at_x[MINE];
-    int64_t at[MINE];
-    RowGrad r{};
-    if (live) {
-        r = row_grad(g, row);
+    if (row >= g.rows) return;
+    const T* x = static_cast<const T*>(g.logits) + row * g.ld;
+    T* dx = static_cast<T*>(g.dlogits) + row * g.ldo;
+    const int vocab = int(g.vocab);
+    float v[EPL], extra[EPL];
 #pragma unroll
-        for (int q = 0; q < MINE; ++q) {
-            const int i = lane + q * L;
-            at[q] = i <= g.top ? special_index(g, row, i) : -1;
-            if (at[q] >= g.vocab) at[q] = -1;
-            at_x[q] = at[q] >= 0 ? load_one(x, at[q]) : 0.f;
-        }
+    for (int i = 0; i < EPL; ++i) {
+        v[i] = lane + i * L < vocab ? load_one(x, lane + i * L) : 0.f;
+        extra[i] = 0.f;
     }
-    __syncwarp();
-    if (live)
-        for (int64_t j = lane; j < g.vocab; j += L) dx[j] = Elem<T>::narrow(grad_at(r, load_one(x, j)));
-    __syncwarp();
-    if (live) {
+    RowGrad r;
+    r.lse = g.lse[row];
+    r.lse_lo = g.lse_lo ? g.lse_lo[row] : 0.f;
+    r.empty = r.lse == -CUDART_INF_F;
+    r.c = g.grad_entropy ? g.grad_entropy[row] : 0.f;
+    r.entropy = g.grad_entropy ? g.entropy[row] : 0.f;
+    r.sum = 0.f;
+    auto term = [&](int64_t at, float value) {
+        r.sum += at < vocab ? value : CUDART_NAN_F;
 #pragma unroll
-        for (int q = 0; q < MINE; ++q)
-            if (at[q] >= 0) dx[at[q]] = Elem<T>::narrow(special_value<T>(g, row, r, at[q], at_x[q]));
+        for (int i = 0; i < EPL; ++i)
+            if (at == lane + i * L) extra[i] += value;
+    };
+    for (int j = 0; j < g.top; ++j) {
+        const int64_t at = g.top_index[row * g.top + j];
+        term(at < 0 ? vocab : at, g.grad_top[row * g.top + j]);
     }
+    if (g.grad_logprobs && g.targets[row] >= 0) term(g.targets[row], g.grad_logprobs[row]);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+        if (lane + i * L < vocab) dx[lane + i * L] = Elem<T>::narrow(r.empty ? 0.f : grad_at(r, v[i]) + extra[i]);
 }
 
-// Longer rows: a CTA takes LPB_SLOTS 16-byte slots per thread of one row.  The special entries are
-// overwritten after a barrier (the CTA that owns an entry owns all writes to it).
+// Longer rows: a team of WARPS warps takes LPB_SLOTS 16-byte slots per thread of a row at a time: a
+// CTA one such chunk, a warp (a row of its own) one after the other.
 constexpr int LPB_SLOTS = 4;
 
-template <typename T>
+template <typename T, int WARPS>
 __global__ void __launch_bounds__(LP_THREADS) logprobs_backward_kernel(const BackwardArgs g, unsigned chunks) {
-    constexpr int E = Elem<T>::PER16;
-    const int tid = threadIdx.x;
-    const int64_t row = blockIdx.x / chunks;
-    const unsigned chunk = blockIdx.x % chunks;
+    constexpr int E = Elem<T>::PER16, THREADS = 32 * WARPS, TEAMS = LP_THREADS / THREADS;
+    const int tid = threadIdx.x % THREADS, lane = threadIdx.x % 32;
+    const int64_t row = TEAMS > 1 ? int64_t(blockIdx.x) * TEAMS + threadIdx.x / THREADS : blockIdx.x / chunks;
+    if (TEAMS > 1 && row >= g.rows) return;
+    const unsigned first = TEAMS > 1 ? 0u : blockIdx.x % chunks, last = TEAMS > 1 ? chunks : first + 1u;
     const T* x = static_cast<const T*>(g.logits) + row * g.ld;
     T* dx = static_cast<T*>(g.dlogits) + row * g.ldo;
     const int head = int((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
     const bool together = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 15) == 0;
     // slot i: elements [i E - head, (i + 1) E - head)
-    const int64_t slot0 = int64_t(chunk) * (LP_THREADS * LPB_SLOTS) + tid;
-    const int64_t lo = int64_t(chunk) * (LP_THREADS * LPB_SLOTS * E) - head;
-    const int64_t hi = lo + LP_THREADS * LPB_SLOTS * E;
+    const int64_t lo = int64_t(first) * (THREADS * LPB_SLOTS * E) - head;
+    const int64_t hi = min(int64_t(last) * (THREADS * LPB_SLOTS * E) - head, g.vocab);
 
     uint4 raw[LPB_SLOTS];
     bool whole[LPB_SLOTS];
+    auto fetch = [&](unsigned chunk) {
+        const int64_t slot0 = int64_t(chunk) * (THREADS * LPB_SLOTS) + tid;
 #pragma unroll
-    for (int i = 0; i < LPB_SLOTS; ++i) {
-        const int64_t j = (slot0 + i * LP_THREADS) * E - head;
-        whole[i] = together && j >= 0 && j + E <= g.vocab;
-        if (whole[i]) raw[i] = load_stream(x + j);
-    }
-    const RowGrad r = row_grad(g, row);
-    int64_t at = -1;
-    float at_x = 0.f;
-    if (tid <= g.top) {
-        at = special_index(g, row, tid);
-        if (at < lo || at >= hi || at >= g.vocab) at = -1;
-        if (at >= 0) at_x = load_one(x, at);
-    }
-    __syncthreads();                      // read before anything is written: dx may be x
+        for (int i = 0; i < LPB_SLOTS; ++i) {
+            const int64_t j = (slot0 + i * THREADS) * E - head;
+            whole[i] = together && j >= 0 && j + E <= g.vocab;
+            if (whole[i]) raw[i] = load_stream(x + j);
+        }
+    };
+    fetch(first);
+    const RowGrad r = row_grad(g, row, lane);
+    const Special s = read_special<T>(r, x, lo, hi);
+    if (WARPS == 1) __syncwarp();
+    else __syncthreads();                 // read before anything is written: dx may be x
+    for (unsigned chunk = first; chunk < last; ++chunk) {
+        if (chunk > first) fetch(chunk);
+        const int64_t slot0 = int64_t(chunk) * (THREADS * LPB_SLOTS) + tid;
 #pragma unroll
-    for (int i = 0; i < LPB_SLOTS; ++i) {
-        const int64_t j = (slot0 + i * LP_THREADS) * E - head;
-        if (whole[i]) {
-            float f[E];
-            widen16B(raw[i], f, static_cast<const T*>(nullptr));
+        for (int i = 0; i < LPB_SLOTS; ++i) {
+            const int64_t j = (slot0 + i * THREADS) * E - head;
+            if (whole[i]) {
+                float f[E];
+                widen16B(raw[i], f, static_cast<const T*>(nullptr));
 #pragma unroll
-            for (int e = 0; e < E; ++e) f[e] = grad_at(r, f[e]);
-            store_stream(dx + j, narrow16B(f, static_cast<const T*>(nullptr)));
-        } else {
-            for (int e = 0; e < E; ++e)
-                if (j + e >= 0 && j + e < g.vocab) dx[j + e] = Elem<T>::narrow(grad_at(r, load_one(x, j + e)));
+                for (int e = 0; e < E; ++e) f[e] = grad_at(r, f[e]);
+                store_stream(dx + j, narrow16B(f, static_cast<const T*>(nullptr)));
+            } else if (j < g.vocab) {
+                for (int e = 0; e < E; ++e)
+                    if (j + e >= 0 && j + e < g.vocab) dx[j + e] = Elem<T>::narrow(grad_at(r, load_one(x, j + e)));
+            }
         }
     }
-    __syncthreads();
-    if (at >= 0) dx[at] = Elem<T>::narrow(special_value<T>(g, row, r, at, at_x));
+    if (WARPS == 1) __syncwarp();
+    else __syncthreads();
+    if (threadIdx.x % THREADS < 32) write_special<T>(g, r, s, dx, lo, hi, lane);
 }
 
 template <typename T>
-cudaError_t backward(const BackwardArgs& g, cudaStream_t stream) {
-    if (g.vocab <= 1024) {
-        const int lanes = g.vocab <= 64 ? 8 : 32;
-        const int64_t blocks = (g.rows + LP_THREADS / lanes - 1) / (LP_THREADS / lanes);
+cudaError_t backward(const BackwardArgs& g, int sm_count, cudaStream_t stream) {
+    if (g.vocab <= 64) {
+        const int64_t blocks = (g.rows + LP_THREADS / 8 - 1) / (LP_THREADS / 8);
         if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-        if (lanes == 8) logprobs_backward_small_kernel<T, 8><<<unsigned(blocks), LP_THREADS, 0, stream>>>(g);
-        else logprobs_backward_small_kernel<T, 32><<<unsigned(blocks), LP_THREADS, 0, stream>>>(g);
+        logprobs_backward_small_kernel<T><<<unsigned(blocks), LP_THREADS, 0, stream>>>(g);
         return cudaGetLastError();
     }
-    constexpr int64_t per = int64_t(LP_THREADS) * LPB_SLOTS * Elem<T>::PER16;
-    const int64_t chunks = (g.vocab + Elem<T>::PER16 - 1 + per - 1) / per;      // with the largest head
+    constexpr int E = Elem<T>::PER16;
+    const int64_t slots = (g.vocab + E - 1) / E + 1;                          // with the largest head
+    if (g.vocab <= 1024 || (g.vocab <= LP_WARP_VOCAB / 4 && g.rows >= 8 * int64_t(sm_count))) {
+        const int64_t blocks = (g.rows + LP_WARPS - 1) / LP_WARPS;
+        if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+        logprobs_backward_kernel<T, 1><<<unsigned(blocks), LP_THREADS, 0, stream>>>(g, unsigned((slots + 32 * LPB_SLOTS - 1) / (32 * LPB_SLOTS)));
+        return cudaGetLastError();
+    }
+    const int64_t chunks = (slots + LP_THREADS * LPB_SLOTS - 1) / (LP_THREADS * LPB_SLOTS);
     if (g.rows * chunks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    logprobs_backward_kernel<T><<<unsigned(g.rows * chunks), LP_THREADS, 0, stream>>>(g, unsigned(chunks));
+    logprobs_backward_kernel<T, LP_WARPS><<<unsigned(g.rows * chunks), LP_THREADS, 0, stream>>>(g, unsigned(chunks));
     return cudaGetLastError();
 }
 
@@ -732,13 +827,13 @@ cudaError_t launch_logprobs(const gar_logprobs_params_t& p, int64_t ld, int sm_c
     return forward<__half>(a, sm_count, s);
 }
 
-cudaError_t launch_logprobs_backward(const gar_logprobs_grad_params_t& p, int64_t ld, int64_t ldo) {
+cudaError_t launch_logprobs_backward(const gar_logprobs_grad_params_t& p, int64_t ld, int64_t ldo, int sm_count) {
     const BackwardArgs g{p.logits, p.dlogits, p.rows, p.vocab, ld, ldo, p.targets, p.lse, p.lse_lo, p.entropy, p.top_index,
                          p.grad_logprobs, p.grad_entropy, p.grad_top, p.top};
     cudaStream_t s = static_cast<cudaStream_t>(p.stream);
-    if (p.dtype == GAR_F32) return backward<float>(g, s);
-    if (p.dtype == GAR_BF16) return backward<__nv_bfloat16>(g, s);
-    return backward<__half>(g, s);
+    if (p.dtype == GAR_F32) return backward<float>(g, sm_count, s);
+    if (p.dtype == GAR_BF16) return backward<__nv_bfloat16>(g, sm_count, s);
+    return backward<__half>(g, sm_count, s);
 }
 
 }  // namespace worker
