@@ -224,6 +224,8 @@ template <int WARPS> struct ForwardShared {
     unsigned long long top[GAR_MAX_TOP];           // this CTA's best, in order (0: none): read by the cluster's first
     unsigned long long warp_key[WARPS];
 };
+// Threads of a CTA whose teams have WARPS warps: eight teams of a warp, or one team.
+__host__ __device__ constexpr int cta_threads(int warps) { return warps == 1 ? 256 : 32 * warps; }
 template <int WARPS> __device__ __forceinline__ void team_sync() {
     if (WARPS == 1) __syncwarp();
     else __syncthreads();
@@ -446,8 +448,8 @@ __device__ __forceinline__ void add_tile(const uint4 (&raw)[LP_UNROLL], float ce
 // exponential (of 16 a cycle and SM, 1.4 at the memory's rate) and five instructions.  The next tile's
 // loads are in flight while a tile is worked on.
 template <typename T, int WARPS>
-__global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const ForwardArgs a, int parts) {
-    constexpr int E = Elem<T>::PER16, THREADS = 32 * WARPS, TEAMS = LP_THREADS / THREADS;
+__global__ void __launch_bounds__(cta_threads(WARPS), 1024 / cta_threads(WARPS)) logprobs_kernel(const ForwardArgs a, int parts) {
+    constexpr int E = Elem<T>::PER16, THREADS = 32 * WARPS, TEAMS = cta_threads(WARPS) / THREADS;
     __shared__ __align__(16) ForwardShared<WARPS> shared[TEAMS];
     ForwardShared<WARPS>& sh = shared[threadIdx.x / THREADS];
     const int tid = threadIdx.x % THREADS, warp = tid / 32, lane = tid % 32;
@@ -584,6 +586,13 @@ cudaError_t forward(const ForwardArgs& a, int sm_count, cudaStream_t stream) {
         logprobs_kernel<T, 1><<<unsigned(blocks), LP_THREADS, 0, stream>>>(a, 1);
         return cudaGetLastError();
     }
+    // Long rows, enough of them: half a CTA's worth of threads per row, so that twice as many rows are in
+    // work on an SM and the end of one (reductions, the top alternatives) hides behind the others
+    if (a.rows >= 8 * int64_t(sm_count)) {
+        if (a.rows > 0x7fffffff) return cudaErrorInvalidConfiguration;
+        logprobs_kernel<T, 4><<<unsigned(a.rows), cta_threads(4), 0, stream>>>(a, 1);
+        return cudaGetLastError();
+    }
     // A row is split over a cluster while that still leaves SMs without work and every CTA a tile
     // of its own (LP_UNROLL slots per thread).
     int parts = 1;
@@ -624,12 +633,19 @@ struct RowGrad {
     int64_t at;                            // lane i: top_index[i], -1 beyond the list
     float   b;                             // its gradient
 };
+// What grad_at reads, from the sums: dx = p (c' log p + sum'), c' = -c, sum' = -(sum + c H).  An empty row
+// (lse = -inf) gets lse = +inf: every p is 0.
+__device__ __forceinline__ void settle(RowGrad& r) {
+    r.empty = r.lse == -CUDART_INF_F;
+    if (r.empty) r.lse = CUDART_INF_F;
+    r.sum = -fmaf(r.c, r.entropy, r.sum);
+    r.c = -r.c;
+}
 // All 32 lanes of a warp call.
 __device__ __forceinline__ RowGrad row_grad(const BackwardArgs& g, int64_t row, int lane) {
     RowGrad r;
     r.lse = g.lse[row];
     r.lse_lo = g.lse_lo ? g.lse_lo[row] : 0.f;
-    r.empty = r.lse == -CUDART_INF_F;
     r.c = g.grad_entropy ? g.grad_entropy[row] : 0.f;
     r.entropy = g.grad_entropy ? g.entropy[row] : 0.f;
     r.target = -1;
@@ -658,13 +674,22 @@ __device__ __forceinline__ RowGrad row_grad(const BackwardArgs& g, int64_t row, 
         for (int o = 16; o; o >>= 1) r.sum += __shfl_xor_sync(0xffffffffu, r.sum, o);
     }
     r.sum += r.a;
+    settle(r);
     return r;
 }
 __device__ __forceinline__ float grad_at(const RowGrad& r, float x) {
     const float lp = max_nan((x - r.lse) - r.lse_lo, LP_FLOOR);
-    const float p = ex2(lp * kLog2e);
-    const float d = -p * fmaf(r.c, lp + r.entropy, r.sum);
-    return r.empty ? 0.f : d;
+    return ex2(lp * kLog2e) * fmaf(r.c, lp, r.sum);
+}
+// the same for two entries
+__device__ __forceinline__ void grad_at2(const RowGrad& r, float& x0, float& x1) {
+    float a, b;
+    unpack2(add2(add2(pack2(x0, x1), pack2(-r.lse, -r.lse)), pack2(-r.lse_lo, -r.lse_lo)), a, b);
+    a = max_nan(a, LP_FLOOR);
+    b = max_nan(b, LP_FLOOR);
+    const f32x2 lp = pack2(a, b);
+    unpack2(mul2(lp, pack2(kLog2e, kLog2e)), a, b);
+    unpack2(mul2(pack2(ex2(a), ex2(b)), fma2(pack2(r.c, r.c), lp, pack2(r.sum, r.sum))), x0, x1);
 }
 
 // The special entries of a row: their logits, read before anything is written (dx may be x), and their
@@ -717,7 +742,6 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_backward_small_kernel(con
     RowGrad r;
     r.lse = g.lse[row];
     r.lse_lo = g.lse_lo ? g.lse_lo[row] : 0.f;
-    r.empty = r.lse == -CUDART_INF_F;
     r.c = g.grad_entropy ? g.grad_entropy[row] : 0.f;
     r.entropy = g.grad_entropy ? g.entropy[row] : 0.f;
     r.sum = 0.f;
@@ -732,6 +756,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_backward_small_kernel(con
         term(at < 0 ? vocab : at, g.grad_top[row * g.top + j]);
     }
     if (g.grad_logprobs && g.targets[row] >= 0) term(g.targets[row], g.grad_logprobs[row]);
+    settle(r);
 #pragma unroll
     for (int i = 0; i < EPL; ++i)
         if (lane + i * L < vocab) dx[lane + i * L] = Elem<T>::narrow(r.empty ? 0.f : grad_at(r, v[i]) + extra[i]);
@@ -769,7 +794,8 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_backward_kernel(const Bac
     };
     fetch(first);
     const RowGrad r = row_grad(g, row, lane);
-    const Special s = read_special<T>(r, x, lo, hi);
+    const bool last_word = threadIdx.x % THREADS < 32;            // the warp that writes the special entries
+    const Special s = last_word ? read_special<T>(r, x, lo, hi) : Special{0.f, 0.f};
     if (WARPS == 1) __syncwarp();
     else __syncthreads();                 // read before anything is written: dx may be x
     for (unsigned chunk = first; chunk < last; ++chunk) {
@@ -782,7 +808,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_backward_kernel(const Bac
                 float f[E];
                 widen16B(raw[i], f, static_cast<const T*>(nullptr));
 #pragma unroll
-                for (int e = 0; e < E; ++e) f[e] = grad_at(r, f[e]);
+                for (int e = 0; e < E; e += 2) grad_at2(r, f[e], f[e + 1]);
                 store_stream(dx + j, narrow16B(f, static_cast<const T*>(nullptr)));
             } else if (j < g.vocab) {
                 for (int e = 0; e < E; ++e)
@@ -792,7 +818,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_backward_kernel(const Bac
     }
     if (WARPS == 1) __syncwarp();
     else __syncthreads();
-    if (threadIdx.x % THREADS < 32) write_special<T>(g, r, s, dx, lo, hi, lane);
+    if (last_word) write_special<T>(g, r, s, dx, lo, hi, lane);
 }
 
 template <typename T>
