@@ -81,29 +81,29 @@ __device__ __forceinline__ unsigned long long shfl_xor64(unsigned long long v, i
     return __shfl_xor_sync(0xffffffffu, v, o);
 }
 
-// What a row comes to, from its joined sums.
+// What a row comes to, from its joined sums.  A NaN or +inf in the row has made s a NaN, and with it
+// everything here.  An empty row gets m = 0 and log s = +inf: every log probability is then -inf.
 struct RowResult {
     float lse, lse_lo, entropy, log_s, m;
-    bool  empty, bad;
 };
 __device__ __forceinline__ RowResult finish(const Softmax& a) {
     RowResult r;
     r.m = a.m;
-    r.bad = a.s != a.s;                          // a NaN or +inf in the row
-    r.empty = !r.bad && a.m == -CUDART_INF_F;
     r.log_s = logf(a.s);
-    r.lse = r.bad ? CUDART_NAN_F : r.empty ? -CUDART_INF_F : a.m + r.log_s;
+    r.lse = __fadd_rn(a.m, r.log_s);
     // the rounding error of m + log s, exactly (two-sum)
     const float part = __fsub_rn(r.lse, a.m);
-    r.lse_lo = r.bad || r.empty ? 0.f : __fadd_rn(__fsub_rn(a.m, __fsub_rn(r.lse, part)), __fsub_rn(r.log_s, part));
-    r.entropy = r.bad ? CUDART_NAN_F : r.empty ? 0.f : r.log_s - (a.u / a.s) * 0.69314718055994531f;
+    r.lse_lo = __fadd_rn(__fsub_rn(a.m, __fsub_rn(r.lse, part)), __fsub_rn(r.log_s, part));
+    r.entropy = r.log_s - (a.u / a.s) * 0.69314718055994531f;
+    if (a.m == -CUDART_INF_F && a.s == 0.f) {
+        r.m = 0.f;
+        r.log_s = CUDART_INF_F;
+        r.lse = -CUDART_INF_F;
+        r.lse_lo = r.entropy = 0.f;
+    }
     return r;
 }
-__device__ __forceinline__ float logprob_of(const RowResult& r, float x) {
-    if (r.bad) return CUDART_NAN_F;
-    if (r.empty) return -CUDART_INF_F;
-    return (x - r.m) - r.log_s;
-}
+__device__ __forceinline__ float logprob_of(const RowResult& r, float x) { return (x - r.m) - r.log_s; }
 
 template <typename T>
 __device__ __forceinline__ float load_one(const T* row, int64_t j) { return Elem<T>::widen(row[j]); }
@@ -516,21 +516,28 @@ __global__ void __launch_bounds__(cta_threads(WARPS), 1024 / cta_threads(WARPS))
     }
     const int64_t edge = edge_entry(v, tid);
     if (edge >= 0) add_one(st, load_one(v.x, edge));
+    // the warp's sums about the warp's maximum
+    const float warp_m = value_of(__reduce_max_sync(0xffffffffu, code_of(st.m)));
+    if (warp_m > st.m) raise(st, warp_m);
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-        Softmax b;
-        b.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-        b.s = __shfl_xor_sync(0xffffffffu, st.s, o);
-        b.u = __shfl_xor_sync(0xffffffffu, st.u, o);
-        join(st, b);
+        st.s += __shfl_xor_sync(0xffffffffu, st.s, o);
+        st.u += __shfl_xor_sync(0xffffffffu, st.u, o);
     }
     Softmax total = st;
     if (WARPS > 1) {
         if (lane == 0) sh.part[warp] = st;
         __syncthreads();
-        total = sh.part[0];
+        total = Softmax{sh.part[0].m, 0.f, 0.f};
 #pragma unroll
-        for (int w = 1; w < WARPS; ++w) join(total, sh.part[w]);
+        for (int w = 1; w < WARPS; ++w) total.m = fmaxf(total.m, sh.part[w].m);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            Softmax b = sh.part[w];
+            if (total.m > b.m) raise(b, total.m);
+            total.s += b.s;
+            total.u += b.u;
+        }
         __syncthreads();
     }
     if (a.top) find_top<T, WARPS>(sh, v, first, second, a.top, turn_shift + 2);
@@ -588,7 +595,7 @@ cudaError_t forward(const ForwardArgs& a, int sm_count, cudaStream_t stream) {
     }
     // Long rows, enough of them: half a CTA's worth of threads per row, so that twice as many rows are in
     // work on an SM and the end of one (reductions, the top alternatives) hides behind the others
-    if (a.rows >= 8 * int64_t(sm_count)) {
+    if (a.rows >= 4 * int64_t(sm_count)) {
         if (a.rows > 0x7fffffff) return cudaErrorInvalidConfiguration;
         logprobs_kernel<T, 4><<<unsigned(a.rows), cta_threads(4), 0, stream>>>(a, 1);
         return cudaGetLastError();
