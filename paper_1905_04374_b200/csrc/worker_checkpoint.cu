@@ -25,6 +25,11 @@ struct FastDiv {
     __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
 };
 
+// How a matrix lies: any rows; rows that start on 16 bytes; or (DENSE) every matrix of the call without
+// gaps between its rows and of whole groups, so that a task's number gives its place everywhere and
+// nothing is divided, multiplied or checked: 70 of 184 instructions per task of the pack.
+enum Layout { CK_ANY = 0, CK_VEC = 1, CK_DENSE = 2 };
+
 // Eight consecutive elements as they lie in memory (Raw8: one or two 16-byte words).
 template <typename T> struct Raw8;
 template <> struct Raw8<float> { uint4 a, b; };
@@ -32,14 +37,14 @@ template <> struct Raw8<__nv_bfloat16> { uint4 a; };
 template <> struct Raw8<__half> { uint4 a; };
 
 // 16-byte accesses where the row starts allow it, single ones otherwise; columns that are not there read as 0
-template <typename T, bool VEC>
+template <typename T, int LAYOUT>
 __device__ __forceinline__ Raw8<T> load8(const T* p, int count) {
     Raw8<T> r{};
     if constexpr (sizeof(T) == 4) {
-        if (VEC && count == 8) {
+        if (LAYOUT != CK_ANY && count == 8) {
             r.a = load_stream(p);
             r.b = load_stream(p + 4);
-        } else {
+        } else if (LAYOUT != CK_DENSE) {
             unsigned w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = i < count ? __float_as_uint(p[i]) : 0u;
@@ -47,9 +52,9 @@ __device__ __forceinline__ Raw8<T> load8(const T* p, int count) {
             r.b = make_uint4(w[4], w[5], w[6], w[7]);
         }
     } else {
-        if (VEC && count == 8) {
+        if (LAYOUT != CK_ANY && count == 8) {
             r.a = load_stream(p);
-        } else {
+        } else if (LAYOUT != CK_DENSE) {
             const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
             unsigned w[8];
 #pragma unroll
@@ -59,22 +64,22 @@ __device__ __forceinline__ Raw8<T> load8(const T* p, int count) {
     }
     return r;
 }
-template <typename T, bool VEC>
+template <typename T, int LAYOUT>
 __device__ __forceinline__ void store8(T* p, int count, const Raw8<T>& r) {
     if constexpr (sizeof(T) == 4) {
-        if (VEC && count == 8) {
+        if (LAYOUT != CK_ANY && count == 8) {
             store_stream(p, r.a);
             store_stream(p + 4, r.b);
-        } else {
+        } else if (LAYOUT != CK_DENSE) {
             const unsigned w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (i < count) p[i] = __uint_as_float(w[i]);
         }
     } else {
-        if (VEC && count == 8) {
+        if (LAYOUT != CK_ANY && count == 8) {
             store_stream(p, r.a);
-        } else {
+        } else if (LAYOUT != CK_DENSE) {
             const unsigned w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
             unsigned short* h = reinterpret_cast<unsigned short*>(p);
 #pragma unroll
@@ -145,6 +150,7 @@ __device__ __forceinline__ float magnitude(unsigned bits) {
 }
 
 // The codes and, from the group's first lane, the scale of eight columns with group maximum `top`.
+template <int LAYOUT>
 __device__ __forceinline__ void save8(const float (&v)[8], float top, int count, bool leader, int8_t* q, float* scale) {
     if (count <= 0) return;
     const bool sound = top <= 3.402823466e38f, live = sound && top >= CK_TINY;
@@ -168,13 +174,15 @@ __device__ __forceinline__ void save8(const float (&v)[8], float top, int count,
     if (!sound) lo = hi = 0u;
     if (count == 8) {
         __stcs(reinterpret_cast<uint2*>(q), make_uint2(lo, hi));
-    } else {
+    } else if (LAYOUT != CK_DENSE) {
         for (int i = 0; i < count; ++i) q[i] = int8_t(((i < 4 ? lo : hi) >> (8 * (i & 3))) & 0xff);
     }
 }
+template <int LAYOUT>
 __device__ __forceinline__ uint2 load_codes(const int8_t* q, int count) {
     if (count == 8) return __ldcs(reinterpret_cast<const uint2*>(q));
     unsigned w[2] = {0, 0};
+    if (LAYOUT != CK_DENSE)
     for (int i = 0; i < count; ++i) w[i >> 2] |= unsigned(uint8_t(q[i])) << (8 * (i & 3));
     return make_uint2(w[0], w[1]);
 }
@@ -228,22 +236,32 @@ __device__ __forceinline__ void act_slope(float x, float& y, float& slope) {
 }
 
 // A thread's task: eight columns of a row.
-struct Task {
+template <int LAYOUT> struct Task {
     int64_t row, col, group;
     int     count;                 // columns that exist; 0: nothing to do
+    __device__ __forceinline__ int64_t at(int64_t ld) const { return row * ld + col; }
+    template <typename A> __device__ __forceinline__ Task(const A& a, unsigned number) {
+        const bool live = number < a.tasks;
+        const unsigned n = live ? number : 0u, r = a.per_row.quotient(n), c = n - r * a.per_row.d;
+        row = a.row0 + r;
+        col = int64_t(c) * 8;
+        group = row * a.groups + (c >> a.lane_shift);
+        const int64_t left = a.cols - col;
+        count = !live || left <= 0 ? 0 : left < 8 ? int(left) : 8;
+    }
+    template <typename A> __device__ __forceinline__ bool masked(const A& a) const { return row % a.tokens >= a.lengths[row / a.tokens]; }
 };
-template <typename A>
-__device__ __forceinline__ Task task_at(const A& a, unsigned number) {
-    Task t;
-    const bool live = number < a.tasks;
-    const unsigned n = live ? number : 0u, r = a.per_row.quotient(n), c = n - r * a.per_row.d;
-    t.row = a.row0 + r;
-    t.col = int64_t(c) * 8;
-    t.group = t.row * a.groups + (c >> a.lane_shift);
-    const int64_t left = a.cols - t.col;
-    t.count = !live || left <= 0 ? 0 : left < 8 ? int(left) : 8;
-    return t;
-}
+template <> struct Task<CK_DENSE> {
+    unsigned number;
+    int64_t  base, group;          // base: tasks before this launch's
+    int      count;
+    template <typename A> __device__ __forceinline__ Task(const A& a, unsigned n) : number(n < a.tasks ? n : 0u), base(a.row0) {
+        group = (base >> a.lane_shift) + (number >> a.lane_shift);
+        count = n < a.tasks ? 8 : 0;
+    }
+    __device__ __forceinline__ int64_t at(int64_t) const { return (base + number) * 8; }
+    template <typename A> __device__ __forceinline__ bool masked(const A&) const { return false; }      // not launched so
+};
 
 struct Saved {
     int8_t* q;
@@ -263,20 +281,20 @@ struct ForwardArgs {
 };
 
 // GATED: y = act(x) * up
-template <typename T, int ACT, bool VEC, bool GATED>
+template <typename T, int ACT, int LAYOUT, bool GATED>
 __global__ void __launch_bounds__(CK_THREADS) activation_forward_kernel(const ForwardArgs a) {
-    Task t[CK_TASKS];
     Raw8<T> x[CK_TASKS], u[CK_TASKS];
 #pragma unroll
     for (int k = 0; k < CK_TASKS; ++k) {
-        t[k] = task_at(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
-        x[k] = load8<T, VEC>(static_cast<const T*>(a.x) + t[k].row * a.ldx + t[k].col, t[k].count);
-        if (GATED) u[k] = load8<T, VEC>(static_cast<const T*>(a.up) + t[k].row * a.ldup + t[k].col, t[k].count);
+        const Task<LAYOUT> t(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
+        x[k] = load8<T, LAYOUT>(static_cast<const T*>(a.x) + t.at(a.ldx), t.count);
+        if (GATED) u[k] = load8<T, LAYOUT>(static_cast<const T*>(a.up) + t.at(a.ldup), t.count);
     }
     const bool leader = (threadIdx.x & (a.lanes - 1)) == 0;
 #pragma unroll
     for (int k = 0; k < CK_TASKS; ++k) {
-        const int count = t[k].count;
+        const Task<LAYOUT> t(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
+        const int count = t.count;
         unsigned top_x = 0, top_u = 0;
         if (a.sx.q || a.sup.q) {
             top_x = top8<T>(x[k]);
@@ -285,23 +303,26 @@ __global__ void __launch_bounds__(CK_THREADS) activation_forward_kernel(const Fo
         }
         float v[8], y[8];
         widen8<T>(x[k], v);
+        if (a.y || a.sy.q) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = act<ACT>(v[i]);
-        if (a.sx.q) save8(v, magnitude<T>(top_x), count, leader, a.sx.q + t[k].row * a.sx.ld + t[k].col, a.sx.scales + t[k].group);
+            for (int i = 0; i < 8; ++i) y[i] = act<ACT>(v[i]);
+        }
+        if (a.sx.q) save8<LAYOUT>(v, magnitude<T>(top_x), count, leader, a.sx.q + t.at(a.sx.ld), a.sx.scales + t.group);
         if (GATED) {
             widen8<T>(u[k], v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] *= v[i];
-            if (a.sup.q) save8(v, magnitude<T>(top_u), count, leader, a.sup.q + t[k].row * a.sup.ld + t[k].col, a.sup.scales + t[k].group);
+            if (a.sup.q) save8<LAYOUT>(v, magnitude<T>(top_u), count, leader, a.sup.q + t.at(a.sup.ld), a.sup.scales + t.group);
         }
+        if (!a.y && !a.sy.q) continue;
         const Raw8<T> out = narrow8<T>(y);
-        if (a.y) store8<T, VEC>(static_cast<T*>(a.y) + t[k].row * a.ldy + t[k].col, count, out);
+        if (a.y) store8<T, LAYOUT>(static_cast<T*>(a.y) + t.at(a.ldy), count, out);
         if (a.sy.q) {
             // y of a column that does not exist is act(0) = 0
             unsigned top_y = top8<T>(out), none = 0;
             group_top<T>(top_y, none, false, a.lanes);
             widen8<T>(out, v);
-            save8(v, magnitude<T>(top_y), count, leader, a.sy.q + t[k].row * a.sy.ld + t[k].col, a.sy.scales + t[k].group);
+            save8<LAYOUT>(v, magnitude<T>(top_y), count, leader, a.sy.q + t.at(a.sy.ld), a.sy.scales + t.group);
         }
     }
 }
@@ -317,27 +338,27 @@ struct BackwardArgs {
     int         groups, lane_shift;
 };
 
-template <typename T, int ACT, bool VEC, bool GATED>
+template <typename T, int ACT, int LAYOUT, bool GATED>
 __global__ void __launch_bounds__(CK_THREADS) activation_backward_kernel(const BackwardArgs a) {
-    Task t[CK_TASKS];
     Raw8<T> dy[CK_TASKS];
     uint2 cx[CK_TASKS], cu[CK_TASKS];
     float sx[CK_TASKS], su[CK_TASKS];
 #pragma unroll
     for (int k = 0; k < CK_TASKS; ++k) {
-        t[k] = task_at(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
-        const int count = t[k].count;
-        dy[k] = load8<T, VEC>(static_cast<const T*>(a.dy) + t[k].row * a.lddy + t[k].col, count);
-        cx[k] = count ? load_codes(a.sx.q + t[k].row * a.sx.ld + t[k].col, count) : make_uint2(0, 0);
-        sx[k] = count ? __ldg(a.sx.scales + t[k].group) : 0.f;
+        const Task<LAYOUT> t(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
+        const int count = t.count;
+        dy[k] = load8<T, LAYOUT>(static_cast<const T*>(a.dy) + t.at(a.lddy), count);
+        cx[k] = count ? load_codes<LAYOUT>(a.sx.q + t.at(a.sx.ld), count) : make_uint2(0, 0);
+        sx[k] = count ? __ldg(a.sx.scales + t.group) : 0.f;
         if (GATED) {
-            cu[k] = count ? load_codes(a.sup.q + t[k].row * a.sup.ld + t[k].col, count) : make_uint2(0, 0);
-            su[k] = count ? __ldg(a.sup.scales + t[k].group) : 0.f;
+            cu[k] = count ? load_codes<LAYOUT>(a.sup.q + t.at(a.sup.ld), count) : make_uint2(0, 0);
+            su[k] = count ? __ldg(a.sup.scales + t.group) : 0.f;
         }
     }
 #pragma unroll
     for (int k = 0; k < CK_TASKS; ++k) {
-        const int count = t[k].count;
+        const Task<LAYOUT> t(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
+        const int count = t.count;
         if (count == 0) continue;
         float d[8], x[8], dx[8];
         widen8<T>(dy[k], d);
@@ -352,7 +373,7 @@ __global__ void __launch_bounds__(CK_THREADS) activation_backward_kernel(const B
                 du[i] = d[i] * y;
                 dx[i] = d[i] * u[i] * slope;
             }
-            store8<T, VEC>(static_cast<T*>(a.dup) + t[k].row * a.lddup + t[k].col, count, narrow8<T>(du));
+            store8<T, LAYOUT>(static_cast<T*>(a.dup) + t.at(a.lddup), count, narrow8<T>(du));
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -361,7 +382,7 @@ __global__ void __launch_bounds__(CK_THREADS) activation_backward_kernel(const B
                 dx[i] = d[i] * slope;
             }
         }
-        store8<T, VEC>(static_cast<T*>(a.dx) + t[k].row * a.lddx + t[k].col, count, narrow8<T>(dx));
+        store8<T, LAYOUT>(static_cast<T*>(a.dx) + t.at(a.lddx), count, narrow8<T>(dx));
     }
 }
 
@@ -375,21 +396,22 @@ struct RestoreArgs {
     const int32_t* lengths;         // MASKED: row w * tokens + t is restored as zeros from t = lengths[w] on
     int64_t  tokens;
 };
-template <typename T, bool VEC, bool MASKED>
+template <typename T, int LAYOUT, bool MASKED>
 __global__ void __launch_bounds__(CK_THREADS) checkpoint_restore_kernel(const RestoreArgs a) {
-    Task t[CK_TASKS];
     uint2 codes[CK_TASKS];
     float scale[CK_TASKS];
 #pragma unroll
     for (int k = 0; k < CK_TASKS; ++k) {
-        t[k] = task_at(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
-        const bool read = t[k].count && !(MASKED && t[k].row % a.tokens >= a.lengths[t[k].row / a.tokens]);
-        codes[k] = read ? load_codes(a.s.q + t[k].row * a.s.ld + t[k].col, t[k].count) : make_uint2(0, 0);
-        scale[k] = read ? __ldg(a.s.scales + t[k].group) : 0.f;
+        const Task<LAYOUT> t(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
+        const bool read = t.count && !(MASKED && t.masked(a));
+        codes[k] = read ? load_codes<LAYOUT>(a.s.q + t.at(a.s.ld), t.count) : make_uint2(0, 0);
+        scale[k] = read ? __ldg(a.s.scales + t.group) : 0.f;
     }
 #pragma unroll
-    for (int k = 0; k < CK_TASKS; ++k)
-        store8<T, VEC>(static_cast<T*>(a.x) + t[k].row * a.ldx + t[k].col, t[k].count, restore8<T>(codes[k], scale[k]));
+    for (int k = 0; k < CK_TASKS; ++k) {
+        const Task<LAYOUT> t(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
+        store8<T, LAYOUT>(static_cast<T*>(a.x) + t.at(a.ldx), t.count, restore8<T>(codes[k], scale[k]));
+    }
 }
 
 // ---- launches ---------------------------------------------------------------------------------
@@ -398,6 +420,8 @@ int log2_lanes(int group) { return group == 32 ? 2 : group == 64 ? 3 : 4; }
 bool aligned16(const void* p, int64_t ld, size_t esize) {
     return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * int64_t(esize)) % 16 == 0);
 }
+// a checkpoint that is not asked for, or whose rows have no gap
+bool gapless(const gar_checkpoint_t& s, int64_t cols) { return !s.q || s.ldq == cols; }
 size_t esize_of(int dtype) { return dtype == GAR_F32 ? 4 : 2; }
 
 // Calls f(row0, tasks, blocks) for row ranges of fewer than 2^31 tasks.
@@ -419,13 +443,19 @@ unsigned tasks_per_row(int64_t cols, int group) {
     return n < (int64_t(1) << 30) ? unsigned(n) : 0u;
 }
 
-// f(T, VEC) and f(T, ACT, VEC) with compile-time arguments
+// f(T, LAYOUT) and f(ACT) with compile-time arguments
 template <int V> using Int = std::integral_constant<int, V>;
+template <typename T, typename F>
+void by_layout(int layout, F f) {
+    if (layout == CK_DENSE) f(T{}, Int<CK_DENSE>{});
+    else if (layout == CK_VEC) f(T{}, Int<CK_VEC>{});
+    else f(T{}, Int<CK_ANY>{});
+}
 template <typename F>
-void by_type(int dtype, bool vec, F f) {
-    if (dtype == GAR_F32) { if (vec) f(float{}, Int<1>{}); else f(float{}, Int<0>{}); }
-    else if (dtype == GAR_BF16) { if (vec) f(__nv_bfloat16{}, Int<1>{}); else f(__nv_bfloat16{}, Int<0>{}); }
-    else { if (vec) f(__half{}, Int<1>{}); else f(__half{}, Int<0>{}); }
+void by_type(int dtype, int layout, F f) {
+    if (dtype == GAR_F32) by_layout<float>(layout, f);
+    else if (dtype == GAR_BF16) by_layout<__nv_bfloat16>(layout, f);
+    else by_layout<__half>(layout, f);
 }
 template <typename F>
 void by_act(int act, F f) {
@@ -451,16 +481,19 @@ cudaError_t launch_activation_forward(const gar_activation_params_t& p) {
     a.lane_shift = log2_lanes(p.group);
     a.lanes = 1 << a.lane_shift;
     const size_t es = esize_of(p.dtype);
-    const bool vec = aligned16(p.x, p.ldx, es) && aligned16(p.up, p.ldup, es) && aligned16(p.y, p.ldy, es);
+    int layout = aligned16(p.x, p.ldx, es) && aligned16(p.up, p.ldup, es) && aligned16(p.y, p.ldy, es) ? CK_VEC : CK_ANY;
+    if (layout == CK_VEC && p.cols % p.group == 0 && p.ldx == p.cols && (!p.up || p.ldup == p.cols) && (!p.y || p.ldy == p.cols) &&
+        gapless(p.x_saved, p.cols) && gapless(p.up_saved, p.cols) && gapless(p.y_saved, p.cols))
+        layout = CK_DENSE;
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     return over_rows(p.rows, per_row, [&](int64_t r0, unsigned tasks, unsigned blocks) {
-        a.row0 = r0;
+        a.row0 = layout == CK_DENSE ? r0 * per_row : r0;
         a.tasks = tasks;
-        by_type(p.dtype, vec, [&](auto t, auto v) {
+        by_type(p.dtype, layout, [&](auto t, auto v) {
             by_act(p.act, [&](auto f) {
-                constexpr bool VEC = decltype(v)::value != 0;
-                if (a.up) activation_forward_kernel<decltype(t), decltype(f)::value, VEC, true><<<blocks, CK_THREADS, 0, stream>>>(a);
-                else activation_forward_kernel<decltype(t), decltype(f)::value, VEC, false><<<blocks, CK_THREADS, 0, stream>>>(a);
+                constexpr int LAYOUT = decltype(v)::value;
+                if (a.up) activation_forward_kernel<decltype(t), decltype(f)::value, LAYOUT, true><<<blocks, CK_THREADS, 0, stream>>>(a);
+                else activation_forward_kernel<decltype(t), decltype(f)::value, LAYOUT, false><<<blocks, CK_THREADS, 0, stream>>>(a);
             });
         });
     });
@@ -478,16 +511,19 @@ cudaError_t launch_activation_backward(const gar_activation_grad_params_t& p) {
     a.groups = int((p.cols + p.group - 1) / p.group);
     a.lane_shift = log2_lanes(p.group);
     const size_t es = esize_of(p.dtype);
-    const bool vec = aligned16(p.dy, p.lddy, es) && aligned16(p.dx, p.lddx, es) && aligned16(p.dup, p.lddup, es);
+    int layout = aligned16(p.dy, p.lddy, es) && aligned16(p.dx, p.lddx, es) && aligned16(p.dup, p.lddup, es) ? CK_VEC : CK_ANY;
+    if (layout == CK_VEC && p.cols % p.group == 0 && p.lddy == p.cols && p.lddx == p.cols && (!p.dup || p.lddup == p.cols) &&
+        gapless(p.x_saved, p.cols) && gapless(p.up_saved, p.cols))
+        layout = CK_DENSE;
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     return over_rows(p.rows, per_row, [&](int64_t r0, unsigned tasks, unsigned blocks) {
-        a.row0 = r0;
+        a.row0 = layout == CK_DENSE ? r0 * per_row : r0;
         a.tasks = tasks;
-        by_type(p.dtype, vec, [&](auto t, auto v) {
+        by_type(p.dtype, layout, [&](auto t, auto v) {
             by_act(p.act, [&](auto f) {
-                constexpr bool VEC = decltype(v)::value != 0;
-                if (a.sup.q) activation_backward_kernel<decltype(t), decltype(f)::value, VEC, true><<<blocks, CK_THREADS, 0, stream>>>(a);
-                else activation_backward_kernel<decltype(t), decltype(f)::value, VEC, false><<<blocks, CK_THREADS, 0, stream>>>(a);
+                constexpr int LAYOUT = decltype(v)::value;
+                if (a.sup.q) activation_backward_kernel<decltype(t), decltype(f)::value, LAYOUT, true><<<blocks, CK_THREADS, 0, stream>>>(a);
+                else activation_backward_kernel<decltype(t), decltype(f)::value, LAYOUT, false><<<blocks, CK_THREADS, 0, stream>>>(a);
             });
         });
     });
@@ -508,14 +544,15 @@ cudaError_t restore(int dtype, const gar_checkpoint_t& saved, int64_t rows, int6
     a.lane_shift = log2_lanes(group);
     a.lengths = lengths;
     a.tokens = tokens;
-    const bool vec = aligned16(x, ldx, esize_of(dtype));
+    int layout = aligned16(x, ldx, esize_of(dtype)) ? CK_VEC : CK_ANY;
+    if (layout == CK_VEC && !lengths && cols % group == 0 && ldx == cols && gapless(saved, cols)) layout = CK_DENSE;
     return over_rows(rows, per_row, [&](int64_t r0, unsigned tasks, unsigned blocks) {
-        a.row0 = r0;
+        a.row0 = layout == CK_DENSE ? r0 * per_row : r0;
         a.tasks = tasks;
-        by_type(dtype, vec, [&](auto t, auto v) {
-            constexpr bool VEC = decltype(v)::value != 0;
-            if (lengths) checkpoint_restore_kernel<decltype(t), VEC, true><<<blocks, CK_THREADS, 0, stream>>>(a);
-            else checkpoint_restore_kernel<decltype(t), VEC, false><<<blocks, CK_THREADS, 0, stream>>>(a);
+        by_type(dtype, layout, [&](auto t, auto v) {
+            constexpr int LAYOUT = decltype(v)::value;
+            if (lengths) checkpoint_restore_kernel<decltype(t), LAYOUT == CK_DENSE ? CK_VEC : LAYOUT, true><<<blocks, CK_THREADS, 0, stream>>>(a);
+            else checkpoint_restore_kernel<decltype(t), LAYOUT, false><<<blocks, CK_THREADS, 0, stream>>>(a);
         });
     });
 }

@@ -245,18 +245,39 @@ __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t 
             *reinterpret_cast<uint4*>(tile + (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4)) = v[k];
         }
     } else {
-#pragma unroll 2
-        for (int k = 0; k < 16; ++k) {
-            const int row = 16 * w + k;
+        // eight columns at any even address: the two aligned 16-byte words around them, shifted together;
+        // single elements where a word would reach beyond the matrix
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(dy);
+        const uintptr_t end = begin + 2 * uintptr_t((int64_t(a.workers) * a.tokens - 1) * a.ld_dy + a.out);
+        const int c = (lane % 16) * 8;
+        const int64_t o = o0 + c;
+#pragma unroll 4
+        for (int k = 0; k < 8; ++k) {
+            const int row = 16 * w + 2 * k + lane / 16;
             const int64_t token = int64_t(step) * WG_K + row;
-            const unsigned short* src = dy + (int64_t(t.worker) * a.tokens + token) * a.ld_dy;
+            const unsigned short* src = dy + (int64_t(t.worker) * a.tokens + token) * a.ld_dy + o;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (token < t.len && o < a.out) {
+                const uintptr_t word = reinterpret_cast<uintptr_t>(src) & ~uintptr_t(15);
+                if (o + 8 <= a.out && word >= begin && word + 32 <= end) {
+                    const uint4 x = __ldg(reinterpret_cast<const uint4*>(word)), y = __ldg(reinterpret_cast<const uint4*>(word) + 1);
+                    const unsigned by = unsigned(reinterpret_cast<uintptr_t>(src) & 15);
+                    unsigned h[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-            for (int i = 0; i < WG_M / 32; ++i) {
-                const int c = lane + 32 * i;
-                const int64_t o = o0 + c;
-                const unsigned short v = token < t.len && o < a.out ? __ldg(src + o) : static_cast<unsigned short>(0);
-                *reinterpret_cast<unsigned short*>(tile + (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4) + (c % 8) * 2) = v;
+                    for (int j = 0; j < 6; ++j) h[j] = by & 8 ? h[j + 2] : h[j];
+#pragma unroll
+                    for (int j = 0; j < 5; ++j) h[j] = by & 4 ? h[j + 1] : h[j];
+                    const unsigned bits = (by & 2) * 8;
+                    v = make_uint4(__funnelshift_r(h[0], h[1], bits), __funnelshift_r(h[1], h[2], bits), __funnelshift_r(h[2], h[3], bits),
+                                   __funnelshift_r(h[3], h[4], bits));
+                } else {
+                    unsigned h[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) h[j] = o + j < a.out ? __ldg(src + j) : 0u;
+                    v = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+                }
             }
+            *reinterpret_cast<uint4*>(tile + (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4)) = v;
         }
     }
 }
