@@ -20,8 +20,9 @@
 //                  fp32, subtract, multiply by the row group's scale, one rounding) -> operand tile in
 //                  shared memory, same layout
 //   MMA warp       of the leading CTA, one lane: four 256 x 256 x 16 instructions per step
-//   store warps    four: tensor memory -> shared memory -> coalesced stores, while the next tile's
-//                  products run into the other half of tensor memory
+//   store warps    four: tensor memory -> shared memory -> TMA stores (plain coalesced ones where the
+//                  result's rows do not start on 16 bytes), while the next tile's products run into the
+//                  other half of tensor memory
 // The bias is one more column tile whose second operand is a block of ones.
 // Hand-offs are mbarriers; every wait is bounded: a wait that gives up raises an error flag, all
 // roles leave their loops once what they have in flight has landed, and the CTA's tiles become NaN.
@@ -41,8 +42,8 @@ constexpr int WG_HALF = WG_N / 2;                     // columns a CTA restores
 // bytes); dy by TMA; both by TMA, x restored beforehand in the caller's workspace.
 enum Mode { WG_PLAIN_DY = 0, WG_FUSED = 1, WG_RESTORED = 2 };
 // Steps in flight: operand tiles (dy's and x's share a slot), copies of the codes.
-__host__ __device__ constexpr int wg_ring(int mode) { return mode == WG_RESTORED ? 6 : 5; }
-__host__ __device__ constexpr int wg_q_ring(int mode) { return mode == WG_RESTORED ? 1 : 6; }
+constexpr int WG_RING = 5;
+__host__ __device__ constexpr int wg_q_ring(int mode) { return mode == WG_RESTORED ? 1 : 4; }
 constexpr int WG_DY_WARP = 0, WG_MMA_WARP = 1, WG_ALLOC_WARP = 2, WG_CODES_WARP = 3;
 constexpr int WG_STORE_WARP0 = 4;                     // 4..7: tensor-memory lanes 32 (warp % 4) ..
 // Groups of four restore warps take steps in turn: a step takes a group about 1500 cycles from its slot
@@ -55,16 +56,16 @@ constexpr int WG_A_BYTES = WG_M / 64 * WG_BLOCK, WG_B_BYTES = WG_HALF / 64 * WG_
 constexpr int WG_GROUP_M = 8;                         // (pair) row tiles that go round a column tile together
 constexpr int WG_BIAS_N = 16;
 
-template <int RING, int Q_RING> struct __align__(1024) WGSmem {
-    uint8_t  a[RING][WG_A_BYTES];
-    uint8_t  b[RING][WG_B_BYTES];
+template <int Q_RING> struct __align__(1024) WGSmem {
+    uint8_t  a[WG_RING][WG_A_BYTES];
+    uint8_t  b[WG_RING][WG_B_BYTES];
     uint8_t  q[Q_RING][WG_Q_BYTES];
-    float    out[4][32 * 32];                             // a store warp's 32 x 32 piece of the tile
+    float    out[4][2][32 * 32];                          // a store warp's pieces of the tile: 32 rows of 128 bytes
     uint16_t ones[512];
-    unsigned long long empty[RING], q_full[Q_RING], q_empty[Q_RING], late[RING], acc_full[2];
-    unsigned long long a_full[RING], b_full[RING], acc_empty[2];           // the leading CTA's are used, for both
+    unsigned long long empty[WG_RING], q_full[Q_RING], q_empty[Q_RING], late[WG_RING], acc_full[2];
+    unsigned long long a_full[WG_RING], b_full[WG_RING], acc_empty[2];           // the leading CTA's are used, for both
     unsigned tmem_base;
-    int      error;
+    int      error, other_error;                          // a wait gave up, here or in the other CTA
 };
 
 struct WGArgs {
@@ -76,7 +77,7 @@ struct WGArgs {
     int            workers, groups, group_shift;
     int            mt, nt;                // pair row tiles, column tiles (the bias tile, if any, is one more)
     int            columns;               // nt + 1 with a bias
-    int            wide;                  // rows of the result start on 16 bytes
+    int            wide;                  // the result's rows start on 16 bytes: stored by TMA
 };
 
 // ---- tcgen05 ------------------------------------------------------------------------------------
@@ -158,6 +159,16 @@ __device__ __forceinline__ void tma_load_pair(unsigned dst, const CUtensorMap* m
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
+// a piece of the result from shared memory (what lies outside the matrix is not written)
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, unsigned src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+template <int LEFT> __device__ __forceinline__ void tma_store_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void tma_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
 // ---- tiles --------------------------------------------------------------------------------------
 struct Tile {
     int     worker, m, n;        // n == nt: the bias
@@ -169,20 +180,19 @@ __device__ __forceinline__ int64_t worker_len(const WGArgs& a, int w) {
     const int64_t l = a.lengths[w];
     return l < 0 ? 0 : l < a.tokens ? l : a.tokens;
 }
-__device__ __forceinline__ Tile tile_at(const WGArgs& a, int64_t index) {
+__device__ __forceinline__ Tile tile_at(const WGArgs& a, unsigned index) {
     Tile t;
-    const int per = a.mt * a.columns;
-    t.worker = int(index / per);
-    const int r = int(index - int64_t(t.worker) * per);
-    const int g = r / (WG_GROUP_M * a.columns), in_group = r - g * WG_GROUP_M * a.columns;
-    const int rows = min(WG_GROUP_M, a.mt - g * WG_GROUP_M);
-    t.n = in_group / rows;
-    t.m = g * WG_GROUP_M + in_group % rows;
+    const unsigned per = unsigned(a.mt) * unsigned(a.columns), worker = index / per, r = index - worker * per;
+    const unsigned per_group = WG_GROUP_M * unsigned(a.columns), g = r / per_group, in_group = r - g * per_group;
+    const unsigned rows = min(unsigned(WG_GROUP_M), unsigned(a.mt) - g * WG_GROUP_M);
+    t.worker = int(worker);
+    t.n = int(in_group / rows);
+    t.m = int(g * WG_GROUP_M + in_group - unsigned(t.n) * rows);
     t.len = worker_len(a, t.worker);
     t.steps = int((t.len + WG_K - 1) / WG_K);
     return t;
 }
-__device__ __forceinline__ int64_t tile_count(const WGArgs& a) { return int64_t(a.workers) * a.mt * a.columns; }
+__device__ __forceinline__ unsigned tile_count(const WGArgs& a) { return unsigned(a.workers) * unsigned(a.mt) * unsigned(a.columns); }
 
 // Slot of a running number in a ring of DEPTH buffers, and the parity of the slot's round.
 template <int DEPTH> struct Ring {
@@ -203,17 +213,6 @@ __device__ __forceinline__ unsigned restore_pair(unsigned biased, unsigned sel0,
         const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
         return *reinterpret_cast<const unsigned*>(&h);
     }
-}
-
-template <typename G> __device__ __forceinline__ void put4(G* p, const float4& v);
-template <> __device__ __forceinline__ void put4(float* p, const float4& v) { __stcs(reinterpret_cast<float4*>(p), v); }
-template <> __device__ __forceinline__ void put4(__nv_bfloat16* p, const float4& v) {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-    __stcs(reinterpret_cast<uint2*>(p), make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b)));
-}
-template <> __device__ __forceinline__ void put4(__half* p, const float4& v) {
-    const __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
-    __stcs(reinterpret_cast<uint2*>(p), make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b)));
 }
 
 // dy by plain loads into the operand layout, zeros past the worker's tokens: warp `w` of a group of
@@ -251,18 +250,29 @@ __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t 
         const uintptr_t end = begin + 2 * uintptr_t((int64_t(a.workers) * a.tokens - 1) * a.ld_dy + a.out);
         const int c = (lane % 16) * 8;
         const int64_t o = o0 + c;
-#pragma unroll 4
-        for (int k = 0; k < 8; ++k) {
-            const int row = 16 * w + 2 * k + lane / 16;
-            const int64_t token = int64_t(step) * WG_K + row;
-            const unsigned short* src = dy + (int64_t(t.worker) * a.tokens + token) * a.ld_dy + o;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (token < t.len && o < a.out) {
-                const uintptr_t word = reinterpret_cast<uintptr_t>(src) & ~uintptr_t(15);
-                if (o + 8 <= a.out && word >= begin && word + 32 <= end) {
-                    const uint4 x = __ldg(reinterpret_cast<const uint4*>(word)), y = __ldg(reinterpret_cast<const uint4*>(word) + 1);
+        const unsigned short* row0 = dy + (int64_t(t.worker) * a.tokens + int64_t(step) * WG_K + 16 * w + lane / 16) * a.ld_dy + o;
+#pragma unroll
+        for (int k0 = 0; k0 < 8; k0 += 4) {
+            uint4 x[4], y[4];
+            bool words[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t token = int64_t(step) * WG_K + 16 * w + 2 * (k0 + k) + lane / 16;
+                const uintptr_t word = reinterpret_cast<uintptr_t>(row0 + 2 * (k0 + k) * a.ld_dy) & ~uintptr_t(15);
+                words[k] = token < t.len && o + 8 <= a.out && word >= begin && word + 32 <= end;
+                if (words[k]) {
+                    x[k] = __ldg(reinterpret_cast<const uint4*>(word));
+                    y[k] = __ldg(reinterpret_cast<const uint4*>(word) + 1);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int row = 16 * w + 2 * (k0 + k) + lane / 16;
+                const unsigned short* src = row0 + 2 * (k0 + k) * a.ld_dy;
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (words[k]) {
                     const unsigned by = unsigned(reinterpret_cast<uintptr_t>(src) & 15);
-                    unsigned h[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                    unsigned h[8] = {x[k].x, x[k].y, x[k].z, x[k].w, y[k].x, y[k].y, y[k].z, y[k].w};
 #pragma unroll
                     for (int j = 0; j < 6; ++j) h[j] = by & 8 ? h[j + 2] : h[j];
 #pragma unroll
@@ -270,14 +280,14 @@ __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t 
                     const unsigned bits = (by & 2) * 8;
                     v = make_uint4(__funnelshift_r(h[0], h[1], bits), __funnelshift_r(h[1], h[2], bits), __funnelshift_r(h[2], h[3], bits),
                                    __funnelshift_r(h[3], h[4], bits));
-                } else {
+                } else if (int64_t(step) * WG_K + row < t.len && o < a.out) {
                     unsigned h[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) h[j] = o + j < a.out ? __ldg(src + j) : 0u;
                     v = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
                 }
+                *reinterpret_cast<uint4*>(tile + (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4)) = v;
             }
-            *reinterpret_cast<uint4*>(tile + (c / 64) * WG_BLOCK + row * 128 + ((((c % 64) / 8) ^ (row & 7)) << 4)) = v;
         }
     }
 }
@@ -286,18 +296,19 @@ __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t 
 // still load a worker's last step if only some of its tokens count.
 template <typename T, typename G, int MODE>
 __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const WGArgs a, const __grid_constant__ CUtensorMap map_dy,
-                                                                          const __grid_constant__ CUtensorMap map_x) {
-    constexpr int WG_RING = wg_ring(MODE), WG_Q_RING = wg_q_ring(MODE), WG_GROUPS = wg_groups(MODE), WG_THREADS = wg_threads(MODE);
+                                                                          const __grid_constant__ CUtensorMap map_x,
+                                                                          const __grid_constant__ CUtensorMap map_dw) {
+    constexpr int WG_Q_RING = wg_q_ring(MODE), WG_GROUPS = wg_groups(MODE), WG_THREADS = wg_threads(MODE);
     constexpr bool TMA_A = MODE != WG_PLAIN_DY;
-    typedef WGSmem<WG_RING, WG_Q_RING> Smem;
+    typedef WGSmem<WG_Q_RING> Smem;
     extern __shared__ uint8_t raw[];
     Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     volatile int* error = &sm.error;
     const unsigned rank = cta_rank();
-    const int64_t pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const unsigned pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     if (tid == 0) {
-        sm.error = 0;
+        sm.error = sm.other_error = 0;
         for (int k = 0; k < WG_RING; ++k) {
             kb_init(&sm.empty[k], 1);
             kb_init(&sm.a_full[k], 1);
@@ -314,6 +325,11 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
         }
         kb_fence_init();
     }
+    if (tid == 32) {
+        prefetch_map(&map_x);
+        if (TMA_A) prefetch_map(&map_dy);
+        if (a.wide) prefetch_map(&map_dw);
+    }
     for (int i = tid; i < 512; i += WG_THREADS) sm.ones[i] = std::is_same<T, __half>::value ? 0x3c00 : 0x3f80;
     fence_async_smem();
     if (warp == WG_ALLOC_WARP) {
@@ -325,7 +341,7 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
     pair_sync();                              // the other CTA's barriers are initialised
     tc_fence_after();
     const unsigned tmem = sm.tmem_base;
-    const int64_t tiles = tile_count(a);
+    const unsigned tiles = tile_count(a);                   // below 2^30: i + pairs does not wrap
     // step s of a tile is number g + s of all the CTA's steps; of those with codes, number gq + s
     unsigned g = 0, gq = 0;
     bool ok = true;
@@ -334,7 +350,7 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
         if (TMA_A && lane == 0) {
             const unsigned leader_full = pair_address(kb_smem_u32(sm.a_full), 0);
             unsigned n_late = 0;
-            for (int64_t i = pair; ok && i < tiles; i += pairs) {
+            for (unsigned i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
                 const int o0 = (2 * t.m + int(rank)) * WG_M;
                 for (int s = 0; s < t.steps; ++s, ++g) {
@@ -371,7 +387,7 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
         }
     } else if (warp == WG_CODES_WARP) {
         if (MODE != WG_RESTORED && lane == 0) {
-            for (int64_t i = pair; ok && i < tiles; i += pairs) {
+            for (unsigned i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
                 if (t.n == a.nt) continue;
                 for (int s = 0; s < t.steps; ++s, ++gq) {
@@ -398,7 +414,7 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
             // a block of ones needs no layout: every address the descriptor reaches holds 1
             const unsigned long long desc_ones = operand_desc(kb_smem_u32(sm.ones), 256, 256, 0);
             unsigned n_acc = 0, n_late = 0;
-            for (int64_t i = pair; ok && i < tiles; i += pairs) {
+            for (unsigned i = pair; ok && i < tiles; i += pairs) {
                 const Tile t = tile_at(a, i);
                 const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
                 const bool partial = t.len % WG_K != 0;
@@ -449,7 +465,7 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
         // who does not follow the slot from round to round.
         const int w = warp - WG_RESTORE_WARP0;
         unsigned n_late = 0;
-        for (int64_t i = pair; a.lengths && i < tiles; i += pairs) {
+        for (unsigned i = pair; a.lengths && i < tiles; i += pairs) {
             const Tile t = tile_at(a, i);
             g += t.steps;
             if (t.len % WG_K == 0) continue;
@@ -474,7 +490,7 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 b_at[k][h] = row * 128 + (piece[k] >> 2) * WG_BLOCK + ((((piece[k] & 3) * 2 + h) ^ tl) << 4);
-        for (int64_t i = pair; ok && i < tiles; i += pairs) {
+        for (unsigned i = pair; ok && i < tiles; i += pairs) {
             const Tile t = tile_at(a, i);
             const bool bias = t.n == a.nt;
             const int64_t c0 = int64_t(t.n) * WG_N + rank * WG_HALF;
@@ -549,9 +565,9 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
         }
     } else if (warp >= WG_STORE_WARP0) {
         const int quarter = warp - WG_STORE_WARP0;               // == warp % 4: tensor-memory lanes 32 quarter ..
-        float* stage = sm.out[quarter];
-        unsigned n_acc = 0;
-        for (int64_t i = pair; ok && i < tiles; i += pairs) {
+        constexpr int COLS = 128 / int(sizeof(G));               // columns of a piece: rows of 128 bytes
+        unsigned n_acc = 0, n_piece = 0;
+        for (unsigned i = pair; ok && i < tiles; i += pairs) {
             const Tile t = tile_at(a, i);
             const Ring<2> acc(n_acc);
             const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M + quarter * 32;
@@ -566,35 +582,56 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
                 else v[0] = 0.f;
                 if (o0 + lane < a.out) static_cast<G*>(a.db)[int64_t(t.worker) * a.ld_grads + o0 + lane] = Elem<G>::narrow(v[0]);
             } else {
-                G* dw = static_cast<G*>(a.dw) + int64_t(t.worker) * a.ld_grads + o0 * a.in;
+                G* dw = static_cast<G*>(a.dw) + int64_t(t.worker) * a.ld_grads + o0 * a.in + int64_t(t.n) * WG_N;
                 const int rows = int(min(int64_t(32), a.out - o0));
                 const int64_t left = a.in - int64_t(t.n) * WG_N;
                 const int cols = left < WG_N ? int(left) : WG_N;
-                dw += int64_t(t.n) * WG_N;
-                for (int c0 = 0; c0 < cols; c0 += 32) {
+                for (int c0 = 0; c0 < cols && rows > 0; c0 += COLS, ++n_piece) {
+                    // this lane's row of the piece, as G
+                    unsigned piece[32];
                     float v[32];
-                    if (t.steps) {
-                        tmem_ld32(src + unsigned(c0), v);
-                    } else {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = 0.f;
-                    }
-                    __syncwarp();
+                    for (int h = 0; h < COLS / 32; ++h) {
+                        if (t.steps) {
+                            tmem_ld32(src + unsigned(c0 + 32 * h), v);
+                        } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)                  // four columns each, in an order that meets in no bank
-                        *reinterpret_cast<float4*>(stage + lane * 32 + ((j ^ (lane & 7)) << 2)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                    __syncwarp();
-                    if (a.wide && cols - c0 >= 32) {
-                        const int j = lane % 8;
-#pragma unroll
-                        for (int rr = 0; rr < 32; rr += 4) {
-                            const int row = rr + lane / 8;
-                            if (row < rows)
-                                put4(dw + int64_t(row) * a.in + c0 + 4 * j, *reinterpret_cast<const float4*>(stage + row * 32 + ((j ^ (row & 7)) << 2)));
+                            for (int j = 0; j < 32; ++j) v[j] = 0.f;
                         }
-                    } else if (lane < cols - c0) {
-                        for (int row = 0; row < rows; ++row)
-                            dw[int64_t(row) * a.in + c0 + lane] = Elem<G>::narrow(stage[row * 32 + (((lane >> 2) ^ (row & 7)) << 2) + (lane & 3)]);
+                        if constexpr (sizeof(G) == 4) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) piece[j] = __float_as_uint(v[j]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; j += 8) {
+                                const float f[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
+                                const uint4 p = narrow16B(f, static_cast<const G*>(nullptr));
+                                piece[16 * h + j / 2] = p.x;
+                                piece[16 * h + j / 2 + 1] = p.y;
+                                piece[16 * h + j / 2 + 2] = p.z;
+                                piece[16 * h + j / 2 + 3] = p.w;
+                            }
+                        }
+                    }
+                    // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
+                    char* stage = reinterpret_cast<char*>(sm.out[quarter][n_piece & 1]);
+                    if (lane == 0) tma_store_read<1>();
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(piece[4 * j], piece[4 * j + 1], piece[4 * j + 2], piece[4 * j + 3]);
+                    if (a.wide) {
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) tma_store(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker);
+                    } else {
+                        __syncwarp();
+                        for (int c = lane; c < min(COLS, cols - c0); c += 32) {
+                            const int at = (c * int(sizeof(G)) >> 4), in = c * int(sizeof(G)) & 15;
+                            for (int row = 0; row < rows; ++row)
+                                dw[int64_t(row) * a.in + c0 + c] = *reinterpret_cast<const G*>(stage + row * 128 + ((at ^ (row & 7)) << 4) + in);
+                        }
+                        __syncwarp();
                     }
                 }
             }
@@ -605,20 +642,21 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
                 ++n_acc;
             }
         }
+        if (lane == 0) tma_store_done();
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (tid == 0 && sm.error)
+        asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(pair_address(kb_smem_u32(&sm.other_error), rank ^ 1u)), "r"(1) : "memory");
+    __syncwarp();
     pair_sync();                              // the other CTA's products and arrivals have ended too
     tc_fence_after();
     if (warp == WG_ALLOC_WARP)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
-    int other;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(other) : "r"(pair_address(kb_smem_u32(&sm.error), rank ^ 1u)) : "memory");
-    pair_sync();                              // read before either CTA ends
-    if (sm.error || other) {
+    if (sm.error || *static_cast<volatile int*>(&sm.other_error)) {
         // a wait gave up: nothing the pair was to write may look like a gradient
-        for (int64_t i = pair; i < tiles; i += pairs) {
+        for (unsigned i = pair; i < tiles; i += pairs) {
             const Tile t = tile_at(a, i);
             for (int e = tid; e < WG_M * WG_N; e += WG_THREADS) {
                 const int64_t o = int64_t(2 * t.m + int(rank)) * WG_M + e / WG_N, c = int64_t(t.n) * WG_N + e % WG_N;
@@ -663,23 +701,28 @@ EncodeTiled encode_tiled() {
     return found;
 }
 
-// [workers][tokens][cols] with row stride `pitch` bytes; boxes of `box` columns x WG_K tokens
-cudaError_t make_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t cols, int64_t tokens, int workers,
-                     int64_t pitch, int box, CUtensorMapSwizzle swizzle) {
+// [depth][rows][cols] with strides of `pitch` and `plane` bytes; boxes of box x box_rows
+cudaError_t make_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t cols, int64_t rows, int depth,
+                     int64_t pitch, int64_t plane, int box, int box_rows, CUtensorMapSwizzle swizzle) {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return cudaErrorNotSupported;
-    const cuuint64_t rows = tokens > 0 ? cuuint64_t(tokens) : 1;
-    const cuuint64_t dims[3] = {cuuint64_t(cols), rows, cuuint64_t(workers)};
-    const cuuint64_t strides[2] = {cuuint64_t(pitch), cuuint64_t(pitch) * rows};
-    const cuuint32_t boxes[3] = {cuuint32_t(box), WG_K, 1}, steps[3] = {1, 1, 1};
+    const cuuint64_t dims[3] = {cuuint64_t(cols), cuuint64_t(rows), cuuint64_t(depth)};
+    const cuuint64_t strides[2] = {cuuint64_t(pitch), cuuint64_t(plane)};
+    const cuuint32_t boxes[3] = {cuuint32_t(box), cuuint32_t(box_rows), 1}, steps[3] = {1, 1, 1};
     const CUresult r = encode(map, type, 3, const_cast<void*>(base), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                               swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
+// the workers' tokens (at least one row, so that the map is valid; none is read without tokens)
+cudaError_t make_token_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t cols, int64_t tokens, int workers,
+                           int64_t pitch, int box, CUtensorMapSwizzle swizzle) {
+    const int64_t rows = tokens > 0 ? tokens : 1;
+    return make_map(map, type, base, cols, rows, workers, pitch, pitch * rows, box, WG_K, swizzle);
+}
 
 template <typename T, typename G, int MODE>
-cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x, int sm_count, cudaStream_t stream) {
-    constexpr int bytes = int(sizeof(WGSmem<wg_ring(MODE), wg_q_ring(MODE)>)) + 1024;
+cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x, const CUtensorMap& map_dw, int sm_count, cudaStream_t stream) {
+    constexpr int bytes = int(sizeof(WGSmem<wg_q_ring(MODE)>)) + 1024;
     static_assert(bytes <= 232448, "a CTA's shared memory");
     auto kernel = weight_grad_kernel<T, G, MODE>;
     if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
@@ -696,21 +739,21 @@ cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, map_dy, map_x);
+    return cudaLaunchKernelEx(&cfg, kernel, a, map_dy, map_x, map_dw);
 }
 template <typename T, int MODE>
-cudaError_t launch_by_grads(int grads_dtype, const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x, int sm_count,
+cudaError_t launch_by_grads(int grads_dtype, const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x, const CUtensorMap& map_dw, int sm_count,
                             cudaStream_t stream) {
-    if (grads_dtype == GAR_F32) return launch<T, float, MODE>(a, map_dy, map_x, sm_count, stream);
-    if (grads_dtype == GAR_BF16) return launch<T, __nv_bfloat16, MODE>(a, map_dy, map_x, sm_count, stream);
-    return launch<T, __half, MODE>(a, map_dy, map_x, sm_count, stream);
+    if (grads_dtype == GAR_F32) return launch<T, float, MODE>(a, map_dy, map_x, map_dw, sm_count, stream);
+    if (grads_dtype == GAR_BF16) return launch<T, __nv_bfloat16, MODE>(a, map_dy, map_x, map_dw, sm_count, stream);
+    return launch<T, __half, MODE>(a, map_dy, map_x, map_dw, sm_count, stream);
 }
 template <typename T>
 cudaError_t launch_by_mode(int mode, int grads_dtype, const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x,
-                           int sm_count, cudaStream_t stream) {
-    if (mode == WG_RESTORED) return launch_by_grads<T, WG_RESTORED>(grads_dtype, a, map_dy, map_x, sm_count, stream);
-    if (mode == WG_FUSED) return launch_by_grads<T, WG_FUSED>(grads_dtype, a, map_dy, map_x, sm_count, stream);
-    return launch_by_grads<T, WG_PLAIN_DY>(grads_dtype, a, map_dy, map_x, sm_count, stream);
+                           const CUtensorMap& map_dw, int sm_count, cudaStream_t stream) {
+    if (mode == WG_RESTORED) return launch_by_grads<T, WG_RESTORED>(grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
+    if (mode == WG_FUSED) return launch_by_grads<T, WG_FUSED>(grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
+    return launch_by_grads<T, WG_PLAIN_DY>(grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
 }
 
 bool rows_on_16(const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }
@@ -736,15 +779,14 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     a.mt = int((p.out_features + 2 * WG_M - 1) / (2 * WG_M));
     a.nt = int((p.in_features + WG_N - 1) / WG_N);
     a.columns = a.nt + (p.bias_grads ? 1 : 0);
-    if (int64_t(a.mt) * a.columns >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
+    if (int64_t(a.mt) * a.columns >= (int64_t(1) << 30) / a.workers) return cudaErrorInvalidConfiguration;
     const int64_t gs = p.grads_dtype == GAR_F32 ? 4 : 2;
-    const int64_t unit = 4 * gs;                  // a store of four gradients
-    a.wide = reinterpret_cast<uintptr_t>(p.weight_grads) % unit == 0 && (p.workers == 1 || p.ld_grads * gs % unit == 0) &&
-             p.in_features * gs % unit == 0;
+    a.wide = reinterpret_cast<uintptr_t>(p.weight_grads) % 16 == 0 && (p.workers == 1 || p.ld_grads * gs % 16 == 0) &&
+             p.in_features * gs % 16 == 0;
 
     const CUtensorMapDataType type = p.dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
-    CUtensorMap map_x, map_dy;
+    CUtensorMap map_x, map_dy, map_dw;
     int mode = rows_on_16(p.dy, ld_dy) ? WG_FUSED : WG_PLAIN_DY;
     if (p.workspace && p.tokens > 0) {
         // x restored once (and dy copied, if its rows do not start on 16 bytes), then products of plain copies
@@ -752,7 +794,7 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
         const int64_t rows = p.tokens * p.workers, ldx = round8(p.in_features);
         char* x = static_cast<char*>(p.workspace);
         if (cudaError_t err = launch_checkpoint_restore_masked(p, x, ldx, stream)) return err;
-        if (cudaError_t err = make_map(&map_x, type, x, p.in_features, p.tokens, p.workers, ldx * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+        if (cudaError_t err = make_token_map(&map_x, type, x, p.in_features, p.tokens, p.workers, ldx * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
         if (!rows_on_16(p.dy, ld_dy)) {
             char* dy = x + gar::align256(size_t(rows) * size_t(ldx) * 2);
             const int64_t ld = round8(p.out_features);
@@ -764,14 +806,23 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
             a.dy = dy;
             a.ld_dy = ld;
         }
-    } else if (cudaError_t err = make_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.x_saved.q, p.in_features, p.tokens, p.workers,
+    } else if (cudaError_t err = make_token_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.x_saved.q, p.in_features, p.tokens, p.workers,
                                           p.x_saved.ldq, WG_HALF, CU_TENSOR_MAP_SWIZZLE_NONE)) {
         return err;
     }
     if (mode == WG_PLAIN_DY) map_dy = map_x;      // not used
-    else if (cudaError_t err = make_map(&map_dy, type, a.dy, p.out_features, p.tokens, p.workers, a.ld_dy * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
-    return p.dtype == GAR_BF16 ? launch_by_mode<__nv_bfloat16>(mode, p.grads_dtype, a, map_dy, map_x, sm_count, stream)
-                               : launch_by_mode<__half>(mode, p.grads_dtype, a, map_dy, map_x, sm_count, stream);
+    else if (cudaError_t err = make_token_map(&map_dy, type, a.dy, p.out_features, p.tokens, p.workers, a.ld_dy * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+    if (!a.wide) {
+        map_dw = map_x;                           // not used
+    } else {
+        const CUtensorMapDataType gt = p.grads_dtype == GAR_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                       : p.grads_dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+        const int64_t pitch = p.in_features * gs, plane = p.workers > 1 ? p.ld_grads * gs : pitch * p.out_features;
+        if (cudaError_t err = make_map(&map_dw, gt, p.weight_grads, p.in_features, p.out_features, p.workers, pitch, plane, int(128 / gs), 32,
+                                       CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+    }
+    return p.dtype == GAR_BF16 ? launch_by_mode<__nv_bfloat16>(mode, p.grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream)
+                               : launch_by_mode<__half>(mode, p.grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
 }
 
 size_t weight_grad_workspace_bytes(const gar_weight_grad_params_t& p, int64_t ld_dy) {
