@@ -181,7 +181,9 @@ typedef struct gar_weight_grad_params_t {
     void*            stream;
 } gar_weight_grad_params_t;
 int gar_linear_weight_grad(const gar_weight_grad_params_t* params);
-/* Bytes of that workspace (host, pure; only sizes and dy's alignment are looked at).  0 on invalid sizes. */
+/* Bytes of that workspace (host, pure; the sizes, dy's alignment and whether lengths are given are looked
+ * at).  0 on invalid sizes and where none is used: up to 512 tokens, without lengths and with dy's rows on
+ * 16 bytes, every CTA restores the columns it works on once by itself. */
 size_t gar_weight_grad_workspace_bytes(const gar_weight_grad_params_t* params);
 
 #ifdef __cplusplus

@@ -283,10 +283,11 @@ gar_weight_grad_params_t weight_grad_sizes(const Tensor& dy, int64_t cols, int64
     return p;
 }
 
-PyObject* weight_grad_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {      // dy, cols, group
+PyObject* weight_grad_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {      // dy, cols, group, with lengths
     HANDLE_TH_ERRORS
-    need(n, 3);
-    const gar_weight_grad_params_t p = weight_grad_sizes(tensor(a[0], "dy"), integer(a[1]), integer(a[2]));
+    need(n, 4);
+    gar_weight_grad_params_t p = weight_grad_sizes(tensor(a[0], "dy"), integer(a[1]), integer(a[2]));
+    if (integer(a[3])) p.lengths = reinterpret_cast<const int32_t*>(16);      // only looked at for being there
     return PyLong_FromSize_t(gar_weight_grad_workspace_bytes(&p));
     END_HANDLE_TH_ERRORS
 }

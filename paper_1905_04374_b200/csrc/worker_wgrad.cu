@@ -38,32 +38,50 @@ namespace {
 
 constexpr int WG_M = 128, WG_N = 256, WG_K = 64;      // rows of a CTA, columns of a pair, tokens per step
 constexpr int WG_HALF = WG_N / 2;                     // columns a CTA restores
-// How the operands come: the restore warps load dy and restore x (rows of dy that do not start on 16
-// bytes); dy by TMA; both by TMA, x restored beforehand in the caller's workspace.
-enum Mode { WG_PLAIN_DY = 0, WG_FUSED = 1, WG_RESTORED = 2 };
-// Steps in flight: operand tiles (dy's and x's share a slot), copies of the codes.
-constexpr int WG_RING = 5;
-__host__ __device__ constexpr int wg_q_ring(int mode) { return mode == WG_RESTORED ? 1 : 4; }
+// How the operands come.
+//   WG_PLAIN_DY  the restore warps load dy (its rows do not start on 16 bytes) and restore x, step by step
+//   WG_FUSED     dy by TMA
+//   WG_RESTORED  both by TMA, x restored beforehand in the caller's workspace
+//   WG_PANEL     at most 512 tokens, so that the restored columns of x stay in shared memory while the
+//                output tiles of one worker go by: each code is restored once per CTA, and a step moves
+//                dy's 16 KB alone (the other modes are bound by the 32 KB a step moves from L2, 690 cycles
+//                against the products' 512)
+enum Mode { WG_PLAIN_DY = 0, WG_FUSED = 1, WG_RESTORED = 2, WG_PANEL = 3 };
+constexpr int WG_PANEL_STEPS = 8;                     // 512 tokens
+template <int MODE> struct Plan {
+    static constexpr int A_RING = MODE == WG_PANEL ? 4 : 5;                  // steps of dy in flight
+    static constexpr int B_SLOTS = MODE == WG_PANEL ? WG_PANEL_STEPS : 5;    // restored tiles
+    // Groups of four restore warps take steps in turn.  A step takes a group about 1500 cycles from its slot
+    // being free to the arrival (waits, reads, 220 instructions, fence), three times what the products take.
+    // A slot of codes belongs to one group for good (Q_RING is a multiple of GROUPS): who waits for a
+    // parity has to have followed the slot's rounds.
+    static constexpr int GROUPS = MODE == WG_RESTORED ? 1 : MODE == WG_PANEL ? 2 : 3;
+    static constexpr int Q_RING = MODE == WG_RESTORED ? 1 : MODE == WG_PANEL ? 2 : 6;
+    static constexpr int Q_BYTES = MODE == WG_RESTORED ? 1024 : 64 * 128;
+    static constexpr int OUT = MODE == WG_RESTORED ? 2 : 1;                  // staged pieces of a store warp
+    static constexpr int THREADS = 32 * (8 + 4 * GROUPS);
+    static_assert(Q_RING % GROUPS == 0, "a slot of codes belongs to one group");
+};
 constexpr int WG_DY_WARP = 0, WG_MMA_WARP = 1, WG_ALLOC_WARP = 2, WG_CODES_WARP = 3;
 constexpr int WG_STORE_WARP0 = 4;                     // 4..7: tensor-memory lanes 32 (warp % 4) ..
-// Groups of four restore warps take steps in turn: a step takes a group about 1500 cycles from its slot
-// being free to the arrival (waits, reads, 220 instructions, fence), three times what the products take.
 constexpr int WG_RESTORE_WARP0 = 8, WG_GROUP_WARPS = 4;
-__host__ __device__ constexpr int wg_groups(int mode) { return mode == WG_RESTORED ? 1 : 3; }
-__host__ __device__ constexpr int wg_threads(int mode) { return 32 * (WG_RESTORE_WARP0 + WG_GROUP_WARPS * wg_groups(mode)); }
 constexpr int WG_BLOCK = 64 * 128;                    // bytes of 64 tokens x 64 columns of an operand
 constexpr int WG_A_BYTES = WG_M / 64 * WG_BLOCK, WG_B_BYTES = WG_HALF / 64 * WG_BLOCK, WG_Q_BYTES = WG_K * WG_HALF;
 constexpr int WG_GROUP_M = 8;                         // (pair) row tiles that go round a column tile together
 constexpr int WG_BIAS_N = 16;
 
-template <int Q_RING> struct __align__(1024) WGSmem {
-    uint8_t  a[WG_RING][WG_A_BYTES];
-    uint8_t  b[WG_RING][WG_B_BYTES];
-    uint8_t  q[Q_RING][WG_Q_BYTES];
-    float    out[4][2][32 * 32];                          // a store warp's pieces of the tile: 32 rows of 128 bytes
+template <int MODE> struct __align__(1024) WGSmem {
+    typedef Plan<MODE> P;
+    uint8_t  a[P::A_RING][WG_A_BYTES];
+    uint8_t  b[P::B_SLOTS][WG_B_BYTES];
+    uint8_t  q[P::Q_RING][P::Q_BYTES];
+    float    out[4][P::OUT][32 * 32];                     // a store warp's pieces of the tile: 32 rows of 128 bytes
     uint16_t ones[512];
-    unsigned long long empty[WG_RING], q_full[Q_RING], q_empty[Q_RING], late[WG_RING], acc_full[2];
-    unsigned long long a_full[WG_RING], b_full[WG_RING], acc_empty[2];           // the leading CTA's are used, for both
+    // the operand slots are read (WG_PANEL: dy's; x's are b_empty); the codes are there, are read; dy's slot is
+    // the restore warps' to fill; the accumulators are complete
+    unsigned long long empty[P::A_RING], b_empty[P::B_SLOTS], q_full[P::Q_RING], q_empty[P::Q_RING], late[P::A_RING], acc_full[2];
+    // the leading CTA's are used, for both: the operands are there; the accumulators are read
+    unsigned long long a_full[P::A_RING], b_full[P::B_SLOTS], acc_empty[2];
     unsigned tmem_base;
     int      error, other_error;                          // a wait gave up, here or in the other CTA
 };
@@ -180,8 +198,18 @@ __device__ __forceinline__ int64_t worker_len(const WGArgs& a, int w) {
     const int64_t l = a.lengths[w];
     return l < 0 ? 0 : l < a.tokens ? l : a.tokens;
 }
+template <int MODE>
 __device__ __forceinline__ Tile tile_at(const WGArgs& a, unsigned index) {
     Tile t;
+    if (MODE == WG_PANEL) {              // the output tiles of a panel (a worker's column tile) one after the other
+        const unsigned panel = index / unsigned(a.mt), worker = panel / unsigned(a.columns);
+        t.m = int(index - panel * unsigned(a.mt));
+        t.n = int(panel - worker * unsigned(a.columns));
+        t.worker = int(worker);
+        t.len = a.tokens;
+        t.steps = int((t.len + WG_K - 1) / WG_K);
+        return t;
+    }
     const unsigned per = unsigned(a.mt) * unsigned(a.columns), worker = index / per, r = index - worker * per;
     const unsigned per_group = WG_GROUP_M * unsigned(a.columns), g = r / per_group, in_group = r - g * per_group;
     const unsigned rows = min(unsigned(WG_GROUP_M), unsigned(a.mt) - g * WG_GROUP_M);
@@ -194,6 +222,17 @@ __device__ __forceinline__ Tile tile_at(const WGArgs& a, unsigned index) {
 }
 __device__ __forceinline__ unsigned tile_count(const WGArgs& a) { return unsigned(a.workers) * unsigned(a.mt) * unsigned(a.columns); }
 
+// The tiles of a pair: every pairs-th one, or (WG_PANEL) a run of neighbours.
+struct Walk {
+    unsigned first, step, end;
+};
+template <int MODE>
+__device__ __forceinline__ Walk walk_of(const WGArgs& a, unsigned pair, unsigned pairs) {
+    const unsigned tiles = tile_count(a);                   // below 2^30: first + step does not wrap
+    if (MODE != WG_PANEL) return {pair, pairs, tiles};
+    return {unsigned(uint64_t(tiles) * pair / pairs), 1u, unsigned(uint64_t(tiles) * (pair + 1) / pairs)};
+}
+
 // Slot of a running number in a ring of DEPTH buffers, and the parity of the slot's round.
 template <int DEPTH> struct Ring {
     unsigned slot, parity;
@@ -201,6 +240,13 @@ template <int DEPTH> struct Ring {
 };
 
 // two codes' bytes of a word -> fp32 codes -> times the scale -> a pair of T
+// WG_PANEL: how often step s's slot of codes (slot s % Q_RING) was used before, `panels` panels of `steps`
+// steps having gone by.
+__device__ __forceinline__ unsigned panel_round(unsigned panels, int steps, int s) {
+    constexpr int RING = Plan<WG_PANEL>::Q_RING;
+    return panels * unsigned((steps - s % RING + RING - 1) / RING) + unsigned(s / RING);
+}
+
 template <typename T>
 __device__ __forceinline__ unsigned restore_pair(unsigned biased, unsigned sel0, unsigned sel1, f32x2 scale) {
     const f32x2 v = pack2(__uint_as_float(__byte_perm(biased, 0x4b000000u, sel0)), __uint_as_float(__byte_perm(biased, 0x4b000000u, sel1)));
@@ -295,12 +341,13 @@ __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t 
 // map_x: the codes, or (WG_RESTORED) the restored activation.  Where dy comes by TMA the restore warps
 // still load a worker's last step if only some of its tokens count.
 template <typename T, typename G, int MODE>
-__global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const WGArgs a, const __grid_constant__ CUtensorMap map_dy,
+__global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(const WGArgs a, const __grid_constant__ CUtensorMap map_dy,
                                                                           const __grid_constant__ CUtensorMap map_x,
                                                                           const __grid_constant__ CUtensorMap map_dw) {
-    constexpr int WG_Q_RING = wg_q_ring(MODE), WG_GROUPS = wg_groups(MODE), WG_THREADS = wg_threads(MODE);
+    typedef Plan<MODE> P;
+    constexpr int WG_RING = P::A_RING, WG_Q_RING = P::Q_RING, WG_GROUPS = P::GROUPS, WG_THREADS = P::THREADS;
     constexpr bool TMA_A = MODE != WG_PLAIN_DY;
-    typedef WGSmem<WG_Q_RING> Smem;
+    typedef WGSmem<MODE> Smem;
     extern __shared__ uint8_t raw[];
     Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -313,6 +360,9 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
             kb_init(&sm.empty[k], 1);
             kb_init(&sm.a_full[k], 1);
             kb_init(&sm.late[k], 1);
+        }
+        for (int k = 0; k < P::B_SLOTS; ++k) {
+            kb_init(&sm.b_empty[k], 1);
             kb_init(&sm.b_full[k], 2 * WG_GROUP_WARPS);
         }
         for (int k = 0; k < WG_Q_RING; ++k) {
@@ -341,7 +391,7 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
     pair_sync();                              // the other CTA's barriers are initialised
     tc_fence_after();
     const unsigned tmem = sm.tmem_base;
-    const unsigned tiles = tile_count(a);                   // below 2^30: i + pairs does not wrap
+    const Walk walk = walk_of<MODE>(a, pair, pairs);
     // step s of a tile is number g + s of all the CTA's steps; of those with codes, number gq + s
     unsigned g = 0, gq = 0;
     bool ok = true;
@@ -350,8 +400,8 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
         if (TMA_A && lane == 0) {
             const unsigned leader_full = pair_address(kb_smem_u32(sm.a_full), 0);
             unsigned n_late = 0;
-            for (unsigned i = pair; ok && i < tiles; i += pairs) {
-                const Tile t = tile_at(a, i);
+            for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
+                const Tile t = tile_at<MODE>(a, i);
                 const int o0 = (2 * t.m + int(rank)) * WG_M;
                 for (int s = 0; s < t.steps; ++s, ++g) {
                     const Ring<WG_RING> r(g);
@@ -386,9 +436,28 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
             }
         }
     } else if (warp == WG_CODES_WARP) {
-        if (MODE != WG_RESTORED && lane == 0) {
-            for (unsigned i = pair; ok && i < tiles; i += pairs) {
-                const Tile t = tile_at(a, i);
+        if (MODE == WG_PANEL && lane == 0) {
+            unsigned panels = 0, last_parity[WG_Q_RING];         // of a slot's latest copy; 2: none
+#pragma unroll
+            for (int k = 0; k < WG_Q_RING; ++k) last_parity[k] = 2u;
+            for (unsigned i = walk.first; ok && i < walk.end; ++i) {
+                const Tile t = tile_at<MODE>(a, i);
+                if (t.n == a.nt || (i != walk.first && t.m != 0)) continue;
+                for (int s = 0; s < t.steps; ++s) {
+                    const unsigned slot = unsigned(s) % WG_Q_RING, parity = panel_round(panels, t.steps, s) & 1u;
+                    if (!kb_wait(kb_smem_u32(&sm.q_empty[slot]), parity ^ 1u, error)) { ok = false; break; }
+                    const unsigned bar = kb_smem_u32(&sm.q_full[slot]);
+                    kb_expect_tx(bar, WG_Q_BYTES);
+                    tma_load(kb_smem_u32(sm.q[slot]), &map_x, t.n * WG_N + int(rank) * WG_HALF, s * WG_K, t.worker, bar);
+                    last_parity[slot] = parity;
+                }
+                ++panels;
+            }
+            for (unsigned k = 0; !ok && k < WG_Q_RING && last_parity[k] < 2u; ++k)
+                kb_wait(kb_smem_u32(&sm.q_full[k]), last_parity[k], error, true, 1u << 10);
+        } else if (MODE != WG_RESTORED && lane == 0) {
+            for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
+                const Tile t = tile_at<MODE>(a, i);
                 if (t.n == a.nt) continue;
                 for (int s = 0; s < t.steps; ++s, ++gq) {
                     const Ring<WG_Q_RING> r(gq);
@@ -413,9 +482,9 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
             const unsigned long long desc_b = operand_desc(kb_smem_u32(sm.b), WG_BLOCK, 1024, 2);
             // a block of ones needs no layout: every address the descriptor reaches holds 1
             const unsigned long long desc_ones = operand_desc(kb_smem_u32(sm.ones), 256, 256, 0);
-            unsigned n_acc = 0, n_late = 0;
-            for (unsigned i = pair; ok && i < tiles; i += pairs) {
-                const Tile t = tile_at(a, i);
+            unsigned n_acc = 0, n_late = 0, panels = 0;
+            for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
+                const Tile t = tile_at<MODE>(a, i);
                 const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
                 const bool partial = t.len % WG_K != 0;
                 if (steps == 0) continue;
@@ -424,10 +493,16 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
                 tc_fence_after();
                 const unsigned d = tmem + acc.slot * WG_N;
                 const bool bias = t.n == a.nt;
+                const bool panel_first = i == walk.first || t.m == 0, panel_last = i + 1 == walk.end || t.m + 1 == a.mt;
                 for (int s = 0; s < steps; ++s, ++g) {
                     const Ring<WG_RING> r(g);
                     if (TMA_A && !kb_wait_warp(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error)) { ok = false; break; }
-                    if (MODE != WG_RESTORED && !kb_wait_warp(kb_smem_u32(&sm.b_full[r.slot]), r.parity, error)) { ok = false; break; }
+                    if (MODE == WG_PANEL) {
+                        if (panel_first && !bias && !kb_wait_warp(kb_smem_u32(&sm.b_full[s]), panels & 1u, error)) { ok = false; break; }
+                    } else if (MODE != WG_RESTORED && !kb_wait_warp(kb_smem_u32(&sm.b_full[r.slot]), r.parity, error)) {
+                        ok = false;
+                        break;
+                    }
                     if (MODE == WG_RESTORED && a.lengths && s + 1 == steps && partial) {
                         const Ring<WG_RING> late(n_late++);
                         if (!kb_wait_warp(kb_smem_u32(&sm.b_full[late.slot]), late.parity, error)) { ok = false; break; }
@@ -435,15 +510,17 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
                     tc_fence_after();
                     // 16 tokens are 2048 bytes; addresses count 16 bytes
                     const unsigned long long da = desc_a + r.slot * (WG_A_BYTES / 16);
-                    const unsigned long long db = bias ? desc_ones : desc_b + r.slot * (WG_B_BYTES / 16);
+                    const unsigned long long db = bias ? desc_ones : desc_b + (MODE == WG_PANEL ? unsigned(s) : r.slot) * (WG_B_BYTES / 16);
                     const unsigned kind = bias ? idesc_bias : idesc, db_step = bias ? 0u : 128u;
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < WG_K / 16; ++k) mma_f16(d, da + k * 128u, db + k * db_step, kind, s > 0 || k > 0);
                         mma_commit(&sm.empty[r.slot]);
+                        if (MODE == WG_PANEL && panel_last && !bias) mma_commit(&sm.b_empty[s]);
                     }
                     __syncwarp();
                 }
+                if (MODE == WG_PANEL && panel_last && !bias) ++panels;
                 if (ok) {
                     if (elect_one()) mma_commit(&sm.acc_full[acc.slot]);
                     __syncwarp();
@@ -465,8 +542,8 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
         // who does not follow the slot from round to round.
         const int w = warp - WG_RESTORE_WARP0;
         unsigned n_late = 0;
-        for (unsigned i = pair; a.lengths && i < tiles; i += pairs) {
-            const Tile t = tile_at(a, i);
+        for (unsigned i = walk.first; a.lengths && i < walk.end; i += walk.step) {
+            const Tile t = tile_at<MODE>(a, i);
             g += t.steps;
             if (t.len % WG_K == 0) continue;
             const Ring<WG_RING> r(g - 1), late(n_late++);
@@ -490,9 +567,11 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 b_at[k][h] = row * 128 + (piece[k] >> 2) * WG_BLOCK + ((((piece[k] & 3) * 2 + h) ^ tl) << 4);
-        for (unsigned i = pair; ok && i < tiles; i += pairs) {
-            const Tile t = tile_at(a, i);
+        unsigned panels = 0;
+        for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
+            const Tile t = tile_at<MODE>(a, i);
             const bool bias = t.n == a.nt;
+            if (MODE == WG_PANEL && (bias || (i != walk.first && t.m != 0))) continue;
             const int64_t c0 = int64_t(t.n) * WG_N + rank * WG_HALF;
             const int len = int(t.len);
             const float* scale_at[2];                             // of the first row, for each piece
@@ -511,25 +590,36 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
                 for (int k = 0; k < 4; ++k)
                     next[k] = inside[k & 1] && token + 8 * (k >> 1) < len ? __ldg(scale_at[k & 1] + at + 8 * (k >> 1) * a.groups) : 0.f;
             };
-            int s = int((mine + WG_GROUPS - g % WG_GROUPS) % WG_GROUPS);       // this group's first step of the tile
+            // this group's first step of the tile; of a panel the group takes the same slots every time
+            int s = MODE == WG_PANEL ? int(mine) : int((mine + WG_GROUPS - g % WG_GROUPS) % WG_GROUPS);
             if (s < t.steps) fetch_scales(s);
             bool ready = false;                                   // the step's slots have been seen free and filled
             for (; s < t.steps; s += WG_GROUPS) {
-                const Ring<WG_RING> r(g + s);
-                const Ring<WG_Q_RING> rq(gq + s);
+                Ring<WG_RING> r(g + s);
+                Ring<WG_Q_RING> rq(gq + s);
+                unsigned long long* free_slot = &sm.empty[r.slot % WG_RING];
+                if (MODE == WG_PANEL) {
+                    r.slot = unsigned(s);
+                    r.parity = panels & 1u;
+                    rq.slot = unsigned(s) % WG_Q_RING;
+                    rq.parity = panel_round(panels, t.steps, s) & 1u;
+                    free_slot = &sm.b_empty[s];
+                }
                 float scale[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) scale[k] = next[k];
                 if (s + WG_GROUPS < t.steps) fetch_scales(s + WG_GROUPS);
                 if (!__all_sync(0xffffffffu, ready)) {
-                    if (!kb_wait_warp(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
+                    if (!kb_wait_warp(kb_smem_u32(free_slot), r.parity ^ 1u, error)) { ok = false; break; }
                     if (!bias && !kb_wait_warp(kb_smem_u32(&sm.q_full[rq.slot]), rq.parity, error)) { ok = false; break; }
                 }
-                // asked early, so that the answer is there when the next step of this group begins
-                const Ring<WG_RING> r2(g + s + WG_GROUPS);
-                const Ring<WG_Q_RING> rq2(gq + s + WG_GROUPS);
-                ready = s + WG_GROUPS < t.steps && !bias;
-                if (ready) ready = kb_test(kb_smem_u32(&sm.empty[r2.slot]), r2.parity ^ 1u) & kb_test(kb_smem_u32(&sm.q_full[rq2.slot]), rq2.parity);
+                if (MODE != WG_PANEL) {
+                    // asked early, so that the answer is there when the next step of this group begins
+                    const Ring<WG_RING> r2(g + s + WG_GROUPS);
+                    const Ring<WG_Q_RING> rq2(gq + s + WG_GROUPS);
+                    ready = s + WG_GROUPS < t.steps && !bias;
+                    if (ready) ready = kb_test(kb_smem_u32(&sm.empty[r2.slot]), r2.parity ^ 1u) & kb_test(kb_smem_u32(&sm.q_full[rq2.slot]), rq2.parity);
+                }
                 if (!bias) {
                     const uint8_t* q = sm.q[rq.slot] + q_at;
                     uint8_t* b = sm.b[r.slot];
@@ -552,7 +642,7 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
                 }
                 const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M;
                 if (!TMA_A) load_dy<false>(a, t, o0, s, sm.a[r.slot], w, lane);
-                else if (a.lengths && (s + 1) * WG_K > len) load_dy<true>(a, t, o0, s, sm.a[r.slot], w, lane);
+                else if (MODE != WG_PANEL && a.lengths && (s + 1) * WG_K > len) load_dy<true>(a, t, o0, s, sm.a[r.slot], w, lane);
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) {
@@ -562,13 +652,14 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
             }
             g += t.steps;
             if (!bias) gq += t.steps;
+            ++panels;
         }
     } else if (warp >= WG_STORE_WARP0) {
         const int quarter = warp - WG_STORE_WARP0;               // == warp % 4: tensor-memory lanes 32 quarter ..
         constexpr int COLS = 128 / int(sizeof(G));               // columns of a piece: rows of 128 bytes
         unsigned n_acc = 0, n_piece = 0;
-        for (unsigned i = pair; ok && i < tiles; i += pairs) {
-            const Tile t = tile_at(a, i);
+        for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
+            const Tile t = tile_at<MODE>(a, i);
             const Ring<2> acc(n_acc);
             const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M + quarter * 32;
             const unsigned src = tmem + acc.slot * WG_N + (unsigned(quarter * 32) << 16);
@@ -614,8 +705,8 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
                         }
                     }
                     // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
-                    char* stage = reinterpret_cast<char*>(sm.out[quarter][n_piece & 1]);
-                    if (lane == 0) tma_store_read<1>();
+                    char* stage = reinterpret_cast<char*>(sm.out[quarter][n_piece % P::OUT]);
+                    if (lane == 0) tma_store_read<P::OUT - 1>();
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
@@ -656,8 +747,8 @@ __global__ void __launch_bounds__(wg_threads(MODE), 1) weight_grad_kernel(const 
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     if (sm.error || *static_cast<volatile int*>(&sm.other_error)) {
         // a wait gave up: nothing the pair was to write may look like a gradient
-        for (unsigned i = pair; i < tiles; i += pairs) {
-            const Tile t = tile_at(a, i);
+        for (unsigned i = walk.first; i < walk.end; i += walk.step) {
+            const Tile t = tile_at<MODE>(a, i);
             for (int e = tid; e < WG_M * WG_N; e += WG_THREADS) {
                 const int64_t o = int64_t(2 * t.m + int(rank)) * WG_M + e / WG_N, c = int64_t(t.n) * WG_N + e % WG_N;
                 if (o >= a.out) continue;
@@ -722,7 +813,7 @@ cudaError_t make_token_map(CUtensorMap* map, CUtensorMapDataType type, const voi
 
 template <typename T, typename G, int MODE>
 cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x, const CUtensorMap& map_dw, int sm_count, cudaStream_t stream) {
-    constexpr int bytes = int(sizeof(WGSmem<wg_q_ring(MODE)>)) + 1024;
+    constexpr int bytes = int(sizeof(WGSmem<MODE>)) + 1024;
     static_assert(bytes <= 232448, "a CTA's shared memory");
     auto kernel = weight_grad_kernel<T, G, MODE>;
     if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
@@ -730,7 +821,7 @@ cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap
     const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(unsigned(2 * (tiles < pairs ? tiles : pairs)));
-    cfg.blockDim = dim3(wg_threads(MODE));
+    cfg.blockDim = dim3(Plan<MODE>::THREADS);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -751,6 +842,7 @@ cudaError_t launch_by_grads(int grads_dtype, const WGArgs& a, const CUtensorMap&
 template <typename T>
 cudaError_t launch_by_mode(int mode, int grads_dtype, const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap& map_x,
                            const CUtensorMap& map_dw, int sm_count, cudaStream_t stream) {
+    if (mode == WG_PANEL) return launch_by_grads<T, WG_PANEL>(grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
     if (mode == WG_RESTORED) return launch_by_grads<T, WG_RESTORED>(grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
     if (mode == WG_FUSED) return launch_by_grads<T, WG_FUSED>(grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
     return launch_by_grads<T, WG_PLAIN_DY>(grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
@@ -758,6 +850,11 @@ cudaError_t launch_by_mode(int mode, int grads_dtype, const WGArgs& a, const CUt
 
 bool rows_on_16(const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }
 int64_t round8(int64_t v) { return (v + 7) / 8 * 8; }
+// More than one output tile to reuse a panel for, tokens that fit one, and dy as TMA takes it: a length
+// that ends inside a step needs dy's last step masked, which this mode does not do.
+bool panel_applies(const gar_weight_grad_params_t& p, int64_t ld_dy) {
+    return rows_on_16(p.dy, ld_dy) && !p.lengths && p.tokens <= WG_PANEL_STEPS * WG_K && p.out_features > 2 * WG_M;
+}
 
 }  // namespace
 
@@ -788,7 +885,8 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     CUtensorMap map_x, map_dy, map_dw;
     int mode = rows_on_16(p.dy, ld_dy) ? WG_FUSED : WG_PLAIN_DY;
-    if (p.workspace && p.tokens > 0) {
+    if (panel_applies(p, ld_dy)) mode = WG_PANEL;
+    if (mode != WG_PANEL && p.workspace && p.tokens > 0) {
         // x restored once (and dy copied, if its rows do not start on 16 bytes), then products of plain copies
         mode = WG_RESTORED;
         const int64_t rows = p.tokens * p.workers, ldx = round8(p.in_features);
@@ -826,6 +924,7 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
 }
 
 size_t weight_grad_workspace_bytes(const gar_weight_grad_params_t& p, int64_t ld_dy) {
+    if (panel_applies(p, ld_dy)) return 0;
     const int64_t rows = p.tokens * p.workers;
     size_t bytes = gar::align256(size_t(rows) * size_t(round8(p.in_features)) * 2);
     if (!rows_on_16(p.dy, ld_dy)) bytes += gar::align256(size_t(rows) * size_t(round8(p.out_features)) * 2);

@@ -206,9 +206,9 @@ def gar_activation_backward(act: str, dy: torch.Tensor, x: Checkpoint, up: Optio
     return ActivationGrad(*r)
 
 
-def gar_weight_grad_workspace_bytes(dy: torch.Tensor, x: Checkpoint) -> int:
-    """Bytes of the workspace gar_linear_weight_grad takes for these operands."""
-    return (_native or _load()).weight_grad_workspace_bytes(dy, x.cols, x.group)
+def gar_weight_grad_workspace_bytes(dy: torch.Tensor, x: Checkpoint, lengths: Optional[torch.Tensor] = None) -> int:
+    """Bytes of the workspace gar_linear_weight_grad takes for these operands (0: it uses none)."""
+    return (_native or _load()).weight_grad_workspace_bytes(dy, x.cols, x.group, lengths is not None)
 
 
 def gar_linear_weight_grad(dy: torch.Tensor, x: Checkpoint, grads: Optional[torch.Tensor] = None, weight_offset: int = 0,

@@ -463,7 +463,7 @@ def check_weight_grad(pkg, dy, ck, grads_dtype="f32", lengths=None, off=0, gap=0
     r = pkg.gar_linear_weight_grad(dy, ck, grads, workspace=False, **place)
     assert r is grads
     # with the activation restored beforehand: the same products in the same order, the same bits
-    space = torch.empty(pkg.gar_weight_grad_workspace_bytes(dy, ck), dtype=torch.uint8, device=DEV)
+    space = torch.empty(pkg.gar_weight_grad_workspace_bytes(dy, ck, lengths), dtype=torch.uint8, device=DEV)
     other = pkg.gar_linear_weight_grad(dy, ck, torch.full_like(grads, 7.0), workspace=space, **place)
     assert torch.equal(other, grads)
     dw, db, sw, sb = weight_grad_64(dy, ck, pkg, lengths)
@@ -524,6 +524,20 @@ def test_weight_grad_lengths_over_many_tiles(pkg, tokens):
     lengths = torch.randint(0, tokens + 1, (n,), generator=gen(tokens), device=DEV, dtype=torch.int32)
     lengths[0], lengths[5], lengths[11] = tokens, 0, min(tokens, 128)
     check_weight_grad(pkg, dy, pkg.gar_checkpoint_pack(x, 128), lengths=lengths)
+
+
+@pytest.mark.parametrize("dtype,grads_dtype", [("bf16", "f32"), ("f16", "bf16")])
+@pytest.mark.parametrize("n,t,out,inp", [(1, 1, 264, 16), (3, 100, 520, 800), (2, 512, 1032, 264), (12, 150, 1104, 2104), (5, 513, 272, 520),
+                                         (40, 65, 800, 1300)])
+def test_weight_grad_panels(pkg, dtype, grads_dtype, n, t, out, inp):
+    """Several output tiles per worker at up to 512 tokens (and one more): panels of one to eight steps, runs of
+    tiles that begin and end inside a panel, workers and bias tiles in between; against 64 bits, and against
+    the same call with lengths that leave every token in (another path, the same order of products)."""
+    dy = normal((n, t, out), dtype, t + out)
+    ck = pkg.gar_checkpoint_pack(normal((n * t, inp), dtype, inp), 64)
+    g = check_weight_grad(pkg, dy, ck, grads_dtype)
+    lengths = torch.full((n,), t, dtype=torch.int32, device=DEV)
+    assert torch.equal(check_weight_grad(pkg, dy, ck, grads_dtype, lengths), g)
 
 
 def test_weight_grad_workers_do_not_meet(pkg):
