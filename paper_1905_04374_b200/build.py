@@ -95,7 +95,7 @@ def _build_worker_module(run, force: bool) -> None:
     run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
          "-I" + os.path.join(ROOT, "include"), "-isystem", os.path.join(base, "include"), "-isystem", sysconfig.get_paths()["include"],
          "-isystem", os.path.join(cuda, "include"), src, "-o", WORKER_MODULE, "-L" + PKG, "-lgar", "-L" + libs, "-lc10", "-lc10_cuda",
-         "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + libs])
+         "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + libs])
 
 
 if __name__ == "__main__":

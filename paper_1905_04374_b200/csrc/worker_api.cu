@@ -1,4 +1,6 @@
 // C entry points of the worker-side operators: argument checks, then one launch.
+#include <atomic>
+
 #include "gar_internal.cuh"
 #include "worker_common.cuh"
 
@@ -64,9 +66,13 @@ Span scales(const gar_checkpoint_t& s, int64_t rows, int64_t cols, int group) {
 }
 
 int sm_count(int* out) {
+    static std::atomic<int> known[64];                 // by device; the same value whoever stores it
     int dev = 0;
     if (int rc = cuda_status(cudaGetDevice(&dev))) return rc;
-    return cuda_status(cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev));
+    if (dev >= 0 && dev < 64 && (*out = known[dev].load(std::memory_order_relaxed)) > 0) return GAR_OK;
+    if (int rc = cuda_status(cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev))) return rc;
+    if (dev >= 0 && dev < 64) known[dev].store(*out, std::memory_order_relaxed);
+    return GAR_OK;
 }
 
 }  // namespace

@@ -4,6 +4,7 @@
 // took 15 to 35).  Nothing is computed here.  Every function returns its tensors, or the
 // gar_status_t of a refused call as an int.
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -14,6 +15,9 @@
 namespace {
 
 using at::Tensor;
+
+// An uninitialised CUDA tensor (the allocation alone, without a trip through the dispatcher).
+Tensor empty(at::IntArrayRef sizes, at::ScalarType type, at::Device dev) { return at::detail::empty_cuda(sizes, type, dev, c10::nullopt); }
 
 // A pointer that is not null for tensors without elements: the library refuses null before it looks at sizes.
 template <typename T = void> T* pointer(const Tensor& t) {
@@ -91,8 +95,7 @@ struct Held {
 };
 Held new_held(int64_t rows, int64_t cols, int64_t group, const Tensor& like) {
     TORCH_CHECK_VALUE(group == 32 || group == 64 || group == 128, "group must be 32, 64 or 128");
-    return {at::empty({rows, (cols + 15) / 16 * 16}, like.options().dtype(at::kChar)),
-            at::empty({rows, (cols + group - 1) / group}, like.options().dtype(at::kFloat))};
+    return {empty({rows, (cols + 15) / 16 * 16}, at::kChar, like.device()), empty({rows, (cols + group - 1) / group}, at::kFloat, like.device())};
 }
 gar_checkpoint_t saved(const Tensor& q, const Tensor& scales, const char* name, int64_t rows, int64_t cols, int64_t group, at::Device dev) {
     TORCH_CHECK_VALUE(group == 32 || group == 64 || group == 128, "group must be 32, 64 or 128");
@@ -110,22 +113,22 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {     // l
     const Tensor& x = tensor(a[0], "logits");
     const Matrix m = matrix(x, "logits");
     const c10::cuda::CUDAGuard guard(x.device());
-    const auto f32 = x.options().dtype(at::kFloat);
     const int64_t top = integer(a[2]);
     gar_logprobs_params_t p{};
     p.dtype = m.dtype; p.rows = m.rows; p.vocab = m.cols; p.ld = m.ld; p.logits = m.p;
     p.top = top >= 0 && top <= GAR_MAX_TOP ? int(top) : -1;
-    const Tensor entropy = at::empty({m.rows}, f32), lse = at::empty({m.rows}, f32), lse_lo = at::empty({m.rows}, f32);
+    const at::Device dev = x.device();
+    const Tensor entropy = empty({m.rows}, at::kFloat, dev), lse = empty({m.rows}, at::kFloat, dev), lse_lo = empty({m.rows}, at::kFloat, dev);
     p.entropy = pointer<float>(entropy); p.lse = pointer<float>(lse); p.lse_lo = pointer<float>(lse_lo);
     Tensor logprobs, top_logprobs, top_index;
     if (given(a[1])) {
         p.targets = vector<int64_t>(tensor(a[1], "targets"), "targets", at::kLong, m.rows, x.device());
-        logprobs = at::empty({m.rows}, f32);
+        logprobs = empty({m.rows}, at::kFloat, dev);
         p.logprobs = pointer<float>(logprobs);
     }
     if (p.top > 0) {
-        top_logprobs = at::empty({m.rows, top}, f32);
-        top_index = at::empty({m.rows, top}, x.options().dtype(at::kLong));
+        top_logprobs = empty({m.rows, top}, at::kFloat, dev);
+        top_index = empty({m.rows, top}, at::kLong, dev);
         p.top_logprobs = pointer<float>(top_logprobs); p.top_index = pointer<int64_t>(top_index);
     }
     p.stream = stream_of(a[3], x.device());
@@ -160,7 +163,7 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         p.top_index = vector<int64_t>(index, "saved.top_index", at::kLong, m.rows * p.top, dev);
         p.grad_top = vector<float>(tensor(a[8], "grad_top"), "grad_top", at::kFloat, m.rows * p.top, dev);
     }
-    const Tensor dx = given(a[9]) ? tensor(a[9], "dlogits") : at::empty({m.rows, m.cols}, x.options());
+    const Tensor dx = given(a[9]) ? tensor(a[9], "dlogits") : empty({m.rows, m.cols}, x.scalar_type(), x.device());
     const Matrix d = matrix_like(dx, "dlogits", x);
     p.dlogits = d.p; p.ld_dlogits = d.ld;
     p.stream = stream_of(a[10], dev);
@@ -191,7 +194,7 @@ PyObject* checkpoint_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {  // q
     const at::ScalarType type = code == GAR_F32 ? at::kFloat : code == GAR_BF16 ? at::kBFloat16 : at::kHalf;
     const c10::cuda::OptionalCUDAGuard guard(q.is_cuda() ? c10::make_optional(q.device()) : c10::nullopt);
     const gar_checkpoint_t s = saved(q, scales, "saved", rows, cols, group, q.device());
-    const Tensor out = given(a[5]) ? tensor(a[5], "out") : at::empty({rows, cols}, q.options().dtype(type));
+    const Tensor out = given(a[5]) ? tensor(a[5], "out") : empty({rows, cols}, type, q.device());
     const Matrix m = matrix(out, "out");
     TORCH_CHECK_TYPE(m.dtype == code, "out must be of the checkpoint's type");
     TORCH_CHECK_VALUE(m.rows == rows && m.cols == cols && out.device() == q.device(), "out must be [", rows, ", ", cols, "] on ", q.device());
@@ -215,7 +218,7 @@ PyObject* activation_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Matrix u = matrix_like(tensor(a[2], "up"), "up", x);
         p.up = u.p; p.ldup = u.ld;
     }
-    const Tensor y = given(a[6]) ? tensor(a[6], "y") : at::empty({m.rows, m.cols}, x.options());
+    const Tensor y = given(a[6]) ? tensor(a[6], "y") : empty({m.rows, m.cols}, x.scalar_type(), x.device());
     const Matrix my = matrix_like(y, "y", x);
     p.y = my.p; p.ldy = my.ld;
     Held hx, hu, hy;
@@ -250,13 +253,13 @@ PyObject* activation_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.act = int(integer(a[0])); p.group = int(integer(a[7]));
     p.dtype = m.dtype; p.rows = m.rows; p.cols = m.cols; p.dy = m.p; p.lddy = m.ld;
     p.x_saved = saved(tensor(a[2], "x.q"), tensor(a[3], "x.scales"), "x", m.rows, m.cols, p.group, dev);
-    const Tensor dx = given(a[8]) ? tensor(a[8], "dx") : at::empty({m.rows, m.cols}, dy.options());
+    const Tensor dx = given(a[8]) ? tensor(a[8], "dx") : empty({m.rows, m.cols}, dy.scalar_type(), dev);
     const Matrix mx = matrix_like(dx, "dx", dy);
     p.dx = mx.p; p.lddx = mx.ld;
     Tensor dup;
     if (given(a[4])) {
         p.up_saved = saved(tensor(a[4], "up.q"), tensor(a[5], "up.scales"), "up", m.rows, m.cols, p.group, dev);
-        dup = given(a[9]) ? tensor(a[9], "dup") : at::empty({m.rows, m.cols}, dy.options());
+        dup = given(a[9]) ? tensor(a[9], "dup") : empty({m.rows, m.cols}, dy.scalar_type(), dev);
         const Matrix mu = matrix_like(dup, "dup", dy);
         p.dup = mu.p; p.lddup = mu.ld;
     } else {
@@ -315,7 +318,7 @@ PyObject* linear_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.bias_grads = at_b >= 0 ? base + at_b * grads.element_size() : nullptr;
     p.ld_grads = g.ld;
     Tensor space;
-    if (a[9] == Py_True) space = at::empty({int64_t(gar_weight_grad_workspace_bytes(&p))}, dy.options().dtype(at::kByte));
+    if (a[9] == Py_True) space = empty({int64_t(gar_weight_grad_workspace_bytes(&p))}, at::kByte, dev);
     else if (a[9] != Py_False) space = tensor(a[9], "workspace");
     if (space.defined() && space.numel() > 0) {
         TORCH_CHECK_TYPE(space.is_cuda() && space.device() == dev && space.is_contiguous(), "workspace must be a contiguous tensor on ", dev);

@@ -28,6 +28,8 @@
 // roles leave their loops once what they have in flight has landed, and the CTA's tiles become NaN.
 #include <cuda.h>
 
+#include <atomic>
+
 #include "gar_internal.cuh"
 #include "mbar.cuh"
 #include "worker_common.cuh"
@@ -816,7 +818,13 @@ cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap
     constexpr int bytes = int(sizeof(WGSmem<MODE>)) + 1024;
     static_assert(bytes <= 232448, "a CTA's shared memory");
     auto kernel = weight_grad_kernel<T, G, MODE>;
-    if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
+    static std::atomic<uint64_t> allowed{0};           // devices on which the kernel may have that much
+    int dev = 0;
+    if (cudaError_t err = cudaGetDevice(&dev)) return err;
+    if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+        if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
+        if (dev < 64) allowed.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+    }
     const int64_t tiles = int64_t(a.workers) * a.mt * a.columns;
     const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
     cudaLaunchConfig_t cfg{};
