@@ -19,6 +19,32 @@ using at::Tensor;
 // An uninitialised CUDA tensor (the allocation alone, without a trip through the dispatcher).
 Tensor empty(at::IntArrayRef sizes, at::ScalarType type, at::Device dev) { return at::detail::empty_cuda(sizes, type, dev, c10::nullopt); }
 
+// Several uninitialised tensors in one allocation (each on 256 bytes), for results that are kept
+// together: an allocation and its release cost more than filling a parameter block.
+class Together {
+public:
+    explicit Together(at::Device dev) : dev_(dev) {}
+    // space for `numel` elements; the handle is the byte offset
+    int64_t reserve(int64_t numel, at::ScalarType type) {
+        const int64_t at = bytes_;
+        bytes_ += (numel * int64_t(c10::elementSize(type)) + 255) / 256 * 256;
+        return at;
+    }
+    void allocate() { whole_ = empty({bytes_}, at::kByte, dev_); }
+    Tensor view(int64_t at, at::IntArrayRef sizes, at::ScalarType type) const {
+        Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole_.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA),
+                                                            c10::scalarTypeToTypeMeta(type));
+        t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+        t.unsafeGetTensorImpl()->set_storage_offset(whole_.storage_offset() + at / int64_t(c10::elementSize(type)));
+        return t;
+    }
+
+private:
+    at::Device dev_;
+    int64_t    bytes_ = 0;
+    Tensor     whole_;
+};
+
 // A pointer that is not null for tensors without elements: the library refuses null before it looks at sizes.
 template <typename T = void> T* pointer(const Tensor& t) {
     void* p = t.data_ptr();
@@ -95,7 +121,11 @@ struct Held {
 };
 Held new_held(int64_t rows, int64_t cols, int64_t group, const Tensor& like) {
     TORCH_CHECK_VALUE(group == 32 || group == 64 || group == 128, "group must be 32, 64 or 128");
-    return {empty({rows, (cols + 15) / 16 * 16}, at::kChar, like.device()), empty({rows, (cols + group - 1) / group}, at::kFloat, like.device())};
+    const int64_t ld = (cols + 15) / 16 * 16, groups = (cols + group - 1) / group;
+    Together t(like.device());
+    const int64_t q = t.reserve(rows * ld, at::kChar), scales = t.reserve(rows * groups, at::kFloat);
+    t.allocate();
+    return {t.view(q, {rows, ld}, at::kChar), t.view(scales, {rows, groups}, at::kFloat)};
 }
 gar_checkpoint_t saved(const Tensor& q, const Tensor& scales, const char* name, int64_t rows, int64_t cols, int64_t group, at::Device dev) {
     TORCH_CHECK_VALUE(group == 32 || group == 64 || group == 128, "group must be 32, 64 or 128");
@@ -117,18 +147,24 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {     // l
     gar_logprobs_params_t p{};
     p.dtype = m.dtype; p.rows = m.rows; p.vocab = m.cols; p.ld = m.ld; p.logits = m.p;
     p.top = top >= 0 && top <= GAR_MAX_TOP ? int(top) : -1;
-    const at::Device dev = x.device();
-    const Tensor entropy = empty({m.rows}, at::kFloat, dev), lse = empty({m.rows}, at::kFloat, dev), lse_lo = empty({m.rows}, at::kFloat, dev);
+    const int64_t k = p.top > 0 ? p.top : 0;
+    Together t(x.device());
+    const int64_t at_ent = t.reserve(m.rows, at::kFloat), at_lse = t.reserve(m.rows, at::kFloat), at_lo = t.reserve(m.rows, at::kFloat),
+                  at_lp = t.reserve(given(a[1]) ? m.rows : 0, at::kFloat), at_top = t.reserve(m.rows * k, at::kFloat),
+                  at_index = t.reserve(m.rows * k, at::kLong);
+    t.allocate();
+    const Tensor entropy = t.view(at_ent, {m.rows}, at::kFloat), lse = t.view(at_lse, {m.rows}, at::kFloat),
+                 lse_lo = t.view(at_lo, {m.rows}, at::kFloat);
     p.entropy = pointer<float>(entropy); p.lse = pointer<float>(lse); p.lse_lo = pointer<float>(lse_lo);
     Tensor logprobs, top_logprobs, top_index;
     if (given(a[1])) {
         p.targets = vector<int64_t>(tensor(a[1], "targets"), "targets", at::kLong, m.rows, x.device());
-        logprobs = empty({m.rows}, at::kFloat, dev);
+        logprobs = t.view(at_lp, {m.rows}, at::kFloat);
         p.logprobs = pointer<float>(logprobs);
     }
-    if (p.top > 0) {
-        top_logprobs = empty({m.rows, top}, at::kFloat, dev);
-        top_index = empty({m.rows, top}, at::kLong, dev);
+    if (k > 0) {
+        top_logprobs = t.view(at_top, {m.rows, k}, at::kFloat);
+        top_index = t.view(at_index, {m.rows, k}, at::kLong);
         p.top_logprobs = pointer<float>(top_logprobs); p.top_index = pointer<int64_t>(top_index);
     }
     p.stream = stream_of(a[3], x.device());

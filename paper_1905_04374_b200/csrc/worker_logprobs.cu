@@ -575,11 +575,11 @@ __global__ void __launch_bounds__(cta_threads(WARPS), 1024 / cta_threads(WARPS))
 template <typename T>
 cudaError_t forward(const ForwardArgs& a, int sm_count, cudaStream_t stream) {
     if (a.vocab <= 256) {
-        const int lanes = a.vocab <= 64 ? 8 : 32;
+        const int lanes = a.vocab <= 16 ? 4 : a.vocab <= 64 ? 8 : 32;
         const int64_t blocks = (a.rows + LP_THREADS / lanes - 1) / (LP_THREADS / lanes);
         if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
         const unsigned n = unsigned(blocks);
-        if (a.vocab <= 16) logprobs_small_kernel<T, 8, 2><<<n, LP_THREADS, 0, stream>>>(a);
+        if (a.vocab <= 16) logprobs_small_kernel<T, 4, 4><<<n, LP_THREADS, 0, stream>>>(a);
         else if (a.vocab <= 64) logprobs_small_kernel<T, 8, 8><<<n, LP_THREADS, 0, stream>>>(a);
         else if (a.vocab <= 128) logprobs_small_kernel<T, 32, 4><<<n, LP_THREADS, 0, stream>>>(a);
         else logprobs_small_kernel<T, 32, 8><<<n, LP_THREADS, 0, stream>>>(a);
