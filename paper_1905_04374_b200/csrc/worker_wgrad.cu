@@ -50,9 +50,10 @@ constexpr int WG_HALF = WG_N / 2;                     // columns a CTA restores
 //                against the products' 512)
 enum Mode { WG_PLAIN_DY = 0, WG_FUSED = 1, WG_RESTORED = 2, WG_PANEL = 3 };
 constexpr int WG_PANEL_STEPS = 8;                     // 512 tokens
+constexpr int WG_CHUNK = 16;                          // steps per accumulator of an fp32 result
 template <int MODE> struct Plan {
-    static constexpr int A_RING = MODE == WG_PANEL ? 4 : 5;                  // steps of dy in flight
-    static constexpr int B_SLOTS = MODE == WG_PANEL ? WG_PANEL_STEPS : 5;    // restored tiles
+    static constexpr int A_RING = MODE == WG_RESTORED ? 5 : 4;               // steps of dy in flight
+    static constexpr int B_SLOTS = MODE == WG_PANEL ? WG_PANEL_STEPS : A_RING;    // restored tiles
     // Groups of four restore warps take steps in turn.  A step takes a group about 1500 cycles from its slot
     // being free to the arrival (waits, reads, 220 instructions, fence), three times what the products take.
     // A slot of codes belongs to one group for good (Q_RING is a multiple of GROUPS): who waits for a
@@ -60,7 +61,7 @@ template <int MODE> struct Plan {
     static constexpr int GROUPS = MODE == WG_RESTORED ? 1 : MODE == WG_PANEL ? 2 : 3;
     static constexpr int Q_RING = MODE == WG_RESTORED ? 1 : MODE == WG_PANEL ? 2 : 6;
     static constexpr int Q_BYTES = MODE == WG_RESTORED ? 1024 : 64 * 128;
-    static constexpr int OUT = MODE == WG_RESTORED ? 2 : 1;                  // staged pieces of a store warp
+    static constexpr int OUT = MODE == WG_PANEL ? 1 : 2;                     // staged pieces of a store warp
     static constexpr int THREADS = 32 * (8 + 4 * GROUPS);
     static_assert(Q_RING % GROUPS == 0, "a slot of codes belongs to one group");
 };
@@ -97,6 +98,7 @@ struct WGArgs {
     int            workers, groups, group_shift;
     int            mt, nt;                // pair row tiles, column tiles (the bias tile, if any, is one more)
     int            columns;               // nt + 1 with a bias
+    int            chunk;                 // steps per accumulator
     int            wide;                  // the result's rows start on 16 bytes: stored by TMA
 };
 
@@ -182,6 +184,12 @@ __device__ __forceinline__ void tma_load_pair(unsigned dst, const CUtensorMap* m
 // a piece of the result from shared memory (what lies outside the matrix is not written)
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, unsigned src, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// the same, added to what is there (fp32)
+__device__ __forceinline__ void tma_add(const CUtensorMap* map, unsigned src, int x, int y, int z) {
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
@@ -489,15 +497,25 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                 const Tile t = tile_at<MODE>(a, i);
                 const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
                 const bool partial = t.len % WG_K != 0;
-                if (steps == 0) continue;
-                const Ring<2> acc(n_acc);
-                if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[acc.slot]), acc.parity ^ 1u, error)) { ok = false; break; }
-                tc_fence_after();
-                const unsigned d = tmem + acc.slot * WG_N;
                 const bool bias = t.n == a.nt;
                 const bool panel_first = i == walk.first || t.m == 0, panel_last = i + 1 == walk.end || t.m + 1 == a.mt;
+                unsigned d = 0;
+                int begun = 0;                                   // the accumulator's first step
                 for (int s = 0; s < steps; ++s, ++g) {
                     const Ring<WG_RING> r(g);
+                    if (s == 0 || s - begun == a.chunk) {
+                        // on to the other accumulator
+                        if (s > 0) {
+                            if (elect_one()) mma_commit(&sm.acc_full[Ring<2>(n_acc).slot]);
+                            __syncwarp();
+                            ++n_acc;
+                        }
+                        const Ring<2> acc(n_acc);
+                        if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[acc.slot]), acc.parity ^ 1u, error)) { ok = false; break; }
+                        tc_fence_after();
+                        d = tmem + acc.slot * WG_N;
+                        begun = s;
+                    }
                     if (TMA_A && !kb_wait_warp(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error)) { ok = false; break; }
                     if (MODE == WG_PANEL) {
                         if (panel_first && !bias && !kb_wait_warp(kb_smem_u32(&sm.b_full[s]), panels & 1u, error)) { ok = false; break; }
@@ -516,15 +534,15 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     const unsigned kind = bias ? idesc_bias : idesc, db_step = bias ? 0u : 128u;
                     if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < WG_K / 16; ++k) mma_f16(d, da + k * 128u, db + k * db_step, kind, s > 0 || k > 0);
+                        for (int k = 0; k < WG_K / 16; ++k) mma_f16(d, da + k * 128u, db + k * db_step, kind, s > begun || k > 0);
                         mma_commit(&sm.empty[r.slot]);
                         if (MODE == WG_PANEL && panel_last && !bias) mma_commit(&sm.b_empty[s]);
                     }
                     __syncwarp();
                 }
                 if (MODE == WG_PANEL && panel_last && !bias) ++panels;
-                if (ok) {
-                    if (elect_one()) mma_commit(&sm.acc_full[acc.slot]);
+                if (ok && steps > 0) {
+                    if (elect_one()) mma_commit(&sm.acc_full[Ring<2>(n_acc).slot]);
                     __syncwarp();
                     ++n_acc;
                 }
@@ -662,77 +680,97 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
         unsigned n_acc = 0, n_piece = 0;
         for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
             const Tile t = tile_at<MODE>(a, i);
-            const Ring<2> acc(n_acc);
             const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M + quarter * 32;
-            const unsigned src = tmem + acc.slot * WG_N + (unsigned(quarter * 32) << 16);
-            if (t.steps) {
-                if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error)) { ok = false; break; }
-                tc_fence_after();
-            }
-            if (t.n == a.nt) {
-                float v[32];
-                if (t.steps) tmem_ld32(src, v);
-                else v[0] = 0.f;
-                if (o0 + lane < a.out) static_cast<G*>(a.db)[int64_t(t.worker) * a.ld_grads + o0 + lane] = Elem<G>::narrow(v[0]);
-            } else {
-                G* dw = static_cast<G*>(a.dw) + int64_t(t.worker) * a.ld_grads + o0 * a.in + int64_t(t.n) * WG_N;
-                const int rows = int(min(int64_t(32), a.out - o0));
-                const int64_t left = a.in - int64_t(t.n) * WG_N;
-                const int cols = left < WG_N ? int(left) : WG_N;
-                for (int c0 = 0; c0 < cols && rows > 0; c0 += COLS, ++n_piece) {
-                    // this lane's row of the piece, as G
-                    unsigned piece[32];
+            // the accumulators of the tile's chunks of tokens, in order: the first is stored, the others added
+            // to it (one chunk of zeros where the worker has no tokens)
+            for (int s0 = 0; s0 < max(t.steps, 1); s0 += a.chunk) {
+                const Ring<2> acc(n_acc);
+                const unsigned src = tmem + acc.slot * WG_N + (unsigned(quarter * 32) << 16);
+                if (t.steps) {
+                    if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error)) { ok = false; break; }
+                    tc_fence_after();
+                }
+                if (s0 > 0 && lane == 0) tma_store_done();           // the chunk before is in memory
+                __syncwarp();
+                if (t.n == a.nt) {
                     float v[32];
+                    if (t.steps) tmem_ld32(src, v);
+                    else v[0] = 0.f;
+                    if (o0 + lane < a.out) {
+                        G* db = static_cast<G*>(a.db) + int64_t(t.worker) * a.ld_grads + o0 + lane;
+                        *db = Elem<G>::narrow(s0 > 0 ? Elem<G>::widen(*db) + v[0] : v[0]);
+                    }
+                } else {
+                    G* dw = static_cast<G*>(a.dw) + int64_t(t.worker) * a.ld_grads + o0 * a.in + int64_t(t.n) * WG_N;
+                    const int rows = int(min(int64_t(32), a.out - o0));
+                    const int64_t left = a.in - int64_t(t.n) * WG_N;
+                    const int cols = left < WG_N ? int(left) : WG_N;
+                    for (int c0 = 0; c0 < cols && rows > 0; c0 += COLS, ++n_piece) {
+                        // this lane's row of the piece, as G
+                        unsigned piece[32];
+                        float v[32];
 #pragma unroll
-                    for (int h = 0; h < COLS / 32; ++h) {
-                        if (t.steps) {
-                            tmem_ld32(src + unsigned(c0 + 32 * h), v);
-                        } else {
+                        for (int h = 0; h < COLS / 32; ++h) {
+                            if (t.steps) {
+                                tmem_ld32(src + unsigned(c0 + 32 * h), v);
+                            } else {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = 0.f;
-                        }
-                        if constexpr (sizeof(G) == 4) {
+                                for (int j = 0; j < 32; ++j) v[j] = 0.f;
+                            }
+                            if constexpr (sizeof(G) == 4) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) piece[j] = __float_as_uint(v[j]);
-                        } else {
+                                for (int j = 0; j < 32; ++j) piece[j] = __float_as_uint(v[j]);
+                            } else {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 8) {
-                                const float f[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
-                                const uint4 p = narrow16B(f, static_cast<const G*>(nullptr));
-                                piece[16 * h + j / 2] = p.x;
-                                piece[16 * h + j / 2 + 1] = p.y;
-                                piece[16 * h + j / 2 + 2] = p.z;
-                                piece[16 * h + j / 2 + 3] = p.w;
+                                for (int j = 0; j < 32; j += 8) {
+                                    const float f[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
+                                    const uint4 p = narrow16B(f, static_cast<const G*>(nullptr));
+                                    piece[16 * h + j / 2] = p.x;
+                                    piece[16 * h + j / 2 + 1] = p.y;
+                                    piece[16 * h + j / 2 + 2] = p.z;
+                                    piece[16 * h + j / 2 + 3] = p.w;
+                                }
                             }
                         }
-                    }
-                    // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
-                    char* stage = reinterpret_cast<char*>(sm.out[quarter][n_piece % P::OUT]);
-                    if (lane == 0) tma_store_read<P::OUT - 1>();
-                    __syncwarp();
+                        // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
+                        char* stage = reinterpret_cast<char*>(sm.out[quarter][n_piece % P::OUT]);
+                        if (lane == 0) tma_store_read<P::OUT - 1>();
+                        __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(piece[4 * j], piece[4 * j + 1], piece[4 * j + 2], piece[4 * j + 3]);
-                    if (a.wide) {
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) tma_store(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker);
-                    } else {
-                        __syncwarp();
-                        for (int c = lane; c < min(COLS, cols - c0); c += 32) {
-                            const int at = (c * int(sizeof(G)) >> 4), in = c * int(sizeof(G)) & 15;
-                            for (int row = 0; row < rows; ++row)
-                                dw[int64_t(row) * a.in + c0 + c] = *reinterpret_cast<const G*>(stage + row * 128 + ((at ^ (row & 7)) << 4) + in);
+                        for (int j = 0; j < 8; ++j)
+                            *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(piece[4 * j], piece[4 * j + 1], piece[4 * j + 2], piece[4 * j + 3]);
+                        if (a.wide) {
+                            fence_async_smem();
+                            __syncwarp();
+                            if (lane == 0 && s0 == 0) tma_store(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker);
+                            if (lane == 0 && s0 > 0) tma_add(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker);
+                        } else {
+                            __syncwarp();
+                            for (int c = lane; c < min(COLS, cols - c0); c += 32) {
+                                const int at = (c * int(sizeof(G)) >> 4), in = c * int(sizeof(G)) & 15;
+                                // eight rows at a time: what is there is asked for before anything is added
+                                for (int row = 0; row < rows; row += 8) {
+                                    G* p = dw + int64_t(row) * a.in + c0 + c;
+                                    float old[8];
+#pragma unroll
+                                    for (int k = 0; k < 8; ++k) old[k] = s0 > 0 && row + k < rows ? Elem<G>::widen(p[int64_t(k) * a.in]) : 0.f;
+#pragma unroll
+                                    for (int k = 0; k < 8; ++k) {
+                                        const G v = *reinterpret_cast<const G*>(stage + (row + k) * 128 + ((at ^ ((row + k) & 7)) << 4) + in);
+                                        if (row + k < rows) p[int64_t(k) * a.in] = s0 > 0 ? Elem<G>::narrow(old[k] + Elem<G>::widen(v)) : v;
+                                    }
+                                }
+                            }
+                            __syncwarp();
                         }
-                        __syncwarp();
                     }
                 }
-            }
-            if (t.steps) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) arrive_at_leader(&sm.acc_empty[acc.slot]);
-                ++n_acc;
+                if (t.steps) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_at_leader(&sm.acc_empty[acc.slot]);
+                    ++n_acc;
+                }
             }
         }
         if (lane == 0) tma_store_done();
@@ -886,6 +924,10 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     a.columns = a.nt + (p.bias_grads ? 1 : 0);
     if (int64_t(a.mt) * a.columns >= (int64_t(1) << 30) / a.workers) return cudaErrorInvalidConfiguration;
     const int64_t gs = p.grads_dtype == GAR_F32 ? 4 : 2;
+    // The tensor core truncates what it adds to an accumulator: the sum loses 1e-9 of itself per token (measured:
+    // 4.4e-6 at 4096 tokens, seven times what rounded additions lose there).  fp32 results are summed in chunks
+    // of 1024 tokens, joined by rounded additions: 1e-6 at any length.  16-bit results round off 2e-3.
+    a.chunk = p.grads_dtype == GAR_F32 ? WG_CHUNK : 0x40000000;
     a.wide = reinterpret_cast<uintptr_t>(p.weight_grads) % 16 == 0 && (p.workers == 1 || p.ld_grads * gs % 16 == 0) &&
              p.in_features * gs % 16 == 0;
 

@@ -16,9 +16,6 @@ import torch
 from .binding import GRAD_DTYPES, _check, lib as _base_lib
 
 GAR_MAX_TOP = 32
-# Outputs from which gar_linear_weight_grad takes a workspace by itself: every 256 outputs restore the
-# activation once more.
-WORKSPACE_OUT = 1024
 ACTIVATIONS = {"identity": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 
@@ -231,8 +228,6 @@ def gar_linear_weight_grad(dy: torch.Tensor, x: Checkpoint, grads: Optional[torc
         grads = torch.empty(dy.shape[0], out * x.cols, dtype=grads_dtype, device=dy.device)
     if bias_offset is not None and bias_offset < 0:
         raise ValueError("bias_offset must not be negative")
-    if workspace is None:
-        workspace = out > WORKSPACE_OUT
     r = (_native or _load()).linear_weight_grad(dy, x.q, x.scales, x.cols, x.group, grads, weight_offset,
                                                 -1 if bias_offset is None else bias_offset, lengths, workspace, _handle(stream))
     if r:
