@@ -25,10 +25,11 @@ struct FastDiv {
     __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
 };
 
-// How a matrix lies: any rows; rows that start on 16 bytes; or (DENSE) every matrix of the call without
+// How a matrix lies: any rows; rows of 16-bit elements that start on 4 bytes (CK_WORD); rows that start
+// on 16 bytes; or (DENSE) every matrix of the call without
 // gaps between its rows and of whole groups, so that a task's number gives its place everywhere and
 // nothing is divided, multiplied or checked: 70 of 184 instructions per task of the pack.
-enum Layout { CK_ANY = 0, CK_VEC = 1, CK_DENSE = 2 };
+enum Layout { CK_ANY = 0, CK_VEC = 1, CK_DENSE = 2, CK_WORD = 3 };
 
 // Eight consecutive elements as they lie in memory (Raw8: one or two 16-byte words).
 template <typename T> struct Raw8;
@@ -41,7 +42,7 @@ template <typename T, int LAYOUT>
 __device__ __forceinline__ Raw8<T> load8(const T* p, int count) {
     Raw8<T> r{};
     if constexpr (sizeof(T) == 4) {
-        if (LAYOUT != CK_ANY && count == 8) {
+        if ((LAYOUT == CK_VEC || LAYOUT == CK_DENSE) && count == 8) {
             r.a = load_stream(p);
             r.b = load_stream(p + 4);
         } else if (LAYOUT != CK_DENSE) {
@@ -52,8 +53,11 @@ __device__ __forceinline__ Raw8<T> load8(const T* p, int count) {
             r.b = make_uint4(w[4], w[5], w[6], w[7]);
         }
     } else {
-        if (LAYOUT != CK_ANY && count == 8) {
+        if ((LAYOUT == CK_VEC || LAYOUT == CK_DENSE) && count == 8) {
             r.a = load_stream(p);
+        } else if (LAYOUT == CK_WORD && count == 8) {
+            const unsigned* w = reinterpret_cast<const unsigned*>(p);
+            r.a = make_uint4(__ldcs(w), __ldcs(w + 1), __ldcs(w + 2), __ldcs(w + 3));
         } else if (LAYOUT != CK_DENSE) {
             const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
             unsigned w[8];
@@ -67,7 +71,7 @@ __device__ __forceinline__ Raw8<T> load8(const T* p, int count) {
 template <typename T, int LAYOUT>
 __device__ __forceinline__ void store8(T* p, int count, const Raw8<T>& r) {
     if constexpr (sizeof(T) == 4) {
-        if (LAYOUT != CK_ANY && count == 8) {
+        if ((LAYOUT == CK_VEC || LAYOUT == CK_DENSE) && count == 8) {
             store_stream(p, r.a);
             store_stream(p + 4, r.b);
         } else if (LAYOUT != CK_DENSE) {
@@ -77,8 +81,14 @@ __device__ __forceinline__ void store8(T* p, int count, const Raw8<T>& r) {
                 if (i < count) p[i] = __uint_as_float(w[i]);
         }
     } else {
-        if (LAYOUT != CK_ANY && count == 8) {
+        if ((LAYOUT == CK_VEC || LAYOUT == CK_DENSE) && count == 8) {
             store_stream(p, r.a);
+        } else if (LAYOUT == CK_WORD && count == 8) {
+            unsigned* w = reinterpret_cast<unsigned*>(p);
+            __stcs(w, r.a.x);
+            __stcs(w + 1, r.a.y);
+            __stcs(w + 2, r.a.z);
+            __stcs(w + 3, r.a.w);
         } else if (LAYOUT != CK_DENSE) {
             const unsigned w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
             unsigned short* h = reinterpret_cast<unsigned short*>(p);
@@ -417,8 +427,21 @@ __global__ void __launch_bounds__(CK_THREADS) checkpoint_restore_kernel(const Re
 // ---- launches ---------------------------------------------------------------------------------
 int log2_lanes(int group) { return group == 32 ? 2 : group == 64 ? 3 : 4; }
 
-bool aligned16(const void* p, int64_t ld, size_t esize) {
-    return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * int64_t(esize)) % 16 == 0);
+// rows that start on `to` bytes
+bool rows_on(int64_t to, const void* p, int64_t ld, size_t esize) {
+    return !p || (reinterpret_cast<uintptr_t>(p) % to == 0 && (ld * int64_t(esize)) % to == 0);
+}
+struct Rows {
+    const void* p;
+    int64_t     ld;
+};
+int layout_of(std::initializer_list<Rows> all, size_t esize) {
+    int layout = CK_VEC;
+    for (const Rows& r : all) {
+        if (!rows_on(4, r.p, r.ld, esize)) return CK_ANY;
+        if (!rows_on(16, r.p, r.ld, esize)) layout = esize == 2 ? CK_WORD : CK_ANY;
+    }
+    return layout;
 }
 // a checkpoint that is not asked for, or whose rows have no gap
 bool gapless(const gar_checkpoint_t& s, int64_t cols) { return !s.q || s.ldq == cols; }
@@ -449,6 +472,7 @@ template <typename T, typename F>
 void by_layout(int layout, F f) {
     if (layout == CK_DENSE) f(T{}, Int<CK_DENSE>{});
     else if (layout == CK_VEC) f(T{}, Int<CK_VEC>{});
+    else if (sizeof(T) == 2 && layout == CK_WORD) f(T{}, Int<sizeof(T) == 2 ? CK_WORD : CK_ANY>{});
     else f(T{}, Int<CK_ANY>{});
 }
 template <typename F>
@@ -481,7 +505,7 @@ cudaError_t launch_activation_forward(const gar_activation_params_t& p) {
     a.lane_shift = log2_lanes(p.group);
     a.lanes = 1 << a.lane_shift;
     const size_t es = esize_of(p.dtype);
-    int layout = aligned16(p.x, p.ldx, es) && aligned16(p.up, p.ldup, es) && aligned16(p.y, p.ldy, es) ? CK_VEC : CK_ANY;
+    int layout = layout_of({{p.x, p.ldx}, {p.up, p.ldup}, {p.y, p.ldy}}, es);
     if (layout == CK_VEC && p.cols % p.group == 0 && p.ldx == p.cols && (!p.up || p.ldup == p.cols) && (!p.y || p.ldy == p.cols) &&
         gapless(p.x_saved, p.cols) && gapless(p.up_saved, p.cols) && gapless(p.y_saved, p.cols))
         layout = CK_DENSE;
@@ -511,7 +535,7 @@ cudaError_t launch_activation_backward(const gar_activation_grad_params_t& p) {
     a.groups = int((p.cols + p.group - 1) / p.group);
     a.lane_shift = log2_lanes(p.group);
     const size_t es = esize_of(p.dtype);
-    int layout = aligned16(p.dy, p.lddy, es) && aligned16(p.dx, p.lddx, es) && aligned16(p.dup, p.lddup, es) ? CK_VEC : CK_ANY;
+    int layout = layout_of({{p.dy, p.lddy}, {p.dx, p.lddx}, {p.dup, p.lddup}}, es);
     if (layout == CK_VEC && p.cols % p.group == 0 && p.lddy == p.cols && p.lddx == p.cols && (!p.dup || p.lddup == p.cols) &&
         gapless(p.x_saved, p.cols) && gapless(p.up_saved, p.cols))
         layout = CK_DENSE;
@@ -544,7 +568,7 @@ cudaError_t restore(int dtype, const gar_checkpoint_t& saved, int64_t rows, int6
     a.lane_shift = log2_lanes(group);
     a.lengths = lengths;
     a.tokens = tokens;
-    int layout = aligned16(x, ldx, esize_of(dtype)) ? CK_VEC : CK_ANY;
+    int layout = layout_of({{x, ldx}}, esize_of(dtype));
     if (layout == CK_VEC && !lengths && cols % group == 0 && ldx == cols && gapless(saved, cols)) layout = CK_DENSE;
     return over_rows(rows, per_row, [&](int64_t r0, unsigned tasks, unsigned blocks) {
         a.row0 = layout == CK_DENSE ? r0 * per_row : r0;
