@@ -191,7 +191,7 @@ int gar_checkpoint_unpack(int dtype, const gar_checkpoint_t* saved, int64_t rows
 
 size_t gar_weight_grad_workspace_bytes(const gar_weight_grad_params_t* p) {
     const int64_t limit = int64_t(1) << 31;
-    if (!p || p->workers < 1 || p->workers > GAR_MAX_N || p->tokens < 0 || p->tokens >= limit / p->workers) return 0;
+    if (!p || p->workers < 1 || p->workers > GAR_MAX_N || p->tokens < 0 || p->tokens >= limit / 2 / p->workers) return 0;
     if (p->out_features < 1 || p->in_features < 1 || p->out_features >= limit || p->in_features >= limit) return 0;
     return gar::worker::weight_grad_workspace_bytes(*p, p->ld_dy ? p->ld_dy : p->out_features);
 }
@@ -203,9 +203,9 @@ int gar_linear_weight_grad(const gar_weight_grad_params_t* p) {
     if (p->workers > GAR_MAX_N || p->dtype == GAR_F32) return GAR_ERR_UNSUPPORTED;
     const size_t es = esize(p->dtype), gs = esize(p->grads_dtype);
     if (!aligned(p->dy, es) || !aligned(p->weight_grads, gs) || !aligned(p->bias_grads, gs)) return GAR_ERR_INVALID_ARG;
-    // sizes a launch can index: tokens of all workers and both widths below 2^31
+    // sizes a launch can index: tokens of all workers below 2^30, both widths below 2^31
     const int64_t limit = int64_t(1) << 31;
-    if (p->tokens >= limit / p->workers || p->out_features >= limit || p->in_features >= limit) return GAR_ERR_UNSUPPORTED;
+    if (p->tokens >= limit / 2 / p->workers || p->out_features >= limit || p->in_features >= limit) return GAR_ERR_UNSUPPORTED;
     int64_t ld_dy = p->ld_dy;
     if (p->ld_grads < 0 || p->ld_grads > (int64_t(1) << 59) / p->workers) return GAR_ERR_INVALID_ARG;
     const int64_t rows = p->tokens * p->workers, weights = p->out_features * p->in_features;

@@ -102,9 +102,22 @@ int64_t integer(PyObject* o) {
     return v;
 }
 void need(Py_ssize_t n, Py_ssize_t want) { TORCH_CHECK_TYPE(n == want, "expected ", want, " arguments, got ", n); }
-void* stream_of(PyObject* o, at::Device dev) {
-    return given(o) ? reinterpret_cast<void*>(integer(o)) : static_cast<void*>(c10::cuda::getCurrentCUDAStream(dev.index()).stream());
-}
+// The device and, where the caller names a stream, that stream made current for the call: what it
+// allocates (results, workspace) then belongs to the stream that uses it.
+class Place {
+public:
+    Place(at::Device dev, PyObject* stream) : dev_(dev), guard_(dev) {
+        if (!given(stream)) return;
+        cudaStream_t s = reinterpret_cast<cudaStream_t>(integer(stream));
+        on_.reset_stream(s ? c10::cuda::getStreamFromExternal(s, dev.index()) : c10::cuda::getDefaultCUDAStream(dev.index()));
+    }
+    void* stream() const { return c10::cuda::getCurrentCUDAStream(dev_.index()).stream(); }
+
+private:
+    at::Device                        dev_;
+    c10::cuda::OptionalCUDAGuard      guard_;
+    c10::cuda::OptionalCUDAStreamGuard on_;
+};
 // the result tuple; undefined tensors become None
 PyObject* tuple_of(std::initializer_list<Tensor> ts) {
     PyObject* r = PyTuple_New(Py_ssize_t(ts.size()));
@@ -142,7 +155,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {     // l
     need(n, 4);
     const Tensor& x = tensor(a[0], "logits");
     const Matrix m = matrix(x, "logits");
-    const c10::cuda::CUDAGuard guard(x.device());
+    const Place place(x.device(), a[3]);
     const int64_t top = integer(a[2]);
     gar_logprobs_params_t p{};
     p.dtype = m.dtype; p.rows = m.rows; p.vocab = m.cols; p.ld = m.ld; p.logits = m.p;
@@ -167,7 +180,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {     // l
         top_index = t.view(at_index, {m.rows, k}, at::kLong);
         p.top_logprobs = pointer<float>(top_logprobs); p.top_index = pointer<int64_t>(top_index);
     }
-    p.stream = stream_of(a[3], x.device());
+    p.stream = place.stream();
     if (const int st = gar_token_logprobs(&p)) return status(st);
     return tuple_of({logprobs, entropy, lse, top_logprobs, top_index, lse_lo});
     END_HANDLE_TH_ERRORS
@@ -180,7 +193,7 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor& x = tensor(a[0], "logits");
     const Matrix m = matrix(x, "logits");
     const at::Device dev = x.device();
-    const c10::cuda::CUDAGuard guard(dev);
+    const Place place(dev, a[10]);
     gar_logprobs_grad_params_t p{};
     p.dtype = m.dtype; p.rows = m.rows; p.vocab = m.cols; p.ld = m.ld; p.logits = m.p;
     p.lse = vector<float>(tensor(a[1], "saved.lse"), "saved.lse", at::kFloat, m.rows, dev);
@@ -202,7 +215,7 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor dx = given(a[9]) ? tensor(a[9], "dlogits") : empty({m.rows, m.cols}, x.scalar_type(), x.device());
     const Matrix d = matrix_like(dx, "dlogits", x);
     p.dlogits = d.p; p.ld_dlogits = d.ld;
-    p.stream = stream_of(a[10], dev);
+    p.stream = place.stream();
     if (const int st = gar_token_logprobs_backward(&p)) return status(st);
     return THPVariable_Wrap(dx);
     END_HANDLE_TH_ERRORS
@@ -213,11 +226,11 @@ PyObject* checkpoint_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {    // x
     need(n, 3);
     const Tensor& x = tensor(a[0], "x");
     const Matrix m = matrix(x, "x");
-    const c10::cuda::CUDAGuard guard(x.device());
+    const Place place(x.device(), a[2]);
     const int64_t group = integer(a[1]);
     const Held h = new_held(m.rows, m.cols, group, x);
     const gar_checkpoint_t s = saved(h.q, h.scales, "checkpoint", m.rows, m.cols, group, x.device());
-    if (const int st = gar_checkpoint_pack(m.dtype, m.p, m.rows, m.cols, m.ld, int(group), &s, stream_of(a[2], x.device()))) return status(st);
+    if (const int st = gar_checkpoint_pack(m.dtype, m.p, m.rows, m.cols, m.ld, int(group), &s, place.stream())) return status(st);
     return tuple_of({h.q, h.scales});
     END_HANDLE_TH_ERRORS
 }
@@ -228,13 +241,14 @@ PyObject* checkpoint_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {  // q
     const Tensor &q = tensor(a[0], "saved.q"), &scales = tensor(a[1], "saved.scales");
     const int64_t cols = integer(a[2]), group = integer(a[3]), code = integer(a[4]), rows = q.size(0);
     const at::ScalarType type = code == GAR_F32 ? at::kFloat : code == GAR_BF16 ? at::kBFloat16 : at::kHalf;
-    const c10::cuda::OptionalCUDAGuard guard(q.is_cuda() ? c10::make_optional(q.device()) : c10::nullopt);
+    TORCH_CHECK_TYPE(q.is_cuda(), "saved.q must be a CUDA tensor");
+    const Place place(q.device(), a[6]);
     const gar_checkpoint_t s = saved(q, scales, "saved", rows, cols, group, q.device());
     const Tensor out = given(a[5]) ? tensor(a[5], "out") : empty({rows, cols}, type, q.device());
     const Matrix m = matrix(out, "out");
     TORCH_CHECK_TYPE(m.dtype == code, "out must be of the checkpoint's type");
     TORCH_CHECK_VALUE(m.rows == rows && m.cols == cols && out.device() == q.device(), "out must be [", rows, ", ", cols, "] on ", q.device());
-    if (const int st = gar_checkpoint_unpack(int(code), &s, rows, cols, int(group), m.p, m.ld, stream_of(a[6], q.device()))) return status(st);
+    if (const int st = gar_checkpoint_unpack(int(code), &s, rows, cols, int(group), m.p, m.ld, place.stream())) return status(st);
     return THPVariable_Wrap(out);
     END_HANDLE_TH_ERRORS
 }
@@ -246,7 +260,7 @@ PyObject* activation_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor& x = tensor(a[1], "x");
     const Matrix m = matrix(x, "x");
     const at::Device dev = x.device();
-    const c10::cuda::CUDAGuard guard(dev);
+    const Place place(dev, a[7]);
     gar_activation_params_t p{};
     p.act = int(integer(a[0])); p.group = int(integer(a[3]));
     p.dtype = m.dtype; p.rows = m.rows; p.cols = m.cols; p.x = m.p; p.ldx = m.ld;
@@ -270,7 +284,7 @@ PyObject* activation_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         hy = new_held(m.rows, m.cols, p.group, x);
         p.y_saved = saved(hy.q, hy.scales, "out", m.rows, m.cols, p.group, dev);
     }
-    p.stream = stream_of(a[7], dev);
+    p.stream = place.stream();
     if (const int st = gar_activation_forward(&p)) return status(st);
     return tuple_of({y, hx.q, hx.scales, hu.q, hu.scales, hy.q, hy.scales});
     END_HANDLE_TH_ERRORS
@@ -283,7 +297,7 @@ PyObject* activation_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor& dy = tensor(a[1], "dy");
     const Matrix m = matrix(dy, "dy");
     const at::Device dev = dy.device();
-    const c10::cuda::CUDAGuard guard(dev);
+    const Place place(dev, a[10]);
     TORCH_CHECK_VALUE(integer(a[6]) == m.cols, "x does not hold [", m.rows, ", ", m.cols, "]");
     gar_activation_grad_params_t p{};
     p.act = int(integer(a[0])); p.group = int(integer(a[7]));
@@ -301,7 +315,7 @@ PyObject* activation_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     } else {
         TORCH_CHECK_VALUE(!given(a[9]), "dup needs up");
     }
-    p.stream = stream_of(a[10], dev);
+    p.stream = place.stream();
     if (const int st = gar_activation_backward(&p)) return status(st);
     return tuple_of({dx, dup});
     END_HANDLE_TH_ERRORS
@@ -340,7 +354,7 @@ PyObject* linear_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Device dev = dy.device();
     const int64_t cols = integer(a[3]), group = integer(a[4]), at_w = integer(a[6]), at_b = integer(a[7]);
     gar_weight_grad_params_t p = weight_grad_sizes(dy, cols, group);
-    const c10::cuda::CUDAGuard guard(dev);
+    const Place place(dev, a[10]);
     const Matrix g = matrix(grads, "grads");
     TORCH_CHECK_VALUE(grads.device() == dev, "grads must sit on ", dev);
     TORCH_CHECK_VALUE(g.rows == p.workers && at_w >= 0 && at_w + p.out_features * cols <= g.cols,
@@ -357,10 +371,10 @@ PyObject* linear_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (a[9] == Py_None) {
         // Every 256 outputs restore the activation once more.  Measured (8 workers, 2048 tokens, 4096 inputs):
         // with a workspace 292 us against 286 at 2048 outputs, 1007 against 1104 at 4 x 8192 tokens and 4096
-        // outputs; fp32 sums of more than 1024 tokens, whose chunks leave the tile's rounds less slack, 158
+        // outputs; fp32 sums of several chunks (768 tokens), which leave the tile's rounds less slack, 158
         // against 166 at 768 outputs; dy copied to aligned rows on the way 42 against 58 at 1023 outputs, 19
         // against 13 at 500.
-        const bool chunks = g.dtype == GAR_F32 && p.tokens > 1024;
+        const bool chunks = g.dtype == GAR_F32 && p.tokens > 768;
         const bool odd = reinterpret_cast<uintptr_t>(p.dy) % 16 != 0 || p.ld_dy % 8 != 0;
         if (p.out_features >= (chunks || odd ? 768 : 2048)) space = empty({int64_t(gar_weight_grad_workspace_bytes(&p))}, at::kByte, dev);
     } else if (a[9] == Py_True) space = empty({int64_t(gar_weight_grad_workspace_bytes(&p))}, at::kByte, dev);
@@ -370,7 +384,7 @@ PyObject* linear_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         p.workspace = space.data_ptr();
         p.workspace_bytes = size_t(space.numel()) * space.element_size();
     }
-    p.stream = stream_of(a[10], dev);
+    p.stream = place.stream();
     return status(gar_linear_weight_grad(&p));
     END_HANDLE_TH_ERRORS
 }

@@ -50,7 +50,7 @@ constexpr int WG_HALF = WG_N / 2;                     // columns a CTA restores
 //                against the products' 512)
 enum Mode { WG_PLAIN_DY = 0, WG_FUSED = 1, WG_RESTORED = 2, WG_PANEL = 3 };
 constexpr int WG_PANEL_STEPS = 8;                     // 512 tokens
-constexpr int WG_CHUNK = 16;                          // steps per accumulator of an fp32 result
+constexpr int WG_CHUNK = 12;                          // steps per accumulator of an fp32 result: 768 tokens
 template <int MODE> struct Plan {
     static constexpr int A_RING = MODE == WG_RESTORED ? 5 : 4;               // steps of dy in flight
     static constexpr int B_SLOTS = MODE == WG_PANEL ? WG_PANEL_STEPS : A_RING;    // restored tiles
@@ -924,9 +924,10 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     a.columns = a.nt + (p.bias_grads ? 1 : 0);
     if (int64_t(a.mt) * a.columns >= (int64_t(1) << 30) / a.workers) return cudaErrorInvalidConfiguration;
     const int64_t gs = p.grads_dtype == GAR_F32 ? 4 : 2;
-    // The tensor core truncates what it adds to an accumulator: the sum loses 1e-9 of itself per token (measured:
-    // 4.4e-6 at 4096 tokens, seven times what rounded additions lose there).  fp32 results are summed in chunks
-    // of 1024 tokens, joined by rounded additions: 1e-6 at any length.  16-bit results round off 2e-3.
+    // The tensor core truncates what it adds to an accumulator: the sum loses 1e-9 of itself per token, twice
+    // that where it grows steadily (measured: 4.4e-6 at 4096 random tokens, 5.6e-6 at 2048 positive ones; rounded
+    // additions lose a tenth).  fp32 results are summed in chunks, joined by rounded additions: 7e-7 and 1.5e-6
+    // at any length, at the price of one more pass over the tile in L2 per chunk.  16-bit results round off 2e-3.
     a.chunk = p.grads_dtype == GAR_F32 ? WG_CHUNK : 0x40000000;
     a.wide = reinterpret_cast<uintptr_t>(p.weight_grads) % 16 == 0 && (p.workers == 1 || p.ld_grads * gs % 16 == 0) &&
              p.in_features * gs % 16 == 0;

@@ -516,7 +516,7 @@ def test_weight_grad_lengths(pkg, out, inp):
     assert torch.equal(a[0], b[0]) and torch.all(a[1] == 0)
 
 
-@pytest.mark.parametrize("tokens", [40, 150, 257])
+@pytest.mark.parametrize("tokens", [40, 150, 257, 800])
 def test_weight_grad_lengths_over_many_tiles(pkg, tokens):
     """Several tiles per CTA pair, workers that end inside a step, on its edge, and empty ones among them."""
     n, out, inp = 12, 1100, 2100
@@ -538,6 +538,23 @@ def test_weight_grad_panels(pkg, dtype, grads_dtype, n, t, out, inp):
     g = check_weight_grad(pkg, dy, ck, grads_dtype)
     lengths = torch.full((n,), t, dtype=torch.int32, device=DEV)
     assert torch.equal(check_weight_grad(pkg, dy, ck, grads_dtype, lengths), g)
+
+
+@pytest.mark.parametrize("n,t,out,inp", [(2, 1100, 136, 264), (1, 2500, 40, 70), (3, 1025, 300, 520), (2, 2049, 33, 250)])
+@pytest.mark.parametrize("grads_dtype", ["f32", "f16"])
+def test_weight_grad_long_sums(pkg, n, t, out, inp, grads_dtype):
+    """Sums of more than 1024 tokens, which fp32 results join from chunks: stored and added by TMA or plainly, with
+    lengths that end in the first chunk, on its edge and in the last one.  All values positive: the sums
+    grow steadily, the case in which additions that truncate lose most.  The chunks' sums stay within 2e-6."""
+    dy, x = normal((n, t, out), "bf16", t).abs(), normal((n * t, inp), "bf16", inp).abs()
+    ck = pkg.gar_checkpoint_pack(x, 64)
+    g = check_weight_grad(pkg, dy, ck, grads_dtype)
+    lengths = torch.tensor([700, 1024, t][:n], dtype=torch.int32, device=DEV)
+    check_weight_grad(pkg, dy, ck, grads_dtype, lengths)
+    if grads_dtype == "f32":
+        dw, _, _, _ = weight_grad_64(dy, ck, pkg)
+        got = g[:, :out * inp].reshape(n, out, inp).double()
+        assert float((got - dw).norm()) <= 2e-6 * float(dw.norm())
 
 
 def test_weight_grad_workers_do_not_meet(pkg):
