@@ -181,16 +181,28 @@ __device__ __forceinline__ void tma_load_pair(unsigned dst, const CUtensorMap* m
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
+// L2 policy of data that is not touched again: the result (738 MB for 11 workers of 4096 x 4096) passes
+// through L2 without driving out the operands, which other tiles still read.
+__device__ __forceinline__ unsigned long long evict_first() {
+    unsigned long long p;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ unsigned long long evict_normal() {
+    unsigned long long p;
+    asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
 // a piece of the result from shared memory (what lies outside the matrix is not written)
-__device__ __forceinline__ void tma_store(const CUtensorMap* map, unsigned src, int x, int y, int z) {
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
-                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, unsigned src, int x, int y, int z, unsigned long long policy) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group.L2::cache_hint [%0, {%2, %3, %4}], [%1], %5;"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z), "l"(policy) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 // the same, added to what is there (fp32)
-__device__ __forceinline__ void tma_add(const CUtensorMap* map, unsigned src, int x, int y, int z) {
-    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
-                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+__device__ __forceinline__ void tma_add(const CUtensorMap* map, unsigned src, int x, int y, int z, unsigned long long policy) {
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group.L2::cache_hint [%0, {%2, %3, %4}], [%1], %5;"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z), "l"(policy) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 template <int LEFT> __device__ __forceinline__ void tma_store_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
@@ -691,6 +703,7 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     tc_fence_after();
                 }
                 if (s0 > 0 && lane == 0) tma_store_done();           // the chunk before is in memory
+                const unsigned long long policy = s0 + a.chunk >= t.steps ? evict_first() : evict_normal();
                 __syncwarp();
                 if (t.n == a.nt) {
                     float v[32];
@@ -742,8 +755,8 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                         if (a.wide) {
                             fence_async_smem();
                             __syncwarp();
-                            if (lane == 0 && s0 == 0) tma_store(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker);
-                            if (lane == 0 && s0 > 0) tma_add(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker);
+                            if (lane == 0 && s0 == 0) tma_store(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker, policy);
+                            if (lane == 0 && s0 > 0) tma_add(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker, policy);
                         } else {
                             __syncwarp();
                             for (int c = lane; c < min(COLS, cols - c0); c += 32) {
