@@ -52,15 +52,16 @@ enum Mode { WG_PLAIN_DY = 0, WG_FUSED = 1, WG_RESTORED = 2, WG_PANEL = 3 };
 constexpr int WG_PANEL_STEPS = 8;                     // 512 tokens
 constexpr int WG_CHUNK = 12;                          // steps per accumulator of an fp32 result: 768 tokens
 template <int MODE> struct Plan {
-    static constexpr int A_RING = MODE == WG_RESTORED ? 5 : 4;               // steps of dy in flight
+    static constexpr int A_RING = MODE == WG_RESTORED || MODE == WG_PANEL ? 5 : 4;       // steps of dy in flight
     static constexpr int B_SLOTS = MODE == WG_PANEL ? WG_PANEL_STEPS : A_RING;    // restored tiles
     // Groups of four restore warps take steps in turn.  A step takes a group about 1500 cycles from its slot
     // being free to the arrival (waits, reads, 220 instructions, fence), three times what the products take.
     // A slot of codes belongs to one group for good (Q_RING is a multiple of GROUPS): who waits for a
     // parity has to have followed the slot's rounds.
     static constexpr int GROUPS = MODE == WG_RESTORED ? 1 : MODE == WG_PANEL ? 2 : 3;
+    // (WG_PANEL's restore warps read codes where they lie: no time to save, and its shared memory is full)
     static constexpr int Q_RING = MODE == WG_RESTORED ? 1 : MODE == WG_PANEL ? 2 : 6;
-    static constexpr int Q_BYTES = MODE == WG_RESTORED ? 1024 : 64 * 128;
+    static constexpr int Q_BYTES = MODE == WG_RESTORED || MODE == WG_PANEL ? 16 : 64 * 128;
     static constexpr int OUT = MODE == WG_PANEL ? 1 : 2;                     // staged pieces of a store warp
     static constexpr int THREADS = 32 * (8 + 4 * GROUPS);
     static_assert(Q_RING % GROUPS == 0, "a slot of codes belongs to one group");
@@ -77,8 +78,8 @@ template <int MODE> struct __align__(1024) WGSmem {
     typedef Plan<MODE> P;
     uint8_t  a[P::A_RING][WG_A_BYTES];
     uint8_t  b[P::B_SLOTS][WG_B_BYTES];
-    uint8_t  q[P::Q_RING][P::Q_BYTES];
     float    out[4][P::OUT][32 * 32];                     // a store warp's pieces of the tile: 32 rows of 128 bytes
+    uint8_t  q[P::Q_RING][P::Q_BYTES];
     uint16_t ones[512];
     // the operand slots are read (WG_PANEL: dy's; x's are b_empty); the codes are there, are read; dy's slot is
     // the restore warps' to fill; the accumulators are complete
@@ -91,10 +92,11 @@ template <int MODE> struct __align__(1024) WGSmem {
 
 struct WGArgs {
     const void*    dy;
+    const int8_t*  q;
     const float*   scales;
     const int32_t* lengths;
     void *         dw, *db;
-    int64_t        tokens, out, in, ld_dy, ld_grads;
+    int64_t        tokens, out, in, ld_dy, ldq, ld_grads;
     int            workers, groups, group_shift;
     int            mt, nt;                // pair row tiles, column tiles (the bias tile, if any, is one more)
     int            columns;               // nt + 1 with a bias
@@ -262,13 +264,6 @@ template <int DEPTH> struct Ring {
 };
 
 // two codes' bytes of a word -> fp32 codes -> times the scale -> a pair of T
-// WG_PANEL: how often step s's slot of codes (slot s % Q_RING) was used before, `panels` panels of `steps`
-// steps having gone by.
-__device__ __forceinline__ unsigned panel_round(unsigned panels, int steps, int s) {
-    constexpr int RING = Plan<WG_PANEL>::Q_RING;
-    return panels * unsigned((steps - s % RING + RING - 1) / RING) + unsigned(s / RING);
-}
-
 template <typename T>
 __device__ __forceinline__ unsigned restore_pair(unsigned biased, unsigned sel0, unsigned sel1, f32x2 scale) {
     const f32x2 v = pack2(__uint_as_float(__byte_perm(biased, 0x4b000000u, sel0)), __uint_as_float(__byte_perm(biased, 0x4b000000u, sel1)));
@@ -458,26 +453,7 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
             }
         }
     } else if (warp == WG_CODES_WARP) {
-        if (MODE == WG_PANEL && lane == 0) {
-            unsigned panels = 0, last_parity[WG_Q_RING];         // of a slot's latest copy; 2: none
-#pragma unroll
-            for (int k = 0; k < WG_Q_RING; ++k) last_parity[k] = 2u;
-            for (unsigned i = walk.first; ok && i < walk.end; ++i) {
-                const Tile t = tile_at<MODE>(a, i);
-                if (t.n == a.nt || (i != walk.first && t.m != 0)) continue;
-                for (int s = 0; s < t.steps; ++s) {
-                    const unsigned slot = unsigned(s) % WG_Q_RING, parity = panel_round(panels, t.steps, s) & 1u;
-                    if (!kb_wait(kb_smem_u32(&sm.q_empty[slot]), parity ^ 1u, error)) { ok = false; break; }
-                    const unsigned bar = kb_smem_u32(&sm.q_full[slot]);
-                    kb_expect_tx(bar, WG_Q_BYTES);
-                    tma_load(kb_smem_u32(sm.q[slot]), &map_x, t.n * WG_N + int(rank) * WG_HALF, s * WG_K, t.worker, bar);
-                    last_parity[slot] = parity;
-                }
-                ++panels;
-            }
-            for (unsigned k = 0; !ok && k < WG_Q_RING && last_parity[k] < 2u; ++k)
-                kb_wait(kb_smem_u32(&sm.q_full[k]), last_parity[k], error, true, 1u << 10);
-        } else if (MODE != WG_RESTORED && lane == 0) {
+        if (MODE != WG_RESTORED && MODE != WG_PANEL && lane == 0) {
             for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
                 const Tile t = tile_at<MODE>(a, i);
                 if (t.n == a.nt) continue;
@@ -633,17 +609,26 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                 if (MODE == WG_PANEL) {
                     r.slot = unsigned(s);
                     r.parity = panels & 1u;
-                    rq.slot = unsigned(s) % WG_Q_RING;
-                    rq.parity = panel_round(panels, t.steps, s) & 1u;
                     free_slot = &sm.b_empty[s];
                 }
                 float scale[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) scale[k] = next[k];
                 if (s + WG_GROUPS < t.steps) fetch_scales(s + WG_GROUPS);
+                uint4 c[4];
+                if (MODE == WG_PANEL) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int token = s * WG_K + row + 8 * (k >> 1);
+                        const int64_t col = c0 + piece[k & 1] * 16;
+                        c[k] = make_uint4(0, 0, 0, 0);
+                        if (token < len && col < a.in)       // rows of codes are padded to 16
+                            c[k] = __ldg(reinterpret_cast<const uint4*>(a.q + (int64_t(t.worker) * a.tokens + token) * a.ldq + col));
+                    }
+                }
                 if (!__all_sync(0xffffffffu, ready)) {
                     if (!kb_wait_warp(kb_smem_u32(free_slot), r.parity ^ 1u, error)) { ok = false; break; }
-                    if (!bias && !kb_wait_warp(kb_smem_u32(&sm.q_full[rq.slot]), rq.parity, error)) { ok = false; break; }
+                    if (MODE != WG_PANEL && !bias && !kb_wait_warp(kb_smem_u32(&sm.q_full[rq.slot]), rq.parity, error)) { ok = false; break; }
                 }
                 if (MODE != WG_PANEL) {
                     // asked early, so that the answer is there when the next step of this group begins
@@ -655,9 +640,8 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                 if (!bias) {
                     const uint8_t* q = sm.q[rq.slot] + q_at;
                     uint8_t* b = sm.b[r.slot];
-                    uint4 c[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) c[k] = *reinterpret_cast<const uint4*>(q + (k >> 1) * 8 * WG_HALF + piece[k & 1] * 16);
+                    for (int k = 0; MODE != WG_PANEL && k < 4; ++k) c[k] = *reinterpret_cast<const uint4*>(q + (k >> 1) * 8 * WG_HALF + piece[k & 1] * 16);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const unsigned words[4] = {c[k].x ^ 0x80808080u, c[k].y ^ 0x80808080u, c[k].z ^ 0x80808080u, c[k].w ^ 0x80808080u};
@@ -679,7 +663,7 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                 __syncwarp();
                 if (lane == 0) {
                     arrive_at_leader(&sm.b_full[r.slot]);
-                    if (!bias) kb_arrive(&sm.q_empty[rq.slot]);
+                    if (MODE != WG_PANEL && !bias) kb_arrive(&sm.q_empty[rq.slot]);
                 }
             }
             g += t.steps;
@@ -920,7 +904,9 @@ bool panel_applies(const gar_weight_grad_params_t& p, int64_t ld_dy) {
 cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy, int sm_count) {
     WGArgs a{};
     a.dy = p.dy;
+    a.q = p.x_saved.q;
     a.scales = p.x_saved.scales;
+    a.ldq = p.x_saved.ldq;
     a.lengths = p.lengths;
     a.dw = p.weight_grads;
     a.db = p.bias_grads;
