@@ -173,18 +173,20 @@ typedef struct gar_weight_grad_params_t {
     void*            weight_grads;/* dev */
     void*            bias_grads;  /* dev; NULL: none */
     int64_t          ld_grads;    /* elements between workers; >= out_features * in_features when workers > 1 */
-    void*            workspace;   /* dev, 256-byte aligned, >= gar_weight_grad_workspace_bytes: x' is restored into it
-                                     once (and dy copied there if its rows do not start on 16 bytes), for layers wide
-                                     enough that restoring it per tile costs more.  NULL: no workspace, every tile
-                                     restores what it multiplies.  The results are the same */
+    void*            workspace;   /* dev, 256-byte aligned, >= gar_weight_grad_workspace_bytes; NULL: none.  With one, a
+                                     call with few output tiles and many tokens cuts the tokens into parts, whose fp32
+                                     sums are kept there and added in order; another restores x' into it once (and
+                                     copies dy there if its rows do not start on 16 bytes) instead of per tile */
     size_t           workspace_bytes;
     void*            stream;
 } gar_weight_grad_params_t;
 int gar_linear_weight_grad(const gar_weight_grad_params_t* params);
-/* Bytes of that workspace (host, pure; the sizes, dy's alignment and whether lengths are given are looked
- * at).  0 on invalid sizes and where none is used: up to 512 tokens, without lengths and with dy's rows on
- * 16 bytes, every CTA restores the columns it works on once by itself. */
+/* Bytes of that workspace (host, pure; the sizes, dy's alignment, and whether lengths and biases are given
+ * are looked at).  0 on invalid sizes and where none is used: up to 512 tokens, without lengths and with
+ * dy's rows on 16 bytes, every CTA restores the columns it works on once by itself. */
 size_t gar_weight_grad_workspace_bytes(const gar_weight_grad_params_t* params);
+/* 1 where the call is faster with a workspace than without (measured rule; grads_dtype is looked at too). */
+int gar_weight_grad_wants_workspace(const gar_weight_grad_params_t* params);
 
 #ifdef __cplusplus
 }

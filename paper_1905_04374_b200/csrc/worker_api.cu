@@ -189,11 +189,16 @@ int gar_checkpoint_unpack(int dtype, const gar_checkpoint_t* saved, int64_t rows
                                                              static_cast<cudaStream_t>(stream)));
 }
 
-size_t gar_weight_grad_workspace_bytes(const gar_weight_grad_params_t* p) {
+static bool sizes_ok(const gar_weight_grad_params_t* p) {
     const int64_t limit = int64_t(1) << 31;
-    if (!p || p->workers < 1 || p->workers > GAR_MAX_N || p->tokens < 0 || p->tokens >= limit / 2 / p->workers) return 0;
-    if (p->out_features < 1 || p->in_features < 1 || p->out_features >= limit || p->in_features >= limit) return 0;
-    return gar::worker::weight_grad_workspace_bytes(*p, p->ld_dy ? p->ld_dy : p->out_features);
+    if (!p || p->workers < 1 || p->workers > GAR_MAX_N || p->tokens < 0 || p->tokens >= limit / 2 / p->workers) return false;
+    return p->out_features >= 1 && p->in_features >= 1 && p->out_features < limit && p->in_features < limit;
+}
+size_t gar_weight_grad_workspace_bytes(const gar_weight_grad_params_t* p) {
+    return sizes_ok(p) ? gar::worker::weight_grad_workspace_bytes(*p, p->ld_dy ? p->ld_dy : p->out_features) : 0;
+}
+int gar_weight_grad_wants_workspace(const gar_weight_grad_params_t* p) {
+    return sizes_ok(p) && gar::worker::weight_grad_wants_workspace(*p, p->ld_dy ? p->ld_dy : p->out_features);
 }
 
 int gar_linear_weight_grad(const gar_weight_grad_params_t* p) {

@@ -336,11 +336,13 @@ gar_weight_grad_params_t weight_grad_sizes(const Tensor& dy, int64_t cols, int64
     return p;
 }
 
-PyObject* weight_grad_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {      // dy, cols, group, with lengths
+PyObject* weight_grad_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {      // dy, cols, group, with lengths, with a bias
     HANDLE_TH_ERRORS
-    need(n, 4);
+    need(n, 5);
     gar_weight_grad_params_t p = weight_grad_sizes(tensor(a[0], "dy"), integer(a[1]), integer(a[2]));
-    if (integer(a[3])) p.lengths = reinterpret_cast<const int32_t*>(16);      // only looked at for being there
+    // only looked at for being there
+    if (integer(a[3])) p.lengths = reinterpret_cast<const int32_t*>(16);
+    if (integer(a[4])) p.bias_grads = reinterpret_cast<void*>(16);
     return PyLong_FromSize_t(gar_weight_grad_workspace_bytes(&p));
     END_HANDLE_TH_ERRORS
 }
@@ -369,14 +371,7 @@ PyObject* linear_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.ld_grads = g.ld;
     Tensor space;
     if (a[9] == Py_None) {
-        // Every 256 outputs restore the activation once more.  Measured (8 workers, 2048 tokens, 4096 inputs):
-        // with a workspace 292 us against 286 at 2048 outputs, 1007 against 1104 at 4 x 8192 tokens and 4096
-        // outputs; fp32 sums of several chunks (768 tokens), which leave the tile's rounds less slack, 158
-        // against 166 at 768 outputs; dy copied to aligned rows on the way 42 against 58 at 1023 outputs, 19
-        // against 13 at 500.
-        const bool chunks = g.dtype == GAR_F32 && p.tokens > 768;
-        const bool odd = reinterpret_cast<uintptr_t>(p.dy) % 16 != 0 || p.ld_dy % 8 != 0;
-        if (p.out_features >= (chunks || odd ? 768 : 2048)) space = empty({int64_t(gar_weight_grad_workspace_bytes(&p))}, at::kByte, dev);
+        if (gar_weight_grad_wants_workspace(&p)) space = empty({int64_t(gar_weight_grad_workspace_bytes(&p))}, at::kByte, dev);
     } else if (a[9] == Py_True) space = empty({int64_t(gar_weight_grad_workspace_bytes(&p))}, at::kByte, dev);
     else if (a[9] != Py_False) space = tensor(a[9], "workspace");
     if (space.defined() && space.numel() > 0) {

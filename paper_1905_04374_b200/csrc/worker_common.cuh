@@ -124,6 +124,7 @@ cudaError_t launch_checkpoint_unpack(int dtype, const gar_checkpoint_t& saved, i
 // The checkpoint of a weight gradient restored in the type of dy, zeros for tokens past the workers' lengths.
 cudaError_t launch_checkpoint_restore_masked(const gar_weight_grad_params_t& p, void* x, int64_t ldx, cudaStream_t stream);
 size_t weight_grad_workspace_bytes(const gar_weight_grad_params_t& p, int64_t ld_dy);
+bool weight_grad_wants_workspace(const gar_weight_grad_params_t& p, int64_t ld_dy);
 cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy, int sm_count);
 
 }  // namespace worker

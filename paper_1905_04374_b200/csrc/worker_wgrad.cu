@@ -28,6 +28,7 @@
 // roles leave their loops once what they have in flight has landed, and the CTA's tiles become NaN.
 #include <cuda.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "gar_internal.cuh"
@@ -96,11 +97,12 @@ struct WGArgs {
     const float*   scales;
     const int32_t* lengths;
     void *         dw, *db;
-    int64_t        tokens, out, in, ld_dy, ldq, ld_grads;
+    int64_t        tokens, out, in, ld_dy, ldq, ld_grads, pitch;     // pitch: elements between the result's rows
     int            workers, groups, group_shift;
     int            mt, nt;                // pair row tiles, column tiles (the bias tile, if any, is one more)
     int            columns;               // nt + 1 with a bias
     int            chunk;                 // steps per accumulator
+    int            splits;                // parts a worker's tokens are cut into, each with a result of its own
     int            wide;                  // the result's rows start on 16 bytes: stored by TMA
 };
 
@@ -214,7 +216,9 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volat
 // ---- tiles --------------------------------------------------------------------------------------
 struct Tile {
     int     worker, m, n;        // n == nt: the bias
-    int     steps;               // of WG_K tokens
+    int     steps;               // of WG_K tokens,
+    int     first;               // from this one on
+    int     plane;               // the result's place among the workers (and splits)
     int64_t len;                 // the worker's tokens that count
 };
 __device__ __forceinline__ int64_t worker_len(const WGArgs& a, int w) {
@@ -232,8 +236,12 @@ __device__ __forceinline__ Tile tile_at(const WGArgs& a, unsigned index) {
         t.worker = int(worker);
         t.len = a.tokens;
         t.steps = int((t.len + WG_K - 1) / WG_K);
+        t.first = 0;
+        t.plane = t.worker;
         return t;
     }
+    const unsigned split = a.splits > 1 ? index % unsigned(a.splits) : 0u;
+    if (a.splits > 1) index /= unsigned(a.splits);
     const unsigned per = unsigned(a.mt) * unsigned(a.columns), worker = index / per, r = index - worker * per;
     const unsigned per_group = WG_GROUP_M * unsigned(a.columns), g = r / per_group, in_group = r - g * per_group;
     const unsigned rows = min(unsigned(WG_GROUP_M), unsigned(a.mt) - g * WG_GROUP_M);
@@ -242,9 +250,18 @@ __device__ __forceinline__ Tile tile_at(const WGArgs& a, unsigned index) {
     t.m = int(g * WG_GROUP_M + in_group - unsigned(t.n) * rows);
     t.len = worker_len(a, t.worker);
     t.steps = int((t.len + WG_K - 1) / WG_K);
+    t.first = 0;
+    t.plane = t.worker;
+    if (a.splits > 1) {
+        // equal parts of the steps a full worker has
+        const int part = (int((a.tokens + WG_K - 1) / WG_K) + a.splits - 1) / a.splits;
+        t.first = int(split) * part;
+        t.steps = max(0, min(part, t.steps - t.first));
+        t.plane = int(split) * a.workers + t.worker;
+    }
     return t;
 }
-__device__ __forceinline__ unsigned tile_count(const WGArgs& a) { return unsigned(a.workers) * unsigned(a.mt) * unsigned(a.columns); }
+__device__ __forceinline__ unsigned tile_count(const WGArgs& a) { return unsigned(a.workers) * unsigned(a.mt) * unsigned(a.columns) * unsigned(a.splits); }
 
 // The tiles of a pair: every pairs-th one, or (WG_PANEL) a run of neighbours.
 struct Walk {
@@ -424,7 +441,8 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     const Ring<WG_RING> r(g);
                     if (!kb_wait(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
                     // dy's part of a step that the restore warps load is missing; a bias tile has no x
-                    const bool copy_dy = !(a.lengths && int64_t(s + 1) * WG_K > t.len), copy_x = MODE == WG_RESTORED && t.n < a.nt;
+                    const int step = t.first + s;
+                    const bool copy_dy = !(a.lengths && int64_t(step + 1) * WG_K > t.len), copy_x = MODE == WG_RESTORED && t.n < a.nt;
                     const unsigned bytes = (copy_dy ? WG_A_BYTES : 0) + (copy_x ? WG_B_BYTES : 0);
                     if (MODE == WG_RESTORED && !copy_dy) kb_arrive(&sm.late[n_late++ % WG_RING]);
                     if (rank == 0) {
@@ -434,14 +452,14 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     const unsigned bar = leader_full + r.slot * 8;
                     if (copy_dy) {
                         const unsigned dst = kb_smem_u32(sm.a[r.slot]);
-                        tma_load_pair(dst, &map_dy, o0, s * WG_K, t.worker, bar);
-                        tma_load_pair(dst + WG_BLOCK, &map_dy, o0 + 64, s * WG_K, t.worker, bar);
+                        tma_load_pair(dst, &map_dy, o0, step * WG_K, t.worker, bar);
+                        tma_load_pair(dst + WG_BLOCK, &map_dy, o0 + 64, step * WG_K, t.worker, bar);
                     }
                     if (copy_x) {
                         const unsigned dst = kb_smem_u32(sm.b[r.slot]);
                         const int c0 = t.n * WG_N + int(rank) * WG_HALF;
-                        tma_load_pair(dst, &map_x, c0, s * WG_K, t.worker, bar);
-                        tma_load_pair(dst + WG_BLOCK, &map_x, c0 + 64, s * WG_K, t.worker, bar);
+                        tma_load_pair(dst, &map_x, c0, step * WG_K, t.worker, bar);
+                        tma_load_pair(dst + WG_BLOCK, &map_x, c0 + 64, step * WG_K, t.worker, bar);
                     }
                 }
             }
@@ -462,7 +480,7 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     if (!kb_wait(kb_smem_u32(&sm.q_empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
                     const unsigned bar = kb_smem_u32(&sm.q_full[r.slot]);
                     kb_expect_tx(bar, WG_Q_BYTES);
-                    tma_load(kb_smem_u32(sm.q[r.slot]), &map_x, t.n * WG_N + int(rank) * WG_HALF, s * WG_K, t.worker, bar);
+                    tma_load(kb_smem_u32(sm.q[r.slot]), &map_x, t.n * WG_N + int(rank) * WG_HALF, (t.first + s) * WG_K, t.worker, bar);
                 }
             }
             for (unsigned k = 0; !ok && k < WG_Q_RING && k < gq; ++k) {
@@ -592,8 +610,8 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
             }
             float next[4];
             auto fetch_scales = [&](int s) {
-                const int64_t at = int64_t(s) * WG_K * a.groups;
-                const int token = s * WG_K + row;
+                const int64_t at = int64_t(t.first + s) * WG_K * a.groups;
+                const int token = (t.first + s) * WG_K + row;
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     next[k] = inside[k & 1] && token + 8 * (k >> 1) < len ? __ldg(scale_at[k & 1] + at + 8 * (k >> 1) * a.groups) : 0.f;
@@ -657,8 +675,8 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     }
                 }
                 const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M;
-                if (!TMA_A) load_dy<false>(a, t, o0, s, sm.a[r.slot], w, lane);
-                else if (MODE != WG_PANEL && a.lengths && (s + 1) * WG_K > len) load_dy<true>(a, t, o0, s, sm.a[r.slot], w, lane);
+                if (!TMA_A) load_dy<false>(a, t, o0, t.first + s, sm.a[r.slot], w, lane);
+                else if (MODE != WG_PANEL && a.lengths && (t.first + s + 1) * WG_K > len) load_dy<true>(a, t, o0, t.first + s, sm.a[r.slot], w, lane);
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) {
@@ -694,11 +712,11 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     if (t.steps) tmem_ld32(src, v);
                     else v[0] = 0.f;
                     if (o0 + lane < a.out) {
-                        G* db = static_cast<G*>(a.db) + int64_t(t.worker) * a.ld_grads + o0 + lane;
+                        G* db = static_cast<G*>(a.db) + int64_t(t.plane) * a.ld_grads + o0 + lane;
                         *db = Elem<G>::narrow(s0 > 0 ? Elem<G>::widen(*db) + v[0] : v[0]);
                     }
                 } else {
-                    G* dw = static_cast<G*>(a.dw) + int64_t(t.worker) * a.ld_grads + o0 * a.in + int64_t(t.n) * WG_N;
+                    G* dw = static_cast<G*>(a.dw) + int64_t(t.plane) * a.ld_grads + o0 * a.pitch + int64_t(t.n) * WG_N;
                     const int rows = int(min(int64_t(32), a.out - o0));
                     const int64_t left = a.in - int64_t(t.n) * WG_N;
                     const int cols = left < WG_N ? int(left) : WG_N;
@@ -739,22 +757,22 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                         if (a.wide) {
                             fence_async_smem();
                             __syncwarp();
-                            if (lane == 0 && s0 == 0) tma_store(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker, policy);
-                            if (lane == 0 && s0 > 0) tma_add(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.worker, policy);
+                            if (lane == 0 && s0 == 0) tma_store(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.plane, policy);
+                            if (lane == 0 && s0 > 0) tma_add(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.plane, policy);
                         } else {
                             __syncwarp();
                             for (int c = lane; c < min(COLS, cols - c0); c += 32) {
                                 const int at = (c * int(sizeof(G)) >> 4), in = c * int(sizeof(G)) & 15;
                                 // eight rows at a time: what is there is asked for before anything is added
                                 for (int row = 0; row < rows; row += 8) {
-                                    G* p = dw + int64_t(row) * a.in + c0 + c;
+                                    G* p = dw + int64_t(row) * a.pitch + c0 + c;
                                     float old[8];
 #pragma unroll
-                                    for (int k = 0; k < 8; ++k) old[k] = s0 > 0 && row + k < rows ? Elem<G>::widen(p[int64_t(k) * a.in]) : 0.f;
+                                    for (int k = 0; k < 8; ++k) old[k] = s0 > 0 && row + k < rows ? Elem<G>::widen(p[int64_t(k) * a.pitch]) : 0.f;
 #pragma unroll
                                     for (int k = 0; k < 8; ++k) {
                                         const G v = *reinterpret_cast<const G*>(stage + (row + k) * 128 + ((at ^ ((row + k) & 7)) << 4) + in);
-                                        if (row + k < rows) p[int64_t(k) * a.in] = s0 > 0 ? Elem<G>::narrow(old[k] + Elem<G>::widen(v)) : v;
+                                        if (row + k < rows) p[int64_t(k) * a.pitch] = s0 > 0 ? Elem<G>::narrow(old[k] + Elem<G>::widen(v)) : v;
                                     }
                                 }
                             }
@@ -790,9 +808,9 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                 const int64_t o = int64_t(2 * t.m + int(rank)) * WG_M + e / WG_N, c = int64_t(t.n) * WG_N + e % WG_N;
                 if (o >= a.out) continue;
                 if (t.n == a.nt) {
-                    if (e % WG_N == 0) static_cast<G*>(a.db)[int64_t(t.worker) * a.ld_grads + o] = Elem<G>::narrow(CUDART_NAN_F);
+                    if (e % WG_N == 0) static_cast<G*>(a.db)[int64_t(t.plane) * a.ld_grads + o] = Elem<G>::narrow(CUDART_NAN_F);
                 } else if (c < a.in) {
-                    static_cast<G*>(a.dw)[int64_t(t.worker) * a.ld_grads + o * a.in + c] = Elem<G>::narrow(CUDART_NAN_F);
+                    static_cast<G*>(a.dw)[int64_t(t.plane) * a.ld_grads + o * a.pitch + c] = Elem<G>::narrow(CUDART_NAN_F);
                 }
             }
         }
@@ -811,6 +829,20 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const unsigned short* s
         for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? __ldg(p + j) : 0u;
         dst[i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
     }
+}
+
+// The parts of a cut worker (WGArgs.splits), added in order and rounded once: column c of row r of the
+// result, c == in: the bias.
+template <typename G>
+__global__ void __launch_bounds__(128) join_parts_kernel(const float* parts, int64_t plane, int64_t pitch, int splits, int workers, int64_t out,
+                                                         int64_t in, G* dw, G* db, int64_t ld) {
+    const int64_t c = int64_t(blockIdx.x) * 128 + threadIdx.x, row = blockIdx.y, w = row / out, o = row - w * out;
+    if (c > in || (c == in && !db)) return;
+    const float* p = parts + w * plane + (c < in ? o * pitch + c : out * pitch + o);
+    float sum = p[0];
+    for (int k = 1; k < splits; ++k) sum += p[int64_t(k) * workers * plane];
+    if (c < in) dw[w * ld + o * in + c] = Elem<G>::narrow(sum);
+    else db[w * ld + o] = Elem<G>::narrow(sum);
 }
 
 // ---- launch -------------------------------------------------------------------------------------
@@ -860,7 +892,7 @@ cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap
         if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
         if (dev < 64) allowed.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
     }
-    const int64_t tiles = int64_t(a.workers) * a.mt * a.columns;
+    const int64_t tiles = int64_t(a.workers) * a.mt * a.columns * a.splits;
     const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(unsigned(2 * (tiles < pairs ? tiles : pairs)));
@@ -899,6 +931,29 @@ bool panel_applies(const gar_weight_grad_params_t& p, int64_t ld_dy) {
     return rows_on_16(p.dy, ld_dy) && !p.lengths && p.tokens <= WG_PANEL_STEPS * WG_K && p.out_features > 2 * WG_M;
 }
 
+// With few output tiles and many tokens the tokens are cut, so that every pair of SMs has a part, of four
+// steps at least (a step takes a pair 0.6 to 2 us when no other tile hides its latencies, the join 4 us in
+// all).  One worker, 4000 tokens, 200 x 300: 50 -> 18 us; 2 x 4096 tokens, 513 x 250: 151 -> 29 us.
+constexpr int WG_PAIRS = 74;
+int splits_of(const gar_weight_grad_params_t& p) {
+    const int64_t mt = (p.out_features + 2 * WG_M - 1) / (2 * WG_M), columns = (p.in_features + WG_N - 1) / WG_N + (p.bias_grads ? 1 : 0);
+    if (mt > WG_PAIRS || columns > WG_PAIRS) return 1;
+    const int64_t tiles = p.workers * mt * columns, steps = (p.tokens + WG_K - 1) / WG_K;
+    const int64_t s = std::min<int64_t>(WG_PAIRS / tiles, steps / 4);
+    return s > 1 ? int(std::min<int64_t>(s, 16)) : 1;
+}
+int64_t round4(int64_t v) { return (v + 3) / 4 * 4; }
+// one part of one worker: weights with rows of whole 16 bytes, biases
+int64_t part_floats(const gar_weight_grad_params_t& p) { return p.out_features * round4(p.in_features) + round4(p.out_features); }
+
+template <typename G>
+cudaError_t join_parts(const WGArgs& a, const gar_weight_grad_params_t& p, cudaStream_t stream) {
+    const dim3 grid(unsigned((p.in_features + 1 + 127) / 128), unsigned(p.workers * p.out_features));
+    join_parts_kernel<G><<<grid, 128, 0, stream>>>(static_cast<const float*>(a.dw), a.ld_grads, a.pitch, a.splits, p.workers, p.out_features,
+                                                   p.in_features, static_cast<G*>(p.weight_grads), static_cast<G*>(p.bias_grads), p.ld_grads);
+    return cudaGetLastError();
+}
+
 }  // namespace
 
 cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy, int sm_count) {
@@ -922,21 +977,32 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     a.nt = int((p.in_features + WG_N - 1) / WG_N);
     a.columns = a.nt + (p.bias_grads ? 1 : 0);
     if (int64_t(a.mt) * a.columns >= (int64_t(1) << 30) / a.workers) return cudaErrorInvalidConfiguration;
-    const int64_t gs = p.grads_dtype == GAR_F32 ? 4 : 2;
+    a.pitch = p.in_features;
+    a.splits = p.workspace ? splits_of(p) : 1;
+    // parts are fp32 results in the workspace
+    int grads_dtype = p.grads_dtype;
+    if (a.splits > 1) {
+        grads_dtype = GAR_F32;
+        a.dw = p.workspace;
+        a.pitch = round4(p.in_features);
+        a.ld_grads = part_floats(p);
+        a.db = p.bias_grads ? static_cast<float*>(p.workspace) + p.out_features * a.pitch : nullptr;
+    }
+    const int64_t gs = grads_dtype == GAR_F32 ? 4 : 2;
     // The tensor core truncates what it adds to an accumulator: the sum loses 1e-9 of itself per token, twice
     // that where it grows steadily (measured: 4.4e-6 at 4096 random tokens, 5.6e-6 at 2048 positive ones; rounded
     // additions lose a tenth).  fp32 results are summed in chunks, joined by rounded additions: 7e-7 and 1.5e-6
     // at any length, at the price of one more pass over the tile in L2 per chunk.  16-bit results round off 2e-3.
-    a.chunk = p.grads_dtype == GAR_F32 ? WG_CHUNK : 0x40000000;
-    a.wide = reinterpret_cast<uintptr_t>(p.weight_grads) % 16 == 0 && (p.workers == 1 || p.ld_grads * gs % 16 == 0) &&
-             p.in_features * gs % 16 == 0;
+    a.chunk = grads_dtype == GAR_F32 ? WG_CHUNK : 0x40000000;
+    const int planes = p.workers * a.splits;
+    a.wide = reinterpret_cast<uintptr_t>(a.dw) % 16 == 0 && (planes == 1 || a.ld_grads * gs % 16 == 0) && a.pitch * gs % 16 == 0;
 
     const CUtensorMapDataType type = p.dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     CUtensorMap map_x, map_dy, map_dw;
     int mode = rows_on_16(p.dy, ld_dy) ? WG_FUSED : WG_PLAIN_DY;
     if (panel_applies(p, ld_dy)) mode = WG_PANEL;
-    if (mode != WG_PANEL && p.workspace && p.tokens > 0) {
+    if (a.splits == 1 && mode != WG_PANEL && p.workspace && p.tokens > 0) {
         // x restored once (and dy copied, if its rows do not start on 16 bytes), then products of plain copies
         mode = WG_RESTORED;
         const int64_t rows = p.tokens * p.workers, ldx = round8(p.in_features);
@@ -963,17 +1029,32 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     if (!a.wide) {
         map_dw = map_x;                           // not used
     } else {
-        const CUtensorMapDataType gt = p.grads_dtype == GAR_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                       : p.grads_dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-        const int64_t pitch = p.in_features * gs, plane = p.workers > 1 ? p.ld_grads * gs : pitch * p.out_features;
-        if (cudaError_t err = make_map(&map_dw, gt, p.weight_grads, p.in_features, p.out_features, p.workers, pitch, plane, int(128 / gs), 32,
+        const CUtensorMapDataType gt = grads_dtype == GAR_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                       : grads_dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+        const int64_t pitch = a.pitch * gs, plane = planes > 1 ? a.ld_grads * gs : pitch * p.out_features;
+        if (cudaError_t err = make_map(&map_dw, gt, a.dw, p.in_features, p.out_features, planes, pitch, plane, int(128 / gs), 32,
                                        CU_TENSOR_MAP_SWIZZLE_128B)) return err;
     }
-    return p.dtype == GAR_BF16 ? launch_by_mode<__nv_bfloat16>(mode, p.grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream)
-                               : launch_by_mode<__half>(mode, p.grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
+    const cudaError_t err = p.dtype == GAR_BF16 ? launch_by_mode<__nv_bfloat16>(mode, grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream)
+                                                : launch_by_mode<__half>(mode, grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
+    if (err != cudaSuccess || a.splits == 1) return err;
+    return p.grads_dtype == GAR_F32    ? join_parts<float>(a, p, stream)
+           : p.grads_dtype == GAR_BF16 ? join_parts<__nv_bfloat16>(a, p, stream) : join_parts<__half>(a, p, stream);
+}
+
+// Every 256 outputs restore the activation once more.  Measured (8 workers, 2048 tokens, 4096 inputs): with a
+// workspace 292 us against 286 at 2048 outputs, 1007 against 1104 at 4 x 8192 tokens and 4096 outputs; fp32 sums
+// of several chunks, which leave the tile's rounds less slack, 158 against 166 at 768 outputs; dy copied to
+// aligned rows on the way 42 against 58 at 1023 outputs, 19 against 13 at 500.
+bool weight_grad_wants_workspace(const gar_weight_grad_params_t& p, int64_t ld_dy) {
+    if (splits_of(p) > 1) return true;
+    if (panel_applies(p, ld_dy)) return false;
+    const bool chunks = p.grads_dtype == GAR_F32 && p.tokens > WG_CHUNK * WG_K;
+    return p.out_features >= (chunks || !rows_on_16(p.dy, ld_dy) ? 768 : 2048);
 }
 
 size_t weight_grad_workspace_bytes(const gar_weight_grad_params_t& p, int64_t ld_dy) {
+    if (splits_of(p) > 1) return gar::align256(size_t(splits_of(p)) * p.workers * size_t(part_floats(p)) * 4);
     if (panel_applies(p, ld_dy)) return 0;
     const int64_t rows = p.tokens * p.workers;
     size_t bytes = gar::align256(size_t(rows) * size_t(round8(p.in_features)) * 2);

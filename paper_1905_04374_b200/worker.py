@@ -84,6 +84,7 @@ def lib():
         L.gar_linear_weight_grad.argtypes = [C.POINTER(GarWeightGradParams)]
         L.gar_weight_grad_workspace_bytes.argtypes = [C.POINTER(GarWeightGradParams)]
         L.gar_weight_grad_workspace_bytes.restype = C.c_size_t
+        L.gar_weight_grad_wants_workspace.argtypes = [C.POINTER(GarWeightGradParams)]
         _typed = True
     return L
 
@@ -203,9 +204,9 @@ def gar_activation_backward(act: str, dy: torch.Tensor, x: Checkpoint, up: Optio
     return ActivationGrad(*r)
 
 
-def gar_weight_grad_workspace_bytes(dy: torch.Tensor, x: Checkpoint, lengths: Optional[torch.Tensor] = None) -> int:
+def gar_weight_grad_workspace_bytes(dy: torch.Tensor, x: Checkpoint, lengths: Optional[torch.Tensor] = None, bias: bool = False) -> int:
     """Bytes of the workspace gar_linear_weight_grad takes for these operands (0: it uses none)."""
-    return (_native or _load()).weight_grad_workspace_bytes(dy, x.cols, x.group, lengths is not None)
+    return (_native or _load()).weight_grad_workspace_bytes(dy, x.cols, x.group, lengths is not None, bias)
 
 
 def gar_linear_weight_grad(dy: torch.Tensor, x: Checkpoint, grads: Optional[torch.Tensor] = None, weight_offset: int = 0,

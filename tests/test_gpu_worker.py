@@ -462,19 +462,22 @@ def check_weight_grad(pkg, dy, ck, grads_dtype="f32", lengths=None, off=0, gap=0
     place = dict(weight_offset=off, bias_offset=off + weights + gap, lengths=lengths)
     r = pkg.gar_linear_weight_grad(dy, ck, grads, workspace=False, **place)
     assert r is grads
-    # with the activation restored beforehand: the same products in the same order, the same bits
-    space = torch.empty(pkg.gar_weight_grad_workspace_bytes(dy, ck, lengths), dtype=torch.uint8, device=DEV)
+    # with a workspace: the same products in the same order, the same bits, unless the tokens are cut into parts
+    space = torch.full((pkg.gar_weight_grad_workspace_bytes(dy, ck, lengths, True),), 255, dtype=torch.uint8, device=DEV)
     other = pkg.gar_linear_weight_grad(dy, ck, torch.full_like(grads, 7.0), workspace=space, **place)
-    assert torch.equal(other, grads)
+    cut = -(-out // 256) * (-(-ck.cols // 256) + 1) * n <= 37 and t > 7 * 64
+    if not cut:
+        assert torch.equal(other, grads)
     dw, db, sw, sb = weight_grad_64(dy, ck, pkg, lengths)
     unit = 2.0 ** -23 * max(t, 8)
-    got = grads[:, off:off + weights].reshape(n, out, ck.cols)
-    close(got, dw, unit * sw + HALF_ULP[grads_dtype] * dw.abs() + TINY[grads_dtype], "dW")
-    got = grads[:, off + weights + gap:off + weights + gap + out]
-    close(got, db, unit * sb + HALF_ULP[grads_dtype] * db.abs() + TINY[grads_dtype], "db")
-    # nothing else of the rows is touched
-    assert torch.all(grads[:, :off] == 7.0) and torch.all(grads[:, off + weights:off + weights + gap] == 7.0)
-    assert torch.all(grads[:, d - tail:] == 7.0) if tail else True
+    for block in (grads, other):
+        got = block[:, off:off + weights].reshape(n, out, ck.cols)
+        close(got, dw, unit * sw + HALF_ULP[grads_dtype] * dw.abs() + TINY[grads_dtype], "dW")
+        got = block[:, off + weights + gap:off + weights + gap + out]
+        close(got, db, unit * sb + HALF_ULP[grads_dtype] * db.abs() + TINY[grads_dtype], "db")
+        # nothing else of the rows is touched
+        assert torch.all(block[:, :off] == 7.0) and torch.all(block[:, off + weights:off + weights + gap] == 7.0)
+        assert torch.all(block[:, d - tail:] == 7.0) if tail else True
     return grads
 
 
@@ -555,6 +558,18 @@ def test_weight_grad_long_sums(pkg, n, t, out, inp, grads_dtype):
         dw, _, _, _ = weight_grad_64(dy, ck, pkg)
         got = g[:, :out * inp].reshape(n, out, inp).double()
         assert float((got - dw).norm()) <= 2e-6 * float(dw.norm())
+
+
+@pytest.mark.parametrize("grads_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,t,out,inp", [(1, 769, 24, 40), (1, 3000, 100, 77), (2, 4099, 300, 600), (5, 1500, 31, 250), (3, 12000, 64, 64)])
+def test_weight_grad_cut_tokens(pkg, grads_dtype, n, t, out, inp):
+    """Few output tiles, many tokens: parts of the tokens joined in order; lengths that leave parts empty."""
+    dy, ck = normal((n, t, out), "bf16", t), pkg.gar_checkpoint_pack(normal((n * t, inp), "bf16", inp), 64)
+    check_weight_grad(pkg, dy, ck, grads_dtype, None, 3, 1, 2)
+    lengths = torch.tensor([65, t // 2, 0, t, 1][:n], dtype=torch.int32, device=DEV)
+    check_weight_grad(pkg, dy, ck, grads_dtype, lengths)
+    a, b = (pkg.gar_linear_weight_grad(dy, ck) for _ in range(2))
+    assert torch.equal(a, b)
 
 
 def test_weight_grad_workers_do_not_meet(pkg):

@@ -24,10 +24,11 @@ def test_every_declared_symbol_is_exported(pkg):
     text = open(os.path.join(ROOT, "include", "gar_worker.h")).read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
     names = sorted(set(re.findall(r"\b(gar_[a-z_0-9]+)\s*\(", text)))
-    assert len(names) == 8
+    assert len(names) == 9
     for name in names:
         assert hasattr(pkg.lib(), name), f"{name} declared in gar_worker.h but not exported"
-        assert hasattr(pkg, name), f"{name} has no Python entry point"
+        # the question whether to bring a workspace is asked inside the binding
+        assert hasattr(pkg, name) or name == "gar_weight_grad_wants_workspace", f"{name} has no Python entry point"
 
 
 def test_struct_mirrors_match_the_header(pkg, tmp_path):
