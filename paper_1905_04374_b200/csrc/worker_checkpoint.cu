@@ -1,9 +1,13 @@
 // Activation checkpoints in 8 bits and the activation passes that write and read them
 // (gar_worker.h).  A thread owns eight consecutive columns of a row; the 4, 8 or 16 lanes that
 // share a scale are neighbours in a warp, so the group's maximum is a few shuffles away and every
-// value is read from memory once.  All of it is bound by memory: the arithmetic is arranged to stay
-// below the issue rate (rounding through the 1.5 * 2^23 constant instead of conversions, codes
-// packed by byte permutes).
+// value is read from memory once.  All of it should be bound by memory, and the arithmetic is
+// arranged to stay below the issue rate: rounding through the 1.5 * 2^23 constant instead of
+// conversions, codes packed by byte permutes, maxima of two inputs in one register, two tasks per
+// thread with all loads first.  Measured (bf16, group 128): gated SiLU 8192 x 8192 forward 96 us =
+// 5.6 TB/s and backward 80 us = 6.8 TB/s under the profiler (its output partly still in L2), 185 us
+// together; pack and unpack 8192 x 4096 41 us, of which the pack 25: 81 % of the issue slots, twice
+// the time of its bytes (profiles/worker_*.md).
 #include "worker_common.cuh"
 
 namespace gar {

@@ -444,9 +444,14 @@ __device__ __forceinline__ void add_tile(const uint4 (&raw)[LP_UNROLL], float ce
     }
 }
 
-// Bound by memory for 16-bit logits as long as the loop stays under the issue rate: per entry about one
-// exponential (of 16 a cycle and SM, 1.4 at the memory's rate) and five instructions.  The next tile's
-// loads are in flight while a tile is worked on.
+// Per entry one exponential (of 16 a cycle and SM; the memory's rate asks for 11.6 entries of 16 bits) and
+// five instructions.  The next turn's loads are in flight while a turn is worked on.  Measured: 4096 x
+// 131072 bf16 200 us without alternatives, 235 with 20 (1.07 GB: 5.4 and 4.6 TB/s, copy peak 6.5;
+// profiles/worker_logprobs_4096x131072.md: issue slots 67 % busy, exponential unit 60 %), fp32 170 us for
+// 2048 x 131072 (6.3 TB/s).  The alternatives cost the row's end: two barriers, a second read of some 40
+// tiles, 10 % more DRAM traffic; it hides behind the other rows of the SM, which is why a row gets a warp up
+// to 16384 entries (16384 x 8192 bf16: 55 us, by CTAs of eight warps 123) and four warps beyond while the
+// rows last (4096 x 32768, 20 alternatives: 76 us, by eight warps 99).  4 x 32768: 8.5 us, latency.
 template <typename T, int WARPS>
 __global__ void __launch_bounds__(cta_threads(WARPS), 1024 / cta_threads(WARPS)) logprobs_kernel(const ForwardArgs a, int parts) {
     constexpr int E = Elem<T>::PER16, THREADS = 32 * WARPS, TEAMS = cta_threads(WARPS) / THREADS;
@@ -770,7 +775,8 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_backward_small_kernel(con
 }
 
 // Longer rows: a team of WARPS warps takes LPB_SLOTS 16-byte slots per thread of a row at a time: a
-// CTA one such chunk, a warp (a row of its own) one after the other.
+// CTA one such chunk, a warp (a row of its own) one after the other.  Bound by memory: 4096 x 131072 bf16
+// 325 us = 6.6 TB/s, 2048 x 32000 43 us, 300 x 50001 fp32 (odd rows) 22.6 us = 5.3 TB/s.
 constexpr int LPB_SLOTS = 4;
 
 template <typename T, int WARPS>

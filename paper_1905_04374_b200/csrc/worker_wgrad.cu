@@ -8,22 +8,32 @@
 //
 // Pairs of CTAs (clusters of two, one CTA per SM) take tiles of 256 outputs x 256 inputs of one
 // worker, 64 tokens a step, with the paired instruction (cta_group::2): each CTA holds 128 of the
-// outputs of dy and restores 128 of the inputs, and its tensor memory gets its own 128 rows of the
-// tile.  One CTA alone (128 x 256, restoring all 256 columns) moves 128 KB through its shared memory
-// per step, 1024 cycles against the 512 of the products; the pair halves the operand reads and the
-// restored bytes per CTA: 80 KB.
-//   dy warp, codes warp   TMA.  dy: two 64-column boxes per step, 128-byte swizzle, straight into the
-//                  operand layout; codes: one box of 128 bytes.  The tensor maps are three-dimensional
-//                  (columns, tokens, workers): what lies past a worker's tokens arrives as zeros and
-//                  no other worker's rows are read.
-//   restore warps  three groups of four take steps in turn: codes -> 16-bit values (byte permute into
-//                  fp32, subtract, multiply by the row group's scale, one rounding) -> operand tile in
-//                  shared memory, same layout
-//   MMA warp       of the leading CTA, one lane: four 256 x 256 x 16 instructions per step
+// outputs of dy and 128 of the inputs of x', and its tensor memory gets its own 128 rows of the tile.
+// One CTA alone (128 x 256, restoring all 256 columns) moved 128 KB through its shared memory per step,
+// 1024 cycles against the 512 of the products; a CTA of the pair moves 80.
+//   dy warp        TMA: two 64-column boxes per step, 128-byte swizzle, straight into the operand
+//                  layout (and the same of x', where it was restored beforehand).  The tensor maps are
+//                  three-dimensional (columns, tokens, workers): what lies past a worker's tokens arrives
+//                  as zeros and no other worker's rows are read
+//   codes warp     TMA: one box of 128 bytes per step
+//   restore warps  groups of four take steps in turn: codes -> 16-bit values (byte permute into fp32,
+//                  subtract, multiply by the row group's scale, one rounding) -> operand tile in shared
+//                  memory, same layout
+//   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
 //   store warps    four: tensor memory -> shared memory -> TMA stores (plain coalesced ones where the
 //                  result's rows do not start on 16 bytes), while the next tile's products run into the
 //                  other half of tensor memory
 // The bias is one more column tile whose second operand is a block of ones.
+// Four ways for the operands to come (enum Mode below), and two for the tokens: a worker's tokens are cut
+// into parts, joined in order by a second kernel, where there are too few tiles for the SMs.
+//
+// What bounds it (B200, 1 kW cap; profiles/worker_weight_grad_*.md).  Long batches: power.  4 workers x 8192
+// tokens, 4096 x 4096: 1.00 to 1.05 ms = 1.05 to 1.1 PFLOP/s with the pass that restores x' (61 us of it),
+// 0.84 ms = 1.31 PFLOP/s for this kernel before the cap lowers the clock to 1.2 GHz; the library's bf16
+// product alone takes 0.79 to 0.87 ms.  Short batches: the rows of the block, 11 x 512 tokens: 0.26 ms
+// for 738 MB (0.11 ms at the rate of a fill), 11 x 128: 0.146 ms.  Small layers: latency, 7 x 100 tokens,
+// 500 x 800 with bias: 14 us, of which launch and set-up 4, dy's odd rows 3, the stores 4.
+//
 // Hand-offs are mbarriers; every wait is bounded: a wait that gives up raises an error flag, all
 // roles leave their loops once what they have in flight has landed, and the CTA's tiles become NaN.
 #include <cuda.h>
