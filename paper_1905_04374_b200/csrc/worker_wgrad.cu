@@ -27,12 +27,13 @@
 // Four ways for the operands to come (enum Mode below), and two for the tokens: a worker's tokens are cut
 // into parts, joined in order by a second kernel, where there are too few tiles for the SMs.
 //
-// What bounds it (B200, 1 kW cap; profiles/worker_weight_grad_*.md).  Long batches: power.  4 workers x 8192
+// What bounds it (B200, 1 kW cap).  Long batches: power.  4 workers x 8192
 // tokens, 4096 x 4096: 1.00 to 1.05 ms = 1.05 to 1.1 PFLOP/s with the pass that restores x' (61 us of it),
-// 0.84 ms = 1.31 PFLOP/s for this kernel before the cap lowers the clock to 1.2 GHz; the library's bf16
+// 0.84 ms = 1.31 PFLOP/s for this kernel alone before the cap lowers the clock to 1.2 GHz; the library's bf16
 // product alone takes 0.79 to 0.87 ms.  Short batches: the rows of the block, 11 x 512 tokens: 0.26 ms
-// for 738 MB (0.11 ms at the rate of a fill), 11 x 128: 0.146 ms.  Small layers: latency, 7 x 100 tokens,
-// 500 x 800 with bias: 14 us, of which launch and set-up 4, dy's odd rows 3, the stores 4.
+// for 738 MB of fp32 rows (0.11 ms at the copy's rate; bf16 rows take 58 us less, just the time of the
+// 369 MB they save, so the stores do not hide), 11 x 128: 0.146 ms.  Small layers: latency, 7 x 100
+// tokens, 500 x 800 with bias: 14 us.
 //
 // Hand-offs are mbarriers; every wait is bounded: a wait that gives up raises an error flag, all
 // roles leave their loops once what they have in flight has landed, and the CTA's tiles become NaN.
