@@ -903,6 +903,7 @@ cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap
         if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
         if (dev < 64) allowed.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
     }
+    if (MODE == WG_PANEL && a.splits != 1) return cudaErrorInvalidConfiguration;      // its tiles know no parts
     const int64_t tiles = int64_t(a.workers) * a.mt * a.columns * a.splits;
     const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
     cudaLaunchConfig_t cfg{};
@@ -945,8 +946,10 @@ bool panel_applies(const gar_weight_grad_params_t& p, int64_t ld_dy) {
 // With few output tiles and many tokens the tokens are cut, so that every pair of SMs has a part, of four
 // steps at least (a step takes a pair 0.6 to 2 us when no other tile hides its latencies, the join 4 us in
 // all).  One worker, 4000 tokens, 200 x 300: 50 -> 18 us; 2 x 4096 tokens, 513 x 250: 151 -> 29 us.
+// A panel's tokens stay whole (WG_PANEL's tiles know no parts).
 constexpr int WG_PAIRS = 74;
-int splits_of(const gar_weight_grad_params_t& p) {
+int splits_of(const gar_weight_grad_params_t& p, int64_t ld_dy) {
+    if (panel_applies(p, ld_dy)) return 1;
     const int64_t mt = (p.out_features + 2 * WG_M - 1) / (2 * WG_M), columns = (p.in_features + WG_N - 1) / WG_N + (p.bias_grads ? 1 : 0);
     if (mt > WG_PAIRS || columns > WG_PAIRS) return 1;
     const int64_t tiles = p.workers * mt * columns, steps = (p.tokens + WG_K - 1) / WG_K;
@@ -989,7 +992,7 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     a.columns = a.nt + (p.bias_grads ? 1 : 0);
     if (int64_t(a.mt) * a.columns >= (int64_t(1) << 30) / a.workers) return cudaErrorInvalidConfiguration;
     a.pitch = p.in_features;
-    a.splits = p.workspace ? splits_of(p) : 1;
+    a.splits = p.workspace ? splits_of(p, ld_dy) : 1;
     // parts are fp32 results in the workspace
     int grads_dtype = p.grads_dtype;
     if (a.splits > 1) {
@@ -1058,14 +1061,14 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
 // of several chunks, which leave the tile's rounds less slack, 158 against 166 at 768 outputs; dy copied to
 // aligned rows on the way 42 against 58 at 1023 outputs, 19 against 13 at 500.
 bool weight_grad_wants_workspace(const gar_weight_grad_params_t& p, int64_t ld_dy) {
-    if (splits_of(p) > 1) return true;
+    if (splits_of(p, ld_dy) > 1) return true;
     if (panel_applies(p, ld_dy)) return false;
     const bool chunks = p.grads_dtype == GAR_F32 && p.tokens > WG_CHUNK * WG_K;
     return p.out_features >= (chunks || !rows_on_16(p.dy, ld_dy) ? 768 : 2048);
 }
 
 size_t weight_grad_workspace_bytes(const gar_weight_grad_params_t& p, int64_t ld_dy) {
-    if (splits_of(p) > 1) return gar::align256(size_t(splits_of(p)) * p.workers * size_t(part_floats(p)) * 4);
+    if (splits_of(p, ld_dy) > 1) return gar::align256(size_t(splits_of(p, ld_dy)) * p.workers * size_t(part_floats(p)) * 4);
     if (panel_applies(p, ld_dy)) return 0;
     const int64_t rows = p.tokens * p.workers;
     size_t bytes = gar::align256(size_t(rows) * size_t(round8(p.in_features)) * 2);

@@ -572,6 +572,20 @@ def test_weight_grad_cut_tokens(pkg, grads_dtype, n, t, out, inp):
     assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("n,t,out,inp", [(5, 473, 616, 15), (4, 497, 424, 403), (1, 512, 520, 64), (2, 449, 264, 100), (1, 448, 1320, 34)])
+def test_weight_grad_few_tiles_of_a_panel(pkg, n, t, out, inp):
+    """Few output tiles at 449 to 512 tokens: enough steps to be cut, but panels are not; with a workspace that
+    is larger than asked for (of NaN bytes) and the one the call takes by itself, the same bits as without."""
+    dy, ck = normal((n, t, out), "f16", t), pkg.gar_checkpoint_pack(normal((n * t, inp), "f16", inp), 64)
+    grads = check_weight_grad(pkg, dy, ck, "f32", None, 7)
+    want = check_weight_grad(pkg, dy, ck)
+    assert torch.equal(grads[:, 7:7 + out * inp], want[:, :out * inp])
+    space = torch.full((1 << 22,), 255, dtype=torch.uint8, device=DEV)
+    for w in (None, space):
+        got = pkg.gar_linear_weight_grad(dy, ck, torch.full_like(want, 7.0), 0, out * inp, workspace=w)
+        assert torch.equal(got[:, :out * inp + out], want[:, :out * inp + out])
+
+
 def test_weight_grad_workers_do_not_meet(pkg):
     """A NaN of one worker (a Byzantine one, say) stays in its own row: the others' bits do not change."""
     n, t = 4, 70                                             # 70 tokens: every worker ends inside a tile

@@ -169,3 +169,18 @@ def test_weight_grad_refusals(pkg):
     refuses(pkg, "gar_linear_weight_grad", params, [dict(workspace=1 << 20, workspace_bytes=need)])
     refuses(pkg, "gar_linear_weight_grad", params, [
         dict(dtype=0), dict(workers=65, ld_grads=1 << 40), dict(out_features=1 << 31), dict(tokens=1 << 30)], UNSUPPORTED)
+
+
+@pytest.mark.parametrize("change,cut", [(dict(), False), (dict(tokens=512), False), (dict(tokens=513), True), (dict(lengths=1 << 21), True),
+                                        (dict(dy=(1 << 20) + 2), True), (dict(out_features=256), True)])
+def test_weight_grad_panels_are_not_cut(pkg, change, cut):
+    """Up to 512 tokens without lengths, more than 256 outputs, aligned dy: panels, whose tokens stay whole however
+    few the output tiles are; otherwise these few tiles are cut into parts, which need a workspace."""
+    p = pkg.GarWeightGradParams()
+    p.dtype, p.grads_dtype, p.group, p.workers, p.tokens, p.out_features, p.in_features = 1, 0, 64, 5, 473, 616, 15
+    p.dy, p.weight_grads, p.ld_grads, p.x_saved = 1 << 20, 1 << 28, 616 * 15, _saved(pkg, 1 << 23, 1 << 24, 16)
+    for name, value in change.items():
+        setattr(p, name, value)
+    L = pkg.worker.lib()
+    assert (L.gar_weight_grad_wants_workspace(C.byref(p)) != 0) == cut
+    assert (L.gar_weight_grad_workspace_bytes(C.byref(p)) > 0) == cut
