@@ -383,6 +383,32 @@ __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t 
     }
 }
 
+// An aligned 16-byte chunk of the result, stored or (fp32) added to what is there.
+template <typename G>
+__device__ __forceinline__ void store_chunk(char* dst, const uint4& v, bool add) {
+    if (sizeof(G) == 4 && add)
+        asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
+                     ::"l"(dst), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)), "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w)) : "memory");
+    else
+        *reinterpret_cast<uint4*>(dst) = v;
+}
+// The same for the elements of a chunk at `off` bytes of a row of `bytes` bytes that lie in the row.
+template <typename G>
+__device__ __forceinline__ void store_elements(char* dst, const uint4& v, int off, int bytes, bool add) {
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+    constexpr int SIZE = int(sizeof(G));
+#pragma unroll
+    for (int e = 0; e < 16 / SIZE; ++e) {
+        if (off + e * SIZE < 0 || off + e * SIZE >= bytes) continue;
+        if constexpr (SIZE == 4) {
+            float* p = reinterpret_cast<float*>(dst) + e;
+            *p = add ? *p + __uint_as_float(w[e]) : __uint_as_float(w[e]);
+        } else {
+            reinterpret_cast<unsigned short*>(dst)[e] = static_cast<unsigned short>(w[e / 2] >> 16 * (e & 1));
+        }
+    }
+}
+
 // map_x: the codes, or (WG_RESTORED) the restored activation.  Where dy comes by TMA the restore warps
 // still load a worker's last step if only some of its tokens count.
 template <typename T, typename G, int MODE>
@@ -731,9 +757,8 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     const int rows = int(min(int64_t(32), a.out - o0));
                     const int64_t left = a.in - int64_t(t.n) * WG_N;
                     const int cols = left < WG_N ? int(left) : WG_N;
-                    for (int c0 = 0; c0 < cols && rows > 0; c0 += COLS, ++n_piece) {
-                        // this lane's row of the piece, as G
-                        unsigned piece[32];
+                    // this lane's row of a piece, as G
+                    auto read_piece = [&](int c0, unsigned* piece) {
                         float v[32];
 #pragma unroll
                         for (int h = 0; h < COLS / 32; ++h) {
@@ -758,36 +783,86 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                                 }
                             }
                         }
-                        // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
-                        char* stage = reinterpret_cast<char*>(sm.out[quarter][n_piece % P::OUT]);
-                        if (lane == 0) tma_store_read<P::OUT - 1>();
-                        __syncwarp();
+                    };
+                    if (a.wide) {
+                        for (int c0 = 0; c0 < cols && rows > 0; c0 += COLS, ++n_piece) {
+                            unsigned piece[32];
+                            read_piece(c0, piece);
+                            // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
+                            char* stage = reinterpret_cast<char*>(sm.out[quarter][n_piece % P::OUT]);
+                            if (lane == 0) tma_store_read<P::OUT - 1>();
+                            __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(piece[4 * j], piece[4 * j + 1], piece[4 * j + 2], piece[4 * j + 3]);
-                        if (a.wide) {
+                            for (int j = 0; j < 8; ++j)
+                                *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(piece[4 * j], piece[4 * j + 1], piece[4 * j + 2], piece[4 * j + 3]);
                             fence_async_smem();
                             __syncwarp();
                             if (lane == 0 && s0 == 0) tma_store(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.plane, policy);
                             if (lane == 0 && s0 > 0) tma_add(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.plane, policy);
-                        } else {
+                        }
+                    } else if (rows > 0) {
+                        // Rows that start anywhere: each is moved up by what its start lies behind a multiple of 32
+                        // bytes, the words that move out of a piece are the next one's first, and what is written
+                        // are whole aligned 16-byte chunks but for the row's ends.
+                        const int bytes = cols * int(sizeof(G));
+                        const int64_t row_bytes = a.pitch * int64_t(sizeof(G));
+                        char* const first = reinterpret_cast<char*>(dw);
+                        const unsigned by = unsigned(reinterpret_cast<uintptr_t>(first + lane * row_bytes)) & 31u;
+                        char* stage = reinterpret_cast<char*>(sm.out[quarter][0]);
+                        unsigned carry[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) carry[j] = 0;
+                        for (int at = 0; at < bytes + 31; at += 128) {
+                            unsigned x[40];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[j] = carry[j];
+                            if (at < bytes) {
+                                read_piece(at / int(sizeof(G)), x + 8);
+                            } else {
+#pragma unroll
+                                for (int j = 8; j < 40; ++j) x[j] = 0;
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) carry[j] = x[32 + j];
+                            const unsigned skip = 7u - by / 4;
+#pragma unroll
+                            for (int j = 0; j < 36; ++j) x[j] = skip & 4 ? x[j + 4] : x[j];
+#pragma unroll
+                            for (int j = 0; j < 34; ++j) x[j] = skip & 2 ? x[j + 2] : x[j];
+#pragma unroll
+                            for (int j = 0; j < 33; ++j) x[j] = skip & 1 ? x[j + 1] : x[j];
+                            const unsigned bits = sizeof(G) == 2 && (by & 2) ? 16u : 32u;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) x[j] = __funnelshift_rc(x[j], x[j + 1], bits);
+                            __syncwarp();                          // the chunks before have been read
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
                             __syncwarp();
-                            for (int c = lane; c < min(COLS, cols - c0); c += 32) {
-                                const int at = (c * int(sizeof(G)) >> 4), in = c * int(sizeof(G)) & 15;
-                                // eight rows at a time: what is there is asked for before anything is added
-                                for (int row = 0; row < rows; row += 8) {
-                                    G* p = dw + int64_t(row) * a.pitch + c0 + c;
-                                    float old[8];
+                            const int j = lane % 8;
+                            const char* const from = stage + lane / 8 * 128;
+                            char* begin = first + lane / 8 * row_bytes;
+                            if (at > 0 && at + 128 <= bytes && rows == 32) {
+                                // no row of the piece ends in it
+                                uint4 v[8];
 #pragma unroll
-                                    for (int k = 0; k < 8; ++k) old[k] = s0 > 0 && row + k < rows ? Elem<G>::widen(p[int64_t(k) * a.pitch]) : 0.f;
+                                for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const uint4*>(from + k * 512 + ((j ^ ((4 * k + lane / 8) & 7)) << 4));
 #pragma unroll
-                                    for (int k = 0; k < 8; ++k) {
-                                        const G v = *reinterpret_cast<const G*>(stage + (row + k) * 128 + ((at ^ ((row + k) & 7)) << 4) + in);
-                                        if (row + k < rows) p[int64_t(k) * a.pitch] = s0 > 0 ? Elem<G>::narrow(old[k] + Elem<G>::widen(v)) : v;
+                                for (int k = 0; k < 8; ++k) {
+                                    store_chunk<G>(reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(begin) & ~uintptr_t(31)) + at + 16 * j, v[k], s0 > 0);
+                                    begin += 4 * row_bytes;
+                                }
+                            } else {
+                                for (int k = 0; k < 8; ++k) {
+                                    const int off = at + 16 * j - int(reinterpret_cast<uintptr_t>(begin) & 31u);
+                                    if (4 * k + lane / 8 < rows && off > -16 && off < bytes) {
+                                        const uint4 v = *reinterpret_cast<const uint4*>(from + k * 512 + ((j ^ ((4 * k + lane / 8) & 7)) << 4));
+                                        if (off >= 0 && off + 16 <= bytes) store_chunk<G>(begin + off, v, s0 > 0);
+                                        else store_elements<G>(begin + off, v, off, bytes, s0 > 0);
                                     }
+                                    begin += 4 * row_bytes;
                                 }
                             }
-                            __syncwarp();
                         }
                     }
                 }
