@@ -383,18 +383,26 @@ __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t 
     }
 }
 
+__device__ __forceinline__ void put_shared(unsigned at, const uint4& v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 get_shared(unsigned at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
 // An aligned 16-byte chunk of the result, stored or (fp32) added to what is there.
-template <typename G>
-__device__ __forceinline__ void store_chunk(char* dst, const uint4& v, bool add) {
-    if (sizeof(G) == 4 && add)
+template <typename G, bool ADD>
+__device__ __forceinline__ void store_chunk(char* dst, const uint4& v) {
+    if (ADD)
         asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
                      ::"l"(dst), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)), "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w)) : "memory");
     else
         *reinterpret_cast<uint4*>(dst) = v;
 }
 // The same for the elements of a chunk at `off` bytes of a row of `bytes` bytes that lie in the row.
-template <typename G>
-__device__ __forceinline__ void store_elements(char* dst, const uint4& v, int off, int bytes, bool add) {
+template <typename G, bool ADD>
+__device__ __forceinline__ void store_elements(char* dst, const uint4& v, int off, int bytes) {
     const unsigned w[4] = {v.x, v.y, v.z, v.w};
     constexpr int SIZE = int(sizeof(G));
 #pragma unroll
@@ -402,9 +410,105 @@ __device__ __forceinline__ void store_elements(char* dst, const uint4& v, int of
         if (off + e * SIZE < 0 || off + e * SIZE >= bytes) continue;
         if constexpr (SIZE == 4) {
             float* p = reinterpret_cast<float*>(dst) + e;
-            *p = add ? *p + __uint_as_float(w[e]) : __uint_as_float(w[e]);
+            *p = ADD ? *p + __uint_as_float(w[e]) : __uint_as_float(w[e]);
         } else {
             reinterpret_cast<unsigned short*>(dst)[e] = static_cast<unsigned short>(w[e / 2] >> 16 * (e & 1));
+        }
+    }
+}
+
+// This lane's row of a piece of the accumulators (128 bytes), as G.
+template <typename G>
+__device__ __forceinline__ void read_piece(unsigned src, bool filled, unsigned* piece) {
+    float v[32];
+#pragma unroll
+    for (int h = 0; h < 4 / int(sizeof(G)); ++h) {
+        if (filled) {
+            tmem_ld32(src + unsigned(32 * h), v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = 0.f;
+        }
+        if constexpr (sizeof(G) == 4) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) piece[j] = __float_as_uint(v[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+                const float f[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
+                const uint4 p = narrow16B(f, static_cast<const G*>(nullptr));
+                piece[16 * h + j / 2] = p.x;
+                piece[16 * h + j / 2 + 1] = p.y;
+                piece[16 * h + j / 2 + 2] = p.z;
+                piece[16 * h + j / 2 + 3] = p.w;
+            }
+        }
+    }
+}
+
+// The accumulator's rows of a warp (cols = `bytes` of G) to rows of the result that start anywhere, `row_bytes`
+// apart: each is moved up by what its start lies behind a multiple of 32 bytes, the words that move out of a piece
+// are the next one's first, and what is written are whole aligned 16-byte chunks but for the row's ends.  Not
+// inlined: its registers are no burden on the other paths.  Measured against single elements from the staging buffer
+// (odd row length): 11 x 512 tokens, 4096 x 4096, bf16 546 -> 281 us, 4 x 4096 tokens, 2048 x 2048, fp32 505 -> 297.
+template <typename G, bool ADD>
+__device__ __noinline__ void store_anywhere(unsigned src, bool filled, unsigned stage, char* first, int64_t row_bytes, int bytes, int rows) {
+    const int lane = threadIdx.x % 32;
+    const unsigned by = unsigned(reinterpret_cast<uintptr_t>(first + lane * row_bytes)) & 31u;
+    unsigned carry[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) carry[j] = 0;
+    for (int at = 0; at < bytes + 31; at += 128) {
+        unsigned x[40];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = carry[j];
+        if (at < bytes) {
+            read_piece<G>(src + unsigned(at / int(sizeof(G))), filled, x + 8);
+        } else {
+#pragma unroll
+            for (int j = 8; j < 40; ++j) x[j] = 0;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) carry[j] = x[32 + j];
+        const unsigned skip = 7u - by / 4;
+#pragma unroll
+        for (int j = 0; j < 36; ++j) x[j] = skip & 4 ? x[j + 4] : x[j];
+#pragma unroll
+        for (int j = 0; j < 34; ++j) x[j] = skip & 2 ? x[j + 2] : x[j];
+#pragma unroll
+        for (int j = 0; j < 33; ++j) x[j] = skip & 1 ? x[j + 1] : x[j];
+        const unsigned bits = sizeof(G) == 2 && (by & 2) ? 16u : 32u;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = __funnelshift_rc(x[j], x[j + 1], bits);
+        __syncwarp();                          // the chunks before have been read
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            put_shared(stage + lane * 128 + ((j ^ (lane & 7)) << 4), make_uint4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]));
+        __syncwarp();
+        const int j = lane % 8;
+        const unsigned from = stage + lane / 8 * 128;
+        char* begin = first + lane / 8 * row_bytes;
+        if (at > 0 && at + 128 <= bytes && rows == 32) {
+            // no row of the piece ends in it
+            uint4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = get_shared(from + k * 512 + ((j ^ ((4 * k + lane / 8) & 7)) << 4));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                store_chunk<G, ADD>(reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(begin) & ~uintptr_t(31)) + at + 16 * j, v[k]);
+                begin += 4 * row_bytes;
+            }
+        } else {
+#pragma unroll 2
+            for (int k = 0; k < 8; ++k) {
+                const int off = at + 16 * j - int(reinterpret_cast<uintptr_t>(begin) & 31u);
+                if (4 * k + lane / 8 < rows && off > -16 && off < bytes) {
+                    const uint4 v = get_shared(from + k * 512 + ((j ^ ((4 * k + lane / 8) & 7)) << 4));
+                    if (off >= 0 && off + 16 <= bytes) store_chunk<G, ADD>(begin + off, v);
+                    else store_elements<G, ADD>(begin + off, v, off, bytes);
+                }
+                begin += 4 * row_bytes;
+            }
         }
     }
 }
@@ -757,37 +861,10 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     const int rows = int(min(int64_t(32), a.out - o0));
                     const int64_t left = a.in - int64_t(t.n) * WG_N;
                     const int cols = left < WG_N ? int(left) : WG_N;
-                    // this lane's row of a piece, as G
-                    auto read_piece = [&](int c0, unsigned* piece) {
-                        float v[32];
-#pragma unroll
-                        for (int h = 0; h < COLS / 32; ++h) {
-                            if (t.steps) {
-                                tmem_ld32(src + unsigned(c0 + 32 * h), v);
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) v[j] = 0.f;
-                            }
-                            if constexpr (sizeof(G) == 4) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) piece[j] = __float_as_uint(v[j]);
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 32; j += 8) {
-                                    const float f[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
-                                    const uint4 p = narrow16B(f, static_cast<const G*>(nullptr));
-                                    piece[16 * h + j / 2] = p.x;
-                                    piece[16 * h + j / 2 + 1] = p.y;
-                                    piece[16 * h + j / 2 + 2] = p.z;
-                                    piece[16 * h + j / 2 + 3] = p.w;
-                                }
-                            }
-                        }
-                    };
                     if (a.wide) {
                         for (int c0 = 0; c0 < cols && rows > 0; c0 += COLS, ++n_piece) {
                             unsigned piece[32];
-                            read_piece(c0, piece);
+                            read_piece<G>(src + unsigned(c0), t.steps > 0, piece);
                             // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
                             char* stage = reinterpret_cast<char*>(sm.out[quarter][n_piece % P::OUT]);
                             if (lane == 0) tma_store_read<P::OUT - 1>();
@@ -801,69 +878,11 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                             if (lane == 0 && s0 > 0) tma_add(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.plane, policy);
                         }
                     } else if (rows > 0) {
-                        // Rows that start anywhere: each is moved up by what its start lies behind a multiple of 32
-                        // bytes, the words that move out of a piece are the next one's first, and what is written
-                        // are whole aligned 16-byte chunks but for the row's ends.
-                        const int bytes = cols * int(sizeof(G));
-                        const int64_t row_bytes = a.pitch * int64_t(sizeof(G));
+                        const unsigned stage = kb_smem_u32(sm.out[quarter][0]);
                         char* const first = reinterpret_cast<char*>(dw);
-                        const unsigned by = unsigned(reinterpret_cast<uintptr_t>(first + lane * row_bytes)) & 31u;
-                        char* stage = reinterpret_cast<char*>(sm.out[quarter][0]);
-                        unsigned carry[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) carry[j] = 0;
-                        for (int at = 0; at < bytes + 31; at += 128) {
-                            unsigned x[40];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) x[j] = carry[j];
-                            if (at < bytes) {
-                                read_piece(at / int(sizeof(G)), x + 8);
-                            } else {
-#pragma unroll
-                                for (int j = 8; j < 40; ++j) x[j] = 0;
-                            }
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) carry[j] = x[32 + j];
-                            const unsigned skip = 7u - by / 4;
-#pragma unroll
-                            for (int j = 0; j < 36; ++j) x[j] = skip & 4 ? x[j + 4] : x[j];
-#pragma unroll
-                            for (int j = 0; j < 34; ++j) x[j] = skip & 2 ? x[j + 2] : x[j];
-#pragma unroll
-                            for (int j = 0; j < 33; ++j) x[j] = skip & 1 ? x[j + 1] : x[j];
-                            const unsigned bits = sizeof(G) == 2 && (by & 2) ? 16u : 32u;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) x[j] = __funnelshift_rc(x[j], x[j + 1], bits);
-                            __syncwarp();                          // the chunks before have been read
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
-                            __syncwarp();
-                            const int j = lane % 8;
-                            const char* const from = stage + lane / 8 * 128;
-                            char* begin = first + lane / 8 * row_bytes;
-                            if (at > 0 && at + 128 <= bytes && rows == 32) {
-                                // no row of the piece ends in it
-                                uint4 v[8];
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const uint4*>(from + k * 512 + ((j ^ ((4 * k + lane / 8) & 7)) << 4));
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) {
-                                    store_chunk<G>(reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(begin) & ~uintptr_t(31)) + at + 16 * j, v[k], s0 > 0);
-                                    begin += 4 * row_bytes;
-                                }
-                            } else {
-                                for (int k = 0; k < 8; ++k) {
-                                    const int off = at + 16 * j - int(reinterpret_cast<uintptr_t>(begin) & 31u);
-                                    if (4 * k + lane / 8 < rows && off > -16 && off < bytes) {
-                                        const uint4 v = *reinterpret_cast<const uint4*>(from + k * 512 + ((j ^ ((4 * k + lane / 8) & 7)) << 4));
-                                        if (off >= 0 && off + 16 <= bytes) store_chunk<G>(begin + off, v, s0 > 0);
-                                        else store_elements<G>(begin + off, v, off, bytes, s0 > 0);
-                                    }
-                                    begin += 4 * row_bytes;
-                                }
-                            }
-                        }
+                        const int64_t row_bytes = a.pitch * int64_t(sizeof(G));
+                        if (sizeof(G) == 4 && s0 > 0) store_anywhere<G, sizeof(G) == 4>(src, true, stage, first, row_bytes, cols * int(sizeof(G)), rows);
+                        else store_anywhere<G, false>(src, t.steps > 0, stage, first, row_bytes, cols * int(sizeof(G)), rows);
                     }
                 }
                 if (t.steps) {
