@@ -20,8 +20,8 @@
 //                  subtract, multiply by the row group's scale, one rounding) -> operand tile in shared
 //                  memory, same layout
 //   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
-//   store warps    four: tensor memory -> shared memory -> TMA stores (plain coalesced ones where the
-//                  result's rows do not start on 16 bytes), while the next tile's products run into the
+//   store warps    four: tensor memory -> shared memory -> TMA stores (where the result's rows do not start on
+//                  16 bytes: shifted to aligned chunks and stored plainly, store_anywhere below), while the next tile's products run into the
 //                  other half of tensor memory
 // The bias is one more column tile whose second operand is a block of ones.
 // Four ways for the operands to come (enum Mode below), and two for the tokens: a worker's tokens are cut
@@ -409,8 +409,9 @@ __device__ __forceinline__ void store_elements(char* dst, const uint4& v, int of
     for (int e = 0; e < 16 / SIZE; ++e) {
         if (off + e * SIZE < 0 || off + e * SIZE >= bytes) continue;
         if constexpr (SIZE == 4) {
-            float* p = reinterpret_cast<float*>(dst) + e;
-            *p = ADD ? *p + __uint_as_float(w[e]) : __uint_as_float(w[e]);
+            // an addition does not wait for what it adds to; the element is this thread's, from chunk to chunk
+            if (ADD) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(dst + 4 * e), "f"(__uint_as_float(w[e])) : "memory");
+            else *reinterpret_cast<float*>(dst + 4 * e) = __uint_as_float(w[e]);
         } else {
             reinterpret_cast<unsigned short*>(dst)[e] = static_cast<unsigned short>(w[e / 2] >> 16 * (e & 1));
         }
@@ -449,8 +450,11 @@ __device__ __forceinline__ void read_piece(unsigned src, bool filled, unsigned* 
 // The accumulator's rows of a warp (cols = `bytes` of G) to rows of the result that start anywhere, `row_bytes`
 // apart: each is moved up by what its start lies behind a multiple of 32 bytes, the words that move out of a piece
 // are the next one's first, and what is written are whole aligned 16-byte chunks but for the row's ends.  Not
-// inlined: its registers are no burden on the other paths.  Measured against single elements from the staging buffer
-// (odd row length): 11 x 512 tokens, 4096 x 4096, bf16 546 -> 281 us, 4 x 4096 tokens, 2048 x 2048, fp32 505 -> 297.
+// inlined: its registers are no burden on the other paths.  Bound by the warp's own instructions, 1600 cycles a piece.
+// Measured against single elements from the staging buffer (odd row length): 11 x 512 tokens, 4096 x 4096: fp32 414 ->
+// 343 us (TMA stores, where rows start on 16 bytes: 261), bf16 546 -> 293 (208); 4 x 4096, 2048 x 2048, fp32 505 -> 212
+// (190); 11 x 128, 2048 x 2048, fp32 107 -> 74 (42).  A row's ends by the row's lane, or by eight lanes per row in a loop
+// of their own, were slower where nothing is added (90 and 99 us for the last).
 template <typename G, bool ADD>
 __device__ __noinline__ void store_anywhere(unsigned src, bool filled, unsigned stage, char* first, int64_t row_bytes, int bytes, int rows) {
     const int lane = threadIdx.x % 32;
