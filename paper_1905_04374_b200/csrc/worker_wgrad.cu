@@ -21,8 +21,8 @@
 //                  memory, same layout
 //   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
 //   store warps    four: tensor memory -> shared memory -> TMA stores (where the result's rows do not start on
-//                  16 bytes: shifted to aligned chunks and stored plainly, store_anywhere below), while the next tile's products run into the
-//                  other half of tensor memory
+//                  16 bytes: shifted to aligned chunks and stored plainly, store_anywhere below), while the
+//                  next tile's products run into the other half of tensor memory
 // The bias is one more column tile whose second operand is a block of ones.
 // Four ways for the operands to come (enum Mode below), and two for the tokens: a worker's tokens are cut
 // into parts, joined in order by a second kernel, where there are too few tiles for the SMs.
