@@ -10,6 +10,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+
 #include "gar_worker.h"
 
 namespace {
@@ -66,6 +68,14 @@ struct Matrix {
     int64_t rows = 0, cols = 0, ld = 0;
     int     dtype = 0;
 };
+// The distance of a matrix's rows.  Rows that share memory are refused: an expanded tensor's stride of 0 means "the
+// number of columns" to the library, which would then read, or write, rows that the tensor does not hold.
+int64_t row_stride(int64_t rows, int64_t cols, int64_t stride, const char* name) {
+    if (rows <= 1) return cols;
+    TORCH_CHECK_VALUE(stride >= std::max<int64_t>(cols, 1), name, " has rows that share memory (row stride ", stride, ", ", cols,
+                      " columns): make it contiguous");
+    return stride;
+}
 Matrix matrix(const Tensor& t, const char* name) {
     Matrix m;
     m.dtype = dtype_code(t, name);
@@ -73,7 +83,7 @@ Matrix matrix(const Tensor& t, const char* name) {
     m.p = pointer(t);
     m.rows = t.size(0);
     m.cols = t.size(1);
-    m.ld = m.rows > 1 ? t.stride(0) : m.cols;
+    m.ld = row_stride(m.rows, m.cols, t.stride(0), name);
     return m;
 }
 // a matrix of the same type, shape and device as another
@@ -146,7 +156,7 @@ gar_checkpoint_t saved(const Tensor& q, const Tensor& scales, const char* name, 
     TORCH_CHECK_TYPE(q.is_cuda() && q.device() == dev && q.scalar_type() == at::kChar && q.stride(1) == 1, name,
                      ".q must be an int8 tensor with unit column stride on ", dev);
     return {pointer<int8_t>(q), vector<float>(scales, name, at::kFloat, rows * ((cols + group - 1) / group), dev),
-            rows > 1 ? q.stride(0) : (q.size(1) + 15) / 16 * 16};
+            rows > 1 ? row_stride(rows, cols, q.stride(0), name) : (q.size(1) + 15) / 16 * 16};
 }
 
 // ---- entry points ---------------------------------------------------------------------------------
@@ -328,7 +338,7 @@ gar_weight_grad_params_t weight_grad_sizes(const Tensor& dy, int64_t cols, int64
     TORCH_CHECK_VALUE(dy.dim() == 3 && (dy.size(2) <= 1 || dy.stride(2) == 1), "dy must be [workers, tokens, out] with unit column stride");
     const int64_t workers = dy.size(0), tokens = dy.size(1), out = dy.size(2);
     TORCH_CHECK_VALUE(workers >= 1 && workers <= GAR_MAX_N, "dy must have 1 to ", GAR_MAX_N, " workers");
-    p.ld_dy = tokens > 1 ? dy.stride(1) : workers > 1 ? dy.stride(0) : out;
+    p.ld_dy = row_stride(workers * tokens, out, tokens > 1 ? dy.stride(1) : dy.stride(0), "dy");
     TORCH_CHECK_VALUE(workers == 1 || tokens <= 1 || dy.stride(0) == tokens * p.ld_dy, "dy: the workers' tokens must be evenly spaced rows");
     p.group = int(group); p.workers = int(workers);
     p.tokens = tokens; p.out_features = out; p.in_features = cols;

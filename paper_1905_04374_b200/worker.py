@@ -1,7 +1,8 @@
 """Binding of the worker-side operators (include/gar_worker.h): argument marshalling only.
 
 Every function has the name of its C entry point.  Matrices are 2-D CUDA tensors with unit column
-stride (any row stride); outputs are allocated, unless given, on the stream the call runs on.  The marshalling
+stride and any row stride that keeps the rows apart (an expanded tensor, whose rows share memory, is
+refused: make it contiguous); outputs are allocated, unless given, on the stream the call runs on.  The marshalling
 itself is compiled (csrc/worker_binding.cpp); the ctypes mirrors of the parameter blocks are for
 callers of the C ABI.  Nothing is computed here and there is no fallback.
 """
