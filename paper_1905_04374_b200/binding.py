@@ -186,11 +186,14 @@ def gar_workspace_bytes(rule, n: int, f: int, d: int) -> int:
 
 
 def _rows(grads: torch.Tensor):
-    """(n, d, ld) of a 2-D tensor whose rows are contiguous."""
+    """(n, d, ld) of a 2-D tensor whose rows are contiguous and apart.  An expanded tensor's row stride of 0 would
+    mean "d" to the library, which then reads rows that the tensor does not hold."""
     if grads.dim() != 2 or grads.stride(1) != 1:
         raise ValueError("grads must be 2-D with unit column stride")
     n, d = grads.shape
     ld = grads.stride(0) if n > 1 else d
+    if ld < d:
+        raise ValueError("grads has rows that share memory: make it contiguous")
     return n, d, ld
 
 
