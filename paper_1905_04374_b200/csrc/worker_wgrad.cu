@@ -22,7 +22,8 @@
 //   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
 //   store warps    four: tensor memory -> shared memory -> TMA stores (where the result's rows do not start on
 //                  16 bytes: shifted to aligned chunks and stored plainly, store_anywhere below), while the
-//                  next tile's products run into the other half of tensor memory
+//                  next tile's products run into the other half of tensor memory; where a tile has many tokens,
+//                  first the sum of its chunks there (Chunk, Halves below)
 // The bias is one more column tile whose second operand is a block of ones.
 // Four ways for the operands to come (enum Mode below), and two for the tokens: a worker's tokens are cut
 // into parts, joined in order by a second kernel, where there are too few tiles for the SMs.
@@ -62,7 +63,13 @@ constexpr int WG_HALF = WG_N / 2;                     // columns a CTA restores
 //                against the products' 512)
 enum Mode { WG_PLAIN_DY = 0, WG_FUSED = 1, WG_RESTORED = 2, WG_PANEL = 3 };
 constexpr int WG_PANEL_STEPS = 8;                     // 512 tokens
-constexpr int WG_CHUNK = 12;                          // steps per accumulator of an fp32 result: 768 tokens
+// Steps per accumulator.  The tensor core truncates what it adds to an accumulator: the sum loses 1e-9 of itself per
+// token, up to 2.8e-9 where it grows steadily (measured: 4.4e-6 at 4096 random tokens, 5.6e-6 at 2048 positive ones;
+// rounded additions lose a tenth).  Sums are therefore taken in chunks, joined by rounded additions in tensor memory, so
+// that the loss has a bound however many tokens there are: 768 tokens for fp32 results (7e-7, growing sums 1.5e-6), 2048
+// for 16-bit ones (2e-6 and 5.6e-6, a fortieth of binary16's rounding).  A join holds the products up for 2000 cycles:
+// 16-bit results at 768 tokens a chunk took 3 % longer with x restored beforehand and 10 to 13 % without.
+template <typename G> struct Chunk { static constexpr int STEPS = sizeof(G) == 4 ? 12 : 32; };
 template <int MODE> struct Plan {
     static constexpr int A_RING = MODE == WG_RESTORED || MODE == WG_PANEL ? 5 : 4;       // steps of dy in flight
     static constexpr int B_SLOTS = MODE == WG_PANEL ? WG_PANEL_STEPS : A_RING;    // restored tiles
@@ -112,7 +119,6 @@ struct WGArgs {
     int            workers, groups, group_shift;
     int            mt, nt;                // pair row tiles, column tiles (the bias tile, if any, is one more)
     int            columns;               // nt + 1 with a bias
-    int            chunk;                 // steps per accumulator
     int            splits;                // parts a worker's tokens are cut into, each with a result of its own
     int            wide;                  // the result's rows start on 16 bytes: stored by TMA
 };
@@ -186,6 +192,47 @@ __device__ __forceinline__ void tmem_ld32(unsigned taddr, float (&v)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
+// this thread's lane of tensor memory: 16 columns of either accumulator, there once the loads are waited for
+__device__ __forceinline__ void load_columns(unsigned sum, unsigned part, float (&a)[16], float (&b)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=f"(a[0]), "=f"(a[1]), "=f"(a[2]), "=f"(a[3]), "=f"(a[4]), "=f"(a[5]), "=f"(a[6]), "=f"(a[7]), "=f"(a[8]), "=f"(a[9]),
+                   "=f"(a[10]), "=f"(a[11]), "=f"(a[12]), "=f"(a[13]), "=f"(a[14]), "=f"(a[15])
+                 : "r"(sum) : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=f"(b[0]), "=f"(b[1]), "=f"(b[2]), "=f"(b[3]), "=f"(b[4]), "=f"(b[5]), "=f"(b[6]), "=f"(b[7]), "=f"(b[8]), "=f"(b[9]),
+                   "=f"(b[10]), "=f"(b[11]), "=f"(b[12]), "=f"(b[13]), "=f"(b[14]), "=f"(b[15])
+                 : "r"(part) : "memory");
+}
+__device__ __forceinline__ void loads_done(float (&a)[16], float (&b)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(a[0]), "+f"(a[1]), "+f"(a[2]), "+f"(a[3]), "+f"(a[4]), "+f"(a[5]), "+f"(a[6]), "+f"(a[7]), "+f"(a[8]), "+f"(a[9]),
+                   "+f"(a[10]), "+f"(a[11]), "+f"(a[12]), "+f"(a[13]), "+f"(a[14]), "+f"(a[15]), "+f"(b[0]), "+f"(b[1]), "+f"(b[2]),
+                   "+f"(b[3]), "+f"(b[4]), "+f"(b[5]), "+f"(b[6]), "+f"(b[7]), "+f"(b[8]), "+f"(b[9]), "+f"(b[10]), "+f"(b[11]),
+                   "+f"(b[12]), "+f"(b[13]), "+f"(b[14]), "+f"(b[15]) :: "memory");
+}
+__device__ __forceinline__ void store_columns(unsigned at, const float (&a)[16], const float (&b)[16]) {
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __fadd_rn(a[i], b[i]);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+                 ::"f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
+                   "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "r"(at) : "memory");
+}
+// `cols` columns of `part` added to those of `sum`, rounded to nearest; the next columns' loads are in flight while
+// some are added.  Not inlined: its registers are no burden on the other paths.
+__device__ __noinline__ void add_accumulator(unsigned sum, unsigned part, int cols) {
+    float a0[16], b0[16], a1[16], b1[16];
+    load_columns(sum, part, a0, b0);
+    for (int c = 0; c < cols; c += 32) {
+        loads_done(a0, b0);
+        load_columns(sum + unsigned(c + 16), part + unsigned(c + 16), a1, b1);
+        store_columns(sum + unsigned(c), a0, b0);
+        loads_done(a1, b1);
+        if (c + 32 < cols) load_columns(sum + unsigned(c + 32), part + unsigned(c + 32), a0, b0);
+        store_columns(sum + unsigned(c + 16), a1, b1);
+    }
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
@@ -203,20 +250,9 @@ __device__ __forceinline__ unsigned long long evict_first() {
     asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
-__device__ __forceinline__ unsigned long long evict_normal() {
-    unsigned long long p;
-    asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
-    return p;
-}
 // a piece of the result from shared memory (what lies outside the matrix is not written)
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, unsigned src, int x, int y, int z, unsigned long long policy) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group.L2::cache_hint [%0, {%2, %3, %4}], [%1], %5;"
-                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z), "l"(policy) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-// the same, added to what is there (fp32)
-__device__ __forceinline__ void tma_add(const CUtensorMap* map, unsigned src, int x, int y, int z, unsigned long long policy) {
-    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group.L2::cache_hint [%0, {%2, %3, %4}], [%1], %5;"
                  ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z), "l"(policy) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
@@ -289,6 +325,20 @@ __device__ __forceinline__ Walk walk_of(const WGArgs& a, unsigned pair, unsigned
 template <int DEPTH> struct Ring {
     unsigned slot, parity;
     __device__ __forceinline__ explicit Ring(unsigned number) : slot(number % DEPTH), parity((number / DEPTH) & 1u) {}
+};
+
+// The two halves of tensor memory as accumulators.  A tile's first chunk of tokens is summed in the half `sum`, where
+// the store warps keep the tile's sum; its other chunks go through the other half, one after the other.  The next
+// tile's half is the other one: free once the last chunk has been added, while this tile's is still being stored.
+// Every use of a half is a round of its two barriers (acc_full, acc_empty).
+struct Halves {
+    unsigned bits = 0;                                    // 0, 1: the parity of half 0, 1; 2: the tile's half; 3: the current one
+    __device__ __forceinline__ unsigned sum() const { return (bits >> 2) & 1u; }
+    __device__ __forceinline__ unsigned half() const { return bits >> 3; }
+    __device__ __forceinline__ unsigned parity() const { return (bits >> half()) & 1u; }
+    __device__ __forceinline__ void used() { bits ^= 1u << half(); }
+    __device__ __forceinline__ void other() { bits = (bits & 7u) | (((bits & 4u) ^ 4u) << 1); }
+    __device__ __forceinline__ void next_tile() { bits = ((bits ^ 4u) & 7u) | (((bits & 4u) ^ 4u) << 1); }
 };
 
 // two codes' bytes of a word -> fp32 codes -> times the scale -> a pair of T
@@ -391,30 +441,16 @@ __device__ __forceinline__ uint4 get_shared(unsigned at) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
     return v;
 }
-// An aligned 16-byte chunk of the result, stored or (fp32) added to what is there.
-template <typename G, bool ADD>
-__device__ __forceinline__ void store_chunk(char* dst, const uint4& v) {
-    if (ADD)
-        asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
-                     ::"l"(dst), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)), "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w)) : "memory");
-    else
-        *reinterpret_cast<uint4*>(dst) = v;
-}
-// The same for the elements of a chunk at `off` bytes of a row of `bytes` bytes that lie in the row.
-template <typename G, bool ADD>
+// The elements of a chunk at `off` bytes of a row of `bytes` bytes that lie in the row.
+template <typename G>
 __device__ __forceinline__ void store_elements(char* dst, const uint4& v, int off, int bytes) {
     const unsigned w[4] = {v.x, v.y, v.z, v.w};
     constexpr int SIZE = int(sizeof(G));
 #pragma unroll
     for (int e = 0; e < 16 / SIZE; ++e) {
         if (off + e * SIZE < 0 || off + e * SIZE >= bytes) continue;
-        if constexpr (SIZE == 4) {
-            // an addition does not wait for what it adds to; the element is this thread's, from chunk to chunk
-            if (ADD) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(dst + 4 * e), "f"(__uint_as_float(w[e])) : "memory");
-            else *reinterpret_cast<float*>(dst + 4 * e) = __uint_as_float(w[e]);
-        } else {
-            reinterpret_cast<unsigned short*>(dst)[e] = static_cast<unsigned short>(w[e / 2] >> 16 * (e & 1));
-        }
+        if constexpr (SIZE == 4) reinterpret_cast<float*>(dst)[e] = __uint_as_float(w[e]);
+        else reinterpret_cast<unsigned short*>(dst)[e] = static_cast<unsigned short>(w[e / 2] >> 16 * (e & 1));
     }
 }
 
@@ -447,6 +483,30 @@ __device__ __forceinline__ void read_piece(unsigned src, bool filled, unsigned* 
     }
 }
 
+// The accumulator's rows of a warp to the result through TMA, in pieces of 128 bytes a row staged in `STAGES` buffers
+// in turn (piece `n`: the running number).  Not inlined: its registers are no burden on the other paths.
+template <typename G, int STAGES>
+__device__ __noinline__ unsigned store_aligned(unsigned src, bool filled, unsigned stages, unsigned n, const CUtensorMap* map, int x, int y, int z, int cols) {
+    const int lane = threadIdx.x % 32;
+    constexpr int COLS = 128 / int(sizeof(G));
+    const unsigned long long policy = evict_first();
+    for (int c0 = 0; c0 < cols; c0 += COLS, ++n) {
+        unsigned piece[32];
+        read_piece<G>(src + unsigned(c0), filled, piece);
+        // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
+        const unsigned stage = stages + n % STAGES * 4096u;
+        if (lane == 0) tma_store_read<STAGES - 1>();
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            put_shared(stage + lane * 128 + ((j ^ (lane & 7)) << 4), make_uint4(piece[4 * j], piece[4 * j + 1], piece[4 * j + 2], piece[4 * j + 3]));
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) tma_store(map, stage, x + c0, y, z, policy);
+    }
+    return n;
+}
+
 // The accumulator's rows of a warp (cols = `bytes` of G) to rows of the result that start anywhere, `row_bytes`
 // apart: each is moved up by what its start lies behind a multiple of 32 bytes, the words that move out of a piece
 // are the next one's first, and what is written are whole aligned 16-byte chunks but for the row's ends.  Not
@@ -454,8 +514,8 @@ __device__ __forceinline__ void read_piece(unsigned src, bool filled, unsigned* 
 // Measured against single elements from the staging buffer (odd row length): 11 x 512 tokens, 4096 x 4096: fp32 414 ->
 // 343 us (TMA stores, where rows start on 16 bytes: 261), bf16 546 -> 293 (208); 4 x 4096, 2048 x 2048, fp32 505 -> 212
 // (190); 11 x 128, 2048 x 2048, fp32 107 -> 74 (42).  A row's ends by the row's lane, or by eight lanes per row in a loop
-// of their own, were slower where nothing is added (90 and 99 us for the last).
-template <typename G, bool ADD>
+// of their own, were slower (90 and 99 us for the last).
+template <typename G>
 __device__ __noinline__ void store_anywhere(unsigned src, bool filled, unsigned stage, char* first, int64_t row_bytes, int bytes, int rows) {
     const int lane = threadIdx.x % 32;
     const unsigned by = unsigned(reinterpret_cast<uintptr_t>(first + lane * row_bytes)) & 31u;
@@ -499,7 +559,7 @@ __device__ __noinline__ void store_anywhere(unsigned src, bool filled, unsigned 
             for (int k = 0; k < 8; ++k) v[k] = get_shared(from + k * 512 + ((j ^ ((4 * k + lane / 8) & 7)) << 4));
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                store_chunk<G, ADD>(reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(begin) & ~uintptr_t(31)) + at + 16 * j, v[k]);
+                *reinterpret_cast<uint4*>(reinterpret_cast<char*>(reinterpret_cast<uintptr_t>(begin) & ~uintptr_t(31)) + at + 16 * j) = v[k];
                 begin += 4 * row_bytes;
             }
         } else {
@@ -508,8 +568,8 @@ __device__ __noinline__ void store_anywhere(unsigned src, bool filled, unsigned 
                 const int off = at + 16 * j - int(reinterpret_cast<uintptr_t>(begin) & 31u);
                 if (4 * k + lane / 8 < rows && off > -16 && off < bytes) {
                     const uint4 v = get_shared(from + k * 512 + ((j ^ ((4 * k + lane / 8) & 7)) << 4));
-                    if (off >= 0 && off + 16 <= bytes) store_chunk<G, ADD>(begin + off, v);
-                    else store_elements<G, ADD>(begin + off, v, off, bytes);
+                    if (off >= 0 && off + 16 <= bytes) *reinterpret_cast<uint4*>(begin + off) = v;
+                    else store_elements<G>(begin + off, v, off, bytes);
                 }
                 begin += 4 * row_bytes;
             }
@@ -526,6 +586,7 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
     typedef Plan<MODE> P;
     constexpr int WG_RING = P::A_RING, WG_Q_RING = P::Q_RING, WG_GROUPS = P::GROUPS, WG_THREADS = P::THREADS;
     constexpr bool TMA_A = MODE != WG_PLAIN_DY;
+    constexpr int CHUNK = Chunk<G>::STEPS;
     typedef WGSmem<MODE> Smem;
     extern __shared__ uint8_t raw[];
     Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
@@ -643,7 +704,8 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
             const unsigned long long desc_b = operand_desc(kb_smem_u32(sm.b), WG_BLOCK, 1024, 2);
             // a block of ones needs no layout: every address the descriptor reaches holds 1
             const unsigned long long desc_ones = operand_desc(kb_smem_u32(sm.ones), 256, 256, 0);
-            unsigned n_acc = 0, n_late = 0, panels = 0;
+            unsigned n_late = 0, panels = 0;
+            Halves acc;
             for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
                 const Tile t = tile_at<MODE>(a, i);
                 const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
@@ -654,17 +716,17 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                 int begun = 0;                                   // the accumulator's first step
                 for (int s = 0; s < steps; ++s, ++g) {
                     const Ring<WG_RING> r(g);
-                    if (s == 0 || s - begun == a.chunk) {
-                        // on to the other accumulator
+                    if (s == 0 || s - begun == CHUNK) {
+                        // on to the tile's half, or from the chunk before to the other one
                         if (s > 0) {
-                            if (elect_one()) mma_commit(&sm.acc_full[Ring<2>(n_acc).slot]);
+                            if (elect_one()) mma_commit(&sm.acc_full[acc.half()]);
                             __syncwarp();
-                            ++n_acc;
+                            acc.used();
+                            acc.other();
                         }
-                        const Ring<2> acc(n_acc);
-                        if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[acc.slot]), acc.parity ^ 1u, error)) { ok = false; break; }
+                        if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[acc.half()]), acc.parity() ^ 1u, error)) { ok = false; break; }
                         tc_fence_after();
-                        d = tmem + acc.slot * WG_N;
+                        d = tmem + acc.half() * WG_N;
                         begun = s;
                     }
                     if (TMA_A && !kb_wait_warp(kb_smem_u32(&sm.a_full[r.slot]), r.parity, error)) { ok = false; break; }
@@ -693,18 +755,18 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                 }
                 if (MODE == WG_PANEL && panel_last && !bias) ++panels;
                 if (ok && steps > 0) {
-                    if (elect_one()) mma_commit(&sm.acc_full[Ring<2>(n_acc).slot]);
+                    if (elect_one()) mma_commit(&sm.acc_full[acc.half()]);
                     __syncwarp();
-                    ++n_acc;
+                    acc.used();
+                    acc.next_tile();
                 }
             }
             // nothing is in flight when the tensor memory is freed: on the good path the store warps have
             // seen every accumulator; after a wait that gave up, wait for what was issued
             if (!ok) {
-                const Ring<2> acc(n_acc);
-                if (elect_one()) mma_commit(&sm.acc_full[acc.slot]);
+                if (elect_one()) mma_commit(&sm.acc_full[acc.half()]);
                 __syncwarp();
-                kb_wait(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error, true, 1u << 10);
+                kb_wait(kb_smem_u32(&sm.acc_full[acc.half()]), acc.parity(), error, true, 1u << 10);
             }
         }
     } else if (warp >= WG_RESTORE_WARP0 && MODE == WG_RESTORED) {
@@ -835,66 +897,51 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
         }
     } else if (warp >= WG_STORE_WARP0) {
         const int quarter = warp - WG_STORE_WARP0;               // == warp % 4: tensor-memory lanes 32 quarter ..
-        constexpr int COLS = 128 / int(sizeof(G));               // columns of a piece: rows of 128 bytes
-        unsigned n_acc = 0, n_piece = 0;
+        unsigned n_piece = 0;
+        Halves acc;
         for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
             const Tile t = tile_at<MODE>(a, i);
             const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M + quarter * 32;
-            // the accumulators of the tile's chunks of tokens, in order: the first is stored, the others added
-            // to it (one chunk of zeros where the worker has no tokens)
-            for (int s0 = 0; s0 < max(t.steps, 1); s0 += a.chunk) {
-                const Ring<2> acc(n_acc);
-                const unsigned src = tmem + acc.slot * WG_N + (unsigned(quarter * 32) << 16);
-                if (t.steps) {
-                    if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[acc.slot]), acc.parity, error)) { ok = false; break; }
-                    tc_fence_after();
+            // the chunks of tokens in order, the later ones added to the first; a worker without tokens has none
+            for (int s0 = 0; s0 < t.steps; s0 += CHUNK) {
+                if (s0 > 0) acc.other();
+                if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[acc.half()]), acc.parity(), error)) { ok = false; break; }
+                tc_fence_after();
+                if (s0 == 0) {
+                    acc.used();                                  // given back below, once it is stored
+                    continue;
                 }
-                if (s0 > 0 && lane == 0) tma_store_done();           // the chunk before is in memory
-                const unsigned long long policy = s0 + a.chunk >= t.steps ? evict_first() : evict_normal();
+                // what lies outside the matrix is added too and never stored
+                add_accumulator(tmem + acc.sum() * WG_N + (unsigned(quarter * 32) << 16), tmem + acc.half() * WG_N + (unsigned(quarter * 32) << 16), t.n == a.nt ? 32 : WG_N);
+                tc_fence_before();
                 __syncwarp();
-                if (t.n == a.nt) {
-                    float v[32];
-                    if (t.steps) tmem_ld32(src, v);
-                    else v[0] = 0.f;
-                    if (o0 + lane < a.out) {
-                        G* db = static_cast<G*>(a.db) + int64_t(t.plane) * a.ld_grads + o0 + lane;
-                        *db = Elem<G>::narrow(s0 > 0 ? Elem<G>::widen(*db) + v[0] : v[0]);
-                    }
-                } else {
-                    G* dw = static_cast<G*>(a.dw) + int64_t(t.plane) * a.ld_grads + o0 * a.pitch + int64_t(t.n) * WG_N;
-                    const int rows = int(min(int64_t(32), a.out - o0));
-                    const int64_t left = a.in - int64_t(t.n) * WG_N;
-                    const int cols = left < WG_N ? int(left) : WG_N;
-                    if (a.wide) {
-                        for (int c0 = 0; c0 < cols && rows > 0; c0 += COLS, ++n_piece) {
-                            unsigned piece[32];
-                            read_piece<G>(src + unsigned(c0), t.steps > 0, piece);
-                            // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
-                            char* stage = reinterpret_cast<char*>(sm.out[quarter][n_piece % P::OUT]);
-                            if (lane == 0) tma_store_read<P::OUT - 1>();
-                            __syncwarp();
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(piece[4 * j], piece[4 * j + 1], piece[4 * j + 2], piece[4 * j + 3]);
-                            fence_async_smem();
-                            __syncwarp();
-                            if (lane == 0 && s0 == 0) tma_store(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.plane, policy);
-                            if (lane == 0 && s0 > 0) tma_add(&map_dw, kb_smem_u32(stage), t.n * WG_N + c0, int(o0), t.plane, policy);
-                        }
-                    } else if (rows > 0) {
-                        const unsigned stage = kb_smem_u32(sm.out[quarter][0]);
-                        char* const first = reinterpret_cast<char*>(dw);
-                        const int64_t row_bytes = a.pitch * int64_t(sizeof(G));
-                        if (sizeof(G) == 4 && s0 > 0) store_anywhere<G, sizeof(G) == 4>(src, true, stage, first, row_bytes, cols * int(sizeof(G)), rows);
-                        else store_anywhere<G, false>(src, t.steps > 0, stage, first, row_bytes, cols * int(sizeof(G)), rows);
-                    }
+                if (lane == 0) arrive_at_leader(&sm.acc_empty[acc.half()]);
+                acc.used();
+            }
+            if (!ok) break;
+            const unsigned src = tmem + acc.sum() * WG_N + (unsigned(quarter * 32) << 16);
+            if (t.n == a.nt) {
+                float v[32];
+                if (t.steps) tmem_ld32(src, v);
+                else v[0] = 0.f;
+                if (o0 + lane < a.out) static_cast<G*>(a.db)[int64_t(t.plane) * a.ld_grads + o0 + lane] = Elem<G>::narrow(v[0]);
+            } else {
+                const int rows = int(min(int64_t(32), a.out - o0));
+                const int64_t left = a.in - int64_t(t.n) * WG_N;
+                const int cols = left < WG_N ? int(left) : WG_N;
+                G* dw = static_cast<G*>(a.dw) + int64_t(t.plane) * a.ld_grads + o0 * a.pitch + int64_t(t.n) * WG_N;
+                if (a.wide) {
+                    if (rows > 0) n_piece = store_aligned<G, P::OUT>(src, t.steps > 0, kb_smem_u32(sm.out[quarter][0]), n_piece, &map_dw, t.n * WG_N, int(o0), t.plane, cols);
+                } else if (rows > 0) {
+                    store_anywhere<G>(src, t.steps > 0, kb_smem_u32(sm.out[quarter][0]), reinterpret_cast<char*>(dw),
+                                      a.pitch * int64_t(sizeof(G)), cols * int(sizeof(G)), rows);
                 }
-                if (t.steps) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) arrive_at_leader(&sm.acc_empty[acc.slot]);
-                    ++n_acc;
-                }
+            }
+            if (t.steps) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_at_leader(&sm.acc_empty[acc.sum()]);
+                acc.next_tile();
             }
         }
         if (lane == 0) tma_store_done();
@@ -1101,11 +1148,6 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
         a.db = p.bias_grads ? static_cast<float*>(p.workspace) + p.out_features * a.pitch : nullptr;
     }
     const int64_t gs = grads_dtype == GAR_F32 ? 4 : 2;
-    // The tensor core truncates what it adds to an accumulator: the sum loses 1e-9 of itself per token, twice
-    // that where it grows steadily (measured: 4.4e-6 at 4096 random tokens, 5.6e-6 at 2048 positive ones; rounded
-    // additions lose a tenth).  fp32 results are summed in chunks, joined by rounded additions: 7e-7 and 1.5e-6
-    // at any length, at the price of one more pass over the tile in L2 per chunk.  16-bit results round off 2e-3.
-    a.chunk = grads_dtype == GAR_F32 ? WG_CHUNK : 0x40000000;
     const int planes = p.workers * a.splits;
     a.wide = reinterpret_cast<uintptr_t>(a.dw) % 16 == 0 && (planes == 1 || a.ld_grads * gs % 16 == 0) && a.pitch * gs % 16 == 0;
 
@@ -1161,7 +1203,7 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
 bool weight_grad_wants_workspace(const gar_weight_grad_params_t& p, int64_t ld_dy) {
     if (splits_of(p, ld_dy) > 1) return true;
     if (panel_applies(p, ld_dy)) return false;
-    const bool chunks = p.grads_dtype == GAR_F32 && p.tokens > WG_CHUNK * WG_K;
+    const bool chunks = p.grads_dtype == GAR_F32 && p.tokens > Chunk<float>::STEPS * WG_K;
     return p.out_features >= (chunks || !rows_on_16(p.dy, ld_dy) ? 768 : 2048);
 }
 

@@ -79,3 +79,99 @@ def test_rows_that_share_memory_are_refused(pkg):
     # a single row may have any stride
     pkg.gar_token_logprobs(x.as_strided((1, cols), (0, 1)), t[:1])
     pkg.gar_linear_weight_grad(x.as_strided((1, 1, cols), (0, 0, 1)), pkg.gar_checkpoint_pack(x[:1]))
+
+
+# ---- sums over many tokens ------------------------------------------------------------------------
+def products_64(pkg, dy, ck, lengths=None):
+    """dW, db and the sum of the terms' magnitudes per worker in 64 bits from the restored activation."""
+    n, t, out = dy.shape
+    x, d = pkg.gar_checkpoint_unpack(ck).double().view(n, t, ck.cols), dy.double()
+    if lengths is not None:
+        live = torch.arange(t, device=DEV)[None, :, None] < lengths[:, None, None]
+        d, x = torch.where(live, d, 0.0), torch.where(live, x, 0.0)
+    return torch.einsum("nto,nti->noi", d, x), d.sum(1), torch.einsum("nto,nti->noi", d.abs(), x.abs()), d.abs().sum(1)
+
+
+def weight_grads(pkg, dy, ck, dtype, lengths, off, space):
+    """(dW, db) from a block whose rows are 1 longer than the layer and start it at `off`."""
+    n, _, out = dy.shape
+    weights = out * ck.cols
+    g = torch.full((n, off + weights + out + 1), 7.0, dtype=dtype, device=DEV)
+    pkg.gar_linear_weight_grad(dy, ck, g, off, off + weights, lengths, workspace=space)
+    assert torch.all(g[:, :off] == 7.0) and torch.all(g[:, -1] == 7.0)
+    return g[:, off:off + weights].reshape(n, out, ck.cols), g[:, off + weights:-1]
+
+
+def half_unit(x, dtype):
+    """Half the distance of the type's numbers around x (normal numbers)."""
+    bits = {torch.float32: 24, torch.bfloat16: 8, torch.float16: 11}[dtype]
+    return torch.exp2(torch.floor(torch.log2(x.abs())) - bits)
+
+
+@pytest.mark.parametrize("out,inp,off", [(300, 520, 3), (264, 264, 8)])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("tokens", [769, 2049, 16384])
+def test_weight_grad_16_bit_results_of_many_tokens(pkg, out, inp, off, dtype, tokens):
+    """Positive operands, so that sums grow steadily, the case in which additions that truncate lose most.  An accumulator
+    takes 2048 tokens in 128 instructions, each of which may lose a unit of the accumulator (half the final one on
+    average) and one of the products' common exponent: 128 2^-23 at most; the joins add 8 2^-24.  That on top
+    of the result's own rounding, half a unit.  One accumulator of 16384 tokens loses 3e-5 and more."""
+    dy = normal((1, tokens, out), torch.bfloat16, tokens).abs()
+    ck = pkg.gar_checkpoint_pack(normal((tokens, inp), torch.bfloat16, out).abs(), 64)
+    dw, db, _, _ = products_64(pkg, dy, ck)
+    for space in (False, True):
+        for got, want in zip(weight_grads(pkg, dy, ck, getattr(torch, dtype), None, off, space), (dw, db)):
+            assert torch.all((got.double() - want).abs() <= half_unit(want, got.dtype) + (128 * 2.0 ** -23 + 8 * 2.0 ** -24) * want)
+
+
+def test_weight_grad_16_bit_results_are_not_biased(pkg):
+    """Positive operands, 16384 tokens, binary16 results.  A result's rounding is off by at most 2^-11 of it either way,
+    2.9e-4 rms, so the mean over 66560 of them by 1.1e-6, five times that at most 5.6e-6; the sums of 2048 tokens
+    are short by 5.7e-6.  A single truncating accumulator is short by 3e-5 and more."""
+    t, out, inp = 16384, 64, 1040
+    dy = normal((1, t, out), torch.bfloat16, 1).abs()
+    ck = pkg.gar_checkpoint_pack(normal((t, inp), torch.bfloat16, 2).abs(), 64)
+    want = products_64(pkg, dy, ck)[0]
+    for space in (False, True):
+        got = weight_grads(pkg, dy, ck, torch.float16, None, 0, space)[0].double()
+        assert abs(float(((got - want) / want).mean())) <= 1.2e-5
+
+
+@pytest.mark.parametrize("out,inp,off", [(40, 72, 0), (33, 70, 3), (520, 264, 0)])
+@pytest.mark.parametrize("dtype,tokens,ends", [("float32", 768, None), ("float32", 1536, None), ("float32", 2304, (767, 768, 769, 1536)),
+                                               ("float32", 1537, (1535, 1536, 1537, 0)), ("bfloat16", 2048, None), ("bfloat16", 4096, None),
+                                               ("float16", 4097, (2047, 2048, 2049, 4096)), ("bfloat16", 6145, (6144, 4095, 6145, 0))])
+def test_weight_grad_at_the_edges_of_chunks(pkg, out, inp, off, dtype, tokens, ends):
+    """Tokens that end on, before and behind a multiple of what an accumulator sums (768 tokens, 2048 for 16-bit
+    results), stored by TMA and plainly, with a bias, several tiles to a pair.  Additions are off by a unit of the running
+    sum at most: one for every token of a chunk, and one for every chunk."""
+    n = 4 if ends else 2
+    dy = normal((n, tokens, out), torch.bfloat16, tokens)
+    ck = pkg.gar_checkpoint_pack(normal((n * tokens, inp), torch.bfloat16, inp), 32)
+    lengths = torch.tensor(ends, dtype=torch.int32, device=DEV) if ends else None
+    dw, db, sw, sb = products_64(pkg, dy, ck, lengths)
+    unit = ((768 if dtype == "float32" else 2048) + 4) * 2.0 ** -23
+    half = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}[dtype]
+    for space in (False, True):
+        w, b = weight_grads(pkg, dy, ck, getattr(torch, dtype), lengths, off, space)
+        assert torch.all((w.double() - dw).abs() <= unit * sw + half * dw.abs() + 2.0 ** -25)
+        assert torch.all((b.double() - db).abs() <= unit * sb + half * db.abs() + 2.0 ** -25)
+        if dtype == "float32":
+            assert float((w.double() - dw).norm()) <= 2e-6 * float(dw.norm())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16"])
+def test_weight_grad_chunks_over_many_tiles(pkg, dtype):
+    """Several tiles of one, two and more chunks for every pair of CTAs, empty workers among them: the halves of tensor
+    memory change hands between tiles and chunks."""
+    n, t, out, inp = 12, 2304, 1100, 1600
+    dy = normal((n, t, out), torch.bfloat16, 1)
+    ck = pkg.gar_checkpoint_pack(normal((n * t, inp), torch.bfloat16, 2), 128)
+    lengths = torch.tensor([t, 0, 700, 768, 769, 2048, 2049, 1, 1536, 0, 1537, t], dtype=torch.int32, device=DEV)
+    dw, db, sw, sb = products_64(pkg, dy, ck, lengths)
+    unit = ((768 if dtype == "float32" else 2048) + 4) * 2.0 ** -23
+    half = {"float32": 2.0 ** -24, "float16": 2.0 ** -11}[dtype]
+    for space in (False, True):
+        w, b = weight_grads(pkg, dy, ck, getattr(torch, dtype), lengths, 0, space)
+        assert torch.all((w.double() - dw).abs() <= unit * sw + half * dw.abs() + 2.0 ** -25)
+        assert torch.all((b.double() - db).abs() <= unit * sb + half * db.abs() + 2.0 ** -25)
