@@ -216,36 +216,75 @@ __device__ __forceinline__ Raw8<T> restore8(const uint2& codes, float scale) {
     return narrow8<T>(v);
 }
 
-__device__ __forceinline__ float sigmoid(float x) {
+__device__ __forceinline__ float rcp(float x) {
     float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(-x * kLog2e)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+__device__ __forceinline__ float sigmoid(float x) { return rcp(1.f + ex2(-x * kLog2e)); }
 
+// The normal distribution at two places: cdf = P(X < x) and the density's e^(-x^2 / 2).  The tail behind |x| is
+//     e^(-x^2 / 2) t P(t),   t = 1 / (1 + 0.275 |x|)
+// (the form of Abramowitz and Stegun 26.2.17), P of degree 8 fitted to e^(x^2 / 2) erfc(x / sqrt 2) / 2 t: 2.8e-7 of the
+// tail at most, in fp32 1e-6 down to -4 and 2e-6 at -6, where the exponent's rounding shows.  (1 + erf(x / sqrt 2)) / 2
+// cancels for negative x: 4 % off at -5, 0 from -5.5 on.  bf16 8192 x 8192, forward and backward: 76 and 60 us; with
+// erff 105 and 95 us, with erfcf 143 and 131.
+__device__ __forceinline__ void normal2(float x0, float x1, float (&cdf)[2], float (&e)[2]) {
+    const float t0 = rcp(fmaf(fabsf(x0), 0.275f, 1.f)), t1 = rcp(fmaf(fabsf(x1), 0.275f, 1.f));
+    const f32x2 t = pack2(t0, t1), x = pack2(x0, x1), c = pack2(-0.5f * kLog2e, -0.5f * kLog2e);
+    unpack2(mul2(mul2(x, x), c), e[0], e[1]);
+    e[0] = ex2(e[0]);
+    e[1] = ex2(e[1]);
+    f32x2 p = pack2(0.0237322034f, 0.0237322034f);
+    constexpr float P[8] = {-0.0965348071f, 0.106157018f, -0.0134071806f, 0.0766527223f, 0.0823775453f, 0.101610145f, 0.10970306f, 0.109709157f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p = fma2(p, t, pack2(P[i], P[i]));
+    float tail0, tail1;
+    unpack2(mul2(mul2(p, t), pack2(e[0], e[1])), tail0, tail1);
+    cdf[0] = x0 < 0.f ? tail0 : 1.f - tail0;
+    cdf[1] = x1 < 0.f ? tail1 : 1.f - tail1;
+}
+
+// act(x) of eight elements
 template <int ACT>
-__device__ __forceinline__ float act(float x) {
-    if (ACT == GAR_ACT_RELU) return max_nan(x, 0.f);
-    if (ACT == GAR_ACT_SILU) return x * sigmoid(x);
-    if (ACT == GAR_ACT_GELU) return 0.5f * x * (1.f + erff(x * 0.70710678118654752f));
-    return x;
+__device__ __forceinline__ void act8(const float (&x)[8], float (&y)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        if constexpr (ACT == GAR_ACT_GELU) {
+            float cdf[2], e[2];
+            normal2(x[i], x[i + 1], cdf, e);
+            y[i] = x[i] * cdf[0];
+            y[i + 1] = x[i + 1] * cdf[1];
+        } else {
+#pragma unroll
+            for (int k = i; k < i + 2; ++k) y[k] = ACT == GAR_ACT_RELU ? max_nan(x[k], 0.f) : ACT == GAR_ACT_SILU ? x[k] * sigmoid(x[k]) : x[k];
+        }
+    }
 }
 // act(x) and act'(x)
 template <int ACT>
-__device__ __forceinline__ void act_slope(float x, float& y, float& slope) {
-    if (ACT == GAR_ACT_RELU) {
-        y = max_nan(x, 0.f);
-        slope = x > 0.f ? 1.f : (x == x ? 0.f : x);
-    } else if (ACT == GAR_ACT_SILU) {
-        const float g = sigmoid(x);
-        y = x * g;
-        slope = fmaf(y, 1.f - g, g);
-    } else if (ACT == GAR_ACT_GELU) {
-        const float cdf = 0.5f * (1.f + erff(x * 0.70710678118654752f));
-        y = x * cdf;
-        slope = fmaf(x * 0.3989422804014327f, ex2(x * x * (-0.5f * kLog2e)), cdf);
-    } else {
-        y = x;
-        slope = 1.f;
+__device__ __forceinline__ void act_slope8(const float (&x)[8], float (&y)[8], float (&slope)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        float cdf[2], e[2];
+        if (ACT == GAR_ACT_GELU) normal2(x[i], x[i + 1], cdf, e);
+#pragma unroll
+        for (int k = i; k < i + 2; ++k) {
+            if (ACT == GAR_ACT_GELU) {
+                y[k] = x[k] * cdf[k - i];
+                slope[k] = fmaf(x[k] * 0.3989422804014327f, e[k - i], cdf[k - i]);
+            } else if (ACT == GAR_ACT_RELU) {
+                y[k] = max_nan(x[k], 0.f);
+                slope[k] = x[k] > 0.f ? 1.f : (x[k] == x[k] ? 0.f : x[k]);
+            } else if (ACT == GAR_ACT_SILU) {
+                const float g = sigmoid(x[k]);
+                y[k] = x[k] * g;
+                slope[k] = fmaf(y[k], 1.f - g, g);
+            } else {
+                y[k] = x[k];
+                slope[k] = 1.f;
+            }
+        }
     }
 }
 
@@ -317,10 +356,7 @@ __global__ void __launch_bounds__(CK_THREADS) activation_forward_kernel(const Fo
         }
         float v[8], y[8];
         widen8<T>(x[k], v);
-        if (a.y || a.sy.q) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = act<ACT>(v[i]);
-        }
+        if (a.y || a.sy.q) act8<ACT>(v, y);
         if (a.sx.q) save8<LAYOUT>(v, magnitude<T>(top_x), count, leader, a.sx.q + t.at(a.sx.ld), a.sx.scales + t.group);
         if (GATED) {
             widen8<T>(u[k], v);
@@ -374,27 +410,22 @@ __global__ void __launch_bounds__(CK_THREADS) activation_backward_kernel(const B
         const Task<LAYOUT> t(a, (blockIdx.x * CK_TASKS + k) * CK_THREADS + threadIdx.x);
         const int count = t.count;
         if (count == 0) continue;
-        float d[8], x[8], dx[8];
+        float d[8], x[8], y[8], slope[8], dx[8];
         widen8<T>(dy[k], d);
         widen8<T>(restore8<T>(cx[k], sx[k]), x);
+        act_slope8<ACT>(x, y, slope);
         if (GATED) {
             float u[8], du[8];
             widen8<T>(restore8<T>(cu[k], su[k]), u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                float y, slope;
-                act_slope<ACT>(x[i], y, slope);
-                du[i] = d[i] * y;
-                dx[i] = d[i] * u[i] * slope;
+                du[i] = d[i] * y[i];
+                dx[i] = d[i] * u[i] * slope[i];
             }
             store8<T, LAYOUT>(static_cast<T*>(a.dup) + t.at(a.lddup), count, narrow8<T>(du));
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float y, slope;
-                act_slope<ACT>(x[i], y, slope);
-                dx[i] = d[i] * slope;
-            }
+            for (int i = 0; i < 8; ++i) dx[i] = d[i] * slope[i];
         }
         store8<T, LAYOUT>(static_cast<T*>(a.dx) + t.at(a.lddx), count, narrow8<T>(dx));
     }

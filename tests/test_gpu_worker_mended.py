@@ -175,3 +175,36 @@ def test_weight_grad_chunks_over_many_tiles(pkg, dtype):
         w, b = weight_grads(pkg, dy, ck, getattr(torch, dtype), lengths, 0, space)
         assert torch.all((w.double() - dw).abs() <= unit * sw + half * dw.abs() + 2.0 ** -25)
         assert torch.all((b.double() - db).abs() <= unit * sb + half * db.abs() + 2.0 ** -25)
+
+
+# ---- GELU of negative values -----------------------------------------------------------------------
+TYPES = {"float32": (2.0 ** -24, 1e-37), "bfloat16": (2.0 ** -8, 1e-37), "float16": (2.0 ** -11, 2.0 ** -25)}
+
+
+def gelu_64(x):
+    """GELU and its derivative in 64 bits."""
+    cdf = 0.5 * torch.special.erfc(-x / math.sqrt(2.0))
+    return x * cdf, cdf + x * torch.exp(-0.5 * x * x) / math.sqrt(2.0 * math.pi)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_gelu_of_negative_values(pkg, dtype):
+    """x in [-6, -2], where GELU falls to 6e-9 of x: relative to the result.  The argument x / sqrt 2 is off by 1.5 units of
+    2^-24, which erfc amplifies by x^2 <= 36, erfc itself by 4 units, the exponential of -x^2 / 2 by about as much as
+    the argument: below 5e-6, and the derivative's two terms are of one size and sign or 4 times apart.  On top of that the
+    output's rounding."""
+    half, tiny = TYPES[dtype]
+    x = torch.linspace(-6.0, -2.0, 8192, device=DEV).view(64, 128).to(getattr(torch, dtype))
+    want, _ = gelu_64(x.double())
+    f = pkg.gar_activation_forward("gelu", x, group=32)
+    assert torch.all((f.y.double() - want).abs() <= (5e-6 + half) * want.abs() + tiny)
+    xr = pkg.gar_checkpoint_unpack(f.x)
+    assert torch.all(xr < -1.9)
+    _, slope = gelu_64(xr.double())
+    g = pkg.gar_activation_backward("gelu", torch.ones_like(x), f.x)
+    assert torch.all((g.dx.double() - slope).abs() <= (1e-5 + half) * slope.abs() + tiny)
+    # gated: the gradient at `up` is dy act(x)
+    f = pkg.gar_activation_forward("gelu", x, torch.ones_like(x), group=32)
+    g = pkg.gar_activation_backward("gelu", torch.ones_like(x), f.x, f.up)
+    want, _ = gelu_64(xr.double())
+    assert torch.all((g.dup.double() - want).abs() <= (5e-6 + half) * want.abs() + tiny)
