@@ -59,8 +59,8 @@ int gar_token_logprobs(const gar_logprobs_params_t* params);
  * top_logprobs[i]:
  *     dx_j = -p_j (a + sum_i b_i + c (log p_j + entropy)) + a [j = t] + sum_i b_i [j = top_index_i]
  * from the logits and the saved lse (and entropy, when grad_entropy is given).  A row without a
- * target has a = 0; an empty row has gradient 0; a target or index outside the vocabulary gives a
- * row of NaN.  dlogits has the logits' type and may be the logits themselves (same ld); any other
+ * target has a = 0.  An empty row has gradient 0 whatever a, c, b_i, its target and its indices are;
+ * in any other row a target or index outside the vocabulary gives a row of NaN.  dlogits has the logits' type and may be the logits themselves (same ld); any other
  * overlap is refused.
  */
 typedef struct gar_logprobs_grad_params_t {

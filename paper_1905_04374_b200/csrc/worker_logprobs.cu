@@ -646,12 +646,13 @@ struct RowGrad {
     float   b;                             // its gradient
 };
 // What grad_at reads, from the sums: dx = p (c' log p + sum'), c' = -c, sum' = -(sum + c H).  An empty row
-// (lse = -inf) gets lse = +inf: every p is 0.
+// (lse = -inf) gets lse = +inf, so that every p is 0, and c' = sum' = 0: the gradients at its results, which are
+// infinite themselves, may be infinities or NaN.
 __device__ __forceinline__ void settle(RowGrad& r) {
     r.empty = r.lse == -CUDART_INF_F;
     if (r.empty) r.lse = CUDART_INF_F;
-    r.sum = -fmaf(r.c, r.entropy, r.sum);
-    r.c = -r.c;
+    r.sum = r.empty ? 0.f : -fmaf(r.c, r.entropy, r.sum);
+    r.c = r.empty ? 0.f : -r.c;
 }
 // All 32 lanes of a warp call.
 __device__ __forceinline__ RowGrad row_grad(const BackwardArgs& g, int64_t row, int lane) {

@@ -208,3 +208,24 @@ def test_gelu_of_negative_values(pkg, dtype):
     g = pkg.gar_activation_backward("gelu", torch.ones_like(x), f.x, f.up)
     want, _ = gelu_64(xr.double())
     assert torch.all((g.dup.double() - want).abs() <= (5e-6 + half) * want.abs() + tiny)
+
+
+# ---- the gradient of rows that are masked throughout -------------------------------------------------
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("vocab", [5, 64, 65, 300, 3000, 20000])
+def test_empty_rows_have_gradient_zero_whatever_comes_in(pkg, dtype, vocab):
+    """A row of -inf has log probabilities of -inf, so what comes back from a loss over them is often infinite or
+    NaN.  Its gradient is 0 at every vocabulary, with targets and indices outside of it too; other rows that name
+    such a target are NaN."""
+    top, rows = 3, 8
+    x = normal((rows, vocab), getattr(torch, dtype), vocab)
+    x[:6] = -math.inf
+    t = torch.tensor([0, 1, 2, 3, vocab, -1, vocab, 1], device=DEV)
+    r = pkg.gar_token_logprobs(x, t, top=top)
+    r.top_index[4, 1] = vocab + 7
+    a, c, b = (torch.ones(s, device=DEV) for s in ((rows,), (rows,), (rows, top)))
+    a[0], a[1], c[2], c[3], b[3, 1], b[5, 0] = math.inf, math.nan, -math.inf, math.nan, math.nan, math.inf
+    for out in (None, torch.full_like(x, 7.0), x.clone()):
+        src = out if out is not None and torch.isinf(out[0, 0]) else x
+        dx = pkg.gar_token_logprobs_backward(src, r, t, a, c, b, dlogits=out)
+        assert torch.all(dx[:6] == 0) and torch.isnan(dx[6]).all() and torch.isfinite(dx[7]).all()
