@@ -17,6 +17,7 @@ namespace {
 constexpr int CK_THREADS = 256;
 constexpr int CK_TASKS = 2;                            // per thread: all loads before the arithmetic
 constexpr float CK_TINY = 7.888609052210118e-31f;     // 2^-100
+constexpr float CK_LARGEST = 2.6793884e+36f;           // the largest scale whose 127-fold is finite in fp32
 
 // Division of a task number by the tasks per row: exact for numerators below 2^31.
 struct FastDiv {
@@ -172,7 +173,7 @@ __device__ __forceinline__ void save8(const float (&v)[8], float top, int count,
     if (leader) {
         // top / 127, correctly rounded: Markstein's correction of the product with the rounded reciprocal
         const float y = 1.f / 127.f, q0 = __fmul_rn(top, y);
-        const float s = __fmaf_rn(__fmaf_rn(-127.f, q0, top), y, q0);
+        const float s = fminf(__fmaf_rn(__fmaf_rn(-127.f, q0, top), y, q0), CK_LARGEST);
         *scale = !sound ? CUDART_NAN_F : live ? s : 0.f;
     }
     // |v inv| <= 127 (1 + 2^-22): the low byte of the sum with 1.5 * 2^23 is the nearest integer, ties to even

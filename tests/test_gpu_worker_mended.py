@@ -229,3 +229,24 @@ def test_empty_rows_have_gradient_zero_whatever_comes_in(pkg, dtype, vocab):
         src = out if out is not None and torch.isinf(out[0, 0]) else x
         dx = pkg.gar_token_logprobs_backward(src, r, t, a, c, b, dlogits=out)
         assert torch.all(dx[:6] == 0) and torch.isnan(dx[6]).all() and torch.isfinite(dx[7]).all()
+
+
+# ---- groups that hold the type's largest value --------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_the_largest_finite_value_is_restored_finite(pkg, dtype, sign):
+    """Masks of the type's lowest value (or its highest) in an activation: a finite group is restored finite, each value
+    within half a step and two roundings (2^-23 of the largest)."""
+    x = normal((4, 256), getattr(torch, dtype), 1)
+    big = torch.finfo(x.dtype).max
+    x[0, 3] = sign * big
+    x[1] = sign * big
+    x[2, 64:] = torch.nextafter(torch.tensor(big), torch.tensor(0.0)) if dtype == "float32" else big / 2
+    ck = pkg.gar_checkpoint_pack(x, 64)
+    got = pkg.gar_checkpoint_unpack(ck).double()
+    assert torch.isfinite(got).all()
+    top = x.double().unflatten(1, (-1, 64)).abs().amax(2).repeat_interleave(64, 1)
+    half = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}[dtype]
+    assert torch.all((got - x.double()).abs() <= top * (0.5 / 127 * (1 + 1e-5) + 2.0 ** -23 + half))
+    f = pkg.gar_activation_forward("silu", x, group=64)
+    assert torch.isfinite(pkg.gar_activation_backward("silu", torch.ones_like(x), f.x).dx).all()
