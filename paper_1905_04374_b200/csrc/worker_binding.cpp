@@ -100,6 +100,13 @@ T* vector(const Tensor& t, const char* name, at::ScalarType type, int64_t numel,
     return pointer<T>(t);
 }
 
+// A tensor of the caller's that the call has written: its version moves on, so that autograd notices if it was saved.
+void written(PyObject* o) {
+    if (o == Py_None) return;
+    const Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // ---- Python arguments -----------------------------------------------------------------------------
 bool given(PyObject* o) { return o != Py_None; }
 const Tensor& tensor(PyObject* o, const char* name) {
@@ -227,6 +234,7 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.dlogits = d.p; p.ld_dlogits = d.ld;
     p.stream = place.stream();
     if (const int st = gar_token_logprobs_backward(&p)) return status(st);
+    written(a[9]);
     return THPVariable_Wrap(dx);
     END_HANDLE_TH_ERRORS
 }
@@ -259,6 +267,7 @@ PyObject* checkpoint_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {  // q
     TORCH_CHECK_TYPE(m.dtype == code, "out must be of the checkpoint's type");
     TORCH_CHECK_VALUE(m.rows == rows && m.cols == cols && out.device() == q.device(), "out must be [", rows, ", ", cols, "] on ", q.device());
     if (const int st = gar_checkpoint_unpack(int(code), &s, rows, cols, int(group), m.p, m.ld, place.stream())) return status(st);
+    written(a[5]);
     return THPVariable_Wrap(out);
     END_HANDLE_TH_ERRORS
 }
@@ -296,6 +305,7 @@ PyObject* activation_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     p.stream = place.stream();
     if (const int st = gar_activation_forward(&p)) return status(st);
+    written(a[6]);
     return tuple_of({y, hx.q, hx.scales, hu.q, hu.scales, hy.q, hy.scales});
     END_HANDLE_TH_ERRORS
 }
@@ -327,6 +337,8 @@ PyObject* activation_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     p.stream = place.stream();
     if (const int st = gar_activation_backward(&p)) return status(st);
+    written(a[8]);
+    written(a[9]);
     return tuple_of({dx, dup});
     END_HANDLE_TH_ERRORS
 }
@@ -390,7 +402,9 @@ PyObject* linear_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         p.workspace_bytes = size_t(space.numel()) * space.element_size();
     }
     p.stream = place.stream();
-    return status(gar_linear_weight_grad(&p));
+    const int st = gar_linear_weight_grad(&p);
+    if (!st) written(a[5]);
+    return status(st);
     END_HANDLE_TH_ERRORS
 }
 

@@ -2,7 +2,10 @@
 
 Every function has the name of its C entry point.  Matrices are 2-D CUDA tensors with unit column
 stride and any row stride that keeps the rows apart (an expanded tensor, whose rows share memory, is
-refused: make it contiguous); outputs are allocated, unless given, on the stream the call runs on.  The marshalling
+refused: make it contiguous); outputs are allocated, unless given, on the stream the call runs on.
+There is no autograd: results carry no gradient function whatever the inputs require, and the gradient of
+a call is the call that computes it.  Tensors that a call writes (y=, dx=, dup=, dlogits=, out=, grads)
+count as modified in place, so autograd refuses a backward pass that saved one of them.  The marshalling
 itself is compiled (csrc/worker_binding.cpp); the ctypes mirrors of the parameter blocks are for
 callers of the C ABI.  Nothing is computed here and there is no fallback.
 """

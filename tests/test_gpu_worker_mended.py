@@ -250,3 +250,40 @@ def test_the_largest_finite_value_is_restored_finite(pkg, dtype, sign):
     assert torch.all((got - x.double()).abs() <= top * (0.5 / 127 * (1 + 1e-5) + 2.0 ** -23 + half))
     f = pkg.gar_activation_forward("silu", x, group=64)
     assert torch.isfinite(pkg.gar_activation_backward("silu", torch.ones_like(x), f.x).dx).all()
+
+
+# ---- autograd -----------------------------------------------------------------------------------------
+def test_tensors_that_a_call_writes_count_as_modified(pkg):
+    """Autograd has to see that a tensor it saved was overwritten; results themselves carry no gradient function."""
+    x = normal((4, 64), torch.bfloat16, 1)
+    t = torch.zeros(4, dtype=torch.int64, device=DEV)
+    ones = torch.ones(4, device=DEV)
+    r = pkg.gar_token_logprobs(x, t)
+    f = pkg.gar_activation_forward("silu", x, x.clone())
+
+    def versions(*outs):
+        return [o._version for o in outs]
+    y, dx, dup, g = (torch.empty_like(x) for _ in range(4))
+    block = torch.empty(1, 64 * 64, device=DEV)
+    before = versions(x, y, dx, dup, g, block)
+    pkg.gar_activation_forward("silu", x, y=y)
+    pkg.gar_activation_backward("silu", x, f.x, f.up, dx=dx, dup=dup)
+    pkg.gar_token_logprobs_backward(x, r, t, ones, dlogits=g)
+    pkg.gar_linear_weight_grad(x.view(1, 4, 64), f.x, block)
+    after = versions(x, y, dx, dup, g, block)
+    assert after[0] == before[0] and all(a > b for a, b in zip(after[1:], before[1:]))
+    pkg.gar_checkpoint_unpack(f.x, y)
+    assert y._version > after[1]
+
+    w = x.float().requires_grad_()
+    h = w * 1
+    loss = (h * h).sum()                                     # saves h
+    out = pkg.gar_activation_forward("relu", h, save_input=False, y=h)
+    assert out.y is h or out.y.data_ptr() == h.data_ptr()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    assert pkg.gar_activation_forward("relu", w, save_input=False).y.grad_fn is None
+    with torch.inference_mode():
+        z = torch.ones(2, 64, device=DEV)
+        pkg.gar_activation_forward("relu", z, save_input=False, y=z)
+    pkg.gar_activation_forward("relu", z, save_input=False, y=z)      # an inference tensor has no version
