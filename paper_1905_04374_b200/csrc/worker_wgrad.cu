@@ -75,15 +75,20 @@ template <int MODE> struct Plan {
     static constexpr int B_SLOTS = MODE == WG_PANEL ? WG_PANEL_STEPS : A_RING;    // restored tiles
     // Groups of four restore warps take steps in turn.  A step takes a group about 1500 cycles from its slot
     // being free to the arrival (waits, reads, 220 instructions, fence), three times what the products take.
-    // A slot of codes belongs to one group for good (Q_RING is a multiple of GROUPS): who waits for a
-    // parity has to have followed the slot's rounds.
+    // A parity tells a barrier's round from the one before, so who waits for it has to know that the last but one is
+    // over.  Of the operands' slots: a group's step before, GROUPS steps ago, found its slot free, so all steps up
+    // to A_RING + GROUPS ago have been consumed, and the slot's last but one was 2 A_RING ago.  Of the slots of
+    // codes, which change between the groups where a bias tile (steps without codes) goes by: they are waited for after the
+    // step's slot has been found free, so all steps up to A_RING ago have been consumed, with their codes, and the
+    // slot's last were Q_RING or more steps ago.
     static constexpr int GROUPS = MODE == WG_RESTORED ? 1 : MODE == WG_PANEL ? 2 : 3;
     // (WG_PANEL's restore warps read codes where they lie: no time to save, and its shared memory is full)
     static constexpr int Q_RING = MODE == WG_RESTORED ? 1 : MODE == WG_PANEL ? 2 : 6;
     static constexpr int Q_BYTES = MODE == WG_RESTORED || MODE == WG_PANEL ? 16 : 64 * 128;
     static constexpr int OUT = MODE == WG_PANEL ? 1 : 2;                     // staged pieces of a store warp
     static constexpr int THREADS = 32 * (8 + 4 * GROUPS);
-    static_assert(Q_RING % GROUPS == 0, "a slot of codes belongs to one group");
+    static_assert(GROUPS <= A_RING, "a group knows the rounds of the operands' slots");
+    static_assert(MODE == WG_RESTORED || MODE == WG_PANEL || A_RING <= Q_RING, "a group knows the rounds of the slots of codes");
 };
 constexpr int WG_DY_WARP = 0, WG_MMA_WARP = 1, WG_ALLOC_WARP = 2, WG_CODES_WARP = 3;
 constexpr int WG_STORE_WARP0 = 4;                     // 4..7: tensor-memory lanes 32 (warp % 4) ..
@@ -860,7 +865,10 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                     const Ring<WG_RING> r2(g + s + WG_GROUPS);
                     const Ring<WG_Q_RING> rq2(gq + s + WG_GROUPS);
                     ready = s + WG_GROUPS < t.steps && !bias;
-                    if (ready) ready = kb_test(kb_smem_u32(&sm.empty[r2.slot]), r2.parity ^ 1u) & kb_test(kb_smem_u32(&sm.q_full[rq2.slot]), rq2.parity);
+                    if (ready) {
+                        const bool free = kb_test(kb_smem_u32(&sm.empty[r2.slot]), r2.parity ^ 1u);      // first: see Plan
+                        ready = kb_test(kb_smem_u32(&sm.q_full[rq2.slot]), rq2.parity) & free;
+                    }
                 }
                 if (!bias) {
                     const uint8_t* q = sm.q[rq.slot] + q_at;

@@ -287,3 +287,22 @@ def test_tensors_that_a_call_writes_count_as_modified(pkg):
         z = torch.ones(2, 64, device=DEV)
         pkg.gar_activation_forward("relu", z, save_input=False, y=z)
     pkg.gar_activation_forward("relu", z, save_input=False, y=z)      # an inference tensor has no version
+
+
+# ---- rings of slots -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("tokens", [60, 128, 250, 320, 513, 700])
+@pytest.mark.parametrize("lead", [0, 1])
+def test_weight_grad_bias_tiles_between_tiles_with_codes(pkg, tokens, lead):
+    """Several tiles for every pair of CTAs, a bias tile (whose steps have no codes) after every eight, one to eleven
+    steps a tile: the slots of codes change between the groups of restore warps.  dy by TMA, and (rows that start
+    anywhere) by the restore warps."""
+    n, out, inp = 37, 200, 2000
+    dy = normal((n, tokens, out + lead), torch.bfloat16, tokens)[:, :, lead:]
+    ck = pkg.gar_checkpoint_pack(normal((n * tokens, inp), torch.bfloat16, inp), 32)
+    lengths = torch.randint(0, tokens + 1, (n,), generator=gen(tokens), device=DEV, dtype=torch.int32)
+    for lens in (None, lengths):
+        dw, db, sw, sb = products_64(pkg, dy, ck, lens)
+        w, b = weight_grads(pkg, dy, ck, torch.float32, lens, 0, False)
+        unit = max(tokens, 8) * 2.0 ** -23
+        assert torch.all((w.double() - dw).abs() <= unit * sw + 2.0 ** -24 * dw.abs())
+        assert torch.all((b.double() - db).abs() <= unit * sb + 2.0 ** -24 * db.abs())
