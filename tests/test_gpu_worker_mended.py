@@ -306,3 +306,74 @@ def test_weight_grad_bias_tiles_between_tiles_with_codes(pkg, tokens, lead):
         unit = max(tokens, 8) * 2.0 ** -23
         assert torch.all((w.double() - dw).abs() <= unit * sw + 2.0 ** -24 * dw.abs())
         assert torch.all((b.double() - db).abs() <= unit * sb + 2.0 ** -24 * db.abs())
+
+
+# ---- graphs and threads -------------------------------------------------------------------------------
+def all_calls(pkg, x, t, dy, stream=None):
+    """Every operator once, on shapes that take several paths (a small and a long vocabulary, panels, restored x, cut
+    tokens); the results."""
+    out = []
+    for z in (x[:, :50], x):
+        r = pkg.gar_token_logprobs(z, t, top=5, stream=stream)
+        out += [*r, pkg.gar_token_logprobs_backward(z, r, t, r.entropy, r.entropy, r.top_logprobs, stream=stream)]
+    f = pkg.gar_activation_forward("gelu", x, x, save_output=True, stream=stream)
+    b = pkg.gar_activation_backward("gelu", x, f.x, f.up, stream=stream)
+    rows, cols = x.shape
+    out += [q[:, :cols] for q in (f.x.q, f.up.q, f.out.q)]   # the padding of the codes is not written
+    out += [f.y, f.x.scales, f.out.scales, b.dx, b.dup, pkg.gar_checkpoint_unpack(f.out, stream=stream)]
+    for workers in (1, 2, 8):                                # 2048 and 1024 tokens cut or restored, 256: panels
+        ck = pkg.gar_checkpoint_pack(x, 64, stream=stream)
+        d = dy.view(workers, rows // workers, -1)
+        out += [pkg.gar_linear_weight_grad(d, ck, stream=stream),
+                pkg.gar_linear_weight_grad(d[:, :, :40].contiguous(), ck, grads_dtype=torch.bfloat16, stream=stream)]
+    return out
+
+
+def test_calls_in_a_graph(pkg):
+    """A captured sequence of all calls, replayed on other inputs, gives the bits of the plain calls."""
+    x, dy = normal((2048, 2056), torch.bfloat16, 1), normal((2048, 2048), torch.bfloat16, 2)
+    t = torch.randint(-1, 50, (2048,), generator=gen(3), device=DEV)
+    all_calls(pkg, x, t, dy)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = all_calls(pkg, x, t, dy)
+    for seed in (10, 20):
+        x.copy_(normal(x.shape, x.dtype, seed))
+        dy.copy_(normal(dy.shape, dy.dtype, seed + 1))
+        t.copy_(torch.randint(-1, 50, (2048,), generator=gen(seed + 2), device=DEV))
+        graph.replay()
+        want = all_calls(pkg, x, t, dy)
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(held, want)):
+            assert torch.equal(a.nan_to_num() if a.is_floating_point() else a, b.nan_to_num() if b.is_floating_point() else b), i
+
+
+def test_calls_from_two_threads(pkg):
+    """Two threads, each with inputs and a stream of its own, give the bits of one."""
+    import threading
+    data = [(normal((2048, 2056), torch.bfloat16, s), torch.randint(-1, 50, (2048,), generator=gen(s), device=DEV),
+             normal((2048, 2048), torch.bfloat16, s + 1)) for s in (1, 5)]
+    want = [all_calls(pkg, *d) for d in data]
+    torch.cuda.synchronize()
+    got, errors = [[], []], []
+
+    def work(i):
+        try:
+            side = torch.cuda.Stream()
+            with torch.cuda.stream(side):
+                for _ in range(5):
+                    got[i].append(all_calls(pkg, *data[i]))
+            side.synchronize()
+        except Exception as e:
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not errors
+    for i in range(2):
+        for run in got[i]:
+            for a, b in zip(run, want[i]):
+                assert torch.equal(a.nan_to_num() if a.is_floating_point() else a, b.nan_to_num() if b.is_floating_point() else b)
