@@ -1,7 +1,7 @@
 // Argument marshalling between torch tensors and the worker-side C ABI (gar_worker.h), as a CPython
 // module: a call allocates its outputs, fills the parameter block and enqueues on the current stream
 // in a few microseconds, which is what the small calls are bound by (the same in Python with ctypes
-// took 15 to 35).  Nothing is computed here.  Every function returns its tensors, or the
+// took 16 to 25).  Nothing is computed here.  Every function returns its tensors, or the
 // gar_status_t of a refused call as an int.
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>

@@ -5,8 +5,8 @@
 // arranged to stay below the issue rate: rounding through the 1.5 * 2^23 constant instead of
 // conversions, codes packed by byte permutes, maxima of two inputs in one register, two tasks per
 // thread with all loads first.  Measured (bf16, group 128): gated SiLU 8192 x 8192 forward 96 us =
-// 5.6 TB/s and backward 80 us = 6.8 TB/s under the profiler (its output partly still in L2), 185 us
-// together; pack and unpack 8192 x 4096 41 us, of which the pack 25: 158 instructions per eight
+// 5.6 TB/s and backward 80 us = 6.8 TB/s under the profiler (its output partly still in L2), 186 to 192 us
+// together; GELU alone 76 us forward, 60 backward; pack and unpack 8192 x 4096 41 us, of which the pack 25: 158 instructions per eight
 // columns of a warp, 81 % of the issue slots.
 #include "worker_common.cuh"
 
@@ -222,6 +222,8 @@ __device__ __forceinline__ float rcp(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// Off by 4e-7 of itself (both functions are approximate to 2^-22) and, for negative x, 1e-7 |x| (the rounded product in
+// the exponent): less than what 16-bit results round off.
 __device__ __forceinline__ float sigmoid(float x) { return rcp(1.f + ex2(-x * kLog2e)); }
 
 // The normal distribution at two places: cdf = P(X < x) and the density's e^(-x^2 / 2).  The tail behind |x| is

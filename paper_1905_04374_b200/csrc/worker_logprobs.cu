@@ -446,7 +446,7 @@ __device__ __forceinline__ void add_tile(const uint4 (&raw)[LP_UNROLL], float ce
 
 // Per entry one exponential (of 16 a cycle and SM; the memory's rate asks for 11.6 entries of 16 bits) and
 // five instructions.  The next turn's loads are in flight while a turn is worked on.  Measured: 4096 x
-// 131072 bf16 200 us without alternatives, 235 with 20 (1.07 GB: 5.4 and 4.6 TB/s, copy peak 6.5;
+// 131072 bf16 200 us without alternatives, 233 to 244 with 20 (1.07 GB: 5.4 and 4.5 TB/s, copy peak 6.5;
 // under the profiler issue slots 67 % busy, exponential unit 60 %), fp32 170 us for
 // 2048 x 131072 (6.3 TB/s).  The alternatives cost the row's end: two barriers, a second read of some 40
 // tiles, 10 % more DRAM traffic; it hides behind the other rows of the SM, which is why a row gets a warp up

@@ -29,12 +29,12 @@
 // into parts, joined in order by a second kernel, where there are too few tiles for the SMs.
 //
 // What bounds it (B200, 1 kW cap).  Long batches: power.  4 workers x 8192
-// tokens, 4096 x 4096: 1.00 to 1.05 ms = 1.05 to 1.1 PFLOP/s with the pass that restores x' (61 us of it),
-// 0.84 ms = 1.31 PFLOP/s for this kernel alone before the cap lowers the clock to 1.2 GHz; the library's bf16
-// product alone takes 0.79 to 0.87 ms.  Short batches: the rows of the block, 11 x 512 tokens: 0.26 ms
-// for 738 MB of fp32 rows (0.11 ms at the copy's rate; bf16 rows take 58 us less, just the time of the
-// 369 MB they save, so the stores do not hide), 11 x 128: 0.146 ms.  Small layers: latency, 7 x 100
-// tokens, 500 x 800 with bias: 14 us.
+// tokens, 4096 x 4096: 1.04 to 1.07 ms = 1.03 to 1.06 PFLOP/s for bf16 rows with the pass that restores x' (61 us of
+// it), 1.09 to 1.11 ms for fp32 rows; 0.86 ms = 1.28 PFLOP/s for this kernel alone, bf16 rows, before the cap lowers
+// the clock to 1.2 GHz; the library's bf16 product alone takes 0.79 to 0.87 ms.  Short batches: the rows of
+// the block, 11 x 512 tokens: 0.26 to 0.27 ms for 738 MB of fp32 rows (0.11 ms at the copy's rate; bf16 rows take
+// 58 to 62 us less, about the time of the 369 MB they save, so the stores do not hide), 11 x 128: 0.142 to 0.157 ms.
+// Small layers: latency, 7 x 100 tokens, 500 x 800 with bias: 16 us.
 //
 // Hand-offs are mbarriers; every wait is bounded: a wait that gives up raises an error flag, all
 // roles leave their loops once what they have in flight has landed, and the CTA's tiles become NaN.
@@ -66,8 +66,8 @@ constexpr int WG_PANEL_STEPS = 8;                     // 512 tokens
 // Steps per accumulator.  The tensor core truncates what it adds to an accumulator: the sum loses 1e-9 of itself per
 // token, up to 2.8e-9 where it grows steadily (measured: 4.4e-6 at 4096 random tokens, 5.6e-6 at 2048 positive ones;
 // rounded additions lose a tenth).  Sums are therefore taken in chunks, joined by rounded additions in tensor memory, so
-// that the loss has a bound however many tokens there are: 768 tokens for fp32 results (7e-7, growing sums 1.5e-6), 2048
-// for 16-bit ones (2e-6 and 5.6e-6, a fortieth of binary16's rounding).  A join holds the products up for 2000 cycles:
+// that the loss has a bound however many tokens there are: 768 tokens for fp32 results (7e-7, growing sums 1.3e-6), 2048
+// for 16-bit ones (growing sums 6e-6, a fortieth of binary16's rounding; the same at 32768 tokens).  A join holds the products up for 2000 cycles:
 // 16-bit results at 768 tokens a chunk took 3 % longer with x restored beforehand and 10 to 13 % without.
 template <typename G> struct Chunk { static constexpr int STEPS = sizeof(G) == 4 ? 12 : 32; };
 template <int MODE> struct Plan {
@@ -516,9 +516,9 @@ __device__ __noinline__ unsigned store_aligned(unsigned src, bool filled, unsign
 // apart: each is moved up by what its start lies behind a multiple of 32 bytes, the words that move out of a piece
 // are the next one's first, and what is written are whole aligned 16-byte chunks but for the row's ends.  Not
 // inlined: its registers are no burden on the other paths.  Bound by the warp's own instructions, 1600 cycles a piece.
-// Measured against single elements from the staging buffer (odd row length): 11 x 512 tokens, 4096 x 4096: fp32 414 ->
-// 343 us (TMA stores, where rows start on 16 bytes: 261), bf16 546 -> 293 (208); 4 x 4096, 2048 x 2048, fp32 505 -> 212
-// (190); 11 x 128, 2048 x 2048, fp32 107 -> 74 (42).  A row's ends by the row's lane, or by eight lanes per row in a loop
+// Measured (odd row length; in brackets TMA stores, where rows start on 16 bytes): 11 x 512 tokens, 4096 x 4096: fp32
+// 327 to 331 us (261 to 265), bf16 274 to 277 (199 to 205), by single elements from the staging buffer 414 and 546; 4 x
+// 4096, 2048 x 2048, fp32 166 to 169 (163 to 166); 11 x 128, 2048 x 2048, fp32 70 (43).  A row's ends by the row's lane, or by eight lanes per row in a loop
 // of their own, were slower (90 and 99 us for the last).
 template <typename G>
 __device__ __noinline__ void store_anywhere(unsigned src, bool filled, unsigned stage, char* first, int64_t row_bytes, int bytes, int rows) {
@@ -1098,7 +1098,7 @@ bool panel_applies(const gar_weight_grad_params_t& p, int64_t ld_dy) {
 
 // With few output tiles and many tokens the tokens are cut, so that every pair of SMs has a part, of four
 // steps at least (a step takes a pair 0.6 to 2 us when no other tile hides its latencies, the join 4 us in
-// all).  One worker, 4000 tokens, 200 x 300: 50 -> 18 us; 2 x 4096 tokens, 513 x 250: 151 -> 29 us.
+// all).  One worker, 4000 tokens, 200 x 300: 17 us, whole 47; 2 x 4096 tokens, 513 x 250: 29 us, whole 115.
 // A panel's tokens stay whole (WG_PANEL's tiles know no parts).
 constexpr int WG_PAIRS = 74;
 int splits_of(const gar_weight_grad_params_t& p, int64_t ld_dy) {
@@ -1204,10 +1204,12 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
            : p.grads_dtype == GAR_BF16 ? join_parts<__nv_bfloat16>(a, p, stream) : join_parts<__half>(a, p, stream);
 }
 
-// Every 256 outputs restore the activation once more.  Measured (8 workers, 2048 tokens, 4096 inputs): with a
-// workspace 292 us against 286 at 2048 outputs, 1007 against 1104 at 4 x 8192 tokens and 4096 outputs; fp32 sums
-// of several chunks, which leave the tile's rounds less slack, 158 against 166 at 768 outputs; dy copied to
-// aligned rows on the way 42 against 58 at 1023 outputs, 19 against 13 at 500.
+// Every 256 outputs restore the activation once more.  Measured, with a workspace against without (8 workers, 2048
+// tokens, 4096 inputs): bf16 results 144 us against 126 at 768 outputs, 234 against 233 at 1536, 290 against 299 at
+// 2048, 1045 against 1150 at 4 x 8192 tokens and 4096 outputs; fp32 results, whose chunks are joined more often, which
+// holds the restore warps up, 116 against 105 at 512, 155 against 153 at 768, 181 against 189 at 1024, 316 against 366
+// at 2048.  dy copied to aligned rows on the way (fp32 results): 191 against 382 at 1023 outputs, 125 against 253 at 499,
+// where the rule, which looks at no other size, does without; 7 x 100 tokens, 500 x 800 19 against 13.
 bool weight_grad_wants_workspace(const gar_weight_grad_params_t& p, int64_t ld_dy) {
     if (splits_of(p, ld_dy) > 1) return true;
     if (panel_applies(p, ld_dy)) return false;

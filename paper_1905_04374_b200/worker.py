@@ -5,7 +5,8 @@ stride and any row stride that keeps the rows apart (an expanded tensor, whose r
 refused: make it contiguous); outputs are allocated, unless given, on the stream the call runs on.
 There is no autograd: results carry no gradient function whatever the inputs require, and the gradient of
 a call is the call that computes it.  Tensors that a call writes (y=, dx=, dup=, dlogits=, out=, grads)
-count as modified in place, so autograd refuses a backward pass that saved one of them.  The marshalling
+count as modified in place, so autograd refuses a backward pass that saved one of them.  With stream= the
+inputs have to stay alive until that stream has read them.  The marshalling
 itself is compiled (csrc/worker_binding.cpp); the ctypes mirrors of the parameter blocks are for
 callers of the C ABI.  Nothing is computed here and there is no fallback.
 """
@@ -221,7 +222,9 @@ def gar_linear_weight_grad(dy: torch.Tensor, x: Checkpoint, grads: Optional[torc
     weight_offset on and, with bias_offset, db_w from there on.  lengths int32 [workers]: tokens that
     count.  Without `grads` a block [workers, out * in] of grads_dtype is made.  workspace: None lets the
     call allocate one for layers where it is faster, False never (the codes are then restored tile by
-    tile), or a uint8 CUDA tensor of gar_weight_grad_workspace_bytes."""
+    tile), or a uint8 CUDA tensor of gar_weight_grad_workspace_bytes.  That is room for the activation restored
+    to 16 bits, twice the checkpoint (and for a copy of dy if its rows do not start on 16 bytes), or for the parts
+    of a sum of many tokens: False where memory is shorter than time."""
     if dy.dtype != x.dtype:
         raise TypeError("dy and the checkpoint must be of one type")
     if dy.dim() != 3:
