@@ -88,7 +88,7 @@ int gar_token_logprobs_backward(const gar_logprobs_grad_params_t* params);
  * share one fp32 scale; with A the largest magnitude of the group
  *     scale = A / 127,   q = rint(x * ((1 / A) * 127))   (int8, ties to even, each step rounded to fp32),
  * and a restored value is q * scale rounded once to the activation's element type, at most half a
- * step (plus that rounding) from the original.  (The scale is at most the largest number that 127 can be
+ * step (and 2e-5 of one for the two roundings of q, plus that rounding) from the original.  (The scale is at most the largest number that 127 can be
  * multiplied with: A / 127 of the largest finite fp32 value, a mask, say, would be restored as infinity.)
  * A group with A < 2^-100 is stored as zeros; a
  * group that holds a NaN or an infinity gets scale NaN and is restored as NaN throughout.
