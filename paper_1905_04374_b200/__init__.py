@@ -1,8 +1,8 @@
 """B200-native gradient aggregation rules (averaging, median, Krum, multi-Krum,
-Bulyan, multi-Bulyan) behind the C ABI of include/gar.h, and the operators a worker
-runs before its gradient is aggregated (include/gar_worker.h).
+Bulyan, multi-Bulyan) behind the C ABI of include/gar.h, the operators a worker
+runs before its gradient is aggregated (include/gar_worker.h), and a worker's layers (include/gar_linear.h).
 
-`binding` and `worker` marshal torch tensors into the C calls; `workloads` draws the seeded
+`binding`, `worker` and `linear` marshal torch tensors into the C calls; `workloads` draws the seeded
 synthetic inputs; `build` compiles libgar.so.  All arithmetic runs in the CUDA
 kernels of csrc/.
 """
@@ -17,4 +17,10 @@ from .worker import (  # noqa: F401
     ACTIVATIONS, GAR_MAX_TOP, Activation, ActivationGrad, Checkpoint, GarActivationGradParams, GarActivationParams, GarCheckpoint,
     GarLogprobsGradParams, GarLogprobsParams, GarWeightGradParams, TokenLogprobs, gar_activation_backward, gar_activation_forward,
     gar_checkpoint_pack, gar_checkpoint_unpack, gar_linear_weight_grad, gar_weight_grad_workspace_bytes, gar_token_logprobs, gar_token_logprobs_backward,
+)
+from .linear import (  # noqa: F401
+    GarDropoutParams, GarGatedLinearGradParams, GarGatedLinearParams, GarLinearLogprobsGradParams, GarLinearLogprobsParams, GatedLinearGrad,
+    LinearLogprobs, gar_dropout, gar_gated_linear_backward, gar_gated_linear_backward_workspace_bytes, gar_gated_linear_forward,
+    gar_gated_linear_workspace_bytes, gar_linear_logprobs, gar_linear_logprobs_backward, gar_linear_logprobs_backward_workspace_bytes,
+    gar_linear_logprobs_workspace_bytes,
 )

@@ -34,7 +34,7 @@ def _units():
              ("k2_select.cu", "k2_select.o", []),
              ("k3_dispatch.cu", "k3_dispatch.o", []),
              ("gar_api.cu", "gar_api.o", [])]
-    for name in ("logprobs", "checkpoint", "wgrad", "api"):
+    for name in ("logprobs", "checkpoint", "wgrad", "linear", "dropout", "api", "linear_api"):
         units.append((f"worker_{name}.cu", f"worker_{name}.o", []))
     for p in K3_P:
         units.append(("k3_inst.cu", f"k3_inst_{p}.o", [f"-DK3_P={p}", f"-DK3_EXACT={1 if p <= 32 else 0}"]))
@@ -47,7 +47,7 @@ def _newest_header(worker: bool) -> float:
             if f.endswith((".cuh", ".h")) and (worker or not f.startswith("worker_"))]
     hdrs.append(os.path.join(ROOT, "include", "gar.h"))
     if worker:
-        hdrs.append(os.path.join(ROOT, "include", "gar_worker.h"))
+        hdrs += [os.path.join(ROOT, "include", name) for name in ("gar_worker.h", "gar_linear.h")]
     hdrs.append(os.path.abspath(__file__))
     return max(os.path.getmtime(h) for h in hdrs)
 
@@ -83,7 +83,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
 def _build_worker_module(run, force: bool) -> None:
     """Compile the tensor marshalling of the worker-side operators against the installed torch."""
     src = os.path.join(CSRC, "worker_binding.cpp")
-    deps = [src, os.path.join(ROOT, "include", "gar.h"), os.path.join(ROOT, "include", "gar_worker.h"), os.path.abspath(__file__)]
+    deps = [src, os.path.join(ROOT, "include", "gar.h"), os.path.join(ROOT, "include", "gar_worker.h"), os.path.join(ROOT, "include", "gar_linear.h"), os.path.abspath(__file__)]
     if not force and os.path.exists(WORKER_MODULE) and os.path.getmtime(WORKER_MODULE) >= max(map(os.path.getmtime, deps)):
         return
     import sysconfig

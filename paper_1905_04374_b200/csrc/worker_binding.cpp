@@ -1,4 +1,4 @@
-// Argument marshalling between torch tensors and the worker-side C ABI (gar_worker.h), as a CPython
+// Argument marshalling between torch tensors and the worker-side C ABI (gar_worker.h, gar_linear.h), as a CPython
 // module: a call allocates its outputs, fills the parameter block and enqueues on the current stream
 // in a few microseconds, which is what the small calls are bound by (the same in Python with ctypes
 // took 16 to 25).  Nothing is computed here.  Every function returns its tensors, or the
@@ -12,6 +12,7 @@
 
 #include <algorithm>
 
+#include "gar_linear.h"
 #include "gar_worker.h"
 
 namespace {
@@ -408,10 +409,240 @@ PyObject* linear_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- a worker's layers (gar_linear.h) ---------------------------------------------------------------
+uint64_t unsigned_integer(PyObject* o) {
+    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    if (v == static_cast<unsigned long long>(-1) && PyErr_Occurred()) throw python_error();
+    return v;
+}
+// a matrix of the type and on the device of another, with the given shape
+Matrix matrix_of(const Tensor& t, const char* name, const Tensor& like, int64_t rows, int64_t cols) {
+    TORCH_CHECK_TYPE(t.is_cuda() && t.scalar_type() == like.scalar_type(), name, " must be a CUDA tensor of type ", like.scalar_type());
+    TORCH_CHECK_VALUE(t.device() == like.device(), name, " must sit on ", like.device());
+    TORCH_CHECK_VALUE(t.dim() == 2 && t.size(0) == rows && t.size(1) == cols, name, " must have shape [", rows, ", ", cols, "]");
+    return matrix(t, name);
+}
+// an operand of a product: two dimensions, as many columns as another
+Matrix weights(const Tensor& t, const char* name, const Tensor& x, int64_t hidden) {
+    TORCH_CHECK_VALUE(t.dim() == 2 && t.size(1) == hidden, name, " must be 2-D with ", hidden, " columns");
+    return matrix_of(t, name, x, t.size(0), hidden);
+}
+const void* bias_of(PyObject* o, const char* name, const Tensor& x, int64_t n) {
+    return given(o) ? vector<void>(tensor(o, name), name, x.scalar_type(), n, x.device()) : nullptr;
+}
+// The workspace of a call: the caller's tensor, or one allocated for the call on its stream.
+Tensor space_for(PyObject* o, size_t bytes, at::Device dev, void** p, size_t* have) {
+    Tensor t;
+    if (given(o)) {
+        t = tensor(o, "workspace");
+        TORCH_CHECK_TYPE(t.is_cuda() && t.device() == dev && t.is_contiguous(), "workspace must be a contiguous tensor on ", dev);
+    } else if (bytes > 0) {
+        t = empty({int64_t(bytes)}, at::kByte, dev);
+    }
+    if (t.defined() && t.numel() > 0) {
+        *p = t.data_ptr();
+        *have = size_t(t.numel()) * t.element_size();
+    }
+    return t;
+}
+
+PyObject* linear_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {    // x, weight, targets, bias, workspace, stream
+    HANDLE_TH_ERRORS
+    need(n, 6);
+    const Tensor& x = tensor(a[0], "x");
+    const Matrix m = matrix(x, "x"), w = weights(tensor(a[1], "weight"), "weight", x, m.cols);
+    const at::Device dev = x.device();
+    const Place place(dev, a[5]);
+    gar_linear_logprobs_params_t p{};
+    p.dtype = m.dtype; p.rows = m.rows; p.hidden = m.cols; p.vocab = w.rows;
+    p.x = m.p; p.ldx = m.ld; p.weight = w.p; p.ldw = w.ld;
+    p.bias = bias_of(a[3], "bias", x, w.rows);
+    Together t(dev);
+    const int64_t at_lse = t.reserve(m.rows, at::kFloat), at_lo = t.reserve(m.rows, at::kFloat), at_lp = t.reserve(given(a[2]) ? m.rows : 0, at::kFloat);
+    t.allocate();
+    const Tensor lse = t.view(at_lse, {m.rows}, at::kFloat), lse_lo = t.view(at_lo, {m.rows}, at::kFloat);
+    p.lse = pointer<float>(lse); p.lse_lo = pointer<float>(lse_lo);
+    Tensor logprobs;
+    if (given(a[2])) {
+        p.targets = vector<int64_t>(tensor(a[2], "targets"), "targets", at::kLong, m.rows, dev);
+        logprobs = t.view(at_lp, {m.rows}, at::kFloat);
+        p.logprobs = pointer<float>(logprobs);
+    }
+    const Tensor space = space_for(a[4], gar_linear_logprobs_workspace_bytes(&p), dev, &p.workspace, &p.workspace_bytes);
+    p.stream = place.stream();
+    if (const int st = gar_linear_logprobs(&p)) return status(st);
+    return tuple_of({logprobs, lse, lse_lo});
+    END_HANDLE_TH_ERRORS
+}
+
+// x, weight, lse, lse_lo, targets, grad_logprobs, bias, grads, weight_offset, bias_offset (-1: none), dx (tensor, True: allocate
+// it, False: none), workspace, stream
+PyObject* linear_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 13);
+    const Tensor& x = tensor(a[0], "x");
+    const Matrix m = matrix(x, "x"), w = weights(tensor(a[1], "weight"), "weight", x, m.cols);
+    const at::Device dev = x.device();
+    const Place place(dev, a[12]);
+    gar_linear_logprobs_grad_params_t p{};
+    p.dtype = m.dtype; p.hidden = m.cols; p.vocab = w.rows;
+    p.workers = 1; p.tokens = m.rows;
+    p.x = m.p; p.ldx = m.ld; p.weight = w.p; p.ldw = w.ld;
+    p.bias = bias_of(a[6], "bias", x, w.rows);
+    p.lse = vector<float>(tensor(a[2], "saved.lse"), "saved.lse", at::kFloat, m.rows, dev);
+    if (given(a[3])) p.lse_lo = vector<float>(tensor(a[3], "saved.lse_lo"), "saved.lse_lo", at::kFloat, m.rows, dev);
+    p.targets = vector<int64_t>(tensor(a[4], "targets"), "targets", at::kLong, m.rows, dev);
+    p.grad_logprobs = vector<float>(tensor(a[5], "grad_logprobs"), "grad_logprobs", at::kFloat, m.rows, dev);
+    if (given(a[7])) {
+        const Tensor& grads = tensor(a[7], "grads");
+        const int64_t at_w = integer(a[8]), at_b = integer(a[9]);
+        const Matrix g = matrix(grads, "grads");
+        TORCH_CHECK_VALUE(grads.device() == dev, "grads must sit on ", dev);
+        TORCH_CHECK_VALUE(g.rows >= 1 && g.rows <= GAR_MAX_N && m.rows % g.rows == 0, "grads must have a row for each of 1 to ", GAR_MAX_N,
+                          " workers, with equally many rows of x");
+        TORCH_CHECK_VALUE(at_w >= 0 && at_w + w.rows * m.cols <= g.cols, "grads has no room for the weights at weight_offset");
+        TORCH_CHECK_VALUE(at_b < 0 || at_b + w.rows <= g.cols, "grads has no room for the bias at bias_offset");
+        p.grads_dtype = g.dtype;
+        p.workers = int(g.rows);
+        p.tokens = m.rows / g.rows;
+        char* base = static_cast<char*>(g.p);
+        p.weight_grads = base + at_w * grads.element_size();
+        p.bias_grads = at_b >= 0 ? base + at_b * grads.element_size() : nullptr;
+        p.ld_grads = g.ld;
+    }
+    Tensor dx;
+    if (a[10] != Py_False) {
+        dx = a[10] == Py_True ? empty({m.rows, m.cols}, x.scalar_type(), dev) : tensor(a[10], "dx");
+        const Matrix d = matrix_like(dx, "dx", x);
+        p.dx = d.p; p.lddx = d.ld;
+    }
+    const Tensor space = space_for(a[11], gar_linear_logprobs_backward_workspace_bytes(&p), dev, &p.workspace, &p.workspace_bytes);
+    p.stream = place.stream();
+    if (const int st = gar_linear_logprobs_backward(&p)) return status(st);
+    written(a[7]);
+    if (a[10] != Py_True && a[10] != Py_False) written(a[10]);
+    return tuple_of({dx});
+    END_HANDLE_TH_ERRORS
+}
+
+// act, x, w_gate, w_up, b_gate, b_up, group, save_input, save_output, y, workspace, stream -> y and the codes and scales of gate, up, y
+PyObject* gated_linear_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 12);
+    const Tensor& x = tensor(a[1], "x");
+    const Matrix m = matrix(x, "x"), wg = weights(tensor(a[2], "w_gate"), "w_gate", x, m.cols);
+    const int64_t inner = wg.rows;
+    const Matrix wu = matrix_of(tensor(a[3], "w_up"), "w_up", x, inner, m.cols);
+    const at::Device dev = x.device();
+    const Place place(dev, a[11]);
+    gar_gated_linear_params_t p{};
+    p.act = int(integer(a[0])); p.group = int(integer(a[6]));
+    p.dtype = m.dtype; p.rows = m.rows; p.hidden = m.cols; p.inner = inner;
+    p.x = m.p; p.ldx = m.ld; p.w_gate = wg.p; p.ld_gate = wg.ld; p.w_up = wu.p; p.ld_up = wu.ld;
+    p.b_gate = bias_of(a[4], "b_gate", x, inner);
+    p.b_up = bias_of(a[5], "b_up", x, inner);
+    const Tensor y = given(a[9]) ? tensor(a[9], "y") : empty({m.rows, inner}, x.scalar_type(), dev);
+    const Matrix my = matrix_of(y, "y", x, m.rows, inner);
+    p.y = my.p; p.ldy = my.ld;
+    Held hg, hu, hy;
+    if (integer(a[7])) {
+        hg = new_held(m.rows, inner, p.group, x);
+        hu = new_held(m.rows, inner, p.group, x);
+        p.gate_saved = saved(hg.q, hg.scales, "gate", m.rows, inner, p.group, dev);
+        p.up_saved = saved(hu.q, hu.scales, "up", m.rows, inner, p.group, dev);
+    }
+    if (integer(a[8])) {
+        hy = new_held(m.rows, inner, p.group, x);
+        p.y_saved = saved(hy.q, hy.scales, "out", m.rows, inner, p.group, dev);
+    }
+    const Tensor space = space_for(a[10], gar_gated_linear_workspace_bytes(&p), dev, &p.workspace, &p.workspace_bytes);
+    p.stream = place.stream();
+    if (const int st = gar_gated_linear_forward(&p)) return status(st);
+    written(a[9]);
+    return tuple_of({y, hg.q, hg.scales, hu.q, hu.scales, hy.q, hy.scales});
+    END_HANDLE_TH_ERRORS
+}
+
+// A matrix whose rows start on 16 bytes, as gar_linear_weight_grad reads it fastest.
+Tensor padded(int64_t rows, int64_t cols, const Tensor& like) {
+    const int64_t ld = (cols + 7) / 8 * 8;
+    Tensor t = empty({rows, ld}, like.scalar_type(), like.device());
+    if (ld != cols) t.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef({rows, cols}), at::IntArrayRef({ld, 1}));
+    return t;
+}
+
+// act, dy, gate.q, gate.scales, up.q, up.scales, inner, group, w_gate, w_up, dx (tensor, True: allocate it, False: none), dgate, dup, workspace, stream
+PyObject* gated_linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 15);
+    const Tensor& dy = tensor(a[1], "dy");
+    const Matrix m = matrix(dy, "dy");
+    const at::Device dev = dy.device();
+    const Place place(dev, a[14]);
+    TORCH_CHECK_VALUE(integer(a[6]) == m.cols, "the checkpoints do not hold [", m.rows, ", ", m.cols, "]");
+    const Tensor& wgt = tensor(a[8], "w_gate");
+    TORCH_CHECK_VALUE(wgt.dim() == 2, "w_gate must be 2-D");
+    const int64_t hidden = wgt.size(1);
+    const Matrix wg = matrix_of(wgt, "w_gate", dy, m.cols, hidden), wu = matrix_of(tensor(a[9], "w_up"), "w_up", dy, m.cols, hidden);
+    gar_gated_linear_grad_params_t p{};
+    p.act = int(integer(a[0])); p.group = int(integer(a[7]));
+    p.dtype = m.dtype; p.rows = m.rows; p.hidden = hidden; p.inner = m.cols; p.dy = m.p; p.lddy = m.ld;
+    p.gate_saved = saved(tensor(a[2], "gate.q"), tensor(a[3], "gate.scales"), "gate", m.rows, m.cols, p.group, dev);
+    p.up_saved = saved(tensor(a[4], "up.q"), tensor(a[5], "up.scales"), "up", m.rows, m.cols, p.group, dev);
+    p.w_gate = wg.p; p.ld_gate = wg.ld; p.w_up = wu.p; p.ld_up = wu.ld;
+    const Tensor dgate = given(a[11]) ? tensor(a[11], "dgate") : padded(m.rows, m.cols, dy), dup = given(a[12]) ? tensor(a[12], "dup") : padded(m.rows, m.cols, dy);
+    const Matrix mg = matrix_like(dgate, "dgate", dy), mu = matrix_like(dup, "dup", dy);
+    p.dgate = mg.p; p.ld_dgate = mg.ld; p.dup = mu.p; p.ld_dup = mu.ld;
+    Tensor dx;
+    if (a[10] != Py_False) {
+        dx = a[10] == Py_True ? empty({m.rows, hidden}, dy.scalar_type(), dev) : tensor(a[10], "dx");
+        const Matrix d = matrix_of(dx, "dx", dy, m.rows, hidden);
+        p.dx = d.p; p.lddx = d.ld;
+    }
+    const Tensor space = space_for(a[13], gar_gated_linear_backward_workspace_bytes(&p), dev, &p.workspace, &p.workspace_bytes);
+    p.stream = place.stream();
+    if (const int st = gar_gated_linear_backward(&p)) return status(st);
+    if (a[10] != Py_True && a[10] != Py_False) written(a[10]);
+    written(a[11]);
+    written(a[12]);
+    return tuple_of({dx, dgate, dup});
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {            // x, p, seed, offset, residual, y, counter, stream
+    HANDLE_TH_ERRORS
+    need(n, 8);
+    const Tensor& x = tensor(a[0], "x");
+    const Matrix m = matrix(x, "x");
+    const at::Device dev = x.device();
+    const Place place(dev, a[7]);
+    gar_dropout_params_t p{};
+    p.dtype = m.dtype; p.rows = m.rows; p.cols = m.cols; p.x = m.p; p.ldx = m.ld;
+    const double probability = PyFloat_AsDouble(a[1]);
+    if (probability == -1.0 && PyErr_Occurred()) throw python_error();
+    p.p = float(probability);
+    p.seed = unsigned_integer(a[2]); p.offset = unsigned_integer(a[3]);
+    if (given(a[4])) {
+        const Matrix r = matrix_like(tensor(a[4], "residual"), "residual", x);
+        p.residual = r.p; p.ld_residual = r.ld;
+    }
+    const Tensor y = given(a[5]) ? tensor(a[5], "y") : empty({m.rows, m.cols}, x.scalar_type(), dev);
+    const Matrix my = matrix_like(y, "y", x);
+    p.y = my.p; p.ldy = my.ld;
+    if (given(a[6])) p.counter = vector<uint64_t>(tensor(a[6], "counter"), "counter", at::kLong, 1, dev);
+    p.stream = place.stream();
+    if (const int st = gar_dropout(&p)) return status(st);
+    written(a[5]);
+    return THPVariable_Wrap(y);
+    END_HANDLE_TH_ERRORS
+}
+
 #define GAR_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {GAR_METHOD(token_logprobs), GAR_METHOD(token_logprobs_backward), GAR_METHOD(checkpoint_pack),
                          GAR_METHOD(checkpoint_unpack), GAR_METHOD(activation_forward), GAR_METHOD(activation_backward),
-                         GAR_METHOD(weight_grad_workspace_bytes), GAR_METHOD(linear_weight_grad), {nullptr, nullptr, 0, nullptr}};
+                         GAR_METHOD(weight_grad_workspace_bytes), GAR_METHOD(linear_weight_grad), GAR_METHOD(linear_logprobs),
+                         GAR_METHOD(linear_logprobs_backward), GAR_METHOD(gated_linear_forward), GAR_METHOD(gated_linear_backward),
+                         GAR_METHOD(dropout), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_gar_worker", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

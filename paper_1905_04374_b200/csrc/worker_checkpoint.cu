@@ -8,6 +8,7 @@
 // 5.6 TB/s and backward 80 us = 6.8 TB/s under the profiler (its output partly still in L2), 186 to 192 us
 // together; GELU alone 76 us forward, 60 backward; pack and unpack 8192 x 4096 41 us, of which the pack 25: 158 instructions per eight
 // columns of a warp, 81 % of the issue slots.
+#include "worker_act.cuh"
 #include "worker_common.cuh"
 
 namespace gar {
@@ -16,8 +17,6 @@ namespace {
 
 constexpr int CK_THREADS = 256;
 constexpr int CK_TASKS = 2;                            // per thread: all loads before the arithmetic
-constexpr float CK_TINY = 7.888609052210118e-31f;     // 2^-100
-constexpr float CK_LARGEST = 2.6793884e+36f;           // the largest scale whose 127-fold is finite in fp32
 
 // Division of a task number by the tasks per row: exact for numerators below 2^31.
 struct FastDiv {
@@ -168,25 +167,10 @@ __device__ __forceinline__ float magnitude(unsigned bits) {
 template <int LAYOUT>
 __device__ __forceinline__ void save8(const float (&v)[8], float top, int count, bool leader, int8_t* q, float* scale) {
     if (count <= 0) return;
-    const bool sound = top <= 3.402823466e38f, live = sound && top >= CK_TINY;
-    const float inv = live ? __fmul_rn(__frcp_rn(top), 127.f) : 0.f;
-    if (leader) {
-        // top / 127, correctly rounded: Markstein's correction of the product with the rounded reciprocal
-        const float y = 1.f / 127.f, q0 = __fmul_rn(top, y);
-        const float s = fminf(__fmaf_rn(__fmaf_rn(-127.f, q0, top), y, q0), CK_LARGEST);
-        *scale = !sound ? CUDART_NAN_F : live ? s : 0.f;
-    }
-    // |v inv| <= 127 (1 + 2^-22): the low byte of the sum with 1.5 * 2^23 is the nearest integer, ties to even
-    // (the products one by one: as a pair, product and sum were contracted to one rounding)
-    const f32x2 magic = pack2(12582912.f, 12582912.f);
-    float r[8];
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) unpack2(add2(pack2(__fmul_rn(v[i], inv), __fmul_rn(v[i + 1], inv)), magic), r[i], r[i + 1]);
-    unsigned lo = __byte_perm(__byte_perm(__float_as_uint(r[0]), __float_as_uint(r[1]), 0x0040),
-                              __byte_perm(__float_as_uint(r[2]), __float_as_uint(r[3]), 0x0040), 0x5410);
-    unsigned hi = __byte_perm(__byte_perm(__float_as_uint(r[4]), __float_as_uint(r[5]), 0x0040),
-                              __byte_perm(__float_as_uint(r[6]), __float_as_uint(r[7]), 0x0040), 0x5410);
-    if (!sound) lo = hi = 0u;
+    const Step step(top);
+    if (leader) *scale = step.scale(top);
+    unsigned lo, hi;
+    codes8(v, step, lo, hi);
     if (count == 8) {
         __stcs(reinterpret_cast<uint2*>(q), make_uint2(lo, hi));
     } else if (LAYOUT != CK_DENSE) {
@@ -217,53 +201,6 @@ __device__ __forceinline__ Raw8<T> restore8(const uint2& codes, float scale) {
     return narrow8<T>(v);
 }
 
-__device__ __forceinline__ float rcp(float x) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-// Off by 4e-7 of itself (both functions are approximate to 2^-22) and, for negative x, 1e-7 |x| (the rounded product in
-// the exponent): less than what 16-bit results round off.
-__device__ __forceinline__ float sigmoid(float x) { return rcp(1.f + ex2(-x * kLog2e)); }
-
-// The normal distribution at two places: cdf = P(X < x) and the density's e^(-x^2 / 2).  The tail behind |x| is
-//     e^(-x^2 / 2) t P(t),   t = 1 / (1 + 0.275 |x|)
-// (the form of Abramowitz and Stegun 26.2.17), P of degree 8 fitted to e^(x^2 / 2) erfc(x / sqrt 2) / 2 t: 2.8e-7 of the
-// tail at most, in fp32 1e-6 down to -4 and 2e-6 at -6, where the exponent's rounding shows.  (1 + erf(x / sqrt 2)) / 2
-// cancels for negative x: 4 % off at -5, 0 from -5.5 on.  bf16 8192 x 8192, forward and backward: 76 and 60 us; with
-// erff 105 and 95 us, with erfcf 143 and 131.
-__device__ __forceinline__ void normal2(float x0, float x1, float (&cdf)[2], float (&e)[2]) {
-    const float t0 = rcp(fmaf(fabsf(x0), 0.275f, 1.f)), t1 = rcp(fmaf(fabsf(x1), 0.275f, 1.f));
-    const f32x2 t = pack2(t0, t1), x = pack2(x0, x1), c = pack2(-0.5f * kLog2e, -0.5f * kLog2e);
-    unpack2(mul2(mul2(x, x), c), e[0], e[1]);
-    e[0] = ex2(e[0]);
-    e[1] = ex2(e[1]);
-    f32x2 p = pack2(0.0237322034f, 0.0237322034f);
-    constexpr float P[8] = {-0.0965348071f, 0.106157018f, -0.0134071806f, 0.0766527223f, 0.0823775453f, 0.101610145f, 0.10970306f, 0.109709157f};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p = fma2(p, t, pack2(P[i], P[i]));
-    float tail0, tail1;
-    unpack2(mul2(mul2(p, t), pack2(e[0], e[1])), tail0, tail1);
-    cdf[0] = x0 < 0.f ? tail0 : 1.f - tail0;
-    cdf[1] = x1 < 0.f ? tail1 : 1.f - tail1;
-}
-
-// act(x) of eight elements
-template <int ACT>
-__device__ __forceinline__ void act8(const float (&x)[8], float (&y)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-        if constexpr (ACT == GAR_ACT_GELU) {
-            float cdf[2], e[2];
-            normal2(x[i], x[i + 1], cdf, e);
-            y[i] = x[i] * cdf[0];
-            y[i + 1] = x[i + 1] * cdf[1];
-        } else {
-#pragma unroll
-            for (int k = i; k < i + 2; ++k) y[k] = ACT == GAR_ACT_RELU ? max_nan(x[k], 0.f) : ACT == GAR_ACT_SILU ? x[k] * sigmoid(x[k]) : x[k];
-        }
-    }
-}
 // act(x) and act'(x)
 template <int ACT>
 __device__ __forceinline__ void act_slope8(const float (&x)[8], float (&y)[8], float (&slope)[8]) {

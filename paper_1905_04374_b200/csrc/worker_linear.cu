@@ -1,0 +1,1215 @@
+// Products with a worker's weights (gar_linear.h) and what is done with them while they are still in tensor
+// memory: log probabilities of tokens without logits, their gradient at the logits, the gated feed-forward
+// block with its checkpoints, and the gradients at the inputs.
+//
+// One kernel: C = A B^T for 16-bit matrices, pairs of CTAs (clusters of two, one CTA per SM) on tiles of
+// 256 rows x 256 columns, 64 elements of the contraction a step, the paired instruction (cta_group::2) with
+// fp32 accumulators in tensor memory, two tiles' worth of it.
+//   copy warp      TMA, one lane: 128 rows of A and 128 rows of B per CTA and step, 128-byte swizzle; A and
+//                  B lie with the contraction along their rows (K-major), or B across them (MN-major: the
+//                  gradient at the inputs, dz W, reads W as it lies)
+//   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
+//   store warps    two groups of four, one per half of tensor memory, so that a tile's epilogue has the time of
+//                  two tiles' products; a thread has one row of the tile, 32 columns at a time
+// and four epilogues (enum Epilogue).  A thread owning a row makes the softmax's statistics, the group
+// maxima of the checkpoints and the row's target its own affair: no exchange between threads.
+//
+// Every wait is bounded (mbar.cuh); a pair whose wait gave up fills its tiles with NaN.
+#include <algorithm>
+#include <atomic>
+
+#include "gar_internal.cuh"
+#include "worker_act.cuh"
+#include "worker_linear.cuh"
+#include "worker_tensor.cuh"
+
+namespace gar {
+namespace worker {
+namespace {
+
+constexpr int LN_M = 128, LN_N = 256, LN_K = 64;      // rows of a CTA, columns of a pair, contraction per step
+constexpr int LN_HALF = LN_N / 2;                     // rows of B that a CTA holds
+constexpr int LN_RING = 5;                            // steps in flight
+constexpr int LN_TILE = LN_M * LN_K * 2;              // bytes of an operand per step and CTA
+constexpr int LN_BLOCK = 64 * 128;                    // bytes of 64 x 64 elements of an MN-major operand
+constexpr int LN_COPY_WARP = 0, LN_MMA_WARP = 1, LN_ALLOC_WARP = 2;
+constexpr int LN_STORE_WARP0 = 4, LN_STORE_WARPS = 8;
+constexpr int LN_THREADS = 32 * (LN_STORE_WARP0 + LN_STORE_WARPS);
+constexpr int LN_GROUP_M = 8;                         // (pair) row tiles that go round a column tile together
+constexpr int LN_PAIRS = 74;                          // pairs of SMs, for the rules that cut work into parts
+
+// What becomes of a tile.
+//   LN_SCORES   z: maximum and sum of exponentials of each row's 256 columns, and the target's z
+//   LN_DLOGITS  z: a ([j = t] - e^(z - lse)), stored in 16 bits
+//   LN_GATED    128 columns of g and of u: act(g) u, stored, and the codes of g and u
+//   LN_SUM      stored in 16 bits, or in fp32, or added to fp32 (parts of a longer contraction)
+enum Epilogue { LN_SCORES = 0, LN_DLOGITS = 1, LN_GATED = 2, LN_SUM = 3 };
+enum Out { OUT_WIDE = 0, OUT_PLAIN = 1, OUT_PART = 2, OUT_ADD = 3 };    // 16 bits by TMA or plainly; fp32, added
+
+struct LNArgs {
+    int64_t        rows, cols;            // of the result (LN_SCORES, LN_DLOGITS: columns from col0 on)
+    int            mt, nt, splits;        // pair row tiles, column tiles, parts of the contraction
+    int            steps0, steps;         // steps of the first pair of operands, of both together
+    int            act, group_shift, groups, out;
+    int64_t        col0, vocab;           // first column of this launch, columns there are
+    const void *   bias, *bias2;          // 16-bit, or null
+    const int64_t* targets;
+    float2*        parts;                 // LN_SCORES [rows][nt]: maximum, sum
+    float*         target_z;              // LN_SCORES [rows]
+    const float *  lse, *lse_lo, *coef;   // LN_DLOGITS [rows]
+    const unsigned* top;                  // the largest |coef|, as bits, where coefficients carry a power of two; or null
+    void*          y;                     // OUT_PLAIN, and the fill after a wait that gave up
+    int64_t        ldy;
+    gar_checkpoint_t s0, s1;              // of g and u
+};
+
+struct __align__(1024) LNSmem {
+    uint8_t  a[LN_RING][LN_TILE];
+    uint8_t  b[LN_RING][LN_TILE];
+    uint8_t  out[LN_STORE_WARPS][32 * 128];               // a store warp's piece: 32 rows of 128 bytes
+    float    add[LN_STORE_WARPS][LN_N];                   // the tile's biases, -inf for columns that do not exist
+    unsigned long long empty[LN_RING], acc_full[2];       // the slots are read; the accumulators are complete
+    unsigned long long full[LN_RING], acc_empty[2];       // the leading CTA's are used, for both
+    unsigned tmem_base;
+    int      error, other_error;                          // a wait gave up, here or in the other CTA
+};
+
+struct Place {
+    int m, n, split, first, steps;
+};
+__device__ __forceinline__ Place place_at(const LNArgs& a, unsigned index) {
+    Place t;
+    const unsigned split = a.splits > 1 ? index % unsigned(a.splits) : 0u;
+    if (a.splits > 1) index /= unsigned(a.splits);
+    const unsigned per_group = LN_GROUP_M * unsigned(a.nt), g = index / per_group, in_group = index - g * per_group;
+    const unsigned rows = min(unsigned(LN_GROUP_M), unsigned(a.mt) - g * LN_GROUP_M);
+    t.n = int(in_group / rows);
+    t.m = int(g * LN_GROUP_M + in_group - unsigned(t.n) * rows);
+    t.split = int(split);
+    t.first = 0;
+    t.steps = a.steps;
+    if (a.splits > 1) {
+        const int part = (a.steps + a.splits - 1) / a.splits;
+        t.first = int(split) * part;
+        t.steps = min(part, a.steps - t.first);
+    }
+    return t;
+}
+
+// 32 columns of this thread's row of the accumulators: asked for, there once waited for
+__device__ __forceinline__ void ask32(unsigned taddr, float (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+                   "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]),
+                   "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]),
+                   "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void wait32(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]),
+                   "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]),
+                   "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]),
+                   "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31]) :: "memory");
+}
+// f(v, c0) for the columns 0 .. cols of a tile, 32 at a time (cols is the warp's own number); the next are on
+// their way while some are worked on
+template <typename F>
+__device__ __forceinline__ void over_columns(unsigned src, int cols, F f) {
+    float v0[32], v1[32];
+    ask32(src, v0);
+    for (int c0 = 0; c0 < cols; c0 += 64) {
+        wait32(v0);
+        if (c0 + 32 < cols) ask32(src + unsigned(c0 + 32), v1);
+        f(v0, c0);
+        if (c0 + 32 >= cols) break;
+        wait32(v1);
+        if (c0 + 64 < cols) ask32(src + unsigned(c0 + 64), v0);
+        f(v1, c0 + 32);
+    }
+}
+__device__ __forceinline__ void add32(float (&v)[32], const float* add) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+        const float4 b = *reinterpret_cast<const float4*>(add + j);
+        v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
+    }
+}
+
+// 32 values as T to the first or second half of this lane's row of the staged piece
+template <typename T>
+__device__ __forceinline__ void stage32(unsigned stage, int lane, int half, const float (&v)[32]) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) {
+        const float f[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
+        put_shared(stage + lane * 128 + (((half * 4 + j / 8) ^ (lane & 7)) << 4), narrow16B(f, static_cast<const T*>(nullptr)));
+    }
+}
+__device__ __forceinline__ void tma_add(const CUtensorMap* map, unsigned src, int x, int y, int z) {
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_put(const CUtensorMap* map, unsigned src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// The staged piece (32 rows of 64 16-bit elements) to rows that start anywhere.
+__device__ __forceinline__ void store_plain(unsigned stage, int lane, unsigned short* dst, int64_t ld, int rows, int cols) {
+    for (int r = 0; r < rows; ++r) {
+        unsigned w;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(stage + r * 128 + (((lane / 4) ^ (r & 7)) << 4) + (lane & 3) * 4));
+        unsigned short* p = dst + r * ld + 2 * lane;
+        if (2 * lane + 1 < cols && reinterpret_cast<uintptr_t>(p) % 4 == 0) {
+            *reinterpret_cast<unsigned*>(p) = w;
+        } else {
+            if (2 * lane < cols) p[0] = static_cast<unsigned short>(w);
+            if (2 * lane + 1 < cols) p[1] = static_cast<unsigned short>(w >> 16);
+        }
+    }
+}
+
+// The columns' biases of a warp's tile: `n` from column c0 on, `fill` where there is no column
+template <typename T>
+__device__ __forceinline__ void fetch_biases(const void* bias, int64_t c0, int64_t cols, int n, float fill, float* add, int lane) {
+    for (int j = lane; j < n; j += 32)
+        add[j] = c0 + j >= cols ? fill : bias ? Elem<T>::widen(static_cast<const T*>(bias)[c0 + j]) : 0.f;
+}
+
+// ---- epilogues: one warp's 32 rows of a tile ------------------------------------------------------
+struct Warp {
+    unsigned src, stage;             // its lanes of the accumulators; its staging buffer
+    float*   add;
+    int      lane;
+    int64_t  row0;                   // the first of its rows
+};
+
+template <typename T>
+__device__ __forceinline__ void scores_tile(const LNArgs& a, const Place& t, const Warp& w) {
+    const int64_t c0 = int64_t(t.n) * LN_N, row = w.row0 + w.lane;
+    const int64_t left = a.cols - c0;
+    const int cols = left < LN_N ? int(left) : LN_N;
+    if (w.row0 >= a.rows) return;
+    const bool adds = a.bias || (cols & 31);
+    if (adds) {
+        fetch_biases<T>(a.bias, c0, a.cols, LN_N, -CUDART_INF_F, w.add, w.lane);
+        __syncwarp();
+    }
+    const bool live = row < a.rows;
+    int64_t t64 = a.targets && live ? a.targets[row] - c0 : -1;
+    const int target = t64 >= 0 && t64 < cols ? int(t64) : -1;
+    float m = -CUDART_INF_F, s = 0.f;
+    over_columns(w.src, cols, [&](float (&v)[32], int at) {
+        if (adds) add32(v, w.add + at);
+        if (__any_sync(0xffffffffu, target >= at && target < at + 32)) {
+            float z = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) z = target == at + j ? v[j] : z;
+            if (target >= at && target < at + 32) a.target_z[row] = z;
+        }
+        float top[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], v[j]);
+        const float higher = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+        if (higher > m) {
+            s *= ex2((m - higher) * kLog2e);
+            m = higher;
+        }
+        // z - m is rounded once and the exponent's unit comes after it: masks of the lowest value do not overflow
+        const float base = m == -CUDART_INF_F ? 0.f : m;
+        const f32x2 minus = pack2(-base, -base), unit = pack2(kLog2e, kLog2e);
+        f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            float e0, e1, e2, e3;
+            unpack2(mul2(add2(pack2(v[j], v[j + 1]), minus), unit), e0, e1);
+            unpack2(mul2(add2(pack2(v[j + 2], v[j + 3]), minus), unit), e2, e3);
+            sum0 = add2(sum0, pack2(ex2(e0), ex2(e1)));
+            sum1 = add2(sum1, pack2(ex2(e2), ex2(e3)));
+        }
+        float p, q;
+        unpack2(add2(sum0, sum1), p, q);
+        s += p + q;
+    });
+    if (live) a.parts[row * a.nt + t.n] = make_float2(m, s);
+}
+
+template <typename T>
+__device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, const Warp& w, const CUtensorMap* map) {
+    const int64_t c0 = int64_t(t.n) * LN_N, row = w.row0 + w.lane;
+    const int64_t left = a.cols - c0;
+    const int cols = left < LN_N ? int(left) : LN_N;
+    if (w.row0 >= a.rows) return;
+    const bool adds = a.bias != nullptr;
+    if (adds) {
+        fetch_biases<T>(a.bias, a.col0 + c0, a.col0 + a.cols, LN_N, -CUDART_INF_F, w.add, w.lane);
+        __syncwarp();
+    }
+    float coef = 0.f, lse = 0.f, lo = 0.f;
+    int target = -1;
+    if (row < a.rows) {
+        coef = a.coef[row];
+        lse = a.lse[row];
+        if (a.lse_lo) lo = a.lse_lo[row];
+        const int64_t t64 = a.targets[row] - a.col0 - c0;
+        target = t64 >= 0 && t64 < cols ? int(t64) : -1;
+        if (a.top) coef *= power_for(*a.top, false);
+    }
+    // a masked row: gradient 0 whatever comes in
+    if (lse == -CUDART_INF_F) coef = 0.f;
+    const bool nothing = coef == 0.f;
+    const f32x2 minus = pack2(-lse, -lse), unit = pack2(kLog2e, kLog2e), minus_lo = pack2(-lo * kLog2e, -lo * kLog2e), by = pack2(-coef, -coef);
+    int half = 0;
+    over_columns(w.src, cols, [&](float (&v)[32], int at) {
+        if (adds) add32(v, w.add + at);
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            float e0, e1;
+            unpack2(fma2(add2(pack2(v[j], v[j + 1]), minus), unit, minus_lo), e0, e1);
+            unpack2(mul2(pack2(ex2(e0), ex2(e1)), by), v[j], v[j + 1]);
+        }
+        if (__any_sync(0xffffffffu, target >= at && target < at + 32)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = target == at + j ? v[j] + coef : v[j];
+        }
+        if (__any_sync(0xffffffffu, nothing)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = nothing ? 0.f : v[j];
+        }
+        if (half == 0) {
+            if (w.lane == 0) tma_store_read<0>();
+            __syncwarp();
+        }
+        stage32<T>(w.stage, w.lane, half, v);
+        if (half == 1 || at + 32 >= cols) {
+            fence_async_smem();
+            __syncwarp();
+            if (w.lane == 0) tma_put(map, w.stage, int(c0) + (at & ~63), int(w.row0), 0);
+        }
+        half ^= 1;
+    });
+}
+
+template <typename T>
+__device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const Warp& w, const CUtensorMap* map) {
+    const int64_t c0 = int64_t(t.n) * LN_N;
+    const int64_t left = a.cols - c0, rows_left = a.rows - w.row0;
+    const int cols = left < LN_N ? int(left) : LN_N, rows = rows_left < 32 ? int(rows_left) : 32;
+    if (rows <= 0) return;
+    if (a.out >= OUT_PART) {
+        over_columns(w.src, cols, [&](float (&v)[32], int at) {
+            if (w.lane == 0) tma_store_read<0>();
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                put_shared(w.stage + w.lane * 128 + ((j ^ (w.lane & 7)) << 4),
+                           make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])));
+            fence_async_smem();
+            __syncwarp();
+            if (w.lane == 0) {
+                if (a.out == OUT_ADD) tma_add(map, w.stage, int(c0) + at, int(w.row0), t.split);
+                else tma_put(map, w.stage, int(c0) + at, int(w.row0), t.split);
+            }
+        });
+        return;
+    }
+    const float by = a.top ? power_for(*a.top, true) : 1.f;
+    int half = 0;
+    over_columns(w.src, cols, [&](float (&v)[32], int at) {
+        if (a.top) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= by;
+        }
+        if (half == 0) {
+            if (w.lane == 0) tma_store_read<0>();
+            __syncwarp();
+        }
+        stage32<T>(w.stage, w.lane, half, v);
+        if (half == 1 || at + 32 >= cols) {
+            const int from = at & ~63;
+            if (a.out == OUT_WIDE) {
+                fence_async_smem();
+                __syncwarp();
+                if (w.lane == 0) tma_put(map, w.stage, int(c0) + from, int(w.row0), 0);
+            } else {
+                __syncwarp();
+                store_plain(w.stage, w.lane, static_cast<unsigned short*>(a.y) + w.row0 * a.ldy + c0 + from, a.ldy, rows, cols - from);
+                __syncwarp();
+            }
+        }
+        half ^= 1;
+    });
+}
+
+// 32 columns' codes of this thread's row to the checkpoint
+__device__ __forceinline__ void store_codes(const float (&v)[32], const Step& step, int8_t* q, int count) {
+    unsigned w[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float f[8] = {v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3], v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7]};
+        codes8(f, step, w[2 * j], w[2 * j + 1]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (16 * k + 16 <= count) {
+            reinterpret_cast<uint4*>(q)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        } else {
+#pragma unroll
+            for (int j = 16 * k; j < 16 * k + 16; ++j)
+                if (j < count) q[j] = int8_t((w[j / 4] >> 8 * (j & 3)) & 0xff);
+        }
+    }
+}
+
+template <int ACT> __device__ __forceinline__ void act32(float (&g)[32], const float (&u)[32]) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) {
+        const float x[8] = {g[j], g[j + 1], g[j + 2], g[j + 3], g[j + 4], g[j + 5], g[j + 6], g[j + 7]};
+        float y[8];
+        act8<ACT>(x, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[j + i] = y[i] * u[j + i];
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void gated_tile(const LNArgs& a, const Place& t, const Warp& w, const CUtensorMap* map) {
+    const int64_t c0 = int64_t(t.n) * LN_HALF, row = w.row0 + w.lane;
+    const int64_t left = a.cols - c0, rows_left = a.rows - w.row0;
+    const int cols = left < LN_HALF ? int(left) : LN_HALF, rows = rows_left < 32 ? int(rows_left) : 32;
+    if (rows <= 0) return;
+    const bool adds = a.bias || a.bias2;
+    if (adds) {
+        fetch_biases<T>(a.bias, c0, a.cols, LN_HALF, 0.f, w.add, w.lane);
+        fetch_biases<T>(a.bias2, c0, a.cols, LN_HALF, 0.f, w.add + LN_HALF, w.lane);
+        __syncwarp();
+    }
+    float g[32], u[32];
+    const bool live = row < a.rows, saves = a.s0.q || a.s1.q;
+    unsigned top_g[4] = {0, 0, 0, 0}, top_u[4] = {0, 0, 0, 0};      // of the groups, as bits: NaN above infinity
+    if (saves) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            ask32(w.src + unsigned(32 * k), g);
+            ask32(w.src + unsigned(LN_HALF + 32 * k), u);
+            wait32(g);
+            wait32(u);
+            if (adds) {
+                add32(g, w.add + 32 * k);
+                add32(u, w.add + LN_HALF + 32 * k);
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                top_g[k] = max(top_g[k], __float_as_uint(g[j]) & 0x7fffffffu);
+                top_u[k] = max(top_u[k], __float_as_uint(u[j]) & 0x7fffffffu);
+            }
+        }
+        if (a.group_shift >= 6) {
+#pragma unroll
+            for (int k = 0; k < 4; k += 2) {
+                top_g[k] = top_g[k + 1] = max(top_g[k], top_g[k + 1]);
+                top_u[k] = top_u[k + 1] = max(top_u[k], top_u[k + 1]);
+            }
+        }
+        if (a.group_shift == 7) {
+            const unsigned tg = max(top_g[0], top_g[2]), tu = max(top_u[0], top_u[2]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                top_g[k] = tg;
+                top_u[k] = tu;
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (32 * k < cols) {
+            ask32(w.src + unsigned(32 * k), g);
+            ask32(w.src + unsigned(LN_HALF + 32 * k), u);
+            wait32(g);
+            wait32(u);
+            if (adds) {
+                add32(g, w.add + 32 * k);
+                add32(u, w.add + LN_HALF + 32 * k);
+            }
+            if (saves && live) {
+                const int64_t c = c0 + 32 * k, group = row * a.groups + (c >> a.group_shift);
+                const bool first = (c & ((1 << a.group_shift) - 1)) == 0;
+                if (a.s0.q) {
+                    const Step step(__uint_as_float(top_g[k]));
+                    if (first) a.s0.scales[group] = step.scale(__uint_as_float(top_g[k]));
+                    store_codes(g, step, a.s0.q + row * a.s0.ldq + c, cols - 32 * k);
+                }
+                if (a.s1.q) {
+                    const Step step(__uint_as_float(top_u[k]));
+                    if (first) a.s1.scales[group] = step.scale(__uint_as_float(top_u[k]));
+                    store_codes(u, step, a.s1.q + row * a.s1.ldq + c, cols - 32 * k);
+                }
+            }
+            if (a.act == GAR_ACT_SILU) act32<GAR_ACT_SILU>(g, u);
+            else if (a.act == GAR_ACT_GELU) act32<GAR_ACT_GELU>(g, u);
+            else if (a.act == GAR_ACT_RELU) act32<GAR_ACT_RELU>(g, u);
+            else act32<GAR_ACT_IDENTITY>(g, u);
+            if (!(k & 1)) {
+                if (w.lane == 0) tma_store_read<0>();
+                __syncwarp();
+            }
+            stage32<T>(w.stage, w.lane, k & 1, g);
+            if ((k & 1) || 32 * (k + 1) >= cols) {
+                const int from = 32 * (k & ~1);
+                if (a.out == OUT_WIDE) {
+                    fence_async_smem();
+                    __syncwarp();
+                    if (w.lane == 0) tma_put(map, w.stage, int(c0) + from, int(w.row0), 0);
+                } else {
+                    __syncwarp();
+                    store_plain(w.stage, w.lane, static_cast<unsigned short*>(a.y) + w.row0 * a.ldy + c0 + from, a.ldy, rows, cols - from);
+                    __syncwarp();
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int EPI>
+__global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, const __grid_constant__ CUtensorMap map_a0,
+                                                              const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_a1,
+                                                              const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_out) {
+    constexpr bool B_MN = EPI == LN_SUM;
+    extern __shared__ uint8_t raw[];
+    LNSmem& sm = *reinterpret_cast<LNSmem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    volatile int* error = &sm.error;
+    const unsigned rank = cta_rank();
+    const unsigned pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    if (tid == 0) {
+        sm.error = sm.other_error = 0;
+        for (int k = 0; k < LN_RING; ++k) {
+            kb_init(&sm.empty[k], 1);
+            kb_init(&sm.full[k], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            kb_init(&sm.acc_full[b], 1);
+            kb_init(&sm.acc_empty[b], 8);
+        }
+        kb_fence_init();
+    }
+    if (tid == 32) {
+        prefetch_map(&map_a0);
+        prefetch_map(&map_b0);
+        if (EPI != LN_SCORES && a.out != OUT_PLAIN) prefetch_map(&map_out);
+    }
+    if (warp == LN_ALLOC_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kb_smem_u32(&sm.tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    pair_sync();                              // the other CTA's barriers are initialised
+    tc_fence_after();
+    const unsigned tmem = sm.tmem_base;
+    const unsigned tiles = unsigned(a.mt) * unsigned(a.nt) * unsigned(a.splits);      // below 2^30
+    bool ok = true;
+
+    if (warp == LN_COPY_WARP) {
+        if (lane == 0) {
+            const unsigned leader_full = pair_address(kb_smem_u32(sm.full), 0);
+            unsigned g = 0;                                  // steps of all tiles so far
+            for (unsigned i = pair; ok && i < tiles; i += pairs) {
+                const Place t = place_at(a, i);
+                const int y = (2 * t.m + int(rank)) * LN_M;
+                for (int s = 0; s < t.steps; ++s, ++g) {
+                    const Ring<LN_RING> r(g);
+                    if (!kb_wait(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
+                    if (rank == 0) kb_expect_tx(kb_smem_u32(&sm.full[r.slot]), 4 * LN_TILE);
+                    const unsigned bar = leader_full + r.slot * 8, da = kb_smem_u32(sm.a[r.slot]), db = kb_smem_u32(sm.b[r.slot]);
+                    const int step = t.first + s;
+                    const bool second = step >= a.steps0;
+                    const int k = (second ? step - a.steps0 : step) * LN_K;
+                    tma_load_pair(da, second ? &map_a1 : &map_a0, k, y, 0, bar);
+                    if (B_MN) {
+                        const int x = t.n * LN_N + int(rank) * LN_HALF;
+                        const CUtensorMap* map = second ? &map_b1 : &map_b0;
+                        tma_load_pair(db, map, x, k, 0, bar);
+                        tma_load_pair(db + LN_BLOCK, map, x + 64, k, 0, bar);
+                    } else if (EPI == LN_GATED) {
+                        tma_load_pair(db, rank == 0 ? &map_b0 : &map_b1, k, t.n * LN_HALF, 0, bar);
+                    } else {
+                        tma_load_pair(db, &map_b0, k, t.n * LN_N + int(rank) * LN_HALF, 0, bar);
+                    }
+                }
+            }
+            // after a wait that gave up: the copies in flight land (the leading CTA counts them in) before
+            // either CTA's shared memory is given back
+            for (unsigned k = 0; !ok && rank == 0 && k < LN_RING && k < g; ++k) {
+                const Ring<LN_RING> r(g - 1 - k);
+                kb_wait(kb_smem_u32(&sm.full[r.slot]), r.parity, error, true, 1u << 10);
+            }
+        }
+    } else if (warp == LN_MMA_WARP) {
+        // The whole warp walks the loop and one elected lane issues.
+        if (rank == 0) {
+            const unsigned idesc = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, LN_N, false, B_MN);
+            const unsigned long long desc_a = operand_desc(kb_smem_u32(sm.a), 16, 1024, 2);
+            const unsigned long long desc_b = operand_desc(kb_smem_u32(sm.b), B_MN ? LN_BLOCK : 16, 1024, 2);
+            // 16 elements of the contraction: 32 bytes along a K-major row, 16 rows of 128 bytes of an MN-major block
+            constexpr unsigned STEP_A = 2, STEP_B = B_MN ? 128 : 2;
+            unsigned g = 0, done = 0;
+            for (unsigned i = pair; ok && i < tiles; i += pairs, ++done) {
+                const Place t = place_at(a, i);
+                const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
+                const unsigned half = done & 1u, round = (done >> 1) & 1u, d = tmem + half * LN_N;
+                if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[half]), round ^ 1u, error)) { ok = false; break; }
+                tc_fence_after();
+                for (int s = 0; s < steps; ++s, ++g) {
+                    const Ring<LN_RING> r(g);
+                    if (!kb_wait_warp(kb_smem_u32(&sm.full[r.slot]), r.parity, error)) { ok = false; break; }
+                    tc_fence_after();
+                    const unsigned long long da = desc_a + r.slot * (LN_TILE / 16), db = desc_b + r.slot * (LN_TILE / 16);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < LN_K / 16; ++k) mma_f16(d, da + k * STEP_A, db + k * STEP_B, idesc, s > 0 || k > 0);
+                        mma_commit(&sm.empty[r.slot]);
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
+                if (elect_one()) mma_commit(&sm.acc_full[half]);
+                __syncwarp();
+            }
+            // nothing is in flight when the tensor memory is freed: on the good path the store warps have
+            // seen every accumulator; after a wait that gave up, wait for what was issued
+            if (!ok) {
+                const unsigned half = done & 1u, round = (done >> 1) & 1u;
+                if (elect_one()) mma_commit(&sm.acc_full[half]);
+                __syncwarp();
+                kb_wait(kb_smem_u32(&sm.acc_full[half]), round, error, true, 1u << 10);
+            }
+        }
+    } else if (warp >= LN_STORE_WARP0) {
+        const int mine = (warp - LN_STORE_WARP0) / 4, quarter = warp % 4;      // half of tensor memory; its lanes 32 quarter ..
+        Warp w;
+        w.src = tmem + unsigned(mine) * LN_N + (unsigned(quarter * 32) << 16);
+        w.stage = kb_smem_u32(sm.out[warp - LN_STORE_WARP0]);
+        w.add = sm.add[warp - LN_STORE_WARP0];
+        w.lane = lane;
+        unsigned done = 0;
+        for (unsigned i = pair; i < tiles; i += pairs, ++done) {
+            if (int(done & 1u) != mine) continue;
+            const Place t = place_at(a, i);
+            if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[mine]), (done >> 1) & 1u, error)) break;
+            tc_fence_after();
+            w.row0 = int64_t(2 * t.m + int(rank)) * LN_M + quarter * 32;
+            if constexpr (EPI == LN_SCORES) scores_tile<T>(a, t, w);
+            if constexpr (EPI == LN_DLOGITS) dlogits_tile<T>(a, t, w, &map_out);
+            if constexpr (EPI == LN_GATED) gated_tile<T>(a, t, w, &map_out);
+            if constexpr (EPI == LN_SUM) sum_tile<T>(a, t, w, &map_out);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at_leader(&sm.acc_empty[mine]);
+        }
+        if (lane == 0) tma_store_done();
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (tid == 0 && sm.error)
+        asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(pair_address(kb_smem_u32(&sm.other_error), rank ^ 1u)), "r"(1) : "memory");
+    __syncwarp();
+    pair_sync();                              // the other CTA's products and arrivals have ended too
+    tc_fence_after();
+    if (warp == LN_ALLOC_WARP)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    if (sm.error || *static_cast<volatile int*>(&sm.other_error)) {
+        // a wait gave up: nothing the pair was to write may look like a result
+        constexpr int WIDTH = EPI == LN_SCORES ? 1 : EPI == LN_GATED ? LN_HALF : LN_N;
+        for (unsigned i = pair; i < tiles; i += pairs) {
+            const Place t = place_at(a, i);
+            for (int e = tid; e < LN_M * WIDTH; e += LN_THREADS) {
+                const int64_t row = int64_t(2 * t.m + int(rank)) * LN_M + e / WIDTH, c = int64_t(t.n) * WIDTH + e % WIDTH;
+                if (row >= a.rows) continue;
+                if constexpr (EPI == LN_SCORES) a.parts[row * a.nt + t.n] = make_float2(CUDART_NAN_F, CUDART_NAN_F);
+                else if (c < a.cols) {
+                    if (EPI == LN_SUM && a.out >= OUT_PART) static_cast<float*>(a.y)[(int64_t(t.split) * a.rows + row) * a.ldy + c] = CUDART_NAN_F;
+                    else static_cast<T*>(a.y)[row * a.ldy + c] = Elem<T>::narrow(CUDART_NAN_F);
+                    if (EPI == LN_GATED && (c & ((1 << a.group_shift) - 1)) == 0) {
+                        if (a.s0.q) a.s0.scales[row * a.groups + (c >> a.group_shift)] = CUDART_NAN_F;
+                        if (a.s1.q) a.s1.scales[row * a.groups + (c >> a.group_shift)] = CUDART_NAN_F;
+                    }
+                }
+            }
+        }
+    }
+}
+
+// ---- around the products ----------------------------------------------------------------------------
+// The parts of a row joined: a warp per row.
+__global__ void __launch_bounds__(256) join_scores_kernel(const float2* parts, const float* target_z, const int64_t* targets, int64_t rows, int nt,
+                                                          int64_t vocab, float* logprobs, float* lse, float* lse_lo) {
+    const int64_t row = int64_t(blockIdx.x) * 8 + threadIdx.x / 32;
+    const int lane = threadIdx.x % 32;
+    if (row >= rows) return;
+    const float2* p = parts + row * nt;
+    float m = -CUDART_INF_F, s = 0.f;
+    for (int k = lane; k < nt; k += 32) {
+        const float2 q = p[k];
+        const float higher = fmaxf(m, q.x);
+        if (higher == -CUDART_INF_F) {
+            s += q.y;                          // 0, or NaN
+        } else {
+            // a part without a finite maximum adds 0; NaN stays
+            s = s * ex2((m - higher) * kLog2e) + q.y * ex2((q.x - higher) * kLog2e);
+            m = higher;
+        }
+    }
+    float top = m;
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (top != -CUDART_INF_F) s *= ex2((m - top) * kLog2e);
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane) return;
+    // the sum of a row without entries is 0, of one with NaN or +inf NaN
+    const float l = logf(s);
+    const float hi = top == -CUDART_INF_F ? (s == 0.f ? top : CUDART_NAN_F) : top + l;
+    if (lse) lse[row] = hi;
+    if (lse_lo) {
+        // two-sum: top + l = hi + lo
+        const float bb = hi - top;
+        const float lo = (top - (hi - bb)) + (l - bb);
+        lse_lo[row] = fabsf(hi) <= 3.402823466e38f ? lo : 0.f;
+    }
+    if (logprobs) {
+        const int64_t t = targets[row];
+        float lp = 0.f;
+        if (t >= vocab) lp = CUDART_NAN_F;
+        else if (t >= 0) lp = top == -CUDART_INF_F ? hi : (target_z[row] - top) - l;
+        logprobs[row] = lp;
+    }
+}
+
+// Rows of 16-bit elements copied to rows that start on 16 bytes, eight elements per thread and turn.  ROWS: rows
+// whose coefficient is 0 are copied as zeros, and the coefficients (the gradient at a row's log probability; 0
+// without a target, NaN for a target outside the vocabulary) and the largest one's magnitude are written.
+struct RowsArgs {
+    const unsigned short* src;
+    int64_t        ld, cols, pieces, per_row;
+    uint4*         dst;                    // null: only the coefficients
+    const int64_t* targets;
+    const float*   grad;
+    int64_t        vocab;
+    float*         coef;
+    unsigned*      top;                    // null: not asked for
+    int            aligned;                // the source's rows start on 16 bytes
+};
+template <bool ROWS>
+__global__ void __launch_bounds__(256) copy_rows_kernel(const RowsArgs a) {
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < a.pieces; i += int64_t(gridDim.x) * 256) {
+        const int64_t row = i / a.per_row, c = (i - row * a.per_row) * 8;
+        bool zero = false;
+        if (ROWS) {
+            const int64_t t = a.targets[row];
+            const float coef = t < 0 ? 0.f : t >= a.vocab ? CUDART_NAN_F : a.grad[row];
+            zero = coef == 0.f;
+            if (c == 0) {
+                a.coef[row] = coef;
+                const unsigned bits = __float_as_uint(coef) & 0x7fffffffu;
+                if (a.top && bits < 0x7f800000u) atomicMax(a.top, bits);      // the same in any order
+            }
+            if (!a.dst) continue;
+        }
+        const unsigned short* p = a.src + row * a.ld + c;
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (!zero) {
+            if (a.aligned && c + 8 <= a.cols) {
+                w = __ldg(reinterpret_cast<const uint4*>(p));
+            } else {
+                unsigned v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = c + j < a.cols ? __ldg(p + j) : 0u;
+                w = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+            }
+        }
+        a.dst[i] = w;
+    }
+}
+
+// The parts of a sum, added in order and rounded once, four columns per thread and turn.
+template <typename T>
+__global__ void __launch_bounds__(256) join_parts_kernel(const float* parts, int64_t plane, int64_t pitch, int splits, int64_t rows, int64_t cols,
+                                                         const unsigned* top, T* y, int64_t ldy) {
+    const int64_t per_row = (cols + 3) / 4, pieces = rows * per_row;
+    const float by = top ? power_for(*top, true) : 1.f;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += int64_t(gridDim.x) * 256) {
+        const int64_t row = i / per_row, c = (i - row * per_row) * 4;
+        const float* p = parts + row * pitch + c;
+        float4 s = __ldcs(reinterpret_cast<const float4*>(p));
+        for (int k = 1; k < splits; ++k) {
+            const float4 q = __ldcs(reinterpret_cast<const float4*>(p + k * plane));
+            s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
+        }
+        T out[4] = {Elem<T>::narrow(s.x * by), Elem<T>::narrow(s.y * by), Elem<T>::narrow(s.z * by), Elem<T>::narrow(s.w * by)};
+        T* dst = y + row * ldy + c;
+        if (c + 4 <= cols && reinterpret_cast<uintptr_t>(dst) % 8 == 0) {
+            *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(out);
+        } else {
+            for (int j = 0; j < 4; ++j)
+                if (c + j < cols) dst[j] = out[j];
+        }
+    }
+}
+
+// ---- launches ---------------------------------------------------------------------------------------
+bool on_16(const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }
+int64_t up_to(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+int64_t parts_of(int64_t v, int64_t m) { return (v + m - 1) / m; }
+CUtensorMapDataType map_type(int dtype) { return dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16; }
+
+// A 16-bit matrix as the tensor maps take it: rows that start on 16 bytes.
+struct Operand {
+    const char* p;
+    int64_t     rows, cols, ld;
+};
+cudaError_t operand_map(CUtensorMap* map, int dtype, const Operand& m, int box_cols, int box_rows) {
+    return make_map(map, map_type(dtype), m.p, m.cols, m.rows, 1, m.ld * 2, m.ld * 2 * m.rows, box_cols, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+// A workspace handed out piece by piece; without memory it only counts.
+class Space {
+public:
+    explicit Space(void* base) : base_(static_cast<char*>(base)) {}
+    char* take(size_t bytes) {
+        char* p = base_ ? base_ + used_ : nullptr;
+        used_ += gar::align256(bytes);
+        return p;
+    }
+    size_t used() const { return used_; }
+
+private:
+    char*  base_;
+    size_t used_ = 0;
+};
+
+unsigned copy_blocks(int64_t pieces, int sm_count) { return unsigned(std::min<int64_t>(int64_t(16) * sm_count, parts_of(pieces, 256))); }
+cudaError_t copy_rows(const Operand& src, char* dst, int64_t ld, int sm_count, cudaStream_t stream) {
+    RowsArgs a{};
+    a.src = reinterpret_cast<const unsigned short*>(src.p);
+    a.ld = src.ld;
+    a.cols = src.cols;
+    a.per_row = ld / 8;
+    a.pieces = src.rows * a.per_row;
+    a.dst = reinterpret_cast<uint4*>(dst);
+    a.aligned = on_16(src.p, src.ld);
+    copy_rows_kernel<false><<<copy_blocks(a.pieces, sm_count), 256, 0, stream>>>(a);
+    return cudaGetLastError();
+}
+// A matrix of the caller's as an operand: where it lies, or copied to the space reserved for it.
+struct Input {
+    Operand m;
+    char*   copy = nullptr;
+    Input(Space& space, const void* p, int64_t rows, int64_t cols, int64_t ld) : m{static_cast<const char*>(p), rows, cols, ld} {
+        if (on_16(p, ld)) return;
+        copy = space.take(size_t(rows) * size_t(up_to(cols, 8)) * 2);
+        copied_ = true;
+    }
+    cudaError_t ready(int sm_count, cudaStream_t stream) {
+        if (!copied_) return cudaSuccess;
+        const int64_t ld = up_to(m.cols, 8);
+        if (cudaError_t err = copy_rows(m, copy, ld, sm_count, stream)) return err;
+        m.p = copy;
+        m.ld = ld;
+        return cudaSuccess;
+    }
+
+private:
+    bool copied_ = false;
+};
+
+struct Maps {
+    CUtensorMap a0, b0, a1, b1, out;
+};
+template <typename T, int EPI>
+cudaError_t launch_as(const LNArgs& a, const Maps& maps, int sm_count, cudaStream_t stream) {
+    constexpr int bytes = int(sizeof(LNSmem)) + 1024;
+    static_assert(bytes <= 232448, "a CTA's shared memory");
+    auto kernel = linear_kernel<T, EPI>;
+    static std::atomic<uint64_t> allowed{0};           // devices on which the kernel may have that much
+    int dev = 0;
+    if (cudaError_t err = cudaGetDevice(&dev)) return err;
+    if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+        if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
+        if (dev < 64) allowed.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+    }
+    const int64_t tiles = int64_t(a.mt) * a.nt * a.splits;
+    if (tiles >= int64_t(1) << 30) return cudaErrorInvalidConfiguration;
+    const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(2 * std::min(tiles, pairs)));
+    cfg.blockDim = dim3(LN_THREADS);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a, maps.a0, maps.b0, maps.a1, maps.b1, maps.out);
+}
+template <int EPI>
+cudaError_t launch(int dtype, const LNArgs& a, const Maps& maps, int sm_count, cudaStream_t stream) {
+    return dtype == GAR_BF16 ? launch_as<__nv_bfloat16, EPI>(a, maps, sm_count, stream) : launch_as<__half, EPI>(a, maps, sm_count, stream);
+}
+
+// z = x W^T over `rows` rows and the columns of `w`: the operands' part of a launch
+cudaError_t logits_maps(Maps& maps, LNArgs& a, int dtype, const Operand& x, const Operand& w) {
+    a.rows = x.rows;
+    a.cols = w.rows;
+    a.mt = int(parts_of(x.rows, 2 * LN_M));
+    a.nt = int(parts_of(w.rows, LN_N));
+    a.splits = 1;
+    a.steps0 = a.steps = int(parts_of(x.cols, LN_K));
+    if (cudaError_t err = operand_map(&maps.a0, dtype, x, LN_K, LN_M)) return err;
+    if (cudaError_t err = operand_map(&maps.b0, dtype, w, LN_K, LN_HALF)) return err;
+    maps.a1 = maps.b1 = maps.out = maps.a0;            // not used unless set
+    return cudaSuccess;
+}
+
+// How a sum over a long contraction into few tiles is cut, so that every pair of SMs has a part, of eight steps at least.
+int splits_for(int64_t rows, int64_t cols, int64_t steps) {
+    const int64_t tiles = parts_of(rows, 2 * LN_M) * parts_of(cols, LN_N);
+    int64_t s = std::min<int64_t>(std::min<int64_t>(LN_PAIRS / tiles, steps / 8), 16);
+    if (s < 2) return 1;
+    const int64_t part = parts_of(steps, s);           // no part is empty
+    return int(parts_of(steps, part));
+}
+
+// dx, or a part of it, in fp32 parts or as it is wanted.
+struct SumTarget {
+    int      dtype;
+    void*    dx;
+    int64_t  rows, cols, ld;
+    float*   parts;                                    // [splits][rows][pitch]; null: straight to dx
+    int64_t  pitch;
+    int      splits;
+    const unsigned* top;
+};
+cudaError_t launch_sum(const SumTarget& d, const Operand& a0, const Operand& b0, const Operand* a1, const Operand* b1, bool add, int sm_count, cudaStream_t stream) {
+    Maps maps;
+    LNArgs a{};
+    a.rows = d.rows;
+    a.cols = d.cols;
+    a.mt = int(parts_of(d.rows, 2 * LN_M));
+    a.nt = int(parts_of(d.cols, LN_N));
+    a.steps0 = int(parts_of(a0.cols, LN_K));
+    a.steps = a.steps0 + (a1 ? int(parts_of(a1->cols, LN_K)) : 0);
+    // (a shorter last piece of the contraction may have steps for fewer parts)
+    const int part = (a.steps + d.splits - 1) / d.splits;
+    a.splits = (a.steps + part - 1) / part;
+    if (cudaError_t err = operand_map(&maps.a0, d.dtype, a0, LN_K, LN_M)) return err;
+    if (cudaError_t err = operand_map(&maps.b0, d.dtype, b0, 64, LN_K)) return err;
+    maps.a1 = maps.a0;
+    maps.b1 = maps.b0;
+    if (a1) {
+        if (cudaError_t err = operand_map(&maps.a1, d.dtype, *a1, LN_K, LN_M)) return err;
+        if (cudaError_t err = operand_map(&maps.b1, d.dtype, *b1, 64, LN_K)) return err;
+    }
+    maps.out = maps.a0;
+    if (d.parts) {
+        a.out = add ? OUT_ADD : OUT_PART;
+        a.y = d.parts;
+        a.ldy = d.pitch;
+        if (cudaError_t err = make_map(&maps.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d.parts, d.cols, d.rows, d.splits, d.pitch * 4, d.pitch * 4 * d.rows, 32, 32,
+                                       CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+    } else {
+        a.out = on_16(d.dx, d.ld) ? OUT_WIDE : OUT_PLAIN;
+        a.y = d.dx;
+        a.ldy = d.ld;
+        a.top = d.top;
+        if (a.out == OUT_WIDE)
+            if (cudaError_t err = operand_map(&maps.out, d.dtype, Operand{static_cast<const char*>(d.dx), d.rows, d.cols, d.ld}, 64, 32)) return err;
+    }
+    return launch<LN_SUM>(d.dtype, a, maps, sm_count, stream);
+}
+cudaError_t join_sum(const SumTarget& d, int sm_count, cudaStream_t stream) {
+    const unsigned blocks = copy_blocks(d.rows * parts_of(d.cols, 4), sm_count);
+    if (d.dtype == GAR_BF16)
+        join_parts_kernel<<<blocks, 256, 0, stream>>>(d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top, static_cast<__nv_bfloat16*>(d.dx), d.ld);
+    else
+        join_parts_kernel<<<blocks, 256, 0, stream>>>(d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top, static_cast<__half*>(d.dx), d.ld);
+    return cudaGetLastError();
+}
+
+// ---- log probabilities ------------------------------------------------------------------------------
+constexpr int64_t LN_PARTS_BYTES = int64_t(64) << 20, LN_PIECE_BYTES = int64_t(64) << 20;
+constexpr int64_t LN_PIECE_MAX = 16384;
+// rows of a launch, so that its parts take 64 MB at most
+int64_t rows_at_once(int64_t rows, int64_t vocab) {
+    const int64_t most = std::max<int64_t>(256, LN_PARTS_BYTES / (8 * parts_of(vocab, LN_N)) / 256 * 256);
+    return std::min(rows, most);
+}
+struct ScoresPlan {
+    Space   space;
+    Input   x, w;
+    int64_t rows;
+    float2* parts;
+    float*  target_z;
+    ScoresPlan(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw)
+        : space(p.workspace), x(space, p.x, p.rows, p.hidden, ldx), w(space, p.weight, p.vocab, p.hidden, ldw), rows(rows_at_once(p.rows, p.vocab)) {
+        parts = reinterpret_cast<float2*>(space.take(size_t(rows) * size_t(parts_of(p.vocab, LN_N)) * 8));
+        target_z = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
+    }
+};
+
+// Columns of a piece of the vocabulary: dz of up to 64 MB, and sums of no more than 2^14 terms; equal pieces.
+int64_t piece_of(int64_t rows, int64_t vocab) {
+    const int64_t most = std::max<int64_t>(LN_N, std::min<int64_t>(LN_PIECE_MAX, LN_PIECE_BYTES / (2 * rows) / LN_N * LN_N));
+    return up_to(parts_of(vocab, parts_of(vocab, most)), LN_N);
+}
+struct GradPlan {
+    Space     space;
+    int64_t   rows, piece, ld_dz, ldx;
+    int       splits;
+    Input     w;
+    char*     x_rows;                      // x with rows that do not count as zeros
+    float*    coef;
+    unsigned* top = nullptr;
+    char*     dz;
+    float*    parts = nullptr;
+    int64_t   pitch;
+    char*     weight_space = nullptr;
+    size_t    weight_bytes = 0;
+    GradPlan(const gar_linear_logprobs_grad_params_t& p, int64_t ldw)
+        : space(p.workspace), rows(p.workers * p.tokens), piece(piece_of(std::max<int64_t>(rows, 1), p.vocab)), ld_dz(up_to(piece, 8)), ldx(up_to(p.hidden, 8)),
+          w(space, p.weight, p.vocab, p.hidden, ldw) {
+        x_rows = space.take(size_t(rows) * size_t(ldx) * 2);
+        coef = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
+        if (p.dtype == GAR_F16) top = reinterpret_cast<unsigned*>(space.take(4));
+        dz = space.take(size_t(rows) * size_t(ld_dz) * 2);
+        pitch = up_to(p.hidden, 4);
+        splits = splits_for(std::max<int64_t>(rows, 1), p.hidden, parts_of(std::min(piece, p.vocab), LN_K));
+        if (p.dx && (splits > 1 || piece < p.vocab)) parts = reinterpret_cast<float*>(space.take(size_t(splits) * size_t(rows) * size_t(pitch) * 4));
+        if (p.weight_grads) {
+            // (the last piece, if it is shorter, may be cut into more parts)
+            const int64_t last = (p.vocab - 1) % piece + 1;
+            weight_bytes = std::max(dense_weight_grad_workspace_bytes(p.workers, p.tokens, std::min(piece, p.vocab), p.hidden, p.bias_grads != nullptr),
+                                    dense_weight_grad_workspace_bytes(p.workers, p.tokens, last, p.hidden, p.bias_grads != nullptr));
+            weight_space = space.take(weight_bytes);
+        }
+    }
+};
+
+}  // namespace
+
+size_t linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw) {
+    gar_linear_logprobs_params_t q = p;
+    q.workspace = nullptr;
+    return ScoresPlan(q, ldx, ldw).space.used();
+}
+
+cudaError_t launch_linear_logprobs(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw, int sm_count) {
+    cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
+    ScoresPlan plan(p, ldx, ldw);
+    if (cudaError_t err = plan.x.ready(sm_count, stream)) return err;
+    if (cudaError_t err = plan.w.ready(sm_count, stream)) return err;
+    for (int64_t r0 = 0; r0 < p.rows; r0 += plan.rows) {
+        Operand x = plan.x.m;
+        x.p += r0 * x.ld * 2;
+        x.rows = std::min(plan.rows, p.rows - r0);
+        Maps maps;
+        LNArgs a{};
+        if (cudaError_t err = logits_maps(maps, a, p.dtype, x, plan.w.m)) return err;
+        a.bias = p.bias;
+        a.targets = p.logprobs ? p.targets + r0 : nullptr;
+        a.parts = plan.parts;
+        a.target_z = plan.target_z;
+        if (cudaError_t err = launch<LN_SCORES>(p.dtype, a, maps, sm_count, stream)) return err;
+        join_scores_kernel<<<unsigned(parts_of(x.rows, 8)), 256, 0, stream>>>(plan.parts, plan.target_z, a.targets, x.rows, a.nt, p.vocab,
+                                                                             p.logprobs ? p.logprobs + r0 : nullptr, p.lse ? p.lse + r0 : nullptr,
+                                                                             p.lse_lo ? p.lse_lo + r0 : nullptr);
+        if (cudaError_t err = cudaGetLastError()) return err;
+    }
+    return cudaSuccess;
+}
+
+size_t linear_logprobs_backward_workspace_bytes(const gar_linear_logprobs_grad_params_t& p, int64_t ldw) {
+    gar_linear_logprobs_grad_params_t q = p;
+    q.workspace = nullptr;
+    return GradPlan(q, ldw).space.used();
+}
+
+cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_params_t& p, int64_t ldx, int64_t ldw, int sm_count) {
+    cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
+    GradPlan plan(p, ldw);
+    if (cudaError_t err = plan.w.ready(sm_count, stream)) return err;
+    const Operand x{plan.x_rows, plan.rows, p.hidden, plan.ldx};
+    if (plan.rows > 0) {
+        if (plan.top)
+            if (cudaError_t err = cudaMemsetAsync(plan.top, 0, 4, stream)) return err;
+        RowsArgs r{};
+        r.src = static_cast<const unsigned short*>(p.x);
+        r.ld = ldx;
+        r.cols = p.hidden;
+        r.per_row = plan.ldx / 8;
+        r.pieces = plan.rows * r.per_row;
+        r.dst = reinterpret_cast<uint4*>(plan.x_rows);
+        r.targets = p.targets;
+        r.grad = p.grad_logprobs;
+        r.vocab = p.vocab;
+        r.coef = plan.coef;
+        r.top = plan.top;
+        r.aligned = on_16(p.x, ldx);
+        copy_rows_kernel<true><<<copy_blocks(r.pieces, sm_count), 256, 0, stream>>>(r);
+        if (cudaError_t err = cudaGetLastError()) return err;
+    }
+    SumTarget d{p.dtype, p.dx, plan.rows, p.hidden, p.lddx ? p.lddx : p.hidden, plan.parts, plan.pitch, plan.splits, plan.top};
+    for (int64_t v0 = 0; v0 < p.vocab; v0 += plan.piece) {
+        Operand w = plan.w.m;
+        w.p += v0 * w.ld * 2;
+        w.rows = std::min(plan.piece, p.vocab - v0);
+        const Operand dz{plan.dz, plan.rows, w.rows, plan.ld_dz};
+        if (plan.rows > 0) {
+            Maps maps;
+            LNArgs a{};
+            if (cudaError_t err = logits_maps(maps, a, p.dtype, x, w)) return err;
+            a.bias = p.bias;
+            a.col0 = v0;
+            a.vocab = p.vocab;
+            a.targets = p.targets;
+            a.lse = p.lse;
+            a.lse_lo = p.lse_lo;
+            a.coef = plan.coef;
+            a.top = plan.top;
+            a.y = plan.dz;
+            a.ldy = plan.ld_dz;
+            if (cudaError_t err = operand_map(&maps.out, p.dtype, dz, 64, 32)) return err;
+            if (cudaError_t err = launch<LN_DLOGITS>(p.dtype, a, maps, sm_count, stream)) return err;
+            if (p.dx)
+                if (cudaError_t err = launch_sum(d, dz, w, nullptr, nullptr, v0 > 0, sm_count, stream)) return err;
+        }
+        if (p.weight_grads) {
+            DenseWeightGrad g{};
+            g.dtype = p.dtype;
+            g.grads_dtype = p.grads_dtype;
+            g.workers = p.workers;
+            g.tokens = p.tokens;
+            g.out = w.rows;
+            g.in = p.hidden;
+            g.dy = plan.dz;
+            g.ld_dy = plan.ld_dz;
+            g.x = plan.x_rows;
+            g.ldx = plan.ldx;
+            const size_t gs = p.grads_dtype == GAR_F32 ? 4 : 2;
+            g.dw = static_cast<char*>(p.weight_grads) + size_t(v0) * size_t(p.hidden) * gs;
+            g.db = p.bias_grads ? static_cast<char*>(p.bias_grads) + size_t(v0) * gs : nullptr;
+            g.ld_grads = p.ld_grads;
+            g.top = plan.top;
+            g.workspace = plan.weight_space;
+            if (cudaError_t err = launch_dense_weight_grad(g, sm_count, stream)) return err;
+        }
+    }
+    return d.parts && plan.rows > 0 ? join_sum(d, sm_count, stream) : cudaSuccess;
+}
+
+// ---- the gated block --------------------------------------------------------------------------------
+namespace {
+struct GatedPlan {
+    Space space;
+    Input x, gate, up;
+    GatedPlan(const gar_gated_linear_params_t& p)
+        : space(p.workspace), x(space, p.x, p.rows, p.hidden, p.ldx), gate(space, p.w_gate, p.inner, p.hidden, p.ld_gate),
+          up(space, p.w_up, p.inner, p.hidden, p.ld_up) {}
+};
+struct GatedGradPlan {
+    Space   space;
+    Input   gate, up, dgate, dup;
+    int     splits;
+    int64_t pitch;
+    float*  parts = nullptr;
+    GatedGradPlan(const gar_gated_linear_grad_params_t& p)
+        : space(p.workspace), gate(space, p.w_gate, p.inner, p.hidden, p.ld_gate), up(space, p.w_up, p.inner, p.hidden, p.ld_up),
+          dgate(space, p.dgate, p.rows, p.inner, p.ld_dgate), dup(space, p.dup, p.rows, p.inner, p.ld_dup),
+          splits(splits_for(std::max<int64_t>(p.rows, 1), p.hidden, 2 * parts_of(p.inner, LN_K))), pitch(up_to(p.hidden, 4)) {
+        if (splits > 1) parts = reinterpret_cast<float*>(space.take(size_t(splits) * size_t(p.rows) * size_t(pitch) * 4));
+    }
+};
+}  // namespace
+
+size_t gated_linear_workspace_bytes(const gar_gated_linear_params_t& p) {
+    gar_gated_linear_params_t q = p;
+    q.workspace = nullptr;
+    return GatedPlan(q).space.used();
+}
+
+cudaError_t launch_gated_linear_forward(const gar_gated_linear_params_t& p, int sm_count) {
+    cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
+    GatedPlan plan(p);
+    for (Input* in : {&plan.x, &plan.gate, &plan.up})
+        if (cudaError_t err = in->ready(sm_count, stream)) return err;
+    Maps maps;
+    LNArgs a{};
+    if (cudaError_t err = logits_maps(maps, a, p.dtype, plan.x.m, plan.gate.m)) return err;
+    a.nt = int(parts_of(p.inner, LN_HALF));
+    if (cudaError_t err = operand_map(&maps.b1, p.dtype, plan.up.m, LN_K, LN_HALF)) return err;
+    a.act = p.act;
+    a.group_shift = p.group == 32 ? 5 : p.group == 64 ? 6 : 7;
+    a.groups = int(parts_of(p.inner, p.group));
+    a.bias = p.b_gate;
+    a.bias2 = p.b_up;
+    a.s0 = p.gate_saved;
+    a.s1 = p.up_saved;
+    a.y = p.y;
+    a.ldy = p.ldy;
+    a.out = on_16(p.y, p.ldy) ? OUT_WIDE : OUT_PLAIN;
+    if (a.out == OUT_WIDE)
+        if (cudaError_t err = operand_map(&maps.out, p.dtype, Operand{static_cast<const char*>(p.y), p.rows, p.inner, p.ldy}, 64, 32)) return err;
+    if (cudaError_t err = launch<LN_GATED>(p.dtype, a, maps, sm_count, stream)) return err;
+    if (!p.y_saved.q) return cudaSuccess;
+    gar_activation_params_t c{};
+    c.dtype = p.dtype;
+    c.act = GAR_ACT_IDENTITY;
+    c.group = p.group;
+    c.rows = p.rows;
+    c.cols = p.inner;
+    c.x = p.y;
+    c.ldx = p.ldy;
+    c.x_saved = p.y_saved;
+    c.stream = p.stream;
+    return launch_activation_forward(c);
+}
+
+size_t gated_linear_backward_workspace_bytes(const gar_gated_linear_grad_params_t& p) {
+    if (!p.dx) return 0;
+    gar_gated_linear_grad_params_t q = p;
+    q.workspace = nullptr;
+    return GatedGradPlan(q).space.used();
+}
+
+cudaError_t launch_gated_linear_backward(const gar_gated_linear_grad_params_t& p, int sm_count) {
+    cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
+    gar_activation_grad_params_t c{};
+    c.dtype = p.dtype;
+    c.act = p.act;
+    c.group = p.group;
+    c.rows = p.rows;
+    c.cols = p.inner;
+    c.dy = p.dy;
+    c.lddy = p.lddy;
+    c.x_saved = p.gate_saved;
+    c.up_saved = p.up_saved;
+    c.dx = p.dgate;
+    c.lddx = p.ld_dgate;
+    c.dup = p.dup;
+    c.lddup = p.ld_dup;
+    c.stream = p.stream;
+    if (cudaError_t err = launch_activation_backward(c)) return err;
+    if (!p.dx) return cudaSuccess;
+    GatedGradPlan plan(p);
+    for (Input* in : {&plan.gate, &plan.up, &plan.dgate, &plan.dup})
+        if (cudaError_t err = in->ready(sm_count, stream)) return err;
+    SumTarget d{p.dtype, p.dx, p.rows, p.hidden, p.lddx, plan.parts, plan.pitch, plan.splits, nullptr};
+    if (cudaError_t err = launch_sum(d, plan.dgate.m, plan.gate.m, &plan.dup.m, &plan.up.m, false, sm_count, stream)) return err;
+    return plan.parts ? join_sum(d, sm_count, stream) : cudaSuccess;
+}
+
+}  // namespace worker
+}  // namespace gar

@@ -38,14 +38,12 @@
 //
 // Hand-offs are mbarriers; every wait is bounded: a wait that gives up raises an error flag, all
 // roles leave their loops once what they have in flight has landed, and the CTA's tiles become NaN.
-#include <cuda.h>
-
 #include <algorithm>
 #include <atomic>
 
 #include "gar_internal.cuh"
-#include "mbar.cuh"
-#include "worker_common.cuh"
+#include "worker_linear.cuh"
+#include "worker_tensor.cuh"
 
 namespace gar {
 namespace worker {
@@ -126,77 +124,9 @@ struct WGArgs {
     int            columns;               // nt + 1 with a bias
     int            splits;                // parts a worker's tokens are cut into, each with a result of its own
     int            wide;                  // the result's rows start on 16 bytes: stored by TMA
+    const unsigned* top;                  // dy carries the power of two for this largest magnitude; null: none
 };
 
-// ---- tcgen05 ------------------------------------------------------------------------------------
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-// Operand descriptor.  MN-major, 128-byte swizzle: blocks of 64 columns `lbo` bytes apart, groups of
-// eight tokens 1024 bytes apart.  Bits [0,14) address / 16, [16,30) lbo / 16, [32,46) sbo / 16,
-// [46,48) = 1 (version), [61,64) = 2 (128-byte swizzle).
-__device__ __forceinline__ unsigned long long operand_desc(unsigned saddr, unsigned lbo, unsigned sbo, unsigned layout) {
-    return static_cast<unsigned long long>((saddr >> 4) & 0x3fffu) | (static_cast<unsigned long long>(lbo >> 4) << 16) |
-           (static_cast<unsigned long long>(sbo >> 4) << 32) | (1ull << 46) | (static_cast<unsigned long long>(layout) << 61);
-}
-// Instruction descriptor, kind::f16: fp32 accumulators (1 at bit 4), both operands bf16 (1) or
-// binary16 (0) at bits 7 and 10, both MN-major (bits 15, 16), N / 8 at bit 17, M / 16 at bit 24.
-__host__ __device__ constexpr unsigned instruction_desc(int type, int n) {
-    return (1u << 4) | (unsigned(type) << 7) | (unsigned(type) << 10) | (1u << 15) | (1u << 16) | (unsigned(n >> 3) << 17) |
-           (unsigned(2 * WG_M >> 4) << 24);
-}
-__device__ __forceinline__ void mma_f16(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-// arrives on the barrier of both CTAs once the instructions issued so far have finished
-__device__ __forceinline__ void mma_commit(unsigned long long* bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(kb_smem_u32(bar)), "h"(static_cast<unsigned short>(3)) : "memory");
-}
-// true in one lane of the warp
-__device__ __forceinline__ bool elect_one() {
-    unsigned r;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
-    return r != 0;
-}
-// ---- the pair -------------------------------------------------------------------------------------
-__device__ __forceinline__ unsigned cta_rank() {
-    unsigned r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void pair_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// this CTA's shared-memory address in CTA `rank` of the pair
-__device__ __forceinline__ unsigned pair_address(unsigned addr, unsigned rank) {
-    unsigned r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-// What is handed over lies in this CTA's own shared or tensor memory and is read by the tensor core
-// (async proxy, after this CTA's own proxy or tcgen05 fence), so the arrival orders nothing at cluster
-// scope: .release.cluster here waits for every load and store the warp has in flight, 1500 cycles a step.
-__device__ __forceinline__ void arrive_at_leader(unsigned long long* bar) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(pair_address(kb_smem_u32(bar), 0)) : "memory");
-}
-// this thread's lane of tensor memory, 32 consecutive columns
-__device__ __forceinline__ void tmem_ld32(unsigned taddr, float (&v)[32]) {
-    unsigned r[32];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-                   "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-                   "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-                 : "r"(taddr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-}
 // this thread's lane of tensor memory: 16 columns of either accumulator, there once the loads are waited for
 __device__ __forceinline__ void load_columns(unsigned sum, unsigned part, float (&a)[16], float (&b)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -238,33 +168,6 @@ __device__ __noinline__ void add_accumulator(unsigned sum, unsigned part, int co
     }
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
-}
-// into this CTA's shared memory, counted in on a barrier of either CTA of the pair
-__device__ __forceinline__ void tma_load_pair(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
-    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
-}
-
-// L2 policy of data that is not touched again: the result (738 MB for 11 workers of 4096 x 4096) passes
-// through L2 without driving out the operands, which other tiles still read.
-__device__ __forceinline__ unsigned long long evict_first() {
-    unsigned long long p;
-    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
-    return p;
-}
-// a piece of the result from shared memory (what lies outside the matrix is not written)
-__device__ __forceinline__ void tma_store(const CUtensorMap* map, unsigned src, int x, int y, int z, unsigned long long policy) {
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group.L2::cache_hint [%0, {%2, %3, %4}], [%1], %5;"
-                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z), "l"(policy) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-template <int LEFT> __device__ __forceinline__ void tma_store_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
-__device__ __forceinline__ void tma_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
-
 // ---- tiles --------------------------------------------------------------------------------------
 struct Tile {
     int     worker, m, n;        // n == nt: the bias
@@ -325,12 +228,6 @@ __device__ __forceinline__ Walk walk_of(const WGArgs& a, unsigned pair, unsigned
     if (MODE != WG_PANEL) return {pair, pairs, tiles};
     return {unsigned(uint64_t(tiles) * pair / pairs), 1u, unsigned(uint64_t(tiles) * (pair + 1) / pairs)};
 }
-
-// Slot of a running number in a ring of DEPTH buffers, and the parity of the slot's round.
-template <int DEPTH> struct Ring {
-    unsigned slot, parity;
-    __device__ __forceinline__ explicit Ring(unsigned number) : slot(number % DEPTH), parity((number / DEPTH) & 1u) {}
-};
 
 // The two halves of tensor memory as accumulators.  A tile's first chunk of tokens is summed in the half `sum`, where
 // the store warps keep the tile's sum; its other chunks go through the other half, one after the other.  The next
@@ -438,14 +335,6 @@ __device__ __forceinline__ void load_dy(const WGArgs& a, const Tile& t, int64_t 
     }
 }
 
-__device__ __forceinline__ void put_shared(unsigned at, const uint4& v) {
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-__device__ __forceinline__ uint4 get_shared(unsigned at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-    return v;
-}
 // The elements of a chunk at `off` bytes of a row of `bytes` bytes that lie in the row.
 template <typename G>
 __device__ __forceinline__ void store_elements(char* dst, const uint4& v, int off, int bytes) {
@@ -461,7 +350,7 @@ __device__ __forceinline__ void store_elements(char* dst, const uint4& v, int of
 
 // This lane's row of a piece of the accumulators (128 bytes), as G.
 template <typename G>
-__device__ __forceinline__ void read_piece(unsigned src, bool filled, unsigned* piece) {
+__device__ __forceinline__ void read_piece(unsigned src, bool filled, float by, unsigned* piece) {
     float v[32];
 #pragma unroll
     for (int h = 0; h < 4 / int(sizeof(G)); ++h) {
@@ -470,6 +359,10 @@ __device__ __forceinline__ void read_piece(unsigned src, bool filled, unsigned* 
         } else {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = 0.f;
+        }
+        if (by != 1.f) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= by;
         }
         if constexpr (sizeof(G) == 4) {
 #pragma unroll
@@ -491,13 +384,13 @@ __device__ __forceinline__ void read_piece(unsigned src, bool filled, unsigned* 
 // The accumulator's rows of a warp to the result through TMA, in pieces of 128 bytes a row staged in `STAGES` buffers
 // in turn (piece `n`: the running number).  Not inlined: its registers are no burden on the other paths.
 template <typename G, int STAGES>
-__device__ __noinline__ unsigned store_aligned(unsigned src, bool filled, unsigned stages, unsigned n, const CUtensorMap* map, int x, int y, int z, int cols) {
+__device__ __noinline__ unsigned store_aligned(unsigned src, bool filled, float by, unsigned stages, unsigned n, const CUtensorMap* map, int x, int y, int z, int cols) {
     const int lane = threadIdx.x % 32;
     constexpr int COLS = 128 / int(sizeof(G));
     const unsigned long long policy = evict_first();
     for (int c0 = 0; c0 < cols; c0 += COLS, ++n) {
         unsigned piece[32];
-        read_piece<G>(src + unsigned(c0), filled, piece);
+        read_piece<G>(src + unsigned(c0), filled, by, piece);
         // the staging buffer's last copy out has been read; 16-byte chunks in the 128-byte swizzle
         const unsigned stage = stages + n % STAGES * 4096u;
         if (lane == 0) tma_store_read<STAGES - 1>();
@@ -521,7 +414,7 @@ __device__ __noinline__ unsigned store_aligned(unsigned src, bool filled, unsign
 // 4096, 2048 x 2048, fp32 166 to 169 (163 to 166); 11 x 128, 2048 x 2048, fp32 70 (43).  A row's ends by the row's lane, or by eight lanes per row in a loop
 // of their own, were slower (90 and 99 us for the last).
 template <typename G>
-__device__ __noinline__ void store_anywhere(unsigned src, bool filled, unsigned stage, char* first, int64_t row_bytes, int bytes, int rows) {
+__device__ __noinline__ void store_anywhere(unsigned src, bool filled, float factor, unsigned stage, char* first, int64_t row_bytes, int bytes, int rows) {
     const int lane = threadIdx.x % 32;
     const unsigned by = unsigned(reinterpret_cast<uintptr_t>(first + lane * row_bytes)) & 31u;
     unsigned carry[8];
@@ -532,7 +425,7 @@ __device__ __noinline__ void store_anywhere(unsigned src, bool filled, unsigned 
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = carry[j];
         if (at < bytes) {
-            read_piece<G>(src + unsigned(at / int(sizeof(G))), filled, x + 8);
+            read_piece<G>(src + unsigned(at / int(sizeof(G))), filled, factor, x + 8);
         } else {
 #pragma unroll
             for (int j = 8; j < 40; ++j) x[j] = 0;
@@ -906,6 +799,7 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
     } else if (warp >= WG_STORE_WARP0) {
         const int quarter = warp - WG_STORE_WARP0;               // == warp % 4: tensor-memory lanes 32 quarter ..
         unsigned n_piece = 0;
+        const float by = a.top ? power_for(*a.top, true) : 1.f;
         Halves acc;
         for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
             const Tile t = tile_at<MODE>(a, i);
@@ -932,16 +826,16 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
                 float v[32];
                 if (t.steps) tmem_ld32(src, v);
                 else v[0] = 0.f;
-                if (o0 + lane < a.out) static_cast<G*>(a.db)[int64_t(t.plane) * a.ld_grads + o0 + lane] = Elem<G>::narrow(v[0]);
+                if (o0 + lane < a.out) static_cast<G*>(a.db)[int64_t(t.plane) * a.ld_grads + o0 + lane] = Elem<G>::narrow(v[0] * by);
             } else {
                 const int rows = int(min(int64_t(32), a.out - o0));
                 const int64_t left = a.in - int64_t(t.n) * WG_N;
                 const int cols = left < WG_N ? int(left) : WG_N;
                 G* dw = static_cast<G*>(a.dw) + int64_t(t.plane) * a.ld_grads + o0 * a.pitch + int64_t(t.n) * WG_N;
                 if (a.wide) {
-                    if (rows > 0) n_piece = store_aligned<G, P::OUT>(src, t.steps > 0, kb_smem_u32(sm.out[quarter][0]), n_piece, &map_dw, t.n * WG_N, int(o0), t.plane, cols);
+                    if (rows > 0) n_piece = store_aligned<G, P::OUT>(src, t.steps > 0, by, kb_smem_u32(sm.out[quarter][0]), n_piece, &map_dw, t.n * WG_N, int(o0), t.plane, cols);
                 } else if (rows > 0) {
-                    store_anywhere<G>(src, t.steps > 0, kb_smem_u32(sm.out[quarter][0]), reinterpret_cast<char*>(dw),
+                    store_anywhere<G>(src, t.steps > 0, by, kb_smem_u32(sm.out[quarter][0]), reinterpret_cast<char*>(dw),
                                       a.pitch * int64_t(sizeof(G)), cols * int(sizeof(G)), rows);
                 }
             }
@@ -1010,33 +904,6 @@ __global__ void __launch_bounds__(128) join_parts_kernel(const float* parts, int
 }
 
 // ---- launch -------------------------------------------------------------------------------------
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's entry point, looked up once.
-EncodeTiled encode_tiled() {
-    static const EncodeTiled found = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult how;
-        const cudaError_t err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &how);
-        return err == cudaSuccess && how == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(p) : nullptr;
-    }();
-    return found;
-}
-
-// [depth][rows][cols] with strides of `pitch` and `plane` bytes; boxes of box x box_rows
-cudaError_t make_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t cols, int64_t rows, int depth,
-                     int64_t pitch, int64_t plane, int box, int box_rows, CUtensorMapSwizzle swizzle) {
-    const EncodeTiled encode = encode_tiled();
-    if (!encode) return cudaErrorNotSupported;
-    const cuuint64_t dims[3] = {cuuint64_t(cols), cuuint64_t(rows), cuuint64_t(depth)};
-    const cuuint64_t strides[2] = {cuuint64_t(pitch), cuuint64_t(plane)};
-    const cuuint32_t boxes[3] = {cuuint32_t(box), cuuint32_t(box_rows), 1}, steps[3] = {1, 1, 1};
-    const CUresult r = encode(map, type, 3, const_cast<void*>(base), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
 // the workers' tokens (at least one row, so that the map is valid; none is read without tokens)
 cudaError_t make_token_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t cols, int64_t tokens, int workers,
                            int64_t pitch, int box, CUtensorMapSwizzle swizzle) {
@@ -1101,24 +968,56 @@ bool panel_applies(const gar_weight_grad_params_t& p, int64_t ld_dy) {
 // all).  One worker, 4000 tokens, 200 x 300: 17 us, whole 47; 2 x 4096 tokens, 513 x 250: 29 us, whole 115.
 // A panel's tokens stay whole (WG_PANEL's tiles know no parts).
 constexpr int WG_PAIRS = 74;
-int splits_of(const gar_weight_grad_params_t& p, int64_t ld_dy) {
-    if (panel_applies(p, ld_dy)) return 1;
-    const int64_t mt = (p.out_features + 2 * WG_M - 1) / (2 * WG_M), columns = (p.in_features + WG_N - 1) / WG_N + (p.bias_grads ? 1 : 0);
+int splits_of(int workers, int64_t tokens, int64_t out, int64_t in, bool bias) {
+    const int64_t mt = (out + 2 * WG_M - 1) / (2 * WG_M), columns = (in + WG_N - 1) / WG_N + (bias ? 1 : 0);
     if (mt > WG_PAIRS || columns > WG_PAIRS) return 1;
-    const int64_t tiles = p.workers * mt * columns, steps = (p.tokens + WG_K - 1) / WG_K;
+    const int64_t tiles = workers * mt * columns, steps = (tokens + WG_K - 1) / WG_K;
     const int64_t s = std::min<int64_t>(WG_PAIRS / tiles, steps / 4);
     return s > 1 ? int(std::min<int64_t>(s, 16)) : 1;
 }
+int splits_of(const gar_weight_grad_params_t& p, int64_t ld_dy) {
+    return panel_applies(p, ld_dy) ? 1 : splits_of(p.workers, p.tokens, p.out_features, p.in_features, p.bias_grads != nullptr);
+}
 int64_t round4(int64_t v) { return (v + 3) / 4 * 4; }
 // one part of one worker: weights with rows of whole 16 bytes, biases
-int64_t part_floats(const gar_weight_grad_params_t& p) { return p.out_features * round4(p.in_features) + round4(p.out_features); }
+int64_t part_floats(int64_t out, int64_t in) { return out * round4(in) + round4(out); }
+int64_t part_floats(const gar_weight_grad_params_t& p) { return part_floats(p.out_features, p.in_features); }
 
 template <typename G>
-cudaError_t join_parts(const WGArgs& a, const gar_weight_grad_params_t& p, cudaStream_t stream) {
-    const dim3 grid(unsigned((p.in_features + 1 + 127) / 128), unsigned(p.workers * p.out_features));
-    join_parts_kernel<G><<<grid, 128, 0, stream>>>(static_cast<const float*>(a.dw), a.ld_grads, a.pitch, a.splits, p.workers, p.out_features,
-                                                   p.in_features, static_cast<G*>(p.weight_grads), static_cast<G*>(p.bias_grads), p.ld_grads);
+cudaError_t join_parts_as(const WGArgs& a, void* dw, void* db, int64_t ld_grads, cudaStream_t stream) {
+    const dim3 grid(unsigned((a.in + 1 + 127) / 128), unsigned(a.workers * a.out));
+    join_parts_kernel<G><<<grid, 128, 0, stream>>>(static_cast<const float*>(a.dw), a.ld_grads, a.pitch, a.splits, a.workers, a.out, a.in,
+                                                   static_cast<G*>(dw), static_cast<G*>(db), ld_grads);
     return cudaGetLastError();
+}
+cudaError_t join_parts(int grads_dtype, const WGArgs& a, void* dw, void* db, int64_t ld_grads, cudaStream_t stream) {
+    return grads_dtype == GAR_F32    ? join_parts_as<float>(a, dw, db, ld_grads, stream)
+           : grads_dtype == GAR_BF16 ? join_parts_as<__nv_bfloat16>(a, dw, db, ld_grads, stream) : join_parts_as<__half>(a, dw, db, ld_grads, stream);
+}
+// The result's place and type: the caller's, or (splits > 1) fp32 parts in `parts`.  The type that the kernel stores.
+int place_result(WGArgs& a, void* dw, void* db, int64_t ld_grads, int grads_dtype, void* parts) {
+    a.dw = dw;
+    a.db = db;
+    a.pitch = a.in;
+    a.ld_grads = ld_grads;
+    if (a.splits > 1) {
+        grads_dtype = GAR_F32;
+        a.dw = parts;
+        a.pitch = round4(a.in);
+        a.ld_grads = part_floats(a.out, a.in);
+        a.db = db ? static_cast<float*>(parts) + a.out * a.pitch : nullptr;
+    }
+    const int64_t gs = grads_dtype == GAR_F32 ? 4 : 2;
+    a.wide = reinterpret_cast<uintptr_t>(a.dw) % 16 == 0 && (a.workers * a.splits == 1 || a.ld_grads * gs % 16 == 0) && a.pitch * gs % 16 == 0;
+    return grads_dtype;
+}
+cudaError_t result_map(CUtensorMap* map, const WGArgs& a, int grads_dtype) {
+    const int64_t gs = grads_dtype == GAR_F32 ? 4 : 2;
+    const int planes = a.workers * a.splits;
+    const CUtensorMapDataType gt = grads_dtype == GAR_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : grads_dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const int64_t pitch = a.pitch * gs, plane = planes > 1 ? a.ld_grads * gs : pitch * a.out;
+    return make_map(map, gt, a.dw, a.in, a.out, planes, pitch, plane, int(128 / gs), 32, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 }  // namespace
@@ -1130,13 +1029,10 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     a.scales = p.x_saved.scales;
     a.ldq = p.x_saved.ldq;
     a.lengths = p.lengths;
-    a.dw = p.weight_grads;
-    a.db = p.bias_grads;
     a.tokens = p.tokens;
     a.out = p.out_features;
     a.in = p.in_features;
     a.ld_dy = ld_dy;
-    a.ld_grads = p.ld_grads;
     a.workers = p.workers;
     a.groups = int((p.in_features + p.group - 1) / p.group);
     a.group_shift = p.group == 32 ? 5 : p.group == 64 ? 6 : 7;
@@ -1144,20 +1040,8 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     a.nt = int((p.in_features + WG_N - 1) / WG_N);
     a.columns = a.nt + (p.bias_grads ? 1 : 0);
     if (int64_t(a.mt) * a.columns >= (int64_t(1) << 30) / a.workers) return cudaErrorInvalidConfiguration;
-    a.pitch = p.in_features;
     a.splits = p.workspace ? splits_of(p, ld_dy) : 1;
-    // parts are fp32 results in the workspace
-    int grads_dtype = p.grads_dtype;
-    if (a.splits > 1) {
-        grads_dtype = GAR_F32;
-        a.dw = p.workspace;
-        a.pitch = round4(p.in_features);
-        a.ld_grads = part_floats(p);
-        a.db = p.bias_grads ? static_cast<float*>(p.workspace) + p.out_features * a.pitch : nullptr;
-    }
-    const int64_t gs = grads_dtype == GAR_F32 ? 4 : 2;
-    const int planes = p.workers * a.splits;
-    a.wide = reinterpret_cast<uintptr_t>(a.dw) % 16 == 0 && (planes == 1 || a.ld_grads * gs % 16 == 0) && a.pitch * gs % 16 == 0;
+    const int grads_dtype = place_result(a, p.weight_grads, p.bias_grads, p.ld_grads, p.grads_dtype, p.workspace);
 
     const CUtensorMapDataType type = p.dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
@@ -1188,20 +1072,46 @@ cudaError_t launch_weight_grad(const gar_weight_grad_params_t& p, int64_t ld_dy,
     }
     if (mode == WG_PLAIN_DY) map_dy = map_x;      // not used
     else if (cudaError_t err = make_token_map(&map_dy, type, a.dy, p.out_features, p.tokens, p.workers, a.ld_dy * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
-    if (!a.wide) {
-        map_dw = map_x;                           // not used
-    } else {
-        const CUtensorMapDataType gt = grads_dtype == GAR_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                       : grads_dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-        const int64_t pitch = a.pitch * gs, plane = planes > 1 ? a.ld_grads * gs : pitch * p.out_features;
-        if (cudaError_t err = make_map(&map_dw, gt, a.dw, p.in_features, p.out_features, planes, pitch, plane, int(128 / gs), 32,
-                                       CU_TENSOR_MAP_SWIZZLE_128B)) return err;
-    }
+    map_dw = map_x;                               // not used unless
+    if (a.wide)
+        if (cudaError_t err = result_map(&map_dw, a, grads_dtype)) return err;
     const cudaError_t err = p.dtype == GAR_BF16 ? launch_by_mode<__nv_bfloat16>(mode, grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream)
                                                 : launch_by_mode<__half>(mode, grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
-    if (err != cudaSuccess || a.splits == 1) return err;
-    return p.grads_dtype == GAR_F32    ? join_parts<float>(a, p, stream)
-           : p.grads_dtype == GAR_BF16 ? join_parts<__nv_bfloat16>(a, p, stream) : join_parts<__half>(a, p, stream);
+    return err != cudaSuccess || a.splits == 1 ? err : join_parts(p.grads_dtype, a, p.weight_grads, p.bias_grads, p.ld_grads, stream);
+}
+
+size_t dense_weight_grad_workspace_bytes(int workers, int64_t tokens, int64_t out, int64_t in, bool bias) {
+    const int splits = splits_of(workers, tokens, out, in, bias);
+    return splits > 1 ? gar::align256(size_t(splits) * workers * size_t(part_floats(out, in)) * 4) : 0;
+}
+
+cudaError_t launch_dense_weight_grad(const DenseWeightGrad& g, int sm_count, cudaStream_t stream) {
+    WGArgs a{};
+    a.dy = g.dy;
+    a.tokens = g.tokens;
+    a.out = g.out;
+    a.in = g.in;
+    a.ld_dy = g.ld_dy;
+    a.workers = g.workers;
+    a.group_shift = 7;                            // no codes are read
+    a.groups = int((g.in + 127) / 128);
+    a.mt = int((g.out + 2 * WG_M - 1) / (2 * WG_M));
+    a.nt = int((g.in + WG_N - 1) / WG_N);
+    a.columns = a.nt + (g.db ? 1 : 0);
+    a.top = g.top;
+    if (int64_t(a.mt) * a.columns >= (int64_t(1) << 30) / a.workers) return cudaErrorInvalidConfiguration;
+    a.splits = splits_of(g.workers, g.tokens, g.out, g.in, g.db != nullptr);
+    const int grads_dtype = place_result(a, g.dw, g.db, g.ld_grads, g.grads_dtype, g.workspace);
+    const CUtensorMapDataType type = g.dtype == GAR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    CUtensorMap map_x, map_dy, map_dw;
+    if (cudaError_t err = make_token_map(&map_x, type, g.x, g.in, g.tokens, g.workers, g.ldx * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+    if (cudaError_t err = make_token_map(&map_dy, type, g.dy, g.out, g.tokens, g.workers, g.ld_dy * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+    map_dw = map_x;                               // not used unless
+    if (a.wide)
+        if (cudaError_t err = result_map(&map_dw, a, grads_dtype)) return err;
+    const cudaError_t err = g.dtype == GAR_BF16 ? launch_by_grads<__nv_bfloat16, WG_RESTORED>(grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream)
+                                                : launch_by_grads<__half, WG_RESTORED>(grads_dtype, a, map_dy, map_x, map_dw, sm_count, stream);
+    return err != cudaSuccess || a.splits == 1 ? err : join_parts(g.grads_dtype, a, g.dw, g.db, g.ld_grads, stream);
 }
 
 // Every 256 outputs restore the activation once more.  Measured, with a workspace against without (8 workers, 2048
