@@ -18,17 +18,6 @@ namespace {
 constexpr int CK_THREADS = 256;
 constexpr int CK_TASKS = 2;                            // per thread: all loads before the arithmetic
 
-// Division of a task number by the tasks per row: exact for numerators below 2^31.
-struct FastDiv {
-    unsigned d = 1, mul = 1, shift = 0;
-    FastDiv() = default;
-    explicit FastDiv(unsigned divisor) : d(divisor) {
-        while ((1ull << shift) < d) ++shift;
-        mul = unsigned(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
-    }
-    __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
-};
-
 // How a matrix lies: any rows; rows of 16-bit elements that start on 4 bytes (CK_WORD); rows that start
 // on 16 bytes; or (DENSE) every matrix of the call without
 // gaps between its rows and of whole groups, so that a task's number gives its place everywhere and

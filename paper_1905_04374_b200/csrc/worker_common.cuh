@@ -114,6 +114,17 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
     return r;
 }
 
+// Division of a task number by the tasks per row: exact for numerators below 2^31.
+struct FastDiv {
+    unsigned d = 1, mul = 1, shift = 0;
+    FastDiv() = default;
+    explicit FastDiv(unsigned divisor) : d(divisor) {
+        while ((1ull << shift) < d) ++shift;
+        mul = unsigned(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
+};
+
 // ---- launchers (arguments checked by the C entry points) ------------------------------------
 cudaError_t launch_logprobs(const gar_logprobs_params_t& p, int64_t ld, int sm_count);
 cudaError_t launch_logprobs_backward(const gar_logprobs_grad_params_t& p, int64_t ld, int64_t ldo, int sm_count);

@@ -17,7 +17,8 @@ struct DropoutArgs {
     const void *x, *residual;
     void*       y;
     int64_t     ldx, ldr, ldy, row0, cols;
-    unsigned    tasks, per_row;                        // of this launch; of a row
+    unsigned    tasks;                                 // of this launch
+    FastDiv     per_row;                               // tasks of a row
     int64_t     blocks0;                               // generator blocks before this launch's
     unsigned    limit;                                 // of 2^16: dropped below
     float       scale;
@@ -81,24 +82,35 @@ __device__ __forceinline__ void store8(T* p, int count, const float (&v)[8]) {
         if (i < count) p[i] = Elem<T>::narrow(v[i]);
 }
 
-// VEC: rows start on 16 bytes (fp32: on 16 too, eight elements are two words)
-template <typename T, bool VEC, bool RESIDUAL>
+// VEC: rows start on 16 bytes (fp32: on 16 too, eight elements are two words).  DENSE: besides, no matrix has gaps between
+// its rows and these are whole tasks, so that a task's number is its place.
+enum Layout { DO_ANY = 0, DO_VEC = 1, DO_DENSE = 2 };
+template <typename T, int LAYOUT, bool RESIDUAL>
 __global__ void __launch_bounds__(DO_THREADS) dropout_kernel(const DropoutArgs a) {
     const uint64_t offset = a.offset + (a.counter ? *a.counter : 0);
+    constexpr bool VEC = LAYOUT != DO_ANY;
     float x[DO_TASKS][8], r[DO_TASKS][8];
     int64_t row[DO_TASKS], col[DO_TASKS];
     int count[DO_TASKS];
 #pragma unroll
     for (int k = 0; k < DO_TASKS; ++k) {
-        const unsigned n = (blockIdx.x * DO_TASKS + k) * DO_THREADS + threadIdx.x, in = n / a.per_row;
-        row[k] = a.row0 + in;
-        col[k] = int64_t(n - in * a.per_row) * 8;
-        const int64_t left = a.cols - col[k];
-        count[k] = n >= a.tasks ? 0 : left < 8 ? int(left) : 8;
+        const unsigned n = (blockIdx.x * DO_TASKS + k) * DO_THREADS + threadIdx.x;
+        if (LAYOUT == DO_DENSE) {
+            row[k] = 0;
+            col[k] = (a.blocks0 + n) * 8;
+            count[k] = n < a.tasks ? 8 : 0;
+        } else {
+            const unsigned in = a.per_row.quotient(n);
+            row[k] = a.row0 + in;
+            col[k] = int64_t(n - in * a.per_row.d) * 8;
+            const int64_t left = a.cols - col[k];
+            count[k] = n >= a.tasks ? 0 : left < 8 ? int(left) : 8;
+        }
         if (count[k] == 0) continue;
         load8<T, VEC>(static_cast<const T*>(a.x) + row[k] * a.ldx + col[k], count[k], x[k]);
         if (RESIDUAL) load8<T, VEC>(static_cast<const T*>(a.residual) + row[k] * a.ldr + col[k], count[k], r[k]);
     }
+    const unsigned limit = a.limit << 16;              // (limit = 2^16: nothing is kept, scale 0)
 #pragma unroll
     for (int k = 0; k < DO_TASKS; ++k) {
         if (count[k] == 0) continue;
@@ -106,9 +118,11 @@ __global__ void __launch_bounds__(DO_THREADS) dropout_kernel(const DropoutArgs a
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const unsigned bits = i & 1 ? d.w[i / 2] >> 16 : d.w[i / 2] & 0xffffu;
-            const float v = bits >= a.limit ? x[k][i] * a.scale : 0.f;
-            y[i] = RESIDUAL ? v + r[k][i] : v;
+            // a half against the limit: both in the high half of a word, where what is below does not matter
+            const bool kept = (i & 1 ? d.w[i / 2] : d.w[i / 2] << 16) >= limit && a.limit < 65536u;
+            const float none = RESIDUAL ? r[k][i] : 0.f;
+            const float some = RESIDUAL ? fmaf(x[k][i], a.scale, none) : x[k][i] * a.scale;
+            y[i] = kept ? some : none;
         }
         store8<T, VEC>(static_cast<T*>(a.y) + row[k] * a.ldy + col[k], count[k], y);
     }
@@ -122,19 +136,23 @@ template <typename T>
 cudaError_t launch_as(const gar_dropout_params_t& p, DropoutArgs& a) {
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     const bool vec = wide<T>(p.x, p.ldx) && wide<T>(p.residual, p.ld_residual) && wide<T>(p.y, p.ldy);
-    const int64_t step = ((int64_t(1) << 31) - DO_THREADS * DO_TASKS) / a.per_row;         // rows of a launch
+    const unsigned per_row = a.per_row.d;
+    const bool dense = vec && p.cols % 8 == 0 && p.ldx == p.cols && p.ldy == p.cols && (!p.residual || p.ld_residual == p.cols);
+    const int64_t step = ((int64_t(1) << 31) - DO_THREADS * DO_TASKS) / per_row;           // rows of a launch
     for (int64_t r0 = 0; r0 < p.rows; r0 += step) {
         const int64_t n = p.rows - r0 < step ? p.rows - r0 : step;
         a.row0 = r0;
-        a.blocks0 = r0 * a.per_row;
-        a.tasks = unsigned(n * a.per_row);
+        a.blocks0 = r0 * per_row;
+        a.tasks = unsigned(n * per_row);
         const unsigned blocks = (a.tasks + DO_THREADS * DO_TASKS - 1) / (DO_THREADS * DO_TASKS);
         if (p.residual) {
-            if (vec) dropout_kernel<T, true, true><<<blocks, DO_THREADS, 0, stream>>>(a);
-            else dropout_kernel<T, false, true><<<blocks, DO_THREADS, 0, stream>>>(a);
+            if (dense) dropout_kernel<T, DO_DENSE, true><<<blocks, DO_THREADS, 0, stream>>>(a);
+            else if (vec) dropout_kernel<T, DO_VEC, true><<<blocks, DO_THREADS, 0, stream>>>(a);
+            else dropout_kernel<T, DO_ANY, true><<<blocks, DO_THREADS, 0, stream>>>(a);
         } else {
-            if (vec) dropout_kernel<T, true, false><<<blocks, DO_THREADS, 0, stream>>>(a);
-            else dropout_kernel<T, false, false><<<blocks, DO_THREADS, 0, stream>>>(a);
+            if (dense) dropout_kernel<T, DO_DENSE, false><<<blocks, DO_THREADS, 0, stream>>>(a);
+            else if (vec) dropout_kernel<T, DO_VEC, false><<<blocks, DO_THREADS, 0, stream>>>(a);
+            else dropout_kernel<T, DO_ANY, false><<<blocks, DO_THREADS, 0, stream>>>(a);
         }
         if (cudaError_t err = cudaGetLastError()) return err;
     }
@@ -150,7 +168,7 @@ cudaError_t launch_dropout(const gar_dropout_params_t& p, unsigned limit, float 
     a.cols = p.cols;
     const int64_t per_row = (p.cols + 7) / 8;
     if (per_row >= int64_t(1) << 30) return cudaErrorInvalidConfiguration;
-    a.per_row = unsigned(per_row);
+    a.per_row = FastDiv(unsigned(per_row));
     a.limit = limit;
     a.scale = scale;
     a.offset = p.offset;

@@ -9,10 +9,15 @@
 //                  B lie with the contraction along their rows (K-major), or B across them (MN-major: the
 //                  gradient at the inputs, dz W, reads W as it lies)
 //   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
-//   store warps    two groups of four, one per half of tensor memory, so that a tile's epilogue has the time of
-//                  two tiles' products; a thread has one row of the tile, 32 columns at a time
+//   store warps    two groups of four, each with half of a tile's columns, while the next tile's products run
+//                  into the other half of tensor memory; a thread has one row, 32 columns at a time
 // and four epilogues (enum Epilogue).  A thread owning a row makes the softmax's statistics, the group
-// maxima of the checkpoints and the row's target its own affair: no exchange between threads.
+// maxima of the checkpoints and the row's target its own affair.
+// Tiles are as wide as the rule in width_for makes them, 256 columns at most.
+//
+// The tensor core truncates what it adds to an accumulator: sums over k terms come out short by 1.0e-9 k of themselves
+// (operands of random signs; measured from k = 512 to 4096: lse off by -2.9e-6, -5.9e-6, -1.2e-5, -2.5e-5, all rows alike
+// to a tenth of that).  The logits, whose log probabilities are fp32 results, are multiplied by 1 + 1e-9 k.
 //
 // Every wait is bounded (mbar.cuh); a pair whose wait gave up fills its tiles with NaN.
 #include <algorithm>
@@ -36,7 +41,8 @@ constexpr int LN_COPY_WARP = 0, LN_MMA_WARP = 1, LN_ALLOC_WARP = 2;
 constexpr int LN_STORE_WARP0 = 4, LN_STORE_WARPS = 8;
 constexpr int LN_THREADS = 32 * (LN_STORE_WARP0 + LN_STORE_WARPS);
 constexpr int LN_GROUP_M = 8;                         // (pair) row tiles that go round a column tile together
-constexpr int LN_PAIRS = 74;                          // pairs of SMs, for the rules that cut work into parts
+constexpr int LN_PAIRS = 74;                          // pairs of SMs, for the rules that cut work into parts and tiles
+constexpr float LN_SHORT = 1.0e-9f;                   // of a sum, lost per term
 
 // What becomes of a tile.
 //   LN_SCORES   z: maximum and sum of exponentials of each row's 256 columns, and the target's z
@@ -49,12 +55,14 @@ enum Out { OUT_WIDE = 0, OUT_PLAIN = 1, OUT_PART = 2, OUT_ADD = 3 };    // 16 bi
 struct LNArgs {
     int64_t        rows, cols;            // of the result (LN_SCORES, LN_DLOGITS: columns from col0 on)
     int            mt, nt, splits;        // pair row tiles, column tiles, parts of the contraction
+    int            width;                 // columns of a tile (LN_GATED: g's and u's together)
+    float          whole;                 // logits: 1 + what the tensor core's sums are short by
     int            steps0, steps;         // steps of the first pair of operands, of both together
-    int            act, group_shift, groups, out;
+    int            group_shift, groups, out;
     int64_t        col0, vocab;           // first column of this launch, columns there are
     const void *   bias, *bias2;          // 16-bit, or null
     const int64_t* targets;
-    float2*        parts;                 // LN_SCORES [rows][nt]: maximum, sum
+    float2*        parts;                 // LN_SCORES [rows][2 nt]: maximum, sum
     float*         target_z;              // LN_SCORES [rows]
     const float *  lse, *lse_lo, *coef;   // LN_DLOGITS [rows]
     const unsigned* top;                  // the largest |coef|, as bits, where coefficients carry a power of two; or null
@@ -67,7 +75,7 @@ struct __align__(1024) LNSmem {
     uint8_t  a[LN_RING][LN_TILE];
     uint8_t  b[LN_RING][LN_TILE];
     uint8_t  out[LN_STORE_WARPS][32 * 128];               // a store warp's piece: 32 rows of 128 bytes
-    float    add[LN_STORE_WARPS][LN_N];                   // the tile's biases, -inf for columns that do not exist
+    float    add[LN_STORE_WARPS][LN_N];                   // a warp's biases, -inf for columns that do not exist
     unsigned long long empty[LN_RING], acc_full[2];       // the slots are read; the accumulators are complete
     unsigned long long full[LN_RING], acc_empty[2];       // the leading CTA's are used, for both
     unsigned tmem_base;
@@ -136,6 +144,21 @@ __device__ __forceinline__ void add32(float (&v)[32], const float* add) {
         v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
     }
 }
+// the logits of 32 columns: the sums made whole, the biases added
+__device__ __forceinline__ void logits32(float (&v)[32], float whole, bool adds, const float* add) {
+    const f32x2 by = pack2(whole, whole);
+    if (adds) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(add + j);
+            unpack2(fma2(pack2(v[j], v[j + 1]), by, pack2(b.x, b.y)), v[j], v[j + 1]);
+            unpack2(fma2(pack2(v[j + 2], v[j + 3]), by, pack2(b.z, b.w)), v[j + 2], v[j + 3]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) unpack2(mul2(pack2(v[j], v[j + 1]), by), v[j], v[j + 1]);
+    }
+}
 
 // 32 values as T to the first or second half of this lane's row of the staged piece
 template <typename T>
@@ -156,17 +179,26 @@ __device__ __forceinline__ void tma_put(const CUtensorMap* map, unsigned src, in
                  ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-// The staged piece (32 rows of 64 16-bit elements) to rows that start anywhere.
+// The staged piece (32 rows of 64 16-bit elements) to rows that start anywhere, eight rows' loads and stores at a time.
 __device__ __forceinline__ void store_plain(unsigned stage, int lane, unsigned short* dst, int64_t ld, int rows, int cols) {
-    for (int r = 0; r < rows; ++r) {
-        unsigned w;
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(stage + r * 128 + (((lane / 4) ^ (r & 7)) << 4) + (lane & 3) * 4));
-        unsigned short* p = dst + r * ld + 2 * lane;
-        if (2 * lane + 1 < cols && reinterpret_cast<uintptr_t>(p) % 4 == 0) {
-            *reinterpret_cast<unsigned*>(p) = w;
-        } else {
-            if (2 * lane < cols) p[0] = static_cast<unsigned short>(w);
-            if (2 * lane + 1 < cols) p[1] = static_cast<unsigned short>(w >> 16);
+    const int c = 2 * lane;
+    dst += c;
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        unsigned w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[k]) : "r"(stage + (r0 + k) * 128 + (((lane / 4) ^ k) << 4) + (lane & 3) * 4));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (r0 + k >= rows) break;
+            if (c + 1 < cols && (reinterpret_cast<uintptr_t>(dst) & 2) == 0) {
+                *reinterpret_cast<unsigned*>(dst) = w[k];
+            } else {
+                if (c < cols) dst[0] = static_cast<unsigned short>(w[k]);
+                if (c + 1 < cols) dst[1] = static_cast<unsigned short>(w[k] >> 16);
+            }
+            dst += ld;
         }
     }
 }
@@ -178,73 +210,105 @@ __device__ __forceinline__ void fetch_biases(const void* bias, int64_t c0, int64
         add[j] = c0 + j >= cols ? fill : bias ? Elem<T>::widen(static_cast<const T*>(bias)[c0 + j]) : 0.f;
 }
 
-// ---- epilogues: one warp's 32 rows of a tile ------------------------------------------------------
+// ---- epilogues: one warp's 32 rows and its group's columns of a tile -------------------------------
 struct Warp {
     unsigned src, stage;             // its lanes of the accumulators; its staging buffer
     float*   add;
-    int      lane;
+    int      lane, group, quarter;
     int64_t  row0;                   // the first of its rows
+};
+// A group's columns of the `cols` a tile has: from, to; whole multiples of `unit` but for the tile's end
+struct Columns {
+    int from, to;
+    __device__ __forceinline__ Columns(int cols, int group, int unit) {
+        const int first = (cols + 2 * unit - 1) / (2 * unit) * unit;
+        from = group ? min(first, cols) : 0;
+        to = group ? cols : min(first, cols);
+    }
 };
 
 template <typename T>
 __device__ __forceinline__ void scores_tile(const LNArgs& a, const Place& t, const Warp& w) {
-    const int64_t c0 = int64_t(t.n) * LN_N, row = w.row0 + w.lane;
-    const int64_t left = a.cols - c0;
-    const int cols = left < LN_N ? int(left) : LN_N;
+    const int64_t c0 = int64_t(t.n) * a.width, row = w.row0 + w.lane;
     if (w.row0 >= a.rows) return;
+    const int64_t left = a.cols - c0;
+    const Columns mine(left < a.width ? int(left) : a.width, w.group, 32);
+    const int cols = mine.to - mine.from;
     const bool adds = a.bias || (cols & 31);
     if (adds) {
-        fetch_biases<T>(a.bias, c0, a.cols, LN_N, -CUDART_INF_F, w.add, w.lane);
+        fetch_biases<T>(a.bias, c0 + mine.from, a.cols, LN_HALF, -CUDART_INF_F, w.add, w.lane);
         __syncwarp();
     }
     const bool live = row < a.rows;
-    int64_t t64 = a.targets && live ? a.targets[row] - c0 : -1;
+    const int64_t t64 = a.targets && live ? a.targets[row] - c0 - mine.from : -1;
     const int target = t64 >= 0 && t64 < cols ? int(t64) : -1;
     float m = -CUDART_INF_F, s = 0.f;
-    over_columns(w.src, cols, [&](float (&v)[32], int at) {
-        if (adds) add32(v, w.add + at);
-        if (__any_sync(0xffffffffu, target >= at && target < at + 32)) {
-            float z = 0.f;
+    if (cols > 0)
+        over_columns(w.src + unsigned(mine.from), cols, [&](float (&v)[32], int at) {
+            logits32(v, a.whole, adds, w.add + at);
+            if (__any_sync(0xffffffffu, target >= at && target < at + 32)) {
+                float z = 0.f;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) z = target == at + j ? v[j] : z;
-            if (target >= at && target < at + 32) a.target_z[row] = z;
-        }
-        float top[4] = {v[0], v[1], v[2], v[3]};
+                for (int j = 0; j < 32; ++j) z = target == at + j ? v[j] : z;
+                if (target >= at && target < at + 32) a.target_z[row] = z;
+            }
+            float top[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-        for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], v[j]);
-        const float higher = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-        if (higher > m) {
-            s *= ex2((m - higher) * kLog2e);
-            m = higher;
-        }
-        // z - m is rounded once and the exponent's unit comes after it: masks of the lowest value do not overflow
-        const float base = m == -CUDART_INF_F ? 0.f : m;
-        const f32x2 minus = pack2(-base, -base), unit = pack2(kLog2e, kLog2e);
-        f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+            for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], v[j]);
+            const float higher = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+            if (higher > m) {
+                s *= ex2((m - higher) * kLog2e);
+                m = higher;
+            }
+            // z - m is rounded once and the exponent's unit comes after it: masks of the lowest value do not overflow
+            const float base = m == -CUDART_INF_F ? 0.f : m;
+            const f32x2 minus = pack2(-base, -base), unit = pack2(kLog2e, kLog2e);
+            f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-            float e0, e1, e2, e3;
-            unpack2(mul2(add2(pack2(v[j], v[j + 1]), minus), unit), e0, e1);
-            unpack2(mul2(add2(pack2(v[j + 2], v[j + 3]), minus), unit), e2, e3);
-            sum0 = add2(sum0, pack2(ex2(e0), ex2(e1)));
-            sum1 = add2(sum1, pack2(ex2(e2), ex2(e3)));
-        }
-        float p, q;
-        unpack2(add2(sum0, sum1), p, q);
-        s += p + q;
-    });
-    if (live) a.parts[row * a.nt + t.n] = make_float2(m, s);
+            for (int j = 0; j < 32; j += 4) {
+                float e0, e1, e2, e3;
+                unpack2(mul2(add2(pack2(v[j], v[j + 1]), minus), unit), e0, e1);
+                unpack2(mul2(add2(pack2(v[j + 2], v[j + 3]), minus), unit), e2, e3);
+                sum0 = add2(sum0, pack2(ex2(e0), ex2(e1)));
+                sum1 = add2(sum1, pack2(ex2(e2), ex2(e3)));
+            }
+            float p, q;
+            unpack2(add2(sum0, sum1), p, q);
+            s += p + q;
+        });
+    if (live) a.parts[(row * a.nt + t.n) * 2 + w.group] = make_float2(m, s);
+}
+
+// 64 columns at a time to the result, staged
+__device__ __forceinline__ void stage_free(const Warp& w) {
+    if (w.lane == 0) tma_store_read<0>();
+    __syncwarp();
+}
+// the staged piece, 64 columns from `col` on, `cols` of which exist
+__device__ __forceinline__ void put_piece(const LNArgs& a, const Warp& w, const CUtensorMap* map, int64_t col, int cols, int z) {
+    if (a.out == OUT_WIDE) {
+        fence_async_smem();
+        __syncwarp();
+        if (w.lane == 0) tma_put(map, w.stage, int(col), int(w.row0), z);
+    } else {
+        const int64_t left = a.rows - w.row0;
+        __syncwarp();
+        store_plain(w.stage, w.lane, static_cast<unsigned short*>(a.y) + w.row0 * a.ldy + col, a.ldy, left < 32 ? int(left) : 32, cols);
+        __syncwarp();
+    }
 }
 
 template <typename T>
 __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, const Warp& w, const CUtensorMap* map) {
-    const int64_t c0 = int64_t(t.n) * LN_N, row = w.row0 + w.lane;
+    const int64_t c0 = int64_t(t.n) * a.width, row = w.row0 + w.lane;
     const int64_t left = a.cols - c0;
-    const int cols = left < LN_N ? int(left) : LN_N;
-    if (w.row0 >= a.rows) return;
+    const Columns mine(left < a.width ? int(left) : a.width, w.group, 64);
+    const int cols = mine.to - mine.from;
+    if (w.row0 >= a.rows || cols <= 0) return;
+    const int64_t first = c0 + mine.from;
     const bool adds = a.bias != nullptr;
     if (adds) {
-        fetch_biases<T>(a.bias, a.col0 + c0, a.col0 + a.cols, LN_N, -CUDART_INF_F, w.add, w.lane);
+        fetch_biases<T>(a.bias, a.col0 + first, a.col0 + a.cols, LN_HALF, -CUDART_INF_F, w.add, w.lane);
         __syncwarp();
     }
     float coef = 0.f, lse = 0.f, lo = 0.f;
@@ -253,7 +317,7 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
         coef = a.coef[row];
         lse = a.lse[row];
         if (a.lse_lo) lo = a.lse_lo[row];
-        const int64_t t64 = a.targets[row] - a.col0 - c0;
+        const int64_t t64 = a.targets[row] - a.col0 - first;
         target = t64 >= 0 && t64 < cols ? int(t64) : -1;
         if (a.top) coef *= power_for(*a.top, false);
     }
@@ -262,8 +326,8 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
     const bool nothing = coef == 0.f;
     const f32x2 minus = pack2(-lse, -lse), unit = pack2(kLog2e, kLog2e), minus_lo = pack2(-lo * kLog2e, -lo * kLog2e), by = pack2(-coef, -coef);
     int half = 0;
-    over_columns(w.src, cols, [&](float (&v)[32], int at) {
-        if (adds) add32(v, w.add + at);
+    over_columns(w.src + unsigned(mine.from), cols, [&](float (&v)[32], int at) {
+        logits32(v, a.whole, adds, w.add + at);
 #pragma unroll
         for (int j = 0; j < 32; j += 2) {
             float e0, e1;
@@ -278,30 +342,25 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = nothing ? 0.f : v[j];
         }
-        if (half == 0) {
-            if (w.lane == 0) tma_store_read<0>();
-            __syncwarp();
-        }
+        if (half == 0) stage_free(w);
         stage32<T>(w.stage, w.lane, half, v);
-        if (half == 1 || at + 32 >= cols) {
-            fence_async_smem();
-            __syncwarp();
-            if (w.lane == 0) tma_put(map, w.stage, int(c0) + (at & ~63), int(w.row0), 0);
-        }
+        if (half == 1 || at + 32 >= cols) put_piece(a, w, map, first + (at & ~63), cols - (at & ~63), 0);
         half ^= 1;
     });
 }
 
 template <typename T>
 __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const Warp& w, const CUtensorMap* map) {
-    const int64_t c0 = int64_t(t.n) * LN_N;
-    const int64_t left = a.cols - c0, rows_left = a.rows - w.row0;
-    const int cols = left < LN_N ? int(left) : LN_N, rows = rows_left < 32 ? int(rows_left) : 32;
-    if (rows <= 0) return;
+    const int64_t c0 = int64_t(t.n) * a.width;
+    const int64_t left = a.cols - c0;
+    const Columns mine(left < a.width ? int(left) : a.width, w.group, 64);
+    const int cols = mine.to - mine.from;
+    if (w.row0 >= a.rows || cols <= 0) return;
+    const int64_t first = c0 + mine.from;
+    const unsigned src = w.src + unsigned(mine.from);
     if (a.out >= OUT_PART) {
-        over_columns(w.src, cols, [&](float (&v)[32], int at) {
-            if (w.lane == 0) tma_store_read<0>();
-            __syncwarp();
+        over_columns(src, cols, [&](float (&v)[32], int at) {
+            stage_free(w);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 put_shared(w.stage + w.lane * 128 + ((j ^ (w.lane & 7)) << 4),
@@ -309,36 +368,22 @@ __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const 
             fence_async_smem();
             __syncwarp();
             if (w.lane == 0) {
-                if (a.out == OUT_ADD) tma_add(map, w.stage, int(c0) + at, int(w.row0), t.split);
-                else tma_put(map, w.stage, int(c0) + at, int(w.row0), t.split);
+                if (a.out == OUT_ADD) tma_add(map, w.stage, int(first) + at, int(w.row0), t.split);
+                else tma_put(map, w.stage, int(first) + at, int(w.row0), t.split);
             }
         });
         return;
     }
     const float by = a.top ? power_for(*a.top, true) : 1.f;
     int half = 0;
-    over_columns(w.src, cols, [&](float (&v)[32], int at) {
+    over_columns(src, cols, [&](float (&v)[32], int at) {
         if (a.top) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] *= by;
         }
-        if (half == 0) {
-            if (w.lane == 0) tma_store_read<0>();
-            __syncwarp();
-        }
+        if (half == 0) stage_free(w);
         stage32<T>(w.stage, w.lane, half, v);
-        if (half == 1 || at + 32 >= cols) {
-            const int from = at & ~63;
-            if (a.out == OUT_WIDE) {
-                fence_async_smem();
-                __syncwarp();
-                if (w.lane == 0) tma_put(map, w.stage, int(c0) + from, int(w.row0), 0);
-            } else {
-                __syncwarp();
-                store_plain(w.stage, w.lane, static_cast<unsigned short*>(a.y) + w.row0 * a.ldy + c0 + from, a.ldy, rows, cols - from);
-                __syncwarp();
-            }
-        }
+        if (half == 1 || at + 32 >= cols) put_piece(a, w, map, first + (at & ~63), cols - (at & ~63), 0);
         half ^= 1;
     });
 }
@@ -363,116 +408,103 @@ __device__ __forceinline__ void store_codes(const float (&v)[32], const Step& st
     }
 }
 
-template <int ACT> __device__ __forceinline__ void act32(float (&g)[32], const float (&u)[32]) {
+// act(g) u of 32 columns as T to a half of this lane's row of the staged piece
+template <typename T, int ACT>
+__device__ __forceinline__ void gate32(unsigned stage, int lane, int half, const float (&g)[32], const float (&u)[32]) {
 #pragma unroll
     for (int j = 0; j < 32; j += 8) {
         const float x[8] = {g[j], g[j + 1], g[j + 2], g[j + 3], g[j + 4], g[j + 5], g[j + 6], g[j + 7]};
         float y[8];
         act8<ACT>(x, y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[j + i] = y[i] * u[j + i];
+        for (int i = 0; i < 8; ++i) y[i] *= u[j + i];
+        put_shared(stage + lane * 128 + (((half * 4 + j / 8) ^ (lane & 7)) << 4), narrow16B(y, static_cast<const T*>(nullptr)));
     }
 }
+// 32 columns of g or u: the accumulators and the biases
+__device__ __forceinline__ void ask_and_add(unsigned src, bool adds, const float* add, float (&v)[32]) {
+    ask32(src, v);
+    wait32(v);
+    if (adds) add32(v, add);
+}
+__device__ __forceinline__ unsigned top32(const float (&v)[32]) {           // the largest magnitude, as bits: NaN above infinity
+    unsigned t[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 32; ++j) t[j & 3] = max(t[j & 3], __float_as_uint(v[j]) & 0x7fffffffu);
+    return max(max(t[0], t[1]), max(t[2], t[3]));
+}
 
-template <typename T>
+// A store group has 64 columns of g and the same 64 of u (fewer at the end).  The maxima of checkpoints' groups are found in
+// a pass of their own over tensor memory; for groups of 128 columns either store group looks at all of them.
+template <typename T, int ACT>
 __device__ __forceinline__ void gated_tile(const LNArgs& a, const Place& t, const Warp& w, const CUtensorMap* map) {
-    const int64_t c0 = int64_t(t.n) * LN_HALF, row = w.row0 + w.lane;
-    const int64_t left = a.cols - c0, rows_left = a.rows - w.row0;
-    const int cols = left < LN_HALF ? int(left) : LN_HALF, rows = rows_left < 32 ? int(rows_left) : 32;
-    if (rows <= 0) return;
-    const bool adds = a.bias || a.bias2;
+    const int half_width = a.width / 2;
+    const int64_t c0 = int64_t(t.n) * half_width, row = w.row0 + w.lane;
+    const int64_t left = a.cols - c0;
+    const int all = left < half_width ? int(left) : half_width;
+    const Columns mine(all, w.group, 64);
+    const int cols = mine.to - mine.from;
+    if (w.row0 >= a.rows || cols <= 0) return;
+    const int64_t first = c0 + mine.from;
+    const bool adds = a.bias || a.bias2, saves = a.s0.q || a.s1.q, live = row < a.rows;
     if (adds) {
         fetch_biases<T>(a.bias, c0, a.cols, LN_HALF, 0.f, w.add, w.lane);
         fetch_biases<T>(a.bias2, c0, a.cols, LN_HALF, 0.f, w.add + LN_HALF, w.lane);
         __syncwarp();
     }
+    const unsigned src_g = w.src, src_u = w.src + unsigned(half_width);
+    unsigned top_g[2] = {0, 0}, top_u[2] = {0, 0};
     float g[32], u[32];
-    const bool live = row < a.rows, saves = a.s0.q || a.s1.q;
-    unsigned top_g[4] = {0, 0, 0, 0}, top_u[4] = {0, 0, 0, 0};      // of the groups, as bits: NaN above infinity
     if (saves) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            ask32(w.src + unsigned(32 * k), g);
-            ask32(w.src + unsigned(LN_HALF + 32 * k), u);
+        const bool whole = a.group_shift == 7;
+        const int from = whole ? 0 : mine.from, to = whole ? all : mine.to;
+#pragma unroll 1
+        for (int c = from; c < to; c += 32) {
+            ask32(src_g + unsigned(c), g);
+            ask32(src_u + unsigned(c), u);
             wait32(g);
             wait32(u);
             if (adds) {
-                add32(g, w.add + 32 * k);
-                add32(u, w.add + LN_HALF + 32 * k);
+                add32(g, w.add + c);
+                add32(u, w.add + LN_HALF + c);
             }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                top_g[k] = max(top_g[k], __float_as_uint(g[j]) & 0x7fffffffu);
-                top_u[k] = max(top_u[k], __float_as_uint(u[j]) & 0x7fffffffu);
-            }
+            const int k = (c >> 5) & 1;
+            const unsigned tg = top32(g), tu = top32(u);
+            if (k == 0 || whole) { top_g[0] = max(top_g[0], tg); top_u[0] = max(top_u[0], tu); }
+            else { top_g[1] = tg; top_u[1] = tu; }
         }
-        if (a.group_shift >= 6) {
-#pragma unroll
-            for (int k = 0; k < 4; k += 2) {
-                top_g[k] = top_g[k + 1] = max(top_g[k], top_g[k + 1]);
-                top_u[k] = top_u[k + 1] = max(top_u[k], top_u[k + 1]);
-            }
-        }
-        if (a.group_shift == 7) {
-            const unsigned tg = max(top_g[0], top_g[2]), tu = max(top_u[0], top_u[2]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                top_g[k] = tg;
-                top_u[k] = tu;
-            }
+        if (whole) {
+            top_g[1] = top_g[0];
+            top_u[1] = top_u[0];
+        } else if (a.group_shift == 6) {
+            top_g[0] = top_g[1] = max(top_g[0], top_g[1]);
+            top_u[0] = top_u[1] = max(top_u[0], top_u[1]);
         }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (32 * k < cols) {
-            ask32(w.src + unsigned(32 * k), g);
-            ask32(w.src + unsigned(LN_HALF + 32 * k), u);
-            wait32(g);
-            wait32(u);
-            if (adds) {
-                add32(g, w.add + 32 * k);
-                add32(u, w.add + LN_HALF + 32 * k);
-            }
-            if (saves && live) {
-                const int64_t c = c0 + 32 * k, group = row * a.groups + (c >> a.group_shift);
-                const bool first = (c & ((1 << a.group_shift) - 1)) == 0;
-                if (a.s0.q) {
-                    const Step step(__uint_as_float(top_g[k]));
-                    if (first) a.s0.scales[group] = step.scale(__uint_as_float(top_g[k]));
-                    store_codes(g, step, a.s0.q + row * a.s0.ldq + c, cols - 32 * k);
-                }
-                if (a.s1.q) {
-                    const Step step(__uint_as_float(top_u[k]));
-                    if (first) a.s1.scales[group] = step.scale(__uint_as_float(top_u[k]));
-                    store_codes(u, step, a.s1.q + row * a.s1.ldq + c, cols - 32 * k);
-                }
-            }
-            if (a.act == GAR_ACT_SILU) act32<GAR_ACT_SILU>(g, u);
-            else if (a.act == GAR_ACT_GELU) act32<GAR_ACT_GELU>(g, u);
-            else if (a.act == GAR_ACT_RELU) act32<GAR_ACT_RELU>(g, u);
-            else act32<GAR_ACT_IDENTITY>(g, u);
-            if (!(k & 1)) {
-                if (w.lane == 0) tma_store_read<0>();
-                __syncwarp();
-            }
-            stage32<T>(w.stage, w.lane, k & 1, g);
-            if ((k & 1) || 32 * (k + 1) >= cols) {
-                const int from = 32 * (k & ~1);
-                if (a.out == OUT_WIDE) {
-                    fence_async_smem();
-                    __syncwarp();
-                    if (w.lane == 0) tma_put(map, w.stage, int(c0) + from, int(w.row0), 0);
-                } else {
-                    __syncwarp();
-                    store_plain(w.stage, w.lane, static_cast<unsigned short*>(a.y) + w.row0 * a.ldy + c0 + from, a.ldy, rows, cols - from);
-                    __syncwarp();
-                }
-            }
+    for (int k = 0; k < 2; ++k) {
+        if (32 * k >= cols) break;
+        const int64_t c = first + 32 * k, group = row * a.groups + (c >> a.group_shift);
+        const bool begins = (c & ((1 << a.group_shift) - 1)) == 0;
+        ask_and_add(src_g + unsigned(mine.from + 32 * k), adds, w.add + mine.from + 32 * k, g);
+        if (a.s0.q && live) {
+            const Step step(__uint_as_float(top_g[k]));
+            if (begins) a.s0.scales[group] = step.scale(__uint_as_float(top_g[k]));
+            store_codes(g, step, a.s0.q + row * a.s0.ldq + c, cols - 32 * k);
         }
+        ask_and_add(src_u + unsigned(mine.from + 32 * k), adds, w.add + LN_HALF + mine.from + 32 * k, u);
+        if (a.s1.q && live) {
+            const Step step(__uint_as_float(top_u[k]));
+            if (begins) a.s1.scales[group] = step.scale(__uint_as_float(top_u[k]));
+            store_codes(u, step, a.s1.q + row * a.s1.ldq + c, cols - 32 * k);
+        }
+        if (k == 0) stage_free(w);
+        gate32<T, ACT>(w.stage, w.lane, k, g, u);
     }
+    put_piece(a, w, map, first, cols, 0);
 }
 
-template <typename T, int EPI>
+template <typename T, int EPI, int ACT>
 __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, const __grid_constant__ CUtensorMap map_a0,
                                                               const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_a1,
                                                               const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_out) {
@@ -491,7 +523,7 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
         }
         for (int b = 0; b < 2; ++b) {
             kb_init(&sm.acc_full[b], 1);
-            kb_init(&sm.acc_empty[b], 8);
+            kb_init(&sm.acc_empty[b], 2 * LN_STORE_WARPS);
         }
         kb_fence_init();
     }
@@ -508,6 +540,8 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
     __syncthreads();
     pair_sync();                              // the other CTA's barriers are initialised
     tc_fence_after();
+    // what the launches before it on the stream have written is there; the next one's CTAs may be set up
+    grid_dependency();
     const unsigned tmem = sm.tmem_base;
     const unsigned tiles = unsigned(a.mt) * unsigned(a.nt) * unsigned(a.splits);      // below 2^30
     bool ok = true;
@@ -522,21 +556,21 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
                 for (int s = 0; s < t.steps; ++s, ++g) {
                     const Ring<LN_RING> r(g);
                     if (!kb_wait(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
-                    if (rank == 0) kb_expect_tx(kb_smem_u32(&sm.full[r.slot]), 4 * LN_TILE);
+                    if (rank == 0) kb_expect_tx(kb_smem_u32(&sm.full[r.slot]), 2 * LN_TILE + unsigned(a.width) * (LN_K * 2));
                     const unsigned bar = leader_full + r.slot * 8, da = kb_smem_u32(sm.a[r.slot]), db = kb_smem_u32(sm.b[r.slot]);
                     const int step = t.first + s;
                     const bool second = step >= a.steps0;
                     const int k = (second ? step - a.steps0 : step) * LN_K;
                     tma_load_pair(da, second ? &map_a1 : &map_a0, k, y, 0, bar);
                     if (B_MN) {
-                        const int x = t.n * LN_N + int(rank) * LN_HALF;
+                        const int x = t.n * a.width + int(rank) * (a.width / 2);
                         const CUtensorMap* map = second ? &map_b1 : &map_b0;
                         tma_load_pair(db, map, x, k, 0, bar);
-                        tma_load_pair(db + LN_BLOCK, map, x + 64, k, 0, bar);
+                        if (a.width == LN_N) tma_load_pair(db + LN_BLOCK, map, x + 64, k, 0, bar);
                     } else if (EPI == LN_GATED) {
-                        tma_load_pair(db, rank == 0 ? &map_b0 : &map_b1, k, t.n * LN_HALF, 0, bar);
+                        tma_load_pair(db, rank == 0 ? &map_b0 : &map_b1, k, t.n * (a.width / 2), 0, bar);
                     } else {
-                        tma_load_pair(db, &map_b0, k, t.n * LN_N + int(rank) * LN_HALF, 0, bar);
+                        tma_load_pair(db, &map_b0, k, t.n * a.width + int(rank) * (a.width / 2), 0, bar);
                     }
                 }
             }
@@ -550,7 +584,7 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
     } else if (warp == LN_MMA_WARP) {
         // The whole warp walks the loop and one elected lane issues.
         if (rank == 0) {
-            const unsigned idesc = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, LN_N, false, B_MN);
+            const unsigned idesc = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, a.width, false, B_MN);
             const unsigned long long desc_a = operand_desc(kb_smem_u32(sm.a), 16, 1024, 2);
             const unsigned long long desc_b = operand_desc(kb_smem_u32(sm.b), B_MN ? LN_BLOCK : 16, 1024, 2);
             // 16 elements of the contraction: 32 bytes along a K-major row, 16 rows of 128 bytes of an MN-major block
@@ -588,26 +622,27 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
             }
         }
     } else if (warp >= LN_STORE_WARP0) {
-        const int mine = (warp - LN_STORE_WARP0) / 4, quarter = warp % 4;      // half of tensor memory; its lanes 32 quarter ..
         Warp w;
-        w.src = tmem + unsigned(mine) * LN_N + (unsigned(quarter * 32) << 16);
+        w.group = (warp - LN_STORE_WARP0) / 4;
+        w.quarter = warp % 4;                                // its lanes of tensor memory: 32 quarter ..
         w.stage = kb_smem_u32(sm.out[warp - LN_STORE_WARP0]);
         w.add = sm.add[warp - LN_STORE_WARP0];
         w.lane = lane;
         unsigned done = 0;
         for (unsigned i = pair; i < tiles; i += pairs, ++done) {
-            if (int(done & 1u) != mine) continue;
             const Place t = place_at(a, i);
-            if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[mine]), (done >> 1) & 1u, error)) break;
+            const unsigned half = done & 1u;
+            if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[half]), (done >> 1) & 1u, error)) break;
             tc_fence_after();
-            w.row0 = int64_t(2 * t.m + int(rank)) * LN_M + quarter * 32;
+            w.src = tmem + half * LN_N + (unsigned(w.quarter * 32) << 16);
+            w.row0 = int64_t(2 * t.m + int(rank)) * LN_M + w.quarter * 32;
             if constexpr (EPI == LN_SCORES) scores_tile<T>(a, t, w);
             if constexpr (EPI == LN_DLOGITS) dlogits_tile<T>(a, t, w, &map_out);
-            if constexpr (EPI == LN_GATED) gated_tile<T>(a, t, w, &map_out);
+            if constexpr (EPI == LN_GATED) gated_tile<T, ACT>(a, t, w, &map_out);
             if constexpr (EPI == LN_SUM) sum_tile<T>(a, t, w, &map_out);
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) arrive_at_leader(&sm.acc_empty[mine]);
+            if (lane == 0) arrive_at_leader(&sm.acc_empty[half]);
         }
         if (lane == 0) tma_store_done();
     }
@@ -623,13 +658,13 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     if (sm.error || *static_cast<volatile int*>(&sm.other_error)) {
         // a wait gave up: nothing the pair was to write may look like a result
-        constexpr int WIDTH = EPI == LN_SCORES ? 1 : EPI == LN_GATED ? LN_HALF : LN_N;
+        const int WIDTH = EPI == LN_SCORES ? 1 : EPI == LN_GATED ? a.width / 2 : a.width;
         for (unsigned i = pair; i < tiles; i += pairs) {
             const Place t = place_at(a, i);
             for (int e = tid; e < LN_M * WIDTH; e += LN_THREADS) {
                 const int64_t row = int64_t(2 * t.m + int(rank)) * LN_M + e / WIDTH, c = int64_t(t.n) * WIDTH + e % WIDTH;
                 if (row >= a.rows) continue;
-                if constexpr (EPI == LN_SCORES) a.parts[row * a.nt + t.n] = make_float2(CUDART_NAN_F, CUDART_NAN_F);
+                if constexpr (EPI == LN_SCORES) a.parts[(row * a.nt + t.n) * 2] = a.parts[(row * a.nt + t.n) * 2 + 1] = make_float2(CUDART_NAN_F, CUDART_NAN_F);
                 else if (c < a.cols) {
                     if (EPI == LN_SUM && a.out >= OUT_PART) static_cast<float*>(a.y)[(int64_t(t.split) * a.rows + row) * a.ldy + c] = CUDART_NAN_F;
                     else static_cast<T*>(a.y)[row * a.ldy + c] = Elem<T>::narrow(CUDART_NAN_F);
@@ -647,6 +682,7 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
 // The parts of a row joined: a warp per row.
 __global__ void __launch_bounds__(256) join_scores_kernel(const float2* parts, const float* target_z, const int64_t* targets, int64_t rows, int nt,
                                                           int64_t vocab, float* logprobs, float* lse, float* lse_lo) {
+    grid_dependency();
     const int64_t row = int64_t(blockIdx.x) * 8 + threadIdx.x / 32;
     const int lane = threadIdx.x % 32;
     if (row >= rows) return;
@@ -687,26 +723,32 @@ __global__ void __launch_bounds__(256) join_scores_kernel(const float2* parts, c
     }
 }
 
-// Rows of 16-bit elements copied to rows that start on 16 bytes, eight elements per thread and turn.  ROWS: rows
-// whose coefficient is 0 are copied as zeros, and the coefficients (the gradient at a row's log probability; 0
-// without a target, NaN for a target outside the vocabulary) and the largest one's magnitude are written.
-struct RowsArgs {
+// Rows of 16-bit elements copied to rows that start on 16 bytes, eight elements per thread and turn; up to four matrices,
+// one per blockIdx.y.  A job with targets is the rows of a head: those whose coefficient is 0 are copied as zeros, and the coefficients
+// (the gradient at a row's log probability; 0 without a target, NaN for a target outside the vocabulary) and the
+// largest one's magnitude are written.
+struct CopyJob {
     const unsigned short* src;
     int64_t        ld, cols, pieces, per_row;
-    uint4*         dst;                    // null: only the coefficients
-    const int64_t* targets;
+    uint4*         dst;
+    int            aligned;                // the source's rows start on 16 bytes
+};
+struct CopyArgs {
+    CopyJob        job[4];
+    const int64_t* targets;                // of the first job; or null
     const float*   grad;
     int64_t        vocab;
     float*         coef;
     unsigned*      top;                    // null: not asked for
-    int            aligned;                // the source's rows start on 16 bytes
 };
-template <bool ROWS>
-__global__ void __launch_bounds__(256) copy_rows_kernel(const RowsArgs a) {
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < a.pieces; i += int64_t(gridDim.x) * 256) {
-        const int64_t row = i / a.per_row, c = (i - row * a.per_row) * 8;
+__global__ void __launch_bounds__(256) copy_rows_kernel(const CopyArgs a) {
+    grid_dependency();
+    const CopyJob& j = a.job[blockIdx.y];
+    const bool head = a.targets && blockIdx.y == 0;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < j.pieces; i += int64_t(gridDim.x) * 256) {
+        const int64_t row = i / j.per_row, c = (i - row * j.per_row) * 8;
         bool zero = false;
-        if (ROWS) {
+        if (head) {
             const int64_t t = a.targets[row];
             const float coef = t < 0 ? 0.f : t >= a.vocab ? CUDART_NAN_F : a.grad[row];
             zero = coef == 0.f;
@@ -715,21 +757,20 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const RowsArgs a) {
                 const unsigned bits = __float_as_uint(coef) & 0x7fffffffu;
                 if (a.top && bits < 0x7f800000u) atomicMax(a.top, bits);      // the same in any order
             }
-            if (!a.dst) continue;
         }
-        const unsigned short* p = a.src + row * a.ld + c;
+        const unsigned short* p = j.src + row * j.ld + c;
         uint4 w = make_uint4(0, 0, 0, 0);
         if (!zero) {
-            if (a.aligned && c + 8 <= a.cols) {
+            if (j.aligned && c + 8 <= j.cols) {
                 w = __ldg(reinterpret_cast<const uint4*>(p));
             } else {
                 unsigned v[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = c + j < a.cols ? __ldg(p + j) : 0u;
+                for (int k = 0; k < 8; ++k) v[k] = c + k < j.cols ? __ldg(p + k) : 0u;
                 w = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
             }
         }
-        a.dst[i] = w;
+        j.dst[i] = w;
     }
 }
 
@@ -737,6 +778,7 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const RowsArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(256) join_parts_kernel(const float* parts, int64_t plane, int64_t pitch, int splits, int64_t rows, int64_t cols,
                                                          const unsigned* top, T* y, int64_t ldy) {
+    grid_dependency();
     const int64_t per_row = (cols + 3) / 4, pieces = rows * per_row;
     const float by = top ? power_for(*top, true) : 1.f;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += int64_t(gridDim.x) * 256) {
@@ -790,48 +832,64 @@ private:
 };
 
 unsigned copy_blocks(int64_t pieces, int sm_count) { return unsigned(std::min<int64_t>(int64_t(16) * sm_count, parts_of(pieces, 256))); }
-cudaError_t copy_rows(const Operand& src, char* dst, int64_t ld, int sm_count, cudaStream_t stream) {
-    RowsArgs a{};
-    a.src = reinterpret_cast<const unsigned short*>(src.p);
-    a.ld = src.ld;
-    a.cols = src.cols;
-    a.per_row = ld / 8;
-    a.pieces = src.rows * a.per_row;
-    a.dst = reinterpret_cast<uint4*>(dst);
-    a.aligned = on_16(src.p, src.ld);
-    copy_rows_kernel<false><<<copy_blocks(a.pieces, sm_count), 256, 0, stream>>>(a);
-    return cudaGetLastError();
+
+// A launch that may be set up while the one before it on the stream ends: every kernel here waits for that one's
+// results first (grid_dependency).
+template <typename... P, typename... A>
+cudaError_t launch_small(void (*kernel)(P...), dim3 grid, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
+
 // A matrix of the caller's as an operand: where it lies, or copied to the space reserved for it.
 struct Input {
     Operand m;
     char*   copy = nullptr;
-    Input(Space& space, const void* p, int64_t rows, int64_t cols, int64_t ld) : m{static_cast<const char*>(p), rows, cols, ld} {
-        if (on_16(p, ld)) return;
-        copy = space.take(size_t(rows) * size_t(up_to(cols, 8)) * 2);
-        copied_ = true;
+    bool    copied;
+    Input(Space& space, const void* p, int64_t rows, int64_t cols, int64_t ld) : m{static_cast<const char*>(p), rows, cols, ld}, copied(!on_16(p, ld)) {
+        if (copied) copy = space.take(size_t(rows) * size_t(up_to(cols, 8)) * 2);
     }
-    cudaError_t ready(int sm_count, cudaStream_t stream) {
-        if (!copied_) return cudaSuccess;
-        const int64_t ld = up_to(m.cols, 8);
-        if (cudaError_t err = copy_rows(m, copy, ld, sm_count, stream)) return err;
-        m.p = copy;
-        m.ld = ld;
-        return cudaSuccess;
+};
+CopyJob copy_job(const Operand& src, void* dst, int64_t ld) {
+    return CopyJob{reinterpret_cast<const unsigned short*>(src.p), src.ld, src.cols, src.rows * (ld / 8), ld / 8, static_cast<uint4*>(dst), on_16(src.p, src.ld)};
+}
+// The copies of a call, in one launch.
+struct Copies {
+    CopyArgs a{};
+    int      n = 0;
+    int64_t  most = 0;
+    void add(const CopyJob& j) {
+        a.job[n++] = j;
+        most = std::max(most, j.pieces);
     }
-
-private:
-    bool copied_ = false;
+    void add(Input& in) {
+        if (!in.copied) return;
+        const int64_t ld = up_to(in.m.cols, 8);
+        add(copy_job(in.m, in.copy, ld));
+        in.m.p = in.copy;
+        in.m.ld = ld;
+    }
+    cudaError_t launch(int sm_count, cudaStream_t stream) const {
+        return most > 0 ? launch_small(copy_rows_kernel, dim3(copy_blocks(most, sm_count), unsigned(n)), stream, a) : cudaSuccess;
+    }
 };
 
 struct Maps {
     CUtensorMap a0, b0, a1, b1, out;
 };
-template <typename T, int EPI>
+template <typename T, int EPI, int ACT>
 cudaError_t launch_as(const LNArgs& a, const Maps& maps, int sm_count, cudaStream_t stream) {
     constexpr int bytes = int(sizeof(LNSmem)) + 1024;
     static_assert(bytes <= 232448, "a CTA's shared memory");
-    auto kernel = linear_kernel<T, EPI>;
+    auto kernel = linear_kernel<T, EPI, ACT>;
     static std::atomic<uint64_t> allowed{0};           // devices on which the kernel may have that much
     int dev = 0;
     if (cudaError_t err = cudaGetDevice(&dev)) return err;
@@ -847,29 +905,51 @@ cudaError_t launch_as(const LNArgs& a, const Maps& maps, int sm_count, cudaStrea
     cfg.blockDim = dim3(LN_THREADS);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a, maps.a0, maps.b0, maps.a1, maps.b1, maps.out);
 }
-template <int EPI>
+template <int EPI, int ACT = 0>
 cudaError_t launch(int dtype, const LNArgs& a, const Maps& maps, int sm_count, cudaStream_t stream) {
-    return dtype == GAR_BF16 ? launch_as<__nv_bfloat16, EPI>(a, maps, sm_count, stream) : launch_as<__half, EPI>(a, maps, sm_count, stream);
+    return dtype == GAR_BF16 ? launch_as<__nv_bfloat16, EPI, ACT>(a, maps, sm_count, stream) : launch_as<__half, EPI, ACT>(a, maps, sm_count, stream);
 }
 
-// z = x W^T over `rows` rows and the columns of `w`: the operands' part of a launch
-cudaError_t logits_maps(Maps& maps, LNArgs& a, int dtype, const Operand& x, const Operand& w) {
+// Columns of a tile, a multiple of `unit` up to 256.  A step's copies come at some 47 bytes per cycle and SM, 16 KB of A and 64
+// bytes per column of B, and the last tile's epilogue, some 22 cycles per column, is hidden by nothing: the width with the
+// least of (rounds of the pairs) x steps x (348 + 1.36 width) + 22 width.  Few tiles get narrow ones, one for each pair; many
+// get 256 columns, or what leaves no part of the last round idle.
+int width_for(int64_t mt, int64_t cols, int64_t steps, int unit, int columns_of = 1) {
+    int best = LN_N;
+    double least = 0;
+    for (int w = LN_N; w >= unit; w -= unit) {
+        const double rounds = double(parts_of(mt * parts_of(cols, w / columns_of), LN_PAIRS));
+        const double t = rounds * double(steps) * (348 + 1.36 * w) + 22.0 * w;
+        if (w == LN_N || t < least) {
+            least = t;
+            best = w;
+        }
+    }
+    return best;
+}
+
+// z = x W^T over `rows` rows and the columns of `w`: the operands' part of a launch, tiles of a multiple of `unit` columns
+cudaError_t logits_maps(Maps& maps, LNArgs& a, int dtype, const Operand& x, const Operand& w, int unit) {
     a.rows = x.rows;
     a.cols = w.rows;
     a.mt = int(parts_of(x.rows, 2 * LN_M));
-    a.nt = int(parts_of(w.rows, LN_N));
     a.splits = 1;
     a.steps0 = a.steps = int(parts_of(x.cols, LN_K));
+    a.width = width_for(a.mt, a.cols, a.steps, unit);
+    a.nt = int(parts_of(w.rows, a.width));
+    a.whole = 1.f + LN_SHORT * float(x.cols);
     if (cudaError_t err = operand_map(&maps.a0, dtype, x, LN_K, LN_M)) return err;
-    if (cudaError_t err = operand_map(&maps.b0, dtype, w, LN_K, LN_HALF)) return err;
+    if (cudaError_t err = operand_map(&maps.b0, dtype, w, LN_K, a.width / 2)) return err;
     maps.a1 = maps.b1 = maps.out = maps.a0;            // not used unless set
     return cudaSuccess;
 }
@@ -899,12 +979,13 @@ cudaError_t launch_sum(const SumTarget& d, const Operand& a0, const Operand& b0,
     a.rows = d.rows;
     a.cols = d.cols;
     a.mt = int(parts_of(d.rows, 2 * LN_M));
-    a.nt = int(parts_of(d.cols, LN_N));
     a.steps0 = int(parts_of(a0.cols, LN_K));
     a.steps = a.steps0 + (a1 ? int(parts_of(a1->cols, LN_K)) : 0);
     // (a shorter last piece of the contraction may have steps for fewer parts)
     const int part = (a.steps + d.splits - 1) / d.splits;
     a.splits = (a.steps + part - 1) / part;
+    a.width = width_for(int64_t(a.mt) * a.splits, d.cols, part, 128);
+    a.nt = int(parts_of(d.cols, a.width));
     if (cudaError_t err = operand_map(&maps.a0, d.dtype, a0, LN_K, LN_M)) return err;
     if (cudaError_t err = operand_map(&maps.b0, d.dtype, b0, 64, LN_K)) return err;
     maps.a1 = maps.a0;
@@ -931,21 +1012,25 @@ cudaError_t launch_sum(const SumTarget& d, const Operand& a0, const Operand& b0,
     return launch<LN_SUM>(d.dtype, a, maps, sm_count, stream);
 }
 cudaError_t join_sum(const SumTarget& d, int sm_count, cudaStream_t stream) {
-    const unsigned blocks = copy_blocks(d.rows * parts_of(d.cols, 4), sm_count);
+    const dim3 grid(copy_blocks(d.rows * parts_of(d.cols, 4), sm_count));
     if (d.dtype == GAR_BF16)
-        join_parts_kernel<<<blocks, 256, 0, stream>>>(d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top, static_cast<__nv_bfloat16*>(d.dx), d.ld);
-    else
-        join_parts_kernel<<<blocks, 256, 0, stream>>>(d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top, static_cast<__half*>(d.dx), d.ld);
-    return cudaGetLastError();
+        return launch_small(join_parts_kernel<__nv_bfloat16>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top,
+                            static_cast<__nv_bfloat16*>(d.dx), d.ld);
+    return launch_small(join_parts_kernel<__half>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top,
+                        static_cast<__half*>(d.dx), d.ld);
 }
 
 // ---- log probabilities ------------------------------------------------------------------------------
 constexpr int64_t LN_PARTS_BYTES = int64_t(64) << 20, LN_PIECE_BYTES = int64_t(64) << 20;
 constexpr int64_t LN_PIECE_MAX = 16384;
-// rows of a launch, so that its parts take 64 MB at most
+constexpr int LN_SCORES_UNIT = 32, LN_STORE_UNIT = 64;         // columns: of a thread's turn; of a staged piece
+// rows of a launch, so that its parts take 64 MB or so
 int64_t rows_at_once(int64_t rows, int64_t vocab) {
-    const int64_t most = std::max<int64_t>(256, LN_PARTS_BYTES / (8 * parts_of(vocab, LN_N)) / 256 * 256);
+    const int64_t most = std::max<int64_t>(256, LN_PARTS_BYTES / (16 * parts_of(vocab, LN_N)) / 256 * 256);
     return std::min(rows, most);
+}
+int64_t scores_tiles(int64_t rows, int64_t hidden, int64_t vocab) {
+    return parts_of(vocab, width_for(parts_of(rows, 2 * LN_M), vocab, parts_of(hidden, LN_K), LN_SCORES_UNIT));
 }
 struct ScoresPlan {
     Space   space;
@@ -955,7 +1040,10 @@ struct ScoresPlan {
     float*  target_z;
     ScoresPlan(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw)
         : space(p.workspace), x(space, p.x, p.rows, p.hidden, ldx), w(space, p.weight, p.vocab, p.hidden, ldw), rows(rows_at_once(p.rows, p.vocab)) {
-        parts = reinterpret_cast<float2*>(space.take(size_t(rows) * size_t(parts_of(p.vocab, LN_N)) * 8));
+        // (the last rows, if they are fewer, may have narrower tiles)
+        const int64_t last = (p.rows - 1) % rows + 1;
+        const int64_t most = std::max(rows * scores_tiles(rows, p.hidden, p.vocab), last * scores_tiles(last, p.hidden, p.vocab));
+        parts = reinterpret_cast<float2*>(space.take(size_t(most) * 16));
         target_z = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
     }
 };
@@ -1009,24 +1097,25 @@ size_t linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t& p, in
 cudaError_t launch_linear_logprobs(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw, int sm_count) {
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     ScoresPlan plan(p, ldx, ldw);
-    if (cudaError_t err = plan.x.ready(sm_count, stream)) return err;
-    if (cudaError_t err = plan.w.ready(sm_count, stream)) return err;
+    Copies copies;
+    copies.add(plan.x);
+    copies.add(plan.w);
+    if (cudaError_t err = copies.launch(sm_count, stream)) return err;
     for (int64_t r0 = 0; r0 < p.rows; r0 += plan.rows) {
         Operand x = plan.x.m;
         x.p += r0 * x.ld * 2;
         x.rows = std::min(plan.rows, p.rows - r0);
         Maps maps;
         LNArgs a{};
-        if (cudaError_t err = logits_maps(maps, a, p.dtype, x, plan.w.m)) return err;
+        if (cudaError_t err = logits_maps(maps, a, p.dtype, x, plan.w.m, LN_SCORES_UNIT)) return err;
         a.bias = p.bias;
         a.targets = p.logprobs ? p.targets + r0 : nullptr;
         a.parts = plan.parts;
         a.target_z = plan.target_z;
         if (cudaError_t err = launch<LN_SCORES>(p.dtype, a, maps, sm_count, stream)) return err;
-        join_scores_kernel<<<unsigned(parts_of(x.rows, 8)), 256, 0, stream>>>(plan.parts, plan.target_z, a.targets, x.rows, a.nt, p.vocab,
-                                                                             p.logprobs ? p.logprobs + r0 : nullptr, p.lse ? p.lse + r0 : nullptr,
-                                                                             p.lse_lo ? p.lse_lo + r0 : nullptr);
-        if (cudaError_t err = cudaGetLastError()) return err;
+        if (cudaError_t err = launch_small(join_scores_kernel, dim3(unsigned(parts_of(x.rows, 8))), stream, plan.parts, plan.target_z, a.targets, x.rows, 2 * a.nt,
+                                           p.vocab, p.logprobs ? p.logprobs + r0 : nullptr, p.lse ? p.lse + r0 : nullptr,
+                                           p.lse_lo ? p.lse_lo + r0 : nullptr)) return err;
     }
     return cudaSuccess;
 }
@@ -1040,26 +1129,19 @@ size_t linear_logprobs_backward_workspace_bytes(const gar_linear_logprobs_grad_p
 cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_params_t& p, int64_t ldx, int64_t ldw, int sm_count) {
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     GradPlan plan(p, ldw);
-    if (cudaError_t err = plan.w.ready(sm_count, stream)) return err;
     const Operand x{plan.x_rows, plan.rows, p.hidden, plan.ldx};
     if (plan.rows > 0) {
         if (plan.top)
             if (cudaError_t err = cudaMemsetAsync(plan.top, 0, 4, stream)) return err;
-        RowsArgs r{};
-        r.src = static_cast<const unsigned short*>(p.x);
-        r.ld = ldx;
-        r.cols = p.hidden;
-        r.per_row = plan.ldx / 8;
-        r.pieces = plan.rows * r.per_row;
-        r.dst = reinterpret_cast<uint4*>(plan.x_rows);
-        r.targets = p.targets;
-        r.grad = p.grad_logprobs;
-        r.vocab = p.vocab;
-        r.coef = plan.coef;
-        r.top = plan.top;
-        r.aligned = on_16(p.x, ldx);
-        copy_rows_kernel<true><<<copy_blocks(r.pieces, sm_count), 256, 0, stream>>>(r);
-        if (cudaError_t err = cudaGetLastError()) return err;
+        Copies copies;
+        copies.add(copy_job(Operand{static_cast<const char*>(p.x), plan.rows, p.hidden, ldx}, plan.x_rows, plan.ldx));
+        copies.add(plan.w);
+        copies.a.targets = p.targets;
+        copies.a.grad = p.grad_logprobs;
+        copies.a.vocab = p.vocab;
+        copies.a.coef = plan.coef;
+        copies.a.top = plan.top;
+        if (cudaError_t err = copies.launch(sm_count, stream)) return err;
     }
     SumTarget d{p.dtype, p.dx, plan.rows, p.hidden, p.lddx ? p.lddx : p.hidden, plan.parts, plan.pitch, plan.splits, plan.top};
     for (int64_t v0 = 0; v0 < p.vocab; v0 += plan.piece) {
@@ -1070,7 +1152,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
         if (plan.rows > 0) {
             Maps maps;
             LNArgs a{};
-            if (cudaError_t err = logits_maps(maps, a, p.dtype, x, w)) return err;
+            if (cudaError_t err = logits_maps(maps, a, p.dtype, x, w, LN_STORE_UNIT)) return err;
             a.bias = p.bias;
             a.col0 = v0;
             a.vocab = p.vocab;
@@ -1079,6 +1161,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
             a.lse_lo = p.lse_lo;
             a.coef = plan.coef;
             a.top = plan.top;
+            a.out = OUT_WIDE;
             a.y = plan.dz;
             a.ldy = plan.ld_dz;
             if (cudaError_t err = operand_map(&maps.out, p.dtype, dz, 64, 32)) return err;
@@ -1143,14 +1226,23 @@ size_t gated_linear_workspace_bytes(const gar_gated_linear_params_t& p) {
 cudaError_t launch_gated_linear_forward(const gar_gated_linear_params_t& p, int sm_count) {
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     GatedPlan plan(p);
-    for (Input* in : {&plan.x, &plan.gate, &plan.up})
-        if (cudaError_t err = in->ready(sm_count, stream)) return err;
+    Copies copies;
+    for (Input* in : {&plan.x, &plan.gate, &plan.up}) copies.add(*in);
+    if (cudaError_t err = copies.launch(sm_count, stream)) return err;
     Maps maps;
     LNArgs a{};
-    if (cudaError_t err = logits_maps(maps, a, p.dtype, plan.x.m, plan.gate.m)) return err;
-    a.nt = int(parts_of(p.inner, LN_HALF));
-    if (cudaError_t err = operand_map(&maps.b1, p.dtype, plan.up.m, LN_K, LN_HALF)) return err;
-    a.act = p.act;
+    a.rows = p.rows;
+    a.cols = p.inner;
+    a.mt = int(parts_of(p.rows, 2 * LN_M));
+    a.splits = 1;
+    a.steps0 = a.steps = int(parts_of(p.hidden, LN_K));
+    // half the columns are g's; a tile has whole groups of a checkpoint
+    a.width = (p.gate_saved.q || p.up_saved.q) && p.group == 128 ? LN_N : width_for(a.mt, p.inner, a.steps, 128, 2);
+    a.nt = int(parts_of(p.inner, a.width / 2));
+    if (cudaError_t err = operand_map(&maps.a0, p.dtype, plan.x.m, LN_K, LN_M)) return err;
+    if (cudaError_t err = operand_map(&maps.b0, p.dtype, plan.gate.m, LN_K, a.width / 2)) return err;
+    if (cudaError_t err = operand_map(&maps.b1, p.dtype, plan.up.m, LN_K, a.width / 2)) return err;
+    maps.a1 = maps.out = maps.a0;                      // not used unless set
     a.group_shift = p.group == 32 ? 5 : p.group == 64 ? 6 : 7;
     a.groups = int(parts_of(p.inner, p.group));
     a.bias = p.b_gate;
@@ -1162,7 +1254,11 @@ cudaError_t launch_gated_linear_forward(const gar_gated_linear_params_t& p, int 
     a.out = on_16(p.y, p.ldy) ? OUT_WIDE : OUT_PLAIN;
     if (a.out == OUT_WIDE)
         if (cudaError_t err = operand_map(&maps.out, p.dtype, Operand{static_cast<const char*>(p.y), p.rows, p.inner, p.ldy}, 64, 32)) return err;
-    if (cudaError_t err = launch<LN_GATED>(p.dtype, a, maps, sm_count, stream)) return err;
+    const cudaError_t ran = p.act == GAR_ACT_SILU   ? launch<LN_GATED, GAR_ACT_SILU>(p.dtype, a, maps, sm_count, stream)
+                            : p.act == GAR_ACT_GELU ? launch<LN_GATED, GAR_ACT_GELU>(p.dtype, a, maps, sm_count, stream)
+                            : p.act == GAR_ACT_RELU ? launch<LN_GATED, GAR_ACT_RELU>(p.dtype, a, maps, sm_count, stream)
+                                                    : launch<LN_GATED, GAR_ACT_IDENTITY>(p.dtype, a, maps, sm_count, stream);
+    if (ran != cudaSuccess) return ran;
     if (!p.y_saved.q) return cudaSuccess;
     gar_activation_params_t c{};
     c.dtype = p.dtype;
@@ -1204,8 +1300,9 @@ cudaError_t launch_gated_linear_backward(const gar_gated_linear_grad_params_t& p
     if (cudaError_t err = launch_activation_backward(c)) return err;
     if (!p.dx) return cudaSuccess;
     GatedGradPlan plan(p);
-    for (Input* in : {&plan.gate, &plan.up, &plan.dgate, &plan.dup})
-        if (cudaError_t err = in->ready(sm_count, stream)) return err;
+    Copies copies;
+    for (Input* in : {&plan.gate, &plan.up, &plan.dgate, &plan.dup}) copies.add(*in);
+    if (cudaError_t err = copies.launch(sm_count, stream)) return err;
     SumTarget d{p.dtype, p.dx, p.rows, p.hidden, p.lddx, plan.parts, plan.pitch, plan.splits, nullptr};
     if (cudaError_t err = launch_sum(d, plan.dgate.m, plan.gate.m, &plan.dup.m, &plan.up.m, false, sm_count, stream)) return err;
     return plan.parts ? join_sum(d, sm_count, stream) : cudaSuccess;

@@ -123,6 +123,13 @@ template <int DEPTH> struct Ring {
     __device__ __forceinline__ explicit Ring(unsigned number) : slot(number % DEPTH), parity((number / DEPTH) & 1u) {}
 };
 
+// Programmatic launches: waits until the launches before this one on the stream have ended and what they wrote is there
+// (at once where this one was launched plainly), then lets the next one's CTAs be set up as SMs get free.
+__device__ __forceinline__ void grid_dependency() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // The power of two that the largest coefficient is brought to 2^14 .. 2^15 with, and its inverse: |k| <= 100.
 __device__ __forceinline__ float power_for(unsigned top, bool inverse) {
     if (top == 0u || top >= 0x7f800000u) return 1.f;
