@@ -6,12 +6,12 @@
 // 256 rows x 256 columns, 64 elements of the contraction a step, the paired instruction (cta_group::2) with
 // fp32 accumulators in tensor memory, two tiles' worth of it.
 //   copy warp      TMA, one lane: 128 rows of A and 128 rows of B per CTA and step, 128-byte swizzle; A and
-//                  B lie with the contraction along their rows (K-major), or B across them (MN-major: the
-//                  gradient at the inputs, dz W, reads W as it lies)
+//                  B lie with the contraction along their rows (K-major), or across them (MN-major: the
+//                  gradient at the inputs, dz W, reads W as it lies, the gradient at the weights, dz^T x, both)
 //   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
 //   store warps    two groups of four, each with half of a tile's columns, while the next tile's products run
 //                  into the other half of tensor memory; a thread has one row, 32 columns at a time
-// and four epilogues (enum Epilogue).  A thread owning a row makes the softmax's statistics, the group
+// and four epilogues (LN_SUM's and LN_OUTER's are one; enum Epilogue).  A thread owning a row makes the softmax's statistics, the group
 // maxima of the checkpoints and the row's target its own affair.
 // Tiles are as wide as the rule in width_for makes them, 256 columns at most.
 //
@@ -49,12 +49,13 @@ constexpr float LN_SHORT = 1.0e-9f;                   // of a sum, lost per term
 //   LN_DLOGITS  z: a ([j = t] - e^(z - lse)), stored in 16 bits
 //   LN_GATED    128 columns of g and of u: act(g) u, stored, and the codes of g and u
 //   LN_SUM      stored in 16 bits, or in fp32, or added to fp32 (parts of a longer contraction)
-enum Epilogue { LN_SCORES = 0, LN_DLOGITS = 1, LN_GATED = 2, LN_SUM = 3 };
+//   LN_OUTER    the same, of every worker's own contraction over its tokens
+enum Epilogue { LN_SCORES = 0, LN_DLOGITS = 1, LN_GATED = 2, LN_SUM = 3, LN_OUTER = 4 };
 enum Out { OUT_WIDE = 0, OUT_PLAIN = 1, OUT_PART = 2, OUT_ADD = 3 };    // 16 bits by TMA or plainly; fp32, added
 
 struct LNArgs {
     int64_t        rows, cols;            // of the result (LN_SCORES, LN_DLOGITS: columns from col0 on)
-    int            mt, nt, splits;        // pair row tiles, column tiles, parts of the contraction
+    int            mt, nt, splits;        // pair row tiles, column tiles, parts of the contraction (LN_OUTER: workers)
     int            width;                 // columns of a tile (LN_GATED: g's and u's together)
     float          whole;                 // logits: 1 + what the tensor core's sums are short by
     int            steps0, steps;         // steps of the first pair of operands, of both together
@@ -67,7 +68,7 @@ struct LNArgs {
     const float *  lse, *lse_lo, *coef;   // LN_DLOGITS [rows]
     const unsigned* top;                  // the largest |coef|, as bits, where coefficients carry a power of two; or null
     void*          y;                     // OUT_PLAIN, and the fill after a wait that gave up
-    int64_t        ldy;
+    int64_t        ldy, plane;            // elements between the result's rows; its parts or workers
     gar_checkpoint_t s0, s1;              // of g and u
 };
 
@@ -85,10 +86,18 @@ struct __align__(1024) LNSmem {
 struct Place {
     int m, n, split, first, steps;
 };
+template <int EPI>
 __device__ __forceinline__ Place place_at(const LNArgs& a, unsigned index) {
     Place t;
-    const unsigned split = a.splits > 1 ? index % unsigned(a.splits) : 0u;
-    if (a.splits > 1) index /= unsigned(a.splits);
+    unsigned split = 0;
+    if (EPI == LN_OUTER) {               // one worker after the other
+        const unsigned per = unsigned(a.mt) * unsigned(a.nt);
+        split = index / per;
+        index -= split * per;
+    } else if (a.splits > 1) {
+        split = index % unsigned(a.splits);
+        index /= unsigned(a.splits);
+    }
     const unsigned per_group = LN_GROUP_M * unsigned(a.nt), g = index / per_group, in_group = index - g * per_group;
     const unsigned rows = min(unsigned(LN_GROUP_M), unsigned(a.mt) - g * LN_GROUP_M);
     t.n = int(in_group / rows);
@@ -96,7 +105,7 @@ __device__ __forceinline__ Place place_at(const LNArgs& a, unsigned index) {
     t.split = int(split);
     t.first = 0;
     t.steps = a.steps;
-    if (a.splits > 1) {
+    if (EPI != LN_OUTER && a.splits > 1) {
         const int part = (a.steps + a.splits - 1) / a.splits;
         t.first = int(split) * part;
         t.steps = min(part, a.steps - t.first);
@@ -349,7 +358,8 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
     });
 }
 
-template <typename T>
+// (LN_OUTER: the result is not touched again and would drive the operands out of L2)
+template <typename T, int EPI>
 __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const Warp& w, const CUtensorMap* map) {
     const int64_t c0 = int64_t(t.n) * a.width;
     const int64_t left = a.cols - c0;
@@ -358,8 +368,14 @@ __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const 
     if (w.row0 >= a.rows || cols <= 0) return;
     const int64_t first = c0 + mine.from;
     const unsigned src = w.src + unsigned(mine.from);
+    const float by = a.top ? power_for(*a.top, true) : 1.f;
+    const unsigned long long policy = EPI == LN_OUTER ? evict_first() : 0;
     if (a.out >= OUT_PART) {
         over_columns(src, cols, [&](float (&v)[32], int at) {
+            if (a.top) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] *= by;
+            }
             stage_free(w);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -368,13 +384,13 @@ __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const 
             fence_async_smem();
             __syncwarp();
             if (w.lane == 0) {
-                if (a.out == OUT_ADD) tma_add(map, w.stage, int(first) + at, int(w.row0), t.split);
+                if (EPI == LN_OUTER) tma_store(map, w.stage, int(first) + at, int(w.row0), t.split, policy);
+                else if (a.out == OUT_ADD) tma_add(map, w.stage, int(first) + at, int(w.row0), t.split);
                 else tma_put(map, w.stage, int(first) + at, int(w.row0), t.split);
             }
         });
         return;
     }
-    const float by = a.top ? power_for(*a.top, true) : 1.f;
     int half = 0;
     over_columns(src, cols, [&](float (&v)[32], int at) {
         if (a.top) {
@@ -383,7 +399,15 @@ __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const 
         }
         if (half == 0) stage_free(w);
         stage32<T>(w.stage, w.lane, half, v);
-        if (half == 1 || at + 32 >= cols) put_piece(a, w, map, first + (at & ~63), cols - (at & ~63), 0);
+        if (half == 1 || at + 32 >= cols) {
+            if (EPI == LN_OUTER) {
+                fence_async_smem();
+                __syncwarp();
+                if (w.lane == 0) tma_store(map, w.stage, int(first) + (at & ~63), int(w.row0), t.split, policy);
+            } else {
+                put_piece(a, w, map, first + (at & ~63), cols - (at & ~63), 0);
+            }
+        }
         half ^= 1;
     });
 }
@@ -508,7 +532,7 @@ template <typename T, int EPI, int ACT>
 __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, const __grid_constant__ CUtensorMap map_a0,
                                                               const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_a1,
                                                               const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_out) {
-    constexpr bool B_MN = EPI == LN_SUM;
+    constexpr bool A_MN = EPI == LN_OUTER, B_MN = EPI == LN_SUM || EPI == LN_OUTER;
     extern __shared__ uint8_t raw[];
     LNSmem& sm = *reinterpret_cast<LNSmem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -551,7 +575,7 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
             const unsigned leader_full = pair_address(kb_smem_u32(sm.full), 0);
             unsigned g = 0;                                  // steps of all tiles so far
             for (unsigned i = pair; ok && i < tiles; i += pairs) {
-                const Place t = place_at(a, i);
+                const Place t = place_at<EPI>(a, i);
                 const int y = (2 * t.m + int(rank)) * LN_M;
                 for (int s = 0; s < t.steps; ++s, ++g) {
                     const Ring<LN_RING> r(g);
@@ -561,12 +585,18 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
                     const int step = t.first + s;
                     const bool second = step >= a.steps0;
                     const int k = (second ? step - a.steps0 : step) * LN_K;
-                    tma_load_pair(da, second ? &map_a1 : &map_a0, k, y, 0, bar);
+                    const int z = EPI == LN_OUTER ? t.split : 0;
+                    if (A_MN) {
+                        tma_load_pair(da, &map_a0, y, k, z, bar);
+                        tma_load_pair(da + LN_BLOCK, &map_a0, y + 64, k, z, bar);
+                    } else {
+                        tma_load_pair(da, second ? &map_a1 : &map_a0, k, y, 0, bar);
+                    }
                     if (B_MN) {
                         const int x = t.n * a.width + int(rank) * (a.width / 2);
                         const CUtensorMap* map = second ? &map_b1 : &map_b0;
-                        tma_load_pair(db, map, x, k, 0, bar);
-                        if (a.width == LN_N) tma_load_pair(db + LN_BLOCK, map, x + 64, k, 0, bar);
+                        tma_load_pair(db, map, x, k, z, bar);
+                        if (a.width == LN_N) tma_load_pair(db + LN_BLOCK, map, x + 64, k, z, bar);
                     } else if (EPI == LN_GATED) {
                         tma_load_pair(db, rank == 0 ? &map_b0 : &map_b1, k, t.n * (a.width / 2), 0, bar);
                     } else {
@@ -584,14 +614,14 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
     } else if (warp == LN_MMA_WARP) {
         // The whole warp walks the loop and one elected lane issues.
         if (rank == 0) {
-            const unsigned idesc = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, a.width, false, B_MN);
-            const unsigned long long desc_a = operand_desc(kb_smem_u32(sm.a), 16, 1024, 2);
+            const unsigned idesc = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, a.width, A_MN, B_MN);
+            const unsigned long long desc_a = operand_desc(kb_smem_u32(sm.a), A_MN ? LN_BLOCK : 16, 1024, 2);
             const unsigned long long desc_b = operand_desc(kb_smem_u32(sm.b), B_MN ? LN_BLOCK : 16, 1024, 2);
             // 16 elements of the contraction: 32 bytes along a K-major row, 16 rows of 128 bytes of an MN-major block
-            constexpr unsigned STEP_A = 2, STEP_B = B_MN ? 128 : 2;
+            constexpr unsigned STEP_A = A_MN ? 128 : 2, STEP_B = B_MN ? 128 : 2;
             unsigned g = 0, done = 0;
             for (unsigned i = pair; ok && i < tiles; i += pairs, ++done) {
-                const Place t = place_at(a, i);
+                const Place t = place_at<EPI>(a, i);
                 const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
                 const unsigned half = done & 1u, round = (done >> 1) & 1u, d = tmem + half * LN_N;
                 if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[half]), round ^ 1u, error)) { ok = false; break; }
@@ -630,7 +660,7 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
         w.lane = lane;
         unsigned done = 0;
         for (unsigned i = pair; i < tiles; i += pairs, ++done) {
-            const Place t = place_at(a, i);
+            const Place t = place_at<EPI>(a, i);
             const unsigned half = done & 1u;
             if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[half]), (done >> 1) & 1u, error)) break;
             tc_fence_after();
@@ -639,7 +669,7 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
             if constexpr (EPI == LN_SCORES) scores_tile<T>(a, t, w);
             if constexpr (EPI == LN_DLOGITS) dlogits_tile<T>(a, t, w, &map_out);
             if constexpr (EPI == LN_GATED) gated_tile<T, ACT>(a, t, w, &map_out);
-            if constexpr (EPI == LN_SUM) sum_tile<T>(a, t, w, &map_out);
+            if constexpr (EPI == LN_SUM || EPI == LN_OUTER) sum_tile<T, EPI>(a, t, w, &map_out);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_at_leader(&sm.acc_empty[half]);
@@ -660,14 +690,15 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
         // a wait gave up: nothing the pair was to write may look like a result
         const int WIDTH = EPI == LN_SCORES ? 1 : EPI == LN_GATED ? a.width / 2 : a.width;
         for (unsigned i = pair; i < tiles; i += pairs) {
-            const Place t = place_at(a, i);
+            const Place t = place_at<EPI>(a, i);
             for (int e = tid; e < LN_M * WIDTH; e += LN_THREADS) {
                 const int64_t row = int64_t(2 * t.m + int(rank)) * LN_M + e / WIDTH, c = int64_t(t.n) * WIDTH + e % WIDTH;
                 if (row >= a.rows) continue;
                 if constexpr (EPI == LN_SCORES) a.parts[(row * a.nt + t.n) * 2] = a.parts[(row * a.nt + t.n) * 2 + 1] = make_float2(CUDART_NAN_F, CUDART_NAN_F);
                 else if (c < a.cols) {
-                    if (EPI == LN_SUM && a.out >= OUT_PART) static_cast<float*>(a.y)[(int64_t(t.split) * a.rows + row) * a.ldy + c] = CUDART_NAN_F;
-                    else static_cast<T*>(a.y)[row * a.ldy + c] = Elem<T>::narrow(CUDART_NAN_F);
+                    const int64_t at = int64_t(t.split) * a.plane + row * a.ldy + c;
+                    if (a.out >= OUT_PART) static_cast<float*>(a.y)[at] = CUDART_NAN_F;
+                    else static_cast<T*>(a.y)[at] = Elem<T>::narrow(CUDART_NAN_F);
                     if (EPI == LN_GATED && (c & ((1 << a.group_shift) - 1)) == 0) {
                         if (a.s0.q) a.s0.scales[row * a.groups + (c >> a.group_shift)] = CUDART_NAN_F;
                         if (a.s1.q) a.s1.scales[row * a.groups + (c >> a.group_shift)] = CUDART_NAN_F;
@@ -772,6 +803,38 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const CopyArgs a) {
         }
         j.dst[i] = w;
     }
+}
+
+// Bias gradients: the columns of a worker's dz added up, eight columns and an eighth of the tokens per thread, the
+// eighths in order.
+template <typename T, typename G>
+__global__ void __launch_bounds__(256) column_sums_kernel(const T* dz, int64_t ld, int64_t tokens, int64_t cols, const unsigned* top, G* db, int64_t ld_grads) {
+    __shared__ float sums[8][32][9];
+    grid_dependency();
+    const int64_t c = (int64_t(blockIdx.x) * 32 + threadIdx.x % 32) * 8;
+    const int part = threadIdx.x / 32;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const T* p = dz + int64_t(blockIdx.y) * tokens * ld + c;
+    // (rows of dz are padded to whole pieces; what lies behind the last column is added and not stored)
+    if (c < cols) {
+#pragma unroll 4
+        for (int64_t t = part; t < tokens; t += 8) {
+            float v[8];
+            widen16B(__ldg(reinterpret_cast<const uint4*>(p + t * ld)), v, static_cast<const T*>(nullptr));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] += v[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[part][threadIdx.x % 32][j] = s[j];
+    __syncthreads();
+    const int64_t mine = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (mine >= cols) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += sums[k][threadIdx.x / 8][threadIdx.x % 8];
+    if (top) sum *= power_for(*top, true);
+    db[int64_t(blockIdx.y) * ld_grads + mine] = Elem<G>::narrow(sum);
 }
 
 // The parts of a sum, added in order and rounded once, four columns per thread and turn.
@@ -999,6 +1062,7 @@ cudaError_t launch_sum(const SumTarget& d, const Operand& a0, const Operand& b0,
         a.out = add ? OUT_ADD : OUT_PART;
         a.y = d.parts;
         a.ldy = d.pitch;
+        a.plane = d.pitch * d.rows;
         if (cudaError_t err = make_map(&maps.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d.parts, d.cols, d.rows, d.splits, d.pitch * 4, d.pitch * 4 * d.rows, 32, 32,
                                        CU_TENSOR_MAP_SWIZZLE_128B)) return err;
     } else {
@@ -1018,6 +1082,61 @@ cudaError_t join_sum(const SumTarget& d, int sm_count, cudaStream_t stream) {
                             static_cast<__nv_bfloat16*>(d.dx), d.ld);
     return launch_small(join_parts_kernel<__half>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top,
                         static_cast<__half*>(d.dx), d.ld);
+}
+
+// ---- weight gradients -------------------------------------------------------------------------------
+// Where this kernel makes them: sums short enough for one accumulator (see gar_linear_weight_grad's chunks) and rows of the
+// block that TMA stores.  Two store groups, and a pair's next tile in the other half of tensor memory, keep up with the block's rows
+// where there are few tokens to a tile: 11 workers x 128 tokens, 16128 x 1024, bf16 rows: 98 us by weight_grad_kernel's four
+// store warps.  Elsewhere weight_grad_kernel makes them.
+bool outer_applies(const DenseWeightGrad& g) {
+    const int64_t gs = g.grads_dtype == GAR_F32 ? 4 : 2;
+    if (g.tokens < 1 || g.tokens > (gs == 4 ? 768 : 2048)) return false;
+    return reinterpret_cast<uintptr_t>(g.dw) % 16 == 0 && (g.workers == 1 || g.ld_grads * gs % 16 == 0) && g.in * gs % 16 == 0 &&
+           (gs == 4 || g.grads_dtype == g.dtype) && parts_of(g.out, 2 * LN_M) * parts_of(g.in, LN_N) < (int64_t(1) << 30) / g.workers / 2;
+}
+cudaError_t token_map(CUtensorMap* map, int dtype, const void* p, int64_t cols, int64_t ld, const DenseWeightGrad& g) {
+    return make_map(map, map_type(dtype), p, cols, g.tokens, g.workers, ld * 2, ld * 2 * g.tokens, 64, LN_K, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+cudaError_t launch_outer(const DenseWeightGrad& g, int sm_count, cudaStream_t stream) {
+    Maps maps;
+    LNArgs a{};
+    const bool wide = g.grads_dtype == GAR_F32;
+    const int64_t gs = wide ? 4 : 2;
+    a.rows = g.out;
+    a.cols = g.in;
+    a.mt = int(parts_of(g.out, 2 * LN_M));
+    a.splits = g.workers;
+    a.steps0 = a.steps = int(parts_of(g.tokens, LN_K));
+    a.width = width_for(int64_t(a.mt) * g.workers, g.in, a.steps, 128);
+    a.nt = int(parts_of(g.in, a.width));
+    a.out = wide ? OUT_PART : OUT_WIDE;
+    a.top = g.top;
+    a.y = g.dw;
+    a.ldy = g.in;
+    a.plane = g.ld_grads;
+    if (cudaError_t err = token_map(&maps.a0, g.dtype, g.dy, g.out, g.ld_dy, g)) return err;
+    if (cudaError_t err = token_map(&maps.b0, g.dtype, g.x, g.in, g.ldx, g)) return err;
+    maps.a1 = maps.b1 = maps.a0;                       // not used
+    const int64_t plane = g.workers > 1 ? g.ld_grads * gs : g.in * g.out * gs;
+    if (cudaError_t err = make_map(&maps.out, wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : map_type(g.dtype), g.dw, g.in, g.out, g.workers, g.in * gs, plane,
+                                   int(128 / gs), 32, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
+    return launch<LN_OUTER>(g.dtype, a, maps, sm_count, stream);
+}
+template <typename T>
+cudaError_t column_sums(const DenseWeightGrad& g, cudaStream_t stream) {
+    const dim3 grid(unsigned(parts_of(g.out, 256)), unsigned(g.workers));
+    const T* dz = static_cast<const T*>(g.dy);
+    if (g.grads_dtype == GAR_F32) return launch_small(column_sums_kernel<T, float>, grid, stream, dz, g.ld_dy, g.tokens, g.out, g.top, static_cast<float*>(g.db), g.ld_grads);
+    if (g.grads_dtype == GAR_BF16)
+        return launch_small(column_sums_kernel<T, __nv_bfloat16>, grid, stream, dz, g.ld_dy, g.tokens, g.out, g.top, static_cast<__nv_bfloat16*>(g.db), g.ld_grads);
+    return launch_small(column_sums_kernel<T, __half>, grid, stream, dz, g.ld_dy, g.tokens, g.out, g.top, static_cast<__half*>(g.db), g.ld_grads);
+}
+cudaError_t weight_grad(DenseWeightGrad g, int sm_count, cudaStream_t stream) {
+    if (!outer_applies(g)) return launch_dense_weight_grad(g, sm_count, stream);
+    if (cudaError_t err = launch_outer(g, sm_count, stream)) return err;
+    if (!g.db) return cudaSuccess;
+    return g.dtype == GAR_BF16 ? column_sums<__nv_bfloat16>(g, stream) : column_sums<__half>(g, stream);
 }
 
 // ---- log probabilities ------------------------------------------------------------------------------
@@ -1187,7 +1306,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
             g.ld_grads = p.ld_grads;
             g.top = plan.top;
             g.workspace = plan.weight_space;
-            if (cudaError_t err = launch_dense_weight_grad(g, sm_count, stream)) return err;
+            if (cudaError_t err = weight_grad(g, sm_count, stream)) return err;
         }
     }
     return d.parts && plan.rows > 0 ? join_sum(d, sm_count, stream) : cudaSuccess;
