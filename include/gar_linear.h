@@ -17,7 +17,7 @@
  * GAR_ERR_UNSUPPORTED except for dropout), exact, summed in fp32 on the tensor
  * cores, which truncate where they add: a sum over k terms is short by some
  * 1e-9 k of itself (2.8e-9 k where it grows steadily); no sum has more than
- * 2^14 terms before it is added, rounded, to the others, but for sums over
+ * 2^15 terms before it is added, rounded, to the others, but for sums over
  * `hidden` and `inner`.  Everything after a product is fp32, each output rounded once.
  *
  * Workspaces: 256-byte aligned, of at least the bytes the sizes call returns
@@ -71,7 +71,7 @@ size_t gar_linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t* p
  *     dz_ij = a_i ([j = t_i] - e^(z_ij - lse_i))         (z computed again, dz rounded to x's type)
  *     dx = dz W,    dW_w = dz_w^T x_w,    db_w[j] = sum_i dz_ij over the worker's rows
  * the latter two stored at weight_grads[w * ld_grads + j * hidden + k] and bias_grads[w * ld_grads + j], as by
- * gar_linear_weight_grad.  The vocabulary is gone through in pieces, whose dz is kept in the workspace: up to 64 MB of
+ * gar_linear_weight_grad.  The vocabulary is gone through in pieces, whose dz is kept in the workspace: up to 96 MB of
  * it.  binary16 dz carry a power of two taken from the largest |a|, so that small gradients do not underflow.
  *   - A row without a target, or with a = 0, gets dx 0 and nothing it holds, NaN included, reaches a weight gradient.
  *   - A row masked throughout has gradient 0; in any other row a target >= vocab gives NaN, in dx and

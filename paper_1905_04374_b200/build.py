@@ -34,7 +34,7 @@ def _units():
              ("k2_select.cu", "k2_select.o", []),
              ("k3_dispatch.cu", "k3_dispatch.o", []),
              ("gar_api.cu", "gar_api.o", [])]
-    for name in ("logprobs", "checkpoint", "wgrad", "linear", "dropout", "api", "linear_api"):
+    for name in ("logprobs", "checkpoint", "wgrad", "linear", "few", "dropout", "api", "linear_api"):
         units.append((f"worker_{name}.cu", f"worker_{name}.o", []))
     for p in K3_P:
         units.append(("k3_inst.cu", f"k3_inst_{p}.o", [f"-DK3_P={p}", f"-DK3_EXACT={1 if p <= 32 else 0}"]))

@@ -11,7 +11,9 @@ namespace gar {
 namespace worker {
 namespace {
 
-constexpr int DO_THREADS = 256, DO_TASKS = 2;          // tasks of eight columns per thread: all loads first
+constexpr int DO_THREADS = 256;
+// tasks of eight columns per thread, all loads first: enough of them in flight to cover the memory's latency
+template <typename T> struct Tasks { static constexpr int N = sizeof(T) == 4 ? 2 : 4; };
 
 struct DropoutArgs {
     const void *x, *residual;
@@ -43,39 +45,51 @@ __device__ __forceinline__ Random8 philox(const DropoutArgs& a, uint64_t block, 
     return Random8{{c0, c1, c2, c3}};
 }
 
-// Eight consecutive elements, 16 bytes at a time or (VEC false) one by one, as far as they exist.
+// Eight consecutive elements as they lie in memory: 16 bytes at a time, or (VEC false) one by one, as far as they exist.
+template <typename T> struct Raw8 { uint4 w[sizeof(T) / 2]; };
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int count, float (&v)[8]) {
-    if constexpr (VEC) {
-        if (count == 8) {
-            if constexpr (sizeof(T) == 4) {
-                float a[4], b[4];
-                widen16B(load_stream(p), a, static_cast<const T*>(nullptr));
-                widen16B(load_stream(p + 4), b, static_cast<const T*>(nullptr));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-            } else {
-                widen16B(load_stream(p), v, static_cast<const T*>(nullptr));
-            }
-            return;
-        }
+__device__ __forceinline__ Raw8<T> load8(const T* p, int count) {
+    Raw8<T> r;
+    if (VEC && count == 8) {
+        r.w[0] = load_stream(p);
+        if constexpr (sizeof(T) == 4) r.w[1] = load_stream(p + 4);
+        return r;
     }
+    float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < count ? Elem<T>::widen(p[i]) : 0.f;
+    if constexpr (sizeof(T) == 4) {
+        const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+        r.w[0] = narrow16B(a, static_cast<const T*>(nullptr));
+        r.w[1] = narrow16B(b, static_cast<const T*>(nullptr));
+    } else {
+        r.w[0] = narrow16B(v, static_cast<const T*>(nullptr));
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw8<T>& r, float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        float a[4], b[4];
+        widen16B(r.w[0], a, static_cast<const T*>(nullptr));
+        widen16B(r.w[1], b, static_cast<const T*>(nullptr));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    } else {
+        widen16B(r.w[0], v, static_cast<const T*>(nullptr));
+    }
 }
 template <typename T, bool VEC>
 __device__ __forceinline__ void store8(T* p, int count, const float (&v)[8]) {
-    if constexpr (VEC) {
-        if (count == 8) {
-            if constexpr (sizeof(T) == 4) {
-                const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
-                store_stream(p, narrow16B(a, static_cast<const T*>(nullptr)));
-                store_stream(p + 4, narrow16B(b, static_cast<const T*>(nullptr)));
-            } else {
-                store_stream(p, narrow16B(v, static_cast<const T*>(nullptr)));
-            }
-            return;
+    if (VEC && count == 8) {
+        if constexpr (sizeof(T) == 4) {
+            const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+            store_stream(p, narrow16B(a, static_cast<const T*>(nullptr)));
+            store_stream(p + 4, narrow16B(b, static_cast<const T*>(nullptr)));
+        } else {
+            store_stream(p, narrow16B(v, static_cast<const T*>(nullptr)));
         }
+        return;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -89,7 +103,8 @@ template <typename T, int LAYOUT, bool RESIDUAL>
 __global__ void __launch_bounds__(DO_THREADS) dropout_kernel(const DropoutArgs a) {
     const uint64_t offset = a.offset + (a.counter ? *a.counter : 0);
     constexpr bool VEC = LAYOUT != DO_ANY;
-    float x[DO_TASKS][8], r[DO_TASKS][8];
+    constexpr int DO_TASKS = Tasks<T>::N;
+    Raw8<T> x[DO_TASKS], r[DO_TASKS];
     int64_t row[DO_TASKS], col[DO_TASKS];
     int count[DO_TASKS];
 #pragma unroll
@@ -107,21 +122,23 @@ __global__ void __launch_bounds__(DO_THREADS) dropout_kernel(const DropoutArgs a
             count[k] = n >= a.tasks ? 0 : left < 8 ? int(left) : 8;
         }
         if (count[k] == 0) continue;
-        load8<T, VEC>(static_cast<const T*>(a.x) + row[k] * a.ldx + col[k], count[k], x[k]);
-        if (RESIDUAL) load8<T, VEC>(static_cast<const T*>(a.residual) + row[k] * a.ldr + col[k], count[k], r[k]);
+        x[k] = load8<T, VEC>(static_cast<const T*>(a.x) + row[k] * a.ldx + col[k], count[k]);
+        if (RESIDUAL) r[k] = load8<T, VEC>(static_cast<const T*>(a.residual) + row[k] * a.ldr + col[k], count[k]);
     }
     const unsigned limit = a.limit << 16;              // (limit = 2^16: nothing is kept, scale 0)
 #pragma unroll
     for (int k = 0; k < DO_TASKS; ++k) {
         if (count[k] == 0) continue;
         const Random8 d = philox(a, uint64_t(a.blocks0) + (blockIdx.x * DO_TASKS + k) * DO_THREADS + threadIdx.x, offset);
-        float y[8];
+        float y[8], vx[8], vr[8];
+        widen8<T>(x[k], vx);
+        if (RESIDUAL) widen8<T>(r[k], vr);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             // a half against the limit: both in the high half of a word, where what is below does not matter
             const bool kept = (i & 1 ? d.w[i / 2] : d.w[i / 2] << 16) >= limit && a.limit < 65536u;
-            const float none = RESIDUAL ? r[k][i] : 0.f;
-            const float some = RESIDUAL ? fmaf(x[k][i], a.scale, none) : x[k][i] * a.scale;
+            const float none = RESIDUAL ? vr[i] : 0.f;
+            const float some = RESIDUAL ? fmaf(vx[i], a.scale, none) : vx[i] * a.scale;
             y[i] = kept ? some : none;
         }
         store8<T, VEC>(static_cast<T*>(a.y) + row[k] * a.ldy + col[k], count[k], y);
@@ -137,6 +154,7 @@ cudaError_t launch_as(const gar_dropout_params_t& p, DropoutArgs& a) {
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     const bool vec = wide<T>(p.x, p.ldx) && wide<T>(p.residual, p.ld_residual) && wide<T>(p.y, p.ldy);
     const unsigned per_row = a.per_row.d;
+    constexpr int DO_TASKS = Tasks<T>::N;
     const bool dense = vec && p.cols % 8 == 0 && p.ldx == p.cols && p.ldy == p.cols && (!p.residual || p.ld_residual == p.cols);
     const int64_t step = ((int64_t(1) << 31) - DO_THREADS * DO_TASKS) / per_row;           // rows of a launch
     for (int64_t r0 = 0; r0 < p.rows; r0 += step) {

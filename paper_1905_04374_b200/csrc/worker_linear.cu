@@ -40,7 +40,6 @@ constexpr int LN_BLOCK = 64 * 128;                    // bytes of 64 x 64 elemen
 constexpr int LN_COPY_WARP = 0, LN_MMA_WARP = 1, LN_ALLOC_WARP = 2;
 constexpr int LN_STORE_WARP0 = 4, LN_STORE_WARPS = 8;
 constexpr int LN_THREADS = 32 * (LN_STORE_WARP0 + LN_STORE_WARPS);
-constexpr int LN_GROUP_M = 8;                         // (pair) row tiles that go round a column tile together
 constexpr int LN_PAIRS = 74;                          // pairs of SMs, for the rules that cut work into parts and tiles
 constexpr float LN_SHORT = 1.0e-9f;                   // of a sum, lost per term
 
@@ -57,6 +56,7 @@ struct LNArgs {
     int64_t        rows, cols;            // of the result (LN_SCORES, LN_DLOGITS: columns from col0 on)
     int            mt, nt, splits;        // pair row tiles, column tiles, parts of the contraction (LN_OUTER: workers)
     int            width;                 // columns of a tile (LN_GATED: g's and u's together)
+    int            group_m;               // (pair) row tiles that go round a column tile together
     float          whole;                 // logits: 1 + what the tensor core's sums are short by
     int            steps0, steps;         // steps of the first pair of operands, of both together
     int            group_shift, groups, out;
@@ -98,10 +98,10 @@ __device__ __forceinline__ Place place_at(const LNArgs& a, unsigned index) {
         split = index % unsigned(a.splits);
         index /= unsigned(a.splits);
     }
-    const unsigned per_group = LN_GROUP_M * unsigned(a.nt), g = index / per_group, in_group = index - g * per_group;
-    const unsigned rows = min(unsigned(LN_GROUP_M), unsigned(a.mt) - g * LN_GROUP_M);
+    const unsigned group_m = unsigned(a.group_m), per_group = group_m * unsigned(a.nt), g = index / per_group, in_group = index - g * per_group;
+    const unsigned rows = min(group_m, unsigned(a.mt) - g * group_m);
     t.n = int(in_group / rows);
-    t.m = int(g * LN_GROUP_M + in_group - unsigned(t.n) * rows);
+    t.m = int(g * group_m + in_group - unsigned(t.n) * rows);
     t.split = int(split);
     t.first = 0;
     t.steps = a.steps;
@@ -948,8 +948,13 @@ struct Copies {
 struct Maps {
     CUtensorMap a0, b0, a1, b1, out;
 };
+// Row tiles that go round a column tile together: B is read from memory once for each such group of rows of A, which
+// should stay in L2: 32 MB of them.  8192 rows, 4096 x 8192 gated: 785 us in groups of 8, 772 of 16 (32 MB), 785 of 24, 829 of 32;
+// 2048 x 32000: 775 of 8, 755 of 16, 744 of 32 (32 MB).
+int group_rows(int64_t steps) { return int(std::max<int64_t>(8, 1024 / steps)); }
+
 template <typename T, int EPI, int ACT>
-cudaError_t launch_as(const LNArgs& a, const Maps& maps, int sm_count, cudaStream_t stream) {
+cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t stream) {
     constexpr int bytes = int(sizeof(LNSmem)) + 1024;
     static_assert(bytes <= 232448, "a CTA's shared memory");
     auto kernel = linear_kernel<T, EPI, ACT>;
@@ -960,6 +965,7 @@ cudaError_t launch_as(const LNArgs& a, const Maps& maps, int sm_count, cudaStrea
         if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
         if (dev < 64) allowed.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
     }
+    a.group_m = group_rows(a.steps);
     const int64_t tiles = int64_t(a.mt) * a.nt * a.splits;
     if (tiles >= int64_t(1) << 30) return cudaErrorInvalidConfiguration;
     const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
@@ -1140,8 +1146,9 @@ cudaError_t weight_grad(DenseWeightGrad g, int sm_count, cudaStream_t stream) {
 }
 
 // ---- log probabilities ------------------------------------------------------------------------------
-constexpr int64_t LN_PARTS_BYTES = int64_t(64) << 20, LN_PIECE_BYTES = int64_t(64) << 20;
-constexpr int64_t LN_PIECE_MAX = 16384;
+constexpr int64_t LN_PARTS_BYTES = int64_t(64) << 20, LN_PIECE_BYTES = int64_t(96) << 20;
+constexpr int64_t LN_PIECE_MAX = 32768;
+constexpr int64_t LN_FEW_PARTS = 512;                          // CTAs of a few rows' kernel at most: two per SM
 constexpr int LN_SCORES_UNIT = 32, LN_STORE_UNIT = 64;         // columns: of a thread's turn; of a staged piece
 // rows of a launch, so that its parts take 64 MB or so
 int64_t rows_at_once(int64_t rows, int64_t vocab) {
@@ -1159,15 +1166,16 @@ struct ScoresPlan {
     float*  target_z;
     ScoresPlan(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw)
         : space(p.workspace), x(space, p.x, p.rows, p.hidden, ldx), w(space, p.weight, p.vocab, p.hidden, ldw), rows(rows_at_once(p.rows, p.vocab)) {
-        // (the last rows, if they are fewer, may have narrower tiles)
+        // (the last rows, if they are fewer, may have narrower tiles; a few rows have a part per CTA)
         const int64_t last = (p.rows - 1) % rows + 1;
-        const int64_t most = std::max(rows * scores_tiles(rows, p.hidden, p.vocab), last * scores_tiles(last, p.hidden, p.vocab));
+        const int64_t most = p.rows <= 16 ? std::max(p.rows * scores_tiles(p.rows, p.hidden, p.vocab), (p.rows * LN_FEW_PARTS + 1) / 2)
+                                          : std::max(rows * scores_tiles(rows, p.hidden, p.vocab), last * scores_tiles(last, p.hidden, p.vocab));
         parts = reinterpret_cast<float2*>(space.take(size_t(most) * 16));
         target_z = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
     }
 };
 
-// Columns of a piece of the vocabulary: dz of up to 64 MB, and sums of no more than 2^14 terms; equal pieces.
+// Columns of a piece of the vocabulary: dz of up to 96 MB (L2 holds it), and sums of no more than 2^15 terms; equal pieces.
 int64_t piece_of(int64_t rows, int64_t vocab) {
     const int64_t most = std::max<int64_t>(LN_N, std::min<int64_t>(LN_PIECE_MAX, LN_PIECE_BYTES / (2 * rows) / LN_N * LN_N));
     return up_to(parts_of(vocab, parts_of(vocab, most)), LN_N);
@@ -1216,6 +1224,12 @@ size_t linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t& p, in
 cudaError_t launch_linear_logprobs(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw, int sm_count) {
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     ScoresPlan plan(p, ldx, ldw);
+    if (few_rows_applies(p.rows, p.hidden, p.weight, ldw, nullptr, 0) && few_scores_parts(sm_count) <= LN_FEW_PARTS) {
+        int count = 0;
+        if (cudaError_t err = launch_few_scores(p, ldx, ldw, 1.f + LN_SHORT * float(p.hidden), plan.parts, plan.target_z, &count, sm_count)) return err;
+        return launch_small(join_scores_kernel, dim3(unsigned(parts_of(p.rows, 8))), stream, plan.parts, plan.target_z, p.logprobs ? p.targets : nullptr, p.rows,
+                            count, p.vocab, p.logprobs, p.lse, p.lse_lo);
+    }
     Copies copies;
     copies.add(plan.x);
     copies.add(plan.w);
@@ -1345,6 +1359,8 @@ size_t gated_linear_workspace_bytes(const gar_gated_linear_params_t& p) {
 cudaError_t launch_gated_linear_forward(const gar_gated_linear_params_t& p, int sm_count) {
     cudaStream_t stream = static_cast<cudaStream_t>(p.stream);
     GatedPlan plan(p);
+    if (!p.gate_saved.q && !p.up_saved.q && !p.y_saved.q && few_rows_applies(p.rows, p.hidden, p.w_gate, p.ld_gate, p.w_up, p.ld_up))
+        return launch_few_gated(p, sm_count);
     Copies copies;
     for (Input* in : {&plan.x, &plan.gate, &plan.up}) copies.add(*in);
     if (cudaError_t err = copies.launch(sm_count, stream)) return err;
