@@ -1095,15 +1095,18 @@ cudaError_t join_sum(const SumTarget& d, int sm_count, cudaStream_t stream) {
 // block that TMA stores.  Two store groups, and a pair's next tile in the other half of tensor memory, keep up with the block's rows
 // where there are few tokens to a tile: 11 workers x 128 tokens, 16128 x 1024, bf16 rows: 98 us by weight_grad_kernel's four
 // store warps.  Elsewhere weight_grad_kernel makes them.
+}  // namespace
 bool outer_applies(const DenseWeightGrad& g) {
     const int64_t gs = g.grads_dtype == GAR_F32 ? 4 : 2;
     if (g.tokens < 1 || g.tokens > (gs == 4 ? 768 : 2048)) return false;
     return reinterpret_cast<uintptr_t>(g.dw) % 16 == 0 && (g.workers == 1 || g.ld_grads * gs % 16 == 0) && g.in * gs % 16 == 0 &&
            (gs == 4 || g.grads_dtype == g.dtype) && parts_of(g.out, 2 * LN_M) * parts_of(g.in, LN_N) < (int64_t(1) << 30) / g.workers / 2;
 }
+namespace {
 cudaError_t token_map(CUtensorMap* map, int dtype, const void* p, int64_t cols, int64_t ld, const DenseWeightGrad& g) {
     return make_map(map, map_type(dtype), p, cols, g.tokens, g.workers, ld * 2, ld * 2 * g.tokens, 64, LN_K, CU_TENSOR_MAP_SWIZZLE_128B);
 }
+}  // namespace
 cudaError_t launch_outer(const DenseWeightGrad& g, int sm_count, cudaStream_t stream) {
     Maps maps;
     LNArgs a{};
@@ -1129,6 +1132,7 @@ cudaError_t launch_outer(const DenseWeightGrad& g, int sm_count, cudaStream_t st
                                    int(128 / gs), 32, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
     return launch<LN_OUTER>(g.dtype, a, maps, sm_count, stream);
 }
+namespace {
 template <typename T>
 cudaError_t column_sums(const DenseWeightGrad& g, cudaStream_t stream) {
     const dim3 grid(unsigned(parts_of(g.out, 256)), unsigned(g.workers));

@@ -35,6 +35,10 @@ struct DenseWeightGrad {
     const unsigned* top;              // dy carries power_for(*top); or null
     void*           workspace;        // of dense_weight_grad_workspace_bytes
 };
+// By the product with two store groups (worker_linear.cu): whether it applies, and the launch (weights only).
+bool outer_applies(const DenseWeightGrad& g);
+cudaError_t launch_outer(const DenseWeightGrad& g, int sm_count, cudaStream_t stream);
+// By weight_grad_kernel.
 size_t dense_weight_grad_workspace_bytes(int workers, int64_t tokens, int64_t out, int64_t in, bool bias);
 cudaError_t launch_dense_weight_grad(const DenseWeightGrad& g, int sm_count, cudaStream_t stream);
 
