@@ -34,8 +34,10 @@ namespace {
 
 constexpr int LN_M = 128, LN_N = 256, LN_K = 64;      // rows of a CTA, columns of a pair, contraction per step
 constexpr int LN_HALF = LN_N / 2;                     // rows of B that a CTA holds
-constexpr int LN_RING = 5;                            // steps in flight
-constexpr int LN_TILE = LN_M * LN_K * 2;              // bytes of an operand per step and CTA
+constexpr int LN_TILE = LN_M * LN_K * 2;              // bytes of A (and, at full width, of B) per step and CTA
+// Steps in flight: five of full width; narrow tiles have more in the same memory, since a step's copies take some 2000 cycles to come
+// and a few narrow tiles wait for nothing else.
+constexpr int LN_RING_BYTES = 5 * 2 * LN_TILE, LN_RING_MOST = 8;
 constexpr int LN_BLOCK = 64 * 128;                    // bytes of 64 x 64 elements of an MN-major operand
 constexpr int LN_COPY_WARP = 0, LN_MMA_WARP = 1, LN_ALLOC_WARP = 2;
 constexpr int LN_STORE_WARP0 = 4, LN_STORE_WARPS = 8;
@@ -56,6 +58,7 @@ struct LNArgs {
     int64_t        rows, cols;            // of the result (LN_SCORES, LN_DLOGITS: columns from col0 on)
     int            mt, nt, splits;        // pair row tiles, column tiles, parts of the contraction (LN_OUTER: workers)
     int            width;                 // columns of a tile (LN_GATED: g's and u's together)
+    int            ring, slot_bytes;      // steps in flight, what one takes in shared memory
     int            group_m;               // (pair) row tiles that go round a column tile together
     float          whole;                 // logits: 1 + what the tensor core's sums are short by
     int            steps0, steps;         // steps of the first pair of operands, of both together
@@ -73,14 +76,24 @@ struct LNArgs {
 };
 
 struct __align__(1024) LNSmem {
-    uint8_t  a[LN_RING][LN_TILE];
-    uint8_t  b[LN_RING][LN_TILE];
+    uint8_t  ring[LN_RING_BYTES];                         // slots: 128 rows of A, half the tile's rows of B
     uint8_t  out[LN_STORE_WARPS][32 * 128];               // a store warp's piece: 32 rows of 128 bytes
     float    add[LN_STORE_WARPS][LN_N];                   // a warp's biases, -inf for columns that do not exist
-    unsigned long long empty[LN_RING], acc_full[2];       // the slots are read; the accumulators are complete
-    unsigned long long full[LN_RING], acc_empty[2];       // the leading CTA's are used, for both
+    unsigned long long empty[LN_RING_MOST], acc_full[2];  // the slots are read; the accumulators are complete
+    unsigned long long full[LN_RING_MOST], acc_empty[2];  // the leading CTA's are used, for both
     unsigned tmem_base;
     int      error, other_error;                          // a wait gave up, here or in the other CTA
+};
+
+// The ring's slots, one after the other.
+struct Slot {
+    unsigned slot = 0, parity = 0;
+    __device__ __forceinline__ void next(const LNArgs& a) {
+        if (++slot == unsigned(a.ring)) {
+            slot = 0;
+            parity ^= 1u;
+        }
+    }
 };
 
 struct Place {
@@ -212,11 +225,18 @@ __device__ __forceinline__ void store_plain(unsigned stage, int lane, unsigned s
     }
 }
 
-// The columns' biases of a warp's tile: `n` from column c0 on, `fill` where there is no column
+// 128 columns' biases from column c0 on, `fill` where there is no column
 template <typename T>
-__device__ __forceinline__ void fetch_biases(const void* bias, int64_t c0, int64_t cols, int n, float fill, float* add, int lane) {
-    for (int j = lane; j < n; j += 32)
-        add[j] = c0 + j >= cols ? fill : bias ? Elem<T>::widen(static_cast<const T*>(bias)[c0 + j]) : 0.f;
+__device__ __forceinline__ void fetch_biases(const void* bias, int64_t c0, int64_t cols, float fill, float* add, int lane) {
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t c = c0 + 32 * k + lane;
+        v[k] = c >= cols ? fill : 0.f;
+        if (bias && c < cols) v[k] = Elem<T>::widen(static_cast<const T*>(bias)[c]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) add[32 * k + lane] = v[k];
 }
 
 // ---- epilogues: one warp's 32 rows and its group's columns of a tile -------------------------------
@@ -236,21 +256,50 @@ struct Columns {
     }
 };
 
-template <typename T>
-__device__ __forceinline__ void scores_tile(const LNArgs& a, const Place& t, const Warp& w) {
+// What a warp reads for a tile from memory, while the tile's products still run: its columns' biases, into its piece of shared
+// memory, and what belongs to its rows.
+struct RowInputs {
+    int64_t target;                  // from the launch's first column on; negative: none here
+    float   coef, lse, lo;
+};
+template <typename T, int EPI>
+__device__ __forceinline__ RowInputs fetch_inputs(const LNArgs& a, const Place& t, const Warp& w) {
+    RowInputs in{-1, 0.f, 0.f, 0.f};
+    if (w.row0 >= a.rows) return in;
+    const int64_t row = w.row0 + w.lane;
+    if (EPI == LN_GATED) {
+        const int64_t c0 = int64_t(t.n) * (a.width / 2);
+        if (a.bias || a.bias2) {
+            fetch_biases<T>(a.bias, c0, a.cols, 0.f, w.add, w.lane);
+            fetch_biases<T>(a.bias2, c0, a.cols, 0.f, w.add + LN_HALF, w.lane);
+        }
+    }
+    if (EPI == LN_SCORES || EPI == LN_DLOGITS) {
+        const int64_t c0 = int64_t(t.n) * a.width, left = a.cols - c0;
+        if (a.bias || (EPI == LN_SCORES && left < a.width)) {
+            const Columns mine(left < a.width ? int(left) : a.width, w.group, EPI == LN_SCORES ? 32 : 64);
+            fetch_biases<T>(a.bias, a.col0 + c0 + mine.from, a.col0 + a.cols, -CUDART_INF_F, w.add, w.lane);
+        }
+        if (row < a.rows && a.targets) in.target = a.targets[row] - a.col0;
+    }
+    if (EPI == LN_DLOGITS && row < a.rows) {
+        in.coef = a.coef[row];
+        in.lse = a.lse[row];
+        if (a.lse_lo) in.lo = a.lse_lo[row];
+        if (a.top) in.coef *= power_for(*a.top, false);
+    }
+    return in;
+}
+
+__device__ __forceinline__ void scores_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in) {
     const int64_t c0 = int64_t(t.n) * a.width, row = w.row0 + w.lane;
     if (w.row0 >= a.rows) return;
     const int64_t left = a.cols - c0;
     const Columns mine(left < a.width ? int(left) : a.width, w.group, 32);
     const int cols = mine.to - mine.from;
-    const bool adds = a.bias || (cols & 31);
-    if (adds) {
-        fetch_biases<T>(a.bias, c0 + mine.from, a.cols, LN_HALF, -CUDART_INF_F, w.add, w.lane);
-        __syncwarp();
-    }
-    const bool live = row < a.rows;
-    const int64_t t64 = a.targets && live ? a.targets[row] - c0 - mine.from : -1;
-    const int target = t64 >= 0 && t64 < cols ? int(t64) : -1;
+    const bool adds = a.bias || left < a.width, live = row < a.rows;
+    const int64_t t64 = in.target - c0 - mine.from;
+    const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
     float m = -CUDART_INF_F, s = 0.f;
     if (cols > 0)
         over_columns(w.src + unsigned(mine.from), cols, [&](float (&v)[32], int at) {
@@ -308,28 +357,18 @@ __device__ __forceinline__ void put_piece(const LNArgs& a, const Warp& w, const 
 }
 
 template <typename T>
-__device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, const Warp& w, const CUtensorMap* map) {
-    const int64_t c0 = int64_t(t.n) * a.width, row = w.row0 + w.lane;
+__device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in, const CUtensorMap* map) {
+    const int64_t c0 = int64_t(t.n) * a.width;
     const int64_t left = a.cols - c0;
     const Columns mine(left < a.width ? int(left) : a.width, w.group, 64);
     const int cols = mine.to - mine.from;
     if (w.row0 >= a.rows || cols <= 0) return;
     const int64_t first = c0 + mine.from;
     const bool adds = a.bias != nullptr;
-    if (adds) {
-        fetch_biases<T>(a.bias, a.col0 + first, a.col0 + a.cols, LN_HALF, -CUDART_INF_F, w.add, w.lane);
-        __syncwarp();
-    }
-    float coef = 0.f, lse = 0.f, lo = 0.f;
-    int target = -1;
-    if (row < a.rows) {
-        coef = a.coef[row];
-        lse = a.lse[row];
-        if (a.lse_lo) lo = a.lse_lo[row];
-        const int64_t t64 = a.targets[row] - a.col0 - first;
-        target = t64 >= 0 && t64 < cols ? int(t64) : -1;
-        if (a.top) coef *= power_for(*a.top, false);
-    }
+    float coef = in.coef;
+    const float lse = in.lse, lo = in.lo;
+    const int64_t t64 = in.target - first;
+    const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
     // a masked row: gradient 0 whatever comes in
     if (lse == -CUDART_INF_F) coef = 0.f;
     const bool nothing = coef == 0.f;
@@ -471,11 +510,6 @@ __device__ __forceinline__ void gated_tile(const LNArgs& a, const Place& t, cons
     if (w.row0 >= a.rows || cols <= 0) return;
     const int64_t first = c0 + mine.from;
     const bool adds = a.bias || a.bias2, saves = a.s0.q || a.s1.q, live = row < a.rows;
-    if (adds) {
-        fetch_biases<T>(a.bias, c0, a.cols, LN_HALF, 0.f, w.add, w.lane);
-        fetch_biases<T>(a.bias2, c0, a.cols, LN_HALF, 0.f, w.add + LN_HALF, w.lane);
-        __syncwarp();
-    }
     const unsigned src_g = w.src, src_u = w.src + unsigned(half_width);
     unsigned top_g[2] = {0, 0}, top_u[2] = {0, 0};
     float g[32], u[32];
@@ -541,7 +575,7 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
     const unsigned pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     if (tid == 0) {
         sm.error = sm.other_error = 0;
-        for (int k = 0; k < LN_RING; ++k) {
+        for (int k = 0; k < LN_RING_MOST; ++k) {
             kb_init(&sm.empty[k], 1);
             kb_init(&sm.full[k], 1);
         }
@@ -574,14 +608,14 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
         if (lane == 0) {
             const unsigned leader_full = pair_address(kb_smem_u32(sm.full), 0);
             unsigned g = 0;                                  // steps of all tiles so far
+            Slot r;
             for (unsigned i = pair; ok && i < tiles; i += pairs) {
                 const Place t = place_at<EPI>(a, i);
                 const int y = (2 * t.m + int(rank)) * LN_M;
-                for (int s = 0; s < t.steps; ++s, ++g) {
-                    const Ring<LN_RING> r(g);
+                for (int s = 0; s < t.steps; ++s, ++g, r.next(a)) {
                     if (!kb_wait(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
                     if (rank == 0) kb_expect_tx(kb_smem_u32(&sm.full[r.slot]), 2 * LN_TILE + unsigned(a.width) * (LN_K * 2));
-                    const unsigned bar = leader_full + r.slot * 8, da = kb_smem_u32(sm.a[r.slot]), db = kb_smem_u32(sm.b[r.slot]);
+                    const unsigned bar = leader_full + r.slot * 8, da = kb_smem_u32(sm.ring) + r.slot * unsigned(a.slot_bytes), db = da + LN_TILE;
                     const int step = t.first + s;
                     const bool second = step >= a.steps0;
                     const int k = (second ? step - a.steps0 : step) * LN_K;
@@ -606,31 +640,32 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
             }
             // after a wait that gave up: the copies in flight land (the leading CTA counts them in) before
             // either CTA's shared memory is given back
-            for (unsigned k = 0; !ok && rank == 0 && k < LN_RING && k < g; ++k) {
-                const Ring<LN_RING> r(g - 1 - k);
-                kb_wait(kb_smem_u32(&sm.full[r.slot]), r.parity, error, true, 1u << 10);
+            for (unsigned k = 0; !ok && rank == 0 && k < unsigned(a.ring) && k < g; ++k) {
+                const unsigned step = g - 1 - k;
+                kb_wait(kb_smem_u32(&sm.full[step % unsigned(a.ring)]), (step / unsigned(a.ring)) & 1u, error, true, 1u << 10);
             }
         }
     } else if (warp == LN_MMA_WARP) {
         // The whole warp walks the loop and one elected lane issues.
         if (rank == 0) {
             const unsigned idesc = instruction_desc(std::is_same<T, __half>::value ? 0 : 1, a.width, A_MN, B_MN);
-            const unsigned long long desc_a = operand_desc(kb_smem_u32(sm.a), A_MN ? LN_BLOCK : 16, 1024, 2);
-            const unsigned long long desc_b = operand_desc(kb_smem_u32(sm.b), B_MN ? LN_BLOCK : 16, 1024, 2);
+            const unsigned long long desc_a = operand_desc(kb_smem_u32(sm.ring), A_MN ? LN_BLOCK : 16, 1024, 2);
+            const unsigned long long desc_b = operand_desc(kb_smem_u32(sm.ring) + LN_TILE, B_MN ? LN_BLOCK : 16, 1024, 2);
             // 16 elements of the contraction: 32 bytes along a K-major row, 16 rows of 128 bytes of an MN-major block
             constexpr unsigned STEP_A = A_MN ? 128 : 2, STEP_B = B_MN ? 128 : 2;
-            unsigned g = 0, done = 0;
+            unsigned done = 0;
+            Slot r;
+            const unsigned slot_step = unsigned(a.slot_bytes) / 16;
             for (unsigned i = pair; ok && i < tiles; i += pairs, ++done) {
                 const Place t = place_at<EPI>(a, i);
                 const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
                 const unsigned half = done & 1u, round = (done >> 1) & 1u, d = tmem + half * LN_N;
                 if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[half]), round ^ 1u, error)) { ok = false; break; }
                 tc_fence_after();
-                for (int s = 0; s < steps; ++s, ++g) {
-                    const Ring<LN_RING> r(g);
+                for (int s = 0; s < steps; ++s, r.next(a)) {
                     if (!kb_wait_warp(kb_smem_u32(&sm.full[r.slot]), r.parity, error)) { ok = false; break; }
                     tc_fence_after();
-                    const unsigned long long da = desc_a + r.slot * (LN_TILE / 16), db = desc_b + r.slot * (LN_TILE / 16);
+                    const unsigned long long da = desc_a + r.slot * slot_step, db = desc_b + r.slot * slot_step;
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < LN_K / 16; ++k) mma_f16(d, da + k * STEP_A, db + k * STEP_B, idesc, s > 0 || k > 0);
@@ -662,12 +697,14 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
         for (unsigned i = pair; i < tiles; i += pairs, ++done) {
             const Place t = place_at<EPI>(a, i);
             const unsigned half = done & 1u;
-            if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[half]), (done >> 1) & 1u, error)) break;
-            tc_fence_after();
             w.src = tmem + half * LN_N + (unsigned(w.quarter * 32) << 16);
             w.row0 = int64_t(2 * t.m + int(rank)) * LN_M + w.quarter * 32;
-            if constexpr (EPI == LN_SCORES) scores_tile<T>(a, t, w);
-            if constexpr (EPI == LN_DLOGITS) dlogits_tile<T>(a, t, w, &map_out);
+            const RowInputs in = fetch_inputs<T, EPI>(a, t, w);
+            if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[half]), (done >> 1) & 1u, error)) break;
+            tc_fence_after();
+            __syncwarp();                                    // the warp's biases are there
+            if constexpr (EPI == LN_SCORES) scores_tile(a, t, w, in);
+            if constexpr (EPI == LN_DLOGITS) dlogits_tile<T>(a, t, w, in, &map_out);
             if constexpr (EPI == LN_GATED) gated_tile<T, ACT>(a, t, w, &map_out);
             if constexpr (EPI == LN_SUM || EPI == LN_OUTER) sum_tile<T, EPI>(a, t, w, &map_out);
             tc_fence_before();
@@ -965,7 +1002,11 @@ cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t str
         if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return err;
         if (dev < 64) allowed.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
     }
-    a.group_m = group_rows(a.steps);
+    // (an outer product's tiles go along its rows, which are then written whole: 11 x 128 tokens, 32000 x 1024, fp32 rows, whole backward
+    // pass without dx 370 us, row tiles in groups of 64 396)
+    a.group_m = EPI == LN_OUTER ? 1 : group_rows(a.steps);
+    a.slot_bytes = LN_TILE + a.width * LN_K;
+    a.ring = std::min(LN_RING_MOST, LN_RING_BYTES / a.slot_bytes);
     const int64_t tiles = int64_t(a.mt) * a.nt * a.splits;
     if (tiles >= int64_t(1) << 30) return cudaErrorInvalidConfiguration;
     const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
