@@ -7,7 +7,11 @@ The model is a classifier of tokens with one hidden layer,
 over every worker's own batch.  Between forward and backward pass nothing of the batch is kept but
 8-bit checkpoints of x, h and y (and the logits, which become their own gradient in place).
 
-    python -m paper_1905_04374_b200.worker_step [--rule multi_bulyan] [--steps 60]
+With --model gated the hidden layer is a gated one with dropout,
+    y = dropout(silu(x Wg^T + bg) * (x Wu^T + bu)),   loss as above from y W2^T + b2,
+the logits are never kept, and what is kept of the batch is y and 8-bit checkpoints of x and both projections.
+
+    python -m paper_1905_04374_b200.worker_step [--rule multi_bulyan] [--steps 60] [--model gated --dropout 0.1]
 """
 from __future__ import annotations
 
@@ -15,6 +19,7 @@ import argparse
 
 import torch
 
+from . import linear as L
 from . import worker as W
 from .binding import gar_aggregate_ex, new_selection, read_selection
 
@@ -24,7 +29,7 @@ class WorkerStep:
 
     def __init__(self, n: int, f: int, inputs: int, hidden: int, classes: int, device="cuda", seed: int = 0):
         self.n, self.f = n, f
-        self.shapes = {"w1": (hidden, inputs), "b1": (hidden,), "w2": (classes, hidden), "b2": (classes,)}
+        self.shapes = self.parameters(inputs, hidden, classes)
         self.offsets, d = {}, 0
         for name, shape in self.shapes.items():
             self.offsets[name] = d
@@ -32,11 +37,17 @@ class WorkerStep:
         self.d = d
         gen = torch.Generator(device=device).manual_seed(seed)
         self.params = torch.zeros(d, device=device)
-        for name, fan in (("w1", inputs), ("w2", hidden)):
-            self.view(name).normal_(0.0, fan ** -0.5, generator=gen)
+        for name, shape in self.shapes.items():
+            if len(shape) == 2:
+                self.view(name).normal_(0.0, shape[1] ** -0.5, generator=gen)
         self.momentum = torch.zeros(d, device=device)
         self.grads = torch.empty(n, d, device=device)
         self.selection = new_selection(device)
+
+    @staticmethod
+    def parameters(inputs: int, hidden: int, classes: int) -> dict:
+        """The model's parameters and their shapes, in the order of the vector."""
+        return {"w1": (hidden, inputs), "b1": (hidden,), "w2": (classes, hidden), "b2": (classes,)}
 
     def view(self, name: str) -> torch.Tensor:
         """One parameter as a matrix or vector."""
@@ -77,6 +88,45 @@ class WorkerStep:
                          sgd_momentum_buf=self.momentum, sgd_lr=lr, sgd_momentum=momentum, store_out=False)
 
 
+class GatedStep(WorkerStep):
+    """The same with a gated hidden layer and dropout, by the operators of a worker's layers."""
+
+    def __init__(self, n: int, f: int, inputs: int, hidden: int, classes: int, device="cuda", seed: int = 0, dropout: float = 0.0):
+        super().__init__(n, f, inputs, hidden, classes, device, seed)
+        self.dropout, self.seed = dropout, seed
+        # the number of the step, on the device: a captured step that is replayed takes a new mask each time
+        self.steps = torch.zeros(1, dtype=torch.int64, device=device)
+
+    @staticmethod
+    def parameters(inputs: int, hidden: int, classes: int) -> dict:
+        return {"wg": (hidden, inputs), "bg": (hidden,), "wu": (hidden, inputs), "bu": (hidden,), "w2": (classes, hidden), "b2": (classes,)}
+
+    def gradients(self, x: torch.Tensor, targets: torch.Tensor) -> torch.Tensor:
+        n, tokens, _ = x.shape
+        w = {name: self.view(name).to(x.dtype) for name in self.shapes}
+        x = x.flatten(0, 1)
+        targets = targets.reshape(-1)
+        # forward: the inputs and both projections are kept in 8 bits, of the logits one number per token
+        x_saved = W.gar_checkpoint_pack(x)
+        hidden = L.gar_gated_linear_forward("silu", x, w["wg"], w["wu"], w["bg"], w["bu"])
+        y = self.drop(hidden.y)
+        scores = L.gar_linear_logprobs(y, w["w2"], targets, bias=w["b2"])
+        losses = -scores.logprobs.view(n, tokens).mean(1)
+        # backward: the head's gradients go into the block's rows, then the hidden layer's
+        up = torch.full((n * tokens,), -1.0 / tokens, device=x.device)
+        dy = self.drop(L.gar_linear_logprobs_backward(y, w["w2"], scores, targets, up, bias=w["b2"], grads=self.grads,
+                                                      weight_offset=self.offsets["w2"], bias_offset=self.offsets["b2"]))
+        back = L.gar_gated_linear_backward("silu", dy, hidden.x, hidden.up, w["wg"], w["wu"], dx=False)
+        W.gar_linear_weight_grad(back.dgate.view(n, tokens, -1), x_saved, self.grads, self.offsets["wg"], self.offsets["bg"])
+        W.gar_linear_weight_grad(back.dup.view(n, tokens, -1), x_saved, self.grads, self.offsets["wu"], self.offsets["bu"])
+        self.steps += 1
+        return losses
+
+    def drop(self, y: torch.Tensor) -> torch.Tensor:
+        """Dropout in place, the same mask for a step's activation and its gradient."""
+        return L.gar_dropout(y, self.dropout, self.seed, y=y, counter=self.steps) if self.dropout else y
+
+
 def batch(n: int, tokens: int, inputs: int, classes: int, step: int, device="cuda"):
     """A seeded synthetic task: every class is a direction, a token is its class's direction plus noise."""
     centres = torch.randn(classes, inputs, generator=torch.Generator(device=device).manual_seed(7), device=device)
@@ -87,9 +137,14 @@ def batch(n: int, tokens: int, inputs: int, classes: int, step: int, device="cud
 
 
 def train(rule="multi_bulyan", n: int = 11, f: int = 2, steps: int = 60, tokens: int = 128, inputs: int = 256, hidden: int = 512,
-          classes: int = 100, attacked: bool = True, device="cuda"):
+          classes: int = 100, attacked: bool = True, device="cuda", model: str = "plain", dropout: float = 0.0):
     """The honest workers' mean loss before every step."""
-    model = WorkerStep(n, f, inputs, hidden, classes, device)
+    if model == "gated":
+        model = GatedStep(n, f, inputs, hidden, classes, device, dropout=dropout)
+    elif model == "plain" and not dropout:
+        model = WorkerStep(n, f, inputs, hidden, classes, device)
+    else:
+        raise ValueError("model must be plain (without dropout) or gated")
     history = []
     for step in range(steps):
         losses = model.gradients(*batch(n, tokens, inputs, classes, step, device))
@@ -110,8 +165,11 @@ def main() -> None:
     ap.add_argument("--workers", type=int, default=11)
     ap.add_argument("--byzantine", type=int, default=2)
     ap.add_argument("--no-attack", action="store_true")
+    ap.add_argument("--model", default="plain", choices=["plain", "gated"])
+    ap.add_argument("--dropout", type=float, default=0.0, help="of the gated model's hidden layer")
     args = ap.parse_args()
-    history = train(args.rule, args.workers, args.byzantine, args.steps, attacked=not args.no_attack)
+    history = train(args.rule, args.workers, args.byzantine, args.steps, attacked=not args.no_attack,
+                    model=args.model, dropout=args.dropout)
     for step in sorted({0, len(history) // 4, len(history) // 2, 3 * len(history) // 4, len(history) - 1}):
         print(f"step {step:4d}  loss of the honest workers {history[step]:.4f}")
 
