@@ -280,7 +280,7 @@ bool few_rows_applies(int64_t rows, int64_t hidden, const void* w0, int64_t ld0,
 }
 int64_t few_scores_parts(int sm_count) { return most_blocks(sm_count); }
 
-cudaError_t launch_few_scores(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw, float whole, float2* parts, float* target_z, int* count,
+cudaError_t launch_few_scores(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw, float lost, float2* parts, float* target_z, int* count,
                               int sm_count) {
     FewArgs a{};
     const unsigned blocks = plan(a, int(p.rows), p.hidden, p.vocab, (p.vocab + 15) / 16, sm_count);
@@ -289,7 +289,7 @@ cudaError_t launch_few_scores(const gar_linear_logprobs_params_t& p, int64_t ldx
     a.w0 = p.weight;
     a.ld0 = ldw;
     a.b0 = p.bias;
-    a.whole = whole;
+    a.whole = 1.f + lost * float(p.hidden) / float(a.split);        // of each warp's part of the contraction
     a.targets = p.logprobs ? p.targets : nullptr;
     a.parts = parts;
     a.target_z = target_z;

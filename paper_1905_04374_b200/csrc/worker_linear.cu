@@ -52,7 +52,7 @@ constexpr float LN_SHORT = 1.0e-9f;                   // of a sum, lost per term
 //   LN_SUM      stored in 16 bits, or in fp32, or added to fp32 (parts of a longer contraction)
 //   LN_OUTER    the same, of every worker's own contraction over its tokens
 enum Epilogue { LN_SCORES = 0, LN_DLOGITS = 1, LN_GATED = 2, LN_SUM = 3, LN_OUTER = 4 };
-enum Out { OUT_WIDE = 0, OUT_PLAIN = 1, OUT_PART = 2, OUT_ADD = 3 };    // 16 bits by TMA or plainly; fp32, added
+enum Out { OUT_WIDE = 0, OUT_PLAIN = 1, OUT_PART = 2, OUT_ADD = 3, OUT_PLAIN32 = 4 };   // 16 bits by TMA or plainly; fp32 by TMA, added, plainly
 
 struct LNArgs {
     int64_t        rows, cols;            // of the result (LN_SCORES, LN_DLOGITS: columns from col0 on)
@@ -225,6 +225,23 @@ __device__ __forceinline__ void store_plain(unsigned stage, int lane, unsigned s
     }
 }
 
+// The same of a piece of 32 rows of 32 fp32 elements, one per lane.
+__device__ __forceinline__ void store_plain32(unsigned stage, int lane, float* dst, int64_t ld, int rows, int cols) {
+    dst += lane;
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[k]) : "r"(stage + (r0 + k) * 128 + (((lane / 4) ^ k) << 4) + (lane & 3) * 4));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (r0 + k < rows && lane < cols) *dst = v[k];
+            dst += ld;
+        }
+    }
+}
+
 // 128 columns' biases from column c0 on, `fill` where there is no column
 template <typename T>
 __device__ __forceinline__ void fetch_biases(const void* bias, int64_t c0, int64_t cols, float fill, float* add, int lane) {
@@ -351,7 +368,7 @@ __device__ __forceinline__ void put_piece(const LNArgs& a, const Warp& w, const 
     } else {
         const int64_t left = a.rows - w.row0;
         __syncwarp();
-        store_plain(w.stage, w.lane, static_cast<unsigned short*>(a.y) + w.row0 * a.ldy + col, a.ldy, left < 32 ? int(left) : 32, cols);
+        store_plain(w.stage, w.lane, static_cast<unsigned short*>(a.y) + z * a.plane + w.row0 * a.ldy + col, a.ldy, left < 32 ? int(left) : 32, cols);
         __syncwarp();
     }
 }
@@ -420,6 +437,14 @@ __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const 
             for (int j = 0; j < 8; ++j)
                 put_shared(w.stage + w.lane * 128 + ((j ^ (w.lane & 7)) << 4),
                            make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])));
+            if (EPI == LN_OUTER && a.out == OUT_PLAIN32) {
+                const int64_t below = a.rows - w.row0;
+                __syncwarp();
+                store_plain32(w.stage, w.lane, static_cast<float*>(a.y) + t.split * a.plane + w.row0 * a.ldy + first + at, a.ldy, below < 32 ? int(below) : 32,
+                              cols - at);
+                __syncwarp();
+                return;
+            }
             fence_async_smem();
             __syncwarp();
             if (w.lane == 0) {
@@ -439,12 +464,12 @@ __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const 
         if (half == 0) stage_free(w);
         stage32<T>(w.stage, w.lane, half, v);
         if (half == 1 || at + 32 >= cols) {
-            if (EPI == LN_OUTER) {
+            if (EPI == LN_OUTER && a.out == OUT_WIDE) {
                 fence_async_smem();
                 __syncwarp();
                 if (w.lane == 0) tma_store(map, w.stage, int(first) + (at & ~63), int(w.row0), t.split, policy);
             } else {
-                put_piece(a, w, map, first + (at & ~63), cols - (at & ~63), 0);
+                put_piece(a, w, map, first + (at & ~63), cols - (at & ~63), EPI == LN_OUTER ? t.split : 0);
             }
         }
         half ^= 1;
@@ -588,7 +613,7 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
     if (tid == 32) {
         prefetch_map(&map_a0);
         prefetch_map(&map_b0);
-        if (EPI != LN_SCORES && a.out != OUT_PLAIN) prefetch_map(&map_out);
+        if (EPI != LN_SCORES && a.out != OUT_PLAIN && a.out != OUT_PLAIN32) prefetch_map(&map_out);
     }
     if (warp == LN_ALLOC_WARP) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kb_smem_u32(&sm.tmem_base)), "r"(512u) : "memory");
@@ -912,7 +937,8 @@ struct Operand {
     int64_t     rows, cols, ld;
 };
 cudaError_t operand_map(CUtensorMap* map, int dtype, const Operand& m, int box_cols, int box_rows) {
-    return make_map(map, map_type(dtype), m.p, m.cols, m.rows, 1, m.ld * 2, m.ld * 2 * m.rows, box_cols, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+    const int64_t pitch = 2 * (m.rows > 1 ? m.ld : up_to(m.cols, 8));         // (a single row's stride may be anything)
+    return make_map(map, map_type(dtype), m.p, m.cols, m.rows, 1, pitch, pitch * m.rows, box_cols, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // A workspace handed out piece by piece; without memory it only counts.
@@ -1132,16 +1158,23 @@ cudaError_t join_sum(const SumTarget& d, int sm_count, cudaStream_t stream) {
 }
 
 // ---- weight gradients -------------------------------------------------------------------------------
-// Where this kernel makes them: sums short enough for one accumulator (see gar_linear_weight_grad's chunks) and rows of the
-// block that TMA stores.  Two store groups, and a pair's next tile in the other half of tensor memory, keep up with the block's rows
-// where there are few tokens to a tile: 11 workers x 128 tokens, 16128 x 1024, bf16 rows: 98 us by weight_grad_kernel's four
-// store warps.  Elsewhere weight_grad_kernel makes them.
+// the block's rows as TMA stores them
+bool block_on_16(const DenseWeightGrad& g) {
+    const int64_t gs = g.grads_dtype == GAR_F32 ? 4 : 2;
+    return reinterpret_cast<uintptr_t>(g.dw) % 16 == 0 && (g.workers == 1 || g.ld_grads * gs % 16 == 0) && g.in * gs % 16 == 0;
+}
 }  // namespace
+// Where this kernel makes them: sums short enough for one accumulator (see gar_linear_weight_grad's chunks).  Two store groups, and a
+// pair's next tile in the other half of tensor memory, keep up with the block's rows where there are few tokens to a tile:
+// 11 workers x 128 tokens, 16128 x 1024, bf16 rows: 70 us, 98 by weight_grad_kernel's four store warps.  Rows that start anywhere are
+// stored in words of 4 bytes (whole backward pass without dx, weight_grad_kernel in brackets): 11 x 128, 100 x 512 15.4 us (22.5); 7 x 100,
+// 2000 x 501, fp32 25.2 (30.8); 2 x 2000, 16000 x 2047, bf16 483 (525); 4 x 700, 8000 x 2050, fp32 260 (269); but 11 x 128, 32000 x 1024, fp32,
+// 1.4 GB of rows with little to compute, 668 (536): those are left to the latter, which shifts rows to 16-byte chunks.
 bool outer_applies(const DenseWeightGrad& g) {
     const int64_t gs = g.grads_dtype == GAR_F32 ? 4 : 2;
     if (g.tokens < 1 || g.tokens > (gs == 4 ? 768 : 2048)) return false;
-    return reinterpret_cast<uintptr_t>(g.dw) % 16 == 0 && (g.workers == 1 || g.ld_grads * gs % 16 == 0) && g.in * gs % 16 == 0 &&
-           (gs == 4 || g.grads_dtype == g.dtype) && parts_of(g.out, 2 * LN_M) * parts_of(g.in, LN_N) < (int64_t(1) << 30) / g.workers / 2;
+    if (gs == 4 && g.tokens < 512 && !block_on_16(g) && g.out * g.in * g.workers > (int64_t(16) << 20)) return false;
+    return (gs == 4 || g.grads_dtype == g.dtype) && parts_of(g.out, 2 * LN_M) * parts_of(g.in, LN_N) < (int64_t(1) << 30) / g.workers / 2;
 }
 namespace {
 cudaError_t token_map(CUtensorMap* map, int dtype, const void* p, int64_t cols, int64_t ld, const DenseWeightGrad& g) {
@@ -1160,7 +1193,8 @@ cudaError_t launch_outer(const DenseWeightGrad& g, int sm_count, cudaStream_t st
     a.steps0 = a.steps = int(parts_of(g.tokens, LN_K));
     a.width = width_for(int64_t(a.mt) * g.workers, g.in, a.steps, 128);
     a.nt = int(parts_of(g.in, a.width));
-    a.out = wide ? OUT_PART : OUT_WIDE;
+    const bool by_tma = block_on_16(g);
+    a.out = wide ? (by_tma ? OUT_PART : OUT_PLAIN32) : by_tma ? OUT_WIDE : OUT_PLAIN;
     a.top = g.top;
     a.y = g.dw;
     a.ldy = g.in;
@@ -1168,7 +1202,9 @@ cudaError_t launch_outer(const DenseWeightGrad& g, int sm_count, cudaStream_t st
     if (cudaError_t err = token_map(&maps.a0, g.dtype, g.dy, g.out, g.ld_dy, g)) return err;
     if (cudaError_t err = token_map(&maps.b0, g.dtype, g.x, g.in, g.ldx, g)) return err;
     maps.a1 = maps.b1 = maps.a0;                       // not used
+    maps.out = maps.a0;
     const int64_t plane = g.workers > 1 ? g.ld_grads * gs : g.in * g.out * gs;
+    if (!by_tma) return launch<LN_OUTER>(g.dtype, a, maps, sm_count, stream);
     if (cudaError_t err = make_map(&maps.out, wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : map_type(g.dtype), g.dw, g.in, g.out, g.workers, g.in * gs, plane,
                                    int(128 / gs), 32, CU_TENSOR_MAP_SWIZZLE_128B)) return err;
     return launch<LN_OUTER>(g.dtype, a, maps, sm_count, stream);
@@ -1271,7 +1307,7 @@ cudaError_t launch_linear_logprobs(const gar_linear_logprobs_params_t& p, int64_
     ScoresPlan plan(p, ldx, ldw);
     if (few_rows_applies(p.rows, p.hidden, p.weight, ldw, nullptr, 0) && few_scores_parts(sm_count) <= LN_FEW_PARTS) {
         int count = 0;
-        if (cudaError_t err = launch_few_scores(p, ldx, ldw, 1.f + LN_SHORT * float(p.hidden), plan.parts, plan.target_z, &count, sm_count)) return err;
+        if (cudaError_t err = launch_few_scores(p, ldx, ldw, LN_SHORT, plan.parts, plan.target_z, &count, sm_count)) return err;
         return launch_small(join_scores_kernel, dim3(unsigned(parts_of(p.rows, 8))), stream, plan.parts, plan.target_z, p.logprobs ? p.targets : nullptr, p.rows,
                             count, p.vocab, p.logprobs, p.lse, p.lse_lo);
     }

@@ -130,10 +130,10 @@ __device__ __forceinline__ void grid_dependency() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// The power of two that the largest coefficient is brought to 2^14 .. 2^15 with, and its inverse: |k| <= 100.
+// The power of two that the largest coefficient is brought to 2^14 .. 2^15 with, and its inverse: |k| <= 120.
 __device__ __forceinline__ float power_for(unsigned top, bool inverse) {
     if (top == 0u || top >= 0x7f800000u) return 1.f;
-    const int k = max(-100, min(100, 14 - (int(top >> 23) - 127)));
+    const int k = max(-120, min(120, 14 - (int(top >> 23) - 127)));
     return __uint_as_float(unsigned(127 + (inverse ? -k : k)) << 23);
 }
 

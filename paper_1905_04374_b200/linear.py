@@ -14,7 +14,7 @@ from typing import NamedTuple, Optional, Union
 import torch
 
 from . import worker
-from .binding import _check
+from .binding import GRAD_DTYPES, _check
 from .worker import ACTIVATIONS, Activation, Checkpoint, GarCheckpoint, TokenLogprobs, _handle
 
 
@@ -100,24 +100,48 @@ class GatedLinearGrad(NamedTuple):
     dup: torch.Tensor
 
 
-def gar_linear_logprobs_workspace_bytes(params: GarLinearLogprobsParams) -> int:
-    """gar_linear_logprobs_workspace_bytes of a parameter block."""
-    return int(lib().gar_linear_logprobs_workspace_bytes(C.byref(params)))
+def _place(t: torch.Tensor):
+    """Address, rows, columns and row stride of a matrix, as the sizes calls look at them."""
+    return t.data_ptr() or 16, t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def gar_linear_logprobs_backward_workspace_bytes(params: GarLinearLogprobsGradParams) -> int:
-    """gar_linear_logprobs_backward_workspace_bytes of a parameter block."""
-    return int(lib().gar_linear_logprobs_backward_workspace_bytes(C.byref(params)))
+def gar_linear_logprobs_workspace_bytes(x: torch.Tensor, weight: torch.Tensor) -> int:
+    """Bytes of the workspace gar_linear_logprobs takes for these operands."""
+    p = GarLinearLogprobsParams(dtype=GRAD_DTYPES[x.dtype])
+    p.x, p.rows, p.hidden, p.ldx = _place(x)
+    p.weight, p.vocab, _, p.ldw = _place(weight)
+    return int(lib().gar_linear_logprobs_workspace_bytes(C.byref(p)))
 
 
-def gar_gated_linear_workspace_bytes(params: GarGatedLinearParams) -> int:
-    """gar_gated_linear_workspace_bytes of a parameter block."""
-    return int(lib().gar_gated_linear_workspace_bytes(C.byref(params)))
+def gar_linear_logprobs_backward_workspace_bytes(x: torch.Tensor, weight: torch.Tensor, grads: Optional[torch.Tensor] = None, bias: bool = False,
+                                                 dx: bool = True) -> int:
+    """Bytes of the workspace gar_linear_logprobs_backward takes for these operands; bias: whether bias gradients are asked for."""
+    p = GarLinearLogprobsGradParams(dtype=GRAD_DTYPES[x.dtype], workers=1, dx=16 if dx else None)
+    p.x, p.tokens, p.hidden, p.ldx = _place(x)
+    p.weight, p.vocab, _, p.ldw = _place(weight)
+    if grads is not None:
+        p.workers, p.tokens, p.grads_dtype, p.weight_grads = grads.shape[0], x.shape[0] // grads.shape[0], GRAD_DTYPES[grads.dtype], 16
+        p.bias_grads = 16 if bias else None
+    return int(lib().gar_linear_logprobs_backward_workspace_bytes(C.byref(p)))
 
 
-def gar_gated_linear_backward_workspace_bytes(params: GarGatedLinearGradParams) -> int:
-    """gar_gated_linear_backward_workspace_bytes of a parameter block."""
-    return int(lib().gar_gated_linear_backward_workspace_bytes(C.byref(params)))
+def gar_gated_linear_workspace_bytes(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor) -> int:
+    """Bytes of the workspace gar_gated_linear_forward takes for these operands (0: none)."""
+    p = GarGatedLinearParams(dtype=GRAD_DTYPES[x.dtype], group=128, y=16)
+    p.x, p.rows, p.hidden, p.ldx = _place(x)
+    p.w_gate, p.inner, _, p.ld_gate = _place(w_gate)
+    p.w_up, _, _, p.ld_up = _place(w_up)
+    return int(lib().gar_gated_linear_workspace_bytes(C.byref(p)))
+
+
+def gar_gated_linear_backward_workspace_bytes(w_gate: torch.Tensor, w_up: torch.Tensor, dgate: torch.Tensor, dup: torch.Tensor) -> int:
+    """Bytes of the workspace gar_gated_linear_backward takes for these operands (0: none)."""
+    p = GarGatedLinearGradParams(dtype=GRAD_DTYPES[dgate.dtype], group=128, dy=16, dx=16)
+    p.w_gate, p.inner, p.hidden, p.ld_gate = _place(w_gate)
+    p.w_up, _, _, p.ld_up = _place(w_up)
+    p.dgate, p.rows, _, p.ld_dgate = _place(dgate)
+    p.dup, _, _, p.ld_dup = _place(dup)
+    return int(lib().gar_gated_linear_backward_workspace_bytes(C.byref(p)))
 
 
 def gar_linear_logprobs(x: torch.Tensor, weight: torch.Tensor, targets: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,

@@ -107,6 +107,42 @@ def test_scores(pkg, dtype, rows, hidden, vocab, bias):
     check_scores(pkg, *head(rows, hidden, vocab, dtype, bias))
 
 
+@pytest.mark.parametrize("rows,vocab", [(40, 31 + 74 * k) for k in (31, 63, 95, 127, 159, 191, 223, 255)] + [(300, 37 * k + 1) for k in (63, 127, 191, 255)])
+def test_scores_of_every_tile_width(pkg, rows, vocab):
+    """Vocabularies that one round of tiles of 32, 64, .. 256 columns covers, forward and backward."""
+    x, w, b, t = head(rows, 128, vocab, "bf16", True, 9)
+    check_scores(pkg, x, w, b, t)
+    a = -torch.rand(rows, generator=gen(1), device=DEV)
+    check_head_gradient(pkg, x, w, b, t, a, 2, "f32")
+
+
+def test_scores_without_targets(pkg):
+    """lse alone; and the gradient from what gar_token_logprobs saved of the same logits, or without the lower part of lse."""
+    for rows in (3, 300):
+        x, w, b, t = head(rows, 64, 500, "bf16", True, 8)
+        t = t.clamp_min(0)
+        r = pkg.gar_linear_logprobs(x, w, bias=b)
+        full = pkg.gar_linear_logprobs(x, w, t, bias=b)
+        assert r.logprobs is None and torch.equal(r.lse, full.lse) and torch.equal(r.lse_lo, full.lse_lo)
+        a = torch.ones(rows, device=DEV)
+        check_head_gradient(pkg, x, w, b, t, a, 1, "f32", saved=r)
+        check_head_gradient(pkg, x, w, b, t, a, 1, "f32", saved=r._replace(lse_lo=None))
+        logits = (x.float() @ w.float().t() + b.float())
+        check_head_gradient(pkg, x, w, b, t, a, 1, "f32", saved=pkg.gar_token_logprobs(logits, t))
+
+
+def test_scores_in_runs_of_rows(pkg):
+    """So many rows and columns that the rows are gone through in runs."""
+    rows, hidden, vocab = 8400, 16, 131000
+    x, w, b, t = head(rows, hidden, vocab, "bf16", True, 2)
+    r = pkg.gar_linear_logprobs(x, w, t, bias=b)
+    for r0 in range(0, rows, 1200):
+        at = slice(r0, r0 + 1200)
+        logprobs, lse, _, d = scores_64(x[at], w, b, t[at])
+        close(r.lse[at], lse, 2 * d + 2e-5, "lse")
+        close(r.logprobs[at], logprobs, 2 * d + 2e-5, "logprobs")
+
+
 @pytest.mark.parametrize("pad,shift", [(0, 1), (8, 0), (3, 5), (8, 8)])
 def test_scores_strides(pkg, pad, shift):
     x, w, b, t = head(70, 136, 300, "bf16", True)
@@ -183,7 +219,7 @@ def check_head_gradient(pkg, x, w, b, t, a, workers, grads_dtype, weight_at=0, b
     return got, grads
 
 
-@pytest.mark.parametrize("dtype,grads", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("f16", "f32")])
+@pytest.mark.parametrize("dtype,grads", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("f16", "f32"), ("bf16", "f16")])
 @pytest.mark.parametrize("workers,tokens,hidden,vocab,bias", [(1, 1, 1, 1, True), (1, 3, 8, 10, False), (2, 64, 64, 256, True), (3, 100, 65, 257, True),
                                                               (5, 33, 500, 100, False), (1, 700, 130, 999, True), (2, 300, 64, 20000, False),
                                                               (16, 5, 96, 600, True), (1, 2048, 256, 512, False)])
@@ -192,6 +228,25 @@ def test_head_gradient(pkg, dtype, grads, workers, tokens, hidden, vocab, bias):
     a = -torch.rand(workers * tokens, generator=gen(1), device=DEV) / tokens
     a[tokens // 2] = 0.0
     check_head_gradient(pkg, x, w, b, t, a, workers, grads, weight_at=2, bias=bias)
+
+
+@pytest.mark.parametrize("grads,tokens,hidden,shift", [("f32", 600, 65, 1), ("f32", 800, 64, 0), ("f32", 300, 64, 3), ("bf16", 2049, 64, 0),
+                                                       ("bf16", 700, 66, 1), ("bf16", 64, 1030, 0)])
+def test_head_gradient_results_that_start_anywhere(pkg, grads, tokens, hidden, shift):
+    """Blocks whose rows lie on 16 bytes and anywhere, sums of one accumulator and of more."""
+    x, w, b, t = head(2 * tokens, hidden, 400, "bf16", True, 6)
+    a = -torch.rand(2 * tokens, generator=gen(7), device=DEV) / tokens
+    check_head_gradient(pkg, x, w, b, t, a, 2, grads, weight_at=shift, bias=True)
+
+
+def test_small_gradients_in_binary16(pkg):
+    """Coefficients of 2^-20 and rows that differ by 2^12 among them: dz would underflow without its power of two."""
+    x, w, b, t = head(200, 64, 3000, "f16", False, 5)
+    a = torch.full((200,), 2.0 ** -20, device=DEV)
+    a[::2] *= 2.0 ** -12
+    # the results themselves are far below binary16's subnormals but for fp32 blocks
+    check_head_gradient(pkg, x, w, b, t, a, 1, "f32", dx=False)
+    check_head_gradient(pkg, x, w, b, t, a * 2.0 ** 60, 1, "f32", dx=False)
 
 
 def test_head_gradient_in_pieces(pkg):

@@ -198,6 +198,18 @@ def test_one_workspace_for_call_after_call(pkg):
     a = torch.rand(x.shape[0], generator=gen(1), device=DEV)
     g0, g1 = (torch.empty(2, w.numel(), device=DEV) for _ in range(2))
     dx = pkg.gar_linear_logprobs_backward(x, w, r, t, a, grads=g0)
+    assert 0 < pkg.gar_linear_logprobs_workspace_bytes(x, w) <= space.numel()
+    assert 0 < pkg.gar_linear_logprobs_backward_workspace_bytes(x, w, g0) <= space.numel()
+    exact = torch.empty(pkg.gar_linear_logprobs_backward_workspace_bytes(x, w, g0), dtype=torch.uint8, device=DEV)
+    assert torch.equal(pkg.gar_linear_logprobs_backward(x, w, r, t, a, grads=g1, workspace=exact), dx) and torch.equal(g0, g1)
+    wide = wg[:, 1:]                                         # rows that do not start on 16 bytes are copied
+    assert pkg.gar_gated_linear_workspace_bytes(x, wg, wu) == 0 and pkg.gar_gated_linear_workspace_bytes(x[:, 1:], wide, wu[:, 1:]) > 0
+    f = pkg.gar_gated_linear_forward("silu", x, wg, wu)
+    need = pkg.gar_gated_linear_backward_workspace_bytes(wg, wu, torch.empty_like(f.y), torch.empty_like(f.y))
+    own = torch.empty(need, dtype=torch.uint8, device=DEV)
+    b0 = pkg.gar_gated_linear_backward("silu", f.y, f.x, f.up, wg, wu)
+    b1 = pkg.gar_gated_linear_backward("silu", f.y, f.x, f.up, wg, wu, dgate=torch.empty_like(f.y), dup=torch.empty_like(f.y), workspace=own)
+    assert need > 0 and same(b0, b1)
     for _ in range(2):
         assert same(pkg.gar_linear_logprobs(x, w, t, workspace=space), r)
         assert torch.equal(pkg.gar_linear_logprobs_backward(x, w, r, t, a, grads=g1, workspace=space), dx) and torch.equal(g0, g1)

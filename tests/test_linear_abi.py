@@ -64,6 +64,10 @@ def refuses(pkg, call, params, cases, status=INVALID):
     assert fn(None) == INVALID
 
 
+def sizes(pkg, call, params):
+    return getattr(pkg.linear.lib(), call)(C.byref(params))
+
+
 def saved(pkg, q, scales, ldq):
     s = pkg.GarCheckpoint()
     s.q, s.scales, s.ldq = q, scales, ldq
@@ -83,12 +87,12 @@ def test_scores_refusals(pkg):
         dict(x=(1 << 20) + 1), dict(weight=(1 << 21) + 1), dict(bias=(1 << 22) + 1), dict(targets=None), dict(logprobs=None, lse=None, lse_lo=None),
         dict(lse=(1 << 20) + 64), dict(logprobs=1 << 21), dict(lse=(1 << 24) + 8), dict(lse_lo=1 << 22), dict(workspace=1 << 20), dict(rows=1 << 60)])
     refuses(pkg, call, params, [dict(dtype=0), dict(vocab=1 << 31), dict(hidden=1 << 31, ldx=0), dict(rows=1 << 30)], UNSUPPORTED)
-    need = pkg.gar_linear_logprobs_workspace_bytes(params())
+    need = sizes(pkg, 'gar_linear_logprobs_workspace_bytes', params())
     assert need == 4 * 512 * 8 + 256                         # the parts of few rows, the targets' logits; x and W lie on 16 bytes
     refuses(pkg, call, params, [dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=BIG + 128)], WORKSPACE)
     p = params()
     p.ldx = 65
-    assert pkg.gar_linear_logprobs_workspace_bytes(p) == need + 4 * 64 * 2
+    assert sizes(pkg, 'gar_linear_logprobs_workspace_bytes', p) == need + 4 * 64 * 2
     p = params()
     p.rows = 0                                               # nothing to do: accepted without a GPU
     assert pkg.linear.lib().gar_linear_logprobs(C.byref(p)) == 0
@@ -111,7 +115,7 @@ def test_scores_backward_refusals(pkg):
         dict(bias_grads=(1 << 28) + 4 * 6399), dict(dx=1 << 20), dict(dx=(1 << 20) + 64), dict(dx=1 << 21), dict(weight_grads=1 << 26, bias_grads=None),
         dict(x=(1 << 20) + 1), dict(dx=(1 << 27) + 1), dict(bias=(1 << 22) + 1), dict(workspace=1 << 27)])
     refuses(pkg, call, params, [dict(dtype=0), dict(workers=65, ld_grads=0), dict(tokens=1 << 30), dict(vocab=1 << 31), dict(hidden=1 << 31)], UNSUPPORTED)
-    need = pkg.gar_linear_logprobs_backward_workspace_bytes(params())
+    need = sizes(pkg, 'gar_linear_logprobs_backward_workspace_bytes', params())
     assert need > 0
     refuses(pkg, call, params, [dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=BIG + 16)], WORKSPACE)
     p = params()
@@ -126,7 +130,7 @@ def test_gradient_is_kept_in_pieces(pkg, tokens, vocab):
     p.dtype, p.grads_dtype, p.workers, p.tokens, p.hidden, p.vocab = 1, 1, 1, tokens, 64, vocab
     p.x, p.weight, p.targets, p.lse, p.grad_logprobs, p.weight_grads = 1 << 40, 1 << 41, 1 << 42, 1 << 43, 1 << 44, 1 << 45
     rest = tokens * (64 * 2 + 4) + (1 << 22)
-    assert 0 < pkg.gar_linear_logprobs_backward_workspace_bytes(p) <= max(96 << 20, tokens * 512) + rest
+    assert 0 < sizes(pkg, 'gar_linear_logprobs_backward_workspace_bytes', p) <= max(96 << 20, tokens * 512) + rest
 
 
 def test_gated_refusals(pkg):
@@ -143,7 +147,7 @@ def test_gated_refusals(pkg):
         {"gate_saved.ldq": 96}, {"up_saved.ldq": 120}, {"y_saved.q": (1 << 31) + 8}, {"gate_saved.scales": None}, dict(y=1 << 20), dict(y=1 << 21),
         dict(y=(1 << 23) - 2), {"up_saved.q": 1 << 20}, {"y_saved.scales": 1 << 28}])
     refuses(pkg, call, params, [dict(dtype=0), dict(inner=1 << 31, **{"gate_saved.q": None, "up_saved.q": None, "y_saved.q": None})], UNSUPPORTED)
-    assert pkg.gar_gated_linear_workspace_bytes(params()) == 0
+    assert sizes(pkg, 'gar_gated_linear_workspace_bytes', params()) == 0
     refuses(pkg, call, params, [dict(ldx=65), dict(w_up=(1 << 22) + 2), dict(ldx=65, workspace=BIG, workspace_bytes=100)], WORKSPACE)
     p = params()
     p.rows = 0
