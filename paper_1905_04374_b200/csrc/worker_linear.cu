@@ -1090,13 +1090,23 @@ cudaError_t logits_maps(Maps& maps, LNArgs& a, int dtype, const Operand& x, cons
     return cudaSuccess;
 }
 
-// How a sum over a long contraction into few tiles is cut, so that every pair of SMs has a part, of eight steps at least.
-int splits_for(int64_t rows, int64_t cols, int64_t steps) {
+// Parts a sum over a long contraction is cut into, `least` at least, so that the tiles fill the rounds of the pairs: the least of
+// rounds x (steps of a part + 6), a step taking some 0.28 us, and of the parts' way through L2 and back (8 bytes at 4 TB/s).
+// Two workers x 2048 tokens, 131072 x 4096: 256 tiles are 3.5 rounds, in two parts 6.9.
+int splits_for(int64_t rows, int64_t cols, int64_t steps, int64_t least, bool parts_anyway) {
     const int64_t tiles = parts_of(rows, 2 * LN_M) * parts_of(cols, LN_N);
-    int64_t s = std::min<int64_t>(std::min<int64_t>(LN_PAIRS / tiles, steps / 8), 16);
-    if (s < 2) return 1;
-    const int64_t part = parts_of(steps, s);           // no part is empty
-    return int(parts_of(steps, part));
+    int64_t best = least;
+    double cost = 0;
+    for (int64_t s = least; s <= std::max<int64_t>(16, least); ++s) {
+        if (s > least && steps < 8 * s) break;
+        const double through = s > 1 || parts_anyway ? double(s) * double(rows) * double(cols) * 8 / 4e6 : 0;          // us
+        const double t = double(parts_of(tiles * s, LN_PAIRS)) * double(parts_of(steps, s) + 6) * 0.28 + through;
+        if (s == least || t < cost) {
+            cost = t;
+            best = s;
+        }
+    }
+    return int(parts_of(steps, parts_of(steps, best)));        // no part is empty
 }
 
 // dx, or a part of it, in fp32 parts or as it is wanted.
@@ -1228,7 +1238,7 @@ cudaError_t weight_grad(DenseWeightGrad g, int sm_count, cudaStream_t stream) {
 
 // ---- log probabilities ------------------------------------------------------------------------------
 constexpr int64_t LN_PARTS_BYTES = int64_t(64) << 20, LN_PIECE_BYTES = int64_t(96) << 20;
-constexpr int64_t LN_PIECE_MAX = 32768;
+constexpr int64_t LN_TERMS = 32768;                            // of a sum on the tensor cores
 constexpr int64_t LN_FEW_PARTS = 512;                          // CTAs of a few rows' kernel at most: two per SM
 constexpr int LN_SCORES_UNIT = 32, LN_STORE_UNIT = 64;         // columns: of a thread's turn; of a staged piece
 // rows of a launch, so that its parts take 64 MB or so
@@ -1256,10 +1266,24 @@ struct ScoresPlan {
     }
 };
 
-// Columns of a piece of the vocabulary: dz of up to 96 MB (L2 holds it), and sums of no more than 2^15 terms; equal pieces.
-int64_t piece_of(int64_t rows, int64_t vocab) {
-    const int64_t most = std::max<int64_t>(LN_N, std::min<int64_t>(LN_PIECE_MAX, LN_PIECE_BYTES / (2 * rows) / LN_N * LN_N));
-    return up_to(parts_of(vocab, parts_of(vocab, most)), LN_N);
+// Columns of a piece of the vocabulary: dz of up to 96 MB (L2 holds it).  Of the sizes between that and half of it the one with the
+// least of (rounds of the pairs over all pieces) x (steps x 0.28 + 1.5 us) and 8 us a piece, for its launches and their ends.
+// Two workers x 2048 tokens, 131072 x 4096: 46 tiles of columns (10 rounds each) instead of 47 (11).
+int64_t piece_of(int64_t rows, int64_t hidden, int64_t vocab) {
+    const int64_t mt = parts_of(rows, 2 * LN_M), all = parts_of(vocab, LN_N);
+    const int64_t most = std::min(all, std::max<int64_t>(1, LN_PIECE_BYTES / (2 * rows) / LN_N));
+    const double round = double(parts_of(hidden, LN_K)) * 0.28 + 1.5;
+    int64_t best = most;
+    double cost = 0;
+    for (int64_t n = most; n >= std::max<int64_t>(1, most / 2); --n) {
+        const int64_t full = all / n, last = all % n;
+        const double t = double(full * parts_of(mt * n, LN_PAIRS) + parts_of(mt * last, LN_PAIRS)) * round + 8.0 * double(full + (last > 0));
+        if (n == most || t < cost) {
+            cost = t;
+            best = n;
+        }
+    }
+    return best * LN_N;
 }
 struct GradPlan {
     Space     space;
@@ -1275,14 +1299,16 @@ struct GradPlan {
     char*     weight_space = nullptr;
     size_t    weight_bytes = 0;
     GradPlan(const gar_linear_logprobs_grad_params_t& p, int64_t ldw)
-        : space(p.workspace), rows(p.workers * p.tokens), piece(piece_of(std::max<int64_t>(rows, 1), p.vocab)), ld_dz(up_to(piece, 8)), ldx(up_to(p.hidden, 8)),
+        : space(p.workspace), rows(p.workers * p.tokens), piece(piece_of(std::max<int64_t>(rows, 1), p.hidden, p.vocab)), ld_dz(up_to(piece, 8)), ldx(up_to(p.hidden, 8)),
           w(space, p.weight, p.vocab, p.hidden, ldw) {
         x_rows = space.take(size_t(rows) * size_t(ldx) * 2);
         coef = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
         if (p.dtype == GAR_F16) top = reinterpret_cast<unsigned*>(space.take(4));
         dz = space.take(size_t(rows) * size_t(ld_dz) * 2);
         pitch = up_to(p.hidden, 4);
-        splits = splits_for(std::max<int64_t>(rows, 1), p.hidden, parts_of(std::min(piece, p.vocab), LN_K));
+        // (sums of 2^15 terms at most)
+        const int64_t terms = std::min(piece, p.vocab);
+        splits = splits_for(std::max<int64_t>(rows, 1), p.hidden, parts_of(terms, LN_K), parts_of(terms, LN_TERMS), piece < p.vocab);
         if (p.dx && (splits > 1 || piece < p.vocab)) parts = reinterpret_cast<float*>(space.take(size_t(splits) * size_t(rows) * size_t(pitch) * 4));
         if (p.weight_grads) {
             // (the last piece, if it is shorter, may be cut into more parts)
@@ -1425,7 +1451,7 @@ struct GatedGradPlan {
     GatedGradPlan(const gar_gated_linear_grad_params_t& p)
         : space(p.workspace), gate(space, p.w_gate, p.inner, p.hidden, p.ld_gate), up(space, p.w_up, p.inner, p.hidden, p.ld_up),
           dgate(space, p.dgate, p.rows, p.inner, p.ld_dgate), dup(space, p.dup, p.rows, p.inner, p.ld_dup),
-          splits(splits_for(std::max<int64_t>(p.rows, 1), p.hidden, 2 * parts_of(p.inner, LN_K))), pitch(up_to(p.hidden, 4)) {
+          splits(splits_for(std::max<int64_t>(p.rows, 1), p.hidden, 2 * parts_of(p.inner, LN_K), 1, false)), pitch(up_to(p.hidden, 4)) {
         if (splits > 1) parts = reinterpret_cast<float*>(space.take(size_t(splits) * size_t(p.rows) * size_t(pitch) * 4));
     }
 };
