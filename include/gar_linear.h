@@ -24,8 +24,8 @@
  * for the same parameters (host, pure; 0 on invalid ones).  Nothing in them
  * is kept from one call for the next; two calls that may run at the same time, replays of captured graphs
  * among them, need one each.  Matrices whose rows do not start
- * on 16 bytes are copied there first, at the cost of reading and writing them
- * once more.
+ * on 16 bytes (in large products: on 32) are copied there first, at the cost of
+ * reading and writing them once more.
  */
 #ifndef GAR_LINEAR_H_
 #define GAR_LINEAR_H_

@@ -957,6 +957,7 @@ private:
     size_t used_ = 0;
 };
 
+double products(int64_t rows, int64_t hidden, int64_t wide) { return double(rows) * double(hidden) * double(wide); }
 unsigned copy_blocks(int64_t pieces, int sm_count) { return unsigned(std::min<int64_t>(int64_t(16) * sm_count, parts_of(pieces, 256))); }
 
 // A launch that may be set up while the one before it on the stream ends: every kernel here waits for that one's
@@ -975,13 +976,21 @@ cudaError_t launch_small(void (*kernel)(P...), dim3 grid, cudaStream_t stream, A
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
-// A matrix of the caller's as an operand: where it lies, or copied to the space reserved for it.
+// A matrix of the caller's as an operand: where it lies, or copied to the space reserved for it.  It is copied where TMA does not take
+// it, and where its rows start between the sectors of 32 bytes, if enough tiles read it: a box's rows of 128 bytes then touch five
+// sectors instead of four.  1000 x 50001, 1000 elements a row, scores: 115 us, with x copied 100; 8192 x 20000 306, with x and W copied 279;
+// with W read by eight tiles its copy costs more than it saves (2048 x 20000, gated 163, copied 175).
+constexpr int64_t LN_PITCH = 16;                       // elements: rows of copies start on 32 bytes
 struct Input {
     Operand m;
     char*   copy = nullptr;
     bool    copied;
-    Input(Space& space, const void* p, int64_t rows, int64_t cols, int64_t ld) : m{static_cast<const char*>(p), rows, cols, ld}, copied(!on_16(p, ld)) {
-        if (copied) copy = space.take(size_t(rows) * size_t(up_to(cols, 8)) * 2);
+    // reads: tiles that read each of its elements; work: products of the call
+    Input(Space& space, const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t reads, double work)
+        : m{static_cast<const char*>(p), rows, cols, ld}, copied(!on_16(p, ld)) {
+        const bool split = rows > 1 && (reinterpret_cast<uintptr_t>(p) % 32 != 0 || ld % 16 != 0);
+        if (split && reads >= 16 && work >= 8e9) copied = true;
+        if (copied) copy = space.take(size_t(rows) * size_t(up_to(cols, LN_PITCH)) * 2);
     }
 };
 CopyJob copy_job(const Operand& src, void* dst, int64_t ld) {
@@ -998,7 +1007,7 @@ struct Copies {
     }
     void add(Input& in) {
         if (!in.copied) return;
-        const int64_t ld = up_to(in.m.cols, 8);
+        const int64_t ld = up_to(in.m.cols, LN_PITCH);
         add(copy_job(in.m, in.copy, ld));
         in.m.p = in.copy;
         in.m.ld = ld;
@@ -1256,7 +1265,8 @@ struct ScoresPlan {
     float2* parts;
     float*  target_z;
     ScoresPlan(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw)
-        : space(p.workspace), x(space, p.x, p.rows, p.hidden, ldx), w(space, p.weight, p.vocab, p.hidden, ldw), rows(rows_at_once(p.rows, p.vocab)) {
+        : space(p.workspace), x(space, p.x, p.rows, p.hidden, ldx, parts_of(p.vocab, LN_N), products(p.rows, p.hidden, p.vocab)),
+          w(space, p.weight, p.vocab, p.hidden, ldw, parts_of(p.rows, 2 * LN_M), products(p.rows, p.hidden, p.vocab)), rows(rows_at_once(p.rows, p.vocab)) {
         // (the last rows, if they are fewer, may have narrower tiles; a few rows have a part per CTA)
         const int64_t last = (p.rows - 1) % rows + 1;
         const int64_t most = p.rows <= 16 ? std::max(p.rows * scores_tiles(p.rows, p.hidden, p.vocab), (p.rows * LN_FEW_PARTS + 1) / 2)
@@ -1299,8 +1309,8 @@ struct GradPlan {
     char*     weight_space = nullptr;
     size_t    weight_bytes = 0;
     GradPlan(const gar_linear_logprobs_grad_params_t& p, int64_t ldw)
-        : space(p.workspace), rows(p.workers * p.tokens), piece(piece_of(std::max<int64_t>(rows, 1), p.hidden, p.vocab)), ld_dz(up_to(piece, 8)), ldx(up_to(p.hidden, 8)),
-          w(space, p.weight, p.vocab, p.hidden, ldw) {
+        : space(p.workspace), rows(p.workers * p.tokens), piece(piece_of(std::max<int64_t>(rows, 1), p.hidden, p.vocab)), ld_dz(up_to(piece, 8)), ldx(up_to(p.hidden, LN_PITCH)),
+          w(space, p.weight, p.vocab, p.hidden, ldw, 2 * parts_of(rows, 2 * LN_M), products(rows, p.hidden, p.vocab)) {
         x_rows = space.take(size_t(rows) * size_t(ldx) * 2);
         coef = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
         if (p.dtype == GAR_F16) top = reinterpret_cast<unsigned*>(space.take(4));
@@ -1439,8 +1449,10 @@ struct GatedPlan {
     Space space;
     Input x, gate, up;
     GatedPlan(const gar_gated_linear_params_t& p)
-        : space(p.workspace), x(space, p.x, p.rows, p.hidden, p.ldx), gate(space, p.w_gate, p.inner, p.hidden, p.ld_gate),
-          up(space, p.w_up, p.inner, p.hidden, p.ld_up) {}
+        : space(p.workspace), x(space, p.x, p.rows, p.hidden, p.ldx, parts_of(p.inner, LN_HALF), work(p)),
+          gate(space, p.w_gate, p.inner, p.hidden, p.ld_gate, parts_of(p.rows, 2 * LN_M), work(p)),
+          up(space, p.w_up, p.inner, p.hidden, p.ld_up, parts_of(p.rows, 2 * LN_M), work(p)) {}
+    static double work(const gar_gated_linear_params_t& p) { return 2 * products(p.rows, p.hidden, p.inner); }
 };
 struct GatedGradPlan {
     Space   space;
@@ -1449,11 +1461,14 @@ struct GatedGradPlan {
     int64_t pitch;
     float*  parts = nullptr;
     GatedGradPlan(const gar_gated_linear_grad_params_t& p)
-        : space(p.workspace), gate(space, p.w_gate, p.inner, p.hidden, p.ld_gate), up(space, p.w_up, p.inner, p.hidden, p.ld_up),
-          dgate(space, p.dgate, p.rows, p.inner, p.ld_dgate), dup(space, p.dup, p.rows, p.inner, p.ld_dup),
+        : space(p.workspace), gate(space, p.w_gate, p.inner, p.hidden, p.ld_gate, parts_of(p.rows, 2 * LN_M), work(p)),
+          up(space, p.w_up, p.inner, p.hidden, p.ld_up, parts_of(p.rows, 2 * LN_M), work(p)),
+          dgate(space, p.dgate, p.rows, p.inner, p.ld_dgate, parts_of(p.hidden, LN_N), work(p)),
+          dup(space, p.dup, p.rows, p.inner, p.ld_dup, parts_of(p.hidden, LN_N), work(p)),
           splits(splits_for(std::max<int64_t>(p.rows, 1), p.hidden, 2 * parts_of(p.inner, LN_K), 1, false)), pitch(up_to(p.hidden, 4)) {
         if (splits > 1) parts = reinterpret_cast<float*>(space.take(size_t(splits) * size_t(p.rows) * size_t(pitch) * 4));
     }
+    static double work(const gar_gated_linear_grad_params_t& p) { return 2 * products(p.rows, p.hidden, p.inner); }
 };
 }  // namespace
 

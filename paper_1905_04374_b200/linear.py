@@ -93,8 +93,8 @@ class LinearLogprobs(NamedTuple):
 
 
 class GatedLinearGrad(NamedTuple):
-    """What gar_gated_linear_backward returns.  Unless given, dgate and dup are made with rows that start on 16 bytes
-    (a row stride of a multiple of 8), as gar_linear_weight_grad reads them fastest."""
+    """What gar_gated_linear_backward returns.  Unless given, dgate and dup are made with rows that start on 32 bytes
+    (a row stride of a multiple of 16), as the products read them fastest."""
     dx: Optional[torch.Tensor]
     dgate: torch.Tensor
     dup: torch.Tensor
