@@ -63,7 +63,7 @@ struct LNArgs {
     float          whole;                 // logits: 1 + what the tensor core's sums are short by
     int            steps0, steps;         // steps of the first pair of operands, of both together
     int            group_shift, groups, out;
-    int64_t        col0, vocab;           // first column of this launch, columns there are
+    int64_t        col0;                  // first column of this launch
     const void *   bias, *bias2;          // 16-bit, or null
     const int64_t* targets;
     float2*        parts;                 // LN_SCORES [rows][2 nt]: maximum, sum
@@ -273,23 +273,33 @@ struct Columns {
     }
 };
 
-// What a warp reads for a tile from memory, while the tile's products still run: its columns' biases, into its piece of shared
-// memory, and what belongs to its rows.
+// What a thread reads for its row of a tile from memory: asked for a tile ahead, looked at when it is the tile's turn.
 struct RowInputs {
-    int64_t target;                  // from the launch's first column on; negative: none here
+    int64_t target;
     float   coef, lse, lo;
 };
-template <typename T, int EPI>
-__device__ __forceinline__ RowInputs fetch_inputs(const LNArgs& a, const Place& t, const Warp& w) {
+template <int EPI>
+__device__ __forceinline__ RowInputs ask_inputs(const LNArgs& a, const Place& t, unsigned rank, int quarter, int lane) {
     RowInputs in{-1, 0.f, 0.f, 0.f};
-    if (w.row0 >= a.rows) return in;
-    const int64_t row = w.row0 + w.lane;
-    if (EPI == LN_GATED) {
+    if (EPI != LN_SCORES && EPI != LN_DLOGITS) return in;
+    const int64_t row = int64_t(2 * t.m + int(rank)) * LN_M + quarter * 32 + lane;
+    if (row >= a.rows) return in;
+    if (a.targets) in.target = a.targets[row];
+    if (EPI == LN_DLOGITS) {
+        in.coef = a.coef[row];
+        in.lse = a.lse[row];
+        if (a.lse_lo) in.lo = a.lse_lo[row];
+    }
+    return in;
+}
+// The biases of a warp's columns of a tile, into its piece of shared memory, while the tile's products still run.
+template <typename T, int EPI>
+__device__ __forceinline__ void fetch_tile_biases(const LNArgs& a, const Place& t, const Warp& w) {
+    if (w.row0 >= a.rows) return;
+    if (EPI == LN_GATED && (a.bias || a.bias2)) {
         const int64_t c0 = int64_t(t.n) * (a.width / 2);
-        if (a.bias || a.bias2) {
-            fetch_biases<T>(a.bias, c0, a.cols, 0.f, w.add, w.lane);
-            fetch_biases<T>(a.bias2, c0, a.cols, 0.f, w.add + LN_HALF, w.lane);
-        }
+        fetch_biases<T>(a.bias, c0, a.cols, 0.f, w.add, w.lane);
+        fetch_biases<T>(a.bias2, c0, a.cols, 0.f, w.add + LN_HALF, w.lane);
     }
     if (EPI == LN_SCORES || EPI == LN_DLOGITS) {
         const int64_t c0 = int64_t(t.n) * a.width, left = a.cols - c0;
@@ -297,15 +307,7 @@ __device__ __forceinline__ RowInputs fetch_inputs(const LNArgs& a, const Place& 
             const Columns mine(left < a.width ? int(left) : a.width, w.group, EPI == LN_SCORES ? 32 : 64);
             fetch_biases<T>(a.bias, a.col0 + c0 + mine.from, a.col0 + a.cols, -CUDART_INF_F, w.add, w.lane);
         }
-        if (row < a.rows && a.targets) in.target = a.targets[row] - a.col0;
     }
-    if (EPI == LN_DLOGITS && row < a.rows) {
-        in.coef = a.coef[row];
-        in.lse = a.lse[row];
-        if (a.lse_lo) in.lo = a.lse_lo[row];
-        if (a.top) in.coef *= power_for(*a.top, false);
-    }
-    return in;
 }
 
 __device__ __forceinline__ void scores_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in) {
@@ -315,7 +317,7 @@ __device__ __forceinline__ void scores_tile(const LNArgs& a, const Place& t, con
     const Columns mine(left < a.width ? int(left) : a.width, w.group, 32);
     const int cols = mine.to - mine.from;
     const bool adds = a.bias || left < a.width, live = row < a.rows;
-    const int64_t t64 = in.target - c0 - mine.from;
+    const int64_t t64 = in.target - a.col0 - c0 - mine.from;
     const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
     float m = -CUDART_INF_F, s = 0.f;
     if (cols > 0)
@@ -382,9 +384,9 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
     if (w.row0 >= a.rows || cols <= 0) return;
     const int64_t first = c0 + mine.from;
     const bool adds = a.bias != nullptr;
-    float coef = in.coef;
+    float coef = a.top ? in.coef * power_for(*a.top, false) : in.coef;
     const float lse = in.lse, lo = in.lo;
-    const int64_t t64 = in.target - first;
+    const int64_t t64 = in.target - a.col0 - first;
     const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
     // a masked row: gradient 0 whatever comes in
     if (lse == -CUDART_INF_F) coef = 0.f;
@@ -719,12 +721,19 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
         w.add = sm.add[warp - LN_STORE_WARP0];
         w.lane = lane;
         unsigned done = 0;
+        Place t = place_at<EPI>(a, pair);                    // (a pair has a tile at least)
+        RowInputs in = ask_inputs<EPI>(a, t, rank, w.quarter, lane);
         for (unsigned i = pair; i < tiles; i += pairs, ++done) {
-            const Place t = place_at<EPI>(a, i);
             const unsigned half = done & 1u;
             w.src = tmem + half * LN_N + (unsigned(w.quarter * 32) << 16);
             w.row0 = int64_t(2 * t.m + int(rank)) * LN_M + w.quarter * 32;
-            const RowInputs in = fetch_inputs<T, EPI>(a, t, w);
+            fetch_tile_biases<T, EPI>(a, t, w);
+            Place next = t;
+            RowInputs next_in = in;
+            if (i + pairs < tiles) {
+                next = place_at<EPI>(a, i + pairs);
+                next_in = ask_inputs<EPI>(a, next, rank, w.quarter, lane);
+            }
             if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[half]), (done >> 1) & 1u, error)) break;
             tc_fence_after();
             __syncwarp();                                    // the warp's biases are there
@@ -735,6 +744,8 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_at_leader(&sm.acc_empty[half]);
+            t = next;
+            in = next_in;
         }
         if (lane == 0) tma_store_done();
     }
@@ -867,20 +878,21 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const CopyArgs a) {
     }
 }
 
-// Bias gradients: the columns of a worker's dz added up, eight columns and an eighth of the tokens per thread, the
-// eighths in order.
+// Bias gradients: the columns of a worker's dz added up, eight columns and every SLICES-th token per thread, the slices in order.
+constexpr int LN_SLICES = 32;
 template <typename T, typename G>
-__global__ void __launch_bounds__(256) column_sums_kernel(const T* dz, int64_t ld, int64_t tokens, int64_t cols, const unsigned* top, G* db, int64_t ld_grads) {
-    __shared__ float sums[8][32][9];
+__global__ void __launch_bounds__(32 * LN_SLICES) column_sums_kernel(const T* dz, int64_t ld, int64_t tokens, int64_t cols, const unsigned* top, G* db,
+                                                                    int64_t ld_grads) {
+    __shared__ float sums[LN_SLICES][32][9];
     grid_dependency();
     const int64_t c = (int64_t(blockIdx.x) * 32 + threadIdx.x % 32) * 8;
-    const int part = threadIdx.x / 32;
+    const int slice = threadIdx.x / 32;
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const T* p = dz + int64_t(blockIdx.y) * tokens * ld + c;
     // (rows of dz are padded to whole pieces; what lies behind the last column is added and not stored)
     if (c < cols) {
 #pragma unroll 4
-        for (int64_t t = part; t < tokens; t += 8) {
+        for (int64_t t = slice; t < tokens; t += LN_SLICES) {
             float v[8];
             widen16B(__ldg(reinterpret_cast<const uint4*>(p + t * ld)), v, static_cast<const T*>(nullptr));
 #pragma unroll
@@ -888,13 +900,13 @@ __global__ void __launch_bounds__(256) column_sums_kernel(const T* dz, int64_t l
         }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[part][threadIdx.x % 32][j] = s[j];
+    for (int j = 0; j < 8; ++j) sums[slice][threadIdx.x % 32][j] = s[j];
     __syncthreads();
     const int64_t mine = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (mine >= cols) return;
+    if (threadIdx.x >= 256 || mine >= cols) return;
     float sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum += sums[k][threadIdx.x / 8][threadIdx.x % 8];
+    for (int k = 0; k < LN_SLICES; ++k) sum += sums[k][threadIdx.x / 8][threadIdx.x % 8];
     if (top) sum *= power_for(*top, true);
     db[int64_t(blockIdx.y) * ld_grads + mine] = Elem<G>::narrow(sum);
 }
@@ -962,11 +974,11 @@ unsigned copy_blocks(int64_t pieces, int sm_count) { return unsigned(std::min<in
 
 // A launch that may be set up while the one before it on the stream ends: every kernel here waits for that one's
 // results first (grid_dependency).
-template <typename... P, typename... A>
+template <int THREADS = 256, typename... P, typename... A>
 cudaError_t launch_small(void (*kernel)(P...), dim3 grid, cudaStream_t stream, A... args) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(THREADS);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1233,10 +1245,10 @@ template <typename T>
 cudaError_t column_sums(const DenseWeightGrad& g, cudaStream_t stream) {
     const dim3 grid(unsigned(parts_of(g.out, 256)), unsigned(g.workers));
     const T* dz = static_cast<const T*>(g.dy);
-    if (g.grads_dtype == GAR_F32) return launch_small(column_sums_kernel<T, float>, grid, stream, dz, g.ld_dy, g.tokens, g.out, g.top, static_cast<float*>(g.db), g.ld_grads);
+    if (g.grads_dtype == GAR_F32) return launch_small<32 * LN_SLICES>(column_sums_kernel<T, float>, grid, stream, dz, g.ld_dy, g.tokens, g.out, g.top, static_cast<float*>(g.db), g.ld_grads);
     if (g.grads_dtype == GAR_BF16)
-        return launch_small(column_sums_kernel<T, __nv_bfloat16>, grid, stream, dz, g.ld_dy, g.tokens, g.out, g.top, static_cast<__nv_bfloat16*>(g.db), g.ld_grads);
-    return launch_small(column_sums_kernel<T, __half>, grid, stream, dz, g.ld_dy, g.tokens, g.out, g.top, static_cast<__half*>(g.db), g.ld_grads);
+        return launch_small<32 * LN_SLICES>(column_sums_kernel<T, __nv_bfloat16>, grid, stream, dz, g.ld_dy, g.tokens, g.out, g.top, static_cast<__nv_bfloat16*>(g.db), g.ld_grads);
+    return launch_small<32 * LN_SLICES>(column_sums_kernel<T, __half>, grid, stream, dz, g.ld_dy, g.tokens, g.out, g.top, static_cast<__half*>(g.db), g.ld_grads);
 }
 cudaError_t weight_grad(DenseWeightGrad g, int sm_count, cudaStream_t stream) {
     if (!outer_applies(g)) return launch_dense_weight_grad(g, sm_count, stream);
@@ -1405,7 +1417,6 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
             if (cudaError_t err = logits_maps(maps, a, p.dtype, x, w, LN_STORE_UNIT)) return err;
             a.bias = p.bias;
             a.col0 = v0;
-            a.vocab = p.vocab;
             a.targets = p.targets;
             a.lse = p.lse;
             a.lse_lo = p.lse_lo;
