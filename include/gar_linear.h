@@ -74,6 +74,7 @@ size_t gar_linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t* p
  * gar_linear_weight_grad.  The vocabulary is gone through in pieces, whose dz is kept in the workspace: up to 96 MB of
  * it.  binary16 dz carry a power of two taken from the largest |a|, so that small gradients do not underflow.
  *   - A row without a target, or with a = 0, gets dx 0 and nothing it holds, NaN included, reaches a weight gradient.
+ *   - No tokens: weight and bias gradients of zeros.
  *   - A row masked throughout has gradient 0; in any other row a target >= vocab gives NaN, in dx and
  *     in its worker's gradients; no row reaches another worker's.
  * 1 <= workers <= GAR_MAX_N; workers * tokens < 2^30.

@@ -829,8 +829,8 @@ __global__ void __launch_bounds__(256) join_scores_kernel(const float2* parts, c
 
 // Rows of 16-bit elements copied to rows that start on 16 bytes, eight elements per thread and turn; up to four matrices,
 // one per blockIdx.y.  A job with targets is the rows of a head: those whose coefficient is 0 are copied as zeros, and the coefficients
-// (the gradient at a row's log probability; 0 without a target, NaN for a target outside the vocabulary) and the
-// largest one's magnitude are written.
+// (the gradient at a row's log probability; 0 without a target, NaN for a target outside the vocabulary) are written.  Where the
+// largest one's magnitude is asked for, the first block behind the jobs finds it, of all rows.
 struct CopyJob {
     const unsigned short* src;
     int64_t        ld, cols, pieces, per_row;
@@ -839,28 +839,46 @@ struct CopyJob {
 };
 struct CopyArgs {
     CopyJob        job[4];
+    int            jobs;
     const int64_t* targets;                // of the first job; or null
     const float*   grad;
-    int64_t        vocab;
+    int64_t        vocab, rows;
     float*         coef;
     unsigned*      top;                    // null: not asked for
 };
+__device__ __forceinline__ float coefficient(const CopyArgs& a, int64_t row) {
+    const int64_t t = a.targets[row];
+    return t < 0 ? 0.f : t >= a.vocab ? CUDART_NAN_F : a.grad[row];
+}
 __global__ void __launch_bounds__(256) copy_rows_kernel(const CopyArgs a) {
     grid_dependency();
+    if (blockIdx.y == unsigned(a.jobs)) {
+        if (blockIdx.x != 0) return;
+        __shared__ unsigned most[8];
+        unsigned top = 0;
+#pragma unroll 8
+        for (int64_t row = threadIdx.x; row < a.rows; row += 256) {
+            const unsigned bits = __float_as_uint(coefficient(a, row)) & 0x7fffffffu;
+            if (bits < 0x7f800000u) top = max(top, bits);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (threadIdx.x % 32 == 0) most[threadIdx.x / 32] = top;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int k = 1; k < 8; ++k) top = max(top, most[k]);
+            *a.top = top;
+        }
+        return;
+    }
     const CopyJob& j = a.job[blockIdx.y];
     const bool head = a.targets && blockIdx.y == 0;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < j.pieces; i += int64_t(gridDim.x) * 256) {
         const int64_t row = i / j.per_row, c = (i - row * j.per_row) * 8;
         bool zero = false;
         if (head) {
-            const int64_t t = a.targets[row];
-            const float coef = t < 0 ? 0.f : t >= a.vocab ? CUDART_NAN_F : a.grad[row];
+            const float coef = coefficient(a, row);
             zero = coef == 0.f;
-            if (c == 0) {
-                a.coef[row] = coef;
-                const unsigned bits = __float_as_uint(coef) & 0x7fffffffu;
-                if (a.top && bits < 0x7f800000u) atomicMax(a.top, bits);      // the same in any order
-            }
+            if (c == 0) a.coef[row] = coef;
         }
         const unsigned short* p = j.src + row * j.ld + c;
         uint4 w = make_uint4(0, 0, 0, 0);
@@ -1024,8 +1042,9 @@ struct Copies {
         in.m.p = in.copy;
         in.m.ld = ld;
     }
-    cudaError_t launch(int sm_count, cudaStream_t stream) const {
-        return most > 0 ? launch_small(copy_rows_kernel, dim3(copy_blocks(most, sm_count), unsigned(n)), stream, a) : cudaSuccess;
+    cudaError_t launch(int sm_count, cudaStream_t stream) {
+        a.jobs = n;
+        return most > 0 ? launch_small(copy_rows_kernel, dim3(copy_blocks(most, sm_count), unsigned(n + (a.top ? 1 : 0))), stream, a) : cudaSuccess;
     }
 };
 
@@ -1393,14 +1412,13 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
     GradPlan plan(p, ldw);
     const Operand x{plan.x_rows, plan.rows, p.hidden, plan.ldx};
     if (plan.rows > 0) {
-        if (plan.top)
-            if (cudaError_t err = cudaMemsetAsync(plan.top, 0, 4, stream)) return err;
         Copies copies;
         copies.add(copy_job(Operand{static_cast<const char*>(p.x), plan.rows, p.hidden, ldx}, plan.x_rows, plan.ldx));
         copies.add(plan.w);
         copies.a.targets = p.targets;
         copies.a.grad = p.grad_logprobs;
         copies.a.vocab = p.vocab;
+        copies.a.rows = plan.rows;
         copies.a.coef = plan.coef;
         copies.a.top = plan.top;
         if (cudaError_t err = copies.launch(sm_count, stream)) return err;

@@ -528,6 +528,7 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
     __syncthreads();
     pair_sync();                              // the other CTA's barriers are initialised
     tc_fence_after();
+    grid_dependency();                        // (up to here it runs while the launch before it on the stream ends)
     const unsigned tmem = sm.tmem_base;
     const Walk walk = walk_of<MODE>(a, pair, pairs);
     // step s of a tile is number g + s of all the CTA's steps; of those with codes, number gq + s
@@ -931,12 +932,14 @@ cudaError_t launch(const WGArgs& a, const CUtensorMap& map_dy, const CUtensorMap
     cfg.blockDim = dim3(Plan<MODE>::THREADS);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a, map_dy, map_x, map_dw);
 }
 template <typename T, int MODE>
