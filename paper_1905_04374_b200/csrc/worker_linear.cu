@@ -9,8 +9,9 @@
 //                  B lie with the contraction along their rows (K-major), or across them (MN-major: the
 //                  gradient at the inputs, dz W, reads W as it lies, the gradient at the weights, dz^T x, both)
 //   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
-//   store warps    two groups of four, each with half of a tile's columns, while the next tile's products run
-//                  into the other half of tensor memory; a thread has one row, 32 columns at a time
+//   store warps    groups of four, each with its share of a tile's columns, while the next tile's products run
+//                  into the other half of tensor memory; a thread has one row, 32 columns at a time.  Two groups, or four
+//                  where a column takes an exponential (struct Shape)
 // and four epilogues (LN_SUM's and LN_OUTER's are one; enum Epilogue).  A thread owning a row makes the softmax's statistics, the group
 // maxima of the checkpoints and the row's target its own affair.
 // Tiles are as wide as the rule in width_for makes them, 256 columns at most.
@@ -40,8 +41,7 @@ constexpr int LN_TILE = LN_M * LN_K * 2;              // bytes of A (and, at ful
 constexpr int LN_RING_BYTES = 5 * 2 * LN_TILE, LN_RING_MOST = 8;
 constexpr int LN_BLOCK = 64 * 128;                    // bytes of 64 x 64 elements of an MN-major operand
 constexpr int LN_COPY_WARP = 0, LN_MMA_WARP = 1, LN_ALLOC_WARP = 2;
-constexpr int LN_STORE_WARP0 = 4, LN_STORE_WARPS = 8;
-constexpr int LN_THREADS = 32 * (LN_STORE_WARP0 + LN_STORE_WARPS);
+constexpr int LN_STORE_WARP0 = 4;
 constexpr int LN_PAIRS = 74;                          // pairs of SMs, for the rules that cut work into parts and tiles
 constexpr float LN_SHORT = 1.0e-9f;                   // of a sum, lost per term
 
@@ -61,12 +61,13 @@ struct LNArgs {
     int            ring, slot_bytes;      // steps in flight, what one takes in shared memory
     int            group_m;               // (pair) row tiles that go round a column tile together
     float          whole;                 // logits: 1 + what the tensor core's sums are short by
+    int            twice;                 // logits: each half of the contraction has a half of tensor memory (a pair has one tile)
     int            steps0, steps;         // steps of the first pair of operands, of both together
     int            group_shift, groups, out;
     int64_t        col0;                  // first column of this launch
     const void *   bias, *bias2;          // 16-bit, or null
     const int64_t* targets;
-    float2*        parts;                 // LN_SCORES [rows][2 nt]: maximum, sum
+    float2*        parts;                 // LN_SCORES [rows][nt]: maximum, sum
     float*         target_z;              // LN_SCORES [rows]
     const float *  lse, *lse_lo, *coef;   // LN_DLOGITS [rows]
     const unsigned* top;                  // the largest |coef|, as bits, where coefficients carry a power of two; or null
@@ -75,10 +76,20 @@ struct LNArgs {
     gar_checkpoint_t s0, s1;              // of g and u
 };
 
-struct __align__(1024) LNSmem {
+// Store warps, their staged pieces of a result (32 rows) and the biases they keep.  The logits' epilogues are bound by latency where the
+// contraction is short (two warps on a scheduler issue in 37 % of the cycles, 4096 x 32000, 128): four groups, of fewer registers.
+template <int EPI> struct Shape {
+    static constexpr bool LOGITS = EPI == LN_SCORES || EPI == LN_DLOGITS;
+    static constexpr int GROUPS = LOGITS ? 4 : 2, STORE_WARPS = 4 * GROUPS, THREADS = 32 * (LN_STORE_WARP0 + STORE_WARPS);
+    static constexpr int PIECE = EPI == LN_SCORES ? 16 : EPI == LN_DLOGITS ? 32 * 64 : 32 * 128, BIASES = LOGITS ? 64 : LN_N;
+};
+template <int EPI> struct __align__(1024) LNSmem {
+    typedef Shape<EPI> S;
     uint8_t  ring[LN_RING_BYTES];                         // slots: 128 rows of A, half the tile's rows of B
-    uint8_t  out[LN_STORE_WARPS][32 * 128];               // a store warp's piece: 32 rows of 128 bytes
-    float    add[LN_STORE_WARPS][LN_N];                   // a warp's biases, -inf for columns that do not exist
+    uint8_t  out[S::STORE_WARPS][S::PIECE];               // a store warp's piece: 32 rows of 128 bytes (LN_DLOGITS: 64)
+    float    add[S::STORE_WARPS][S::BIASES];              // a warp's biases, -inf for columns that do not exist
+    float2   part[EPI == LN_SCORES ? 2 : 1][4][EPI == LN_SCORES ? LN_M : 1];        // the groups' maxima and sums, by half of tensor memory
+    unsigned long long part_full[2];                      // they are there
     unsigned long long empty[LN_RING_MOST], acc_full[2];  // the slots are read; the accumulators are complete
     unsigned long long full[LN_RING_MOST], acc_empty[2];  // the leading CTA's are used, for both
     unsigned tmem_base;
@@ -157,6 +168,43 @@ __device__ __forceinline__ void over_columns(unsigned src, int cols, F f) {
         wait32(v1);
         if (c0 + 64 < cols) ask32(src + unsigned(c0 + 64), v0);
         f(v1, c0 + 32);
+    }
+}
+// The same for the logits' epilogues, one after the other (four warps of a scheduler take turns); twice: the sum of both halves of
+// tensor memory.
+__device__ __forceinline__ void ask16(unsigned taddr, float (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+                   "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void wait16(float (&a)[16], float (&b)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(a[0]), "+f"(a[1]), "+f"(a[2]), "+f"(a[3]), "+f"(a[4]), "+f"(a[5]), "+f"(a[6]), "+f"(a[7]), "+f"(a[8]), "+f"(a[9]),
+                   "+f"(a[10]), "+f"(a[11]), "+f"(a[12]), "+f"(a[13]), "+f"(a[14]), "+f"(a[15]), "+f"(b[0]), "+f"(b[1]), "+f"(b[2]),
+                   "+f"(b[3]), "+f"(b[4]), "+f"(b[5]), "+f"(b[6]), "+f"(b[7]), "+f"(b[8]), "+f"(b[9]), "+f"(b[10]), "+f"(b[11]),
+                   "+f"(b[12]), "+f"(b[13]), "+f"(b[14]), "+f"(b[15]) :: "memory");
+}
+template <typename F>
+__device__ __forceinline__ void over_logits(unsigned src, bool twice, int cols, F f) {
+#pragma unroll 1
+    for (int c0 = 0; c0 < cols; c0 += 32) {
+        float v[32];
+        if (!twice) {
+            ask32(src + unsigned(c0), v);
+            wait32(v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 32; k += 16) {
+                float a[16], b[16];
+                ask16(src + unsigned(c0 + k), a);
+                ask16(src + unsigned(c0 + k + LN_N), b);
+                wait16(a, b);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[k + j] = a[j] + b[j];
+            }
+        }
+        f(v, c0);
     }
 }
 __device__ __forceinline__ void add32(float (&v)[32], const float* add) {
@@ -242,18 +290,18 @@ __device__ __forceinline__ void store_plain32(unsigned stage, int lane, float* d
     }
 }
 
-// 128 columns' biases from column c0 on, `fill` where there is no column
-template <typename T>
+// N columns' biases from column c0 on, `fill` where there is no column
+template <typename T, int N>
 __device__ __forceinline__ void fetch_biases(const void* bias, int64_t c0, int64_t cols, float fill, float* add, int lane) {
-    float v[4];
+    float v[N / 32];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N / 32; ++k) {
         const int64_t c = c0 + 32 * k + lane;
         v[k] = c >= cols ? fill : 0.f;
         if (bias && c < cols) v[k] = Elem<T>::widen(static_cast<const T*>(bias)[c]);
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) add[32 * k + lane] = v[k];
+    for (int k = 0; k < N / 32; ++k) add[32 * k + lane] = v[k];
 }
 
 // ---- epilogues: one warp's 32 rows and its group's columns of a tile -------------------------------
@@ -266,10 +314,9 @@ struct Warp {
 // A group's columns of the `cols` a tile has: from, to; whole multiples of `unit` but for the tile's end
 struct Columns {
     int from, to;
-    __device__ __forceinline__ Columns(int cols, int group, int unit) {
-        const int first = (cols + 2 * unit - 1) / (2 * unit) * unit;
-        from = group ? min(first, cols) : 0;
-        to = group ? cols : min(first, cols);
+    template <int GROUPS, int UNIT> static __device__ __forceinline__ Columns of(int cols, int group) {
+        const int each = (cols + GROUPS * UNIT - 1) / (GROUPS * UNIT) * UNIT;
+        return Columns{min(group * each, cols), min((group + 1) * each, cols)};
     }
 };
 
@@ -298,30 +345,30 @@ __device__ __forceinline__ void fetch_tile_biases(const LNArgs& a, const Place& 
     if (w.row0 >= a.rows) return;
     if (EPI == LN_GATED && (a.bias || a.bias2)) {
         const int64_t c0 = int64_t(t.n) * (a.width / 2);
-        fetch_biases<T>(a.bias, c0, a.cols, 0.f, w.add, w.lane);
-        fetch_biases<T>(a.bias2, c0, a.cols, 0.f, w.add + LN_HALF, w.lane);
+        fetch_biases<T, LN_HALF>(a.bias, c0, a.cols, 0.f, w.add, w.lane);
+        fetch_biases<T, LN_HALF>(a.bias2, c0, a.cols, 0.f, w.add + LN_HALF, w.lane);
     }
     if (EPI == LN_SCORES || EPI == LN_DLOGITS) {
         const int64_t c0 = int64_t(t.n) * a.width, left = a.cols - c0;
         if (a.bias || (EPI == LN_SCORES && left < a.width)) {
-            const Columns mine(left < a.width ? int(left) : a.width, w.group, EPI == LN_SCORES ? 32 : 64);
-            fetch_biases<T>(a.bias, a.col0 + c0 + mine.from, a.col0 + a.cols, -CUDART_INF_F, w.add, w.lane);
+            const Columns mine = Columns::of<4, 32>(left < a.width ? int(left) : a.width, w.group);
+            fetch_biases<T, 64>(a.bias, a.col0 + c0 + mine.from, a.col0 + a.cols, -CUDART_INF_F, w.add, w.lane);
         }
     }
 }
 
-__device__ __forceinline__ void scores_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in) {
+// The group's maximum and sum of this thread's row
+__device__ __forceinline__ float2 scores_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in) {
     const int64_t c0 = int64_t(t.n) * a.width, row = w.row0 + w.lane;
-    if (w.row0 >= a.rows) return;
     const int64_t left = a.cols - c0;
-    const Columns mine(left < a.width ? int(left) : a.width, w.group, 32);
+    const Columns mine = Columns::of<4, 32>(left < a.width ? int(left) : a.width, w.group);
     const int cols = mine.to - mine.from;
-    const bool adds = a.bias || left < a.width, live = row < a.rows;
+    const bool adds = a.bias || left < a.width;
     const int64_t t64 = in.target - a.col0 - c0 - mine.from;
     const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
     float m = -CUDART_INF_F, s = 0.f;
-    if (cols > 0)
-        over_columns(w.src + unsigned(mine.from), cols, [&](float (&v)[32], int at) {
+    if (cols > 0 && w.row0 < a.rows)
+        over_logits(w.src + unsigned(mine.from), a.twice, cols, [&](float (&v)[32], int at) {
             logits32(v, a.whole, adds, w.add + at);
             if (__any_sync(0xffffffffu, target >= at && target < at + 32)) {
                 float z = 0.f;
@@ -353,7 +400,16 @@ __device__ __forceinline__ void scores_tile(const LNArgs& a, const Place& t, con
             unpack2(add2(sum0, sum1), p, q);
             s += p + q;
         });
-    if (live) a.parts[(row * a.nt + t.n) * 2 + w.group] = make_float2(m, s);
+    return make_float2(m, s);
+}
+// The groups' parts of a row as one
+__device__ __forceinline__ float2 join4(const float2 (&p)[4]) {
+    const float m = fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x));
+    const float base = m == -CUDART_INF_F ? 0.f : m;
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s += p[k].y * ex2((p[k].x - base) * kLog2e);      // a part without entries is -inf, 0
+    return make_float2(m, s);
 }
 
 // 64 columns at a time to the result, staged
@@ -379,7 +435,7 @@ template <typename T>
 __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in, const CUtensorMap* map) {
     const int64_t c0 = int64_t(t.n) * a.width;
     const int64_t left = a.cols - c0;
-    const Columns mine(left < a.width ? int(left) : a.width, w.group, 64);
+    const Columns mine = Columns::of<4, 32>(left < a.width ? int(left) : a.width, w.group);
     const int cols = mine.to - mine.from;
     if (w.row0 >= a.rows || cols <= 0) return;
     const int64_t first = c0 + mine.from;
@@ -392,8 +448,7 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
     if (lse == -CUDART_INF_F) coef = 0.f;
     const bool nothing = coef == 0.f;
     const f32x2 minus = pack2(-lse, -lse), unit = pack2(kLog2e, kLog2e), minus_lo = pack2(-lo * kLog2e, -lo * kLog2e), by = pack2(-coef, -coef);
-    int half = 0;
-    over_columns(w.src + unsigned(mine.from), cols, [&](float (&v)[32], int at) {
+    over_logits(w.src + unsigned(mine.from), a.twice, cols, [&](float (&v)[32], int at) {
         logits32(v, a.whole, adds, w.add + at);
 #pragma unroll
         for (int j = 0; j < 32; j += 2) {
@@ -409,10 +464,16 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = nothing ? 0.f : v[j];
         }
-        if (half == 0) stage_free(w);
-        stage32<T>(w.stage, w.lane, half, v);
-        if (half == 1 || at + 32 >= cols) put_piece(a, w, map, first + (at & ~63), cols - (at & ~63), 0);
-        half ^= 1;
+        stage_free(w);
+        // rows of 64 bytes, 16-byte chunks in the 64-byte swizzle
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float f[8] = {v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3], v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7]};
+            put_shared(w.stage + w.lane * 64 + ((j ^ ((w.lane >> 1) & 3)) << 4), narrow16B(f, static_cast<const T*>(nullptr)));
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (w.lane == 0) tma_put(map, w.stage, int(first) + at, int(w.row0), 0);
     });
 }
 
@@ -421,7 +482,7 @@ template <typename T, int EPI>
 __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const Warp& w, const CUtensorMap* map) {
     const int64_t c0 = int64_t(t.n) * a.width;
     const int64_t left = a.cols - c0;
-    const Columns mine(left < a.width ? int(left) : a.width, w.group, 64);
+    const Columns mine = Columns::of<2, 64>(left < a.width ? int(left) : a.width, w.group);
     const int cols = mine.to - mine.from;
     if (w.row0 >= a.rows || cols <= 0) return;
     const int64_t first = c0 + mine.from;
@@ -532,7 +593,7 @@ __device__ __forceinline__ void gated_tile(const LNArgs& a, const Place& t, cons
     const int64_t c0 = int64_t(t.n) * half_width, row = w.row0 + w.lane;
     const int64_t left = a.cols - c0;
     const int all = left < half_width ? int(left) : half_width;
-    const Columns mine(all, w.group, 64);
+    const Columns mine = Columns::of<2, 64>(all, w.group);
     const int cols = mine.to - mine.from;
     if (w.row0 >= a.rows || cols <= 0) return;
     const int64_t first = c0 + mine.from;
@@ -590,12 +651,13 @@ __device__ __forceinline__ void gated_tile(const LNArgs& a, const Place& t, cons
 }
 
 template <typename T, int EPI, int ACT>
-__global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, const __grid_constant__ CUtensorMap map_a0,
+__global__ void __launch_bounds__(Shape<EPI>::THREADS, 1) linear_kernel(const LNArgs a, const __grid_constant__ CUtensorMap map_a0,
                                                               const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_a1,
                                                               const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_out) {
     constexpr bool A_MN = EPI == LN_OUTER, B_MN = EPI == LN_SUM || EPI == LN_OUTER;
     extern __shared__ uint8_t raw[];
-    LNSmem& sm = *reinterpret_cast<LNSmem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    constexpr int STORE_WARPS = Shape<EPI>::STORE_WARPS, THREADS = Shape<EPI>::THREADS;
+    LNSmem<EPI>& sm = *reinterpret_cast<LNSmem<EPI>*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     volatile int* error = &sm.error;
     const unsigned rank = cta_rank();
@@ -608,7 +670,8 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
         }
         for (int b = 0; b < 2; ++b) {
             kb_init(&sm.acc_full[b], 1);
-            kb_init(&sm.acc_empty[b], 2 * LN_STORE_WARPS);
+            kb_init(&sm.acc_empty[b], 2 * STORE_WARPS);
+            kb_init(&sm.part_full[b], STORE_WARPS);
         }
         kb_fence_init();
     }
@@ -689,13 +752,15 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
                 const unsigned half = done & 1u, round = (done >> 1) & 1u, d = tmem + half * LN_N;
                 if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[half]), round ^ 1u, error)) { ok = false; break; }
                 tc_fence_after();
+                const int turn = Shape<EPI>::LOGITS && a.twice ? (steps + 1) / 2 : steps;      // from here on into the other half
                 for (int s = 0; s < steps; ++s, r.next(a)) {
                     if (!kb_wait_warp(kb_smem_u32(&sm.full[r.slot]), r.parity, error)) { ok = false; break; }
                     tc_fence_after();
                     const unsigned long long da = desc_a + r.slot * slot_step, db = desc_b + r.slot * slot_step;
                     if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < LN_K / 16; ++k) mma_f16(d, da + k * STEP_A, db + k * STEP_B, idesc, s > 0 || k > 0);
+                        for (int k = 0; k < LN_K / 16; ++k)
+                            mma_f16(s >= turn ? d + LN_N : d, da + k * STEP_A, db + k * STEP_B, idesc, (s > 0 && s != turn) || k > 0);
                         mma_commit(&sm.empty[r.slot]);
                     }
                     __syncwarp();
@@ -737,7 +802,18 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
             if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[half]), (done >> 1) & 1u, error)) break;
             tc_fence_after();
             __syncwarp();                                    // the warp's biases are there
-            if constexpr (EPI == LN_SCORES) scores_tile(a, t, w, in);
+            if constexpr (EPI == LN_SCORES) {
+                const int own = w.quarter * 32 + lane;
+                sm.part[half][w.group][own] = scores_tile(a, t, w, in);
+                __syncwarp();
+                if (lane == 0) kb_arrive(&sm.part_full[half]);
+                if (w.group == 0) {
+                    if (!kb_wait_warp(kb_smem_u32(&sm.part_full[half]), (done >> 1) & 1u, error)) break;
+                    const float2 p[4] = {sm.part[half][0][own], sm.part[half][1][own], sm.part[half][2][own], sm.part[half][3][own]};
+                    const int64_t row = w.row0 + lane;
+                    if (row < a.rows) a.parts[row * a.nt + t.n] = join4(p);
+                }
+            }
             if constexpr (EPI == LN_DLOGITS) dlogits_tile<T>(a, t, w, in, &map_out);
             if constexpr (EPI == LN_GATED) gated_tile<T, ACT>(a, t, w, &map_out);
             if constexpr (EPI == LN_SUM || EPI == LN_OUTER) sum_tile<T, EPI>(a, t, w, &map_out);
@@ -764,10 +840,10 @@ __global__ void __launch_bounds__(LN_THREADS, 1) linear_kernel(const LNArgs a, c
         const int WIDTH = EPI == LN_SCORES ? 1 : EPI == LN_GATED ? a.width / 2 : a.width;
         for (unsigned i = pair; i < tiles; i += pairs) {
             const Place t = place_at<EPI>(a, i);
-            for (int e = tid; e < LN_M * WIDTH; e += LN_THREADS) {
+            for (int e = tid; e < LN_M * WIDTH; e += THREADS) {
                 const int64_t row = int64_t(2 * t.m + int(rank)) * LN_M + e / WIDTH, c = int64_t(t.n) * WIDTH + e % WIDTH;
                 if (row >= a.rows) continue;
-                if constexpr (EPI == LN_SCORES) a.parts[(row * a.nt + t.n) * 2] = a.parts[(row * a.nt + t.n) * 2 + 1] = make_float2(CUDART_NAN_F, CUDART_NAN_F);
+                if constexpr (EPI == LN_SCORES) a.parts[row * a.nt + t.n] = make_float2(CUDART_NAN_F, CUDART_NAN_F);
                 else if (c < a.cols) {
                     const int64_t at = int64_t(t.split) * a.plane + row * a.ldy + c;
                     if (a.out >= OUT_PART) static_cast<float*>(a.y)[at] = CUDART_NAN_F;
@@ -966,9 +1042,10 @@ struct Operand {
     const char* p;
     int64_t     rows, cols, ld;
 };
-cudaError_t operand_map(CUtensorMap* map, int dtype, const Operand& m, int box_cols, int box_rows) {
+cudaError_t operand_map(CUtensorMap* map, int dtype, const Operand& m, int box_cols, int box_rows,
+                        CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
     const int64_t pitch = 2 * (m.rows > 1 ? m.ld : up_to(m.cols, 8));         // (a single row's stride may be anything)
-    return make_map(map, map_type(dtype), m.p, m.cols, m.rows, 1, pitch, pitch * m.rows, box_cols, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+    return make_map(map, map_type(dtype), m.p, m.cols, m.rows, 1, pitch, pitch * m.rows, box_cols, box_rows, swizzle);
 }
 
 // A workspace handed out piece by piece; without memory it only counts.
@@ -1058,7 +1135,7 @@ int group_rows(int64_t steps) { return int(std::max<int64_t>(8, 1024 / steps)); 
 
 template <typename T, int EPI, int ACT>
 cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t stream) {
-    constexpr int bytes = int(sizeof(LNSmem)) + 1024;
+    constexpr int bytes = int(sizeof(LNSmem<EPI>)) + 1024;
     static_assert(bytes <= 232448, "a CTA's shared memory");
     auto kernel = linear_kernel<T, EPI, ACT>;
     static std::atomic<uint64_t> allowed{0};           // devices on which the kernel may have that much
@@ -1076,9 +1153,12 @@ cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t str
     const int64_t tiles = int64_t(a.mt) * a.nt * a.splits;
     if (tiles >= int64_t(1) << 30) return cudaErrorInvalidConfiguration;
     const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
+    // logits: where a pair has one tile at most, the other half of tensor memory takes half of the contraction, which halves what is lost
+    a.twice = Shape<EPI>::LOGITS && tiles <= pairs && a.steps > 1;
+    a.whole = 1.f + LN_SHORT * float(LN_K) * float(a.steps) / (a.twice ? 2.f : 1.f);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(unsigned(2 * std::min(tiles, pairs)));
-    cfg.blockDim = dim3(LN_THREADS);
+    cfg.blockDim = dim3(Shape<EPI>::THREADS);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -1123,7 +1203,6 @@ cudaError_t logits_maps(Maps& maps, LNArgs& a, int dtype, const Operand& x, cons
     a.steps0 = a.steps = int(parts_of(x.cols, LN_K));
     a.width = width_for(a.mt, a.cols, a.steps, unit);
     a.nt = int(parts_of(w.rows, a.width));
-    a.whole = 1.f + LN_SHORT * float(x.cols);
     if (cudaError_t err = operand_map(&maps.a0, dtype, x, LN_K, LN_M)) return err;
     if (cudaError_t err = operand_map(&maps.b0, dtype, w, LN_K, a.width / 2)) return err;
     maps.a1 = maps.b1 = maps.out = maps.a0;            // not used unless set
@@ -1280,14 +1359,14 @@ cudaError_t weight_grad(DenseWeightGrad g, int sm_count, cudaStream_t stream) {
 constexpr int64_t LN_PARTS_BYTES = int64_t(64) << 20, LN_PIECE_BYTES = int64_t(96) << 20;
 constexpr int64_t LN_TERMS = 32768;                            // of a sum on the tensor cores
 constexpr int64_t LN_FEW_PARTS = 512;                          // CTAs of a few rows' kernel at most: two per SM
-constexpr int LN_SCORES_UNIT = 32, LN_STORE_UNIT = 64;         // columns: of a thread's turn; of a staged piece
+constexpr int LN_UNIT = 32;                                    // columns of a thread's turn
 // rows of a launch, so that its parts take 64 MB or so
 int64_t rows_at_once(int64_t rows, int64_t vocab) {
-    const int64_t most = std::max<int64_t>(256, LN_PARTS_BYTES / (16 * parts_of(vocab, LN_N)) / 256 * 256);
+    const int64_t most = std::max<int64_t>(256, LN_PARTS_BYTES / (8 * parts_of(vocab, LN_N)) / 256 * 256);
     return std::min(rows, most);
 }
 int64_t scores_tiles(int64_t rows, int64_t hidden, int64_t vocab) {
-    return parts_of(vocab, width_for(parts_of(rows, 2 * LN_M), vocab, parts_of(hidden, LN_K), LN_SCORES_UNIT));
+    return parts_of(vocab, width_for(parts_of(rows, 2 * LN_M), vocab, parts_of(hidden, LN_K), LN_UNIT));
 }
 struct ScoresPlan {
     Space   space;
@@ -1300,9 +1379,9 @@ struct ScoresPlan {
           w(space, p.weight, p.vocab, p.hidden, ldw, parts_of(p.rows, 2 * LN_M), products(p.rows, p.hidden, p.vocab)), rows(rows_at_once(p.rows, p.vocab)) {
         // (the last rows, if they are fewer, may have narrower tiles; a few rows have a part per CTA)
         const int64_t last = (p.rows - 1) % rows + 1;
-        const int64_t most = p.rows <= 16 ? std::max(p.rows * scores_tiles(p.rows, p.hidden, p.vocab), (p.rows * LN_FEW_PARTS + 1) / 2)
+        const int64_t most = p.rows <= 16 ? std::max(p.rows * scores_tiles(p.rows, p.hidden, p.vocab), p.rows * LN_FEW_PARTS)
                                           : std::max(rows * scores_tiles(rows, p.hidden, p.vocab), last * scores_tiles(last, p.hidden, p.vocab));
-        parts = reinterpret_cast<float2*>(space.take(size_t(most) * 16));
+        parts = reinterpret_cast<float2*>(space.take(size_t(most) * 8));
         target_z = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
     }
 };
@@ -1388,13 +1467,13 @@ cudaError_t launch_linear_logprobs(const gar_linear_logprobs_params_t& p, int64_
         x.rows = std::min(plan.rows, p.rows - r0);
         Maps maps;
         LNArgs a{};
-        if (cudaError_t err = logits_maps(maps, a, p.dtype, x, plan.w.m, LN_SCORES_UNIT)) return err;
+        if (cudaError_t err = logits_maps(maps, a, p.dtype, x, plan.w.m, LN_UNIT)) return err;
         a.bias = p.bias;
         a.targets = p.logprobs ? p.targets + r0 : nullptr;
         a.parts = plan.parts;
         a.target_z = plan.target_z;
         if (cudaError_t err = launch<LN_SCORES>(p.dtype, a, maps, sm_count, stream)) return err;
-        if (cudaError_t err = launch_small(join_scores_kernel, dim3(unsigned(parts_of(x.rows, 8))), stream, plan.parts, plan.target_z, a.targets, x.rows, 2 * a.nt,
+        if (cudaError_t err = launch_small(join_scores_kernel, dim3(unsigned(parts_of(x.rows, 8))), stream, plan.parts, plan.target_z, a.targets, x.rows, a.nt,
                                            p.vocab, p.logprobs ? p.logprobs + r0 : nullptr, p.lse ? p.lse + r0 : nullptr,
                                            p.lse_lo ? p.lse_lo + r0 : nullptr)) return err;
     }
@@ -1432,7 +1511,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
         if (plan.rows > 0) {
             Maps maps;
             LNArgs a{};
-            if (cudaError_t err = logits_maps(maps, a, p.dtype, x, w, LN_STORE_UNIT)) return err;
+            if (cudaError_t err = logits_maps(maps, a, p.dtype, x, w, LN_UNIT)) return err;
             a.bias = p.bias;
             a.col0 = v0;
             a.targets = p.targets;
@@ -1443,7 +1522,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
             a.out = OUT_WIDE;
             a.y = plan.dz;
             a.ldy = plan.ld_dz;
-            if (cudaError_t err = operand_map(&maps.out, p.dtype, dz, 64, 32)) return err;
+            if (cudaError_t err = operand_map(&maps.out, p.dtype, dz, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return err;
             if (cudaError_t err = launch<LN_DLOGITS>(p.dtype, a, maps, sm_count, stream)) return err;
             if (p.dx)
                 if (cudaError_t err = launch_sum(d, dz, w, nullptr, nullptr, v0 > 0, sm_count, stream)) return err;
