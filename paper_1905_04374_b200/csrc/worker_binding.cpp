@@ -370,6 +370,9 @@ PyObject* weight_grad_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t 
     END_HANDLE_TH_ERRORS
 }
 
+// whether `n` elements from `at` on lie in a row of `cols` (at + n may not fit 64 bits)
+bool has_room(int64_t cols, int64_t at, int64_t n) { return at >= 0 && n <= cols && at <= cols - n; }
+
 // dy, q, scales, cols, group, grads, weight_offset, bias_offset (-1: none), lengths, workspace (tensor,
 // True: allocate one, False: none, None: one where it is faster), stream
 PyObject* linear_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -382,9 +385,9 @@ PyObject* linear_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Place place(dev, a[10]);
     const Matrix g = matrix(grads, "grads");
     TORCH_CHECK_VALUE(grads.device() == dev, "grads must sit on ", dev);
-    TORCH_CHECK_VALUE(g.rows == p.workers && at_w >= 0 && at_w + p.out_features * cols <= g.cols,
+    TORCH_CHECK_VALUE(g.rows == p.workers && has_room(g.cols, at_w, p.out_features * cols),
                       "grads must have a row per worker and room for the weights at weight_offset");
-    TORCH_CHECK_VALUE(at_b < 0 || at_b + p.out_features <= g.cols, "grads has no room for the bias at bias_offset");
+    TORCH_CHECK_VALUE(at_b < 0 || has_room(g.cols, at_b, p.out_features), "grads has no room for the bias at bias_offset");
     p.grads_dtype = g.dtype;
     p.x_saved = saved(tensor(a[1], "x.q"), tensor(a[2], "x.scales"), "x", p.workers * p.tokens, cols, group, dev);
     if (given(a[8])) p.lengths = vector<int32_t>(tensor(a[8], "lengths"), "lengths", at::kInt, p.workers, dev);
@@ -500,8 +503,8 @@ PyObject* linear_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) 
         TORCH_CHECK_VALUE(grads.device() == dev, "grads must sit on ", dev);
         TORCH_CHECK_VALUE(g.rows >= 1 && g.rows <= GAR_MAX_N && m.rows % g.rows == 0, "grads must have a row for each of 1 to ", GAR_MAX_N,
                           " workers, with equally many rows of x");
-        TORCH_CHECK_VALUE(at_w >= 0 && at_w + w.rows * m.cols <= g.cols, "grads has no room for the weights at weight_offset");
-        TORCH_CHECK_VALUE(at_b < 0 || at_b + w.rows <= g.cols, "grads has no room for the bias at bias_offset");
+        TORCH_CHECK_VALUE(has_room(g.cols, at_w, w.rows * m.cols), "grads has no room for the weights at weight_offset");
+        TORCH_CHECK_VALUE(at_b < 0 || has_room(g.cols, at_b, w.rows), "grads has no room for the bias at bias_offset");
         p.grads_dtype = g.dtype;
         p.workers = int(g.rows);
         p.tokens = m.rows / g.rows;

@@ -262,6 +262,21 @@ def test_refusals(pkg):
             pytest.fail(f"call {i} was not refused")
 
 
+def test_offsets_near_the_end_of_64_bits_are_refused(pkg):
+    x, t, w, wg, wu, counter = inputs(6)
+    r = pkg.gar_linear_logprobs(x, w, t)
+    a = torch.ones(x.shape[0], device=DEV)
+    block = torch.empty(1, w.numel() + w.shape[0], device=DEV)
+    saved = pkg.gar_checkpoint_pack(x)
+    dy = torch.zeros(1, x.shape[0], 64, dtype=x.dtype, device=DEV)
+    far = 2 ** 63 - 1
+    for call in (lambda **at: pkg.gar_linear_logprobs_backward(x, w, r, t, a, grads=block, **at),
+                 lambda **at: pkg.gar_linear_weight_grad(dy, saved, block, **at)):
+        for at in (dict(weight_offset=far), dict(weight_offset=far - w.numel()), dict(weight_offset=0, bias_offset=far)):
+            with pytest.raises(ValueError):
+                call(**at)
+
+
 def test_written_tensors_count_as_modified(pkg):
     x, t, w, wg, wu, _ = inputs(7)
     f = pkg.gar_gated_linear_forward("silu", x, wg, wu)
