@@ -75,7 +75,8 @@ size_t gar_linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t* p
 int gar_linear_logprobs(const gar_linear_logprobs_params_t* p) {
     int64_t ldx, ldw;
     if (int rc = scores_ok(p, &ldx, &ldw)) return rc;
-    if (!aligned(p->x, 2) || !aligned(p->weight, 2) || !aligned(p->bias, 2)) return GAR_ERR_INVALID_ARG;
+    if (!aligned(p->x, 2) || !aligned(p->weight, 2) || !aligned(p->bias, 2) || !aligned(p->targets, 8)) return GAR_ERR_INVALID_ARG;
+    if (!aligned(p->logprobs, 4) || !aligned(p->lse, 4) || !aligned(p->lse_lo, 4)) return GAR_ERR_INVALID_ARG;
     if ((p->logprobs && !p->targets) || (!p->logprobs && !p->lse && !p->lse_lo)) return GAR_ERR_INVALID_ARG;
     const Span all[7] = {vec(p->logprobs, p->rows, 4), vec(p->lse, p->rows, 4), vec(p->lse_lo, p->rows, 4), span(p->x, p->rows, p->hidden, ldx, 2),
                          span(p->weight, p->vocab, p->hidden, ldw, 2), vec(p->bias, p->vocab, 2), vec(p->targets, p->rows, 8)};
@@ -99,7 +100,8 @@ int gar_linear_logprobs_backward(const gar_linear_logprobs_grad_params_t* p) {
     const size_t gs = esize(p->grads_dtype);
     if (!p->targets || !p->lse || !p->grad_logprobs || (!p->dx && !p->weight_grads) || (p->bias_grads && !p->weight_grads)) return GAR_ERR_INVALID_ARG;
     if (!aligned(p->x, 2) || !aligned(p->weight, 2) || !aligned(p->bias, 2) || !aligned(p->dx, 2) || !aligned(p->weight_grads, gs) ||
-        !aligned(p->bias_grads, gs)) return GAR_ERR_INVALID_ARG;
+        !aligned(p->bias_grads, gs) || !aligned(p->targets, 8) || !aligned(p->lse, 4) || !aligned(p->lse_lo, 4) ||
+        !aligned(p->grad_logprobs, 4)) return GAR_ERR_INVALID_ARG;
     int64_t lddx = p->lddx;
     if (p->dx && !shape_ok(rows, p->hidden, &lddx)) return GAR_ERR_INVALID_ARG;
     if (p->weight_grads) {

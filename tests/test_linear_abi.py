@@ -99,6 +99,25 @@ def test_scores_refusals(pkg):
     assert pkg.linear.lib().gar_linear_logprobs_workspace_bytes(None) == 0
 
 
+def test_vectors_off_their_alignment_are_refused(pkg):
+    def scores():
+        p = pkg.GarLinearLogprobsParams()
+        p.dtype, p.rows, p.hidden, p.vocab = 1, 4, 64, 100
+        p.x, p.weight, p.bias, p.targets, p.logprobs, p.lse, p.lse_lo = (1 << b for b in range(20, 27))
+        p.workspace, p.workspace_bytes = BIG, 1 << 20
+        return p
+
+    def grads():
+        p = pkg.GarLinearLogprobsGradParams()
+        p.dtype, p.workers, p.tokens, p.hidden, p.vocab = 1, 1, 4, 64, 100
+        p.x, p.weight, p.bias, p.targets, p.lse, p.lse_lo, p.grad_logprobs, p.dx = (1 << b for b in range(20, 28))
+        p.workspace, p.workspace_bytes = BIG, 1 << 24
+        return p
+    refuses(pkg, "gar_linear_logprobs", scores, [dict(targets=(1 << 23) + 4), dict(logprobs=(1 << 24) + 2), dict(lse=(1 << 25) + 2), dict(lse_lo=(1 << 26) + 1)])
+    refuses(pkg, "gar_linear_logprobs_backward", grads, [dict(targets=(1 << 23) + 4), dict(lse=(1 << 24) + 2), dict(lse_lo=(1 << 25) + 1),
+                                                         dict(grad_logprobs=(1 << 26) + 2)])
+
+
 def test_scores_backward_refusals(pkg):
     def params():
         p = pkg.GarLinearLogprobsGradParams()
