@@ -70,7 +70,8 @@ struct LNArgs {
     float2*        parts;                 // LN_SCORES [rows][nt]: maximum, sum
     float*         target_z;              // LN_SCORES [rows]
     const float *  lse, *lse_lo, *coef;   // LN_DLOGITS [rows]
-    const unsigned* top;                  // the largest |coef|, as bits, where coefficients carry a power of two; or null
+    const unsigned* top;                  // every worker's largest |coef|, as bits, where coefficients carry a power of two; or null
+    unsigned       tokens;                // rows of a worker, for `top`
     void*          y;                     // OUT_PLAIN, and the fill after a wait that gave up
     int64_t        ldy, plane;            // elements between the result's rows; its parts or workers
     gar_checkpoint_t s0, s1;              // of g and u
@@ -457,7 +458,8 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
     if (w.row0 >= a.rows || cols <= 0) return;
     const int64_t first = c0 + mine.from;
     const bool adds = a.bias != nullptr;
-    float coef = a.top ? in.coef * power_for(*a.top, false) : in.coef;
+    float coef = in.coef;
+    if (a.top && w.row0 + w.lane < a.rows) coef *= power_for(a.top[unsigned(w.row0 + w.lane) / a.tokens], false);
     const float lse = in.lse, lo = in.lo;
     const int64_t t64 = in.target - a.col0 - first;
     const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
@@ -504,7 +506,9 @@ __device__ __forceinline__ void sum_tile(const LNArgs& a, const Place& t, const 
     if (w.row0 >= a.rows || cols <= 0) return;
     const int64_t first = c0 + mine.from;
     const unsigned src = w.src + unsigned(mine.from);
-    const float by = a.top ? power_for(*a.top, true) : 1.f;
+    // (LN_SUM: a row of the result is a token's)
+    float by = 1.f;
+    if (a.top && (EPI == LN_OUTER || w.row0 + w.lane < a.rows)) by = power_for(a.top[EPI == LN_OUTER ? unsigned(t.split) : unsigned(w.row0 + w.lane) / a.tokens], true);
     const unsigned long long policy = EPI == LN_OUTER ? evict_first() : 0;
     if (a.out >= OUT_PART) {
         over_columns(src, cols, [&](float (&v)[32], int at) {
@@ -923,7 +927,8 @@ __global__ void __launch_bounds__(256) join_scores_kernel(const float2* parts, c
 // Rows of 16-bit elements copied to rows that start on 16 bytes, eight elements per thread and turn; up to four matrices,
 // one per blockIdx.y.  A job with targets is the rows of a head: those whose coefficient is 0 are copied as zeros, and the coefficients
 // (the gradient at a row's log probability; 0 without a target, NaN for a target outside the vocabulary) are written.  Where the
-// largest one's magnitude is asked for, the first block behind the jobs finds it, of all rows.
+// largest one's magnitude is asked for, the blocks behind the jobs find it, a worker each: one for all workers would let one
+// worker's coefficients push the others' dz below binary16's range.
 struct CopyJob {
     const unsigned short* src;
     int64_t        ld, cols, pieces, per_row;
@@ -935,9 +940,10 @@ struct CopyArgs {
     int            jobs;
     const int64_t* targets;                // of the first job; or null
     const float*   grad;
-    int64_t        vocab, rows;
+    int64_t        vocab, tokens;
+    int            workers;
     float*         coef;
-    unsigned*      top;                    // null: not asked for
+    unsigned*      top;                    // [workers]; null: not asked for
 };
 __device__ __forceinline__ float coefficient(const CopyArgs& a, int64_t row) {
     const int64_t t = a.targets[row];
@@ -946,20 +952,22 @@ __device__ __forceinline__ float coefficient(const CopyArgs& a, int64_t row) {
 __global__ void __launch_bounds__(256) copy_rows_kernel(const CopyArgs a) {
     grid_dependency();
     if (blockIdx.y == unsigned(a.jobs)) {
-        if (blockIdx.x != 0) return;
         __shared__ unsigned most[8];
-        unsigned top = 0;
+        for (int w = int(blockIdx.x); w < a.workers; w += int(gridDim.x)) {
+            unsigned top = 0;
 #pragma unroll 8
-        for (int64_t row = threadIdx.x; row < a.rows; row += 256) {
-            const unsigned bits = __float_as_uint(coefficient(a, row)) & 0x7fffffffu;
-            if (bits < 0x7f800000u) top = max(top, bits);
-        }
-        top = __reduce_max_sync(0xffffffffu, top);
-        if (threadIdx.x % 32 == 0) most[threadIdx.x / 32] = top;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int k = 1; k < 8; ++k) top = max(top, most[k]);
-            *a.top = top;
+            for (int64_t i = threadIdx.x; i < a.tokens; i += 256) {
+                const unsigned bits = __float_as_uint(coefficient(a, w * a.tokens + i)) & 0x7fffffffu;
+                if (bits < 0x7f800000u) top = max(top, bits);
+            }
+            top = __reduce_max_sync(0xffffffffu, top);
+            if (threadIdx.x % 32 == 0) most[threadIdx.x / 32] = top;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                for (int k = 1; k < 8; ++k) top = max(top, most[k]);
+                a.top[w] = top;
+            }
+            __syncthreads();                           // `most` has been read
         }
         return;
     }
@@ -1018,20 +1026,20 @@ __global__ void __launch_bounds__(32 * LN_SLICES) column_sums_kernel(const T* dz
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < LN_SLICES; ++k) sum += sums[k][threadIdx.x / 8][threadIdx.x % 8];
-    if (top) sum *= power_for(*top, true);
+    if (top) sum *= power_for(top[blockIdx.y], true);
     db[int64_t(blockIdx.y) * ld_grads + mine] = Elem<G>::narrow(sum);
 }
 
 // The parts of a sum, added in order and rounded once, four columns per thread and turn.
 template <typename T>
 __global__ void __launch_bounds__(256) join_parts_kernel(const float* parts, int64_t plane, int64_t pitch, int splits, int64_t rows, int64_t cols,
-                                                         const unsigned* top, T* y, int64_t ldy) {
+                                                         const unsigned* top, unsigned tokens, T* y, int64_t ldy) {
     grid_dependency();
     const int64_t per_row = (cols + 3) / 4, pieces = rows * per_row;
-    const float by = top ? power_for(*top, true) : 1.f;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += int64_t(gridDim.x) * 256) {
         const int64_t row = i / per_row, c = (i - row * per_row) * 4;
         const float* p = parts + row * pitch + c;
+        const float by = top ? power_for(top[unsigned(row) / tokens], true) : 1.f;
         float4 s = __ldcs(reinterpret_cast<const float4*>(p));
         for (int k = 1; k < splits; ++k) {
             const float4 q = __ldcs(reinterpret_cast<const float4*>(p + k * plane));
@@ -1253,7 +1261,8 @@ struct SumTarget {
     float*   parts;                                    // [splits][rows][pitch]; null: straight to dx
     int64_t  pitch;
     int      splits;
-    const unsigned* top;
+    const unsigned* top;                               // dz carries power_for(top[row / tokens]); or null
+    unsigned tokens;
 };
 cudaError_t launch_sum(const SumTarget& d, const Operand& a0, const Operand& b0, const Operand* a1, const Operand* b1, bool add, int sm_count, cudaStream_t stream) {
     Maps maps;
@@ -1289,6 +1298,7 @@ cudaError_t launch_sum(const SumTarget& d, const Operand& a0, const Operand& b0,
         a.y = d.dx;
         a.ldy = d.ld;
         a.top = d.top;
+        a.tokens = d.tokens;
         if (a.out == OUT_WIDE)
             if (cudaError_t err = operand_map(&maps.out, d.dtype, Operand{static_cast<const char*>(d.dx), d.rows, d.cols, d.ld}, 64, 32)) return err;
     }
@@ -1297,9 +1307,9 @@ cudaError_t launch_sum(const SumTarget& d, const Operand& a0, const Operand& b0,
 cudaError_t join_sum(const SumTarget& d, int sm_count, cudaStream_t stream) {
     const dim3 grid(copy_blocks(d.rows * parts_of(d.cols, 4), sm_count));
     if (d.dtype == GAR_BF16)
-        return launch_small(join_parts_kernel<__nv_bfloat16>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top,
+        return launch_small(join_parts_kernel<__nv_bfloat16>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top, d.tokens,
                             static_cast<__nv_bfloat16*>(d.dx), d.ld);
-    return launch_small(join_parts_kernel<__half>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top,
+    return launch_small(join_parts_kernel<__half>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top, d.tokens,
                         static_cast<__half*>(d.dx), d.ld);
 }
 
@@ -1440,7 +1450,7 @@ struct GradPlan {
           w(space, p.weight, p.vocab, p.hidden, ldw, 2 * parts_of(rows, 2 * LN_M), products(rows, p.hidden, p.vocab)) {
         x_rows = space.take(size_t(rows) * size_t(ldx) * 2);
         coef = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
-        if (p.dtype == GAR_F16) top = reinterpret_cast<unsigned*>(space.take(4));
+        if (p.dtype == GAR_F16) top = reinterpret_cast<unsigned*>(space.take(size_t(p.workers) * 4));
         dz = space.take(size_t(rows) * size_t(ld_dz) * 2);
         pitch = up_to(p.hidden, 4);
         // (sums of 2^15 terms at most)
@@ -1514,12 +1524,14 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
         copies.a.targets = p.targets;
         copies.a.grad = p.grad_logprobs;
         copies.a.vocab = p.vocab;
-        copies.a.rows = plan.rows;
+        copies.a.tokens = p.tokens;
+        copies.a.workers = p.workers;
         copies.a.coef = plan.coef;
         copies.a.top = plan.top;
         if (cudaError_t err = copies.launch(sm_count, stream)) return err;
     }
-    SumTarget d{p.dtype, p.dx, plan.rows, p.hidden, p.lddx ? p.lddx : p.hidden, plan.parts, plan.pitch, plan.splits, plan.top};
+    SumTarget d{p.dtype, p.dx, plan.rows, p.hidden, p.lddx ? p.lddx : p.hidden, plan.parts, plan.pitch, plan.splits, plan.top,
+                unsigned(p.tokens)};
     for (int64_t v0 = 0; v0 < p.vocab; v0 += plan.piece) {
         Operand w = plan.w.m;
         w.p += v0 * w.ld * 2;
@@ -1536,6 +1548,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
             a.lse_lo = p.lse_lo;
             a.coef = plan.coef;
             a.top = plan.top;
+            a.tokens = unsigned(p.tokens);
             a.out = OUT_WIDE;
             a.y = plan.dz;
             a.ldy = plan.ld_dz;
@@ -1685,7 +1698,7 @@ cudaError_t launch_gated_linear_backward(const gar_gated_linear_grad_params_t& p
     Copies copies;
     for (Input* in : {&plan.gate, &plan.up, &plan.dgate, &plan.dup}) copies.add(*in);
     if (cudaError_t err = copies.launch(sm_count, stream)) return err;
-    SumTarget d{p.dtype, p.dx, p.rows, p.hidden, p.lddx, plan.parts, plan.pitch, plan.splits, nullptr};
+    SumTarget d{p.dtype, p.dx, p.rows, p.hidden, p.lddx, plan.parts, plan.pitch, plan.splits, nullptr, 1};
     if (cudaError_t err = launch_sum(d, plan.dgate.m, plan.gate.m, &plan.dup.m, &plan.up.m, false, sm_count, stream)) return err;
     return plan.parts ? join_sum(d, sm_count, stream) : cudaSuccess;
 }

@@ -33,7 +33,7 @@ struct DenseWeightGrad {
     int64_t         ld_dy, ldx;
     void *          dw, *db;
     int64_t         ld_grads;
-    const unsigned* top;              // dy carries power_for(*top); or null
+    const unsigned* top;              // a worker's dy carries power_for(top[worker]); or null
     void*           workspace;        // of dense_weight_grad_workspace_bytes
 };
 // By the product with two store groups (worker_linear.cu): whether it applies, and the launch (weights only).

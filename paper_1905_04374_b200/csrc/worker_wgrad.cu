@@ -124,7 +124,7 @@ struct WGArgs {
     int            columns;               // nt + 1 with a bias
     int            splits;                // parts a worker's tokens are cut into, each with a result of its own
     int            wide;                  // the result's rows start on 16 bytes: stored by TMA
-    const unsigned* top;                  // dy carries the power of two for this largest magnitude; null: none
+    const unsigned* top;                  // a worker's dy carries the power of two for its largest magnitude; null: none
 };
 
 // this thread's lane of tensor memory: 16 columns of either accumulator, there once the loads are waited for
@@ -800,10 +800,10 @@ __global__ void __launch_bounds__(Plan<MODE>::THREADS, 1) weight_grad_kernel(con
     } else if (warp >= WG_STORE_WARP0) {
         const int quarter = warp - WG_STORE_WARP0;               // == warp % 4: tensor-memory lanes 32 quarter ..
         unsigned n_piece = 0;
-        const float by = a.top ? power_for(*a.top, true) : 1.f;
         Halves acc;
         for (unsigned i = walk.first; ok && i < walk.end; i += walk.step) {
             const Tile t = tile_at<MODE>(a, i);
+            const float by = a.top ? power_for(a.top[t.worker], true) : 1.f;
             const int64_t o0 = int64_t(2 * t.m + int(rank)) * WG_M + quarter * 32;
             // the chunks of tokens in order, the later ones added to the first; a worker without tokens has none
             for (int s0 = 0; s0 < t.steps; s0 += CHUNK) {
