@@ -28,6 +28,7 @@
 #include "worker_act.cuh"
 #include "worker_linear.cuh"
 #include "worker_tensor.cuh"
+#include "worker_tiles.cuh"
 
 namespace gar {
 namespace worker {
@@ -54,15 +55,13 @@ constexpr float LN_SHORT = 1.0e-9f;                   // of a sum, lost per term
 enum Epilogue { LN_SCORES = 0, LN_DLOGITS = 1, LN_GATED = 2, LN_SUM = 3, LN_OUTER = 4 };
 enum Out { OUT_WIDE = 0, OUT_PLAIN = 1, OUT_PART = 2, OUT_ADD = 3, OUT_PLAIN32 = 4 };   // 16 bits by TMA or plainly; fp32 by TMA, added, plainly
 
-struct LNArgs {
+struct LNArgs : Tiling {
     int64_t        rows, cols;            // of the result (LN_SCORES, LN_DLOGITS: columns from col0 on)
-    int            mt, nt, splits;        // pair row tiles, column tiles, parts of the contraction (LN_OUTER: workers)
     int            width;                 // columns of a tile (LN_GATED: g's and u's together)
     int            ring, slot_bytes;      // steps in flight, what one takes in shared memory
-    int            group_m;               // (pair) row tiles that go round a column tile together
     float          whole;                 // logits: 1 + what the tensor core's sums are short by
     int            twice;                 // logits: each half of the contraction has a half of tensor memory (a pair has one tile)
-    int            steps0, steps;         // steps of the first pair of operands, of both together
+    int            steps0;                // steps of the first pair of operands (`steps`: of both together)
     int            group_shift, groups, out;
     int64_t        col0;                  // first column of this launch
     const void *   bias, *bias2;          // 16-bit, or null
@@ -109,35 +108,8 @@ struct Slot {
     }
 };
 
-struct Place {
-    int m, n, split, first, steps;
-};
 template <int EPI>
-__device__ __forceinline__ Place place_at(const LNArgs& a, unsigned index) {
-    Place t;
-    unsigned split = 0;
-    if (EPI == LN_OUTER) {               // one worker after the other
-        const unsigned per = unsigned(a.mt) * unsigned(a.nt);
-        split = index / per;
-        index -= split * per;
-    } else if (a.splits > 1) {
-        split = index % unsigned(a.splits);
-        index /= unsigned(a.splits);
-    }
-    const unsigned group_m = unsigned(a.group_m), per_group = group_m * unsigned(a.nt), g = index / per_group, in_group = index - g * per_group;
-    const unsigned rows = min(group_m, unsigned(a.mt) - g * group_m);
-    t.n = int(in_group / rows);
-    t.m = int(g * group_m + in_group - unsigned(t.n) * rows);
-    t.split = int(split);
-    t.first = 0;
-    t.steps = a.steps;
-    if (EPI != LN_OUTER && a.splits > 1) {
-        const int part = (a.steps + a.splits - 1) / a.splits;
-        t.first = int(split) * part;
-        t.steps = min(part, a.steps - t.first);
-    }
-    return t;
-}
+__device__ __forceinline__ Place place_at(const LNArgs& a, unsigned index) { return place_in<EPI == LN_OUTER>(a, index); }
 
 // 32 columns of this thread's row of the accumulators: asked for, there once waited for
 __device__ __forceinline__ void ask32(unsigned taddr, float (&v)[32]) {
@@ -723,6 +695,8 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1) linear_kernel(const LN
             for (unsigned i = pair; ok && i < tiles; i += pairs) {
                 const Place t = place_at<EPI>(a, i);
                 const int y = (2 * t.m + int(rank)) * LN_M;
+                // this CTA's half of the tile's columns; past 2^31, where there are none, it wraps to below 0, where there are none either
+                const int x = int(unsigned(t.n) * unsigned(a.width) + rank * unsigned(a.width / 2));
                 for (int s = 0; s < t.steps; ++s, ++g, r.next(a)) {
                     if (!kb_wait(kb_smem_u32(&sm.empty[r.slot]), r.parity ^ 1u, error)) { ok = false; break; }
                     if (rank == 0) kb_expect_tx(kb_smem_u32(&sm.full[r.slot]), 2 * LN_TILE + unsigned(a.width) * (LN_K * 2));
@@ -738,14 +712,13 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1) linear_kernel(const LN
                         tma_load_pair(da, second ? &map_a1 : &map_a0, k, y, 0, bar);
                     }
                     if (B_MN) {
-                        const int x = t.n * a.width + int(rank) * (a.width / 2);
                         const CUtensorMap* map = second ? &map_b1 : &map_b0;
                         tma_load_pair(db, map, x, k, z, bar);
-                        if (a.width == LN_N) tma_load_pair(db + LN_BLOCK, map, x + 64, k, z, bar);
+                        if (a.width == LN_N) tma_load_pair(db + LN_BLOCK, map, int(unsigned(x) + 64u), k, z, bar);
                     } else if (EPI == LN_GATED) {
                         tma_load_pair(db, rank == 0 ? &map_b0 : &map_b1, k, t.n * (a.width / 2), 0, bar);
                     } else {
-                        tma_load_pair(db, &map_b0, k, t.n * a.width + int(rank) * (a.width / 2), 0, bar);
+                        tma_load_pair(db, &map_b0, k, x, 0, bar);
                     }
                 }
             }
@@ -1153,10 +1126,6 @@ struct Copies {
 struct Maps {
     CUtensorMap a0, b0, a1, b1, out;
 };
-// Row tiles that go round a column tile together: B is read from memory once for each such group of rows of A, which
-// should stay in L2: 32 MB of them.  8192 rows, 4096 x 8192 gated: 785 us in groups of 8, 772 of 16 (32 MB), 785 of 24, 829 of 32;
-// 2048 x 32000: 775 of 8, 755 of 16, 744 of 32 (32 MB).
-int group_rows(int64_t steps) { return int(std::max<int64_t>(8, 1024 / steps)); }
 
 template <typename T, int EPI, int ACT>
 cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t stream) {
@@ -1172,7 +1141,7 @@ cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t str
     }
     // (an outer product's tiles go along its rows, which are then written whole: 11 x 128 tokens, 32000 x 1024, fp32 rows, whole backward
     // pass without dx 370 us, row tiles in groups of 64 396)
-    a.group_m = EPI == LN_OUTER ? 1 : group_rows(a.steps);
+    a.group_m = EPI == LN_OUTER ? 1 : group_rows(a.steps, a.mt);
     a.slot_bytes = LN_TILE + a.width * LN_K;
     a.ring = std::min(LN_RING_MOST, LN_RING_BYTES / a.slot_bytes);
     const int64_t tiles = int64_t(a.mt) * a.nt * a.splits;

@@ -39,3 +39,25 @@ def test_a_large_coefficient_stays_with_its_worker(pkg, workers, tokens, hidden,
         if grads == "f32":
             own = [c for c in range(want.shape[1]) if c < vocab * hidden or bias_at <= c < bias_at + vocab]
             assert torch.equal(got[-1, own], want[-1, own] * power)
+
+
+# ---- so many columns that a group of row tiles times them passes 32 bits ------------------------------
+def test_scores_of_two_to_the_thirty_columns(pkg):
+    """17 rows with one step of the contraction, 2^22 column tiles and more.  Logits 0 but for some columns."""
+    rows, vocab = 17, (1 << 30) + 300
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GB")
+    w = torch.zeros(vocab, 8, dtype=torch.bfloat16, device=DEV)
+    at = torch.tensor([0, 255, 256, (1 << 29) + 77, (1 << 30) - 1, 1 << 30, vocab - 2, vocab - 1], device=DEV)
+    w[at, 0] = -torch.arange(1, 9, device=DEV).bfloat16()
+    x = torch.zeros(rows, 8, dtype=torch.bfloat16, device=DEV)
+    x[:, 0] = torch.linspace(0.25, 1.25, rows, device=DEV).bfloat16()
+    t = torch.cat([at, at[:4] + 9, at[:5]])
+    r = pkg.gar_linear_logprobs(x, w, t)
+    z = -x[:, :1].double() * torch.arange(1, 9, device=DEV)
+    lse = torch.log((vocab - 8) + torch.exp(z).sum(1))
+    picked = torch.cat([z.diagonal(), torch.zeros(4, dtype=torch.float64, device=DEV), z[12:, :5].diagonal()])
+    # whole numbers of columns but for eight: the sums are exact to a few roundings
+    close(r.lse, lse, 1e-5, "lse")
+    close(r.logprobs, picked - lse, 1e-5, "logprobs")
