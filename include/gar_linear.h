@@ -76,7 +76,7 @@ size_t gar_linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t* p
  * that small gradients do not underflow: dz have all their bits down to 2^-28 of that |a|, what is below 2^-39 of it is lost.
  *   - A row without a target, or with a = 0, gets dx 0 and nothing it holds, NaN included, reaches a weight gradient.
  *   - No tokens: weight and bias gradients of zeros.
- *   - A row masked throughout has gradient 0; in any other row a target >= vocab gives NaN, in dx and
+ *   - The same holds for a row masked throughout, lse = -inf, whatever its coefficient and its target; in any other row a target >= vocab gives NaN, in dx and
  *     in its worker's gradients; no row reaches another worker's.
  * 1 <= workers <= GAR_MAX_N; workers * tokens < 2^30.
  */

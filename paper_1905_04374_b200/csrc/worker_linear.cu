@@ -435,8 +435,6 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
     const float lse = in.lse, lo = in.lo;
     const int64_t t64 = in.target - a.col0 - first;
     const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
-    // a masked row: gradient 0 whatever comes in
-    if (lse == -CUDART_INF_F) coef = 0.f;
     const bool nothing = coef == 0.f;
     const f32x2 minus = pack2(-lse, -lse), unit = pack2(kLog2e, kLog2e), minus_lo = pack2(-lo * kLog2e, -lo * kLog2e), by = pack2(-coef, -coef);
     over_logits(w.src + unsigned(mine.from), a.twice, cols, [&](float (&v)[32], int at) {
@@ -899,7 +897,8 @@ __global__ void __launch_bounds__(256) join_scores_kernel(const float2* parts, c
 
 // Rows of 16-bit elements copied to rows that start on 16 bytes, eight elements per thread and turn; up to four matrices,
 // one per blockIdx.y.  A job with targets is the rows of a head: those whose coefficient is 0 are copied as zeros, and the coefficients
-// (the gradient at a row's log probability; 0 without a target, NaN for a target outside the vocabulary) are written.  Where the
+// (the gradient at a row's log probability; 0 without a target and in a row masked throughout, whatever comes in; NaN for a target
+// outside the vocabulary) are written.  Where the
 // largest one's magnitude is asked for, the blocks behind the jobs find it, a worker each: one for all workers would let one
 // worker's coefficients push the others' dz below binary16's range.
 struct CopyJob {
@@ -912,7 +911,7 @@ struct CopyArgs {
     CopyJob        job[4];
     int            jobs;
     const int64_t* targets;                // of the first job; or null
-    const float*   grad;
+    const float *  grad, *lse;
     int64_t        vocab, tokens;
     int            workers;
     float*         coef;
@@ -920,7 +919,7 @@ struct CopyArgs {
 };
 __device__ __forceinline__ float coefficient(const CopyArgs& a, int64_t row) {
     const int64_t t = a.targets[row];
-    return t < 0 ? 0.f : t >= a.vocab ? CUDART_NAN_F : a.grad[row];
+    return t < 0 || a.lse[row] == -CUDART_INF_F ? 0.f : t >= a.vocab ? CUDART_NAN_F : a.grad[row];
 }
 __global__ void __launch_bounds__(256) copy_rows_kernel(const CopyArgs a) {
     grid_dependency();
@@ -1492,6 +1491,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
         copies.add(plan.w);
         copies.a.targets = p.targets;
         copies.a.grad = p.grad_logprobs;
+        copies.a.lse = p.lse;
         copies.a.vocab = p.vocab;
         copies.a.tokens = p.tokens;
         copies.a.workers = p.workers;

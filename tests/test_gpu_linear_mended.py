@@ -61,3 +61,26 @@ def test_scores_of_two_to_the_thirty_columns(pkg):
     # whole numbers of columns but for eight: the sums are exact to a few roundings
     close(r.lse, lse, 1e-5, "lse")
     close(r.logprobs, picked - lse, 1e-5, "logprobs")
+
+
+# ---- rows masked throughout ------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_a_masked_row_counts_for_nothing(pkg, dtype):
+    """A row whose logits are all -inf (an infinity in x before a column of negative weights) has gradient 0: neither its coefficient nor
+    what it holds reaches the other rows of its worker."""
+    rows, hidden, vocab = 50, 64, 256
+    x, w, _, t = head(rows, hidden, vocab, dtype, False, 22)
+    t = t.clamp_min(0)
+    w[:, 5] = -w[:, 5].abs() - 0.25
+    a = -torch.rand(rows, generator=gen(9), device=DEV) - 0.5
+    a[7] = 0.0
+    want_dx, want = check_head_gradient(pkg, x, w, None, t, a, 1, "f32")
+    x[7, 5], a[7] = math.inf, 2.0 ** 60
+    saved = pkg.gar_linear_logprobs(x, w, t)
+    assert float(saved.lse[7]) == -math.inf and float(saved.logprobs[7]) == -math.inf
+    got = torch.empty_like(want).fill_(7.0)
+    dx = pkg.gar_linear_logprobs_backward(x, w, saved, t, a, grads=got)
+    assert torch.equal(got, want) and torch.equal(dx, want_dx)
+    t[7] = vocab + 3                                         # not even a target outside the vocabulary
+    dx = pkg.gar_linear_logprobs_backward(x, w, saved, t, a, grads=got)
+    assert torch.equal(got, want) and torch.equal(dx, want_dx)
