@@ -88,7 +88,7 @@ template <int EPI> struct __align__(1024) LNSmem {
     typedef Shape<EPI> S;
     uint8_t  ring[LN_RING_BYTES];                         // slots: 128 rows of A, half the tile's rows of B
     uint8_t  out[S::STORE_WARPS][S::PIECE];               // a store warp's piece: 32 rows of 128 bytes (LN_DLOGITS: 64)
-    float    add[S::STORE_WARPS][S::BIASES];              // a warp's biases, -inf for columns that do not exist
+    float    add[S::STORE_WARPS][S::BIASES];              // a warp's biases
     float2   part[EPI == LN_SCORES ? 2 : 1][4][EPI == LN_SCORES ? LN_M : 1];        // the groups' maxima and sums, by half of tensor memory
     unsigned long long part_full[2];                      // they are there
     unsigned long long empty[LN_RING_MOST], acc_full[2];  // the slots are read; the accumulators are complete
@@ -280,15 +280,14 @@ __device__ __forceinline__ void store_plain32(unsigned stage, int lane, float* d
     }
 }
 
-// N columns' biases from column c0 on, `fill` where there is no column
+// N columns' biases from column c0 on, 0 where there is no column
 template <typename T, int N>
-__device__ __forceinline__ void fetch_biases(const void* bias, int64_t c0, int64_t cols, float fill, float* add, int lane) {
+__device__ __forceinline__ void fetch_biases(const void* bias, int64_t c0, int64_t cols, float* add, int lane) {
     float v[N / 32];
 #pragma unroll
     for (int k = 0; k < N / 32; ++k) {
         const int64_t c = c0 + 32 * k + lane;
-        v[k] = c >= cols ? fill : 0.f;
-        if (bias && c < cols) v[k] = Elem<T>::widen(static_cast<const T*>(bias)[c]);
+        v[k] = bias && c < cols ? Elem<T>::widen(static_cast<const T*>(bias)[c]) : 0.f;
     }
 #pragma unroll
     for (int k = 0; k < N / 32; ++k) add[32 * k + lane] = v[k];
@@ -335,14 +334,14 @@ __device__ __forceinline__ void fetch_tile_biases(const LNArgs& a, const Place& 
     if (w.row0 >= a.rows) return;
     if (EPI == LN_GATED && (a.bias || a.bias2)) {
         const int64_t c0 = int64_t(t.n) * (a.width / 2);
-        fetch_biases<T, LN_HALF>(a.bias, c0, a.cols, 0.f, w.add, w.lane);
-        fetch_biases<T, LN_HALF>(a.bias2, c0, a.cols, 0.f, w.add + LN_HALF, w.lane);
+        fetch_biases<T, LN_HALF>(a.bias, c0, a.cols, w.add, w.lane);
+        fetch_biases<T, LN_HALF>(a.bias2, c0, a.cols, w.add + LN_HALF, w.lane);
     }
     if (EPI == LN_SCORES || EPI == LN_DLOGITS) {
         const int64_t c0 = int64_t(t.n) * a.width, left = a.cols - c0;
-        if (a.bias || (EPI == LN_SCORES && left < a.width)) {
+        if (a.bias) {
             const Columns mine = Columns::of<4, 32>(left < a.width ? int(left) : a.width, w.group);
-            fetch_biases<T, 64>(a.bias, a.col0 + c0 + mine.from, a.col0 + a.cols, -CUDART_INF_F, w.add, w.lane);
+            fetch_biases<T, 64>(a.bias, a.col0 + c0 + mine.from, a.col0 + a.cols, w.add, w.lane);
         }
     }
 }
@@ -353,13 +352,17 @@ __device__ __forceinline__ float2 scores_tile(const LNArgs& a, const Place& t, c
     const int64_t left = a.cols - c0;
     const Columns mine = Columns::of<4, 32>(left < a.width ? int(left) : a.width, w.group);
     const int cols = mine.to - mine.from;
-    const bool adds = a.bias || left < a.width;
+    const bool adds = a.bias != nullptr;
     const int64_t t64 = in.target - a.col0 - c0 - mine.from;
     const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
     float m = -CUDART_INF_F, s = 0.f;
     if (cols > 0 && w.row0 < a.rows)
         over_logits(w.src + unsigned(mine.from), a.twice, cols, [&](float (&v)[32], int at) {
             logits32(v, a.whole, adds, w.add + at);
+            if (at + 32 > cols) {                        // columns that do not exist (0 times an infinity of the row is NaN there)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = at + j < cols ? v[j] : -CUDART_INF_F;
+            }
             if (__any_sync(0xffffffffu, target >= at && target < at + 32)) {
                 float z = 0.f;
 #pragma unroll

@@ -84,3 +84,19 @@ def test_a_masked_row_counts_for_nothing(pkg, dtype):
     t[7] = vocab + 3                                         # not even a target outside the vocabulary
     dx = pkg.gar_linear_logprobs_backward(x, w, saved, t, a, grads=got)
     assert torch.equal(got, want) and torch.equal(dx, want_dx)
+
+
+# ---- infinities next to columns that do not exist ----------------------------------------------------
+@pytest.mark.parametrize("rows", [3, 40])
+@pytest.mark.parametrize("vocab", [1, 31, 200, 256, 999])
+def test_a_row_of_minus_infinity_at_every_width(pkg, rows, vocab):
+    """All of a row's logits are -inf: so are lse and log probability, whether or not the last tile of columns is full."""
+    x, w, b, t = head(rows, 72, vocab, "bf16", True, 23)
+    t = t.clamp_min(0)
+    w[:, 5] = -w[:, 5].abs() - 0.25
+    x[1, 5] = math.inf
+    r = pkg.gar_linear_logprobs(x, w, t, bias=b)
+    logprobs, lse, _, d = scores_64(x, w, b, t)
+    assert float(lse[1]) == -math.inf and float(logprobs[1]) == -math.inf
+    close(r.lse, lse, 2 * d + 2e-5, "lse")
+    close(r.logprobs, logprobs, 2 * d + 2e-5, "logprobs")
