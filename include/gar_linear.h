@@ -16,9 +16,11 @@
  * The matrix products are those of 16-bit elements (GAR_BF16 or GAR_F16; GAR_F32 is
  * GAR_ERR_UNSUPPORTED except for dropout), exact, summed in fp32 on the tensor
  * cores, which truncate where they add: a sum over k terms is short by some
- * 1e-9 k of itself (2.8e-9 k where it grows steadily); no sum has more than
- * 2^15 terms before it is added, rounded, to the others, but for sums over
- * `hidden` and `inner`.  Everything after a product is fp32, each output rounded once.
+ * 1e-9 k of itself, where it grows steadily by 1.4e-9 k (bfloat16) to 6e-9 k (binary16), where nothing is cut off by nothing;
+ * at the very most by 4e-8 k (up to 16 rows 7e-8 k) of the terms' magnitudes.
+ * Logits are summed in chunks of 512 terms (up to 640 in one), the chunks' sums added in fp32, rounded; the sums over `hidden`
+ * and `inner` that end in 16 bits or in checkpoints are whole; other sums have 2^15 terms at most before they are added, rounded, to
+ * the rest.  Everything after a product is fp32, each output rounded once.
  *
  * Workspaces: 256-byte aligned, of at least the bytes the sizes call returns
  * for the same parameters (host, pure; 0 on invalid ones).  Nothing in them

@@ -20,6 +20,7 @@ namespace {
 
 constexpr int FW_WARPS = 8, FW_THREADS = 32 * FW_WARPS;
 constexpr int FW_UNIT = 128;                          // elements of the contraction a warp takes at a time: 256 bytes of a row
+constexpr int FW_CHUNK = 512 / FW_UNIT;               // units of a warp that its accumulators take: the tensor core truncates what it adds (worker_linear.cu)
 constexpr int FW_SMEM = 100 << 10;                    // x in shared memory: two CTAs on an SM
 
 struct FewArgs {
@@ -31,7 +32,6 @@ struct FewArgs {
     int            rows, units, pitch;    // of x; of FW_UNIT; bytes between rows of x in shared memory
     int            split;                 // warps that share a contraction: 1, 2, 4, 8
     int64_t        hidden, wide, tiles;   // wide: weight rows (of each projection)
-    float          whole;
     const int64_t* targets;
     float2*        parts;                 // [rows][gridDim.x]
     float*         target_z;
@@ -125,11 +125,21 @@ __global__ void __launch_bounds__(FW_THREADS, 2) few_rows_kernel(const FewArgs a
 
     for (int64_t first = int64_t(blockIdx.x) * sets; first < a.tiles; first += int64_t(gridDim.x) * sets) {
         const int64_t tile = first + set;
-        float acc[NT][4];
+        float acc[NT][4], sum[NT][4];                  // of a chunk; of the chunks, rounded where they are added
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) acc[n][c] = 0.f;
+            for (int c = 0; c < 4; ++c) acc[n][c] = sum[n][c] = 0.f;
+        auto join = [&]() {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    sum[n][c] += acc[n][c];
+                    acc[n][c] = 0.f;
+                }
+        };
+        int left = FW_CHUNK;
         for (int u = part; u < a.units; u += a.split) {
             uint4 w[4][2];
 #pragma unroll
@@ -144,7 +154,12 @@ __global__ void __launch_bounds__(FW_THREADS, 2) few_rows_kernel(const FewArgs a
                     mma_16x8x16<T>(acc[n], w[c][0].x, w[c][1].x, w[c][0].y, w[c][1].y, b.x, b.y);
                     mma_16x8x16<T>(acc[n], w[c][0].z, w[c][1].z, w[c][0].w, w[c][1].w, b.z, b.w);
                 }
+            if (--left == 0) {
+                join();
+                left = FW_CHUNK;
+            }
         }
+        join();
         // the next tile's first unit is on its way while this one is finished
         const bool mine0 = live0, mine1 = live1;
         const int64_t v0 = r0, v1 = r1;
@@ -154,14 +169,14 @@ __global__ void __launch_bounds__(FW_THREADS, 2) few_rows_kernel(const FewArgs a
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) joined[warp][n][c][lane] = acc[n][c];
+                for (int c = 0; c < 4; ++c) joined[warp][n][c][lane] = sum[n][c];
             __syncthreads();
             if (part == 0)
                 for (int k = 1; k < a.split; ++k)
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) acc[n][c] += joined[warp + k][n][c][lane];
+                        for (int c = 0; c < 4; ++c) sum[n][c] += joined[warp + k][n][c][lane];
         }
         if (part != 0 || tile >= a.tiles) continue;
         if constexpr (GATED) {
@@ -169,13 +184,13 @@ __global__ void __launch_bounds__(FW_THREADS, 2) few_rows_kernel(const FewArgs a
             const float bg = a.b0 ? Elem<T>::widen(static_cast<const T*>(a.b0)[v0]) : 0.f, bu = a.b1 ? Elem<T>::widen(static_cast<const T*>(a.b1)[v0]) : 0.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float x[8] = {acc[n][0] + bg, acc[n][1] + bg, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                const float x[8] = {sum[n][0] + bg, sum[n][1] + bg, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                 float y[8];
                 act8<ACT>(x, y);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const int r = n * 8 + 2 * t + c;
-                    if (r < a.rows) static_cast<T*>(a.y)[r * a.ldy + v0] = Elem<T>::narrow(y[c] * (acc[n][2 + c] + bu));
+                    if (r < a.rows) static_cast<T*>(a.y)[r * a.ldy + v0] = Elem<T>::narrow(y[c] * (sum[n][2 + c] + bu));
                 }
             }
         } else {
@@ -188,7 +203,7 @@ __global__ void __launch_bounds__(FW_THREADS, 2) few_rows_kernel(const FewArgs a
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const float z = fmaf(acc[n][2 * half + c], a.whole, bias);
+                        const float z = sum[n][2 * half + c] + bias;
                         if (target[n][c] == v) a.target_z[n * 8 + 2 * t + c] = z;
                         const float higher = fmaxf(m[n][c], z);
                         const float base = higher == -CUDART_INF_F ? 0.f : higher;
@@ -280,7 +295,7 @@ bool few_rows_applies(int64_t rows, int64_t hidden, const void* w0, int64_t ld0,
 }
 int64_t few_scores_parts(int sm_count) { return most_blocks(sm_count); }
 
-cudaError_t launch_few_scores(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw, float lost, float2* parts, float* target_z, int* count,
+cudaError_t launch_few_scores(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw, float2* parts, float* target_z, int* count,
                               int sm_count) {
     FewArgs a{};
     const unsigned blocks = plan(a, int(p.rows), p.hidden, p.vocab, (p.vocab + 15) / 16, sm_count);
@@ -289,7 +304,6 @@ cudaError_t launch_few_scores(const gar_linear_logprobs_params_t& p, int64_t ldx
     a.w0 = p.weight;
     a.ld0 = ldw;
     a.b0 = p.bias;
-    a.whole = 1.f + lost * float(p.hidden) / float(a.split);        // of each warp's part of the contraction
     a.targets = p.logprobs ? p.targets : nullptr;
     a.parts = parts;
     a.target_z = target_z;

@@ -9,16 +9,21 @@
 //                  B lie with the contraction along their rows (K-major), or across them (MN-major: the
 //                  gradient at the inputs, dz W, reads W as it lies, the gradient at the weights, dz^T x, both)
 //   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
-//   store warps    groups of four, each with its share of a tile's columns, while the next tile's products run
+//   store warps    groups of four, each with its share of a tile's columns, while the next products run
 //                  into the other half of tensor memory; a thread has one row, 32 columns at a time.  Two groups, or four
 //                  where a column takes an exponential (struct Shape)
 // and four epilogues (LN_SUM's and LN_OUTER's are one; enum Epilogue).  A thread owning a row makes the softmax's statistics, the group
 // maxima of the checkpoints and the row's target its own affair.
 // Tiles are as wide as the rule in width_for makes them, 256 columns at most.
 //
-// The tensor core truncates what it adds to an accumulator: sums over k terms come out short by 1.0e-9 k of themselves
-// (operands of random signs; measured from k = 512 to 4096: lse off by -2.9e-6, -5.9e-6, -1.2e-5, -2.5e-5, all rows alike
-// to a tenth of that).  The logits, whose log probabilities are fp32 results, are multiplied by 1 + 1e-9 k.
+// The tensor core truncates what it adds: a product to a multiple of 2^-25 of the largest magnitude among the accumulator and the
+// products it is added with, the accumulator to 24 bits (measured with single terms next to 1; mma.sync 2^-24).  Sums over k terms come out
+// short by 1.0e-9 k of themselves (random signs; from k = 512 to 4096 lse off by -2.9e-6, -5.9e-6, -1.2e-5, -2.5e-5), by
+// 1.4e-9 k (bf16) to 6e-9 k (binary16, whose products have more bits to lose) where the terms have one sign, by nothing where they are few.
+// The logits, whose log probabilities are fp32 results, are therefore summed in chunks of 512 terms (up to 640 in one): the halves of
+// tensor memory take a chunk each in turn, and the store warps add them up, rounded, in registers (linear_kernel's LONG).
+// lse is then 2.2e-7 (binary16 3.0e-7) off, relative, from 512 to 16384 terms (5000 columns, random signs; in one accumulator
+// 1.9e-6 at 4096), at the same speed.
 //
 // Every wait is bounded (mbar.cuh); a pair whose wait gave up fills its tiles with NaN.
 #include <algorithm>
@@ -44,7 +49,11 @@ constexpr int LN_BLOCK = 64 * 128;                    // bytes of 64 x 64 elemen
 constexpr int LN_COPY_WARP = 0, LN_MMA_WARP = 1, LN_ALLOC_WARP = 2;
 constexpr int LN_STORE_WARP0 = 4;
 constexpr int LN_PAIRS = 74;                          // pairs of SMs, for the rules that cut work into parts and tiles
-constexpr float LN_SHORT = 1.0e-9f;                   // of a sum, lost per term
+// Steps of the contraction that a logit's accumulator takes where there are several (LONG), and up to which there is one.  A second chunk
+// of a few steps would be over before the epilogue of 128 columns a thread: 4096 x 32000, scores and gradient with dx, 576 terms: 101 to 112 and
+// 310 us in one accumulator, 138 and 338 in two; 640: 122 and 333, 142 and 346; 768: 142 and 369, 148 and 364; 1024: 190 and 457, 182 and 457.
+// Chunks of 256 terms halve the loss and hold the products up: 8192 x 32000, 2048: 840 us instead of 765.
+constexpr int LN_CHUNK = 8, LN_ONE = 10;
 
 // What becomes of a tile.
 //   LN_SCORES   z: maximum and sum of exponentials of each row's 256 columns, and the target's z
@@ -59,8 +68,6 @@ struct LNArgs : Tiling {
     int64_t        rows, cols;            // of the result (LN_SCORES, LN_DLOGITS: columns from col0 on)
     int            width;                 // columns of a tile (LN_GATED: g's and u's together)
     int            ring, slot_bytes;      // steps in flight, what one takes in shared memory
-    float          whole;                 // logits: 1 + what the tensor core's sums are short by
-    int            twice;                 // logits: each half of the contraction has a half of tensor memory (a pair has one tile)
     int            steps0;                // steps of the first pair of operands (`steps`: of both together)
     int            group_shift, groups, out;
     int64_t        col0;                  // first column of this launch
@@ -78,18 +85,19 @@ struct LNArgs : Tiling {
 
 // Store warps, their staged pieces of a result (32 rows) and the biases they keep.  The logits' epilogues are bound by latency where the
 // contraction is short (two warps on a scheduler issue in 37 % of the cycles): four groups, of fewer registers.  4096 x 32000, 128: 82.6 us,
-// with four groups 73.0; the gradient 274 and 258.
-template <int EPI> struct Shape {
+// with four groups 73.0; the gradient 274 and 258.  LONG: a thread keeps the sums of its columns, 128 of them in two groups.
+template <int EPI, bool LONG> struct Shape {
     static constexpr bool LOGITS = EPI == LN_SCORES || EPI == LN_DLOGITS;
-    static constexpr int GROUPS = LOGITS ? 4 : 2, STORE_WARPS = 4 * GROUPS, THREADS = 32 * (LN_STORE_WARP0 + STORE_WARPS);
-    static constexpr int PIECE = EPI == LN_SCORES ? 16 : EPI == LN_DLOGITS ? 32 * 64 : 32 * 128, BIASES = LOGITS ? 64 : LN_N;
+    static_assert(LOGITS || !LONG, "chunks are the logits'");
+    static constexpr int GROUPS = LOGITS && !LONG ? 4 : 2, STORE_WARPS = 4 * GROUPS, THREADS = 32 * (LN_STORE_WARP0 + STORE_WARPS);
+    static constexpr int PIECE = EPI == LN_SCORES ? 16 : EPI == LN_DLOGITS ? 32 * 64 : 32 * 128, BIASES = LOGITS ? LN_N / GROUPS : LN_N;
 };
-template <int EPI> struct __align__(1024) LNSmem {
-    typedef Shape<EPI> S;
+template <int EPI, bool LONG> struct __align__(1024) LNSmem {
+    typedef Shape<EPI, LONG> S;
     uint8_t  ring[LN_RING_BYTES];                         // slots: 128 rows of A, half the tile's rows of B
     uint8_t  out[S::STORE_WARPS][S::PIECE];               // a store warp's piece: 32 rows of 128 bytes (LN_DLOGITS: 64)
     float    add[S::STORE_WARPS][S::BIASES];              // a warp's biases
-    float2   part[EPI == LN_SCORES ? 2 : 1][4][EPI == LN_SCORES ? LN_M : 1];        // the groups' maxima and sums, by half of tensor memory
+    float2   part[EPI == LN_SCORES ? 2 : 1][S::GROUPS][EPI == LN_SCORES ? LN_M : 1]; // the groups' maxima and sums, of two tiles in turn
     unsigned long long part_full[2];                      // they are there
     unsigned long long empty[LN_RING_MOST], acc_full[2];  // the slots are read; the accumulators are complete
     unsigned long long full[LN_RING_MOST], acc_empty[2];  // the leading CTA's are used, for both
@@ -144,63 +152,68 @@ __device__ __forceinline__ void over_columns(unsigned src, int cols, F f) {
         f(v1, c0 + 32);
     }
 }
-// The same for the logits' epilogues, one after the other (four warps of a scheduler take turns); twice: the sum of both halves of
-// tensor memory.
 __device__ __forceinline__ void ask16(unsigned taddr, float (&v)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                  : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
                    "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
                  : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void wait16(float (&a)[16], float (&b)[16]) {
+__device__ __forceinline__ void wait16(float (&a)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+f"(a[0]), "+f"(a[1]), "+f"(a[2]), "+f"(a[3]), "+f"(a[4]), "+f"(a[5]), "+f"(a[6]), "+f"(a[7]), "+f"(a[8]), "+f"(a[9]),
-                   "+f"(a[10]), "+f"(a[11]), "+f"(a[12]), "+f"(a[13]), "+f"(a[14]), "+f"(a[15]), "+f"(b[0]), "+f"(b[1]), "+f"(b[2]),
-                   "+f"(b[3]), "+f"(b[4]), "+f"(b[5]), "+f"(b[6]), "+f"(b[7]), "+f"(b[8]), "+f"(b[9]), "+f"(b[10]), "+f"(b[11]),
-                   "+f"(b[12]), "+f"(b[13]), "+f"(b[14]), "+f"(b[15]) :: "memory");
+                   "+f"(a[10]), "+f"(a[11]), "+f"(a[12]), "+f"(a[13]), "+f"(a[14]), "+f"(a[15]) :: "memory");
 }
-template <typename F>
-__device__ __forceinline__ void over_logits(unsigned src, bool twice, int cols, F f) {
+// What a thread has of its row's logits: its columns of the accumulators, 32 at a time (four warps of a scheduler take turns);
+// or (LONG) the sums of the chunks so far, all its columns of them.
+template <bool LONG> struct Logits {
+    unsigned src;
+    __device__ __forceinline__ void chunk(unsigned from, int, bool) { src = from; }
+    template <typename F> __device__ __forceinline__ void each(int cols, F f) {
 #pragma unroll 1
-    for (int c0 = 0; c0 < cols; c0 += 32) {
-        float v[32];
-        if (!twice) {
+        for (int c0 = 0; c0 < cols; c0 += 32) {
+            float v[32];
             ask32(src + unsigned(c0), v);
             wait32(v);
-        } else {
+            f(v, c0);
+        }
+    }
+};
+template <> struct Logits<true> {
+    float sum[4][32];
+    // a chunk's accumulators, from `from` on (cols is the warp's own number)
+    __device__ __forceinline__ void chunk(unsigned from, int cols, bool first) {
 #pragma unroll
-            for (int k = 0; k < 32; k += 16) {
-                float a[16], b[16];
-                ask16(src + unsigned(c0 + k), a);
-                ask16(src + unsigned(c0 + k + LN_N), b);
-                wait16(a, b);
+        for (int k = 0; k < 4; ++k) {
+            if (32 * k >= cols) break;
+            if (first) {
+                ask32(from + unsigned(32 * k), sum[k]);
+                wait32(sum[k]);
+                continue;
+            }
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[k + j] = a[j] + b[j];
+            for (int h = 0; h < 32; h += 16) {
+                float v[16];
+                ask16(from + unsigned(32 * k + h), v);
+                wait16(v);
+#pragma unroll
+                for (int j = 0; j < 16; j += 2) unpack2(add2(pack2(sum[k][h + j], sum[k][h + j + 1]), pack2(v[j], v[j + 1])), sum[k][h + j], sum[k][h + j + 1]);
             }
         }
-        f(v, c0);
     }
-}
+    template <typename F> __device__ __forceinline__ void each(int cols, F f) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (32 * k >= cols) break;
+            f(sum[k], 32 * k);
+        }
+    }
+};
 __device__ __forceinline__ void add32(float (&v)[32], const float* add) {
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
         const float4 b = *reinterpret_cast<const float4*>(add + j);
-        v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
-    }
-}
-// the logits of 32 columns: the sums made whole, the biases added
-__device__ __forceinline__ void logits32(float (&v)[32], float whole, bool adds, const float* add) {
-    const f32x2 by = pack2(whole, whole);
-    if (adds) {
-#pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-            const float4 b = *reinterpret_cast<const float4*>(add + j);
-            unpack2(fma2(pack2(v[j], v[j + 1]), by, pack2(b.x, b.y)), v[j], v[j + 1]);
-            unpack2(fma2(pack2(v[j + 2], v[j + 3]), by, pack2(b.z, b.w)), v[j + 2], v[j + 3]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; j += 2) unpack2(mul2(pack2(v[j], v[j + 1]), by), v[j], v[j + 1]);
+        unpack2(add2(pack2(v[j], v[j + 1]), pack2(b.x, b.y)), v[j], v[j + 1]);
+        unpack2(add2(pack2(v[j + 2], v[j + 3]), pack2(b.z, b.w)), v[j + 2], v[j + 3]);
     }
 }
 
@@ -329,7 +342,7 @@ __device__ __forceinline__ RowInputs ask_inputs(const LNArgs& a, const Place& t,
     return in;
 }
 // The biases of a warp's columns of a tile, into its piece of shared memory, while the tile's products still run.
-template <typename T, int EPI>
+template <typename T, int EPI, bool LONG>
 __device__ __forceinline__ void fetch_tile_biases(const LNArgs& a, const Place& t, const Warp& w) {
     if (w.row0 >= a.rows) return;
     if (EPI == LN_GATED && (a.bias || a.bias2)) {
@@ -340,25 +353,32 @@ __device__ __forceinline__ void fetch_tile_biases(const LNArgs& a, const Place& 
     if (EPI == LN_SCORES || EPI == LN_DLOGITS) {
         const int64_t c0 = int64_t(t.n) * a.width, left = a.cols - c0;
         if (a.bias) {
-            const Columns mine = Columns::of<4, 32>(left < a.width ? int(left) : a.width, w.group);
-            fetch_biases<T, 64>(a.bias, a.col0 + c0 + mine.from, a.col0 + a.cols, w.add, w.lane);
+            typedef Shape<EPI, LONG> S;
+            const Columns mine = Columns::of<S::GROUPS, 32>(left < a.width ? int(left) : a.width, w.group);
+            fetch_biases<T, S::BIASES>(a.bias, a.col0 + c0 + mine.from, a.col0 + a.cols, w.add, w.lane);
         }
     }
 }
 
+// A group's columns of a tile of logits
+template <int GROUPS>
+__device__ __forceinline__ Columns logits_columns(const LNArgs& a, const Place& t, int group) {
+    const int64_t left = a.cols - int64_t(t.n) * a.width;
+    return Columns::of<GROUPS, 32>(left < a.width ? int(left) : a.width, group);
+}
+
 // The group's maximum and sum of this thread's row
-__device__ __forceinline__ float2 scores_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in) {
+template <bool LONG>
+__device__ __forceinline__ float2 scores_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in, const Columns& mine, Logits<LONG>& logits) {
     const int64_t c0 = int64_t(t.n) * a.width, row = w.row0 + w.lane;
-    const int64_t left = a.cols - c0;
-    const Columns mine = Columns::of<4, 32>(left < a.width ? int(left) : a.width, w.group);
     const int cols = mine.to - mine.from;
     const bool adds = a.bias != nullptr;
     const int64_t t64 = in.target - a.col0 - c0 - mine.from;
     const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
     float m = -CUDART_INF_F, s = 0.f;
     if (cols > 0 && w.row0 < a.rows)
-        over_logits(w.src + unsigned(mine.from), a.twice, cols, [&](float (&v)[32], int at) {
-            logits32(v, a.whole, adds, w.add + at);
+        logits.each(cols, [&](float (&v)[32], int at) {
+            if (adds) add32(v, w.add + at);
             if (at + 32 > cols) {                        // columns that do not exist (0 times an infinity of the row is NaN there)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = at + j < cols ? v[j] : -CUDART_INF_F;
@@ -396,12 +416,15 @@ __device__ __forceinline__ float2 scores_tile(const LNArgs& a, const Place& t, c
     return make_float2(m, s);
 }
 // The groups' parts of a row as one
-__device__ __forceinline__ float2 join4(const float2 (&p)[4]) {
-    const float m = fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x));
+template <int GROUPS>
+__device__ __forceinline__ float2 join_groups(const float2 (&p)[GROUPS][LN_M], int row) {
+    float m = p[0][row].x;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, p[k][row].x);
     const float base = m == -CUDART_INF_F ? 0.f : m;
     float s = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) s += p[k].y * ex2((p[k].x - base) * kLog2e);      // a part without entries is -inf, 0
+    for (int k = 0; k < GROUPS; ++k) s += p[k][row].y * ex2((p[k][row].x - base) * kLog2e);      // a part without entries is -inf, 0
     return make_float2(m, s);
 }
 
@@ -424,14 +447,12 @@ __device__ __forceinline__ void put_piece(const LNArgs& a, const Warp& w, const 
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in, const CUtensorMap* map) {
-    const int64_t c0 = int64_t(t.n) * a.width;
-    const int64_t left = a.cols - c0;
-    const Columns mine = Columns::of<4, 32>(left < a.width ? int(left) : a.width, w.group);
+template <typename T, bool LONG>
+__device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, const Warp& w, const RowInputs& in, const Columns& mine, Logits<LONG>& logits,
+                                             const CUtensorMap* map) {
     const int cols = mine.to - mine.from;
     if (w.row0 >= a.rows || cols <= 0) return;
-    const int64_t first = c0 + mine.from;
+    const int64_t first = int64_t(t.n) * a.width + mine.from;
     const bool adds = a.bias != nullptr;
     float coef = in.coef;
     if (a.top && w.row0 + w.lane < a.rows) coef *= power_for(a.top[unsigned(w.row0 + w.lane) / a.tokens], false);
@@ -440,8 +461,8 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
     const int target = in.target >= 0 && t64 >= 0 && t64 < cols ? int(t64) : -1;
     const bool nothing = coef == 0.f;
     const f32x2 minus = pack2(-lse, -lse), unit = pack2(kLog2e, kLog2e), minus_lo = pack2(-lo * kLog2e, -lo * kLog2e), by = pack2(-coef, -coef);
-    over_logits(w.src + unsigned(mine.from), a.twice, cols, [&](float (&v)[32], int at) {
-        logits32(v, a.whole, adds, w.add + at);
+    logits.each(cols, [&](float (&v)[32], int at) {
+        if (adds) add32(v, w.add + at);
 #pragma unroll
         for (int j = 0; j < 32; j += 2) {
             float e0, e1;
@@ -644,14 +665,15 @@ __device__ __forceinline__ void gated_tile(const LNArgs& a, const Place& t, cons
     put_piece(a, w, map, first, cols, 0);
 }
 
-template <typename T, int EPI, int ACT>
-__global__ void __launch_bounds__(Shape<EPI>::THREADS, 1) linear_kernel(const LNArgs a, const __grid_constant__ CUtensorMap map_a0,
+template <typename T, int EPI, int ACT, bool LONG>
+__global__ void __launch_bounds__(Shape<EPI, LONG>::THREADS, 1) linear_kernel(const LNArgs a, const __grid_constant__ CUtensorMap map_a0,
                                                               const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_a1,
                                                               const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_out) {
     constexpr bool A_MN = EPI == LN_OUTER, B_MN = EPI == LN_SUM || EPI == LN_OUTER;
     extern __shared__ uint8_t raw[];
-    constexpr int STORE_WARPS = Shape<EPI>::STORE_WARPS, THREADS = Shape<EPI>::THREADS;
-    LNSmem<EPI>& sm = *reinterpret_cast<LNSmem<EPI>*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    typedef Shape<EPI, LONG> S;
+    constexpr int STORE_WARPS = S::STORE_WARPS, THREADS = S::THREADS;
+    LNSmem<EPI, LONG>& sm = *reinterpret_cast<LNSmem<EPI, LONG>*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     volatile int* error = &sm.error;
     const unsigned rank = cta_rank();
@@ -741,28 +763,30 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1) linear_kernel(const LN
             unsigned done = 0;
             Slot r;
             const unsigned slot_step = unsigned(a.slot_bytes) / 16;
-            for (unsigned i = pair; ok && i < tiles; i += pairs, ++done) {
+            for (unsigned i = pair; ok && i < tiles; i += pairs) {
                 const Place t = place_at<EPI>(a, i);
                 const int steps = __shfl_sync(0xffffffffu, t.steps, 0);
-                const unsigned half = done & 1u, round = (done >> 1) & 1u, d = tmem + half * LN_N;
-                if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[half]), round ^ 1u, error)) { ok = false; break; }
-                tc_fence_after();
-                const int turn = Shape<EPI>::LOGITS && a.twice ? (steps + 1) / 2 : steps;      // from here on into the other half
-                for (int s = 0; s < steps; ++s, r.next(a)) {
-                    if (!kb_wait_warp(kb_smem_u32(&sm.full[r.slot]), r.parity, error)) { ok = false; break; }
+                // an accumulator after the other, of the whole contraction or (LONG) of a chunk of it
+                for (int s0 = 0; s0 < steps; s0 += LONG ? LN_CHUNK : steps, ++done) {
+                    const unsigned half = done & 1u, round = (done >> 1) & 1u, d = tmem + half * LN_N;
+                    if (!kb_wait_warp(kb_smem_u32(&sm.acc_empty[half]), round ^ 1u, error)) { ok = false; break; }
                     tc_fence_after();
-                    const unsigned long long da = desc_a + r.slot * slot_step, db = desc_b + r.slot * slot_step;
-                    if (elect_one()) {
+                    const int here = LONG ? min(LN_CHUNK, steps - s0) : steps;
+                    for (int s = 0; s < here; ++s, r.next(a)) {
+                        if (!kb_wait_warp(kb_smem_u32(&sm.full[r.slot]), r.parity, error)) { ok = false; break; }
+                        tc_fence_after();
+                        const unsigned long long da = desc_a + r.slot * slot_step, db = desc_b + r.slot * slot_step;
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < LN_K / 16; ++k)
-                            mma_f16(s >= turn ? d + LN_N : d, da + k * STEP_A, db + k * STEP_B, idesc, (s > 0 && s != turn) || k > 0);
-                        mma_commit(&sm.empty[r.slot]);
+                            for (int k = 0; k < LN_K / 16; ++k) mma_f16(d, da + k * STEP_A, db + k * STEP_B, idesc, s > 0 || k > 0);
+                            mma_commit(&sm.empty[r.slot]);
+                        }
+                        __syncwarp();
                     }
+                    if (!ok) break;
+                    if (elect_one()) mma_commit(&sm.acc_full[half]);
                     __syncwarp();
                 }
-                if (!ok) break;
-                if (elect_one()) mma_commit(&sm.acc_full[half]);
-                __syncwarp();
             }
             // nothing is in flight when the tensor memory is freed: on the good path the store warps have
             // seen every accumulator; after a wait that gave up, wait for what was issued
@@ -780,43 +804,67 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1) linear_kernel(const LN
         w.stage = kb_smem_u32(sm.out[warp - LN_STORE_WARP0]);
         w.add = sm.add[warp - LN_STORE_WARP0];
         w.lane = lane;
-        unsigned done = 0;
+        unsigned done = 0, turn = 0;                         // accumulators and tiles so far
         Place t = place_at<EPI>(a, pair);                    // (a pair has a tile at least)
         RowInputs in = ask_inputs<EPI>(a, t, rank, w.quarter, lane);
-        for (unsigned i = pair; i < tiles; i += pairs, ++done) {
-            const unsigned half = done & 1u;
-            w.src = tmem + half * LN_N + (unsigned(w.quarter * 32) << 16);
+        for (unsigned i = pair; ok && i < tiles; i += pairs, ++turn) {
+            if (LONG && i != pair) {                         // (its first chunk is long enough to wait for them)
+                t = place_at<EPI>(a, i);
+                in = ask_inputs<EPI>(a, t, rank, w.quarter, lane);
+            }
             w.row0 = int64_t(2 * t.m + int(rank)) * LN_M + w.quarter * 32;
-            fetch_tile_biases<T, EPI>(a, t, w);
+            fetch_tile_biases<T, EPI, LONG>(a, t, w);
             Place next = t;
             RowInputs next_in = in;
-            if (i + pairs < tiles) {
+            if (!LONG && i + pairs < tiles) {
                 next = place_at<EPI>(a, i + pairs);
                 next_in = ask_inputs<EPI>(a, next, rank, w.quarter, lane);
             }
-            if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[half]), (done >> 1) & 1u, error)) break;
-            tc_fence_after();
-            __syncwarp();                                    // the warp's biases are there
+            [[maybe_unused]] Logits<LONG> logits;
+            [[maybe_unused]] Columns mine{0, 0};
+            if constexpr (S::LOGITS) mine = logits_columns<S::GROUPS>(a, t, w.group);
+            // the accumulators of the chunks, or the one there is: its half is given back when it has been read
+            for (int s0 = 0;;) {
+                const unsigned half = done & 1u;
+                if (!kb_wait_warp(kb_smem_u32(&sm.acc_full[half]), (done >> 1) & 1u, error)) { ok = false; break; }
+                tc_fence_after();
+                __syncwarp();                                // the warp's biases are there
+                w.src = tmem + half * LN_N + (unsigned(w.quarter * 32) << 16);
+                if constexpr (S::LOGITS) logits.chunk(w.src + unsigned(mine.from), w.row0 < a.rows ? mine.to - mine.from : 0, s0 == 0);
+                if (!LONG) break;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_at_leader(&sm.acc_empty[half]);
+                ++done;
+                s0 += LN_CHUNK;
+                if (s0 >= t.steps) break;
+            }
+            if (!ok) break;
             if constexpr (EPI == LN_SCORES) {
                 const int own = w.quarter * 32 + lane;
-                sm.part[half][w.group][own] = scores_tile(a, t, w, in);
+                const unsigned at = turn & 1u;
+                sm.part[at][w.group][own] = scores_tile<LONG>(a, t, w, in, mine, logits);
                 __syncwarp();
-                if (lane == 0) kb_arrive(&sm.part_full[half]);
+                if (lane == 0) kb_arrive(&sm.part_full[at]);
                 if (w.group == 0) {
-                    if (!kb_wait_warp(kb_smem_u32(&sm.part_full[half]), (done >> 1) & 1u, error)) break;
-                    const float2 p[4] = {sm.part[half][0][own], sm.part[half][1][own], sm.part[half][2][own], sm.part[half][3][own]};
+                    if (!kb_wait_warp(kb_smem_u32(&sm.part_full[at]), (turn >> 1) & 1u, error)) break;
                     const int64_t row = w.row0 + lane;
-                    if (row < a.rows) a.parts[row * a.nt + t.n] = join4(p);
+                    if (row < a.rows) a.parts[row * a.nt + t.n] = join_groups<S::GROUPS>(sm.part[at], own);
                 }
             }
-            if constexpr (EPI == LN_DLOGITS) dlogits_tile<T>(a, t, w, in, &map_out);
+            if constexpr (EPI == LN_DLOGITS) dlogits_tile<T, LONG>(a, t, w, in, mine, logits, &map_out);
             if constexpr (EPI == LN_GATED) gated_tile<T, ACT>(a, t, w, &map_out);
             if constexpr (EPI == LN_SUM || EPI == LN_OUTER) sum_tile<T, EPI>(a, t, w, &map_out);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at_leader(&sm.acc_empty[half]);
-            t = next;
-            in = next_in;
+            if (!LONG) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_at_leader(&sm.acc_empty[done & 1u]);
+                ++done;
+            }
+            if (!LONG) {
+                t = next;
+                in = next_in;
+            }
         }
         if (lane == 0) tma_store_done();
     }
@@ -1129,11 +1177,11 @@ struct Maps {
     CUtensorMap a0, b0, a1, b1, out;
 };
 
-template <typename T, int EPI, int ACT>
+template <typename T, int EPI, int ACT, bool LONG>
 cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t stream) {
-    constexpr int bytes = int(sizeof(LNSmem<EPI>)) + 1024;
+    constexpr int bytes = int(sizeof(LNSmem<EPI, LONG>)) + 1024;
     static_assert(bytes <= 232448, "a CTA's shared memory");
-    auto kernel = linear_kernel<T, EPI, ACT>;
+    auto kernel = linear_kernel<T, EPI, ACT, LONG>;
     static std::atomic<uint64_t> allowed{0};           // devices on which the kernel may have that much
     int dev = 0;
     if (cudaError_t err = cudaGetDevice(&dev)) return err;
@@ -1149,12 +1197,9 @@ cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t str
     const int64_t tiles = int64_t(a.mt) * a.nt * a.splits;
     if (tiles >= int64_t(1) << 30) return cudaErrorInvalidConfiguration;
     const int64_t pairs = sm_count / 2 > 1 ? sm_count / 2 : 1;
-    // logits: where a pair has one tile at most, the other half of tensor memory takes half of the contraction, which halves what is lost
-    a.twice = Shape<EPI>::LOGITS && tiles <= pairs && a.steps > 1;
-    a.whole = 1.f + LN_SHORT * float(LN_K) * float(a.steps) / (a.twice ? 2.f : 1.f);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(unsigned(2 * std::min(tiles, pairs)));
-    cfg.blockDim = dim3(Shape<EPI>::THREADS);
+    cfg.blockDim = dim3(Shape<EPI, LONG>::THREADS);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -1167,9 +1212,13 @@ cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t str
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a, maps.a0, maps.b0, maps.a1, maps.b1, maps.out);
 }
-template <int EPI, int ACT = 0>
+template <int EPI, int ACT = 0, bool LONG = false>
 cudaError_t launch(int dtype, const LNArgs& a, const Maps& maps, int sm_count, cudaStream_t stream) {
-    return dtype == GAR_BF16 ? launch_as<__nv_bfloat16, EPI, ACT>(a, maps, sm_count, stream) : launch_as<__half, EPI, ACT>(a, maps, sm_count, stream);
+    return dtype == GAR_BF16 ? launch_as<__nv_bfloat16, EPI, ACT, LONG>(a, maps, sm_count, stream) : launch_as<__half, EPI, ACT, LONG>(a, maps, sm_count, stream);
+}
+template <int EPI>
+cudaError_t launch_logits(int dtype, const LNArgs& a, const Maps& maps, int sm_count, cudaStream_t stream) {
+    return a.steps > LN_ONE ? launch<EPI, 0, true>(dtype, a, maps, sm_count, stream) : launch<EPI>(dtype, a, maps, sm_count, stream);
 }
 
 // Columns of a tile, a multiple of `unit` up to 256.  A step's copies come at some 47 bytes per cycle and SM, 16 KB of A and 64
@@ -1451,7 +1500,7 @@ cudaError_t launch_linear_logprobs(const gar_linear_logprobs_params_t& p, int64_
     ScoresPlan plan(p, ldx, ldw);
     if (few_rows_applies(p.rows, p.hidden, p.weight, ldw, nullptr, 0) && few_scores_parts(sm_count) <= LN_FEW_PARTS) {
         int count = 0;
-        if (cudaError_t err = launch_few_scores(p, ldx, ldw, LN_SHORT, plan.parts, plan.target_z, &count, sm_count)) return err;
+        if (cudaError_t err = launch_few_scores(p, ldx, ldw, plan.parts, plan.target_z, &count, sm_count)) return err;
         return launch_small(join_scores_kernel, dim3(unsigned(parts_of(p.rows, 8))), stream, plan.parts, plan.target_z, p.logprobs ? p.targets : nullptr, p.rows,
                             count, p.vocab, p.logprobs, p.lse, p.lse_lo);
     }
@@ -1470,7 +1519,7 @@ cudaError_t launch_linear_logprobs(const gar_linear_logprobs_params_t& p, int64_
         a.targets = p.logprobs ? p.targets + r0 : nullptr;
         a.parts = plan.parts;
         a.target_z = plan.target_z;
-        if (cudaError_t err = launch<LN_SCORES>(p.dtype, a, maps, sm_count, stream)) return err;
+        if (cudaError_t err = launch_logits<LN_SCORES>(p.dtype, a, maps, sm_count, stream)) return err;
         if (cudaError_t err = launch_small(join_scores_kernel, dim3(unsigned(parts_of(x.rows, 8))), stream, plan.parts, plan.target_z, a.targets, x.rows, a.nt,
                                            p.vocab, p.logprobs ? p.logprobs + r0 : nullptr, p.lse ? p.lse + r0 : nullptr,
                                            p.lse_lo ? p.lse_lo + r0 : nullptr)) return err;
@@ -1525,7 +1574,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
             a.y = plan.dz;
             a.ldy = plan.ld_dz;
             if (cudaError_t err = operand_map(&maps.out, p.dtype, dz, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return err;
-            if (cudaError_t err = launch<LN_DLOGITS>(p.dtype, a, maps, sm_count, stream)) return err;
+            if (cudaError_t err = launch_logits<LN_DLOGITS>(p.dtype, a, maps, sm_count, stream)) return err;
             if (p.dx)
                 if (cudaError_t err = launch_sum(d, dz, w, nullptr, nullptr, v0 > 0, sm_count, stream)) return err;
         }

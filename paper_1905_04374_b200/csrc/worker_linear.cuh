@@ -16,11 +16,10 @@ size_t gated_linear_backward_workspace_bytes(const gar_gated_linear_grad_params_
 cudaError_t launch_gated_linear_backward(const gar_gated_linear_grad_params_t& p, int sm_count);
 cudaError_t launch_dropout(const gar_dropout_params_t& p, unsigned limit, float scale);
 
-// A few rows (worker_few.cu): whether it applies, the parts a row's scores come in at most, the launches (lost: what the tensor
-// core's sums lose per term).
+// A few rows (worker_few.cu): whether it applies, the parts a row's scores come in at most, the launches.
 bool few_rows_applies(int64_t rows, int64_t hidden, const void* w0, int64_t ld0, const void* w1, int64_t ld1);
 int64_t few_scores_parts(int sm_count);
-cudaError_t launch_few_scores(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw, float lost, float2* parts, float* target_z, int* count,
+cudaError_t launch_few_scores(const gar_linear_logprobs_params_t& p, int64_t ldx, int64_t ldw, float2* parts, float* target_z, int* count,
                               int sm_count);
 cudaError_t launch_few_gated(const gar_gated_linear_params_t& p, int sm_count);
 

@@ -100,3 +100,79 @@ def test_a_row_of_minus_infinity_at_every_width(pkg, rows, vocab):
     assert float(lse[1]) == -math.inf and float(logprobs[1]) == -math.inf
     close(r.lse, lse, 2 * d + 2e-5, "lse")
     close(r.logprobs, logprobs, 2 * d + 2e-5, "logprobs")
+
+
+# ---- sums of any operands --------------------------------------------------------------------------
+def chunk_of(k):
+    """Terms that go into one accumulator."""
+    return k if k <= 640 else 512
+
+
+def sums_off(k, rows):
+    """Of the terms' magnitudes M, at most.  A product is cut to a multiple of 2^-25 (mma.sync, up to 16 rows: 2^-24) of the largest magnitude
+    among the accumulator and the 16 products of its instruction, which is below M; so is the accumulator, and their sum to 24 bits, 2^-23 of M
+    at most.  That is (17 unit + 2^-23) M for 16 terms.  The chunks' sums are added with half a unit of 24 bits each."""
+    unit = 2.0 ** -24 if rows <= 16 else 2.0 ** -25
+    return chunk_of(k) * (17 / 16 * unit + 2.0 ** -27) + 2.0 ** -24 * (-(-k // chunk_of(k)) + 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_what_an_addition_keeps(pkg, dtype):
+    """The unit of the bound above: terms of 2^-25 (2^-24) next to 1 are added whole, in the same instruction and behind it."""
+    for rows, unit in ((4, 24), (40, 25)):
+        for first in (1, 16):
+            n = 2 ** (unit - 23)                             # together one unit of fp32's last place next to 1
+            w, x = torch.zeros(1, 64, dtype=DTYPES[dtype], device=DEV), torch.zeros(rows, 64, dtype=DTYPES[dtype], device=DEV)
+            w[:, 0], x[:, 0] = 1.0, 1.0
+            w[:, first:first + n], x[:, first:first + n] = 2.0 ** -13, 2.0 ** (13 - unit)
+            assert bool((pkg.gar_linear_logprobs(x, w).lse == 1 + 2.0 ** -23).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [4, 12, 40, 600])
+@pytest.mark.parametrize("hidden", [4096, 6144])
+def test_logits_that_are_exact(pkg, dtype, rows, hidden):
+    """Hidden states with one element other than 0: the logits are single products, which fp32 holds.  lse and log probabilities are
+    off by the softmax's own arithmetic and their rounding only (2^-22 of lse, 1e-5)."""
+    vocab = 600
+    w = normal((vocab, hidden), dtype, 31, 1.0)
+    x = torch.zeros(rows, hidden, dtype=DTYPES[dtype], device=DEV)
+    at = torch.randint(0, hidden, (rows,), generator=gen(32), device=DEV)
+    x[torch.arange(rows, device=DEV), at] = 256.0
+    t = torch.randint(0, vocab, (rows,), generator=gen(33), device=DEV)
+    r = pkg.gar_linear_logprobs(x, w, t)
+    logprobs, lse, _, _ = scores_64(x, w, None, t)
+    # z up to some 800: of it 4e-6, as a factor for what other sums lose would make, is 3e-3
+    assert float(lse.abs().min()) > 500
+    close(r.lse, lse, 1e-5 + 2.0 ** -22 * lse.abs(), "lse")
+    close(r.logprobs, logprobs, 1e-5 + 2.0 ** -22 * (lse.abs() + logprobs.abs()), "logprobs")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,hidden,vocab", [(4, 4096, 500), (4, 6200, 500), (16, 3000, 70), (40, 520, 300), (40, 640, 300), (40, 641, 300), (40, 768, 300), (40, 4096, 500), (40, 16384, 500), (300, 4096, 10),
+                                               (2000, 1500, 5000), (600, 16384, 1200)])
+@pytest.mark.parametrize("signs", ["one", "random"])
+def test_logits_of_long_sums(pkg, dtype, rows, hidden, vocab, signs):
+    """Terms of one sign, where the tensor core loses most, and of random signs."""
+    g = gen(hidden + rows)
+    x, w = torch.randn(rows, hidden, generator=g, device=DEV), torch.randn(vocab, hidden, generator=g, device=DEV)
+    if signs == "one":
+        x, w = x.abs() + 0.5, (w.abs() + 0.5) * (20.0 / hidden)
+    else:
+        w *= 3.0 / math.sqrt(hidden)
+    x, w = x.to(DTYPES[dtype]), w.to(DTYPES[dtype])
+    t = torch.randint(0, vocab, (rows,), generator=g, device=DEV)
+    r = pkg.gar_linear_logprobs(x, w, t)
+    z, mag = x.double() @ w.double().t(), x.double().abs() @ w.double().abs().t()
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None])
+    off = mag * sums_off(hidden, rows)
+    # lse moves by the mean of the logits' errors under p, a log probability by its own logit's besides
+    mean, picked = (p * off).sum(1), off.gather(1, t[:, None])[:, 0]
+    logprobs = z.gather(1, t[:, None])[:, 0] - lse
+    close(r.lse, lse, 1.01 * mean + 1e-5 + 2.0 ** -22 * lse.abs(), "lse")
+    close(r.logprobs, logprobs, 1.01 * (mean + picked) + 1e-5 + 2.0 ** -22 * (lse.abs() + logprobs.abs()), "logprobs")
+    if signs == "random" and vocab >= 300:
+        # The rows' mean, which leaves the loss of the sums alone: 1e-9 per term of a chunk's own sum, of the logits, whose mean
+        # under p is below lse; and as much again.
+        assert float(((r.lse.double() + r.lse_lo.double()) / lse - 1).mean().abs()) <= 2e-9 * chunk_of(hidden)
