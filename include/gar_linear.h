@@ -9,7 +9,8 @@
  * device, all buffers owned by the caller, every call asynchronous on
  * `stream`, argument errors returned before anything is launched, GAR_ERR_CUDA
  * for launch failures, no exceptions, no CPU fallback, bit-identical output
- * for the same input.  Matrices are row-major with unit column stride and a
+ * for the same call.  (How a call's work is cut up goes by its sizes, so that a row's last bits
+ * may differ between calls of different numbers of rows, a token scored alone and in a batch for instance.)  Matrices are row-major with unit column stride and a
  * row stride `ld` in elements (0 means the number of columns), at any alignment
  * of the element type.  A call with no rows writes no rows.
  *

@@ -161,9 +161,10 @@ int gar_activation_backward(const gar_activation_grad_params_t* params);
  * NaN included, reaches its sums.  No tokens: zeros.
  * dy is bf16 or binary16 (GAR_ERR_UNSUPPORTED for fp32) and x' is restored in the same type; the
  * products are exact and summed in fp32 on the tensor cores.  These truncate where they add: a sum is
- * short by 1e-9 of itself per token, up to 2.8e-9 where it grows steadily.  It is therefore taken over
- * 768 tokens at a time (16-bit gradients: 2048) and the parts are added rounded: before its own rounding
- * a gradient is off by some 1e-6 (16-bit: 6e-6) of the sum of its terms' magnitudes at most, at any length.
+ * short by 1e-9 of itself per token, up to 2.8e-9 where it grows steadily (6e-9 where dy and x' have all of
+ * binary16's bits).  It is therefore taken over 768 tokens at a time (16-bit gradients: 2048) and the parts are added
+ * rounded: before its own rounding a gradient is off by some 1e-6 (binary16 dy 3e-6, 16-bit gradients 6e-6) of the
+ * sum of its terms' magnitudes, at any length.
  * 1 <= workers <= GAR_MAX_N.
  */
 typedef struct gar_weight_grad_params_t {

@@ -11,7 +11,7 @@
 //   MMA warp       of the leading CTA: four 256 x 256 x 16 instructions per step
 //   store warps    groups of four, each with its share of a tile's columns, while the next products run
 //                  into the other half of tensor memory; a thread has one row, 32 columns at a time.  Two groups, or four
-//                  where a column takes an exponential (struct Shape)
+//                  where a column takes an exponential and one accumulator holds the sums (struct Shape)
 // and four epilogues (LN_SUM's and LN_OUTER's are one; enum Epilogue).  A thread owning a row makes the softmax's statistics, the group
 // maxima of the checkpoints and the row's target its own affair.
 // Tiles are as wide as the rule in width_for makes them, 256 columns at most.
@@ -241,9 +241,9 @@ __device__ __forceinline__ void store_plain(unsigned stage, int lane, unsigned s
     const int c = 2 * lane;
     dst += c;
     if (rows == 32 && cols >= 64 && ((reinterpret_cast<uintptr_t>(dst) | (ld << 1)) & 2) == 0) {
-        // A whole piece of rows that start on 4 bytes: nothing to check (weight gradient of 14 workers x 95 tokens,
-        // 250 x 11558: 70.8 -> 62.4 us). Odd rows put together from shuffled words were slower than the halves
-        // below (251 columns: 74.5 -> 85.3 us).
+        // A whole piece of rows that start on 4 bytes: nothing to check (14 workers x 95 tokens, 11558 outputs x 250 inputs, whole
+        // backward pass without dx: 70.8 -> 62.4 us). Odd rows put together from shuffled words were slower than the halves
+        // below (251 inputs: 74.5 -> 85.3 us).
 #pragma unroll 1
         for (int r0 = 0; r0 < 32; r0 += 8) {
             unsigned w[8];
@@ -1190,7 +1190,7 @@ cudaError_t launch_as(LNArgs a, const Maps& maps, int sm_count, cudaStream_t str
         if (dev < 64) allowed.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
     }
     // (an outer product's tiles go along its rows, which are then written whole: 11 x 128 tokens, 32000 x 1024, fp32 rows, whole backward
-    // pass without dx 370 us, row tiles in groups of 64 396)
+    // pass without dx 370 us, row tiles in groups of 64 396; in other runs 410 to 420)
     a.group_m = EPI == LN_OUTER ? 1 : group_rows(a.steps, a.mt);
     a.slot_bytes = LN_TILE + a.width * LN_K;
     a.ring = std::min(LN_RING_MOST, LN_RING_BYTES / a.slot_bytes);
@@ -1345,7 +1345,7 @@ bool block_on_16(const DenseWeightGrad& g) {
 // 11 workers x 128 tokens, 16128 x 1024, bf16 rows: 70 us, 98 by weight_grad_kernel's four store warps.  Rows that start anywhere are
 // stored in words of 4 bytes (whole backward pass without dx, weight_grad_kernel in brackets): 11 x 128, 100 x 512 15.4 us (22.5); 7 x 100,
 // 2000 x 501, fp32 25.2 (30.8); 2 x 2000, 16000 x 2047, bf16 483 (525); 4 x 700, 8000 x 2050, fp32 260 (269); but 11 x 128, 32000 x 1024, fp32,
-// 1.4 GB of rows with little to compute, 668 (536): those are left to the latter, which shifts rows to 16-byte chunks.
+// 1.4 GB of rows with little to compute, 668 (525 to 546): those are left to the latter, which shifts rows to 16-byte chunks.
 bool outer_applies(const DenseWeightGrad& g) {
     const int64_t gs = g.grads_dtype == GAR_F32 ? 4 : 2;
     if (g.tokens < 1 || g.tokens > (gs == 4 ? 768 : 2048)) return false;

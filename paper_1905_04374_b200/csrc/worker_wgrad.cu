@@ -63,7 +63,7 @@ enum Mode { WG_PLAIN_DY = 0, WG_FUSED = 1, WG_RESTORED = 2, WG_PANEL = 3 };
 constexpr int WG_PANEL_STEPS = 8;                     // 512 tokens
 // Steps per accumulator.  The tensor core truncates what it adds to an accumulator: the sum loses 1e-9 of itself per
 // token, up to 2.8e-9 where it grows steadily (measured: 4.4e-6 at 4096 random tokens, 5.6e-6 at 2048 positive ones;
-// rounded additions lose a tenth).  Sums are therefore taken in chunks, joined by rounded additions in tensor memory, so
+// rounded additions lose a tenth; binary16 operands with all their bits 6e-9, restored ones, whose products have fewer, 2.2e-9).  Sums are therefore taken in chunks, joined by rounded additions in tensor memory, so
 // that the loss has a bound however many tokens there are: 768 tokens for fp32 results (7e-7, growing sums 1.3e-6), 2048
 // for 16-bit ones (growing sums 6e-6, a fortieth of binary16's rounding; the same at 32768 tokens).  A join holds the products up for 2000 cycles:
 // 16-bit results at 768 tokens a chunk took 3 % longer with x restored beforehand and 10 to 13 % without.
