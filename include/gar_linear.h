@@ -75,8 +75,9 @@ size_t gar_linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t* p
  *     dx = dz W,    dW_w = dz_w^T x_w,    db_w[j] = sum_i dz_ij over the worker's rows
  * the latter two stored at weight_grads[w * ld_grads + j * hidden + k] and bias_grads[w * ld_grads + j], as by
  * gar_linear_weight_grad.  The vocabulary is gone through in pieces, whose dz is kept in the workspace: up to 96 MB of
- * it, or 256 columns where those take more.  binary16 dz carry a power of two taken from the largest |a| of their worker, so
- * that small gradients do not underflow: dz have all their bits down to 2^-28 of that |a|, what is below 2^-39 of it is lost.
+ * it, or 256 columns where those take more.  binary16 dz carry a power of two taken from the largest |a| of their worker (of their
+ * row, where no weight gradients are asked for), so that small gradients do not underflow: dz have all their bits down to 2^-28 of that
+ * |a|, what is below 2^-39 of it is lost.
  *   - A row without a target, or with a = 0, gets dx 0 and nothing it holds, NaN included, reaches a weight gradient.
  *   - No tokens: weight and bias gradients of zeros.
  *   - The same holds for a row masked throughout, lse = -inf, whatever its coefficient and its target; in any other row a target >= vocab gives NaN, in dx and

@@ -76,7 +76,7 @@ struct LNArgs : Tiling {
     float2*        parts;                 // LN_SCORES [rows][nt]: maximum, sum
     float*         target_z;              // LN_SCORES [rows]
     const float *  lse, *lse_lo, *coef;   // LN_DLOGITS [rows]
-    const unsigned* top;                  // every worker's largest |coef|, as bits, where coefficients carry a power of two; or null
+    const unsigned* top;                  // every worker's largest |coef|, or (tokens = 1) every row's, as bits, where they carry a power of two; or null
     unsigned       tokens;                // rows of a worker, for `top`
     void*          y;                     // OUT_PLAIN, and the fill after a wait that gave up
     int64_t        ldy, plane;            // elements between the result's rows; its parts or workers
@@ -1459,7 +1459,8 @@ struct GradPlan {
     Input     w;
     char*     x_rows;                      // x with rows that do not count as zeros
     float*    coef;
-    unsigned* top = nullptr;
+    unsigned* top = nullptr;               // a number per worker; without weight gradients no rows are added up and every row goes by its own
+    unsigned  tops = 0;                    // rows that share one
     char*     dz;
     float*    parts = nullptr;
     int64_t   pitch;
@@ -1470,7 +1471,10 @@ struct GradPlan {
           w(space, p.weight, p.vocab, p.hidden, ldw, 2 * parts_of(rows, 2 * LN_M), products(rows, p.hidden, p.vocab)) {
         x_rows = space.take(size_t(rows) * size_t(ldx) * 2);
         coef = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
-        if (p.dtype == GAR_F16) top = reinterpret_cast<unsigned*>(space.take(size_t(p.workers) * 4));
+        if (p.dtype == GAR_F16) {
+            top = p.weight_grads ? reinterpret_cast<unsigned*>(space.take(size_t(p.workers) * 4)) : reinterpret_cast<unsigned*>(coef);
+            tops = p.weight_grads ? unsigned(p.tokens) : 1u;
+        }
         dz = space.take(size_t(rows) * size_t(ld_dz) * 2);
         pitch = up_to(p.hidden, 4);
         // (sums of 2^15 terms at most)
@@ -1548,11 +1552,10 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
         copies.a.tokens = p.tokens;
         copies.a.workers = p.workers;
         copies.a.coef = plan.coef;
-        copies.a.top = plan.top;
+        copies.a.top = p.weight_grads ? plan.top : nullptr;
         if (cudaError_t err = copies.launch(sm_count, stream)) return err;
     }
-    SumTarget d{p.dtype, p.dx, plan.rows, p.hidden, p.lddx ? p.lddx : p.hidden, plan.parts, plan.pitch, plan.splits, plan.top,
-                unsigned(p.tokens)};
+    SumTarget d{p.dtype, p.dx, plan.rows, p.hidden, p.lddx ? p.lddx : p.hidden, plan.parts, plan.pitch, plan.splits, plan.top, plan.tops};
     for (int64_t v0 = 0; v0 < p.vocab; v0 += plan.piece) {
         Operand w = plan.w.m;
         w.p += v0 * w.ld * 2;
@@ -1569,7 +1572,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
             a.lse_lo = p.lse_lo;
             a.coef = plan.coef;
             a.top = plan.top;
-            a.tokens = unsigned(p.tokens);
+            a.tokens = plan.tops;
             a.out = OUT_WIDE;
             a.y = plan.dz;
             a.ldy = plan.ld_dz;

@@ -130,8 +130,9 @@ __device__ __forceinline__ void grid_dependency() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// The power of two that the largest coefficient is brought to 2^14 .. 2^15 with, and its inverse: |k| <= 120.
+// The power of two that a coefficient (its bits, of either sign) is brought to 2^14 .. 2^15 with, and its inverse: |k| <= 120.  1 for 0, infinities and NaN.
 __device__ __forceinline__ float power_for(unsigned top, bool inverse) {
+    top &= 0x7fffffffu;
     if (top == 0u || top >= 0x7f800000u) return 1.f;
     const int k = max(-120, min(120, 14 - (int(top >> 23) - 127)));
     return __uint_as_float(unsigned(127 + (inverse ? -k : k)) << 23);

@@ -41,6 +41,24 @@ def test_a_large_coefficient_stays_with_its_worker(pkg, workers, tokens, hidden,
             assert torch.equal(got[-1, own], want[-1, own] * power)
 
 
+@pytest.mark.parametrize("rows,hidden,vocab", [(40, 64, 300), (33, 65, 257), (20, 64, 40000), (9000, 32, 5000)])
+def test_a_large_coefficient_stays_with_its_row(pkg, rows, hidden, vocab):
+    """Without weight gradients nothing adds rows up: the gradient at a row's hidden state goes by its own coefficient alone."""
+    x, w, b, t = head(rows, hidden, vocab, "f16", True, 24)
+    t = t.clamp_min(0)
+    a = -(torch.rand(rows, generator=gen(8), device=DEV) + 0.5)
+    saved = pkg.gar_linear_logprobs(x, w, t, bias=b)
+    want = pkg.gar_linear_logprobs_backward(x, w, saved, t, a, bias=b)
+    check_head_gradient(pkg, x, w, b, t, a, 1, "f32", saved=saved)
+    some = torch.arange(rows, device=DEV) % 3 == 0
+    for power in (2.0 ** 40, 2.0 ** -20, 2.0 ** 6):
+        dx = pkg.gar_linear_logprobs_backward(x, w, saved, t, torch.where(some, a * power, a), bias=b)
+        assert torch.equal(dx[~some], want[~some])
+    # a power of two of a row's coefficient is one of its gradient, but for what binary16 rounds off its subnormals
+    off = 2.0 ** -25 * 64 * (want[some].double().abs() < 2.0 ** -14)
+    close(dx[some], want[some].double() * 64, off, "scaled rows")
+
+
 # ---- so many columns that a group of row tiles times them passes 32 bits ------------------------------
 def test_scores_of_two_to_the_thirty_columns(pkg):
     """17 rows with one step of the contraction, 2^22 column tiles and more.  Logits 0 but for some columns."""
