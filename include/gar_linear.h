@@ -71,7 +71,8 @@ size_t gar_linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t* p
 /*
  * Gradients of the above for `workers` workers at once, row w * tokens + t being worker w's token
  * t, from the saved lse and the gradient a at the log probabilities: with
- *     dz_ij = a_i ([j = t_i] - e^(z_ij - lse_i))         (z computed again, dz rounded to x's type)
+ *     dz_ij = a_i ([j = t_i] - e^(z_ij - lse_i))         (z computed again, dz rounded to x's type; of up to 128 rows
+ *                                                         what that leaves out is rounded and used besides)
  *     dx = dz W,    dW_w = dz_w^T x_w,    db_w[j] = sum_i dz_ij over the worker's rows
  * the latter two stored at weight_grads[w * ld_grads + j * hidden + k] and bias_grads[w * ld_grads + j], as by
  * gar_linear_weight_grad.  The vocabulary is gone through in pieces, whose dz is kept in the workspace: up to 96 MB of

@@ -78,6 +78,7 @@ struct LNArgs : Tiling {
     const float *  lse, *lse_lo, *coef;   // LN_DLOGITS [rows]
     const unsigned* top;                  // every worker's largest |coef|, or (tokens = 1) every row's, as bits, where they carry a power of two; or null
     unsigned       tokens;                // rows of a worker, for `top`
+    unsigned       fold;                  // LN_DLOGITS: dz in two parts, every worker's `fold` rows once more behind them for what the first left out; 0: one
     void*          y;                     // OUT_PLAIN, and the fill after a wait that gave up
     int64_t        ldy, plane;            // elements between the result's rows; its parts or workers
     gar_checkpoint_t s0, s1;              // of g and u
@@ -322,23 +323,42 @@ struct Columns {
     }
 };
 
+// Rows in two parts: a worker's `fold` rows, then the same once more.  Which of the caller's rows one is, and of which part.
+struct Folded {
+    unsigned row;
+    bool     rest;
+};
+__device__ __forceinline__ Folded unfold(unsigned row, unsigned fold) {
+    const unsigned worker = row / (2 * fold), at = row - worker * 2 * fold;
+    return at < fold ? Folded{worker * fold + at, false} : Folded{worker * fold + at - fold, true};
+}
+
 // What a thread reads for its row of a tile from memory: asked for a tile ahead, looked at when it is the tile's turn.
 struct RowInputs {
     int64_t target;
     float   coef, lse, lo;
+    bool    rest;                    // the row of the second part of dz
 };
 template <int EPI>
 __device__ __forceinline__ RowInputs ask_inputs(const LNArgs& a, const Place& t, unsigned rank, int quarter, int lane) {
-    RowInputs in{-1, 0.f, 0.f, 0.f};
+    RowInputs in{-1, 0.f, 0.f, 0.f, false};
     if (EPI != LN_SCORES && EPI != LN_DLOGITS) return in;
     const int64_t row = int64_t(2 * t.m + int(rank)) * LN_M + quarter * 32 + lane;
     if (row >= a.rows) return in;
-    if (a.targets) in.target = a.targets[row];
-    if (EPI == LN_DLOGITS) {
-        in.coef = a.coef[row];
-        in.lse = a.lse[row];
-        if (a.lse_lo) in.lo = a.lse_lo[row];
+    if (EPI == LN_SCORES) {
+        if (a.targets) in.target = a.targets[row];
+        return in;
     }
+    int64_t token = row;
+    if (a.fold) {
+        const Folded f = unfold(unsigned(row), a.fold);
+        token = f.row;
+        in.rest = f.rest;
+    }
+    in.target = a.targets[token];
+    in.coef = a.coef[row];
+    in.lse = a.lse[token];
+    if (a.lse_lo) in.lo = a.lse_lo[token];
     return in;
 }
 // The biases of a warp's columns of a tile, into its piece of shared memory, while the tile's products still run.
@@ -476,6 +496,14 @@ __device__ __forceinline__ void dlogits_tile(const LNArgs& a, const Place& t, co
         if (__any_sync(0xffffffffu, nothing)) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = nothing ? 0.f : v[j];
+        }
+        if (a.fold && __any_sync(0xffffffffu, in.rest)) {
+            // what the first part's rounding left out; nothing of what it holds as an infinity
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                const float kept = Elem<T>::widen(Elem<T>::narrow(v[j]));
+                if (in.rest) v[j] = fabsf(kept) <= 3.402823466e38f ? v[j] - kept : 0.f;
+            }
         }
         stage_free(w);
         // rows of 64 bytes, 16-byte chunks in the 64-byte swizzle
@@ -965,6 +993,7 @@ struct CopyArgs {
     const float *  grad, *lse;
     int64_t        vocab, tokens;
     int            workers;
+    unsigned       fold;                   // the first job's rows are written twice, worker by worker (unfold); 0: once
     float*         coef;
     unsigned*      top;                    // [workers]; null: not asked for
 };
@@ -999,12 +1028,14 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const CopyArgs a) {
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < j.pieces; i += int64_t(gridDim.x) * 256) {
         const int64_t row = i / j.per_row, c = (i - row * j.per_row) * 8;
         bool zero = false;
+        int64_t from = row;
         if (head) {
-            const float coef = coefficient(a, row);
+            if (a.fold) from = unfold(unsigned(row), a.fold).row;
+            const float coef = coefficient(a, from);
             zero = coef == 0.f;
             if (c == 0) a.coef[row] = coef;
         }
-        const unsigned short* p = j.src + row * j.ld + c;
+        const unsigned short* p = j.src + from * j.ld + c;
         uint4 w = make_uint4(0, 0, 0, 0);
         if (!zero) {
             if (j.aligned && c + 8 <= j.cols) {
@@ -1053,19 +1084,25 @@ __global__ void __launch_bounds__(32 * LN_SLICES) column_sums_kernel(const T* dz
     db[int64_t(blockIdx.y) * ld_grads + mine] = Elem<G>::narrow(sum);
 }
 
-// The parts of a sum, added in order and rounded once, four columns per thread and turn.
+// The parts of a sum, added in order and rounded once, four columns per thread and turn.  fold: a row's sum and that of its second
+// part, `fold` rows behind it.
 template <typename T>
 __global__ void __launch_bounds__(256) join_parts_kernel(const float* parts, int64_t plane, int64_t pitch, int splits, int64_t rows, int64_t cols,
-                                                         const unsigned* top, unsigned tokens, T* y, int64_t ldy) {
+                                                         const unsigned* top, unsigned tokens, unsigned fold, T* y, int64_t ldy) {
     grid_dependency();
     const int64_t per_row = (cols + 3) / 4, pieces = rows * per_row;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < pieces; i += int64_t(gridDim.x) * 256) {
         const int64_t row = i / per_row, c = (i - row * per_row) * 4;
-        const float* p = parts + row * pitch + c;
-        const float by = top ? power_for(top[unsigned(row) / tokens], true) : 1.f;
+        const int64_t at = fold ? row + row / fold * fold : row;
+        const float* p = parts + at * pitch + c;
+        const float by = top ? power_for(top[unsigned(at) / tokens], true) : 1.f;
         float4 s = __ldcs(reinterpret_cast<const float4*>(p));
         for (int k = 1; k < splits; ++k) {
             const float4 q = __ldcs(reinterpret_cast<const float4*>(p + k * plane));
+            s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
+        }
+        for (int k = 0; fold && k < splits; ++k) {
+            const float4 q = __ldcs(reinterpret_cast<const float4*>(p + fold * pitch + k * plane));
             s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
         }
         T out[4] = {Elem<T>::narrow(s.x * by), Elem<T>::narrow(s.y * by), Elem<T>::narrow(s.z * by), Elem<T>::narrow(s.w * by)};
@@ -1282,7 +1319,7 @@ struct SumTarget {
     int64_t  pitch;
     int      splits;
     const unsigned* top;                               // dz carries power_for(top[row / tokens]); or null
-    unsigned tokens;
+    unsigned tokens, fold;                             // fold: dz in two parts (LNArgs::fold); always with `parts`
 };
 cudaError_t launch_sum(const SumTarget& d, const Operand& a0, const Operand& b0, const Operand* a1, const Operand* b1, bool add, int sm_count, cudaStream_t stream) {
     Maps maps;
@@ -1325,11 +1362,12 @@ cudaError_t launch_sum(const SumTarget& d, const Operand& a0, const Operand& b0,
     return launch<LN_SUM>(d.dtype, a, maps, sm_count, stream);
 }
 cudaError_t join_sum(const SumTarget& d, int sm_count, cudaStream_t stream) {
-    const dim3 grid(copy_blocks(d.rows * parts_of(d.cols, 4), sm_count));
+    const int64_t rows = d.fold ? d.rows / 2 : d.rows;
+    const dim3 grid(copy_blocks(rows * parts_of(d.cols, 4), sm_count));
     if (d.dtype == GAR_BF16)
-        return launch_small(join_parts_kernel<__nv_bfloat16>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top, d.tokens,
+        return launch_small(join_parts_kernel<__nv_bfloat16>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, rows, d.cols, d.top, d.tokens, d.fold,
                             static_cast<__nv_bfloat16*>(d.dx), d.ld);
-    return launch_small(join_parts_kernel<__half>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, d.rows, d.cols, d.top, d.tokens,
+    return launch_small(join_parts_kernel<__half>, grid, stream, d.parts, d.rows * d.pitch, d.pitch, d.splits, rows, d.cols, d.top, d.tokens, d.fold,
                         static_cast<__half*>(d.dx), d.ld);
 }
 
@@ -1452,9 +1490,14 @@ int64_t piece_of(int64_t rows, int64_t hidden, int64_t vocab) {
     }
     return best * LN_N;
 }
+// Rows up to which dz, which is rounded to 16 bits, comes in two parts, the second of what rounding the first left out, a row each: a
+// pair's tile of 256 rows has room for both, at no product's cost.  Few coefficients decide a gradient there, whose roundings do not
+// average out: 8 workers x 2 tokens, 10 columns, bf16: gradients 2.6e-3 off in the mean, 1.7e-3 with both parts, which is the rounding of the result.
+constexpr int64_t LN_TWO_PARTS = LN_M;
 struct GradPlan {
     Space     space;
-    int64_t   rows, piece, ld_dz, ldx;
+    unsigned  fold;                        // dz in two parts
+    int64_t   tokens, rows, piece, ld_dz, ldx;            // of a worker, of all: of dz, in both parts
     int       splits;
     Input     w;
     char*     x_rows;                      // x with rows that do not count as zeros
@@ -1467,25 +1510,25 @@ struct GradPlan {
     char*     weight_space = nullptr;
     size_t    weight_bytes = 0;
     GradPlan(const gar_linear_logprobs_grad_params_t& p, int64_t ldw)
-        : space(p.workspace), rows(p.workers * p.tokens), piece(piece_of(std::max<int64_t>(rows, 1), p.hidden, p.vocab)), ld_dz(up_to(piece, 8)), ldx(up_to(p.hidden, LN_PITCH)),
+        : space(p.workspace), fold(p.workers * p.tokens <= LN_TWO_PARTS ? unsigned(p.tokens) : 0u), tokens(fold ? 2 * p.tokens : p.tokens), rows(p.workers * tokens), piece(piece_of(std::max<int64_t>(rows, 1), p.hidden, p.vocab)), ld_dz(up_to(piece, 8)), ldx(up_to(p.hidden, LN_PITCH)),
           w(space, p.weight, p.vocab, p.hidden, ldw, 2 * parts_of(rows, 2 * LN_M), products(rows, p.hidden, p.vocab)) {
         x_rows = space.take(size_t(rows) * size_t(ldx) * 2);
         coef = reinterpret_cast<float*>(space.take(size_t(rows) * 4));
         if (p.dtype == GAR_F16) {
             top = p.weight_grads ? reinterpret_cast<unsigned*>(space.take(size_t(p.workers) * 4)) : reinterpret_cast<unsigned*>(coef);
-            tops = p.weight_grads ? unsigned(p.tokens) : 1u;
+            tops = p.weight_grads ? unsigned(tokens) : 1u;
         }
         dz = space.take(size_t(rows) * size_t(ld_dz) * 2);
         pitch = up_to(p.hidden, 4);
         // (sums of 2^15 terms at most)
         const int64_t terms = std::min(piece, p.vocab);
-        splits = splits_for(std::max<int64_t>(rows, 1), p.hidden, parts_of(terms, LN_K), parts_of(terms, LN_TERMS), piece < p.vocab);
-        if (p.dx && (splits > 1 || piece < p.vocab)) parts = reinterpret_cast<float*>(space.take(size_t(splits) * size_t(rows) * size_t(pitch) * 4));
+        splits = splits_for(std::max<int64_t>(rows, 1), p.hidden, parts_of(terms, LN_K), parts_of(terms, LN_TERMS), piece < p.vocab || fold);
+        if (p.dx && (splits > 1 || piece < p.vocab || fold)) parts = reinterpret_cast<float*>(space.take(size_t(splits) * size_t(rows) * size_t(pitch) * 4));
         if (p.weight_grads) {
             // (the last piece, if it is shorter, may be cut into more parts)
             const int64_t last = (p.vocab - 1) % piece + 1;
-            weight_bytes = std::max(dense_weight_grad_workspace_bytes(p.workers, p.tokens, std::min(piece, p.vocab), p.hidden, p.bias_grads != nullptr),
-                                    dense_weight_grad_workspace_bytes(p.workers, p.tokens, last, p.hidden, p.bias_grads != nullptr));
+            weight_bytes = std::max(dense_weight_grad_workspace_bytes(p.workers, tokens, std::min(piece, p.vocab), p.hidden, p.bias_grads != nullptr),
+                                    dense_weight_grad_workspace_bytes(p.workers, tokens, last, p.hidden, p.bias_grads != nullptr));
             weight_space = space.take(weight_bytes);
         }
     }
@@ -1551,11 +1594,12 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
         copies.a.vocab = p.vocab;
         copies.a.tokens = p.tokens;
         copies.a.workers = p.workers;
+        copies.a.fold = plan.fold;
         copies.a.coef = plan.coef;
         copies.a.top = p.weight_grads ? plan.top : nullptr;
         if (cudaError_t err = copies.launch(sm_count, stream)) return err;
     }
-    SumTarget d{p.dtype, p.dx, plan.rows, p.hidden, p.lddx ? p.lddx : p.hidden, plan.parts, plan.pitch, plan.splits, plan.top, plan.tops};
+    SumTarget d{p.dtype, p.dx, plan.rows, p.hidden, p.lddx ? p.lddx : p.hidden, plan.parts, plan.pitch, plan.splits, plan.top, plan.tops, plan.fold};
     for (int64_t v0 = 0; v0 < p.vocab; v0 += plan.piece) {
         Operand w = plan.w.m;
         w.p += v0 * w.ld * 2;
@@ -1573,6 +1617,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
             a.coef = plan.coef;
             a.top = plan.top;
             a.tokens = plan.tops;
+            a.fold = plan.fold;
             a.out = OUT_WIDE;
             a.y = plan.dz;
             a.ldy = plan.ld_dz;
@@ -1586,7 +1631,7 @@ cudaError_t launch_linear_logprobs_backward(const gar_linear_logprobs_grad_param
             g.dtype = p.dtype;
             g.grads_dtype = p.grads_dtype;
             g.workers = p.workers;
-            g.tokens = p.tokens;
+            g.tokens = plan.tokens;
             g.out = w.rows;
             g.in = p.hidden;
             g.dy = plan.dz;
@@ -1722,7 +1767,7 @@ cudaError_t launch_gated_linear_backward(const gar_gated_linear_grad_params_t& p
     Copies copies;
     for (Input* in : {&plan.gate, &plan.up, &plan.dgate, &plan.dup}) copies.add(*in);
     if (cudaError_t err = copies.launch(sm_count, stream)) return err;
-    SumTarget d{p.dtype, p.dx, p.rows, p.hidden, p.lddx, plan.parts, plan.pitch, plan.splits, nullptr, 1};
+    SumTarget d{p.dtype, p.dx, p.rows, p.hidden, p.lddx, plan.parts, plan.pitch, plan.splits, nullptr, 1, 0};
     if (cudaError_t err = launch_sum(d, plan.dgate.m, plan.gate.m, &plan.dup.m, &plan.up.m, false, sm_count, stream)) return err;
     return plan.parts ? join_sum(d, sm_count, stream) : cudaSuccess;
 }

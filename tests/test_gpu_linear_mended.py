@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from tests.test_gpu_linear import DEV, DTYPES, check_head_gradient, close, gen, head, normal, scores_64
+from tests.test_gpu_linear import DEV, DTYPES, HALF, TINY, check_head_gradient, close, gen, head, normal, scores_64, short
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +194,39 @@ def test_logits_of_long_sums(pkg, dtype, rows, hidden, vocab, signs):
         # The rows' mean, which leaves the loss of the sums alone: 1e-9 per term of a chunk's own sum, of the logits, whose mean
         # under p is below lse; and as much again.
         assert float(((r.lse.double() + r.lse_lo.double()) / lse - 1).mean().abs()) <= 2e-9 * chunk_of(hidden)
+
+
+# ---- gradients of few rows ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,grads", [("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("workers,tokens,hidden,vocab", [(1, 1, 1, 1), (8, 2, 2354, 10), (1, 1, 64, 300), (3, 5, 65, 257), (16, 8, 136, 1000), (1, 128, 700, 50),
+                                                         (2, 20, 64, 40000), (1, 64, 96, 9), (1, 129, 64, 300)])
+def test_gradients_of_few_rows(pkg, dtype, grads, workers, tokens, hidden, vocab):
+    """Up to 128 rows a coefficient's rounding to 16 bits decides a gradient, and does not average out: dz comes in two parts, off by
+    u^2 of itself (binary16: and by what lies below 2^-25 of 2^-14 of its worker's largest coefficient) instead of u."""
+    rows = workers * tokens
+    x, w, b, t = head(rows, hidden, vocab, dtype, True, 25)
+    a = -(torch.rand(rows, generator=gen(10), device=DEV) + 0.5) / tokens
+    if rows > 3:
+        a[2], t[3] = 0.0, -1
+    saved = pkg.gar_linear_logprobs(x, w, t, bias=b)
+    block = torch.full((workers, vocab * hidden + vocab), 7.0, dtype=DTYPES[grads], device=DEV)
+    dx = pkg.gar_linear_logprobs_backward(x, w, saved, t, a, bias=b, grads=block, bias_offset=vocab * hidden)
+    alone = pkg.gar_linear_logprobs_backward(x, w, saved, t, a, bias=b)
+    _, _, p, d = scores_64(x, w, b, t)
+    coef = torch.where(t >= 0, a.double(), 0.0)
+    hot = torch.zeros_like(p).scatter_(1, t.clamp(min=0)[:, None], (t >= 0).double()[:, None])
+    dz = coef[:, None] * (hot - p)
+    u = HALF[dtype]
+    off = (u * u if rows <= 128 else u) * dz.abs() + coef.abs()[:, None] * p * (2 * d[:, None] + 2e-5) + TINY[dtype] * 2.0 ** -14 * coef.abs().max()
+    wa, xa = w.double().abs(), x.double().abs()
+    want = dz @ w.double()
+    tol = off @ wa + 2 * short(vocab) * (dz.abs() @ wa) + u * want.abs() + TINY[dtype]
+    close(dx, want, tol, "dx")
+    close(alone, want, tol, "dx alone")
+    for k in range(workers):
+        at = slice(k * tokens, (k + 1) * tokens)
+        want = dz[at].t() @ x[at].double()
+        tol = off[at].t() @ xa[at] + 2 * short(tokens) * (dz[at].abs().t() @ xa[at]) + HALF[grads] * want.abs() + TINY[grads]
+        close(block[k, :vocab * hidden].view(vocab, hidden), want, tol, "weights")
+        want = dz[at].sum(0)
+        close(block[k, vocab * hidden:], want, off[at].sum(0) + 2 * short(tokens) * dz[at].abs().sum(0) + HALF[grads] * want.abs() + TINY[grads], "bias")
