@@ -19,7 +19,7 @@
  * cores, which truncate where they add: a sum over k terms is short by some
  * 1e-9 k of itself, where it grows steadily by 1.4e-9 k (bfloat16) to 6e-9 k (binary16), where nothing is cut off by nothing;
  * at the very most by 4e-8 k (up to 16 rows 7e-8 k) of the terms' magnitudes.
- * Logits are summed in chunks of 512 terms (up to 640 in one), the chunks' sums added in fp32, rounded; the sums over `hidden`
+ * Logits are summed in chunks of 512 terms (up to 640 in one; of up to 16 rows mostly 128), the chunks' sums added in fp32, rounded; the sums over `hidden`
  * and `inner` that end in 16 bits or in checkpoints are whole; other sums have 2^15 terms at most before they are added, rounded, to
  * the rest.  Everything after a product is fp32, each output rounded once.
  *
@@ -114,7 +114,8 @@ size_t gar_linear_logprobs_backward_workspace_bytes(const gar_linear_logprobs_gr
 /*
  * The gated feed-forward block: g = x Wg^T + bg, u = x Wu^T + bu, y = act(g) * u, with 8-bit checkpoints
  * of g, u and of the stored, rounded y where they are asked for (gar_worker.h; g and u are coded from their fp32
- * values).  g and u themselves are not kept.
+ * values: one as near the border between two codes as its sum is off gets either, and is restored a whole step away from
+ * where the other would be; ReLU's derivative next to 0 goes with it).  g and u themselves are not kept.
  */
 typedef struct gar_gated_linear_params_t {
     int32_t          dtype, act, group;       /* GAR_BF16 or GAR_F16; gar_act_t; of the checkpoints */

@@ -20,7 +20,6 @@ namespace {
 
 constexpr int FW_WARPS = 8, FW_THREADS = 32 * FW_WARPS;
 constexpr int FW_UNIT = 128;                          // elements of the contraction a warp takes at a time: 256 bytes of a row
-constexpr int FW_CHUNK = 512 / FW_UNIT;               // units of a warp that its accumulators take: the tensor core truncates what it adds (worker_linear.cu)
 constexpr int FW_SMEM = 100 << 10;                    // x in shared memory: two CTAs on an SM
 
 struct FewArgs {
@@ -125,27 +124,23 @@ __global__ void __launch_bounds__(FW_THREADS, 2) few_rows_kernel(const FewArgs a
 
     for (int64_t first = int64_t(blockIdx.x) * sets; first < a.tiles; first += int64_t(gridDim.x) * sets) {
         const int64_t tile = first + set;
-        float acc[NT][4], sum[NT][4];                  // of a chunk; of the chunks, rounded where they are added
+        // the tensor core truncates what it adds: its sums are of a unit, which are added up rounded
+        float sum[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) acc[n][c] = sum[n][c] = 0.f;
-        auto join = [&]() {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    sum[n][c] += acc[n][c];
-                    acc[n][c] = 0.f;
-                }
-        };
-        int left = FW_CHUNK;
+            for (int c = 0; c < 4; ++c) sum[n][c] = 0.f;
         for (int u = part; u < a.units; u += a.split) {
             uint4 w[4][2];
 #pragma unroll
             for (int c = 0; c < 4; ++c) { w[c][0] = next[c][0]; w[c][1] = next[c][1]; }
             if (u + a.split < a.units) fetch(u + a.split);
             const uint8_t* xk = xs + g * a.pitch + (u * FW_UNIT + 8 * t) * 2;
+            float acc[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[n][c] = 0.f;
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -154,12 +149,11 @@ __global__ void __launch_bounds__(FW_THREADS, 2) few_rows_kernel(const FewArgs a
                     mma_16x8x16<T>(acc[n], w[c][0].x, w[c][1].x, w[c][0].y, w[c][1].y, b.x, b.y);
                     mma_16x8x16<T>(acc[n], w[c][0].z, w[c][1].z, w[c][0].w, w[c][1].w, b.z, b.w);
                 }
-            if (--left == 0) {
-                join();
-                left = FW_CHUNK;
-            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sum[n][c] += acc[n][c];
         }
-        join();
         // the next tile's first unit is on its way while this one is finished
         const bool mine0 = live0, mine1 = live1;
         const int64_t v0 = r0, v1 = r1;
