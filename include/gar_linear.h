@@ -9,19 +9,23 @@
  * device, all buffers owned by the caller, every call asynchronous on
  * `stream`, argument errors returned before anything is launched, GAR_ERR_CUDA
  * for launch failures, no exceptions, no CPU fallback, bit-identical output
- * for the same call.  (How a call's work is cut up goes by its sizes, so that a row's last bits
- * may differ between calls of different numbers of rows, a token scored alone and in a batch for instance.)  Matrices are row-major with unit column stride and a
- * row stride `ld` in elements (0 means the number of columns), at any alignment
- * of the element type.  A call with no rows writes no rows.
+ * for the same call.  (How a call's work is cut up goes by its sizes, so that a
+ * row's last bits may differ between calls of different numbers of rows, a token
+ * scored alone and in a batch for instance.)  Matrices are row-major with unit
+ * column stride and a row stride `ld` in elements (0 means the number of
+ * columns), at any alignment of the element type.  A call with no rows writes no
+ * rows.
  *
  * The matrix products are those of 16-bit elements (GAR_BF16 or GAR_F16; GAR_F32 is
  * GAR_ERR_UNSUPPORTED except for dropout), exact, summed in fp32 on the tensor
  * cores, which truncate where they add: a sum over k terms is short by some
- * 1e-9 k of itself, where it grows steadily by 1.4e-9 k (bfloat16) to 6e-9 k (binary16), where nothing is cut off by nothing;
- * at the very most by 4e-8 k (up to 16 rows 7e-8 k) of the terms' magnitudes.
- * Logits are summed in chunks of 512 terms (up to 640 in one; of up to 16 rows mostly 128), the chunks' sums added in fp32, rounded; the sums over `hidden`
- * and `inner` that end in 16 bits or in checkpoints are whole; other sums have 2^15 terms at most before they are added, rounded, to
- * the rest.  Everything after a product is fp32, each output rounded once.
+ * 1e-9 k of itself, where it grows steadily by 1.4e-9 k (bfloat16) to 6e-9 k
+ * (binary16), where nothing is cut off by nothing; at the very most by 4e-8 k (up
+ * to 16 rows 7e-8 k) of the terms' magnitudes.  Logits are summed in chunks of 512
+ * terms (up to 640 in one; of up to 16 rows mostly 128), whose sums are added in
+ * fp32, rounded; the sums over `hidden` and `inner` that end in 16 bits or in
+ * checkpoints are whole; other sums have 2^15 terms at most before they are added,
+ * rounded, to the rest.  Everything after a product is fp32, each output rounded once.
  *
  * Workspaces: 256-byte aligned, of at least the bytes the sizes call returns
  * for the same parameters (host, pure; 0 on invalid ones).  Nothing in them
@@ -80,9 +84,9 @@ size_t gar_linear_logprobs_workspace_bytes(const gar_linear_logprobs_params_t* p
  * row, where no weight gradients are asked for), so that small gradients do not underflow: dz have all their bits down to 2^-28 of that
  * |a|, what is below 2^-39 of it is lost.
  *   - A row without a target, or with a = 0, gets dx 0 and nothing it holds, NaN included, reaches a weight gradient.
+ *     The same holds for a row masked throughout, lse = -inf, whatever its coefficient and its target.
+ *   - In any other row a target >= vocab gives NaN, in dx and in its worker's gradients; no row reaches another worker's.
  *   - No tokens: weight and bias gradients of zeros.
- *   - The same holds for a row masked throughout, lse = -inf, whatever its coefficient and its target; in any other row a target >= vocab gives NaN, in dx and
- *     in its worker's gradients; no row reaches another worker's.
  * 1 <= workers <= GAR_MAX_N; workers * tokens < 2^30.
  */
 typedef struct gar_linear_logprobs_grad_params_t {
